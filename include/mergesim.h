@@ -506,6 +506,151 @@ ms_status ms_sim_set_train_param(ms_sim* sim, int32_t which, int32_t id, int32_t
 #define MS_OP_GRAD_OTHER 16    /* objective, elementwise, neuron and filter reverses, update */
 #define MS_OP_GRAD_WEIGHTS_SMALL 17  /* weight gradients of the other DotInc groups */
 
+/* ------------------------------------------- operators on device arrays */
+
+/* Operators for models that read and learn from tokens, called on arrays of
+ * the caller's own (none is a part of the paper's method): a table of token
+ * vectors, a lowpass synapse whose time constant the input sets, and
+ * orthogonalised updates of weight matrices.  Their outputs are laid out as
+ * feeds ([batch][steps][dim]).
+ *
+ * Every pointer but the descriptors is device memory on `device`; the calls
+ * enqueue on `stream` (a hipStream_t, NULL = the device's default stream) and
+ * return without waiting.  They allocate nothing, read nothing back and may be
+ * captured into a HIP graph.  Scratch memory is the caller's: a `workspace` of
+ * the size that the _workspace call gives (which needs no GPU), 256-byte
+ * aligned, whose contents before and after do not matter, and which no other
+ * call may use until this one has finished on the device.  Equal inputs give
+ * equal bits, whatever ran before.
+ *
+ * Types: MS_DTYPE_F32 or MS_DTYPE_BF16 arrays; everything is computed in 32
+ * bits and rounded to nearest even once, at the end.  Strides are in elements,
+ * rows themselves are contiguous, and a stride of 0 in a descriptor stands for
+ * the packed one.  Output arrays must not overlap other arrays.  Empty inputs
+ * (no tokens, no steps, no rows) are valid.  MS_E_INVALID, before anything is
+ * enqueued, for a size, stride, type, option, null pointer, misaligned pointer
+ * or workspace that does not fit. */
+#define MS_DTYPE_F32 0
+#define MS_DTYPE_BF16 1
+#define MS_IDS_I32 0
+#define MS_IDS_I64 1
+
+/* Table lookup: out[i] = scale * table[token[i]], n_tokens rows of dim.  Its
+ * gradient: dtable[v] = scale * (sum of drows[i] over the i with token[i] == v,
+ * in an order that depends on the tokens alone).  A token outside [0, vocab) is
+ * padding: its row is zeros and it adds to no gradient.  The gradient is dense;
+ * with accumulate != 0 it is added to what dtable holds, and rows whose token
+ * does not occur are not touched. */
+typedef struct {
+  int64_t n_tokens, vocab, dim; /* n_tokens < 2^31, 1 <= vocab < 2^31, 1 <= dim < 2^24 */
+  int64_t table_stride;         /* between rows of table or dtable; 0 = dim */
+  int64_t row_stride;           /* between rows of out or drows; 0 = dim */
+  double scale;
+  int32_t ids;                  /* MS_IDS_*: type of the tokens */
+  int32_t dtype;                /* MS_DTYPE_*: of table and out, or of drows */
+  int32_t grad_dtype;           /* of dtable */
+  int32_t accumulate;
+  int32_t device;
+  void* stream;
+} ms_embed_desc;
+
+ms_status ms_embed(const ms_embed_desc* desc, const void* tokens, const void* table, void* out);
+ms_status ms_embed_grad_workspace(const ms_embed_desc* desc, int64_t* bytes_out);
+ms_status ms_embed_grad(const ms_embed_desc* desc, const void* tokens, const void* drows, void* dtable,
+                        void* workspace, int64_t workspace_bytes);
+
+/* Gated lowpass: a lowpass synapse (y <- a y + (1 - a) v) whose coefficient is
+ * set at every step and for every channel by a logit g:
+ *     a = 1 / (1 + exp(-g));   y[t] = a[t] y[t-1] + (1 - a[t]) v[t],   y[-1] = y0.
+ * g = -inf forgets the state (a sequence starts), g = +inf keeps it.
+ * lengths (int32 [batch], clamped to [0, steps]; NULL = steps): what lies past
+ * a row's length is not used, y there is 0 and the state stays.
+ *   y0    [batch][dim] float32, or NULL for zeros
+ *   y     [batch][steps][dim] (y_stride)
+ *   last  [batch][dim] float32, the state after the last step; may be NULL
+ *   kept  float32, ms_gated_lowpass_kept() elements: states that the gradient
+ *         starts from, in a layout of the library's own; NULL if no gradient
+ *         is wanted
+ * The gradient, from dL/dy and dL/dlast (NULL for zeros):
+ *     d[t] = dy[t] + a[t+1] d[t+1],  dv = (1 - a) d,  dg = a (1 - a) (y[t-1] - v) d
+ *   dy    [batch][steps][dim] (y_stride); dv, dg: packed, 0 past a row's length
+ *   dy0   [batch][dim] float32; may be NULL
+ * v, g, kept and lengths are those of the forward call.  State is held in 32
+ * bits throughout. */
+typedef struct {
+  int64_t batch, steps, dim;    /* batch, steps >= 0 and < 2^31, 1 <= dim < 2^24 */
+  int64_t v_stride[2];          /* between batch rows, between steps; 0, 0 = packed */
+  int64_t g_stride[2];
+  int64_t y_stride[2];          /* of y, or of dy in the gradient */
+  int32_t dtype;                /* MS_DTYPE_*: of v, g, y and their gradients */
+  int32_t device;
+  void* stream;
+} ms_gated_lowpass_desc;
+
+ms_status ms_gated_lowpass_kept(const ms_gated_lowpass_desc* desc, int64_t* elements_out);
+ms_status ms_gated_lowpass_workspace(const ms_gated_lowpass_desc* desc, int64_t* bytes_out);
+ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* desc, const void* v, const void* g, const float* y0,
+                           const int32_t* lengths, void* y, float* last, float* kept, void* workspace,
+                           int64_t workspace_bytes);
+ms_status ms_gated_lowpass_grad(const ms_gated_lowpass_desc* desc, const void* v, const void* g,
+                                const float* kept, const int32_t* lengths, const void* dy, const float* dlast,
+                                void* dv, void* dg, float* dy0, void* workspace, int64_t workspace_bytes);
+
+/* One step of the gated lowpass for sequences that are being served: row i
+ * advances the state in slot slots[i] of state [slots][dim] (float32, updated
+ * in place; state_stride between slots) and writes it to y[i].  slots == NULL:
+ * row i uses slot i.  A slot outside [0, n_slots) is an idle row: y is 0 and no
+ * state changes.  Slots of rows that are not idle must differ. */
+typedef struct {
+  int64_t rows, n_slots, dim;
+  int64_t v_stride, g_stride, y_stride, state_stride; /* 0 = dim */
+  int32_t dtype;                /* MS_DTYPE_*: of v, g and y */
+  int32_t device;
+  void* stream;
+} ms_gated_step_desc;
+
+ms_status ms_gated_lowpass_step(const ms_gated_step_desc* desc, const void* v, const void* g, float* state,
+                                const int32_t* slots, void* y);
+
+/* Orthogonalised updates.  Of each matrix X [rows][cols] of a batch:
+ *     X <- X / (|X| + eps)                       (|X|: Frobenius norm)
+ *     X <- (c0 I + c1 A + c2 A A) X,  A = X X'   (`steps` times; A = X' X and
+ *                                                 products from the right where rows > cols)
+ * which moves the singular values of X towards one and keeps its singular
+ * vectors.  MS_E_INVALID where c0..c2 let a singular value of an iterate, or
+ * the polynomial, exceed 1000 in size.  The products run on 16-bit matrix instructions
+ * with 32-bit sums: float32 matrices as the sum of two 16-bit parts (22 bits),
+ * bf16 matrices as one (11 bits, finer than the result's rounding).
+ *
+ * ms_orthogonal_update trains a float32 weight with it:
+ *     momentum <- momentum_decay * momentum + grad
+ *     X = grad + momentum_decay * momentum   (nesterov != 0), or momentum
+ *     weight <- (1 - rate * weight_decay) * weight - rate * orthogonalised(X)
+ * weight and momentum: float32, packed [batch][rows][cols], updated in place;
+ * grad: dtype, x_stride. */
+typedef struct {
+  int64_t batch, rows, cols;    /* rows, cols in [1, 65536] */
+  int64_t x_stride[2];          /* of x or grad: between matrices, between rows; 0, 0 = packed */
+  int64_t out_stride[2];
+  double coef[3], eps;          /* eps >= 0 */
+  int32_t steps;                /* in [1, 100] */
+  int32_t dtype;                /* MS_DTYPE_*: of x and out, or of grad */
+  int32_t device;
+  void* stream;
+} ms_orth_desc;
+
+typedef struct {
+  double rate, momentum_decay, weight_decay;
+  int32_t nesterov;
+} ms_orth_rule;
+
+/* update != 0: for ms_orthogonal_update, else for ms_orthogonalise. */
+ms_status ms_orth_workspace(const ms_orth_desc* desc, int32_t update, int64_t* bytes_out);
+ms_status ms_orthogonalise(const ms_orth_desc* desc, const void* x, void* out, void* workspace,
+                           int64_t workspace_bytes);
+ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rule, float* weight,
+                               float* momentum, const void* grad, void* workspace, int64_t workspace_bytes);
+
 const char* ms_last_error(void);
 
 #ifdef __cplusplus

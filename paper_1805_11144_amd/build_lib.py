@@ -12,7 +12,7 @@ OUT = os.path.join(HERE, "libmergesim.so")
 BUILD = os.path.join(HERE, "_build")
 
 HOST_SOURCES = ["build.cpp", "ir.cpp", "planner.cpp", "launch_plan.cpp", "window_fuse.cpp", "resident.cpp", "plan_json.cpp", "abi_host.cpp"]
-HIP_SOURCES = ["runtime.hip"]
+HIP_SOURCES = ["runtime.hip", "operators.hip"]
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 

@@ -1,0 +1,593 @@
+// The operators on device arrays of the C ABI: argument checks, workspace
+// layouts and launches.  The kernels are in kernels_embed.hpp,
+// kernels_gated.hpp and kernels_orth.hpp.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <string>
+
+#include "hip_host.hpp"
+#include "host.hpp"
+#include "kernels_embed.hpp"
+#include "kernels_gated.hpp"
+#include "kernels_orth.hpp"
+
+using namespace ms;
+
+namespace {
+
+void need(bool ok, const char* what) {
+  if (!ok) fail(MS_E_INVALID, what);
+}
+
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxBlocks = (int64_t)1 << 23;   // workgroups of 256: the grid's threads fit 32 bits
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+size_t size_of(int32_t dtype) { return dtype == MS_DTYPE_BF16 ? 2 : 4; }
+
+void need_dtype(int32_t d) { need(d == MS_DTYPE_F32 || d == MS_DTYPE_BF16, "unknown dtype"); }
+
+void need_aligned(const void* p, size_t to, const char* what) {
+  if ((uintptr_t)p % to != 0) fail(MS_E_INVALID, std::string(what) + " is not aligned to its type");
+}
+
+void need_workspace(const void* ws, int64_t have, int64_t want) {
+  if (want == 0) return;
+  need(ws != nullptr, "NULL workspace");
+  need((uintptr_t)ws % 256 == 0, "workspace must be 256-byte aligned");
+  need(have >= want, "workspace too small");
+}
+
+// A piece of the workspace; every piece begins on 256 bytes.
+struct Carve {
+  char* base;
+  int64_t used = 0;
+  template <class T>
+  T* take(int64_t n) {
+    T* p = (T*)(base + used);
+    used += up(n * (int64_t)sizeof(T), 256);
+    return p;
+  }
+};
+
+// The widest access, in values, that sizes, strides and pointers allow: at
+// most 16 bytes of the narrowest type.
+struct Wide {
+  int64_t v;
+  explicit Wide(size_t elem) : v(16 / (int64_t)elem) {}
+  Wide& of(int64_t n) {
+    while (n % v != 0) v /= 2;
+    return *this;
+  }
+  Wide& at(const void* p, size_t elem) {
+    while ((uintptr_t)p % ((size_t)v * elem) != 0) v /= 2;
+    return *this;
+  }
+};
+
+// Calls f with the access width as a compile-time number.
+template <int MAX, class F>
+void with_width(int64_t v, F&& f) {
+  if constexpr (MAX >= 8)
+    if (v == 8) return f(std::integral_constant<int, 8>{});
+  if constexpr (MAX >= 4)
+    if (v == 4) return f(std::integral_constant<int, 4>{});
+  if (v == 2) return f(std::integral_constant<int, 2>{});
+  f(std::integral_constant<int, 1>{});
+}
+
+// Calls f with the element type and the access width (at most MAX).
+template <int MAX, class F>
+void with_type(int32_t dtype, int64_t v, F&& f) {
+  if (dtype == MS_DTYPE_BF16) with_width<MAX>(v, [&](auto w) { f((__bf16)0.0f, w); });
+  else with_width<std::min(MAX, 4)>(v, [&](auto w) { f(0.0f, w); });
+}
+
+int32_t threads_per_row(int64_t nv) {
+  int32_t t = 1;
+  while (t < nv && t < 256) t *= 2;
+  return t;
+}
+
+unsigned row_blocks(int64_t rows, int32_t tpr) {
+  const int64_t per = 256 / tpr;
+  return (unsigned)std::min<int64_t>((rows + per - 1) / per, kMaxBlocks);
+}
+
+// ------------------------------------------------------------------ tables
+struct Embed {
+  int64_t ts, os;
+};
+
+Embed check_embed(const ms_embed_desc* d) {
+  need(d != nullptr, "NULL descriptor");
+  need(d->n_tokens >= 0 && d->n_tokens < ((int64_t)1 << 31), "n_tokens must be in [0, 2^31)");
+  need(d->vocab >= 1 && d->vocab < ((int64_t)1 << 31), "vocab must be in [1, 2^31)");
+  need(d->dim >= 1 && d->dim < (1 << 24), "dim must be in [1, 2^24)");
+  need_dtype(d->dtype);
+  need_dtype(d->grad_dtype);
+  need(d->ids == MS_IDS_I32 || d->ids == MS_IDS_I64, "unknown token type");
+  need(std::isfinite(d->scale), "scale must be finite");
+  Embed e{d->table_stride ? d->table_stride : d->dim, d->row_stride ? d->row_stride : d->dim};
+  need(e.ts >= d->dim && e.ts < kMaxStride && e.os >= d->dim && e.os < kMaxStride,
+       "row strides must be at least dim");
+  return e;
+}
+
+struct EmbedWork {
+  uint32_t *keys[2], *pos[2], *counts, *start;
+  int64_t bytes;
+};
+
+EmbedWork embed_work(const ms_embed_desc* d, void* ws) {
+  Carve c{(char*)ws};
+  EmbedWork w;
+  for (int i = 0; i < 2; ++i) w.keys[i] = c.take<uint32_t>(d->n_tokens), w.pos[i] = c.take<uint32_t>(d->n_tokens);
+  w.counts = c.take<uint32_t>((d->n_tokens + kSortTile - 1) / kSortTile * 256);
+  w.start = c.take<uint32_t>(d->vocab + 1);
+  w.bytes = c.used;
+  return w;
+}
+
+template <class I>
+void sort_tokens(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int& in, hipStream_t st) {
+  const int64_t n = d->n_tokens;
+  const unsigned tiles = (unsigned)((n + kSortTile - 1) / kSortTile);
+  in = 0;
+  for (int shift = 0; shift < 32 && (d->vocab >> shift) != 0; shift += 8, in ^= 1) {
+    const uint32_t *k = shift ? w.keys[in] : nullptr, *p = shift ? w.pos[in] : nullptr;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_count<I>), dim3(tiles), dim3(256), 0, st, tokens, k, n, d->vocab, shift,
+                       w.counts);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_move<I>), dim3(tiles), dim3(256), 0, st, tokens, k, p, n, d->vocab, shift,
+                       (const uint32_t*)w.counts, w.keys[in ^ 1], w.pos[in ^ 1]);
+  }
+}
+
+// ------------------------------------------------------------------ gated
+struct Gated {
+  GatedArgs a;
+  int64_t keeps;
+};
+
+void stride_pair(const int64_t* s, int64_t steps, int64_t dim, int64_t& b, int64_t& t) {
+  const bool packed = s[0] == 0 && s[1] == 0;
+  t = packed ? dim : s[1];
+  b = packed ? steps * dim : s[0];
+  need(b >= 0 && t >= 0 && b < kMaxStride && t < kMaxStride, "strides must not be negative");
+}
+
+Gated check_gated(const ms_gated_lowpass_desc* d) {
+  need(d != nullptr, "NULL descriptor");
+  need(d->steps >= 0 && d->steps < ((int64_t)1 << 31), "steps must be in [0, 2^31)");
+  need(d->dim >= 1 && d->dim < (1 << 24), "dim must be in [1, 2^24)");
+  need(d->batch >= 0 && d->batch < ((int64_t)1 << 31) && d->batch * d->dim < ((int64_t)1 << 31),
+       "batch * dim must be below 2^31");
+  need_dtype(d->dtype);
+  Gated g{};
+  GatedArgs& a = g.a;
+  a.batch = d->batch, a.steps = d->steps, a.dim = d->dim;
+  stride_pair(d->v_stride, d->steps, d->dim, a.vb, a.vt);
+  stride_pair(d->g_stride, d->steps, d->dim, a.gb, a.gt);
+  stride_pair(d->y_stride, d->steps, d->dim, a.yb, a.yt);
+  // Enough chunks that a few channels fill the device, none so short that
+  // joining them costs more than going through it.
+  const int64_t channels = std::max<int64_t>(d->batch * d->dim, 1);
+  const int64_t want = std::max<int64_t>(1, ((int64_t)1 << 19) / channels);
+  int64_t chunk = std::max<int64_t>(up((d->steps + want - 1) / want, kKeep), 64);
+  chunk = std::max(chunk, up((d->steps + 65534) / 65535, kKeep));
+  a.chunk = (int32_t)std::min<int64_t>(chunk, (int64_t)1 << 30);
+  a.nchunk = (int32_t)((d->steps + a.chunk - 1) / a.chunk);
+  g.keeps = (d->steps + kKeep - 1) / kKeep;
+  return g;
+}
+
+int64_t gated_work(const Gated& g) {
+  return g.a.nchunk > 1 ? up(g.a.batch * g.a.nchunk * 2 * g.a.dim * 4, 256) : 0;
+}
+
+dim3 gated_grid(const GatedArgs& a) {
+  return dim3((unsigned)((a.batch * a.nv + 255) / 256), (unsigned)a.nchunk);
+}
+
+// ------------------------------------------------------------------- orth
+struct Orth {
+  int64_t n, m, np, mp;
+  int tile;
+  int parts;              // fp16 parts of a value
+  double sx, sa, sq;      // scales of X, A and Q
+  int64_t xm, xr, om, orow;
+};
+
+Orth check_orth(const ms_orth_desc* d, bool update) {
+  need(d != nullptr, "NULL descriptor");
+  need(d->rows >= 1 && d->rows <= 65536 && d->cols >= 1 && d->cols <= 65536, "rows and cols must be in [1, 65536]");
+  need(d->batch >= 0, "batch must not be negative");
+  need(d->steps >= 1 && d->steps <= 100, "steps must be in [1, 100]");
+  need_dtype(d->dtype);
+  need(d->eps >= 0 && std::isfinite(d->eps), "eps must be finite and not negative");
+  Orth o;
+  auto pair = [&](const int64_t* s, int64_t& mat, int64_t& row) {
+    const bool packed = s[0] == 0 && s[1] == 0;
+    row = packed ? d->cols : s[1];
+    mat = packed ? d->rows * d->cols : s[0];
+    need(row >= d->cols && row < kMaxStride && mat >= 0 && mat < kMaxStride, "strides must be at least a row");
+  };
+  pair(d->x_stride, o.xm, o.xr);
+  pair(d->out_stride, o.om, o.orow);
+  o.n = std::min(d->rows, d->cols), o.m = std::max(d->rows, d->cols);
+  o.parts = update || d->dtype == MS_DTYPE_F32 ? 2 : 1;
+  // 128 x 128 tiles from 512 rows on
+  o.tile = o.n >= 512 ? 128 : 64;
+  o.np = up(o.n, o.tile), o.mp = up(o.m, o.tile);
+  need(d->batch <= kMaxBlocks / ((o.np / 64) * (o.mp / 64)), "too many matrices of this size");
+  // How large an iterate's singular values and the polynomial can get: the
+  // first are at most 1, and f(s) = s (c0 + c1 s^2 + c2 s^4) takes its extremes
+  // over [0, top] at the ends or where its derivative is 0.
+  double top = 1.0, poly = 0.0;
+  const double *c = d->coef;
+  need(std::isfinite(c[0]) && std::isfinite(c[1]) && std::isfinite(c[2]), "coefficients must be finite");
+  double bound = 1.0;
+  for (int k = 0; k < d->steps; ++k) {
+    const auto q = [&](double t) { return std::fabs(c[0] + c[1] * t + c[2] * t * t); };   // t = s^2
+    double most_f = top * q(top * top), most_q = std::max(q(0.0), q(top * top));
+    const auto at = [&](double t) {
+      if (t > 0.0 && t < top * top) most_f = std::max(most_f, std::sqrt(t) * q(t)), most_q = std::max(most_q, q(t));
+    };
+    if (c[2] != 0.0) {
+      at(-c[1] / (2.0 * c[2]));
+      const double disc = 9.0 * c[1] * c[1] - 20.0 * c[0] * c[2];
+      if (disc >= 0.0) at((-3.0 * c[1] + std::sqrt(disc)) / (10.0 * c[2])), at((-3.0 * c[1] - std::sqrt(disc)) / (10.0 * c[2]));
+    } else if (c[1] != 0.0) {
+      at(-c[0] / (3.0 * c[1]));
+    }
+    poly = std::max(poly, most_q);
+    top = most_f;
+    bound = std::max(bound, top);
+    need(bound <= 1000.0 && poly <= 1000.0, "the coefficients let the iterates grow past 1000");
+  }
+  // an entry is at most the largest singular value; a factor of two to spare
+  const auto scale = [](double b) { return std::ldexp(1.0, (int)std::floor(std::log2(32768.0 / b))); };
+  o.sx = scale(bound), o.sa = scale(bound * bound), o.sq = scale(std::max(poly, 1e-3));
+  return o;
+}
+
+struct OrthWork {
+  double* parts;
+  half_t *x, *t[2], *a, *q;
+  int64_t bytes;
+};
+
+OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
+  Carve c{(char*)ws};
+  OrthWork w;
+  const int64_t big = d->batch * o.parts * o.np * o.mp, small = d->batch * o.parts * o.np * o.np;
+  w.parts = c.take<double>(d->batch * kOrthParts);
+  w.x = c.take<half_t>(big);
+  w.t[0] = c.take<half_t>(big);
+  w.t[1] = c.take<half_t>(big);
+  w.a = c.take<half_t>(small);
+  w.q = c.take<half_t>(small);
+  w.bytes = c.used;
+  return w;
+}
+
+template <int PL, int TILE, int END, class T>
+void orth_gemm(const OrthGemm& g, int64_t batch, hipStream_t st) {
+  constexpr size_t lds = 2 * 2 * PL * TILE * 40 * sizeof(half_t);
+  const int64_t tm = g.M / TILE, tn = g.N / TILE;
+  const int64_t per = END == kEndGram || END == kEndPoly ? tm * (tm + 1) / 2 : tm * tn;
+  const void* k = (const void*)k_orth_gemm<PL, TILE, END, T>;
+  if (lds > 65536) HIPCHECK(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_gemm<PL, TILE, END, T>), dim3((unsigned)(batch * per)), dim3(256), lds, st, g);
+}
+
+// T: type of x (or the gradient); UPDATE: with momentum, into a weight.
+template <class T, bool UPDATE, int PL, int TILE>
+void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, OrthGemm out, hipStream_t st) {
+  const int64_t blocks = d->batch * (o.np / 64) * (o.mp / 64);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE>), dim3((unsigned)(d->batch * kOrthParts)), dim3(256), 0, st, src,
+                     w.parts);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, PL>), dim3((unsigned)blocks), dim3(256), 0, st, src,
+                     (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], (int32_t)o.np, (int32_t)o.mp);
+  using R = std::conditional_t<UPDATE, float, T>;
+  for (int k = 0; k < d->steps; ++k) {
+    OrthGemm g{};
+    g.l = g.r = w.x, g.M = g.N = (int32_t)o.np, g.K = (int32_t)o.mp, g.c = w.a;
+    g.f = (float)(o.sa / (o.sx * o.sx));
+    orth_gemm<PL, TILE, kEndGram, R>(g, d->batch, st);
+    g.l = g.r = w.a, g.K = (int32_t)o.np, g.c = w.q, g.a = w.a;
+    g.f = (float)(d->coef[2] * o.sq / (o.sa * o.sa));
+    g.c0 = (float)(d->coef[0] * o.sq), g.c1 = (float)(d->coef[1] * o.sq / o.sa);
+    orth_gemm<PL, TILE, kEndPoly, R>(g, d->batch, st);
+    OrthGemm x = out;
+    x.l = w.q, x.r = w.t[k % 2], x.M = (int32_t)o.np, x.N = (int32_t)o.mp, x.K = (int32_t)o.np;
+    if (k + 1 < d->steps) {
+      x.c = w.x, x.ct = w.t[(k + 1) % 2], x.f = (float)(1.0 / o.sq);
+      orth_gemm<PL, TILE, kEndNext, R>(x, d->batch, st);
+    } else {
+      x.f = (float)(1.0 / (o.sq * o.sx));
+      orth_gemm<PL, TILE, UPDATE ? kEndUpdate : kEndOut, R>(x, d->batch, st);
+    }
+  }
+  HIPCHECK(hipGetLastError());
+}
+
+template <class T, bool UPDATE, int PL>
+void orth_tiled(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, const OrthGemm& out,
+                hipStream_t st) {
+  if (o.tile == 128) orth_run<T, UPDATE, PL, 128>(d, o, src, w, out, st);
+  else orth_run<T, UPDATE, PL, 64>(d, o, src, w, out, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+ms_status ms_embed(const ms_embed_desc* d, const void* tokens, const void* table, void* out) {
+  return guarded([&] {
+    const Embed e = check_embed(d);
+    if (d->n_tokens == 0) return;
+    need(tokens && table && out, "NULL array");
+    const size_t es = size_of(d->dtype);
+    need_aligned(tokens, d->ids == MS_IDS_I64 ? 8 : 4, "tokens");
+    need_aligned(table, es, "table");
+    need_aligned(out, es, "out");
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    const int64_t v = Wide(es).of(d->dim).of(e.ts).of(e.os).at(table, es).at(out, es).v;
+    const int32_t nv = (int32_t)(d->dim / v), tpr = threads_per_row(nv);
+    with_type<8>(d->dtype, v, [&](auto zero, auto width) {
+      using T = decltype(zero);
+      constexpr int V = decltype(width)::value;
+      auto go = [&](auto id) {
+        using I = decltype(id);
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed<T, I, V>), dim3(row_blocks(d->n_tokens, tpr)), dim3(256), 0, st,
+                           (const I*)tokens, (const T*)table, (T*)out, d->n_tokens, d->vocab, nv, tpr, e.ts, e.os,
+                           (float)d->scale);
+      };
+      if (d->ids == MS_IDS_I64) go((int64_t)0);
+      else go((int32_t)0);
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_embed_grad_workspace(const ms_embed_desc* d, int64_t* bytes_out) {
+  return guarded([&] {
+    check_embed(d);
+    need(bytes_out != nullptr, "NULL output");
+    *bytes_out = embed_work(d, nullptr).bytes;
+  });
+}
+
+ms_status ms_embed_grad(const ms_embed_desc* d, const void* tokens, const void* drows, void* dtable, void* workspace,
+                        int64_t workspace_bytes) {
+  return guarded([&] {
+    const Embed e = check_embed(d);
+    need(dtable && (d->n_tokens == 0 || (tokens && drows)), "NULL array");
+    const size_t es = size_of(d->dtype), gs = size_of(d->grad_dtype);
+    need_aligned(tokens, d->ids == MS_IDS_I64 ? 8 : 4, "tokens");
+    need_aligned(drows, es, "drows");
+    need_aligned(dtable, gs, "dtable");
+    EmbedWork w = embed_work(d, workspace);
+    need_workspace(workspace, workspace_bytes, w.bytes);
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    int in = 0;
+    if (d->n_tokens > 0) {
+      if (d->ids == MS_IDS_I64) sort_tokens(d, (const int64_t*)tokens, w, in, st);
+      else sort_tokens(d, (const int32_t*)tokens, w, in, st);
+    }
+    const unsigned vblocks = (unsigned)std::min<int64_t>((d->vocab + 256) / 256, kMaxBlocks);
+    hipLaunchKernelGGL(k_sort_starts, dim3(vblocks), dim3(256), 0, st, (const uint32_t*)w.keys[in], d->n_tokens, d->vocab,
+                       w.start);
+    const int64_t v = Wide(es).of(d->dim).of(e.ts).of(e.os).at(drows, es).at(dtable, gs).v;
+    const int32_t nv = (int32_t)(d->dim / v), tpr = threads_per_row(nv);
+    with_type<8>(d->dtype, v, [&](auto zero, auto width) {
+      using T = decltype(zero);
+      constexpr int V = decltype(width)::value;
+      auto go = [&](auto gz) {
+        using D = decltype(gz);
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed_sum<T, D, V>), dim3(row_blocks(d->vocab, tpr)), dim3(256), 0, st,
+                           (const uint32_t*)w.pos[in], (const uint32_t*)w.start, (const T*)drows, (D*)dtable, d->vocab, nv,
+                           tpr, e.os, e.ts, (float)d->scale, d->accumulate);
+      };
+      if (d->grad_dtype == MS_DTYPE_BF16) go((__bf16)0.0f);
+      else go(0.0f);
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_gated_lowpass_kept(const ms_gated_lowpass_desc* d, int64_t* elements_out) {
+  return guarded([&] {
+    const Gated g = check_gated(d);
+    need(elements_out != nullptr, "NULL output");
+    *elements_out = g.a.batch * g.keeps * g.a.dim;
+  });
+}
+
+ms_status ms_gated_lowpass_workspace(const ms_gated_lowpass_desc* d, int64_t* bytes_out) {
+  return guarded([&] {
+    const Gated g = check_gated(d);
+    need(bytes_out != nullptr, "NULL output");
+    *bytes_out = gated_work(g);
+  });
+}
+
+ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* d, const void* v, const void* g, const float* y0,
+                           const int32_t* lengths, void* y, float* last, float* kept, void* workspace,
+                           int64_t workspace_bytes) {
+  return guarded([&] {
+    Gated p = check_gated(d);
+    GatedArgs& a = p.a;
+    if (a.batch == 0) return;
+    const size_t es = size_of(d->dtype);
+    need(a.yt >= a.dim || a.steps <= 1, "the steps of y must not overlap");
+    need(a.yb >= a.dim || a.batch <= 1, "the rows of y must not overlap");
+    need(a.steps == 0 || (v && g && y), "NULL array");
+    for (const void* q : {v, g, (const void*)y}) need_aligned(q, es, "v, g or y");
+    for (const void* q : {(const void*)y0, (const void*)lengths, (const void*)last, (const void*)kept})
+      need_aligned(q, 4, "y0, lengths, last or kept");
+    if (a.steps > 0) need_workspace(workspace, workspace_bytes, gated_work(p));
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    if (a.steps == 0) {
+      if (last)
+        hipLaunchKernelGGL(k_gated_none, dim3((unsigned)((a.batch * a.dim + 255) / 256)), dim3(256), 0, st, y0, last,
+                           a.batch * a.dim);
+      HIPCHECK(hipGetLastError());
+      return;
+    }
+    a.lengths = lengths;
+    const int64_t w = std::min<int64_t>(4, Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es)
+                                               .at(g, es).at(y, es).v);
+    a.nv = a.dim / w;
+    float* join = (float*)workspace;
+    with_type<4>(d->dtype, w, [&](auto zero, auto width) {
+      using T = decltype(zero);
+      constexpr int V = decltype(width)::value;
+      if (a.nchunk > 1)
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_part<T, V>), gated_grid(a), dim3(256), 0, st, a, (const T*)v,
+                           (const T*)g, join);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated<T, V>), gated_grid(a), dim3(256), 0, st, a, (const T*)v, (const T*)g, y0,
+                         (const float*)join, (T*)y, last, kept);
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_gated_lowpass_grad(const ms_gated_lowpass_desc* d, const void* v, const void* g, const float* kept,
+                                const int32_t* lengths, const void* dy, const float* dlast, void* dv, void* dg,
+                                float* dy0, void* workspace, int64_t workspace_bytes) {
+  return guarded([&] {
+    Gated p = check_gated(d);
+    GatedArgs& a = p.a;
+    if (a.batch == 0) return;
+    const size_t es = size_of(d->dtype);
+    need(a.steps == 0 || (v && g && kept && dy && dv && dg), "NULL array");
+    for (const void* q : {v, g, dy, (const void*)dv, (const void*)dg}) need_aligned(q, es, "v, g, dy, dv or dg");
+    for (const void* q : {(const void*)kept, (const void*)lengths, (const void*)dlast, (const void*)dy0})
+      need_aligned(q, 4, "kept, lengths, dlast or dy0");
+    if (a.steps > 0) need_workspace(workspace, workspace_bytes, gated_work(p));
+    DeviceGuard guard(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    if (a.steps == 0) {
+      if (dy0)
+        hipLaunchKernelGGL(k_gated_none, dim3((unsigned)((a.batch * a.dim + 255) / 256)), dim3(256), 0, st, dlast, dy0,
+                           a.batch * a.dim);
+      HIPCHECK(hipGetLastError());
+      return;
+    }
+    a.lengths = lengths;
+    const int64_t w = std::min<int64_t>(2, Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es)
+                                               .at(g, es).at(dy, es).at(dv, es).at(dg, es).v);
+    a.nv = a.dim / w;
+    float* join = (float*)workspace;
+    with_type<2>(d->dtype, w, [&](auto zero, auto width) {
+      using T = decltype(zero);
+      constexpr int V = decltype(width)::value;
+      if (a.nchunk > 1)
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad_part<T, V>), gated_grid(a), dim3(256), 0, st, a, (const T*)g,
+                           (const T*)dy, join);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad<T, V>), gated_grid(a), dim3(256), 0, st, a, (const T*)v,
+                         (const T*)g, kept, (const T*)dy, dlast, (const float*)join, (T*)dv, (T*)dg, dy0);
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_gated_lowpass_step(const ms_gated_step_desc* d, const void* v, const void* g, float* state,
+                                const int32_t* slots, void* y) {
+  return guarded([&] {
+    need(d != nullptr, "NULL descriptor");
+    need(d->rows >= 0 && d->rows < ((int64_t)1 << 31) && d->n_slots >= 0 && d->n_slots < ((int64_t)1 << 31),
+         "rows and n_slots must be in [0, 2^31)");
+    need(d->dim >= 1 && d->dim < (1 << 24), "dim must be in [1, 2^24)");
+    need_dtype(d->dtype);
+    const auto stride = [&](int64_t s) {
+      const int64_t r = s ? s : d->dim;
+      need(r >= d->dim && r < kMaxStride, "row strides must be at least dim");
+      return r;
+    };
+    const int64_t vs = stride(d->v_stride), gs = stride(d->g_stride), ys = stride(d->y_stride),
+                  ss = stride(d->state_stride);
+    if (d->rows == 0) return;
+    need(v && g && y && (state || d->n_slots == 0), "NULL array");
+    const size_t es = size_of(d->dtype);
+    for (const void* q : {v, g, (const void*)y}) need_aligned(q, es, "v, g or y");
+    for (const void* q : {(const void*)state, (const void*)slots}) need_aligned(q, 4, "state or slots");
+    DeviceGuard dg(d->device);
+    const int64_t w = std::min<int64_t>(
+        4, Wide(es).of(d->dim).of(vs).of(gs).of(ys).of(ss).at(v, es).at(g, es).at(y, es).at(state, 4).v);
+    const int32_t nv = (int32_t)(d->dim / w), tpr = threads_per_row(nv);
+    with_type<4>(d->dtype, w, [&](auto zero, auto width) {
+      using T = decltype(zero);
+      constexpr int V = decltype(width)::value;
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_served<T, V>), dim3(row_blocks(d->rows, tpr)), dim3(256), 0,
+                         (hipStream_t)d->stream, (const T*)v, (const T*)g, state, slots, (T*)y, d->rows, d->n_slots, nv,
+                         tpr, vs, gs, ys, ss);
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_orth_workspace(const ms_orth_desc* d, int32_t update, int64_t* bytes_out) {
+  return guarded([&] {
+    const Orth o = check_orth(d, update != 0);
+    need(bytes_out != nullptr, "NULL output");
+    *bytes_out = orth_work(d, o, nullptr).bytes;
+  });
+}
+
+ms_status ms_orthogonalise(const ms_orth_desc* d, const void* x, void* out, void* workspace, int64_t workspace_bytes) {
+  return guarded([&] {
+    const Orth o = check_orth(d, false);
+    if (d->batch == 0) return;
+    need(x && out, "NULL array");
+    need(o.om >= (d->rows - 1) * o.orow + d->cols || d->batch <= 1, "the matrices of out must not overlap");
+    const size_t es = size_of(d->dtype);
+    need_aligned(x, es, "x");
+    need_aligned(out, es, "out");
+    OrthWork w = orth_work(d, o, workspace);
+    need_workspace(workspace, workspace_bytes, w.bytes);
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    OrthSrc src{x, nullptr, o.xm, o.xr, d->rows, d->cols, 0.0f, 0};
+    OrthGemm g{};
+    g.out = out, g.mat = o.om, g.row = o.orow, g.rows = d->rows, g.cols = d->cols;
+    if (d->dtype == MS_DTYPE_BF16) orth_tiled<__bf16, false, 1>(d, o, src, w, g, st);
+    else orth_tiled<float, false, 2>(d, o, src, w, g, st);
+  });
+}
+
+ms_status ms_orthogonal_update(const ms_orth_desc* d, const ms_orth_rule* rule, float* weight, float* momentum,
+                               const void* grad, void* workspace, int64_t workspace_bytes) {
+  return guarded([&] {
+    const Orth o = check_orth(d, true);
+    need(rule != nullptr, "NULL rule");
+    need(std::isfinite(rule->rate) && std::isfinite(rule->momentum_decay) && std::isfinite(rule->weight_decay),
+         "rates must be finite");
+    if (d->batch == 0) return;
+    need(weight && momentum && grad, "NULL array");
+    need_aligned(weight, 4, "weight");
+    need_aligned(momentum, 4, "momentum");
+    need_aligned(grad, size_of(d->dtype), "grad");
+    OrthWork w = orth_work(d, o, workspace);
+    need_workspace(workspace, workspace_bytes, w.bytes);
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    OrthSrc src{grad, momentum, o.xm, o.xr, d->rows, d->cols, (float)rule->momentum_decay, rule->nesterov};
+    OrthGemm g{};
+    g.out = weight, g.mat = d->rows * d->cols, g.row = d->cols, g.rows = d->rows, g.cols = d->cols;
+    g.keep = (float)(1.0 - rule->rate * rule->weight_decay), g.rate = (float)rule->rate;
+    if (d->dtype == MS_DTYPE_BF16) orth_tiled<__bf16, true, 2>(d, o, src, w, g, st);
+    else orth_tiled<float, true, 2>(d, o, src, w, g, st);
+  });
+}
+
+}  // extern "C"

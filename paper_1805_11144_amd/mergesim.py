@@ -25,6 +25,8 @@ DECODE_DENSE, DECODE_EVENT = 0, 1
 PARAM_GAIN, PARAM_BIAS, PARAM_DECODERS = 0, 1, 2
 (STATE_VOLTAGE, STATE_REFRACTORY, STATE_SYNAPSE, STATE_PROBE_SYNAPSE, STATE_LEARNED_DECODERS,
  STATE_PES_ACTIVITY) = range(6)
+DTYPE_F32, DTYPE_BF16 = 0, 1
+IDS_I32, IDS_I64 = 0, 1
 (OP_FEED, OP_RESET, OP_COPY, OP_COPY_INC, OP_ELEMENTWISE_INC, OP_DOT_INC, OP_LIF, OP_LIF_RATE, OP_LOWPASS,
  OP_ENSEMBLE, OP_SYNAPSE_SCATTER, OP_LEARNED_DECODE, OP_PES, OP_PES_DECODE_UPDATE) = range(14)
 OP_GRAD_WEIGHTS, OP_GRAD_INPUTS, OP_GRAD_OTHER, OP_GRAD_WEIGHTS_SMALL = 14, 15, 16, 17
@@ -34,6 +36,7 @@ _dp = C.POINTER(C.c_double)
 _fp = C.POINTER(C.c_float)
 _i32 = C.c_int32
 _i64 = C.c_int64
+_vp = C.c_void_p
 
 
 class EnsembleDesc(C.Structure):
@@ -71,6 +74,34 @@ class Feed(C.Structure):
 
 class Target(C.Structure):
     _fields_ = [("probe_id", _i32), ("on_device", _i32), ("data", _fp)]
+
+
+class EmbedDesc(C.Structure):
+    _fields_ = [("n_tokens", _i64), ("vocab", _i64), ("dim", _i64), ("table_stride", _i64), ("row_stride", _i64),
+                ("scale", C.c_double), ("ids", _i32), ("dtype", _i32), ("grad_dtype", _i32), ("accumulate", _i32),
+                ("device", _i32), ("stream", C.c_void_p)]
+
+
+class GatedLowpassDesc(C.Structure):
+    _fields_ = [("batch", _i64), ("steps", _i64), ("dim", _i64), ("v_stride", _i64 * 2), ("g_stride", _i64 * 2),
+                ("y_stride", _i64 * 2), ("dtype", _i32), ("device", _i32), ("stream", C.c_void_p)]
+
+
+class GatedStepDesc(C.Structure):
+    _fields_ = [("rows", _i64), ("n_slots", _i64), ("dim", _i64), ("v_stride", _i64), ("g_stride", _i64),
+                ("y_stride", _i64), ("state_stride", _i64), ("dtype", _i32), ("device", _i32),
+                ("stream", C.c_void_p)]
+
+
+class OrthDesc(C.Structure):
+    _fields_ = [("batch", _i64), ("rows", _i64), ("cols", _i64), ("x_stride", _i64 * 2), ("out_stride", _i64 * 2),
+                ("coef", C.c_double * 3), ("eps", C.c_double), ("steps", _i32), ("dtype", _i32), ("device", _i32),
+                ("stream", C.c_void_p)]
+
+
+class OrthRule(C.Structure):
+    _fields_ = [("rate", C.c_double), ("momentum_decay", C.c_double), ("weight_decay", C.c_double),
+                ("nesterov", _i32)]
 
 
 class MergesimError(RuntimeError):
@@ -117,8 +148,22 @@ _SIGNATURES = [
                            _dp], _i32),
     ("ms_sim_train_param", [C.c_void_p, _i32, _i32, _i32, _i32, _fp, _i64, C.POINTER(_i64)], _i32),
     ("ms_sim_set_train_param", [C.c_void_p, _i32, _i32, _i32, _fp, _i64], _i32),
+    ("ms_embed", [C.POINTER(EmbedDesc), _vp, _vp, _vp], _i32),
+    ("ms_embed_grad_workspace", [C.POINTER(EmbedDesc), C.POINTER(_i64)], _i32),
+    ("ms_embed_grad", [C.POINTER(EmbedDesc), _vp, _vp, _vp, _vp, _i64], _i32),
+    ("ms_gated_lowpass_kept", [C.POINTER(GatedLowpassDesc), C.POINTER(_i64)], _i32),
+    ("ms_gated_lowpass_workspace", [C.POINTER(GatedLowpassDesc), C.POINTER(_i64)], _i32),
+    ("ms_gated_lowpass", [C.POINTER(GatedLowpassDesc), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64], _i32),
+    ("ms_gated_lowpass_grad", [C.POINTER(GatedLowpassDesc), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64],
+     _i32),
+    ("ms_gated_lowpass_step", [C.POINTER(GatedStepDesc), _vp, _vp, _vp, _vp, _vp], _i32),
+    ("ms_orth_workspace", [C.POINTER(OrthDesc), _i32, C.POINTER(_i64)], _i32),
+    ("ms_orthogonalise", [C.POINTER(OrthDesc), _vp, _vp, _vp, _i64], _i32),
+    ("ms_orthogonal_update", [C.POINTER(OrthDesc), C.POINTER(OrthRule), _vp, _vp, _vp, _vp, _i64], _i32),
     ("ms_last_error", [], C.c_char_p),
 ]
+# calls of the HIP sources: absent from a library of the host part alone
+_DEVICE_CALLS = ("ms_sim_", "ms_embed", "ms_gated_", "ms_orth")
 
 
 def load_library(path: str = LIB_PATH, host_only: bool = False):
@@ -134,7 +179,7 @@ def load_library(path: str = LIB_PATH, host_only: bool = False):
     lib = C.CDLL(path)
     for name, args, res in _SIGNATURES:
         fn = getattr(lib, name, None)
-        if fn is None and host_only and name.startswith("ms_sim_") and name != "ms_sim_opts_default":
+        if fn is None and host_only and name.startswith(_DEVICE_CALLS) and name != "ms_sim_opts_default":
             continue
         if fn is None:
             raise ImportError(f"{path} does not export {name}")
