@@ -542,7 +542,7 @@ ms_status ms_sim_set_train_param(ms_sim* sim, int32_t which, int32_t id, int32_t
  * with accumulate != 0 it is added to what dtable holds, and rows whose token
  * does not occur are not touched. */
 typedef struct {
-  int64_t n_tokens, vocab, dim; /* n_tokens < 2^31, 1 <= vocab < 2^31, 1 <= dim < 2^24 */
+  int64_t n_tokens, vocab, dim; /* n_tokens < 2^29, 1 <= vocab < 2^31, 1 <= dim < 2^24 */
   int64_t table_stride;         /* between rows of table or dtable; 0 = dim */
   int64_t row_stride;           /* between rows of out or drows; 0 = dim */
   double scale;

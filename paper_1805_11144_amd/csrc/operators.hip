@@ -105,7 +105,7 @@ struct Embed {
 
 Embed check_embed(const ms_embed_desc* d) {
   need(d != nullptr, "NULL descriptor");
-  need(d->n_tokens >= 0 && d->n_tokens < ((int64_t)1 << 31), "n_tokens must be in [0, 2^31)");
+  need(d->n_tokens >= 0 && d->n_tokens < ((int64_t)1 << 29), "n_tokens must be in [0, 2^29)");
   need(d->vocab >= 1 && d->vocab < ((int64_t)1 << 31), "vocab must be in [1, 2^31)");
   need(d->dim >= 1 && d->dim < (1 << 24), "dim must be in [1, 2^24)");
   need_dtype(d->dtype);
@@ -120,6 +120,7 @@ Embed check_embed(const ms_embed_desc* d) {
 
 struct EmbedWork {
   uint32_t *keys[2], *pos[2], *counts, *start;
+  float* part;
   int64_t bytes;
 };
 
@@ -127,23 +128,41 @@ EmbedWork embed_work(const ms_embed_desc* d, void* ws) {
   Carve c{(char*)ws};
   EmbedWork w;
   for (int i = 0; i < 2; ++i) w.keys[i] = c.take<uint32_t>(d->n_tokens), w.pos[i] = c.take<uint32_t>(d->n_tokens);
-  w.counts = c.take<uint32_t>((d->n_tokens + kSortTile - 1) / kSortTile * 256);
+  w.counts = c.take<uint32_t>((d->n_tokens + kSortTile - 1) / kSortTile << kSortBits);
   w.start = c.take<uint32_t>(d->vocab + 1);
+  w.part = c.take<float>((d->n_tokens + kRun - 1) / kRun * 2 * d->dim);
   w.bytes = c.used;
   return w;
 }
 
+template <class I, int N>
+void sort_small(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int key_bits, hipStream_t st) {
+  constexpr size_t lds = 1024 * N * 6 + 16 * 256 * 4 + 16;
+  const void* k = (const void*)k_sort_small<I, N>;
+  if (lds > 65536) HIPCHECK(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+  const int passes = (key_bits + 7) / 8, bits = (key_bits + passes - 1) / passes;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_small<I, N>), dim3(1), dim3(1024), lds, st, tokens, (int32_t)d->n_tokens,
+                     d->vocab, passes, bits, w.keys[0], w.pos[0]);
+}
+
+// Sorted pairs to keys[in], pos[in].
 template <class I>
 void sort_tokens(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int& in, hipStream_t st) {
   const int64_t n = d->n_tokens;
-  const unsigned tiles = (unsigned)((n + kSortTile - 1) / kSortTile);
+  int key_bits = 1;
+  while (d->vocab >> key_bits) ++key_bits;   // keys are in [0, vocab]
   in = 0;
-  for (int shift = 0; shift < 32 && (d->vocab >> shift) != 0; shift += 8, in ^= 1) {
-    const uint32_t *k = shift ? w.keys[in] : nullptr, *p = shift ? w.pos[in] : nullptr;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_count<I>), dim3(tiles), dim3(256), 0, st, tokens, k, n, d->vocab, shift,
-                       w.counts);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_move<I>), dim3(tiles), dim3(256), 0, st, tokens, k, p, n, d->vocab, shift,
-                       (const uint32_t*)w.counts, w.keys[in ^ 1], w.pos[in ^ 1]);
+  if (n <= 1024) return sort_small<I, 1>(d, tokens, w, key_bits, st);
+  if (n <= 4096) return sort_small<I, 4>(d, tokens, w, key_bits, st);
+  if (n <= 16384) return sort_small<I, 16>(d, tokens, w, key_bits, st);
+  const unsigned tiles = (unsigned)((n + kSortTile - 1) / kSortTile);
+  const int passes = (key_bits + kSortBits - 1) / kSortBits, bits = (key_bits + passes - 1) / passes;
+  for (int p = 0; p < passes; ++p, in ^= 1) {
+    const uint32_t *k = p ? w.keys[in] : nullptr, *q = p ? w.pos[in] : nullptr;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_count<I>), dim3(tiles), dim3(256), 0, st, tokens, k, n, d->vocab, p * bits,
+                       bits, w.counts);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_move<I>), dim3(tiles), dim3(256), 0, st, tokens, k, q, n, d->vocab, p * bits,
+                       bits, (const uint32_t*)w.counts, w.keys[in ^ 1], w.pos[in ^ 1]);
   }
 }
 
@@ -382,19 +401,21 @@ ms_status ms_embed_grad(const ms_embed_desc* d, const void* tokens, const void* 
       if (d->ids == MS_IDS_I64) sort_tokens(d, (const int64_t*)tokens, w, in, st);
       else sort_tokens(d, (const int32_t*)tokens, w, in, st);
     }
-    const unsigned vblocks = (unsigned)std::min<int64_t>((d->vocab + 256) / 256, kMaxBlocks);
-    hipLaunchKernelGGL(k_sort_starts, dim3(vblocks), dim3(256), 0, st, (const uint32_t*)w.keys[in], d->n_tokens, d->vocab,
-                       w.start);
     const int64_t v = Wide(es).of(d->dim).of(e.ts).of(e.os).at(drows, es).at(dtable, gs).v;
     const int32_t nv = (int32_t)(d->dim / v), tpr = threads_per_row(nv);
+    const unsigned nchunk = (unsigned)((d->n_tokens + kRun - 1) / kRun);
+    const unsigned searches = (unsigned)std::min<int64_t>((d->vocab + 256) / 256, kMaxBlocks / 2);
     with_type<8>(d->dtype, v, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed_pieces<T, V>), dim3(nchunk + searches), dim3(256), 0, st,
+                         (const uint32_t*)w.keys[in], (const uint32_t*)w.pos[in], d->n_tokens, d->vocab, (const T*)drows, nv,
+                         e.os, nchunk, w.start, w.part);
       auto go = [&](auto gz) {
         using D = decltype(gz);
         hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed_sum<T, D, V>), dim3(row_blocks(d->vocab, tpr)), dim3(256), 0, st,
-                           (const uint32_t*)w.pos[in], (const uint32_t*)w.start, (const T*)drows, (D*)dtable, d->vocab, nv,
-                           tpr, e.os, e.ts, (float)d->scale, d->accumulate);
+                           (const uint32_t*)w.pos[in], (const uint32_t*)w.start, (const T*)drows, (const float*)w.part, (D*)dtable,
+                           d->vocab, nv, tpr, e.os, e.ts, (float)d->scale, d->accumulate);
       };
       if (d->grad_dtype == MS_DTYPE_BF16) go((__bf16)0.0f);
       else go(0.0f);
