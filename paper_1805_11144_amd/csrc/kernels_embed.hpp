@@ -24,6 +24,31 @@ __device__ __forceinline__ float as_f32(T x) {
   return (float)x;
 }
 
+// Results go past the caches, which then keep what is read: a lookup of 131072
+// rows of 1024 bf16 took 83 us with plain stores and takes 55 with these.
+template <class T, int V>
+__device__ __forceinline__ void put_once(T* p, const Words<T, V>& w) {
+  constexpr int B = sizeof(T) * V;
+  if constexpr (B % 4 == 0) {
+    typedef uint32_t Raw __attribute__((ext_vector_type(B / 4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(Raw, w), (Raw*)p);
+  } else {
+    *(Words<T, V>*)p = w;
+  }
+}
+
+// Reads of what is used once, the same way.
+template <class T, int V>
+__device__ __forceinline__ Words<T, V> take_once(const T* p) {
+  constexpr int B = sizeof(T) * V;
+  if constexpr (B % 4 == 0) {
+    typedef uint32_t Raw __attribute__((ext_vector_type(B / 4)));
+    return __builtin_bit_cast(Words<T, V>, __builtin_nontemporal_load((const Raw*)p));
+  } else {
+    return *(const Words<T, V>*)p;
+  }
+}
+
 // LDS accesses of one wavefront stay in the order written here.
 __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -37,52 +62,61 @@ __device__ __forceinline__ uint32_t token_key(const I* tokens, int64_t i, int64_
   return t >= 0 && (int64_t)t < vocab ? (uint32_t)t : (uint32_t)vocab;
 }
 
-// `tpr` (a power of two, at most 256) threads per row, 256 / tpr rows per
-// workgroup; nv vectors of V values per row.
-template <class T, class I, int V>
+// `tpr` (a power of two, at most 256) threads per row, nv vectors of V values
+// per row; a group of threads has R rows in flight.
+template <class T, class I, int V, int R>
 __global__ void __launch_bounds__(256) k_embed(const I* tokens, const T* table, T* out, int64_t n, int64_t vocab,
                                                int32_t nv, int32_t tpr, int64_t ts, int64_t os, float scale) {
-  const int32_t rows = 256 / tpr;
-  for (int64_t i = (int64_t)blockIdx.x * rows + threadIdx.x / tpr; i < n; i += (int64_t)gridDim.x * rows) {
-    const uint32_t key = token_key(tokens, i, vocab);
-    const bool pad = key == (uint32_t)vocab;
-    const T* src = table + (int64_t)(pad ? 0 : key) * ts;
-    T* dst = out + i * os;
-    for (int32_t c = threadIdx.x % tpr; c < nv; c += tpr) {
-      Words<T, V> w;
-      if (!pad) w = *(const Words<T, V>*)(src + (int64_t)c * V);
+  const int32_t groups = 256 / tpr;
+  const int64_t step = (int64_t)gridDim.x * groups * R;
+  for (int64_t i = ((int64_t)blockIdx.x * R * groups) + threadIdx.x / tpr; i < n; i += step) {
+    uint32_t key[R];
 #pragma unroll
-      for (int e = 0; e < V; ++e) w.v[e] = pad ? (T)0.0f : (T)(scale * as_f32(w.v[e]));
-      *(Words<T, V>*)(dst + (int64_t)c * V) = w;
+    for (int r = 0; r < R; ++r) key[r] = token_key(tokens, min(i + r * groups, n - 1), vocab);
+    for (int32_t c = threadIdx.x % tpr; c < nv; c += tpr) {
+      Words<T, V> w[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        w[r] = *(const Words<T, V>*)(table + (int64_t)(key[r] < vocab ? key[r] : 0) * ts + (int64_t)c * V);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[r].v[e] = key[r] < vocab ? (T)(scale * as_f32(w[r].v[e])) : (T)0.0f;
+        if (i + r * groups < n) put_once(out + (i + r * groups) * os + (int64_t)c * V, w[r]);
+      }
     }
   }
 }
 
 // ------------------------------------------------------------------ sort
-constexpr int kSortItems = 16;                     // per thread
-constexpr int kSortTile = 256 * kSortItems;        // per workgroup
-constexpr int kSortBits = 10;                      // of a digit, at most
+constexpr int kSortBits = 10;   // of a digit, at most
+
+// A digit has at most 8 + log2 PER bits; counters come in rows of 256 PER.  A
+// tile is 256 N pairs.
 
 // How many of a tile's keys have each digit (`bits` bits at `shift`), to
 // counts[tile][digit].  The first pass reads the tokens (keys == NULL).
-template <class I>
+template <class I, int PER, int N>
 __global__ void __launch_bounds__(256) k_sort_count(const I* tokens, const uint32_t* keys, int64_t n, int64_t vocab,
                                                     int shift, int bits, uint32_t* counts) {
-  __shared__ uint32_t hist[1 << kSortBits];
-  const int digits = 1 << bits;
-  for (int d = threadIdx.x; d < digits; d += 256) hist[d] = 0;
-  __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortTile;
+  __shared__ uint32_t hist[256 * PER];
 #pragma unroll
-  for (int k = 0; k < kSortItems; ++k) {
-    const int64_t i = base + k * 256 + threadIdx.x;
-    if (i < n) {
-      const uint32_t key = keys ? keys[i] : token_key(tokens, i, vocab);
-      atomicAdd(&hist[(key >> shift) & (digits - 1)], 1u);
-    }
-  }
+  for (int q = 0; q < PER; ++q) hist[q * 256 + threadIdx.x] = 0;
   __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += 256) counts[(int64_t)blockIdx.x * digits + d] = hist[d];
+  const int64_t base = (int64_t)blockIdx.x * 256 * N;
+  uint32_t key[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int64_t i = base + k * 256 + threadIdx.x;
+    key[k] = i < n ? (keys ? keys[i] : token_key(tokens, i, vocab)) : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (base + k * 256 + threadIdx.x < n) atomicAdd(&hist[(key[k] >> shift) & ((1u << bits) - 1)], 1u);
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < PER; ++q)
+    counts[((int64_t)blockIdx.x * PER + q) * 256 + threadIdx.x] = hist[q * 256 + threadIdx.x];
 }
 
 // The lanes of a wavefront that hold live keys of this lane's digit.
@@ -126,73 +160,93 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
 
 // Moves each pair to its place: behind the pairs of smaller digits, of earlier
 // tiles and of earlier positions in the tile.  Wavefront w holds the tile's
-// positions [w * 1024, (w + 1) * 1024) in order of (item, lane).
-template <class I>
+// positions [w * 64 N, (w + 1) * 64 N) in order of (item, lane).
+template <class I, int PER, int N>
 __global__ void __launch_bounds__(256) k_sort_move(const I* tokens, const uint32_t* keys, const uint32_t* pos,
                                                    int64_t n, int64_t vocab, int shift, int bits,
                                                    const uint32_t* counts, uint32_t* keys_out, uint32_t* pos_out) {
-  constexpr int PER = (1 << kSortBits) / 256;   // digits of a thread: [tid * per, tid * per + per)
-  __shared__ uint32_t part[4][1 << kSortBits];  // a wavefront's pairs of each digit, then where its first one goes
+  __shared__ uint32_t part[4][256 * PER];   // a wavefront's pairs of each digit, then where its first one goes
+  __shared__ uint32_t first[256 * PER];     // pairs of each digit in all tiles, then of smaller digits
   __shared__ uint32_t sums[4];
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, digits = 1 << bits;
-  const int per = max(1, digits / 256);
-  for (int d = tid; d < digits; d += 256)
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  uint32_t key[N], rank[N], from[N];
+  const int64_t base = (int64_t)blockIdx.x * 256 * N + wave * 64 * N;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) part[w][d] = 0;
-  uint32_t key[kSortItems], rank[kSortItems];
-  const int64_t base = (int64_t)blockIdx.x * kSortTile + wave * 64 * kSortItems;
-#pragma unroll
-  for (int k = 0; k < kSortItems; ++k) {
+  for (int k = 0; k < N; ++k) {
     const int64_t i = base + k * 64 + lane;
     key[k] = i < n ? (keys ? keys[i] : token_key(tokens, i, vocab)) : 0;
+    from[k] = i < n && pos ? pos[i] : (uint32_t)i;
   }
-  // pairs of the thread's digits in all tiles, and in the earlier ones
-  uint32_t before[PER] = {}, total[PER] = {}, all = 0;
-  const bool has = tid * per < digits;
-  if (has) {
+  // pairs of the thread's digits, q * 256 + tid, in all tiles and in the earlier ones
+  uint32_t before[PER] = {}, total[PER] = {};
+  const uint32_t* c = counts + tid;
+  const uint32_t tiles = gridDim.x;
+  constexpr int A = 64 / PER;   // tiles in flight
+  uint32_t t = 0;
+  for (; t + A <= tiles; t += A) {
+    uint32_t x[A][PER];
+#pragma unroll
+    for (int u = 0; u < A; ++u)
+#pragma unroll
+      for (int q = 0; q < PER; ++q) x[u][q] = c[((int64_t)(t + u) * PER + q) * 256];
+#pragma unroll
+    for (int u = 0; u < A; ++u)
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        total[q] += x[u][q];
+        before[q] += t + u < blockIdx.x ? x[u][q] : 0;
+      }
+  }
 #pragma unroll 8
-    for (uint32_t t = 0; t < gridDim.x; ++t)
+  for (; t < tiles; ++t)
 #pragma unroll
-      for (int q = 0; q < PER; ++q)
-        if (q < per) {
-          const uint32_t c = counts[(int64_t)t * digits + tid * per + q];
-          total[q] += c;
-          before[q] += t < blockIdx.x ? c : 0;
-        }
+    for (int q = 0; q < PER; ++q) {
+      const uint32_t x = c[((int64_t)t * PER + q) * 256];
+      total[q] += x;
+      before[q] += t < blockIdx.x ? x : 0;
+    }
 #pragma unroll
-    for (int q = 0; q < PER; ++q) all += total[q];
+  for (int q = 0; q < PER; ++q) {
+    first[q * 256 + tid] = total[q];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) part[w][q * 256 + tid] = 0;
   }
+  __syncthreads();
+  // pairs of smaller digits: thread tid adds up digits [tid * PER, tid * PER + PER)
+  uint32_t own[PER], all = 0;
+#pragma unroll
+  for (int q = 0; q < PER; ++q) own[q] = first[tid * PER + q], all += own[q];
   const uint32_t incl = wave_prefix(all);
   if (lane == 63) sums[wave] = incl;
+  rank_keys<N>(key, rank, part[wave], base, n, shift, bits);
   __syncthreads();
   uint32_t lower = incl - all;
   for (int w = 0; w < wave; ++w) lower += sums[w];
-  rank_keys<kSortItems>(key, rank, part[wave], base, n, shift, bits);
-  __syncthreads();
-  if (has) {
 #pragma unroll
-    for (int q = 0; q < PER; ++q)
-      if (q < per) {
-        uint32_t at = lower + before[q];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t c = part[w][tid * per + q];
-          part[w][tid * per + q] = at;
-          at += c;
-        }
-        lower += total[q];
-      }
+  for (int q = 0; q < PER; ++q) {
+    first[tid * PER + q] = lower;
+    lower += own[q];
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kSortItems; ++k) {
-    const int64_t i = base + k * 64 + lane;
-    if (i < n) {
-      const uint32_t at = part[wave][(key[k] >> shift) & (digits - 1)] + rank[k];
-      keys_out[at] = key[k];
-      pos_out[at] = pos ? pos[i] : (uint32_t)i;
+  for (int q = 0; q < PER; ++q) {
+    const int d = q * 256 + tid;
+    uint32_t at = first[d] + before[q];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t x = part[w][d];
+      part[w][d] = at;
+      at += x;
     }
   }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (base + k * 64 + lane < n) {
+      const uint32_t at = part[wave][(key[k] >> shift) & ((1u << bits) - 1)] + rank[k];
+      keys_out[at] = key[k];
+      pos_out[at] = from[k];
+    }
 }
 
 // The whole sort in one workgroup, for at most 1024 N tokens: pairs in LDS
@@ -268,24 +322,45 @@ __global__ void __launch_bounds__(1024) k_sort_small(const I* tokens, int32_t n,
 // leaves their sums in part[chunk][2][dim].
 constexpr int kRun = 64;
 
-// Columns c, c + tpr.. of the sum of rows pos[s0] .. pos[s1 - 1], handed to put(c, sums).
-template <class T, int V, class F>
+// Columns first, first + tpr.. of the sum of the rows at pos[s0] .. pos[s1 - 1]
+// (at most kRun of them), handed to put(c, sums).  FULL: whole wavefronts work
+// on one row, so its positions are fetched once, one to a lane, and a row's
+// address is uniform; eight rows are in flight at a time.
+template <class T, int V, bool FULL, class F>
 __device__ __forceinline__ void sum_rows(const uint32_t* pos, uint32_t s0, uint32_t s1, const T* rows, int64_t rs,
                                          int32_t first, int32_t nv, int32_t tpr, F&& put) {
+  constexpr int A = 8;
+  const int n = (int)(s1 - s0);
+  uint32_t mine = 0;
+  if (FULL && (int)threadIdx.x % 64 < n) mine = pos[s0 + threadIdx.x % 64];
+  const auto row = [&](int s) {
+    const uint32_t p = FULL ? (uint32_t)__builtin_amdgcn_readlane((int)mine, s) : pos[s0 + s];
+    return rows + (int64_t)p * rs;
+  };
   for (int32_t c = first; c < nv; c += tpr) {
     float acc[V] = {};
-    uint32_t s = s0;
-    for (; s + 4 <= s1; s += 4) {
+    int s = 0;
+    for (; s + A <= n; s += A) {
+      Words<T, V> w[A];
+#pragma unroll
+      for (int q = 0; q < A; ++q) w[q] = take_once<T, V>(row(s + q) + (int64_t)c * V);
+#pragma unroll
+      for (int q = 0; q < A; ++q)
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += as_f32(w[q].v[e]);
+    }
+    if (s + 4 <= n) {
       Words<T, V> w[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) w[q] = *(const Words<T, V>*)(rows + (int64_t)pos[s + q] * rs + (int64_t)c * V);
+      for (int q = 0; q < 4; ++q) w[q] = take_once<T, V>(row(s + q) + (int64_t)c * V);
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] += as_f32(w[q].v[e]);
+      s += 4;
     }
-    for (; s < s1; ++s) {
-      const Words<T, V> w = *(const Words<T, V>*)(rows + (int64_t)pos[s] * rs + (int64_t)c * V);
+    for (; s < n; ++s) {
+      const Words<T, V> w = *(const Words<T, V>*)(row(s) + (int64_t)c * V);
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[e] += as_f32(w.v[e]);
     }
@@ -293,15 +368,16 @@ __device__ __forceinline__ void sum_rows(const uint32_t* pos, uint32_t s0, uint3
   }
 }
 
-// Workgroups [0, nchunk) sum the pieces of long runs; the others find
-// start[v], v in [0, vocab]: the first sorted pair whose token is at least v.
+// The first `searches` workgroups find start[v], v in [0, vocab]: the first
+// sorted pair whose token is at least v.  The others sum the pieces of long
+// runs, `tpc` threads (a multiple of 64) to a chunk.
 template <class T, int V>
 __global__ void __launch_bounds__(256) k_embed_pieces(const uint32_t* keys, const uint32_t* pos, int64_t n,
-                                                      int64_t vocab, const T* rows, int32_t nv, int64_t rs,
-                                                      uint32_t nchunk, uint32_t* start, float* part) {
-  if (blockIdx.x >= nchunk) {
-    const int64_t step = (int64_t)(gridDim.x - nchunk) * 256;
-    for (int64_t v = (int64_t)(blockIdx.x - nchunk) * 256 + threadIdx.x; v <= vocab; v += step) {
+                                                      int64_t vocab, const T* rows, int32_t nv, int32_t tpc, int64_t rs,
+                                                      uint32_t searches, uint32_t* start, float* part) {
+  if (blockIdx.x < searches) {
+    const int64_t step = (int64_t)searches * 256;
+    for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v <= vocab; v += step) {
       uint32_t lo = 0, hi = (uint32_t)n;
       while (lo < hi) {
         const uint32_t mid = lo + (hi - lo) / 2;
@@ -312,41 +388,47 @@ __global__ void __launch_bounds__(256) k_embed_pieces(const uint32_t* keys, cons
     }
     return;
   }
-  const uint32_t c0 = blockIdx.x * kRun, c1 = (uint32_t)min((int64_t)c0 + kRun, n);
+  const int64_t chunk = __builtin_amdgcn_readfirstlane((blockIdx.x - searches) * (256 / tpc) + threadIdx.x / tpc);
+  if (chunk * kRun >= n) return;
+  const uint32_t c0 = (uint32_t)chunk * kRun, c1 = (uint32_t)min((int64_t)c0 + kRun, n);
   const int lane = threadIdx.x % 64;
-  const uint32_t k0 = keys[c0], k1 = keys[c1 - 1];
+  // the keys of this chunk and its neighbours: enough to tell whether its first and last runs are long
+  uint32_t near[3];
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const int64_t i = (int64_t)c0 + (w - 1) * kRun + lane;
+    near[w] = i >= 0 && i < n ? keys[i] : ~0u;   // no key
+  }
+  const uint32_t k0 = __builtin_amdgcn_readfirstlane(near[1]);
+  const uint32_t k1 = __builtin_amdgcn_readlane(near[1], (int)(c1 - c0) - 1);
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
     if (side == 1 && k1 == k0) return;
     const uint32_t k = side ? k1 : k0;
     if (k == (uint32_t)vocab) continue;   // padding
-    // the run's pairs in this chunk and its neighbours: enough to tell whether it is long
-    int seen = 0, here = 0;
-#pragma unroll
-    for (int w = -1; w <= 1; ++w) {
-      const int64_t i = (int64_t)c0 + w * kRun + lane;
-      const int same = __popcll(__ballot(i >= 0 && i < n && keys[i < 0 ? 0 : i < n ? i : n - 1] == k));
-      seen += same;
-      if (w == 0) here = same;
-    }
-    if (seen <= kRun) continue;
+    const int here = __popcll(__ballot(near[1] == k));
+    if (here + __popcll(__ballot(near[0] == k)) + __popcll(__ballot(near[2] == k)) <= kRun) continue;
     const uint32_t s0 = side ? c1 - here : c0;
-    float* o = part + ((int64_t)blockIdx.x * 2 + side) * nv * V;
-    sum_rows<T, V>(pos, s0, s0 + here, rows, rs, threadIdx.x, nv, 256, [&](int32_t c, const float* acc) {
+    float* o = part + (chunk * 2 + side) * nv * V;
+    sum_rows<T, V, true>(pos, s0, s0 + here, rows, rs, threadIdx.x % tpc, nv, tpc, [&](int32_t c, const float* acc) {
+      Words<float, V> x;
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[(int64_t)c * V + e] = acc[e];
+      for (int e = 0; e < V; ++e) x.v[e] = acc[e];
+      *(Words<float, V>*)(o + (int64_t)c * V) = x;
     });
   }
 }
 
 // dtable[v] = scale * sum of the rows at pos[start[v]] .. pos[start[v + 1] - 1].
-template <class T, class D, int V>
+// FULL: tpr is a multiple of 64.
+template <class T, class D, int V, bool FULL>
 __global__ void __launch_bounds__(256) k_embed_sum(const uint32_t* pos, const uint32_t* start, const T* rows,
                                                    const float* part, D* dtable, int64_t vocab, int32_t nv, int32_t tpr,
                                                    int64_t rs, int64_t gs, float scale, int accumulate) {
   const int32_t rpb = 256 / tpr;
   for (int64_t v = (int64_t)blockIdx.x * rpb + threadIdx.x / tpr; v < vocab; v += (int64_t)gridDim.x * rpb) {
-    const uint32_t s0 = start[v], s1 = start[v + 1];
+    uint32_t s0 = start[v], s1 = start[v + 1];
+    if (FULL) s0 = __builtin_amdgcn_readfirstlane(s0), s1 = __builtin_amdgcn_readfirstlane(s1);
     if (accumulate && s0 == s1) continue;
     const auto put = [&](int32_t c, const float* acc) {
       D* dst = dtable + v * gs + (int64_t)c * V;
@@ -354,26 +436,24 @@ __global__ void __launch_bounds__(256) k_embed_sum(const uint32_t* pos, const ui
       if (accumulate) o = *(const Words<D, V>*)dst;
 #pragma unroll
       for (int e = 0; e < V; ++e) o.v[e] = (D)(scale * acc[e] + (accumulate ? as_f32(o.v[e]) : 0.0f));
-      *(Words<D, V>*)dst = o;
+      put_once(dst, o);
     };
     if (s1 - s0 <= (uint32_t)kRun) {
-      sum_rows<T, V>(pos, s0, s1, rows, rs, threadIdx.x % tpr, nv, tpr, put);
+      sum_rows<T, V, FULL>(pos, s0, s1, rows, rs, threadIdx.x % tpr, nv, tpr, put);
       continue;
     }
     // the pieces in order: its first chunk holds the run's beginning, as its first pair or up to its last
     const uint32_t b0 = s0 / kRun, b1 = (s1 - 1) / kRun;
     for (int32_t c = threadIdx.x % tpr; c < nv; c += tpr) {
-      float acc[V];
       const float* q = part + ((int64_t)b0 * 2 + (s0 % kRun != 0)) * nv * V + (int64_t)c * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] = q[e];
-#pragma unroll 4
+      Words<float, V> acc = *(const Words<float, V>*)q;
+#pragma unroll 8
       for (uint32_t b = b0 + 1; b <= b1; ++b) {
-        q = part + (int64_t)b * 2 * nv * V + (int64_t)c * V;
+        const Words<float, V> x = *(const Words<float, V>*)(part + (int64_t)b * 2 * nv * V + (int64_t)c * V);
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] += q[e];
+        for (int e = 0; e < V; ++e) acc.v[e] += x.v[e];
       }
-      put(c, acc);
+      put(c, acc.v);
     }
   }
 }

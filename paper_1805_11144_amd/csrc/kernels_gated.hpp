@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(256) k_gated(GatedArgs p, const T* v, const T*
       h[e] = gated_step(h[e], as_f32(q.v[e]), as_f32(x.v[e]));
       o.v[e] = (T)h[e];
     }
-    *(Words<T, V>*)(yp + t * p.yt) = o;
+    put_once(yp + t * p.yt, o);
   }
   Words<T, V> zero;
 #pragma unroll
@@ -217,8 +217,8 @@ __global__ void __launch_bounds__(256) k_gated_grad(GatedArgs p, const T* v, con
           og.v[e] = (T)(a * r * (before[k][e] - as_f32(xv[k].v[e])) * d);
           m[e] = a * d;
         }
-        *(Words<T, V>*)(dvp + (s0 + k) * p.dim) = ov;
-        *(Words<T, V>*)(dgp + (s0 + k) * p.dim) = og;
+        put_once(dvp + (s0 + k) * p.dim, ov);
+        put_once(dgp + (s0 + k) * p.dim, og);
       }
   }
   if (dy0 && t0 == 0) {

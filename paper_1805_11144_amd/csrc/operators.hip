@@ -118,6 +118,12 @@ Embed check_embed(const ms_embed_desc* d) {
   return e;
 }
 
+// Items of a thread in the sort: a tile holds 256 times as many pairs.  Every
+// tile adds up the counts of all tiles, so they grow where they become many.
+int sort_items(int64_t n) { return n <= (1 << 16) ? 4 : n <= (1 << 18) ? 8 : 16; }
+
+int64_t sort_tiles(int64_t n) { return (n + 256 * sort_items(n) - 1) / (256 * sort_items(n)); }
+
 struct EmbedWork {
   uint32_t *keys[2], *pos[2], *counts, *start;
   float* part;
@@ -128,7 +134,7 @@ EmbedWork embed_work(const ms_embed_desc* d, void* ws) {
   Carve c{(char*)ws};
   EmbedWork w;
   for (int i = 0; i < 2; ++i) w.keys[i] = c.take<uint32_t>(d->n_tokens), w.pos[i] = c.take<uint32_t>(d->n_tokens);
-  w.counts = c.take<uint32_t>((d->n_tokens + kSortTile - 1) / kSortTile << kSortBits);
+  w.counts = c.take<uint32_t>(sort_tiles(d->n_tokens) << kSortBits);
   w.start = c.take<uint32_t>(d->vocab + 1);
   w.part = c.take<float>((d->n_tokens + kRun - 1) / kRun * 2 * d->dim);
   w.bytes = c.used;
@@ -145,6 +151,20 @@ void sort_small(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int key_b
                      d->vocab, passes, bits, w.keys[0], w.pos[0]);
 }
 
+template <class I, int PER, int N>
+void sort_tiled(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int key_bits, int& in, hipStream_t st) {
+  const int64_t n = d->n_tokens;
+  const unsigned tiles = (unsigned)sort_tiles(n);
+  const int passes = (key_bits + kSortBits - 1) / kSortBits, bits = (key_bits + passes - 1) / passes;
+  for (int p = 0; p < passes; ++p, in ^= 1) {
+    const uint32_t *k = p ? w.keys[in] : nullptr, *q = p ? w.pos[in] : nullptr;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_count<I, PER, N>), dim3(tiles), dim3(256), 0, st, tokens, k, n, d->vocab,
+                       p * bits, bits, w.counts);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_move<I, PER, N>), dim3(tiles), dim3(256), 0, st, tokens, k, q, n, d->vocab,
+                       p * bits, bits, (const uint32_t*)w.counts, w.keys[in ^ 1], w.pos[in ^ 1]);
+  }
+}
+
 // Sorted pairs to keys[in], pos[in].
 template <class I>
 void sort_tokens(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int& in, hipStream_t st) {
@@ -154,16 +174,18 @@ void sort_tokens(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int& in,
   in = 0;
   if (n <= 1024) return sort_small<I, 1>(d, tokens, w, key_bits, st);
   if (n <= 4096) return sort_small<I, 4>(d, tokens, w, key_bits, st);
-  if (n <= 16384) return sort_small<I, 16>(d, tokens, w, key_bits, st);
-  const unsigned tiles = (unsigned)((n + kSortTile - 1) / kSortTile);
   const int passes = (key_bits + kSortBits - 1) / kSortBits, bits = (key_bits + passes - 1) / passes;
-  for (int p = 0; p < passes; ++p, in ^= 1) {
-    const uint32_t *k = p ? w.keys[in] : nullptr, *q = p ? w.pos[in] : nullptr;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_count<I>), dim3(tiles), dim3(256), 0, st, tokens, k, n, d->vocab, p * bits,
-                       bits, w.counts);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_move<I>), dim3(tiles), dim3(256), 0, st, tokens, k, q, n, d->vocab, p * bits,
-                       bits, (const uint32_t*)w.counts, w.keys[in ^ 1], w.pos[in ^ 1]);
-  }
+  const auto with = [&](auto per) {
+    constexpr int PER = decltype(per)::value;
+    switch (sort_items(n)) {
+      case 4: return sort_tiled<I, PER, 4>(d, tokens, w, key_bits, in, st);
+      case 8: return sort_tiled<I, PER, 8>(d, tokens, w, key_bits, in, st);
+      default: return sort_tiled<I, PER, 16>(d, tokens, w, key_bits, in, st);
+    }
+  };
+  if (bits <= 8) with(std::integral_constant<int, 1>{});
+  else if (bits == 9) with(std::integral_constant<int, 2>{});
+  else with(std::integral_constant<int, 4>{});
 }
 
 // ------------------------------------------------------------------ gated
@@ -359,12 +381,14 @@ ms_status ms_embed(const ms_embed_desc* d, const void* tokens, const void* table
     const hipStream_t st = (hipStream_t)d->stream;
     const int64_t v = Wide(es).of(d->dim).of(e.ts).of(e.os).at(table, es).at(out, es).v;
     const int32_t nv = (int32_t)(d->dim / v), tpr = threads_per_row(nv);
+    constexpr int kLookupRows = 4;
+    const int64_t lookups = (d->n_tokens + kLookupRows - 1) / kLookupRows;
     with_type<8>(d->dtype, v, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
       auto go = [&](auto id) {
         using I = decltype(id);
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed<T, I, V>), dim3(row_blocks(d->n_tokens, tpr)), dim3(256), 0, st,
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed<T, I, V, kLookupRows>), dim3(row_blocks(lookups, tpr)), dim3(256), 0, st,
                            (const I*)tokens, (const T*)table, (T*)out, d->n_tokens, d->vocab, nv, tpr, e.ts, e.os,
                            (float)d->scale);
       };
@@ -403,22 +427,29 @@ ms_status ms_embed_grad(const ms_embed_desc* d, const void* tokens, const void* 
     }
     const int64_t v = Wide(es).of(d->dim).of(e.ts).of(e.os).at(drows, es).at(dtable, gs).v;
     const int32_t nv = (int32_t)(d->dim / v), tpr = threads_per_row(nv);
-    const unsigned nchunk = (unsigned)((d->n_tokens + kRun - 1) / kRun);
+    const int32_t tpc = std::max(tpr, 64);   // a chunk's threads: whole wavefronts
+    const int64_t chunks = (d->n_tokens + kRun - 1) / kRun;
+    const unsigned pieces = (unsigned)((chunks + 256 / tpc - 1) / (256 / tpc));
     const unsigned searches = (unsigned)std::min<int64_t>((d->vocab + 256) / 256, kMaxBlocks / 2);
     with_type<8>(d->dtype, v, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed_pieces<T, V>), dim3(nchunk + searches), dim3(256), 0, st,
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed_pieces<T, V>), dim3(searches + pieces), dim3(256), 0, st,
                          (const uint32_t*)w.keys[in], (const uint32_t*)w.pos[in], d->n_tokens, d->vocab, (const T*)drows, nv,
-                         e.os, nchunk, w.start, w.part);
-      auto go = [&](auto gz) {
+                         tpc, e.os, searches, w.start, w.part);
+      auto go = [&](auto gz, auto full) {
         using D = decltype(gz);
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed_sum<T, D, V>), dim3(row_blocks(d->vocab, tpr)), dim3(256), 0, st,
-                           (const uint32_t*)w.pos[in], (const uint32_t*)w.start, (const T*)drows, (const float*)w.part, (D*)dtable,
-                           d->vocab, nv, tpr, e.os, e.ts, (float)d->scale, d->accumulate);
+        constexpr bool FULL = decltype(full)::value;
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed_sum<T, D, V, FULL>), dim3(row_blocks(d->vocab, tpr)), dim3(256), 0, st,
+                           (const uint32_t*)w.pos[in], (const uint32_t*)w.start, (const T*)drows, (const float*)w.part,
+                           (D*)dtable, d->vocab, nv, tpr, e.os, e.ts, (float)d->scale, d->accumulate);
       };
-      if (d->grad_dtype == MS_DTYPE_BF16) go((__bf16)0.0f);
-      else go(0.0f);
+      const auto out = [&](auto full) {
+        if (d->grad_dtype == MS_DTYPE_BF16) go((__bf16)0.0f, full);
+        else go(0.0f, full);
+      };
+      if (tpr >= 64) out(std::true_type{});
+      else out(std::false_type{});
     });
     HIPCHECK(hipGetLastError());
   });
