@@ -2,29 +2,42 @@
 // over whole sequences, its gradient, and its single step.
 //
 // A run of steps maps the state that enters it to the one that leaves it by
-// y -> A y + Y, A the product of its a[t] and Y what it leaves from zero, so
-// runs can be taken at once and joined: with (A1, Y1) before (A2, Y2) the two
-// together are (A1 A2, A2 Y1 + Y2).  Each channel's steps are cut into chunks;
-// one kernel leaves every chunk's (A, Y), the next joins those before its own
-// and goes through its steps from the state that it finds.  The gradient runs
-// the same way from the end: m = a d goes from a step to the one before it, with
-// d[t] = dy[t] + m[t+1].
+// y -> A y + Y, A the product of its a[t] and Y what it leaves from zero.  The
+// gradient runs the same way from the end: m = a d goes from a step to the one
+// before it, with d[t] = dy[t] + m[t+1], so a run maps m -> A m + M.
+//
+// Memory bounds it: each array has to be read or written once, a step costs
+// two transcendental instructions and about ten others for its 3 (gradient: 5)
+// values.  So every value is read once and stays in registers until its result
+// is known.  A wavefront takes kKeep = 16 steps of 64 V channels, fetched
+// together; its lanes know their runs' maps, and the wavefronts of a workgroup,
+// which hold consecutive runs, join them in LDS.  Sequences longer than a
+// workgroup's 128 steps are cut into such chunks.  With enough channels, or a
+// few chunks, a workgroup goes through its chunks one after the other (LINK =
+// false).  Otherwise the chunks run side by side (LINK): each leaves its map
+// for the later ones, and every kSpan-th the state that it ends with; a chunk
+// waits for the state at its span's beginning and the maps in between.  The
+// order of these operations is fixed, so the result does not depend on timing.
 #pragma once
 
 #include "kernels_embed.hpp"
 
-// Steps between the states that the forward pass leaves for the gradient.  The
-// gradient computes the states between them again, in registers.
+// Steps of a wavefront, and between the states that the forward pass leaves for
+// the gradient, which computes the states between them again.
 constexpr int kKeep = 16;
+constexpr int kSpan = 8;   // chunks from one published state to the next
 
-// A thread takes V neighbouring channels of one batch row: thread i of the
-// grid's x axis is row i / nv and channels (i % nv) V .. + V; blockIdx.y is the
-// chunk.
+// A lane takes V neighbouring channels of one batch row: lane i of all is row
+// i / nv and channels (i % nv) V .. + V.
 struct GatedArgs {
   int64_t batch, steps, dim, nv;    // nv = dim / V
   int64_t vb, vt, gb, gt, yb, yt;   // strides of v, g and y (dy in the gradient)
   const int32_t* lengths;
-  int32_t chunk, nchunk;            // steps per chunk (a multiple of kKeep), chunks
+  int32_t nchunk, groups;           // chunks of blockDim / 64 * kKeep steps; workgroups per chunk
+  // LINK: what chunks leave for each other, all ones before the launch
+  uint64_t* maps;                   // [nchunk][batch * dim]: (A, Y)
+  uint32_t* states;                 // [nchunk / kSpan][batch * dim]
+  uint32_t* ticket;
 };
 
 __device__ __forceinline__ int32_t row_length(const GatedArgs& p, int64_t b) {
@@ -38,7 +51,6 @@ __device__ __forceinline__ void gate(float g, float& a, float& rest) {
   const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
   a = g >= 0.0f ? big : small;
   rest = g >= 0.0f ? small : big;
-  if (g != g) a = rest = g;
 }
 
 // One step of the filter.
@@ -48,182 +60,327 @@ __device__ __forceinline__ float gated_step(float y, float g, float v) {
   return fmaf(a, y, r * v);
 }
 
-// (A, Y) of each chunk to join[batch][chunk][2][dim].
-template <class T, int V>
-__global__ void __launch_bounds__(256) k_gated_part(GatedArgs p, const T* v, const T* g, float* join) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= p.batch * p.nv) return;
-  const int64_t b = i / p.nv, c = (i - b * p.nv) * V;
-  const int32_t t0 = blockIdx.y * p.chunk, t1 = min(t0 + p.chunk, row_length(p, b));
-  float A[V], Y[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) A[e] = 1.0f, Y[e] = 0.0f;
-  const T *vp = v + b * p.vb + c, *gp = g + b * p.gb + c;
-#pragma unroll 8
-  for (int32_t t = t0; t < t1; ++t) {
-    const Words<T, V> x = *(const Words<T, V>*)(vp + t * p.vt), q = *(const Words<T, V>*)(gp + t * p.gt);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      float a, r;
-      gate(as_f32(q.v[e]), a, r);
-      A[e] *= a;
-      Y[e] = fmaf(a, Y[e], r * as_f32(x.v[e]));
-    }
-  }
-  float* o = join + ((b * p.nchunk + blockIdx.y) * 2) * p.dim + c;
-#pragma unroll
-  for (int e = 0; e < V; ++e) o[e] = A[e], o[p.dim + e] = Y[e];
+// What is published is never all ones, which stands for "not yet": a NaN's bits
+// can come from the inputs, so NaN is published as the one of this pattern.
+__device__ __forceinline__ uint32_t published(float x) {
+  return x != x ? 0x7fc00000u : __builtin_bit_cast(uint32_t, x);
 }
 
-// The filter's steps of one chunk, from y0 and the chunks before it.
-template <class T, int V>
-__global__ void __launch_bounds__(256) k_gated(GatedArgs p, const T* v, const T* g, const float* y0, const float* join,
-                                               T* y, float* last, float* kept) {
+__global__ void __launch_bounds__(256) k_gated_clear(uint32_t* words, int64_t n, uint32_t* ticket) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= p.batch * p.nv) return;
-  const int64_t b = i / p.nv, c = (i - b * p.nv) * V;
-  const int32_t len = row_length(p, b);
-  const int32_t t0 = blockIdx.y * p.chunk, tend = (int32_t)min((int64_t)t0 + p.chunk, p.steps);
-  const int32_t t1 = min(tend, len);
-  float h[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) h[e] = y0 ? y0[b * p.dim + c + e] : 0.0f;
-  const float* j = join + b * p.nchunk * 2 * p.dim + c;
-  for (int32_t k = 0; k < (int32_t)blockIdx.y; ++k, j += 2 * p.dim) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = fmaf(j[e], h[e], j[p.dim + e]);
-  }
-  const T *vp = v + b * p.vb + c, *gp = g + b * p.gb + c;
-  T* yp = y + b * p.yb + c;
-  float* kp = kept + (b * ((p.steps + kKeep - 1) / kKeep)) * p.dim + c;
-#pragma unroll 8
-  for (int32_t t = t0; t < t1; ++t) {
-    if (kept && t % kKeep == 0) {
-#pragma unroll
-      for (int e = 0; e < V; ++e) kp[(t / kKeep) * p.dim + e] = h[e];
-    }
-    const Words<T, V> x = *(const Words<T, V>*)(vp + t * p.vt), q = *(const Words<T, V>*)(gp + t * p.gt);
-    Words<T, V> o;
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      h[e] = gated_step(h[e], as_f32(q.v[e]), as_f32(x.v[e]));
-      o.v[e] = (T)h[e];
-    }
-    put_once(yp + t * p.yt, o);
-  }
-  Words<T, V> zero;
-#pragma unroll
-  for (int e = 0; e < V; ++e) zero.v[e] = (T)0.0f;
-  for (int32_t t = max(t0, t1); t < tend; ++t) *(Words<T, V>*)(yp + t * p.yt) = zero;
-  // the chunk that holds the row's end (the first one of an empty row)
-  if (last && (len == 0 ? t0 == 0 : len > t0 && len <= t0 + p.chunk)) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) last[b * p.dim + c + e] = h[e];
-  }
+  if (i == 0) *ticket = 0;
+  for (int64_t k = i; k < n; k += (int64_t)gridDim.x * 256) words[k] = ~0u;
 }
 
-// last of rows without steps.
+// last (dy0) of rows without steps.
 __global__ void __launch_bounds__(256) k_gated_none(const float* from, float* to, int64_t n) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i < n) to[i] = from ? from[i] : 0.0f;
 }
 
-// The gradient's chunk: (A, M) with m = A m' + M for the m' that enters at its end.
-template <class T, int V>
-__global__ void __launch_bounds__(256) k_gated_grad_part(GatedArgs p, const T* g, const T* dy, float* join) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= p.batch * p.nv) return;
-  const int64_t b = i / p.nv, c = (i - b * p.nv) * V;
-  const int32_t t0 = blockIdx.y * p.chunk, t1 = min(t0 + p.chunk, row_length(p, b));
-  float A[V], M[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) A[e] = 1.0f, M[e] = 0.0f;
-  const T *gp = g + b * p.gb + c, *dp = dy + b * p.yb + c;
-#pragma unroll 8
-  for (int32_t t = t1 - 1; t >= t0; --t) {
-    const Words<T, V> x = *(const Words<T, V>*)(dp + t * p.yt), q = *(const Words<T, V>*)(gp + t * p.gt);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      float a, r;
-      gate(as_f32(q.v[e]), a, r);
-      A[e] *= a;
-      M[e] = a * (as_f32(x.v[e]) + M[e]);
-    }
-  }
-  float* o = join + ((b * p.nchunk + blockIdx.y) * 2) * p.dim + c;
-#pragma unroll
-  for (int e = 0; e < V; ++e) o[e] = A[e], o[p.dim + e] = M[e];
+// The chunk and the channel group of a workgroup.  Chunks that wait for others
+// take theirs in the order in which they start (`order` counts along the
+// direction of the recurrence), so a workgroup waits only for such that started
+// before it, and these publish their maps without waiting for anyone: every
+// wait ends.
+struct GatedPlace {
+  int32_t order;
+  int64_t group;
+};
+
+template <bool LINK>
+__device__ __forceinline__ GatedPlace gated_place(const GatedArgs& p, uint32_t* box) {
+  if (!LINK) return {0, (int64_t)blockIdx.x};
+  if (threadIdx.x == 0) *box = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  const uint32_t t = __builtin_amdgcn_readfirstlane(*box);
+  return {(int32_t)(t / (uint32_t)p.groups), (int64_t)(t % (uint32_t)p.groups)};
 }
 
-template <class T, int V>
-__global__ void __launch_bounds__(256) k_gated_grad(GatedArgs p, const T* v, const T* g, const float* kept, const T* dy,
-                                                    const float* dlast, const float* join, T* dv, T* dg, float* dy0) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= p.batch * p.nv) return;
-  const int64_t b = i / p.nv, c = (i - b * p.nv) * V;
-  const int32_t t0 = blockIdx.y * p.chunk, tend = (int32_t)min((int64_t)t0 + p.chunk, p.steps);
-  const int32_t t1 = min(tend, row_length(p, b));
-  float m[V];
+// The value that enters chunk number `order` for the channels at `at`: `first`
+// at the beginning, else from what earlier chunks published.  A, Y: the chunk's
+// own map.  Every word is one atomic access of its own, so a word that is there
+// is whole; a chunk's words need no order among themselves.
+template <int V>
+__device__ __forceinline__ void gated_link(const GatedArgs& p, int32_t order, int64_t at, const float* A, const float* Y,
+                                           const float* first, float* h) {
+  const int64_t channels = p.batch * p.dim;
+  const int32_t span = order / kSpan, from = span * kSpan;
+  if (order + 1 < p.nchunk) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) m[e] = dlast ? dlast[b * p.dim + c + e] : 0.0f;
-  for (int32_t k = p.nchunk - 1; k > (int32_t)blockIdx.y; --k) {
-    const float* j = join + (b * p.nchunk + k) * 2 * p.dim + c;
-#pragma unroll
-    for (int e = 0; e < V; ++e) m[e] = fmaf(j[e], m[e], j[p.dim + e]);
+    for (int e = 0; e < V; ++e)
+      __hip_atomic_store(p.maps + order * channels + at + e, (uint64_t)published(Y[e]) << 32 | published(A[e]),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  const T *vp = v + b * p.vb + c, *gp = g + b * p.gb + c, *dp = dy + b * p.yb + c;
-  T *dvp = dv + b * p.steps * p.dim + c, *dgp = dg + b * p.steps * p.dim + c;
-  Words<T, V> zero;
+  uint64_t map[kSpan - 1][V];
+  uint32_t state[V];
+  bool wait;
+  do {
+    wait = false;
 #pragma unroll
-  for (int e = 0; e < V; ++e) zero.v[e] = (T)0.0f;
-  for (int32_t t = max(t0, t1); t < tend; ++t) {
-    *(Words<T, V>*)(dvp + t * p.dim) = zero;
-    *(Words<T, V>*)(dgp + t * p.dim) = zero;
-  }
-  const int64_t nkeep = (p.steps + kKeep - 1) / kKeep;
-  for (int32_t s0 = t1 > t0 ? (t1 - 1) / kKeep * kKeep : t0 - 1; s0 >= t0; s0 -= kKeep) {
-    const int n = min(kKeep, t1 - s0);
-    Words<T, V> xv[kKeep], xg[kKeep];
-    float before[kKeep][V];   // y[t - 1]
+    for (int e = 0; e < V; ++e) {
+      state[e] = 0;
+      if (span > 0)
+        state[e] = __hip_atomic_load(p.states + (span - 1) * channels + at + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      wait |= state[e] == ~0u;
+    }
 #pragma unroll
-    for (int k = 0; k < kKeep; ++k)
-      if (k < n) {
-        xv[k] = *(const Words<T, V>*)(vp + (s0 + k) * p.vt);
-        xg[k] = *(const Words<T, V>*)(gp + (s0 + k) * p.gt);
-      }
-    float h[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = kept[(b * nkeep + s0 / kKeep) * p.dim + c + e];
-#pragma unroll
-    for (int k = 0; k < kKeep; ++k)
-      if (k < n) {
+    for (int k = 0; k < kSpan - 1; ++k)
+      if (from + k < order)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          before[k][e] = h[e];
-          h[e] = gated_step(h[e], as_f32(xg[k].v[e]), as_f32(xv[k].v[e]));
+          map[k][e] = __hip_atomic_load(p.maps + (from + k) * channels + at + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          wait |= map[k][e] == ~0ull;
         }
+    if (wait) __builtin_amdgcn_s_sleep(1);
+  } while (wait);
+#pragma unroll
+  for (int e = 0; e < V; ++e) h[e] = span > 0 ? __builtin_bit_cast(float, state[e]) : first[e];
+#pragma unroll
+  for (int k = 0; k < kSpan - 1; ++k)
+    if (from + k < order)
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        h[e] = fmaf(__builtin_bit_cast(float, (uint32_t)map[k][e]), h[e],
+                    __builtin_bit_cast(float, (uint32_t)(map[k][e] >> 32)));
+  if (order % kSpan == kSpan - 1 && order + 1 < p.nchunk) {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      __hip_atomic_store(p.states + span * channels + at + e, published(fmaf(A[e], h[e], Y[e])), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+
+// A workgroup's runs: each wavefront's map, and what enters the chunk.
+template <int V>
+struct GatedRuns {
+  float A[8][V][64], Y[8][V][64];
+};
+
+// The value that enters this wavefront's run.  `run` counts wavefronts along
+// the direction of the recurrence; `carry` holds, in wavefront 0 and on its
+// own, what enters the next chunk.  Called by all wavefronts.
+template <bool LINK, int V>
+__device__ __forceinline__ void gated_enter(const GatedArgs& p, GatedRuns<V>& runs, float (*enter)[64], int run, int nrun,
+                                            int32_t order, int64_t at, bool live, const float* A, const float* Y,
+                                            float* carry, float* h) {
+  const int lane = threadIdx.x % 64;
+#pragma unroll
+  for (int e = 0; e < V; ++e) runs.A[run][e][lane] = A[e], runs.Y[run][e][lane] = Y[e];
+  __syncthreads();
+  if (run == 0) {
+    float cA[V], cY[V];   // the chunk's map
+#pragma unroll
+    for (int e = 0; e < V; ++e) cA[e] = A[e], cY[e] = Y[e];
+    for (int w = 1; w < nrun; ++w)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float a = runs.A[w][e][lane];
+        cA[e] *= a;
+        cY[e] = fmaf(a, cY[e], runs.Y[w][e][lane]);
+      }
+    if (LINK && live) gated_link<V>(p, order, at, cA, cY, carry, carry);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      enter[e][lane] = carry[e];
+      if (!LINK) carry[e] = fmaf(cA[e], carry[e], cY[e]);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < V; ++e) h[e] = enter[e][lane];
+  for (int w = 0; w < run; ++w)
+#pragma unroll
+    for (int e = 0; e < V; ++e) h[e] = fmaf(runs.A[w][e][lane], h[e], runs.Y[w][e][lane]);
+}
+
+template <class T, int V, bool LINK>
+__global__ void __launch_bounds__(512) k_gated(GatedArgs p, const T* v, const T* g, const float* y0, T* y, float* last,
+                                               float* kept) {
+  __shared__ GatedRuns<V> runs[2];
+  __shared__ float enter[V][64];
+  __shared__ uint32_t box;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
+  const GatedPlace place = gated_place<LINK>(p, &box);
+  const int64_t i = place.group * 64 + lane;
+  const bool live = i < p.batch * p.nv;
+  const int64_t b = live ? i / p.nv : 0, c = live ? (i - b * p.nv) * V : 0, at = b * p.dim + c;
+  const int32_t len = live ? row_length(p, b) : 0;
+  const T *vp = v + b * p.vb + c, *gp = g + b * p.gb + c;
+  T* yp = y + b * p.yb + c;
+  const int64_t keeps = (p.steps + kKeep - 1) / kKeep;
+  float carry[V] = {};
+  if (wave == 0 && live && y0)
+#pragma unroll
+    for (int e = 0; e < V; ++e) carry[e] = y0[at + e];
+  for (int32_t k = place.order; k < (LINK ? place.order + 1 : p.nchunk); ++k) {
+    const int64_t s0 = ((int64_t)k * waves + wave) * kKeep;
+    float a[kKeep][V], u[kKeep][V];   // y -> a y + u
+    const bool full = __all(s0 + kKeep <= len);
+    if (full) {
+      Words<T, V> xv[kKeep], xg[kKeep];
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q) {
+        xg[q] = take_once<T, V>(gp + (s0 + q) * p.gt);
+        xv[q] = take_once<T, V>(vp + (s0 + q) * p.vt);
       }
 #pragma unroll
-    for (int k = kKeep - 1; k >= 0; --k)
-      if (k < n) {
-        const Words<T, V> x = *(const Words<T, V>*)(dp + (s0 + k) * p.yt);
+      for (int q = 0; q < kKeep; ++q)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          float r;
+          gate(as_f32(xg[q].v[e]), a[q][e], r);
+          u[q][e] = r * as_f32(xv[q].v[e]);
+        }
+    } else {
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) a[q][e] = 1.0f, u[q][e] = 0.0f;
+        if (s0 + q < len) {
+          const Words<T, V> xg = take_once<T, V>(gp + (s0 + q) * p.gt), xv = take_once<T, V>(vp + (s0 + q) * p.vt);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            float r;
+            gate(as_f32(xg.v[e]), a[q][e], r);
+            u[q][e] = r * as_f32(xv.v[e]);
+          }
+        }
+      }
+    }
+    float A[V], Y[V], h[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      A[e] = a[0][e], Y[e] = u[0][e];
+#pragma unroll
+      for (int q = 1; q < kKeep; ++q) A[e] *= a[q][e], Y[e] = fmaf(a[q][e], Y[e], u[q][e]);
+    }
+    gated_enter<LINK, V>(p, runs[k & 1], enter, wave, waves, k, at, live, A, Y, carry, h);
+    if (live && s0 < p.steps) {
+      if (kept) {
+        Words<float, V> x;
+#pragma unroll
+        for (int e = 0; e < V; ++e) x.v[e] = h[e];
+        put_once(kept + (b * keeps + s0 / kKeep) * p.dim + c, x);
+      }
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q) {
+        Words<T, V> o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          h[e] = fmaf(a[q][e], h[e], u[q][e]);
+          o.v[e] = full || s0 + q < len ? (T)h[e] : (T)0.0f;
+        }
+        if (full || s0 + q < p.steps) put_once(yp + (s0 + q) * p.yt, o);
+      }
+    }
+    // steps past a row's length keep its state, so the last run ends with it
+    if (last && live && k == p.nchunk - 1 && wave == waves - 1)
+#pragma unroll
+      for (int e = 0; e < V; ++e) last[at + e] = h[e];
+  }
+}
+
+// The gradient.  A wavefront's states come from the one that the forward pass
+// left at its first step.
+template <class T, int V, bool LINK>
+__global__ void __launch_bounds__(512) k_gated_grad(GatedArgs p, const T* v, const T* g, const float* kept, const T* dy,
+                                                    const float* dlast, T* dv, T* dg, float* dy0) {
+  __shared__ GatedRuns<V> runs[2];
+  __shared__ float enter[V][64];
+  __shared__ uint32_t box;
+  const int lane = threadIdx.x % 64, waves = blockDim.x / 64;
+  const int run = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave = waves - 1 - run;
+  const GatedPlace place = gated_place<LINK>(p, &box);
+  const int64_t i = place.group * 64 + lane;
+  const bool live = i < p.batch * p.nv;
+  const int64_t b = live ? i / p.nv : 0, c = live ? (i - b * p.nv) * V : 0, at = b * p.dim + c;
+  const int32_t len = live ? row_length(p, b) : 0;
+  const T *vp = v + b * p.vb + c, *gp = g + b * p.gb + c, *dp = dy + b * p.yb + c;
+  T *dvp = dv + b * p.steps * p.dim + c, *dgp = dg + b * p.steps * p.dim + c;
+  const int64_t keeps = (p.steps + kKeep - 1) / kKeep;
+  float carry[V] = {};
+  if (run == 0 && live && dlast)
+#pragma unroll
+    for (int e = 0; e < V; ++e) carry[e] = dlast[at + e];
+  for (int32_t k = place.order; k < (LINK ? place.order + 1 : p.nchunk); ++k) {
+    const int64_t s0 = ((int64_t)(p.nchunk - 1 - k) * waves + wave) * kKeep;
+    const bool some = live && s0 < len, full = __all(s0 + kKeep <= len);
+    float a[kKeep][V], r[kKeep][V], x[kKeep][V], z[kKeep][V];   // z: dy
+    float h[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) h[e] = some ? kept[(b * keeps + s0 / kKeep) * p.dim + c + e] : 0.0f;
+    if (full) {
+      Words<T, V> xv[kKeep], xg[kKeep], xd[kKeep];
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q) {
+        xg[q] = take_once<T, V>(gp + (s0 + q) * p.gt);
+        xv[q] = take_once<T, V>(vp + (s0 + q) * p.vt);
+        xd[q] = take_once<T, V>(dp + (s0 + q) * p.yt);
+      }
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          gate(as_f32(xg[q].v[e]), a[q][e], r[q][e]);
+          x[q][e] = as_f32(xv[q].v[e]);
+          z[q][e] = as_f32(xd[q].v[e]);
+        }
+    } else {
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) a[q][e] = 1.0f, r[q][e] = x[q][e] = z[q][e] = 0.0f;
+        if (s0 + q < len) {
+          const Words<T, V> xg = take_once<T, V>(gp + (s0 + q) * p.gt), xv = take_once<T, V>(vp + (s0 + q) * p.vt),
+                            xd = take_once<T, V>(dp + (s0 + q) * p.yt);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            gate(as_f32(xg.v[e]), a[q][e], r[q][e]);
+            x[q][e] = as_f32(xv.v[e]);
+            z[q][e] = as_f32(xd.v[e]);
+          }
+        }
+      }
+    }
+    // x <- a (1 - a) (y[t-1] - v)
+#pragma unroll
+    for (int q = 0; q < kKeep; ++q)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float before = h[e];
+        h[e] = fmaf(a[q][e], h[e], r[q][e] * x[q][e]);
+        x[q][e] = a[q][e] * r[q][e] * (before - x[q][e]);
+      }
+    float A[V], M[V], m[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      A[e] = a[kKeep - 1][e], M[e] = a[kKeep - 1][e] * z[kKeep - 1][e];
+#pragma unroll
+      for (int q = kKeep - 2; q >= 0; --q) A[e] *= a[q][e], M[e] = a[q][e] * (z[q][e] + M[e]);
+    }
+    gated_enter<LINK, V>(p, runs[k & 1], enter, run, waves, k, at, live, A, M, carry, m);
+    if (live && s0 < p.steps) {
+#pragma unroll
+      for (int q = kKeep - 1; q >= 0; --q) {
         Words<T, V> ov, og;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          float a, r;
-          gate(as_f32(xg[k].v[e]), a, r);
-          const float d = as_f32(x.v[e]) + m[e];
-          ov.v[e] = (T)(r * d);
-          og.v[e] = (T)(a * r * (before[k][e] - as_f32(xv[k].v[e])) * d);
-          m[e] = a * d;
+          const float d = z[q][e] + m[e];
+          ov.v[e] = (T)(r[q][e] * d);
+          og.v[e] = (T)(x[q][e] * d);
+          if (full || s0 + q < len) m[e] = a[q][e] * d;
+          else ov.v[e] = og.v[e] = (T)0.0f;
         }
-        put_once(dvp + (s0 + k) * p.dim, ov);
-        put_once(dgp + (s0 + k) * p.dim, og);
+        if (full || s0 + q < p.steps) {
+          put_once(dvp + (s0 + q) * p.dim, ov);
+          put_once(dgp + (s0 + q) * p.dim, og);
+        }
       }
-  }
-  if (dy0 && t0 == 0) {
+    }
+    if (dy0 && live && k == p.nchunk - 1 && run == waves - 1)
 #pragma unroll
-    for (int e = 0; e < V; ++e) dy0[b * p.dim + c + e] = m[e];
+      for (int e = 0; e < V; ++e) dy0[at + e] = m[e];
   }
 }
 

@@ -214,24 +214,57 @@ Gated check_gated(const ms_gated_lowpass_desc* d) {
   stride_pair(d->v_stride, d->steps, d->dim, a.vb, a.vt);
   stride_pair(d->g_stride, d->steps, d->dim, a.gb, a.gt);
   stride_pair(d->y_stride, d->steps, d->dim, a.yb, a.yt);
-  // Enough chunks that a few channels fill the device, none so short that
-  // joining them costs more than going through it.
-  const int64_t channels = std::max<int64_t>(d->batch * d->dim, 1);
-  const int64_t want = std::max<int64_t>(1, ((int64_t)1 << 19) / channels);
-  int64_t chunk = std::max<int64_t>(up((d->steps + want - 1) / want, kKeep), 64);
-  chunk = std::max(chunk, up((d->steps + 65534) / 65535, kKeep));
-  a.chunk = (int32_t)std::min<int64_t>(chunk, (int64_t)1 << 30);
-  a.nchunk = (int32_t)((d->steps + a.chunk - 1) / a.chunk);
   g.keeps = (d->steps + kKeep - 1) / kKeep;
   return g;
 }
 
-int64_t gated_work(const Gated& g) {
-  return g.a.nchunk > 1 ? up(g.a.batch * g.a.nchunk * 2 * g.a.dim * 4, 256) : 0;
+constexpr int kGatedWaves = 8;   // of a workgroup, at most
+
+// Scratch memory of chunks that run side by side: their maps and states, the
+// ticket.
+struct GatedWork {
+  uint64_t* maps;
+  uint32_t *states, *ticket;
+  int64_t bytes;
+};
+
+GatedWork gated_work(const Gated& g, void* ws) {
+  const int64_t channels = g.a.batch * g.a.dim, chunks = (g.keeps + kGatedWaves - 1) / kGatedWaves;
+  Carve c{(char*)ws};
+  GatedWork w{};
+  if (chunks > 1) {
+    w.maps = c.take<uint64_t>(chunks * channels);
+    w.states = c.take<uint32_t>(chunks / kSpan * channels);
+    w.ticket = c.take<uint32_t>(1);
+  }
+  w.bytes = c.used;
+  return w;
 }
 
-dim3 gated_grid(const GatedArgs& a) {
-  return dim3((unsigned)((a.batch * a.nv + 255) / 256), (unsigned)a.nchunk);
+// Threads of a workgroup, and whether chunks run side by side.  A workgroup
+// that goes through chunks one after the other takes about 2.5 us for each, and
+// needs a second one on its CU to keep memory busy; linked chunks cost a launch
+// that clears what they publish, and their waits.
+struct GatedShape {
+  unsigned threads;
+  bool link;
+};
+
+GatedShape gated_shape(Gated& g) {
+  GatedArgs& a = g.a;
+  int waves = 1;
+  while (waves < kGatedWaves && waves < g.keeps) waves *= 2;
+  a.nchunk = (int32_t)((g.keeps + waves - 1) / waves);
+  a.groups = (int32_t)((a.batch * a.nv + 63) / 64);
+  const bool link = a.nchunk > 4 && a.groups < 1024 && (int64_t)a.nchunk * a.groups < ((int64_t)1 << 22);
+  return {(unsigned)waves * 64, link};
+}
+
+void gated_clear(GatedArgs& a, const GatedWork& w, hipStream_t st) {
+  a.maps = w.maps, a.states = w.states, a.ticket = w.ticket;
+  const int64_t words = ((char*)w.ticket - (char*)w.maps) / 4;
+  hipLaunchKernelGGL(k_gated_clear, dim3((unsigned)std::min<int64_t>((words + 255) / 256, 2048)), dim3(256), 0, st,
+                     (uint32_t*)w.maps, words, w.ticket);
 }
 
 // ------------------------------------------------------------------- orth
@@ -467,7 +500,7 @@ ms_status ms_gated_lowpass_workspace(const ms_gated_lowpass_desc* d, int64_t* by
   return guarded([&] {
     const Gated g = check_gated(d);
     need(bytes_out != nullptr, "NULL output");
-    *bytes_out = gated_work(g);
+    *bytes_out = gated_work(g, nullptr).bytes;
   });
 }
 
@@ -485,7 +518,8 @@ ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* d, const void* v, const 
     for (const void* q : {v, g, (const void*)y}) need_aligned(q, es, "v, g or y");
     for (const void* q : {(const void*)y0, (const void*)lengths, (const void*)last, (const void*)kept})
       need_aligned(q, 4, "y0, lengths, last or kept");
-    if (a.steps > 0) need_workspace(workspace, workspace_bytes, gated_work(p));
+    const GatedWork work = gated_work(p, workspace);
+    if (a.steps > 0) need_workspace(workspace, workspace_bytes, work.bytes);
     DeviceGuard dg(d->device);
     const hipStream_t st = (hipStream_t)d->stream;
     if (a.steps == 0) {
@@ -496,18 +530,20 @@ ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* d, const void* v, const 
       return;
     }
     a.lengths = lengths;
-    const int64_t w = std::min<int64_t>(4, Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es)
-                                               .at(g, es).at(y, es).v);
+    Wide wide = Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es).at(g, es).at(y, es);
+    const int64_t w = std::min<int64_t>(2, wide.at(kept, 4).v);
     a.nv = a.dim / w;
-    float* join = (float*)workspace;
-    with_type<4>(d->dtype, w, [&](auto zero, auto width) {
+    const GatedShape shape = gated_shape(p);
+    if (shape.link) gated_clear(a, work, st);
+    with_type<2>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
-      if (a.nchunk > 1)
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_part<T, V>), gated_grid(a), dim3(256), 0, st, a, (const T*)v,
-                           (const T*)g, join);
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated<T, V>), gated_grid(a), dim3(256), 0, st, a, (const T*)v, (const T*)g, y0,
-                         (const float*)join, (T*)y, last, kept);
+      if (shape.link)
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated<T, V, true>), dim3((unsigned)(a.nchunk * a.groups)), dim3(shape.threads),
+                           0, st, a, (const T*)v, (const T*)g, y0, (T*)y, last, kept);
+      else
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated<T, V, false>), dim3((unsigned)a.groups), dim3(shape.threads), 0, st, a,
+                           (const T*)v, (const T*)g, y0, (T*)y, last, kept);
     });
     HIPCHECK(hipGetLastError());
   });
@@ -525,7 +561,8 @@ ms_status ms_gated_lowpass_grad(const ms_gated_lowpass_desc* d, const void* v, c
     for (const void* q : {v, g, dy, (const void*)dv, (const void*)dg}) need_aligned(q, es, "v, g, dy, dv or dg");
     for (const void* q : {(const void*)kept, (const void*)lengths, (const void*)dlast, (const void*)dy0})
       need_aligned(q, 4, "kept, lengths, dlast or dy0");
-    if (a.steps > 0) need_workspace(workspace, workspace_bytes, gated_work(p));
+    const GatedWork work = gated_work(p, workspace);
+    if (a.steps > 0) need_workspace(workspace, workspace_bytes, work.bytes);
     DeviceGuard guard(d->device);
     const hipStream_t st = (hipStream_t)d->stream;
     if (a.steps == 0) {
@@ -539,15 +576,18 @@ ms_status ms_gated_lowpass_grad(const ms_gated_lowpass_desc* d, const void* v, c
     const int64_t w = std::min<int64_t>(2, Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es)
                                                .at(g, es).at(dy, es).at(dv, es).at(dg, es).v);
     a.nv = a.dim / w;
-    float* join = (float*)workspace;
+    const GatedShape shape = gated_shape(p);
+    if (shape.link) gated_clear(a, work, st);
     with_type<2>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
-      if (a.nchunk > 1)
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad_part<T, V>), gated_grid(a), dim3(256), 0, st, a, (const T*)g,
-                           (const T*)dy, join);
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad<T, V>), gated_grid(a), dim3(256), 0, st, a, (const T*)v,
-                         (const T*)g, kept, (const T*)dy, dlast, (const float*)join, (T*)dv, (T*)dg, dy0);
+      if (shape.link)
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad<T, V, true>), dim3((unsigned)(a.nchunk * a.groups)),
+                           dim3(shape.threads), 0, st, a, (const T*)v, (const T*)g, kept, (const T*)dy, dlast, (T*)dv, (T*)dg,
+                           dy0);
+      else
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad<T, V, false>), dim3((unsigned)a.groups), dim3(shape.threads), 0, st, a,
+                           (const T*)v, (const T*)g, kept, (const T*)dy, dlast, (T*)dv, (T*)dg, dy0);
     });
     HIPCHECK(hipGetLastError());
   });

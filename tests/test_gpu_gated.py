@@ -299,3 +299,36 @@ def test_another_stream_and_a_graph():
             assert torch.equal(x, want[name] * (1.0 if name == "dg" else sign)), name
         for x in (v, y0, dy, dlast):
             x.mul_(-1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("b,t,d", [(2, 3000, 130), (1, 2113, 257), (70, 600, 31), (40, 1700, 1024)])
+def test_many_chunks(b, t, d, dtype):
+    """Chunks side by side over several spans, and one after the other in many workgroups."""
+    v, g, y0, lengths, dy, dlast = inputs(b, t, d, dtype, 14, True, True)
+    want = reference(v, g, y0, lengths, dy, dlast)
+    got = both_passes(v, g, y0, lengths, dy, dlast)
+    for name, x in got.items():
+        check(x, want[name], name)
+    again = both_passes(v, g, y0, lengths, dy, dlast)
+    assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_any_nan_travels_between_chunks(dtype):
+    """NaN of every bit pattern in the inputs, all ones among them."""
+    b, t, d = 1, 3000, 8
+    v, g, y0, _, dy, dlast = inputs(b, t, d, dtype, 15)
+    raw = torch.int32 if dtype == F32 else torch.int16
+    v.view(raw)[0, 200, 1] = -1
+    g.view(raw)[0, 200, 2] = -1
+    y0.view(torch.int32)[0, 3] = -1
+    dy.view(raw)[0, 2500, 4] = -1
+    dlast.view(torch.int32)[0, 5] = -1
+    y, last, kept = M.gated_lowpass(v, g, y0=y0, keep=True)
+    bad = torch.isnan(y[0])
+    assert bad[200:, 1].all() and bad[200:, 2].all() and bad[:, 3].all() and not bad[:200, 1:3].any()
+    assert not bad[:, [0, 4, 5, 6, 7]].any() and torch.isnan(last[0]).tolist() == [False] + [True] * 3 + [False] * 4
+    dv, dg, dy0 = M.gated_lowpass_grad(v, g, kept, dy, dlast=dlast)
+    assert torch.isnan(dv[0, :2501, 4]).all() and not torch.isnan(dv[0, 2501:, 4]).any() and torch.isnan(dv[0, :, 5]).all()
+    assert torch.isnan(dy0[0, 2]) and torch.isnan(dy0[0, 4]) and torch.isnan(dy0[0, 5]) and not torch.isnan(dy0[0, 6])
