@@ -7,17 +7,25 @@
 // before it, with d[t] = dy[t] + m[t+1], so a run maps m -> A m + M.
 //
 // Memory bounds it: each array has to be read or written once, a step costs
-// two transcendental instructions and about ten others for its 3 (gradient: 5)
-// values.  So every value is read once and stays in registers until its result
-// is known.  A wavefront takes kKeep = 16 steps of 64 V channels, fetched
-// together; its lanes know their runs' maps, and the wavefronts of a workgroup,
-// which hold consecutive runs, join them in LDS.  Sequences longer than a
-// workgroup's 128 steps are cut into such chunks.  With enough channels, or a
-// few chunks, a workgroup goes through its chunks one after the other (LINK =
-// false).  Otherwise the chunks run side by side (LINK): each leaves its map
-// for the later ones, and every kSpan-th the state that it ends with; a chunk
-// waits for the state at its span's beginning and the maps in between.  The
-// order of these operations is fixed, so the result does not depend on timing.
+// two transcendental instructions and about fifteen others for its 3 (gradient:
+// 5) values.  So every value is read once and stays in registers until its
+// result is known.  A wavefront takes kKeep = 16 steps of 64 V channels,
+// fetched together; its lanes find their runs' maps, and the wavefronts of a
+// workgroup, which hold consecutive runs, join them in LDS.  Sequences longer
+// than a workgroup's 128 steps are cut into such chunks.  With enough channels,
+// or a few chunks, a workgroup goes through its chunks one after the other
+// (LINK = false).  Otherwise the chunks run side by side (LINK): each publishes
+// its map for the later ones, and every kSpan-th the state that it ends with;
+// a chunk waits for the state at its span's beginning and the maps in between,
+// a wavefront for each.  The order of the operations is fixed, so the result
+// does not depend on timing.
+//
+// Measured at 4 x 16384 x 2048 bf16 (0.81 GB): 445 us in two passes (maps, then
+// steps: v and g are read twice), 190 us in one, with the first wavefront
+// waiting for all maps, 163 us with a wavefront for each, 149 us without any
+// waiting (wrong results), 146 us without the exponentials too.  Chunks of 64
+// steps take 235 us, of 256 steps 193; one channel per lane 229.  A third
+// workgroup on each CU (gates kept as one number) does not help: 171.
 #pragma once
 
 #include "kernels_embed.hpp"
@@ -25,15 +33,17 @@
 // Steps of a wavefront, and between the states that the forward pass leaves for
 // the gradient, which computes the states between them again.
 constexpr int kKeep = 16;
-constexpr int kSpan = 8;   // chunks from one published state to the next
+constexpr int kGatedWaves = 8;   // of a workgroup, at most
+constexpr int kSpan = 8;         // chunks from one published state to the next
 
-// A lane takes V neighbouring channels of one batch row: lane i of all is row
-// i / nv and channels (i % nv) V .. + V.
+// A lane takes V neighbouring channels of one batch row, V channels wide words
+// of at most 4 bytes.
 struct GatedArgs {
   int64_t batch, steps, dim, nv;    // nv = dim / V
   int64_t vb, vt, gb, gt, yb, yt;   // strides of v, g and y (dy in the gradient)
   const int32_t* lengths;
   int32_t nchunk, groups;           // chunks of blockDim / 64 * kKeep steps; workgroups per chunk
+  int32_t per_row;                  // workgroups per batch row (SPAN = false)
   // LINK: what chunks leave for each other, all ones before the launch
   uint64_t* maps;                   // [nchunk][batch * dim]: (A, Y)
   uint32_t* states;                 // [nchunk / kSpan][batch * dim]
@@ -51,6 +61,46 @@ __device__ __forceinline__ void gate(float g, float& a, float& rest) {
   const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
   a = g >= 0.0f ? big : small;
   rest = g >= 0.0f ? small : big;
+}
+
+// Both gates in one number: the smaller, negative where it is a.
+__device__ __forceinline__ float gate_packed(float g) {
+  const float e = __expf(-fabsf(g));
+  const float small = e * __builtin_amdgcn_rcpf(1.0f + e);
+  return g >= 0.0f ? small : -small;   // -0 at g = -inf
+}
+
+__device__ __forceinline__ void gate_of(float s, float& a, float& rest) {
+  const float small = fabsf(s), big = 1.0f - small;
+  const bool rest_small = !__builtin_signbit(s);
+  a = rest_small ? big : small;
+  rest = rest_small ? small : big;
+}
+
+// What follows from x is computed anew after this, not kept in registers.
+// Keeps the instructions of every fourth step apart, so that values of all
+// steps are not wanted at once.
+__device__ __forceinline__ void step_apart(int q) {
+  if (q % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+}
+
+template <class X>
+__device__ __forceinline__ void again(X& x) {
+  asm volatile("" : "+v"(x));
+}
+
+// A lane's V values of one step, as they come from memory, in one register.
+template <class T, int V>
+__device__ __forceinline__ uint32_t take_raw(const T* p) {
+  static_assert(sizeof(T) * V <= 4, "one register");
+  if constexpr (sizeof(T) * V == 4) return __builtin_nontemporal_load((const uint32_t*)p);
+  else return __builtin_bit_cast(uint16_t, *p);
+}
+
+template <class T>
+__device__ __forceinline__ float raw_value(uint32_t w, int e) {
+  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w);
+  else return __builtin_bit_cast(float, e ? w & 0xffff0000u : w << 16);
 }
 
 // One step of the filter.
@@ -97,79 +147,90 @@ __device__ __forceinline__ GatedPlace gated_place(const GatedArgs& p, uint32_t* 
   return {(int32_t)(t / (uint32_t)p.groups), (int64_t)(t % (uint32_t)p.groups)};
 }
 
-// The value that enters chunk number `order` for the channels at `at`: `first`
-// at the beginning, else from what earlier chunks published.  A, Y: the chunk's
-// own map.  Every word is one atomic access of its own, so a word that is there
-// is whole; a chunk's words need no order among themselves.
-template <int V>
-__device__ __forceinline__ void gated_link(const GatedArgs& p, int32_t order, int64_t at, const float* A, const float* Y,
-                                           const float* first, float* h) {
-  const int64_t channels = p.batch * p.dim;
-  const int32_t span = order / kSpan, from = span * kSpan;
-  if (order + 1 < p.nchunk) {
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      __hip_atomic_store(p.maps + order * channels + at + e, (uint64_t)published(Y[e]) << 32 | published(A[e]),
-                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// The channels of a lane.  SPAN: lanes are dealt to all rows' channels in
+// order, for rows that would leave many of a wavefront's idle.  Otherwise a
+// wavefront stays in one row: its addresses are a uniform part and one offset
+// per lane, which saves two thirds of the gradient's registers.
+struct GatedLane {
+  bool live;
+  int64_t b;
+  uint32_t c;
+  int32_t len;
+};
+
+template <bool SPAN, int V>
+__device__ __forceinline__ GatedLane gated_lane(const GatedArgs& p, int64_t group) {
+  const int lane = threadIdx.x % 64;
+  GatedLane l;
+  if constexpr (SPAN) {
+    const int64_t i = group * 64 + lane;
+    l.live = i < p.batch * p.nv;
+    l.b = l.live ? i / p.nv : 0;
+    l.c = l.live ? (uint32_t)(i - l.b * p.nv) * V : 0;
+    l.len = l.live ? row_length(p, l.b) : 0;
+  } else {
+    const uint32_t row = __builtin_amdgcn_readfirstlane((uint32_t)group / (uint32_t)p.per_row);
+    const int32_t i = (int32_t)((uint32_t)group - row * (uint32_t)p.per_row) * 64 + lane;
+    l.b = row;
+    l.live = i < p.nv;
+    l.c = l.live ? (uint32_t)i * V : 0;
+    l.len = __builtin_amdgcn_readfirstlane(row_length(p, l.b));
   }
-  uint64_t map[kSpan - 1][V];
-  uint32_t state[V];
+  return l;
+}
+
+// What a workgroup's wavefronts tell each other: the maps of their runs, the
+// value that enters the chunk or its span, and the maps of the span's earlier
+// chunks.
+template <int V>
+struct GatedRuns {
+  float A[kGatedWaves][V][64], Y[kGatedWaves][V][64];
+};
+
+template <bool LINK, int V>
+struct GatedShared {
+  GatedRuns<V> runs[2];   // LINK: this chunk's, and the span's earlier ones; else one for every other chunk
+  float enter[V][64];
+};
+
+__device__ __forceinline__ uint32_t link_load(const uint32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t link_load(const uint64_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Waits for V published words.
+template <int V, class W>
+__device__ __forceinline__ void link_wait(const W* p, W* w) {
   bool wait;
   do {
     wait = false;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      state[e] = 0;
-      if (span > 0)
-        state[e] = __hip_atomic_load(p.states + (span - 1) * channels + at + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      wait |= state[e] == ~0u;
+      w[e] = link_load(p + e);
+      wait |= w[e] == (W)~(W)0;
     }
-#pragma unroll
-    for (int k = 0; k < kSpan - 1; ++k)
-      if (from + k < order)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          map[k][e] = __hip_atomic_load(p.maps + (from + k) * channels + at + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          wait |= map[k][e] == ~0ull;
-        }
-    if (wait) __builtin_amdgcn_s_sleep(1);
   } while (wait);
-#pragma unroll
-  for (int e = 0; e < V; ++e) h[e] = span > 0 ? __builtin_bit_cast(float, state[e]) : first[e];
-#pragma unroll
-  for (int k = 0; k < kSpan - 1; ++k)
-    if (from + k < order)
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        h[e] = fmaf(__builtin_bit_cast(float, (uint32_t)map[k][e]), h[e],
-                    __builtin_bit_cast(float, (uint32_t)(map[k][e] >> 32)));
-  if (order % kSpan == kSpan - 1 && order + 1 < p.nchunk) {
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      __hip_atomic_store(p.states + span * channels + at + e, published(fmaf(A[e], h[e], Y[e])), __ATOMIC_RELAXED,
-                         __HIP_MEMORY_SCOPE_AGENT);
-  }
 }
 
-// A workgroup's runs: each wavefront's map, and what enters the chunk.
-template <int V>
-struct GatedRuns {
-  float A[8][V][64], Y[8][V][64];
-};
-
-// The value that enters this wavefront's run.  `run` counts wavefronts along
-// the direction of the recurrence; `carry` holds, in wavefront 0 and on its
-// own, what enters the next chunk.  Called by all wavefronts.
+// The value that enters this wavefront's run.  `run` counts wavefronts, and
+// `order` chunks, along the direction of the recurrence; `carry` holds, in
+// wavefront 0, what enters the first chunk, and with LINK = false then the next
+// one.  Called by all wavefronts.  Published words are atomic accesses of their
+// own, so a word that is there is whole; they need no order among themselves.
 template <bool LINK, int V>
-__device__ __forceinline__ void gated_enter(const GatedArgs& p, GatedRuns<V>& runs, float (*enter)[64], int run, int nrun,
-                                            int32_t order, int64_t at, bool live, const float* A, const float* Y,
-                                            float* carry, float* h) {
+__device__ __forceinline__ void gated_enter(const GatedArgs& p, GatedShared<LINK, V>& sh, int run, int nrun, int32_t order,
+                                            int64_t at, bool live, const float* A, const float* Y, float* carry, float* h) {
   const int lane = threadIdx.x % 64;
+  GatedRuns<V>& runs = sh.runs[LINK ? 0 : order & 1];
 #pragma unroll
   for (int e = 0; e < V; ++e) runs.A[run][e][lane] = A[e], runs.Y[run][e][lane] = Y[e];
   __syncthreads();
+  const int64_t channels = p.batch * p.dim;
+  const int32_t span = order / kSpan, from = span * kSpan;
+  float cA[V], cY[V];   // the chunk's map, in wavefront 0
   if (run == 0) {
-    float cA[V], cY[V];   // the chunk's map
 #pragma unroll
     for (int e = 0; e < V; ++e) cA[e] = A[e], cY[e] = Y[e];
     for (int w = 1; w < nrun; ++w)
@@ -179,35 +240,65 @@ __device__ __forceinline__ void gated_enter(const GatedArgs& p, GatedRuns<V>& ru
         cA[e] *= a;
         cY[e] = fmaf(a, cY[e], runs.Y[w][e][lane]);
       }
-    if (LINK && live) gated_link<V>(p, order, at, cA, cY, carry, carry);
+    if (LINK && live && order + 1 < p.nchunk)
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      enter[e][lane] = carry[e];
-      if (!LINK) carry[e] = fmaf(cA[e], carry[e], cY[e]);
+      for (int e = 0; e < V; ++e)
+        __hip_atomic_store(p.maps + order * channels + at + e, (uint64_t)published(cY[e]) << 32 | published(cA[e]),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!LINK || span == 0)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        sh.enter[e][lane] = carry[e];
+        if (!LINK) carry[e] = fmaf(cA[e], carry[e], cY[e]);
+      }
+  }
+  if constexpr (LINK) {   // eight wavefronts: one for each earlier map of the span, the last one for its state
+    static_assert(kSpan == kGatedWaves, "a wavefront each");
+    if (run < kSpan - 1 && from + run < order) {
+      uint64_t w[V] = {};
+      if (live) link_wait<V>(p.maps + (from + run) * channels + at, w);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        sh.runs[1].A[run][e][lane] = __builtin_bit_cast(float, (uint32_t)w[e]);
+        sh.runs[1].Y[run][e][lane] = __builtin_bit_cast(float, (uint32_t)(w[e] >> 32));
+      }
+    }
+    if (run == kSpan - 1 && span > 0) {
+      uint32_t w[V] = {};
+      if (live) link_wait<V>(p.states + (span - 1) * channels + at, w);
+#pragma unroll
+      for (int e = 0; e < V; ++e) sh.enter[e][lane] = __builtin_bit_cast(float, w[e]);
     }
   }
   __syncthreads();
 #pragma unroll
-  for (int e = 0; e < V; ++e) h[e] = enter[e][lane];
+  for (int e = 0; e < V; ++e) h[e] = sh.enter[e][lane];
+  if constexpr (LINK) {
+    for (int k = 0; from + k < order; ++k)
+#pragma unroll
+      for (int e = 0; e < V; ++e) h[e] = fmaf(sh.runs[1].A[k][e][lane], h[e], sh.runs[1].Y[k][e][lane]);
+    if (run == 0 && live && order % kSpan == kSpan - 1 && order + 1 < p.nchunk)
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        __hip_atomic_store(p.states + span * channels + at + e, published(fmaf(cA[e], h[e], cY[e])), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+  }
   for (int w = 0; w < run; ++w)
 #pragma unroll
     for (int e = 0; e < V; ++e) h[e] = fmaf(runs.A[w][e][lane], h[e], runs.Y[w][e][lane]);
 }
 
-template <class T, int V, bool LINK>
-__global__ void __launch_bounds__(512) k_gated(GatedArgs p, const T* v, const T* g, const float* y0, T* y, float* last,
+template <class T, int V, bool LINK, bool SPAN>
+__global__ void __launch_bounds__(64 * kGatedWaves) k_gated(GatedArgs p, const T* v, const T* g, const float* y0, T* y, float* last,
                                                float* kept) {
-  __shared__ GatedRuns<V> runs[2];
-  __shared__ float enter[V][64];
+  __shared__ GatedShared<LINK, V> shared;
   __shared__ uint32_t box;
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
   const GatedPlace place = gated_place<LINK>(p, &box);
-  const int64_t i = place.group * 64 + lane;
-  const bool live = i < p.batch * p.nv;
-  const int64_t b = live ? i / p.nv : 0, c = live ? (i - b * p.nv) * V : 0, at = b * p.dim + c;
-  const int32_t len = live ? row_length(p, b) : 0;
-  const T *vp = v + b * p.vb + c, *gp = g + b * p.gb + c;
-  T* yp = y + b * p.yb + c;
+  const auto [live, b, c, len] = gated_lane<SPAN, V>(p, place.group);
+  const int64_t at = b * p.dim + c, end = max(len, 1) - 1;   // steps past `end` are read there, and not used
+  const T *vp = v + b * p.vb, *gp = g + b * p.gb;
+  T* yp = y + b * p.yb;
   const int64_t keeps = (p.steps + kKeep - 1) / kKeep;
   float carry[V] = {};
   if (wave == 0 && live && y0)
@@ -216,37 +307,30 @@ __global__ void __launch_bounds__(512) k_gated(GatedArgs p, const T* v, const T*
   for (int32_t k = place.order; k < (LINK ? place.order + 1 : p.nchunk); ++k) {
     const int64_t s0 = ((int64_t)k * waves + wave) * kKeep;
     float a[kKeep][V], u[kKeep][V];   // y -> a y + u
-    const bool full = __all(s0 + kKeep <= len);
-    if (full) {
-      Words<T, V> xv[kKeep], xg[kKeep];
+    const bool full = SPAN ? __all(s0 + kKeep <= len) : s0 + kKeep <= len;
+    {
+      uint32_t xv[kKeep], xg[kKeep];
 #pragma unroll
       for (int q = 0; q < kKeep; ++q) {
-        xg[q] = take_once<T, V>(gp + (s0 + q) * p.gt);
-        xv[q] = take_once<T, V>(vp + (s0 + q) * p.vt);
+        const int64_t s = full ? s0 + q : min(s0 + q, end);
+        xg[q] = take_raw<T, V>(gp + s * p.gt + c);
+        xv[q] = take_raw<T, V>(vp + s * p.vt + c);
       }
 #pragma unroll
       for (int q = 0; q < kKeep; ++q)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           float r;
-          gate(as_f32(xg[q].v[e]), a[q][e], r);
-          u[q][e] = r * as_f32(xv[q].v[e]);
+          gate(raw_value<T>(xg[q], e), a[q][e], r);
+          u[q][e] = r * raw_value<T>(xv[q], e);
         }
-    } else {
+    }
+    if (!full) {
 #pragma unroll
-      for (int q = 0; q < kKeep; ++q) {
+      for (int q = 0; q < kKeep; ++q)
+        if (s0 + q >= len)
 #pragma unroll
-        for (int e = 0; e < V; ++e) a[q][e] = 1.0f, u[q][e] = 0.0f;
-        if (s0 + q < len) {
-          const Words<T, V> xg = take_once<T, V>(gp + (s0 + q) * p.gt), xv = take_once<T, V>(vp + (s0 + q) * p.vt);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float r;
-            gate(as_f32(xg.v[e]), a[q][e], r);
-            u[q][e] = r * as_f32(xv.v[e]);
-          }
-        }
-      }
+          for (int e = 0; e < V; ++e) a[q][e] = 1.0f, u[q][e] = 0.0f;
     }
     float A[V], Y[V], h[V];
 #pragma unroll
@@ -255,7 +339,7 @@ __global__ void __launch_bounds__(512) k_gated(GatedArgs p, const T* v, const T*
 #pragma unroll
       for (int q = 1; q < kKeep; ++q) A[e] *= a[q][e], Y[e] = fmaf(a[q][e], Y[e], u[q][e]);
     }
-    gated_enter<LINK, V>(p, runs[k & 1], enter, wave, waves, k, at, live, A, Y, carry, h);
+    gated_enter<LINK, V>(p, shared, wave, waves, k, at, live, A, Y, carry, h);
     if (live && s0 < p.steps) {
       if (kept) {
         Words<float, V> x;
@@ -271,7 +355,7 @@ __global__ void __launch_bounds__(512) k_gated(GatedArgs p, const T* v, const T*
           h[e] = fmaf(a[q][e], h[e], u[q][e]);
           o.v[e] = full || s0 + q < len ? (T)h[e] : (T)0.0f;
         }
-        if (full || s0 + q < p.steps) put_once(yp + (s0 + q) * p.yt, o);
+        if (full || s0 + q < p.steps) put_once(yp + (s0 + q) * p.yt + c, o);
       }
     }
     // steps past a row's length keep its state, so the last run ends with it
@@ -283,21 +367,18 @@ __global__ void __launch_bounds__(512) k_gated(GatedArgs p, const T* v, const T*
 
 // The gradient.  A wavefront's states come from the one that the forward pass
 // left at its first step.
-template <class T, int V, bool LINK>
-__global__ void __launch_bounds__(512) k_gated_grad(GatedArgs p, const T* v, const T* g, const float* kept, const T* dy,
+template <class T, int V, bool LINK, bool SPAN>
+__global__ void __launch_bounds__(64 * kGatedWaves) k_gated_grad(GatedArgs p, const T* v, const T* g, const float* kept, const T* dy,
                                                     const float* dlast, T* dv, T* dg, float* dy0) {
-  __shared__ GatedRuns<V> runs[2];
-  __shared__ float enter[V][64];
+  __shared__ GatedShared<LINK, V> shared;
   __shared__ uint32_t box;
-  const int lane = threadIdx.x % 64, waves = blockDim.x / 64;
+  const int waves = blockDim.x / 64;
   const int run = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave = waves - 1 - run;
   const GatedPlace place = gated_place<LINK>(p, &box);
-  const int64_t i = place.group * 64 + lane;
-  const bool live = i < p.batch * p.nv;
-  const int64_t b = live ? i / p.nv : 0, c = live ? (i - b * p.nv) * V : 0, at = b * p.dim + c;
-  const int32_t len = live ? row_length(p, b) : 0;
-  const T *vp = v + b * p.vb + c, *gp = g + b * p.gb + c, *dp = dy + b * p.yb + c;
-  T *dvp = dv + b * p.steps * p.dim + c, *dgp = dg + b * p.steps * p.dim + c;
+  const auto [live, b, c, len] = gated_lane<SPAN, V>(p, place.group);
+  const int64_t at = b * p.dim + c, end = max(len, 1) - 1;   // steps past `end` are read there, and not used
+  const T *vp = v + b * p.vb, *gp = g + b * p.gb, *dp = dy + b * p.yb;
+  T *dvp = dv + b * p.steps * p.dim, *dgp = dg + b * p.steps * p.dim;
   const int64_t keeps = (p.steps + kKeep - 1) / kKeep;
   float carry[V] = {};
   if (run == 0 && live && dlast)
@@ -305,77 +386,87 @@ __global__ void __launch_bounds__(512) k_gated_grad(GatedArgs p, const T* v, con
     for (int e = 0; e < V; ++e) carry[e] = dlast[at + e];
   for (int32_t k = place.order; k < (LINK ? place.order + 1 : p.nchunk); ++k) {
     const int64_t s0 = ((int64_t)(p.nchunk - 1 - k) * waves + wave) * kKeep;
-    const bool some = live && s0 < len, full = __all(s0 + kKeep <= len);
-    float a[kKeep][V], r[kKeep][V], x[kKeep][V], z[kKeep][V];   // z: dy
+    const bool some = live && s0 < len, full = SPAN ? __all(s0 + kKeep <= len) : s0 + kKeep <= len;
+    float s[kKeep][V], x[kKeep][V];   // the gates in one; a (1 - a) (y[t-1] - v)
+    uint32_t z[kKeep];                // dy
     float h[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) h[e] = some ? kept[(b * keeps + s0 / kKeep) * p.dim + c + e] : 0.0f;
-    if (full) {
-      Words<T, V> xv[kKeep], xg[kKeep], xd[kKeep];
+    {
+      uint32_t xv[kKeep], xg[kKeep];
 #pragma unroll
       for (int q = 0; q < kKeep; ++q) {
-        xg[q] = take_once<T, V>(gp + (s0 + q) * p.gt);
-        xv[q] = take_once<T, V>(vp + (s0 + q) * p.vt);
-        xd[q] = take_once<T, V>(dp + (s0 + q) * p.yt);
+        const int64_t st = full ? s0 + q : min(s0 + q, end);
+        xg[q] = take_raw<T, V>(gp + st * p.gt + c);
+        xv[q] = take_raw<T, V>(vp + st * p.vt + c);
+        z[q] = take_raw<T, V>(dp + st * p.yt + c);
       }
 #pragma unroll
       for (int q = 0; q < kKeep; ++q)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          gate(as_f32(xg[q].v[e]), a[q][e], r[q][e]);
-          x[q][e] = as_f32(xv[q].v[e]);
-          z[q][e] = as_f32(xd[q].v[e]);
+          s[q][e] = gate_packed(raw_value<T>(xg[q], e));
+          x[q][e] = raw_value<T>(xv[q], e);
+          if (e == V - 1) step_apart(q);
         }
-    } else {
-#pragma unroll
-      for (int q = 0; q < kKeep; ++q) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) a[q][e] = 1.0f, r[q][e] = x[q][e] = z[q][e] = 0.0f;
-        if (s0 + q < len) {
-          const Words<T, V> xg = take_once<T, V>(gp + (s0 + q) * p.gt), xv = take_once<T, V>(vp + (s0 + q) * p.vt),
-                            xd = take_once<T, V>(dp + (s0 + q) * p.yt);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            gate(as_f32(xg.v[e]), a[q][e], r[q][e]);
-            x[q][e] = as_f32(xv.v[e]);
-            z[q][e] = as_f32(xd.v[e]);
-          }
-        }
-      }
     }
-    // x <- a (1 - a) (y[t-1] - v)
+    if (!full) {   // a = 1 and nothing else
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q)
+        if (s0 + q >= len)
+#pragma unroll
+          for (int e = 0; e < V; ++e) s[q][e] = x[q][e] = 0.0f, z[q] = 0;
+    }
 #pragma unroll
     for (int q = 0; q < kKeep; ++q)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
+        float a, r;
+        gate_of(s[q][e], a, r);
         const float before = h[e];
-        h[e] = fmaf(a[q][e], h[e], r[q][e] * x[q][e]);
-        x[q][e] = a[q][e] * r[q][e] * (before - x[q][e]);
+        h[e] = fmaf(a, h[e], r * x[q][e]);
+        x[q][e] = a * r * (before - x[q][e]);
+        again(x[q][e]);   // and is computed here, not where it is used
+        if (e == V - 1) step_apart(q);
       }
     float A[V], M[V], m[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      A[e] = a[kKeep - 1][e], M[e] = a[kKeep - 1][e] * z[kKeep - 1][e];
+    for (int e = 0; e < V; ++e) A[e] = 1.0f, M[e] = 0.0f;
 #pragma unroll
-      for (int q = kKeep - 2; q >= 0; --q) A[e] *= a[q][e], M[e] = a[q][e] * (z[q][e] + M[e]);
+    for (int q = kKeep - 1; q >= 0; --q) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float a, r;
+        again(s[q][e]);
+        gate_of(s[q][e], a, r);
+        A[e] *= a;
+        M[e] = a * (raw_value<T>(z[q], e) + M[e]);
+      }
+      step_apart(q);
     }
-    gated_enter<LINK, V>(p, runs[k & 1], enter, run, waves, k, at, live, A, M, carry, m);
+    gated_enter<LINK, V>(p, shared, run, waves, k, at, live, A, M, carry, m);
+#pragma unroll
+    for (int q = 0; q < kKeep; ++q) again(z[q]);
     if (live && s0 < p.steps) {
 #pragma unroll
       for (int q = kKeep - 1; q >= 0; --q) {
         Words<T, V> ov, og;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float d = z[q][e] + m[e];
-          ov.v[e] = (T)(r[q][e] * d);
+          float a, r;
+          again(s[q][e]);
+          gate_of(s[q][e], a, r);
+          const float d = raw_value<T>(z[q], e) + m[e];
+          ov.v[e] = (T)(r * d);
           og.v[e] = (T)(x[q][e] * d);
-          if (full || s0 + q < len) m[e] = a[q][e] * d;
+          if (full || s0 + q < len) m[e] = a * d;
           else ov.v[e] = og.v[e] = (T)0.0f;
         }
         if (full || s0 + q < p.steps) {
-          put_once(dvp + (s0 + q) * p.dim, ov);
-          put_once(dgp + (s0 + q) * p.dim, og);
+          put_once(dvp + (s0 + q) * p.dim + c, ov);
+          put_once(dgp + (s0 + q) * p.dim + c, og);
         }
+        step_apart(q);
       }
     }
     if (dy0 && live && k == p.nchunk - 1 && run == waves - 1)

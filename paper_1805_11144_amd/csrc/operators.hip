@@ -76,15 +76,17 @@ void with_width(int64_t v, F&& f) {
     if (v == 8) return f(std::integral_constant<int, 8>{});
   if constexpr (MAX >= 4)
     if (v == 4) return f(std::integral_constant<int, 4>{});
-  if (v == 2) return f(std::integral_constant<int, 2>{});
+  if constexpr (MAX >= 2)
+    if (v == 2) return f(std::integral_constant<int, 2>{});
   f(std::integral_constant<int, 1>{});
 }
 
-// Calls f with the element type and the access width (at most MAX).
-template <int MAX, class F>
+// Calls f with the element type and the access width (at most M16 bf16 or M32
+// float32 values).
+template <int M16, int M32, class F>
 void with_type(int32_t dtype, int64_t v, F&& f) {
-  if (dtype == MS_DTYPE_BF16) with_width<MAX>(v, [&](auto w) { f((__bf16)0.0f, w); });
-  else with_width<std::min(MAX, 4)>(v, [&](auto w) { f(0.0f, w); });
+  if (dtype == MS_DTYPE_BF16) with_width<M16>(v, [&](auto w) { f((__bf16)0.0f, w); });
+  else with_width<M32>(v, [&](auto w) { f(0.0f, w); });
 }
 
 int32_t threads_per_row(int64_t nv) {
@@ -218,8 +220,6 @@ Gated check_gated(const ms_gated_lowpass_desc* d) {
   return g;
 }
 
-constexpr int kGatedWaves = 8;   // of a workgroup, at most
-
 // Scratch memory of chunks that run side by side: their maps and states, the
 // ticket.
 struct GatedWork {
@@ -247,7 +247,7 @@ GatedWork gated_work(const Gated& g, void* ws) {
 // that clears what they publish, and their waits.
 struct GatedShape {
   unsigned threads;
-  bool link;
+  bool link, span;
 };
 
 GatedShape gated_shape(Gated& g) {
@@ -255,9 +255,23 @@ GatedShape gated_shape(Gated& g) {
   int waves = 1;
   while (waves < kGatedWaves && waves < g.keeps) waves *= 2;
   a.nchunk = (int32_t)((g.keeps + waves - 1) / waves);
-  a.groups = (int32_t)((a.batch * a.nv + 63) / 64);
+  a.per_row = (int32_t)((a.nv + 63) / 64);
+  const bool span = a.per_row * 64 > a.nv + a.nv / 4;   // over a fifth of the lanes would idle
+  a.groups = (int32_t)(span ? (a.batch * a.nv + 63) / 64 : a.batch * a.per_row);
   const bool link = a.nchunk > 4 && a.groups < 1024 && (int64_t)a.nchunk * a.groups < ((int64_t)1 << 22);
-  return {(unsigned)waves * 64, link};
+  return {(unsigned)waves * 64, link, span};
+}
+
+// Calls f(link, span, grid) with the shape's choices as compile-time values.
+template <class F>
+void gated_launch(const GatedShape& s, const GatedArgs& a, F&& f) {
+  const auto with = [&](auto link) {
+    const dim3 grid((unsigned)(s.link ? a.nchunk * a.groups : a.groups));
+    if (s.span) f(link, std::true_type{}, grid);
+    else f(link, std::false_type{}, grid);
+  };
+  if (s.link) with(std::true_type{});
+  else with(std::false_type{});
 }
 
 void gated_clear(GatedArgs& a, const GatedWork& w, hipStream_t st) {
@@ -416,7 +430,7 @@ ms_status ms_embed(const ms_embed_desc* d, const void* tokens, const void* table
     const int32_t nv = (int32_t)(d->dim / v), tpr = threads_per_row(nv);
     constexpr int kLookupRows = 4;
     const int64_t lookups = (d->n_tokens + kLookupRows - 1) / kLookupRows;
-    with_type<8>(d->dtype, v, [&](auto zero, auto width) {
+    with_type<8, 4>(d->dtype, v, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
       auto go = [&](auto id) {
@@ -464,7 +478,7 @@ ms_status ms_embed_grad(const ms_embed_desc* d, const void* tokens, const void* 
     const int64_t chunks = (d->n_tokens + kRun - 1) / kRun;
     const unsigned pieces = (unsigned)((chunks + 256 / tpc - 1) / (256 / tpc));
     const unsigned searches = (unsigned)std::min<int64_t>((d->vocab + 256) / 256, kMaxBlocks / 2);
-    with_type<8>(d->dtype, v, [&](auto zero, auto width) {
+    with_type<8, 4>(d->dtype, v, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
       hipLaunchKernelGGL(HIP_KERNEL_NAME(k_embed_pieces<T, V>), dim3(searches + pieces), dim3(256), 0, st,
@@ -531,19 +545,17 @@ ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* d, const void* v, const 
     }
     a.lengths = lengths;
     Wide wide = Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es).at(g, es).at(y, es);
-    const int64_t w = std::min<int64_t>(2, wide.at(kept, 4).v);
+    const int64_t w = std::min<int64_t>(4 / (int64_t)es, wide.at(kept, 4).v);   // a word of 4 bytes to a lane
     a.nv = a.dim / w;
     const GatedShape shape = gated_shape(p);
     if (shape.link) gated_clear(a, work, st);
-    with_type<2>(d->dtype, w, [&](auto zero, auto width) {
+    with_type<2, 1>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
-      if (shape.link)
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated<T, V, true>), dim3((unsigned)(a.nchunk * a.groups)), dim3(shape.threads),
-                           0, st, a, (const T*)v, (const T*)g, y0, (T*)y, last, kept);
-      else
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated<T, V, false>), dim3((unsigned)a.groups), dim3(shape.threads), 0, st, a,
-                           (const T*)v, (const T*)g, y0, (T*)y, last, kept);
+      gated_launch(shape, a, [&](auto link, auto span, dim3 grid) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated<T, V, decltype(link)::value, decltype(span)::value>), grid,
+                           dim3(shape.threads), 0, st, a, (const T*)v, (const T*)g, y0, (T*)y, last, kept);
+      });
     });
     HIPCHECK(hipGetLastError());
   });
@@ -573,21 +585,19 @@ ms_status ms_gated_lowpass_grad(const ms_gated_lowpass_desc* d, const void* v, c
       return;
     }
     a.lengths = lengths;
-    const int64_t w = std::min<int64_t>(2, Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es)
+    const int64_t w = std::min<int64_t>(4 / (int64_t)es, Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es)
                                                .at(g, es).at(dy, es).at(dv, es).at(dg, es).v);
     a.nv = a.dim / w;
     const GatedShape shape = gated_shape(p);
     if (shape.link) gated_clear(a, work, st);
-    with_type<2>(d->dtype, w, [&](auto zero, auto width) {
+    with_type<2, 1>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
-      if (shape.link)
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad<T, V, true>), dim3((unsigned)(a.nchunk * a.groups)),
+      gated_launch(shape, a, [&](auto link, auto span, dim3 grid) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad<T, V, decltype(link)::value, decltype(span)::value>), grid,
                            dim3(shape.threads), 0, st, a, (const T*)v, (const T*)g, kept, (const T*)dy, dlast, (T*)dv, (T*)dg,
                            dy0);
-      else
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad<T, V, false>), dim3((unsigned)a.groups), dim3(shape.threads), 0, st, a,
-                           (const T*)v, (const T*)g, kept, (const T*)dy, dlast, (T*)dv, (T*)dg, dy0);
+      });
     });
     HIPCHECK(hipGetLastError());
   });
@@ -617,7 +627,7 @@ ms_status ms_gated_lowpass_step(const ms_gated_step_desc* d, const void* v, cons
     const int64_t w = std::min<int64_t>(
         4, Wide(es).of(d->dim).of(vs).of(gs).of(ys).of(ss).at(v, es).at(g, es).at(y, es).at(state, 4).v);
     const int32_t nv = (int32_t)(d->dim / w), tpr = threads_per_row(nv);
-    with_type<4>(d->dtype, w, [&](auto zero, auto width) {
+    with_type<4, 4>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
       hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_served<T, V>), dim3(row_blocks(d->rows, tpr)), dim3(256), 0,
