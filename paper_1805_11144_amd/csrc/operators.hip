@@ -13,6 +13,7 @@
 #include "kernels_embed.hpp"
 #include "kernels_gated.hpp"
 #include "kernels_orth.hpp"
+#include "kernels_orth_small.hpp"
 
 using namespace ms;
 
@@ -288,7 +289,11 @@ struct Orth {
   int parts;              // fp16 parts of a value
   double sx, sa, sq;      // scales of X, A and Q
   int64_t xm, xr, om, orow;
+  int small;              // row tiles of 16 where a matrix fits into one workgroup's LDS, else 0
+  int64_t stride;         // of its rows there
 };
+
+constexpr int64_t kOrthLds = 156 * 1024;   // of 160 KB
 
 Orth check_orth(const ms_orth_desc* d, bool update) {
   need(d != nullptr, "NULL descriptor");
@@ -308,10 +313,13 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
   pair(d->out_stride, o.om, o.orow);
   o.n = std::min(d->rows, d->cols), o.m = std::max(d->rows, d->cols);
   o.parts = update || d->dtype == MS_DTYPE_F32 ? 2 : 1;
-  // 128 x 128 tiles from 512 rows on
-  o.tile = o.n >= 512 ? 128 : 64;
+  // 128 x 128 tiles from 1536 rows on
+  o.tile = o.n >= 1536 ? 128 : 64;
   o.np = up(o.n, o.tile), o.mp = up(o.m, o.tile);
   need(d->batch <= kMaxBlocks / ((o.np / 64) * (o.mp / 64)), "too many matrices of this size");
+  o.stride = up(o.m, 64) + 4;
+  o.small = (int)up(o.n, 16) / 16;
+  if (o.small > 4 || orth_small_floats(o.small, o.stride) * 4 > kOrthLds) o.small = 0;
   // How large an iterate's singular values and the polynomial can get: the
   // first are at most 1, and f(s) = s (c0 + c1 s^2 + c2 s^4) takes its extremes
   // over [0, top] at the ends or where its derivative is 0.
@@ -351,7 +359,8 @@ struct OrthWork {
 
 OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
   Carve c{(char*)ws};
-  OrthWork w;
+  OrthWork w{};
+  if (o.small) return w;
   const int64_t big = d->batch * o.parts * o.np * o.mp, small = d->batch * o.parts * o.np * o.np;
   w.parts = c.take<double>(d->batch * kOrthParts);
   w.x = c.take<half_t>(big);
@@ -404,10 +413,36 @@ void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork
   HIPCHECK(hipGetLastError());
 }
 
+template <class T, bool UPDATE>
+void orth_small(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, const OrthGemm& out, hipStream_t st) {
+  OrthSmall p{};
+  p.src = src, p.out = out.out, p.omat = out.mat, p.orow = out.row;
+  p.n = (int32_t)o.n, p.m = (int32_t)o.m, p.stride = (int32_t)o.stride, p.steps = d->steps;
+  p.c0 = (float)d->coef[0], p.c1 = (float)d->coef[1], p.c2 = (float)d->coef[2];
+  p.keep = out.keep, p.rate = out.rate, p.eps = d->eps;
+  const size_t lds = (size_t)orth_small_floats(o.small, o.stride) * 4;
+  const auto go = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if (lds > 65536)
+      HIPCHECK(hipFuncSetAttribute((const void*)k_orth_small<T, UPDATE, NT>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)kOrthLds));
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_small<T, UPDATE, NT>), dim3((unsigned)d->batch), dim3(64 * kOrthWaves), lds, st,
+                       p);
+  };
+  switch (o.small) {
+    case 1: go(std::integral_constant<int, 1>{}); break;
+    case 2: go(std::integral_constant<int, 2>{}); break;
+    case 3: go(std::integral_constant<int, 3>{}); break;
+    default: go(std::integral_constant<int, 4>{});
+  }
+  HIPCHECK(hipGetLastError());
+}
+
 template <class T, bool UPDATE, int PL>
-void orth_tiled(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, const OrthGemm& out,
+void orth(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, const OrthGemm& out,
                 hipStream_t st) {
-  if (o.tile == 128) orth_run<T, UPDATE, PL, 128>(d, o, src, w, out, st);
+  if (o.small) orth_small<T, UPDATE>(d, o, src, out, st);
+  else if (o.tile == 128) orth_run<T, UPDATE, PL, 128>(d, o, src, w, out, st);
   else orth_run<T, UPDATE, PL, 64>(d, o, src, w, out, st);
 }
 
@@ -662,8 +697,8 @@ ms_status ms_orthogonalise(const ms_orth_desc* d, const void* x, void* out, void
     OrthSrc src{x, nullptr, o.xm, o.xr, d->rows, d->cols, 0.0f, 0};
     OrthGemm g{};
     g.out = out, g.mat = o.om, g.row = o.orow, g.rows = d->rows, g.cols = d->cols;
-    if (d->dtype == MS_DTYPE_BF16) orth_tiled<__bf16, false, 1>(d, o, src, w, g, st);
-    else orth_tiled<float, false, 2>(d, o, src, w, g, st);
+    if (d->dtype == MS_DTYPE_BF16) orth<__bf16, false, 1>(d, o, src, w, g, st);
+    else orth<float, false, 2>(d, o, src, w, g, st);
   });
 }
 
@@ -687,8 +722,8 @@ ms_status ms_orthogonal_update(const ms_orth_desc* d, const ms_orth_rule* rule, 
     OrthGemm g{};
     g.out = weight, g.mat = d->rows * d->cols, g.row = d->cols, g.rows = d->rows, g.cols = d->cols;
     g.keep = (float)(1.0 - rule->rate * rule->weight_decay), g.rate = (float)rule->rate;
-    if (d->dtype == MS_DTYPE_BF16) orth_tiled<__bf16, true, 2>(d, o, src, w, g, st);
-    else orth_tiled<float, true, 2>(d, o, src, w, g, st);
+    if (d->dtype == MS_DTYPE_BF16) orth<__bf16, true, 2>(d, o, src, w, g, st);
+    else orth<float, true, 2>(d, o, src, w, g, st);
   });
 }
 
