@@ -22,9 +22,10 @@
 
 typedef _Float16 half_t;
 typedef half_t halfx8 __attribute__((ext_vector_type(8)));
+typedef half_t halfx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr int kOrthParts = 64;   // partial sums of a matrix's norm
+constexpr int kOrthParts = 256;   // partial sums of a matrix's norm
 
 // A matrix as the caller holds it.
 struct OrthSrc {
@@ -37,24 +38,46 @@ struct OrthSrc {
 };
 
 // Partial sums of squares in 64 bits: no float32 input overflows or loses
-// them.  An update also advances its momentum.
-template <class T, bool UPDATE>
+// them.  An update also advances its momentum.  A workgroup takes every
+// kOrthParts-th run of 1024 elements (matrices with packed rows: FLAT) or row.
+template <class T, bool UPDATE, bool FLAT>
 __global__ void __launch_bounds__(256) k_orth_norm(OrthSrc s, double* parts) {
   __shared__ double red[4];
   const int64_t mat = blockIdx.x / kOrthParts, part = blockIdx.x % kOrthParts;
   const T* x = (const T*)s.x + mat * s.mat;
   float* mom = UPDATE ? s.momentum + mat * s.rows * s.cols : nullptr;
   double sum = 0.0;
-  for (int64_t r = part; r < s.rows; r += kOrthParts)
-    for (int64_t c = threadIdx.x; c < s.cols; c += 256) {
-      float v = as_f32(x[r * s.row + c]);
-      if constexpr (UPDATE) {
-        const float m = fmaf(s.decay, mom[r * s.cols + c], v);
-        mom[r * s.cols + c] = m;
-        v = s.nesterov ? fmaf(s.decay, m, v) : m;
-      }
-      sum += (double)v * v;
+  const auto take = [&](float v, float* m) {
+    if constexpr (UPDATE) {
+      *m = fmaf(s.decay, *m, v);
+      v = s.nesterov ? fmaf(s.decay, *m, v) : *m;
     }
+    sum += (double)v * v;
+  };
+  if constexpr (FLAT) {
+    const int64_t n = s.rows * s.cols;
+    for (int64_t i0 = part * 1024 + threadIdx.x; i0 < n; i0 += kOrthParts * 1024) {
+      float v[4], m[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t i = i0 + q * 256;
+        v[q] = i < n ? as_f32(x[i]) : 0.0f;
+        m[q] = UPDATE && i < n ? mom[i] : 0.0f;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        take(v[q], &m[q]);
+        if (UPDATE && i0 + q * 256 < n) mom[i0 + q * 256] = m[q];
+      }
+    }
+  } else {
+    for (int64_t r = part; r < s.rows; r += kOrthParts)
+      for (int64_t c = threadIdx.x; c < s.cols; c += 256) {
+        float m = UPDATE ? mom[r * s.cols + c] : 0.0f;
+        take(as_f32(x[r * s.row + c]), &m);
+        if (UPDATE) mom[r * s.cols + c] = m;
+      }
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_down(sum, o, 64);
   if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = sum;
@@ -79,7 +102,9 @@ __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* par
   const int64_t mat = blockIdx.x / (tn * tm);
   const int32_t u = blockIdx.x % (tn * tm), i0 = u / tm * 64, j0 = u % tm * 64;
   if (tid < 64) {
-    double p = parts[mat * kOrthParts + tid];
+    double p = 0.0;
+#pragma unroll
+    for (int q = 0; q < kOrthParts / 64; ++q) p += parts[mat * kOrthParts + q * 64 + tid];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) p += __shfl_down(p, o, 64);
     if (tid == 0) inv_s = scale / (sqrt(p) + eps);
@@ -127,6 +152,7 @@ enum OrthEnd { kEndGram, kEndPoly, kEndNext, kEndOut, kEndUpdate };
 struct OrthGemm {
   const half_t *l, *r;        // L [M][K], R [N][K]
   int32_t M, N, K;            // padded
+  int32_t batch;
   half_t* c;                  // C [M][N], or null
   half_t* ct;                 // its transpose (kEndNext)
   const half_t* a;            // A (kEndPoly)
@@ -138,24 +164,38 @@ struct OrthGemm {
   float keep, rate;           // weight <- keep weight - rate X
 };
 
-// C = L R' on TILE x TILE tiles, a workgroup of four wavefronts each; K in
-// slices of 32, fetched into registers while the one before is multiplied, two
-// buffers in LDS (rows padded to 40 numbers, so that the 16-byte reads of a
-// fragment spread over the banks).
-template <int PL, int TILE, int END, class T>
-__global__ void __launch_bounds__(256) k_orth_gemm(OrthGemm g) {
-  constexpr int KS = 32, P = 40, W = TILE / 2, B = W / 32, U = PL * TILE * KS / 8 / 256;
+// 16 bytes per lane from memory straight to LDS: lane i's to dst + 16 i (dst
+// uniform over the wavefront).
+__device__ __forceinline__ void fetch_lds(const half_t* src, half_t* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+// C = L R' on TILE x TILE tiles.  Four wavefronts share a tile, each a quarter;
+// K runs in slices of KS through two buffers in LDS, the next slice on its way
+// while one is multiplied.  KG = 2: a second group of four takes every other
+// slice, and the two sums are added at the end; where tiles are fewer than the
+// CUs, that is what shortens a call.
+// A slice's rows are KS / 8 chunks of 16 bytes without padding (memory goes to
+// LDS in lane order); chunk c of row r sits at c ^ (r / (64 / KS * 2)), so the
+// rows of a fragment read different banks.
+template <int PL, int TILE, int KS, int KG, int END, class T>
+__global__ void __launch_bounds__(256 * KG) k_orth_gemm(OrthGemm g) {
+  constexpr int W = TILE / 2, B = W / 32, CH = KS / 8, U = PL * TILE * CH / 256;
   constexpr bool SYM = END == kEndGram || END == kEndPoly;
-  static_assert(U >= 1, "every thread fetches");
-  extern __shared__ __attribute__((aligned(16))) half_t lds[];
-  typedef half_t Slab[2][PL][TILE][P];
-  Slab& Ls = *(Slab*)lds;
-  Slab& Rs = *(Slab*)(lds + sizeof(Slab) / sizeof(half_t));
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, wm = wave / 2, wn = wave % 2;
+  constexpr int SLAB = PL * TILE * KS;   // one operand of one slice
+  extern __shared__ __attribute__((aligned(16))) half_t lds[];   // [KG][2][2 operands][SLAB]
+  const int tid = threadIdx.x % 256, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 256);
+  const int wm = wave / 2, wn = wave % 2;
   const int32_t tm = g.M / TILE, tn = g.N / TILE;
   const int32_t per = SYM ? tm * (tm + 1) / 2 : tm * tn;
-  const int64_t mat = blockIdx.x / per;
-  int32_t u = blockIdx.x % per, ti, tj;
+  // workgroups i, i + 8.. run on one XCD: it gets a contiguous part of the
+  // tiles, whose columns and rows it then finds in its L2
+  const uint32_t share = gridDim.x / 8, tile = blockIdx.x % 8 * share + blockIdx.x / 8;
+  if (tile >= (uint32_t)g.batch * per) return;
+  const int64_t mat = tile / per;
+  int32_t u = tile % per, ti, tj;
   if (SYM) {   // tiles ti <= tj, by columns
     tj = (int32_t)((sqrtf(8.0f * u + 1.0f) - 1.0f) * 0.5f);
     while (tj * (tj + 1) / 2 > u) --tj;
@@ -164,24 +204,24 @@ __global__ void __launch_bounds__(256) k_orth_gemm(OrthGemm g) {
   } else {
     ti = u % tm, tj = u / tm;
   }
+  const auto swizzle = [](int row) { return row / (128 / KS) % CH; };
   const int64_t lplane = (int64_t)g.M * g.K, rplane = (int64_t)g.N * g.K;
   const half_t* L = g.l + mat * PL * lplane + (int64_t)ti * TILE * g.K;
   const half_t* R = g.r + mat * PL * rplane + (int64_t)tj * TILE * g.K;
-  halfx8 fl[U], fr[U];
-  auto fetch = [&](int32_t k0) {
+  half_t* own = lds + group * 4 * SLAB;
+  // the lane's chunks of a slice: U of each operand
+  uint32_t off[U];   // in values, within a plane
+#pragma unroll
+  for (int q = 0; q < U; ++q) {
+    const int i = (q * 4 + wave) * 64 + lane, row = i / CH % TILE, c = i % CH ^ swizzle(row);
+    off[q] = (uint32_t)row * (uint32_t)g.K + 8 * c;
+  }
+  const auto fetch = [&](int32_t k0, int buf) {
 #pragma unroll
     for (int q = 0; q < U; ++q) {
-      const int i = q * 256 + tid, p = i / (TILE * KS / 8), row = i / (KS / 8) % TILE, k = 8 * (i % (KS / 8));
-      fl[q] = *(const halfx8*)(L + p * lplane + (int64_t)row * g.K + k0 + k);
-      fr[q] = *(const halfx8*)(R + p * rplane + (int64_t)row * g.K + k0 + k);
-    }
-  };
-  auto store = [&](int buf) {
-#pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const int i = q * 256 + tid, p = i / (TILE * KS / 8), row = i / (KS / 8) % TILE, k = 8 * (i % (KS / 8));
-      *(halfx8*)&Ls[buf][p][row][k] = fl[q];
-      *(halfx8*)&Rs[buf][p][row][k] = fr[q];
+      const int i0 = (q * 4 + wave) * 64, p = i0 / (TILE * CH);
+      fetch_lds(L + p * lplane + k0 + off[q], own + (buf * 2 + 0) * SLAB + 8 * i0);
+      fetch_lds(R + p * rplane + k0 + off[q], own + (buf * 2 + 1) * SLAB + 8 * i0);
     }
   };
   floatx16 acc[B][B];
@@ -189,37 +229,62 @@ __global__ void __launch_bounds__(256) k_orth_gemm(OrthGemm g) {
   for (int i = 0; i < B; ++i)
 #pragma unroll
     for (int j = 0; j < B; ++j) acc[i][j] = floatx16{};
-  fetch(0);
-  store(0);
-  __syncthreads();
+  const int32_t slices = g.K / KS;
+  if (group < slices) fetch(group * KS, 0);
   int buf = 0;
-  for (int32_t k0 = 0; k0 < g.K; k0 += KS) {
-    const bool more = k0 + KS < g.K;
-    if (more) fetch(k0 + KS);
+  for (int32_t s0 = 0; s0 < slices; s0 += KG, buf ^= 1) {
+    const int32_t s = s0 + group;
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wavefront's part of the slice is in LDS
+    __syncthreads();                      // and everyone's; and the other buffer is read
+    const half_t *Ls = own + (buf * 2 + 0) * SLAB, *Rs = own + (buf * 2 + 1) * SLAB;
+    halfx8 a[KS / 16][PL][B], b[KS / 16][PL][B];
+    if (s < slices) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ks += 16) {
-      halfx8 a[PL][B], b[PL][B];
+      for (int ks = 0; ks < KS / 16; ++ks)
 #pragma unroll
-      for (int p = 0; p < PL; ++p)
+        for (int p = 0; p < PL; ++p)
 #pragma unroll
-        for (int i = 0; i < B; ++i) {
-          a[p][i] = *(const halfx8*)&Ls[buf][p][wm * W + i * 32 + lane % 32][ks + 8 * (lane / 32)];
-          b[p][i] = *(const halfx8*)&Rs[buf][p][wn * W + i * 32 + lane % 32][ks + 8 * (lane / 32)];
-        }
+          for (int i = 0; i < B; ++i) {
+            const int ra = wm * W + i * 32 + lane % 32, rb = wn * W + i * 32 + lane % 32, c = 2 * ks + lane / 32;
+            a[ks][p][i] = *(const halfx8*)(Ls + p * TILE * KS + ra * KS + 8 * (c ^ swizzle(ra)));
+            b[ks][p][i] = *(const halfx8*)(Rs + p * TILE * KS + rb * KS + 8 * (c ^ swizzle(rb)));
+          }
+    }
+    if (s + KG < slices) fetch((s + KG) * KS, buf ^ 1);
+    if (s < slices) {
+#pragma unroll
+      for (int ks = 0; ks < KS / 16; ++ks)
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+#pragma unroll
+          for (int j = 0; j < B; ++j) {
+            if constexpr (PL == 2) {
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][1][i], b[ks][0][j], acc[i][j], 0, 0, 0);
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][1][j], acc[i][j], 0, 0, 0);
+            }
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][0][j], acc[i][j], 0, 0, 0);
+          }
+    }
+  }
+  if constexpr (KG == 2) {   // the second group's sums through LDS
+    __syncthreads();
+    float* sums = (float*)lds + wave * B * B * 16 * 64 + lane;
+    if (group == 1) {
 #pragma unroll
       for (int i = 0; i < B; ++i)
 #pragma unroll
-        for (int j = 0; j < B; ++j) {
-          if constexpr (PL == 2) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1][i], b[0][j], acc[i][j], 0, 0, 0);
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][i], b[1][j], acc[i][j], 0, 0, 0);
-          }
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][i], b[0][j], acc[i][j], 0, 0, 0);
-        }
+        for (int j = 0; j < B; ++j)
+#pragma unroll
+          for (int q = 0; q < 16; ++q) sums[((i * B + j) * 16 + q) * 64] = acc[i][j][q];
     }
-    if (more) store(buf ^ 1);
     __syncthreads();
-    buf ^= 1;
+    if (group == 1) return;
+#pragma unroll
+    for (int i = 0; i < B; ++i)
+#pragma unroll
+      for (int j = 0; j < B; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[i][j][q] += sums[((i * B + j) * 16 + q) * 64];
   }
   // a lane holds column lane % 32 and rows 8 (q / 4) + 4 (lane / 32) + q % 4 of each 32 x 32 block
   const int64_t cplane = (int64_t)g.M * g.N;
@@ -232,31 +297,39 @@ __global__ void __launch_bounds__(256) k_orth_gemm(OrthGemm g) {
     for (int j = 0; j < B; ++j) {
       const int64_t col = (int64_t)tj * TILE + wn * W + j * 32 + lane % 32;
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        const int64_t row = (int64_t)ti * TILE + wm * W + i * 32 + 8 * (q / 4) + 4 * (lane / 32) + q % 4;
-        float v = g.f * acc[i][j][q];
-        if constexpr (END == kEndOut || END == kEndUpdate) {
-          const bool tall = g.rows > g.cols;
-          const int64_t r = tall ? col : row, c = tall ? row : col;
-          if (r < g.rows && c < g.cols) {
-            T* o = (T*)g.out + mat * g.mat + r * g.row + c;
-            if constexpr (END == kEndOut) *o = (T)v;
-            else *o = (T)(g.keep * (float)*o - g.rate * v);
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int64_t row0 = (int64_t)ti * TILE + wm * W + i * 32 + 8 * q4 + 4 * (lane / 32);
+        halfx4 hi, lo;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t row = row0 + q;
+          float v = g.f * acc[i][j][4 * q4 + q];
+          if constexpr (END == kEndOut || END == kEndUpdate) {
+            const bool tall = g.rows > g.cols;
+            const int64_t r = tall ? col : row, c = tall ? row : col;
+            if (r < g.rows && c < g.cols) {
+              T* o = (T*)g.out + mat * g.mat + r * g.row + c;
+              if constexpr (END == kEndOut) *o = (T)v;
+              else *o = (T)(g.keep * (float)*o - g.rate * v);
+            }
+          } else {
+            if constexpr (END == kEndPoly) {
+              float av = (float)A[row * g.N + col];
+              if (PL == 2) av += (float)A[cplane + row * g.N + col];
+              v += g.c1 * av + (row == col ? g.c0 : 0.0f);
+            }
+            half_t h, l;
+            split(v, h, l);
+            hi[q] = h, lo[q] = l;
+            C[row * g.N + col] = h;
+            if (PL == 2) C[cplane + row * g.N + col] = l;
           }
-        } else {
-          if constexpr (END == kEndPoly) {
-            float av = (float)A[row * g.N + col];
-            if (PL == 2) av += (float)A[cplane + row * g.N + col];
-            v += g.c1 * av + (row == col ? g.c0 : 0.0f);
-          }
-          half_t hi, lo;
-          split(v, hi, lo);
-          C[row * g.N + col] = hi;
-          if (PL == 2) C[cplane + row * g.N + col] = lo;
-          if (SYM ? ti != tj : END == kEndNext) {
-            half_t* D = SYM ? C : CT;
-            D[col * g.M + row] = hi;
-            if (PL == 2) D[cplane + col * g.M + row] = lo;
+        }
+        if constexpr (SYM || END == kEndNext) {
+          if (END == kEndNext || ti != tj) {
+            half_t* D = (SYM ? C : CT) + col * g.M + row0;
+            *(halfx4*)D = hi;
+            if (PL == 2) *(halfx4*)(D + cplane) = lo;
           }
         }
       }

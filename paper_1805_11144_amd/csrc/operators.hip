@@ -316,7 +316,7 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
   // 128 x 128 tiles from 1536 rows on
   o.tile = o.n >= 1536 ? 128 : 64;
   o.np = up(o.n, o.tile), o.mp = up(o.m, o.tile);
-  need(d->batch <= kMaxBlocks / ((o.np / 64) * (o.mp / 64)), "too many matrices of this size");
+  need(d->batch <= kMaxBlocks / std::max<int64_t>(kOrthParts, (o.np / 64) * (o.mp / 64)), "too many matrices of this size");
   o.stride = up(o.m, 64) + 4;
   o.small = (int)up(o.n, 16) / 16;
   if (o.small > 4 || orth_small_floats(o.small, o.stride) * 4 > kOrthLds) o.small = 0;
@@ -373,41 +373,48 @@ OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
 }
 
 template <int PL, int TILE, int END, class T>
-void orth_gemm(const OrthGemm& g, int64_t batch, hipStream_t st) {
-  constexpr size_t lds = 2 * 2 * PL * TILE * 40 * sizeof(half_t);
+void orth_gemm(const OrthGemm& g, hipStream_t st) {
+  constexpr int KS = PL == 2 && TILE == 128 ? 32 : 64, KG = TILE == 64 ? 2 : 1;
+  constexpr size_t lds = KG * 2 * 2 * PL * TILE * KS * sizeof(half_t);
+  static_assert(lds >= 4 * 16 * 64 * 4 * (TILE / 64) * (TILE / 64) * (KG - 1) && lds <= 160 * 1024, "LDS");
   const int64_t tm = g.M / TILE, tn = g.N / TILE;
   const int64_t per = END == kEndGram || END == kEndPoly ? tm * (tm + 1) / 2 : tm * tn;
-  const void* k = (const void*)k_orth_gemm<PL, TILE, END, T>;
-  if (lds > 65536) HIPCHECK(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_gemm<PL, TILE, END, T>), dim3((unsigned)(batch * per)), dim3(256), lds, st, g);
+  const void* k = (const void*)k_orth_gemm<PL, TILE, KS, KG, END, T>;
+  if (lds >= 65536) HIPCHECK(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_gemm<PL, TILE, KS, KG, END, T>), dim3((unsigned)up(g.batch * per, 8)),
+                     dim3(256 * KG), lds, st, g);
 }
 
 // T: type of x (or the gradient); UPDATE: with momentum, into a weight.
 template <class T, bool UPDATE, int PL, int TILE>
 void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, OrthGemm out, hipStream_t st) {
   const int64_t blocks = d->batch * (o.np / 64) * (o.mp / 64);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE>), dim3((unsigned)(d->batch * kOrthParts)), dim3(256), 0, st, src,
-                     w.parts);
+  const dim3 norms((unsigned)(d->batch * kOrthParts));
+  if (src.row == src.cols)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE, true>), norms, dim3(256), 0, st, src, w.parts);
+  else
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE, false>), norms, dim3(256), 0, st, src, w.parts);
   hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, PL>), dim3((unsigned)blocks), dim3(256), 0, st, src,
                      (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], (int32_t)o.np, (int32_t)o.mp);
   using R = std::conditional_t<UPDATE, float, T>;
   for (int k = 0; k < d->steps; ++k) {
     OrthGemm g{};
+    g.batch = out.batch = (int32_t)d->batch;
     g.l = g.r = w.x, g.M = g.N = (int32_t)o.np, g.K = (int32_t)o.mp, g.c = w.a;
     g.f = (float)(o.sa / (o.sx * o.sx));
-    orth_gemm<PL, TILE, kEndGram, R>(g, d->batch, st);
+    orth_gemm<PL, TILE, kEndGram, R>(g, st);
     g.l = g.r = w.a, g.K = (int32_t)o.np, g.c = w.q, g.a = w.a;
     g.f = (float)(d->coef[2] * o.sq / (o.sa * o.sa));
     g.c0 = (float)(d->coef[0] * o.sq), g.c1 = (float)(d->coef[1] * o.sq / o.sa);
-    orth_gemm<PL, TILE, kEndPoly, R>(g, d->batch, st);
+    orth_gemm<PL, TILE, kEndPoly, R>(g, st);
     OrthGemm x = out;
     x.l = w.q, x.r = w.t[k % 2], x.M = (int32_t)o.np, x.N = (int32_t)o.mp, x.K = (int32_t)o.np;
     if (k + 1 < d->steps) {
       x.c = w.x, x.ct = w.t[(k + 1) % 2], x.f = (float)(1.0 / o.sq);
-      orth_gemm<PL, TILE, kEndNext, R>(x, d->batch, st);
+      orth_gemm<PL, TILE, kEndNext, R>(x, st);
     } else {
       x.f = (float)(1.0 / (o.sq * o.sx));
-      orth_gemm<PL, TILE, UPDATE ? kEndUpdate : kEndOut, R>(x, d->batch, st);
+      orth_gemm<PL, TILE, UPDATE ? kEndUpdate : kEndOut, R>(x, st);
     }
   }
   HIPCHECK(hipGetLastError());
