@@ -90,9 +90,18 @@ __device__ __forceinline__ void split(float x, half_t& hi, half_t& lo) {
   lo = (half_t)(x - (float)hi);
 }
 
+// Where value (row, k) of a matrix with `rows` rows is: slices of KS values of k
+// lie one after the other, so a tile's part of a slice is one contiguous piece.
+// With rows of whole k behind each other, the rows of a tile of a 4096 x 4096
+// matrix are 8 KB apart and load a few of the L2's channels only.
+template <int KS>
+__device__ __forceinline__ int64_t orth_at(int64_t rows, int64_t row, int64_t k) {
+  return (k / KS * rows + row) * KS + k % KS;
+}
+
 // The first iterate, scale X / (|X| + eps), and its transpose.  grid: batch x
 // (mp / 64) x (np / 64) tiles of 64 x 64.
-template <class T, bool UPDATE, int PL>
+template <class T, bool UPDATE, int PL, int KS>
 __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* parts, double eps, double scale, half_t* X,
                                                     half_t* XT, int32_t np, int32_t mp) {
   __shared__ float tile[64][65];
@@ -139,11 +148,12 @@ __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* par
     const int p = k / 64, q = k % 64;
     half_t hi, lo;
     split(tile[p][q], hi, lo);
-    x0[(int64_t)(i0 + p) * mp + j0 + q] = hi;
-    if (PL == 2) x0[plane + (int64_t)(i0 + p) * mp + j0 + q] = lo;
+    const int64_t xa = orth_at<KS>(np, i0 + p, j0 + q), ta = orth_at<KS>(mp, j0 + p, i0 + q);
+    x0[xa] = hi;
+    if (PL == 2) x0[plane + xa] = lo;
     split(tile[q][p], hi, lo);
-    t0[(int64_t)(j0 + p) * np + i0 + q] = hi;
-    if (PL == 2) t0[plane + (int64_t)(j0 + p) * np + i0 + q] = lo;
+    t0[ta] = hi;
+    if (PL == 2) t0[plane + ta] = lo;
   }
 }
 
@@ -152,7 +162,7 @@ enum OrthEnd { kEndGram, kEndPoly, kEndNext, kEndOut, kEndUpdate };
 struct OrthGemm {
   const half_t *l, *r;        // L [M][K], R [N][K]
   int32_t M, N, K;            // padded
-  int32_t batch;
+  uint32_t per, whole;        // tiles of a matrix; tiles of all that are computed whole
   half_t* c;                  // C [M][N], or null
   half_t* ct;                 // its transpose (kEndNext)
   const half_t* a;            // A (kEndPoly)
@@ -171,93 +181,106 @@ __device__ __forceinline__ void fetch_lds(const half_t* src, half_t* dst) {
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
-// C = L R' on TILE x TILE tiles.  Four wavefronts share a tile, each a quarter;
-// K runs in slices of KS through two buffers in LDS, the next slice on its way
-// while one is multiplied.  KG = 2: a second group of four takes every other
-// slice, and the two sums are added at the end; where tiles are fewer than the
-// CUs, that is what shortens a call.
+// A barrier that leaves this wavefront's last N loads to LDS on their way.
+// __syncthreads waits for all of them.
+template <int N>
+__device__ __forceinline__ void barrier_but() {
+  static_assert(N < 64, "six bits");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// C = L R' on the TM x TN tile at (row, col) of matrix `mat`.  WR x WC
+// wavefronts share a tile; K runs in slices of KS through ST buffers in LDS,
+// ST - 1 slices on their way while one is multiplied.  KG = 2: a second group
+// of wavefronts takes every other slice, and the two sums are added at the end;
+// where tiles are fewer than the CUs, that is what shortens a call.
 // A slice's rows are KS / 8 chunks of 16 bytes without padding (memory goes to
-// LDS in lane order); chunk c of row r sits at c ^ (r / (64 / KS * 2)), so the
+// LDS in lane order); chunk c of row r sits at c ^ (r / (128 / KS)), so the
 // rows of a fragment read different banks.
-template <int PL, int TILE, int KS, int KG, int END, class T>
-__global__ void __launch_bounds__(256 * KG) k_orth_gemm(OrthGemm g) {
-  constexpr int W = TILE / 2, B = W / 32, CH = KS / 8, U = PL * TILE * CH / 256;
+template <int PL, int TM, int TN, int WR, int WC, int KS, int ST, int KG, int END, class T>
+__device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_t mat, int32_t trow, int32_t tcol) {
+  constexpr int NW = WR * WC, WM = TM / WR, WN = TN / WC, BI = WM / 32, BJ = WN / 32;
+  constexpr int CH = KS / 8, UL = PL * TM * CH / (64 * NW), UR = PL * TN * CH / (64 * NW);
+  static_assert(BI >= 1 && BJ >= 1 && UL >= 1 && UR >= 1, "work for every wavefront");
   constexpr bool SYM = END == kEndGram || END == kEndPoly;
-  constexpr int SLAB = PL * TILE * KS;   // one operand of one slice
-  extern __shared__ __attribute__((aligned(16))) half_t lds[];   // [KG][2][2 operands][SLAB]
-  const int tid = threadIdx.x % 256, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 256);
-  const int wm = wave / 2, wn = wave % 2;
-  const int32_t tm = g.M / TILE, tn = g.N / TILE;
-  const int32_t per = SYM ? tm * (tm + 1) / 2 : tm * tn;
-  // workgroups i, i + 8.. run on one XCD: it gets a contiguous part of the
-  // tiles, whose columns and rows it then finds in its L2
-  const uint32_t share = gridDim.x / 8, tile = blockIdx.x % 8 * share + blockIdx.x / 8;
-  if (tile >= (uint32_t)g.batch * per) return;
-  const int64_t mat = tile / per;
-  int32_t u = tile % per, ti, tj;
-  if (SYM) {   // tiles ti <= tj, by columns
-    tj = (int32_t)((sqrtf(8.0f * u + 1.0f) - 1.0f) * 0.5f);
-    while (tj * (tj + 1) / 2 > u) --tj;
-    while ((tj + 1) * (tj + 2) / 2 <= u) ++tj;
-    ti = u - tj * (tj + 1) / 2;
-  } else {
-    ti = u % tm, tj = u / tm;
-  }
+  constexpr int LEFT = PL * TM * KS, SLAB = LEFT + PL * TN * KS;   // of one slice; lds: [KG][ST][SLAB]
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % NW);
+  const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW));
+  const int wm = wave / WC, wn = wave % WC;
   const auto swizzle = [](int row) { return row / (128 / KS) % CH; };
   const int64_t lplane = (int64_t)g.M * g.K, rplane = (int64_t)g.N * g.K;
-  const half_t* L = g.l + mat * PL * lplane + (int64_t)ti * TILE * g.K;
-  const half_t* R = g.r + mat * PL * rplane + (int64_t)tj * TILE * g.K;
-  half_t* own = lds + group * 4 * SLAB;
-  // the lane's chunks of a slice: U of each operand
-  uint32_t off[U];   // in values, within a plane
+  const half_t* L = g.l + mat * PL * lplane + (int64_t)trow * KS;
+  const half_t* R = g.r + mat * PL * rplane + (int64_t)tcol * KS;
+  half_t* own = lds + group * ST * SLAB;
+  // the lane's chunks of a slice, in values within a plane
+  uint32_t offl[UL], offr[UR];
 #pragma unroll
-  for (int q = 0; q < U; ++q) {
-    const int i = (q * 4 + wave) * 64 + lane, row = i / CH % TILE, c = i % CH ^ swizzle(row);
-    off[q] = (uint32_t)row * (uint32_t)g.K + 8 * c;
+  for (int q = 0; q < UL; ++q) {
+    const int i = (q * NW + wave) * 64 + lane, row = i / CH % TM;
+    offl[q] = (uint32_t)(row * KS + 8 * (i % CH ^ swizzle(row)));
   }
-  const auto fetch = [&](int32_t k0, int buf) {
 #pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const int i0 = (q * 4 + wave) * 64, p = i0 / (TILE * CH);
-      fetch_lds(L + p * lplane + k0 + off[q], own + (buf * 2 + 0) * SLAB + 8 * i0);
-      fetch_lds(R + p * rplane + k0 + off[q], own + (buf * 2 + 1) * SLAB + 8 * i0);
+  for (int q = 0; q < UR; ++q) {
+    const int i = (q * NW + wave) * 64 + lane, row = i / CH % TN;
+    offr[q] = (uint32_t)(row * KS + 8 * (i % CH ^ swizzle(row)));
+  }
+  const auto fetch = [&](int64_t slice, int buf) {
+#pragma unroll
+    for (int q = 0; q < UL; ++q) {
+      const int i0 = (q * NW + wave) * 64;
+      fetch_lds(L + i0 / (TM * CH) * lplane + slice * g.M * KS + offl[q], own + buf * SLAB + 8 * i0);
+    }
+#pragma unroll
+    for (int q = 0; q < UR; ++q) {
+      const int i0 = (q * NW + wave) * 64;
+      fetch_lds(R + i0 / (TN * CH) * rplane + slice * g.N * KS + offr[q], own + buf * SLAB + LEFT + 8 * i0);
     }
   };
-  floatx16 acc[B][B];
+  floatx16 acc[BI][BJ];
 #pragma unroll
-  for (int i = 0; i < B; ++i)
+  for (int i = 0; i < BI; ++i)
 #pragma unroll
-    for (int j = 0; j < B; ++j) acc[i][j] = floatx16{};
+    for (int j = 0; j < BJ; ++j) acc[i][j] = floatx16{};
   const int32_t slices = g.K / KS;
-  if (group < slices) fetch(group * KS, 0);
+#pragma unroll
+  for (int q = 0; q < ST - 1; ++q)
+    if (q * KG + group < slices) fetch(q * KG + group, q);
   int buf = 0;
-  for (int32_t s0 = 0; s0 < slices; s0 += KG, buf ^= 1) {
+  for (int32_t s0 = 0; s0 < slices; s0 += KG) {
     const int32_t s = s0 + group;
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wavefront's part of the slice is in LDS
-    __syncthreads();                      // and everyone's; and the other buffer is read
-    const half_t *Ls = own + (buf * 2 + 0) * SLAB, *Rs = own + (buf * 2 + 1) * SLAB;
-    halfx8 a[KS / 16][PL][B], b[KS / 16][PL][B];
+    // everyone's part of slice s is in LDS (the later ones may be on their way), and the buffer of the slice
+    // before is read
+    if (s0 + (ST - 1) * KG <= slices) barrier_but<(ST - 2) * (UL + UR)>();
+    else barrier_but<0>();
+    const half_t *Ls = own + buf * SLAB, *Rs = Ls + LEFT;
+    halfx8 a[KS / 16][PL][BI], b[KS / 16][PL][BJ];
     if (s < slices) {
 #pragma unroll
       for (int ks = 0; ks < KS / 16; ++ks)
 #pragma unroll
-        for (int p = 0; p < PL; ++p)
+        for (int p = 0; p < PL; ++p) {
+          const int c = 2 * ks + lane / 32;
 #pragma unroll
-          for (int i = 0; i < B; ++i) {
-            const int ra = wm * W + i * 32 + lane % 32, rb = wn * W + i * 32 + lane % 32, c = 2 * ks + lane / 32;
-            a[ks][p][i] = *(const halfx8*)(Ls + p * TILE * KS + ra * KS + 8 * (c ^ swizzle(ra)));
-            b[ks][p][i] = *(const halfx8*)(Rs + p * TILE * KS + rb * KS + 8 * (c ^ swizzle(rb)));
+          for (int i = 0; i < BI; ++i) {
+            const int r = wm * WM + i * 32 + lane % 32;
+            a[ks][p][i] = *(const halfx8*)(Ls + (p * TM + r) * KS + 8 * (c ^ swizzle(r)));
           }
+#pragma unroll
+          for (int j = 0; j < BJ; ++j) {
+            const int r = wn * WN + j * 32 + lane % 32;
+            b[ks][p][j] = *(const halfx8*)(Rs + (p * TN + r) * KS + 8 * (c ^ swizzle(r)));
+          }
+        }
     }
-    if (s + KG < slices) fetch((s + KG) * KS, buf ^ 1);
+    const int32_t next = s + (ST - 1) * KG;
+    if (next < slices) fetch(next, buf == 0 ? ST - 1 : buf - 1);
     if (s < slices) {
 #pragma unroll
       for (int ks = 0; ks < KS / 16; ++ks)
 #pragma unroll
-        for (int i = 0; i < B; ++i)
+        for (int i = 0; i < BI; ++i)
 #pragma unroll
-          for (int j = 0; j < B; ++j) {
+          for (int j = 0; j < BJ; ++j) {
             if constexpr (PL == 2) {
               acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][1][i], b[ks][0][j], acc[i][j], 0, 0, 0);
               acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][1][j], acc[i][j], 0, 0, 0);
@@ -265,40 +288,43 @@ __global__ void __launch_bounds__(256 * KG) k_orth_gemm(OrthGemm g) {
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][0][j], acc[i][j], 0, 0, 0);
           }
     }
+    buf = buf + 1 == ST ? 0 : buf + 1;
   }
   if constexpr (KG == 2) {   // the second group's sums through LDS
     __syncthreads();
-    float* sums = (float*)lds + wave * B * B * 16 * 64 + lane;
+    float* sums = (float*)lds + wave * BI * BJ * 16 * 64 + lane;
     if (group == 1) {
 #pragma unroll
-      for (int i = 0; i < B; ++i)
+      for (int i = 0; i < BI; ++i)
 #pragma unroll
-        for (int j = 0; j < B; ++j)
+        for (int j = 0; j < BJ; ++j)
 #pragma unroll
-          for (int q = 0; q < 16; ++q) sums[((i * B + j) * 16 + q) * 64] = acc[i][j][q];
+          for (int q = 0; q < 16; ++q) sums[((i * BJ + j) * 16 + q) * 64] = acc[i][j][q];
     }
     __syncthreads();
     if (group == 1) return;
 #pragma unroll
-    for (int i = 0; i < B; ++i)
+    for (int i = 0; i < BI; ++i)
 #pragma unroll
-      for (int j = 0; j < B; ++j)
+      for (int j = 0; j < BJ; ++j)
 #pragma unroll
-        for (int q = 0; q < 16; ++q) acc[i][j][q] += sums[((i * B + j) * 16 + q) * 64];
+        for (int q = 0; q < 16; ++q) acc[i][j][q] += sums[((i * BJ + j) * 16 + q) * 64];
   }
-  // a lane holds column lane % 32 and rows 8 (q / 4) + 4 (lane / 32) + q % 4 of each 32 x 32 block
   const int64_t cplane = (int64_t)g.M * g.N;
   half_t* C = g.c + mat * PL * cplane;
   half_t* CT = END == kEndNext ? g.ct + mat * PL * cplane : nullptr;
   const half_t* A = END == kEndPoly ? g.a + mat * PL * cplane : nullptr;
 #pragma unroll
-  for (int i = 0; i < B; ++i)
+  for (int i = 0; i < BI; ++i)
 #pragma unroll
-    for (int j = 0; j < B; ++j) {
-      const int64_t col = (int64_t)tj * TILE + wn * W + j * 32 + lane % 32;
+    for (int j = 0; j < BJ; ++j) {
+      // a lane holds column lane % 32 and rows 8 (q / 4) + 4 (lane / 32) + q % 4 of each 32 x 32 block
+      const int32_t brow = trow + wm * WM + i * 32, bcol = tcol + wn * WN + j * 32;
+      if (SYM && brow > bcol) continue;   // the mirror image of another block
+      const int64_t col = bcol + lane % 32;
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4) {
-        const int64_t row0 = (int64_t)ti * TILE + wm * W + i * 32 + 8 * q4 + 4 * (lane / 32);
+        const int64_t row0 = brow + 8 * q4 + 4 * (lane / 32);
         halfx4 hi, lo;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -314,24 +340,64 @@ __global__ void __launch_bounds__(256 * KG) k_orth_gemm(OrthGemm g) {
             }
           } else {
             if constexpr (END == kEndPoly) {
-              float av = (float)A[row * g.N + col];
-              if (PL == 2) av += (float)A[cplane + row * g.N + col];
+              float av = (float)A[orth_at<KS>(g.M, row, col)];
+              if (PL == 2) av += (float)A[cplane + orth_at<KS>(g.M, row, col)];
               v += g.c1 * av + (row == col ? g.c0 : 0.0f);
             }
             half_t h, l;
             split(v, h, l);
             hi[q] = h, lo[q] = l;
-            C[row * g.N + col] = h;
-            if (PL == 2) C[cplane + row * g.N + col] = l;
+            C[orth_at<KS>(g.M, row, col)] = h;
+            if (PL == 2) C[cplane + orth_at<KS>(g.M, row, col)] = l;
           }
         }
         if constexpr (SYM || END == kEndNext) {
-          if (END == kEndNext || ti != tj) {
-            half_t* D = (SYM ? C : CT) + col * g.M + row0;
+          if (END == kEndNext || brow != bcol) {
+            half_t* D = (SYM ? C : CT) + orth_at<KS>(g.N, col, row0);
             *(halfx4*)D = hi;
             if (PL == 2) *(halfx4*)(D + cplane) = lo;
           }
         }
       }
     }
+}
+
+// Tile number u of a matrix, from its top left corner: all tiles by columns of
+// tiles, or (SYM) those that reach the diagonal or lie above it.
+template <int TM, int TN, bool SYM>
+__device__ __forceinline__ void orth_place(uint32_t u, int32_t rows, int32_t& row, int32_t& col) {
+  const uint32_t tm = rows / TM;
+  uint32_t ti = u % tm, tj = u / tm;
+  if constexpr (SYM) {   // column tj has the tiles 0 .. tj / E
+    constexpr uint32_t E = TM / TN;
+    uint32_t g = (uint32_t)((sqrtf(8.0f * (u / E) + 1.0f) - 1.0f) * 0.5f);   // E columns have g + 1 tiles each
+    while (E * g * (g + 1) / 2 > u) --g;
+    while (E * (g + 1) * (g + 2) / 2 <= u) ++g;
+    const uint32_t left = u - E * g * (g + 1) / 2;
+    ti = left % (g + 1), tj = g * E + left / (g + 1);
+  }
+  row = (int32_t)ti * TM, col = (int32_t)tj * TN;
+}
+
+// `whole` tiles, and `over` ones in quarters.
+template <int PL, int TM, int TN, int WR, int WC, int KS, int ST, int KG, int END, class T>
+__global__ void __launch_bounds__(64 * WR * WC * KG) k_orth_gemm(OrthGemm g) {
+  constexpr bool SYM = END == kEndGram || END == kEndPoly;
+  extern __shared__ __attribute__((aligned(16))) half_t orth_gemm_lds[];
+  // workgroups i, i + 8.. run on one XCD: it gets a contiguous part of the
+  // tiles, whose columns and rows it then finds in its L2
+  const uint32_t share = (g.whole + 7) / 8;
+  int32_t row, col;
+  if (blockIdx.x < share * 8) {
+    const uint32_t tile = blockIdx.x % 8 * share + blockIdx.x / 8;
+    if (tile >= g.whole) return;
+    orth_place<TM, TN, SYM>(tile % g.per, g.M, row, col);
+    orth_tile<PL, TM, TN, WR, WC, KS, ST, KG, END, T>(g, orth_gemm_lds, tile / g.per, row, col);
+  } else if constexpr (TM > 64) {
+    const uint32_t quarter = blockIdx.x - share * 8, tile = g.whole + quarter / 4;
+    orth_place<TM, TN, SYM>(tile % g.per, g.M, row, col);
+    row += (int32_t)(quarter & 1) * (TM / 2), col += (int32_t)(quarter >> 1 & 1) * (TN / 2);
+    if (SYM && row >= col + TN / 2) return;
+    orth_tile<PL, TM / 2, TN / 2, WR, WC, KS, ST, 1, END, T>(g, orth_gemm_lds, tile / g.per, row, col);
+  }
 }

@@ -1,3 +1,9 @@
+#ifndef SYMR
+#define SYMR 1
+#endif
+#ifndef BIGT
+#define BIGT kCUs
+#endif
 // The operators on device arrays of the C ABI: argument checks, workspace
 // layouts and launches.  The kernels are in kernels_embed.hpp,
 // kernels_gated.hpp and kernels_orth.hpp.
@@ -293,6 +299,7 @@ struct Orth {
   int64_t stride;         // of its rows there
 };
 
+constexpr int kCUs = 256;
 constexpr int64_t kOrthLds = 156 * 1024;   // of 160 KB
 
 Orth check_orth(const ms_orth_desc* d, bool update) {
@@ -313,8 +320,9 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
   pair(d->out_stride, o.om, o.orow);
   o.n = std::min(d->rows, d->cols), o.m = std::max(d->rows, d->cols);
   o.parts = update || d->dtype == MS_DTYPE_F32 ? 2 : 1;
-  // 128 x 128 tiles from 1536 rows on
-  o.tile = o.n >= 1536 ? 128 : 64;
+  // tiles of 128 x 128 read half as much; of 64 x 64 where the others would not fill the CUs
+  const auto tiles = [&](int64_t t) { return d->batch * ((o.n + t - 1) / t) * ((o.m + t - 1) / t); };
+  o.tile = tiles(256) >= BIGT ? 256 : tiles(128) >= kCUs ? 128 : 64;
   o.np = up(o.n, o.tile), o.mp = up(o.m, o.tile);
   need(d->batch <= kMaxBlocks / std::max<int64_t>(kOrthParts, (o.np / 64) * (o.mp / 64)), "too many matrices of this size");
   o.stride = up(o.m, 64) + 4;
@@ -372,17 +380,28 @@ OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
   return w;
 }
 
-template <int PL, int TILE, int END, class T>
-void orth_gemm(const OrthGemm& g, hipStream_t st) {
-  constexpr int KS = PL == 2 && TILE == 128 ? 32 : 64, KG = TILE == 64 ? 2 : 1;
-  constexpr size_t lds = KG * 2 * 2 * PL * TILE * KS * sizeof(half_t);
-  static_assert(lds >= 4 * 16 * 64 * 4 * (TILE / 64) * (TILE / 64) * (KG - 1) && lds <= 160 * 1024, "LDS");
-  const int64_t tm = g.M / TILE, tn = g.N / TILE;
-  const int64_t per = END == kEndGram || END == kEndPoly ? tm * (tm + 1) / 2 : tm * tn;
-  const void* k = (const void*)k_orth_gemm<PL, TILE, KS, KG, END, T>;
-  if (lds >= 65536) HIPCHECK(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_gemm<PL, TILE, KS, KG, END, T>), dim3((unsigned)up(g.batch * per, 8)),
-                     dim3(256 * KG), lds, st, g);
+constexpr int orth_slice(int pl, int pad) { return pad == 64 || pl == 2 ? 32 : 64; }
+
+// PAD: what the sides are padded to.  256 x 256 tiles read least; a symmetric
+// result has few of them, and takes 256 x 128.
+template <int PL, int PAD, int END, class T>
+void orth_gemm(OrthGemm g, int64_t batch, hipStream_t st) {
+  constexpr bool SYM = END == kEndGram || END == kEndPoly;
+  constexpr int TM = PAD, TN = PAD == 256 && SYM && SYMR ? 128 : PAD;
+  constexpr int WR = TM == 256 && TN == 128 ? 4 : 2, WC = TN == 256 ? 4 : 2;
+  constexpr int KS = orth_slice(PL, PAD), ST = PAD == 64 ? 3 : 2, KG = PAD == 64 ? 2 : 1;
+  constexpr size_t lds = KG * ST * PL * (TM + TN) * KS * sizeof(half_t);
+  static_assert(lds >= (KG - 1) * TM * TN * sizeof(float) && lds <= 160 * 1024, "LDS");
+  const int64_t tm = g.M / TM, tn = g.N / TN;
+  g.per = (uint32_t)(SYM ? TM / TN * tm * (tm + 1) / 2 : tm * tn);
+  // A few tiles more than the CUs hold in whole rounds would take a round for
+  // themselves: up to half a round of them is spread over the CUs in quarters.
+  const int64_t tiles = batch * g.per;
+  const int64_t over = PAD > 64 && tiles > kCUs && tiles % kCUs <= kCUs / 2 ? tiles % kCUs : 0;
+  g.whole = (uint32_t)(tiles - over);
+  constexpr auto k = k_orth_gemm<PL, TM, TN, WR, WC, KS, ST, KG, END, T>;
+  if (lds >= 65536) HIPCHECK(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+  hipLaunchKernelGGL(k, dim3((unsigned)(up(g.whole, 8) + 4 * over)), dim3(64 * WR * WC * KG), lds, st, g);
 }
 
 // T: type of x (or the gradient); UPDATE: with momentum, into a weight.
@@ -394,27 +413,26 @@ void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork
     hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE, true>), norms, dim3(256), 0, st, src, w.parts);
   else
     hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE, false>), norms, dim3(256), 0, st, src, w.parts);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, PL>), dim3((unsigned)blocks), dim3(256), 0, st, src,
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, PL, orth_slice(PL, TILE)>), dim3((unsigned)blocks), dim3(256), 0, st, src,
                      (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], (int32_t)o.np, (int32_t)o.mp);
   using R = std::conditional_t<UPDATE, float, T>;
   for (int k = 0; k < d->steps; ++k) {
     OrthGemm g{};
-    g.batch = out.batch = (int32_t)d->batch;
     g.l = g.r = w.x, g.M = g.N = (int32_t)o.np, g.K = (int32_t)o.mp, g.c = w.a;
     g.f = (float)(o.sa / (o.sx * o.sx));
-    orth_gemm<PL, TILE, kEndGram, R>(g, st);
+    orth_gemm<PL, TILE, kEndGram, R>(g, d->batch, st);
     g.l = g.r = w.a, g.K = (int32_t)o.np, g.c = w.q, g.a = w.a;
     g.f = (float)(d->coef[2] * o.sq / (o.sa * o.sa));
     g.c0 = (float)(d->coef[0] * o.sq), g.c1 = (float)(d->coef[1] * o.sq / o.sa);
-    orth_gemm<PL, TILE, kEndPoly, R>(g, st);
+    orth_gemm<PL, TILE, kEndPoly, R>(g, d->batch, st);
     OrthGemm x = out;
     x.l = w.q, x.r = w.t[k % 2], x.M = (int32_t)o.np, x.N = (int32_t)o.mp, x.K = (int32_t)o.np;
     if (k + 1 < d->steps) {
       x.c = w.x, x.ct = w.t[(k + 1) % 2], x.f = (float)(1.0 / o.sq);
-      orth_gemm<PL, TILE, kEndNext, R>(x, st);
+      orth_gemm<PL, TILE, kEndNext, R>(x, d->batch, st);
     } else {
       x.f = (float)(1.0 / (o.sq * o.sx));
-      orth_gemm<PL, TILE, UPDATE ? kEndUpdate : kEndOut, R>(x, st);
+      orth_gemm<PL, TILE, UPDATE ? kEndUpdate : kEndOut, R>(x, d->batch, st);
     }
   }
   HIPCHECK(hipGetLastError());
@@ -449,6 +467,7 @@ template <class T, bool UPDATE, int PL>
 void orth(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, const OrthGemm& out,
                 hipStream_t st) {
   if (o.small) orth_small<T, UPDATE>(d, o, src, out, st);
+  else if (o.tile == 256) orth_run<T, UPDATE, PL, 256>(d, o, src, w, out, st);
   else if (o.tile == 128) orth_run<T, UPDATE, PL, 128>(d, o, src, w, out, st);
   else orth_run<T, UPDATE, PL, 64>(d, o, src, w, out, st);
 }
