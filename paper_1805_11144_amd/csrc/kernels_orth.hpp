@@ -25,6 +25,7 @@ typedef half_t halfx8 __attribute__((ext_vector_type(8)));
 typedef half_t halfx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
+constexpr int kOrthSlice = 32;    // values of k in a slice
 constexpr int kOrthParts = 256;   // partial sums of a matrix's norm
 
 // A matrix as the caller holds it.
@@ -39,8 +40,9 @@ struct OrthSrc {
 
 // Partial sums of squares in 64 bits: no float32 input overflows or loses
 // them.  An update also advances its momentum.  A workgroup takes every
-// kOrthParts-th run of 1024 elements (matrices with packed rows: FLAT) or row.
-template <class T, bool UPDATE, bool FLAT>
+// kOrthParts-th run of 4096 values of a packed matrix, V at a time, or (V = 0)
+// every kOrthParts-th row.
+template <class T, bool UPDATE, int V>
 __global__ void __launch_bounds__(256) k_orth_norm(OrthSrc s, double* parts) {
   __shared__ double red[4];
   const int64_t mat = blockIdx.x / kOrthParts, part = blockIdx.x % kOrthParts;
@@ -54,21 +56,25 @@ __global__ void __launch_bounds__(256) k_orth_norm(OrthSrc s, double* parts) {
     }
     sum += (double)v * v;
   };
-  if constexpr (FLAT) {
+  if constexpr (V > 0) {
+    constexpr int A = 16 / V;
     const int64_t n = s.rows * s.cols;
-    for (int64_t i0 = part * 1024 + threadIdx.x; i0 < n; i0 += kOrthParts * 1024) {
-      float v[4], m[4];
+    for (int64_t i0 = part * 4096 + threadIdx.x * V; i0 < n; i0 += kOrthParts * 4096) {
+      Words<T, V> v[A];
+      Words<float, V> m[A];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t i = i0 + q * 256;
-        v[q] = i < n ? as_f32(x[i]) : 0.0f;
-        m[q] = UPDATE && i < n ? mom[i] : 0.0f;
+      for (int q = 0; q < A; ++q) {
+        const int64_t i = min(i0 + q * 256 * V, n - V);   // past the end: read, and not used
+        v[q] = *(const Words<T, V>*)(x + i);
+        if (UPDATE) m[q] = *(const Words<float, V>*)(mom + i);
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        take(v[q], &m[q]);
-        if (UPDATE && i0 + q * 256 < n) mom[i0 + q * 256] = m[q];
-      }
+      for (int q = 0; q < A; ++q)
+        if (i0 + q * 256 * V < n) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) take(as_f32(v[q].v[e]), &m[q].v[e]);
+          if (UPDATE) *(Words<float, V>*)(mom + i0 + q * 256 * V) = m[q];
+        }
     }
   } else {
     for (int64_t r = part; r < s.rows; r += kOrthParts)
@@ -189,7 +195,7 @@ __device__ __forceinline__ void barrier_but() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// C = L R' on the TM x TN tile at (row, col) of matrix `mat`.  WR x WC
+// C = L R' on the TILE x TILE tile at (row, col) of matrix `mat`.  2 x WC
 // wavefronts share a tile; K runs in slices of KS through ST buffers in LDS,
 // ST - 1 slices on their way while one is multiplied.  KG = 2: a second group
 // of wavefronts takes every other slice, and the two sums are added at the end;
@@ -197,13 +203,13 @@ __device__ __forceinline__ void barrier_but() {
 // A slice's rows are KS / 8 chunks of 16 bytes without padding (memory goes to
 // LDS in lane order); chunk c of row r sits at c ^ (r / (128 / KS)), so the
 // rows of a fragment read different banks.
-template <int PL, int TM, int TN, int WR, int WC, int KS, int ST, int KG, int END, class T>
+template <int PL, int TILE, int WC, int KS, int ST, int KG, int END, class T>
 __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_t mat, int32_t trow, int32_t tcol) {
-  constexpr int NW = WR * WC, WM = TM / WR, WN = TN / WC, BI = WM / 32, BJ = WN / 32;
-  constexpr int CH = KS / 8, UL = PL * TM * CH / (64 * NW), UR = PL * TN * CH / (64 * NW);
-  static_assert(BI >= 1 && BJ >= 1 && UL >= 1 && UR >= 1, "work for every wavefront");
+  constexpr int NW = 2 * WC, WM = TILE / 2, WN = TILE / WC, BI = WM / 32, BJ = WN / 32;
+  constexpr int CH = KS / 8, U = PL * TILE * CH / (64 * NW);
+  static_assert(BI >= 1 && BJ >= 1 && U >= 1, "work for every wavefront");
   constexpr bool SYM = END == kEndGram || END == kEndPoly;
-  constexpr int LEFT = PL * TM * KS, SLAB = LEFT + PL * TN * KS;   // of one slice; lds: [KG][ST][SLAB]
+  constexpr int LEFT = PL * TILE * KS, SLAB = 2 * LEFT;   // of one slice; lds: [KG][ST][SLAB]
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % NW);
   const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW));
   const int wm = wave / WC, wn = wave % WC;
@@ -213,27 +219,18 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
   const half_t* R = g.r + mat * PL * rplane + (int64_t)tcol * KS;
   half_t* own = lds + group * ST * SLAB;
   // the lane's chunks of a slice, in values within a plane
-  uint32_t offl[UL], offr[UR];
+  uint32_t off[U];
 #pragma unroll
-  for (int q = 0; q < UL; ++q) {
-    const int i = (q * NW + wave) * 64 + lane, row = i / CH % TM;
-    offl[q] = (uint32_t)(row * KS + 8 * (i % CH ^ swizzle(row)));
-  }
-#pragma unroll
-  for (int q = 0; q < UR; ++q) {
-    const int i = (q * NW + wave) * 64 + lane, row = i / CH % TN;
-    offr[q] = (uint32_t)(row * KS + 8 * (i % CH ^ swizzle(row)));
+  for (int q = 0; q < U; ++q) {
+    const int i = (q * NW + wave) * 64 + lane, row = i / CH % TILE;
+    off[q] = (uint32_t)(row * KS + 8 * (i % CH ^ swizzle(row)));
   }
   const auto fetch = [&](int64_t slice, int buf) {
 #pragma unroll
-    for (int q = 0; q < UL; ++q) {
-      const int i0 = (q * NW + wave) * 64;
-      fetch_lds(L + i0 / (TM * CH) * lplane + slice * g.M * KS + offl[q], own + buf * SLAB + 8 * i0);
-    }
-#pragma unroll
-    for (int q = 0; q < UR; ++q) {
-      const int i0 = (q * NW + wave) * 64;
-      fetch_lds(R + i0 / (TN * CH) * rplane + slice * g.N * KS + offr[q], own + buf * SLAB + LEFT + 8 * i0);
+    for (int q = 0; q < U; ++q) {
+      const int i0 = (q * NW + wave) * 64, p = i0 / (TILE * CH);
+      fetch_lds(L + p * lplane + slice * g.M * KS + off[q], own + buf * SLAB + 8 * i0);
+      fetch_lds(R + p * rplane + slice * g.N * KS + off[q], own + buf * SLAB + LEFT + 8 * i0);
     }
   };
   floatx16 acc[BI][BJ];
@@ -250,7 +247,7 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
     const int32_t s = s0 + group;
     // everyone's part of slice s is in LDS (the later ones may be on their way), and the buffer of the slice
     // before is read
-    if (s0 + (ST - 1) * KG <= slices) barrier_but<(ST - 2) * (UL + UR)>();
+    if (s0 + (ST - 1) * KG <= slices) barrier_but<(ST - 2) * 2 * U>();
     else barrier_but<0>();
     const half_t *Ls = own + buf * SLAB, *Rs = Ls + LEFT;
     halfx8 a[KS / 16][PL][BI], b[KS / 16][PL][BJ];
@@ -263,12 +260,12 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
 #pragma unroll
           for (int i = 0; i < BI; ++i) {
             const int r = wm * WM + i * 32 + lane % 32;
-            a[ks][p][i] = *(const halfx8*)(Ls + (p * TM + r) * KS + 8 * (c ^ swizzle(r)));
+            a[ks][p][i] = *(const halfx8*)(Ls + (p * TILE + r) * KS + 8 * (c ^ swizzle(r)));
           }
 #pragma unroll
           for (int j = 0; j < BJ; ++j) {
             const int r = wn * WN + j * 32 + lane % 32;
-            b[ks][p][j] = *(const halfx8*)(Rs + (p * TN + r) * KS + 8 * (c ^ swizzle(r)));
+            b[ks][p][j] = *(const halfx8*)(Rs + (p * TILE + r) * KS + 8 * (c ^ swizzle(r)));
           }
         }
     }
@@ -362,42 +359,39 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
     }
 }
 
-// Tile number u of a matrix, from its top left corner: all tiles by columns of
-// tiles, or (SYM) those that reach the diagonal or lie above it.
-template <int TM, int TN, bool SYM>
-__device__ __forceinline__ void orth_place(uint32_t u, int32_t rows, int32_t& row, int32_t& col) {
-  const uint32_t tm = rows / TM;
-  uint32_t ti = u % tm, tj = u / tm;
-  if constexpr (SYM) {   // column tj has the tiles 0 .. tj / E
-    constexpr uint32_t E = TM / TN;
-    uint32_t g = (uint32_t)((sqrtf(8.0f * (u / E) + 1.0f) - 1.0f) * 0.5f);   // E columns have g + 1 tiles each
-    while (E * g * (g + 1) / 2 > u) --g;
-    while (E * (g + 1) * (g + 2) / 2 <= u) ++g;
-    const uint32_t left = u - E * g * (g + 1) / 2;
-    ti = left % (g + 1), tj = g * E + left / (g + 1);
+// Tile number u of a matrix: all tiles by columns, or (SYM) those on and above
+// the diagonal.
+template <bool SYM>
+__device__ __forceinline__ void orth_place(uint32_t u, uint32_t tm, uint32_t& ti, uint32_t& tj) {
+  ti = u % tm, tj = u / tm;
+  if constexpr (SYM) {
+    tj = (uint32_t)((sqrtf(8.0f * u + 1.0f) - 1.0f) * 0.5f);
+    while (tj * (tj + 1) / 2 > u) --tj;
+    while ((tj + 1) * (tj + 2) / 2 <= u) ++tj;
+    ti = u - tj * (tj + 1) / 2;
   }
-  row = (int32_t)ti * TM, col = (int32_t)tj * TN;
 }
 
-// `whole` tiles, and `over` ones in quarters.
-template <int PL, int TM, int TN, int WR, int WC, int KS, int ST, int KG, int END, class T>
-__global__ void __launch_bounds__(64 * WR * WC * KG) k_orth_gemm(OrthGemm g) {
+// `whole` tiles, and the others in quarters.
+template <int PL, int TILE, int WC, int KS, int ST, int KG, int END, class T>
+__global__ void __launch_bounds__(128 * WC * KG) k_orth_gemm(OrthGemm g) {
   constexpr bool SYM = END == kEndGram || END == kEndPoly;
   extern __shared__ __attribute__((aligned(16))) half_t orth_gemm_lds[];
   // workgroups i, i + 8.. run on one XCD: it gets a contiguous part of the
   // tiles, whose columns and rows it then finds in its L2
   const uint32_t share = (g.whole + 7) / 8;
-  int32_t row, col;
+  uint32_t ti, tj;
   if (blockIdx.x < share * 8) {
     const uint32_t tile = blockIdx.x % 8 * share + blockIdx.x / 8;
     if (tile >= g.whole) return;
-    orth_place<TM, TN, SYM>(tile % g.per, g.M, row, col);
-    orth_tile<PL, TM, TN, WR, WC, KS, ST, KG, END, T>(g, orth_gemm_lds, tile / g.per, row, col);
-  } else if constexpr (TM > 64) {
-    const uint32_t quarter = blockIdx.x - share * 8, tile = g.whole + quarter / 4;
-    orth_place<TM, TN, SYM>(tile % g.per, g.M, row, col);
-    row += (int32_t)(quarter & 1) * (TM / 2), col += (int32_t)(quarter >> 1 & 1) * (TN / 2);
-    if (SYM && row >= col + TN / 2) return;
-    orth_tile<PL, TM / 2, TN / 2, WR, WC, KS, ST, 1, END, T>(g, orth_gemm_lds, tile / g.per, row, col);
+    orth_place<SYM>(tile % g.per, g.M / TILE, ti, tj);
+    orth_tile<PL, TILE, WC, KS, ST, KG, END, T>(g, orth_gemm_lds, tile / g.per, ti * TILE, tj * TILE);
+  } else if constexpr (TILE > 64) {
+    constexpr uint32_t HALF = TILE / 2;
+    const uint32_t part = blockIdx.x - share * 8, tile = g.whole + part / 4;
+    orth_place<SYM>(tile % g.per, g.M / TILE, ti, tj);
+    ti = 2 * ti + part % 2, tj = 2 * tj + part / 2 % 2;
+    if (SYM && ti > tj) return;
+    orth_tile<PL, HALF, WC, KS, ST, 1, END, T>(g, orth_gemm_lds, tile / g.per, ti * HALF, tj * HALF);
   }
 }

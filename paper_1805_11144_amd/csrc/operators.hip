@@ -1,9 +1,3 @@
-#ifndef SYMR
-#define SYMR 1
-#endif
-#ifndef BIGT
-#define BIGT kCUs
-#endif
 // The operators on device arrays of the C ABI: argument checks, workspace
 // layouts and launches.  The kernels are in kernels_embed.hpp,
 // kernels_gated.hpp and kernels_orth.hpp.
@@ -289,9 +283,51 @@ void gated_clear(GatedArgs& a, const GatedWork& w, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------- orth
+constexpr int kCUs = 256;
+
+// Tiles that a product can take.
+enum OrthTile { kTile64, kTile128, kTile256 };
+
+// A launch's tiles: whole ones, and those computed in parts.  A few tiles more
+// than the CUs hold in whole rounds would take a round for themselves: up to
+// half a round of them is spread over the CUs in quarters.
+struct OrthTiles {
+  int64_t per, whole, over;
+};
+
+OrthTiles orth_tiles(OrthTile kind, bool sym, int64_t batch, int64_t rows, int64_t cols) {
+  const int64_t side = 64 << kind, r = (rows + side - 1) / side, c = (cols + side - 1) / side;
+  const int64_t per = sym ? r * (r + 1) / 2 : r * c, tiles = batch * per;
+  const int64_t over = kind != kTile64 && tiles > kCUs && tiles % kCUs <= kCUs / 2 ? tiles % kCUs : 0;
+  return {per, tiles - over, over};
+}
+
+// What a product takes with a kind of tile, in us for 4096 values of k: rounds
+// of the CUs times what one took on this card, for one part and two.
+double orth_cost(OrthTile kind, int parts, bool sym, int64_t batch, int64_t rows, int64_t cols) {
+  static const double round[2][3] = {{20, 38, 130}, {42, 112, 333}};
+  const OrthTiles t = orth_tiles(kind, sym, batch, rows, cols);
+  return ((double)((t.whole + kCUs - 1) / kCUs) + (t.over ? 0.3 : 0.0)) * round[parts - 1][kind];
+}
+
+// The cheapest tile whose sides divide `pad`: large ones read less, small ones
+// are more, for the CUs to share.
+OrthTile orth_choose(int64_t pad, int parts, bool sym, int64_t batch, int64_t rows, int64_t cols, double* cost) {
+  OrthTile best = kTile64;
+  double least = orth_cost(best, parts, sym, batch, rows, cols);
+  const auto offer = [&](OrthTile k) {
+    const double c = orth_cost(k, parts, sym, batch, rows, cols);
+    if (c < least) best = k, least = c;
+  };
+  if (pad >= 128) offer(kTile128);
+  if (pad >= 256) offer(kTile256);
+  if (cost) *cost = least;
+  return best;
+}
+
 struct Orth {
   int64_t n, m, np, mp;
-  int tile;
+  int64_t pad;            // to whole tiles of this side
   int parts;              // fp16 parts of a value
   double sx, sa, sq;      // scales of X, A and Q
   int64_t xm, xr, om, orow;
@@ -299,13 +335,13 @@ struct Orth {
   int64_t stride;         // of its rows there
 };
 
-constexpr int kCUs = 256;
 constexpr int64_t kOrthLds = 156 * 1024;   // of 160 KB
 
 Orth check_orth(const ms_orth_desc* d, bool update) {
   need(d != nullptr, "NULL descriptor");
   need(d->rows >= 1 && d->rows <= 65536 && d->cols >= 1 && d->cols <= 65536, "rows and cols must be in [1, 65536]");
   need(d->batch >= 0, "batch must not be negative");
+  need(d->batch <= kMaxBlocks, "too many matrices of this size");
   need(d->steps >= 1 && d->steps <= 100, "steps must be in [1, 100]");
   need_dtype(d->dtype);
   need(d->eps >= 0 && std::isfinite(d->eps), "eps must be finite and not negative");
@@ -321,9 +357,15 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
   o.n = std::min(d->rows, d->cols), o.m = std::max(d->rows, d->cols);
   o.parts = update || d->dtype == MS_DTYPE_F32 ? 2 : 1;
   // tiles of 128 x 128 read half as much; of 64 x 64 where the others would not fill the CUs
-  const auto tiles = [&](int64_t t) { return d->batch * ((o.n + t - 1) / t) * ((o.m + t - 1) / t); };
-  o.tile = tiles(256) >= BIGT ? 256 : tiles(128) >= kCUs ? 128 : 64;
-  o.np = up(o.n, o.tile), o.mp = up(o.m, o.tile);
+  double least = INFINITY;
+  for (int64_t pad : {64, 128, 256}) {   // larger tiles pad more
+    const int64_t n = up(o.n, pad), m = up(o.m, pad);
+    double square, next;
+    orth_choose(pad, o.parts, true, d->batch, n, n, &square);
+    orth_choose(pad, o.parts, false, d->batch, n, m, &next);
+    const double cost = square * (m + n) + next * n;
+    if (cost < least) least = cost, o.pad = pad, o.np = n, o.mp = m;
+  }
   need(d->batch <= kMaxBlocks / std::max<int64_t>(kOrthParts, (o.np / 64) * (o.mp / 64)), "too many matrices of this size");
   o.stride = up(o.m, 64) + 4;
   o.small = (int)up(o.n, 16) / 16;
@@ -380,59 +422,61 @@ OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
   return w;
 }
 
-constexpr int orth_slice(int pl, int pad) { return pad == 64 || pl == 2 ? 32 : 64; }
-
-// PAD: what the sides are padded to.  256 x 256 tiles read least; a symmetric
-// result has few of them, and takes 256 x 128.
-template <int PL, int PAD, int END, class T>
-void orth_gemm(OrthGemm g, int64_t batch, hipStream_t st) {
-  constexpr bool SYM = END == kEndGram || END == kEndPoly;
-  constexpr int TM = PAD, TN = PAD == 256 && SYM && SYMR ? 128 : PAD;
-  constexpr int WR = TM == 256 && TN == 128 ? 4 : 2, WC = TN == 256 ? 4 : 2;
-  constexpr int KS = orth_slice(PL, PAD), ST = PAD == 64 ? 3 : 2, KG = PAD == 64 ? 2 : 1;
-  constexpr size_t lds = KG * ST * PL * (TM + TN) * KS * sizeof(half_t);
-  static_assert(lds >= (KG - 1) * TM * TN * sizeof(float) && lds <= 160 * 1024, "LDS");
-  const int64_t tm = g.M / TM, tn = g.N / TN;
-  g.per = (uint32_t)(SYM ? TM / TN * tm * (tm + 1) / 2 : tm * tn);
-  // A few tiles more than the CUs hold in whole rounds would take a round for
-  // themselves: up to half a round of them is spread over the CUs in quarters.
-  const int64_t tiles = batch * g.per;
-  const int64_t over = PAD > 64 && tiles > kCUs && tiles % kCUs <= kCUs / 2 ? tiles % kCUs : 0;
-  g.whole = (uint32_t)(tiles - over);
-  constexpr auto k = k_orth_gemm<PL, TM, TN, WR, WC, KS, ST, KG, END, T>;
+template <int PL, int END, class T, int TILE, int WC, int ST, int KG>
+void orth_launch(OrthGemm g, const OrthTiles& t, hipStream_t st) {
+  constexpr size_t lds = KG * ST * PL * 2 * TILE * kOrthSlice * sizeof(half_t);
+  static_assert(lds >= (KG - 1) * TILE * TILE * sizeof(float) && lds <= 160 * 1024, "LDS");
+  g.per = (uint32_t)t.per, g.whole = (uint32_t)t.whole;
+  constexpr auto k = k_orth_gemm<PL, TILE, WC, kOrthSlice, ST, KG, END, T>;
   if (lds >= 65536) HIPCHECK(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-  hipLaunchKernelGGL(k, dim3((unsigned)(up(g.whole, 8) + 4 * over)), dim3(64 * WR * WC * KG), lds, st, g);
+  hipLaunchKernelGGL(k, dim3((unsigned)(up(t.whole, 8) + 4 * t.over)), dim3(128 * WC * KG), lds, st, g);
+}
+
+template <int PL, int END, class T>
+void orth_gemm(const OrthGemm& g, int64_t pad, int64_t batch, hipStream_t st) {
+  constexpr bool SYM = END == kEndGram || END == kEndPoly;
+  constexpr int DEEP = PL == 1 ? 4 : 2;   // slices in LDS
+  const OrthTile kind = orth_choose(pad, PL, SYM, batch, g.M, g.N, nullptr);
+  const OrthTiles t = orth_tiles(kind, SYM, batch, g.M, g.N);
+  if (kind == kTile64) orth_launch<PL, END, T, 64, 2, 3, 2>(g, t, st);
+  else if (kind == kTile128) orth_launch<PL, END, T, 128, 2, DEEP, 1>(g, t, st);
+  else orth_launch<PL, END, T, 256, 4, DEEP, 1>(g, t, st);
 }
 
 // T: type of x (or the gradient); UPDATE: with momentum, into a weight.
-template <class T, bool UPDATE, int PL, int TILE>
+template <class T, bool UPDATE, int PL>
 void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, OrthGemm out, hipStream_t st) {
   const int64_t blocks = d->batch * (o.np / 64) * (o.mp / 64);
   const dim3 norms((unsigned)(d->batch * kOrthParts));
-  if (src.row == src.cols)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE, true>), norms, dim3(256), 0, st, src, w.parts);
-  else
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE, false>), norms, dim3(256), 0, st, src, w.parts);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, PL, orth_slice(PL, TILE)>), dim3((unsigned)blocks), dim3(256), 0, st, src,
+  const auto norm = [&](auto width) {
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE, decltype(width)::value>), norms, dim3(256), 0, st, src, w.parts);
+  };
+  // packed matrices as one run of values, four at a time where that is aligned
+  if (src.row != src.cols) norm(std::integral_constant<int, 0>{});
+  else if (src.rows * src.cols % 4 == 0 && src.mat % 4 == 0 && (uintptr_t)src.x % (4 * sizeof(T)) == 0 &&
+           (uintptr_t)src.momentum % 16 == 0)
+    norm(std::integral_constant<int, 4>{});
+  else norm(std::integral_constant<int, 1>{});
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, PL, kOrthSlice>), dim3((unsigned)blocks), dim3(256), 0, st, src,
                      (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], (int32_t)o.np, (int32_t)o.mp);
   using R = std::conditional_t<UPDATE, float, T>;
   for (int k = 0; k < d->steps; ++k) {
     OrthGemm g{};
     g.l = g.r = w.x, g.M = g.N = (int32_t)o.np, g.K = (int32_t)o.mp, g.c = w.a;
     g.f = (float)(o.sa / (o.sx * o.sx));
-    orth_gemm<PL, TILE, kEndGram, R>(g, d->batch, st);
+    orth_gemm<PL, kEndGram, R>(g, o.pad, d->batch, st);
     g.l = g.r = w.a, g.K = (int32_t)o.np, g.c = w.q, g.a = w.a;
     g.f = (float)(d->coef[2] * o.sq / (o.sa * o.sa));
     g.c0 = (float)(d->coef[0] * o.sq), g.c1 = (float)(d->coef[1] * o.sq / o.sa);
-    orth_gemm<PL, TILE, kEndPoly, R>(g, d->batch, st);
+    orth_gemm<PL, kEndPoly, R>(g, o.pad, d->batch, st);
     OrthGemm x = out;
     x.l = w.q, x.r = w.t[k % 2], x.M = (int32_t)o.np, x.N = (int32_t)o.mp, x.K = (int32_t)o.np;
     if (k + 1 < d->steps) {
       x.c = w.x, x.ct = w.t[(k + 1) % 2], x.f = (float)(1.0 / o.sq);
-      orth_gemm<PL, TILE, kEndNext, R>(x, d->batch, st);
+      orth_gemm<PL, kEndNext, R>(x, o.pad, d->batch, st);
     } else {
       x.f = (float)(1.0 / (o.sq * o.sx));
-      orth_gemm<PL, TILE, UPDATE ? kEndUpdate : kEndOut, R>(x, d->batch, st);
+      orth_gemm<PL, UPDATE ? kEndUpdate : kEndOut, R>(x, o.pad, d->batch, st);
     }
   }
   HIPCHECK(hipGetLastError());
@@ -467,9 +511,7 @@ template <class T, bool UPDATE, int PL>
 void orth(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, const OrthGemm& out,
                 hipStream_t st) {
   if (o.small) orth_small<T, UPDATE>(d, o, src, out, st);
-  else if (o.tile == 256) orth_run<T, UPDATE, PL, 256>(d, o, src, w, out, st);
-  else if (o.tile == 128) orth_run<T, UPDATE, PL, 128>(d, o, src, w, out, st);
-  else orth_run<T, UPDATE, PL, 64>(d, o, src, w, out, st);
+  else orth_run<T, UPDATE, PL>(d, o, src, w, out, st);
 }
 
 }  // namespace
