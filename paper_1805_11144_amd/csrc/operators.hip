@@ -630,7 +630,7 @@ ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* d, const void* v, const 
     if (a.batch == 0) return;
     const size_t es = size_of(d->dtype);
     need(a.yt >= a.dim || a.steps <= 1, "the steps of y must not overlap");
-    need(a.yb >= a.dim || a.batch <= 1, "the rows of y must not overlap");
+    need(a.yb >= a.dim || a.batch <= 1 || a.steps == 0, "the rows of y must not overlap");
     need(a.steps == 0 || (v && g && y), "NULL array");
     for (const void* q : {v, g, (const void*)y}) need_aligned(q, es, "v, g or y");
     for (const void* q : {(const void*)y0, (const void*)lengths, (const void*)last, (const void*)kept})

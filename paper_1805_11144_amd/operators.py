@@ -15,99 +15,116 @@ from .mergesim import (DTYPE_BF16, DTYPE_F32, IDS_I32, IDS_I64, EmbedDesc, Gated
 
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)   # raises small singular values fast; leaves them within 0.3 of one
 
-_state = {}
+_torch = _lib = _stream = None
+_DTYPES, _IDS = {}, {}
 
 
 def _setup():
-    """(torch, library): checked once that they share one HIP runtime."""
-    if not _state:
-        import torch
-        lib = _ms.load_library()
-        with open("/proc/self/maps") as f:
-            runtimes = {line.split()[-1] for line in f if "libamdhip64" in line}
-        if len(runtimes) > 1:
-            raise ImportError("the library was loaded with another HIP runtime than torch's: import torch first "
-                              f"({', '.join(sorted(runtimes))})")
-        _state["dtypes"] = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
-        _state["ids"] = {torch.int32: IDS_I32, torch.int64: IDS_I64}
-        _state["both"] = torch, lib
-    return _state["both"]
+    """Loads torch and the library, once, and checks that they share one HIP runtime."""
+    global _torch, _lib, _stream
+    import torch
+    lib = _ms.load_library()
+    with open("/proc/self/maps") as f:
+        runtimes = {line.split()[-1] for line in f if "libamdhip64" in line}
+    if len(runtimes) > 1:
+        raise ImportError("the library was loaded with another HIP runtime than torch's: import torch first "
+                          f"({', '.join(sorted(runtimes))})")
+    _DTYPES.update({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16})
+    _IDS.update({torch.int32: IDS_I32, torch.int64: IDS_I64})
+    # the current stream's handle without a Stream object around it: 2 of the 11 us of a small call
+    _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    _torch, _lib = torch, lib
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
-
-
-def _dtype(t, name):
-    d = _state["dtypes"].get(t.dtype)
-    _need(d is not None, f"{name} is {t.dtype}: float32 or bfloat16 is wanted")
+def _gpu(t, dims, what):
+    if _lib is None:
+        _setup()
+    if not t.is_cuda or t.dim() not in dims:
+        raise ValueError(f"{what} on a GPU is wanted, not {tuple(t.shape)} on {t.device}")
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise ValueError(f"{what} is {t.dtype}: float32 or bfloat16 is wanted")
     return d
 
 
-def _like(t, first, name, shape=None, dtype=None):
-    """Checks a tensor's device, and its shape and type where given."""
-    _need(t.is_cuda and t.device == first.device, f"{name} must be on the GPU of the other arrays ({first.device})")
-    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} has shape {tuple(t.shape)}, not {shape}")
-    _need(dtype is None or t.dtype == dtype, f"{name} is {t.dtype}, not {dtype}")
+def _like(t, first, name, shape, dtype):
+    """Checks a tensor's device, shape and type."""
+    if t.device != first.device:
+        raise ValueError(f"{name} must be on the GPU of the other arrays ({first.device}), not on {t.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+    return t
 
 
-def _packed(t, name):
-    _need(t.is_contiguous(), f"{name} must be contiguous")
+def _packed(t, first, name, shape, dtype):
+    """The address of a contiguous tensor, or None for None."""
+    if t is None:
+        return None
+    if not _like(t, first, name, shape, dtype).is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _on(d, t, torch):
+def _on(d, t):
     """The descriptor's device and stream: torch's current one there."""
     d.device = t.device.index
-    d.stream = torch.cuda.current_stream(t.device).cuda_stream
+    d.stream = _stream(d.device)
     return C.byref(d)
 
 
 def _row_stride(t, name):
     """Elements between the rows of a matrix [n, dim] whose rows are contiguous."""
     n, dim = t.shape
-    _need(dim == 1 or t.stride(1) == 1, f"{name}'s rows must be contiguous")
+    rows, cols = t.stride()
+    if dim > 1 and cols != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
     if n <= 1:
         return dim
-    _need(t.stride(0) >= dim, f"{name}'s rows overlap")
-    return t.stride(0)
+    if rows < dim:
+        raise ValueError(f"{name}'s rows overlap")
+    return rows
 
 
-def _scratch(torch, like, call, *args):
-    """Scratch memory of the size that `call` names."""
+def _scratch(t, n):
+    """(tensor, address, bytes) of n bytes of scratch memory on t's GPU."""
+    if n == 0:
+        return None, None, 0
+    w = _torch.empty(n, dtype=_torch.uint8, device=t.device)
+    return w, w.data_ptr(), n
+
+
+def _size(call, *args):
     n = C.c_int64()
     _check(call(*args, C.byref(n)))
-    if n.value == 0:
-        return None, None, 0
-    w = torch.empty(n.value, dtype=torch.uint8, device=like.device)
-    return w, w.data_ptr(), n.value
+    return n.value
 
 
 # ------------------------------------------------------------------------ tables
-def _embed_desc(torch, tokens, rows, table_stride, row_stride, vocab, scale):
-    d = EmbedDesc()
-    ids = _state["ids"].get(tokens.dtype)
-    _need(ids is not None, f"tokens are {tokens.dtype}: int32 or int64 is wanted")
-    d.n_tokens, d.vocab, d.dim = tokens.numel(), vocab, rows.shape[-1]
-    d.table_stride, d.row_stride, d.scale, d.ids, d.dtype = table_stride, row_stride, scale, ids, _dtype(rows, "rows")
-    return d
+def _embed_desc(tokens, first):
+    if tokens.device != first.device:
+        raise ValueError(f"tokens must be on the GPU of the other arrays ({first.device}), not on {tokens.device}")
+    ids = _IDS.get(tokens.dtype)
+    if ids is None:
+        raise ValueError(f"tokens are {tokens.dtype}: int32 or int64 is wanted")
+    return EmbedDesc(n_tokens=tokens.numel(), ids=ids)
 
 
 def embed(tokens, table, scale=1.0, out=None):
     """out[..., :] = scale * table[tokens[...], :], zeros for tokens outside the table (ms_embed).
 
     tokens: int32 or int64 of any shape; table [vocab, dim] float32 or bfloat16."""
-    torch, lib = _setup()
-    _need(table.is_cuda and table.dim() == 2, "table must be a matrix on a GPU")
-    _like(tokens, table, "tokens")
+    dtype = _gpu(table, (2,), "a table [vocab, dim]")
+    d = _embed_desc(tokens, table)
     tokens = tokens.contiguous()
     shape = (*tokens.shape, table.shape[1])
     if out is None:
-        out = torch.empty(shape, dtype=table.dtype, device=table.device)
-    _like(out, table, "out", shape, table.dtype)
-    d = _embed_desc(torch, tokens, table, _row_stride(table, "table"), 0, table.shape[0], scale)
-    _check(lib.ms_embed(_on(d, table, torch), tokens.data_ptr(), table.data_ptr(), _packed(out, "out")))
+        out = _torch.empty(shape, dtype=table.dtype, device=table.device)
+    d.vocab, d.dim = table.shape
+    d.table_stride, d.scale, d.dtype = _row_stride(table, "table"), scale, dtype
+    _check(_lib.ms_embed(_on(d, table), tokens.data_ptr(), table.data_ptr(),
+                         _packed(out, table, "out", shape, table.dtype)))
     return out
 
 
@@ -116,56 +133,48 @@ def embed_grad(tokens, drows, vocab=None, scale=1.0, out=None, accumulate=False)
     rows of drows [*tokens.shape, dim], in an order that depends on the tokens alone.
 
     float32, or the type of `out`; accumulate: added to what `out` holds."""
-    torch, lib = _setup()
-    _need(drows.is_cuda and drows.dim() >= 1, "drows must be on a GPU")
+    dtype = _gpu(drows, range(1, 64), "drows [*tokens.shape, dim]")
     dim = drows.shape[-1]
-    _like(drows, drows, "drows", (*tokens.shape, dim))
-    _like(tokens, drows, "tokens")
-    _need(out is not None or not accumulate, "accumulate needs out")
+    d = _embed_desc(tokens, drows)
+    _like(drows, drows, "drows", (*tokens.shape, dim), drows.dtype)
     if out is None:
-        _need(vocab is not None, "vocab or out is wanted")
-        out = torch.empty((vocab, dim), dtype=torch.float32, device=drows.device)
-    _like(out, drows, "out", (out.shape[0] if vocab is None else vocab, dim))
+        if accumulate or vocab is None:
+            raise ValueError("accumulate needs out" if accumulate else "vocab or out is wanted")
+        out = _torch.empty((vocab, dim), dtype=_torch.float32, device=drows.device)
+    grad_dtype = _gpu(out, (2,), "out [vocab, dim]")
+    _like(out, drows, "out", (out.shape[0] if vocab is None else vocab, dim), out.dtype)
     tokens, rows = tokens.contiguous(), drows.reshape(-1, dim)
     if rows.shape[0] > 1 and (rows.stride(0) < dim or (dim > 1 and rows.stride(1) != 1)):
         rows = rows.contiguous()   # a broadcast gradient
-    d = _embed_desc(torch, tokens, rows, _row_stride(out, "out"), _row_stride(rows, "drows"), out.shape[0], scale)
-    d.grad_dtype, d.accumulate = _dtype(out, "out"), int(bool(accumulate))
-    ref = _on(d, drows, torch)
-    keep, ws, n = _scratch(torch, drows, lib.ms_embed_grad_workspace, ref)
-    _check(lib.ms_embed_grad(ref, tokens.data_ptr(), rows.data_ptr(), out.data_ptr(), ws, n))
+    d.vocab, d.dim = out.shape
+    d.table_stride, d.row_stride = _row_stride(out, "out"), _row_stride(rows, "drows")
+    d.scale, d.dtype, d.grad_dtype, d.accumulate = scale, dtype, grad_dtype, int(bool(accumulate))
+    ref = _on(d, drows)
+    hold, ws, n = _scratch(drows, _size(_lib.ms_embed_grad_workspace, ref))
+    _check(_lib.ms_embed_grad(ref, tokens.data_ptr(), rows.data_ptr(), out.data_ptr(), ws, n))
     return out
 
 
 # ----------------------------------------------------------------- gated lowpass
-def _sequence(t, name):
-    """(tensor, [batch stride, step stride]) of [batch, steps, dim] with contiguous channels."""
+def _sequence(t, strides):
+    """[batch, steps, dim] with contiguous channels, its strides written down; copied where they cannot be
+    (two strides of 0 stand for a packed array)."""
+    if t.is_contiguous():
+        return t
     batch, steps, dim = t.shape
-    _need(dim >= 1, f"{name} has no channels")
     sb, ss = t.stride(0) if batch > 1 else 0, t.stride(1) if steps > 1 else 0
-    if (dim > 1 and t.stride(2) != 1) or (batch * steps > 1 and sb == ss == 0):
-        t = t.contiguous()
-        sb = ss = 0
-    return t, (sb, ss)
+    if (dim > 1 and t.stride(2) != 1) or sb == ss == 0:
+        return t.contiguous()
+    strides[0], strides[1] = sb, ss
+    return t
 
 
 def _gated_desc(v, g, y):
-    _need(v.is_cuda and v.dim() == 3, "v must be [batch, steps, dim] on a GPU")
+    dtype = _gpu(v, (3,), "v [batch, steps, dim]")
     _like(g, v, "g", v.shape, v.dtype)
-    d = GatedLowpassDesc()
-    d.batch, d.steps, d.dim = v.shape
-    d.dtype = _dtype(v, "v")
-    v, (d.v_stride[0], d.v_stride[1]) = _sequence(v, "v")
-    g, (d.g_stride[0], d.g_stride[1]) = _sequence(g, "g")
-    y, (d.y_stride[0], d.y_stride[1]) = _sequence(y, "y")
-    return d, v, g, y
-
-
-def _optional(torch, t, v, name, shape, dtype):
-    if t is None:
-        return None
-    _like(t, v, name, shape, dtype)
-    return _packed(t, name)
+    batch, steps, dim = v.shape
+    d = GatedLowpassDesc(batch=batch, steps=steps, dim=dim, dtype=dtype)
+    return d, _sequence(v, d.v_stride), _sequence(g, d.g_stride), y if y is None else _sequence(y, d.y_stride)
 
 
 def gated_lowpass(v, g, y0=None, lengths=None, keep=False):
@@ -175,46 +184,36 @@ def gated_lowpass(v, g, y0=None, lengths=None, keep=False):
     v, g [batch, steps, dim], float32 or bfloat16; y0 [batch, dim] float32; lengths int32 [batch].
     Returns (y, last): y like v, zeros past a row's length, and the state after its last step, float32.
     keep: also the states that gated_lowpass_grad starts from."""
-    torch, lib = _setup()
-    _need(v.is_cuda and v.dim() == 3, "v must be [batch, steps, dim] on a GPU")
+    d, v, g, _ = _gated_desc(v, g, None)
     batch, steps, dim = v.shape
-    y = torch.empty((batch, steps, dim), dtype=v.dtype, device=v.device)
-    last = torch.empty((batch, dim), dtype=torch.float32, device=v.device)
-    d, v, g, y = _gated_desc(v, g, y)
-    ref = _on(d, v, torch)
-    kept = None
-    if keep:
-        n = C.c_int64()
-        _check(lib.ms_gated_lowpass_kept(ref, C.byref(n)))
-        kept = torch.empty(n.value, dtype=torch.float32, device=v.device)
-    hold, ws, n = _scratch(torch, v, lib.ms_gated_lowpass_workspace, ref)
-    _check(lib.ms_gated_lowpass(ref, v.data_ptr(), g.data_ptr(),
-                                _optional(torch, y0, v, "y0", (batch, dim), torch.float32),
-                                _optional(torch, lengths, v, "lengths", (batch,), torch.int32),
-                                y.data_ptr(), last.data_ptr(), None if kept is None else kept.data_ptr(), ws, n))
+    f32 = _torch.float32
+    y = _torch.empty((batch, steps, dim), dtype=v.dtype, device=v.device)
+    last = _torch.empty((batch, dim), dtype=f32, device=v.device)
+    y0p, lp = _packed(y0, v, "y0", (batch, dim), f32), _packed(lengths, v, "lengths", (batch,), _torch.int32)
+    ref = _on(d, v)
+    kept = _torch.empty(_size(_lib.ms_gated_lowpass_kept, ref), dtype=f32, device=v.device) if keep else None
+    hold, ws, n = _scratch(v, _size(_lib.ms_gated_lowpass_workspace, ref))
+    _check(_lib.ms_gated_lowpass(ref, v.data_ptr(), g.data_ptr(), y0p, lp, y.data_ptr(), last.data_ptr(),
+                                 kept.data_ptr() if keep else None, ws, n))
     return (y, last, kept) if keep else (y, last)
 
 
 def gated_lowpass_grad(v, g, kept, dy, dlast=None, lengths=None):
     """(dv, dg, dy0) of gated_lowpass from dL/dy and dL/dlast (ms_gated_lowpass_grad); kept: what the forward
     call with keep=True left."""
-    torch, lib = _setup()
-    _need(v.is_cuda and v.dim() == 3, "v must be [batch, steps, dim] on a GPU")
+    d, v, g, dy = _gated_desc(v, g, dy)
     _like(dy, v, "dy", v.shape, v.dtype)
     batch, steps, dim = v.shape
-    dv = torch.empty((batch, steps, dim), dtype=v.dtype, device=v.device)
-    dg = torch.empty_like(dv)
-    dy0 = torch.empty((batch, dim), dtype=torch.float32, device=v.device)
-    d, v, g, dy = _gated_desc(v, g, dy)
-    ref = _on(d, v, torch)
-    n = C.c_int64()
-    _check(lib.ms_gated_lowpass_kept(ref, C.byref(n)))
-    _like(kept, v, "kept", (n.value,), torch.float32)
-    hold, ws, n = _scratch(torch, v, lib.ms_gated_lowpass_workspace, ref)
-    _check(lib.ms_gated_lowpass_grad(ref, v.data_ptr(), g.data_ptr(), _packed(kept, "kept"),
-                                     _optional(torch, lengths, v, "lengths", (batch,), torch.int32), dy.data_ptr(),
-                                     _optional(torch, dlast, v, "dlast", (batch, dim), torch.float32),
-                                     dv.data_ptr(), dg.data_ptr(), dy0.data_ptr(), ws, n))
+    f32 = _torch.float32
+    dv = _torch.empty((batch, steps, dim), dtype=v.dtype, device=v.device)
+    dg = _torch.empty((batch, steps, dim), dtype=v.dtype, device=v.device)
+    dy0 = _torch.empty((batch, dim), dtype=f32, device=v.device)
+    ref = _on(d, v)
+    keptp = _packed(kept, v, "kept", (_size(_lib.ms_gated_lowpass_kept, ref),), f32)
+    lp, dlp = _packed(lengths, v, "lengths", (batch,), _torch.int32), _packed(dlast, v, "dlast", (batch, dim), f32)
+    hold, ws, n = _scratch(v, _size(_lib.ms_gated_lowpass_workspace, ref))
+    _check(_lib.ms_gated_lowpass_grad(ref, v.data_ptr(), g.data_ptr(), keptp, lp, dy.data_ptr(), dlp, dv.data_ptr(),
+                                      dg.data_ptr(), dy0.data_ptr(), ws, n))
     return dv, dg, dy0
 
 
@@ -222,50 +221,47 @@ def gated_lowpass_step(v, g, state, slots=None, out=None):
     """One step for the sequences being served (ms_gated_lowpass_step): row i of v, g [rows, dim] advances
     state[slots[i]] (float32 [slots, dim], in place; row i's own slot without `slots`, int32) and returns it in
     v's type; a slot outside the cache marks an idle row, whose result is zeros."""
-    torch, lib = _setup()
-    _need(v.is_cuda and v.dim() == 2, "v must be [rows, dim] on a GPU")
-    rows, dim = v.shape
-    _like(g, v, "g", v.shape, v.dtype)
-    _like(state, v, "state", (state.shape[0], dim), torch.float32)
+    dtype = _gpu(v, (2,), "v [rows, dim]")
+    rows, dim = shape = v.shape
+    _like(g, v, "g", shape, v.dtype)
+    _like(state, v, "state", (state.shape[0], dim), _torch.float32)
     if out is None:
-        out = torch.empty((rows, dim), dtype=v.dtype, device=v.device)
-    _like(out, v, "out", v.shape, v.dtype)
-    d = GatedStepDesc()
-    d.rows, d.n_slots, d.dim, d.dtype = rows, state.shape[0], dim, _dtype(v, "v")
-    d.v_stride, d.g_stride = _row_stride(v, "v"), _row_stride(g, "g")
-    d.y_stride, d.state_stride = _row_stride(out, "out"), _row_stride(state, "state")
-    _check(lib.ms_gated_lowpass_step(_on(d, v, torch), v.data_ptr(), g.data_ptr(), state.data_ptr(),
-                                     _optional(torch, slots, v, "slots", (rows,), torch.int32), out.data_ptr()))
+        out = _torch.empty((rows, dim), dtype=v.dtype, device=v.device)
+    else:
+        _like(out, v, "out", shape, v.dtype)
+    d = GatedStepDesc(rows, state.shape[0], dim, _row_stride(v, "v"), _row_stride(g, "g"), _row_stride(out, "out"),
+                      _row_stride(state, "state"), dtype)
+    _check(_lib.ms_gated_lowpass_step(_on(d, v), v.data_ptr(), g.data_ptr(), state.data_ptr(),
+                                      _packed(slots, v, "slots", (rows,), _torch.int32), out.data_ptr()))
     return out
 
 
 # ---------------------------------------------------------- orthogonalised updates
 def _orth_desc(x, steps, coefficients, eps):
-    _need(x.is_cuda and x.dim() in (2, 3), "a matrix or a batch of matrices on a GPU is wanted")
-    d = OrthDesc()
+    dtype = _gpu(x, (2, 3), "a matrix or a batch of matrices")
     rows, cols = x.shape[-2:]
     batch = x.shape[0] if x.dim() == 3 else 1
-    if (cols > 1 and x.stride(-1) != 1) or (rows > 1 and x.stride(-2) < cols):
-        x = x.contiguous()
-    d.batch, d.rows, d.cols = batch, rows, cols
-    d.x_stride[1] = x.stride(-2) if rows > 1 else cols
-    d.x_stride[0] = x.stride(0) if x.dim() == 3 and batch > 1 else 0
-    d.coef[0], d.coef[1], d.coef[2] = coefficients
-    d.eps, d.steps, d.dtype = eps, steps, _dtype(x, "x")
+    d = OrthDesc(batch=batch, rows=rows, cols=cols, eps=eps, steps=steps, dtype=dtype)
+    d.coef[:] = coefficients
+    if not x.is_contiguous():
+        if (cols > 1 and x.stride(-1) != 1) or (rows > 1 and x.stride(-2) < cols):
+            x = x.contiguous()
+        else:
+            d.x_stride[1] = x.stride(-2) if rows > 1 else cols
+            d.x_stride[0] = x.stride(0) if x.dim() == 3 and batch > 1 else 0
     return d, x
 
 
 def orthogonalise(x, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, out=None):
     """Brings the singular values of a matrix [rows, cols], or of each of a batch, towards one
     (ms_orthogonalise): X <- (c0 I + c1 XX' + c2 XX'XX') X, `steps` times from X / (|X| + eps)."""
-    torch, lib = _setup()
     d, x = _orth_desc(x, steps, coefficients, eps)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _like(out, x, "out", x.shape, x.dtype)
-    ref = _on(d, x, torch)
-    hold, ws, n = _scratch(torch, x, lib.ms_orth_workspace, ref, 0)
-    _check(lib.ms_orthogonalise(ref, x.data_ptr(), _packed(out, "out"), ws, n))
+        out = _torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    outp = _packed(out, x, "out", x.shape, x.dtype)
+    ref = _on(d, x)
+    hold, ws, n = _scratch(x, _size(_lib.ms_orth_workspace, ref, 0))
+    _check(_lib.ms_orthogonalise(ref, x.data_ptr(), outp, ws, n))
     return out
 
 
@@ -276,12 +272,10 @@ def orthogonal_update(weight, momentum, grad, rate, momentum_decay=0.95, weight_
     momentum_decay momentum), or of the momentum alone without nesterov.
 
     weight, momentum: float32, contiguous; grad: float32 or bfloat16."""
-    torch, lib = _setup()
     d, grad = _orth_desc(grad, steps, coefficients, eps)
-    _like(weight, grad, "weight", grad.shape, torch.float32)
-    _like(momentum, grad, "momentum", grad.shape, torch.float32)
+    f32 = _torch.float32
+    wp, mp = _packed(weight, grad, "weight", grad.shape, f32), _packed(momentum, grad, "momentum", grad.shape, f32)
     rule = OrthRule(rate, momentum_decay, weight_decay, int(bool(nesterov)))
-    ref = _on(d, grad, torch)
-    hold, ws, n = _scratch(torch, grad, lib.ms_orth_workspace, ref, 1)
-    _check(lib.ms_orthogonal_update(ref, C.byref(rule), _packed(weight, "weight"), _packed(momentum, "momentum"),
-                                    grad.data_ptr(), ws, n))
+    ref = _on(d, grad)
+    hold, ws, n = _scratch(grad, _size(_lib.ms_orth_workspace, ref, 1))
+    _check(_lib.ms_orthogonal_update(ref, C.byref(rule), wp, mp, grad.data_ptr(), ws, n))
