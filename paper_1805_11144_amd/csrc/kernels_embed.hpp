@@ -6,7 +6,7 @@
 // The gradient adds the rows of equal tokens.  Atomic additions would make
 // their order, and so the last bits, depend on timing; here (token, position)
 // pairs are brought into token order by a stable radix sort (least significant
-// digit first, 8 bits a pass), so each table row is the sum of a run of
+// digit first, 8 to 10 bits a pass), so each table row is the sum of a run of
 // positions in ascending order.
 #pragma once
 
@@ -91,14 +91,15 @@ __global__ void __launch_bounds__(256) k_embed(const I* tokens, const T* table, 
 // ------------------------------------------------------------------ sort
 constexpr int kSortBits = 10;   // of a digit, at most
 
-// A digit has at most 8 + log2 PER bits; counters come in rows of 256 PER.  A
-// tile is 256 N pairs.
+// A digit has BITS bits, 8 to 10, and counters come in rows of 256 PER = 2^BITS.
+// A tile is 256 N pairs.
 
-// How many of a tile's keys have each digit (`bits` bits at `shift`), to
+// How many of a tile's keys have each digit at `shift`, to
 // counts[tile][digit].  The first pass reads the tokens (keys == NULL).
-template <class I, int PER, int N>
+template <class I, int BITS, int N>
 __global__ void __launch_bounds__(256) k_sort_count(const I* tokens, const uint32_t* keys, int64_t n, int64_t vocab,
-                                                    int shift, int bits, uint32_t* counts) {
+                                                    int shift, uint32_t* counts) {
+  constexpr int PER = 1 << (BITS - 8);
   __shared__ uint32_t hist[256 * PER];
 #pragma unroll
   for (int q = 0; q < PER; ++q) hist[q * 256 + threadIdx.x] = 0;
@@ -112,7 +113,7 @@ __global__ void __launch_bounds__(256) k_sort_count(const I* tokens, const uint3
   }
 #pragma unroll
   for (int k = 0; k < N; ++k)
-    if (base + k * 256 + threadIdx.x < n) atomicAdd(&hist[(key[k] >> shift) & ((1u << bits) - 1)], 1u);
+    if (base + k * 256 + threadIdx.x < n) atomicAdd(&hist[(key[k] >> shift) & ((1u << BITS) - 1)], 1u);
   __syncthreads();
 #pragma unroll
   for (int q = 0; q < PER; ++q)
@@ -120,9 +121,11 @@ __global__ void __launch_bounds__(256) k_sort_count(const I* tokens, const uint3
 }
 
 // The lanes of a wavefront that hold live keys of this lane's digit.
-__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool live) {
+template <int BITS>
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, bool live) {
   uint64_t same = __ballot(live);
-  for (int b = 0; b < bits; ++b) {
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
     const uint64_t set = __ballot((d >> b) & 1);
     same &= (d >> b) & 1 ? set : ~set;
   }
@@ -131,15 +134,15 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool live) 
 
 // Ranks a wavefront's keys, item by item, among its earlier keys of the same
 // digit; count[digit] ends as their number.
-template <int N>
+template <int BITS, int N>
 __device__ __forceinline__ void rank_keys(const uint32_t* key, uint32_t* rank, uint32_t* count, int64_t base, int64_t n,
-                                          int shift, int bits) {
+                                          int shift) {
   const int lane = threadIdx.x % 64;
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const bool live = base + k * 64 + lane < n;
-    const uint32_t d = (key[k] >> shift) & ((1u << bits) - 1);
-    const uint64_t same = same_digit(d, bits, live), lower = same & ((1ull << lane) - 1);
+    const uint32_t d = (key[k] >> shift) & ((1u << BITS) - 1);
+    const uint64_t same = same_digit<BITS>(d, live), lower = same & ((1ull << lane) - 1);
     const uint32_t seen = count[d];   // every lane reads before the digit's first lane adds
     wave_order();
     rank[k] = seen + __popcll(lower);
@@ -161,10 +164,11 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
 // Moves each pair to its place: behind the pairs of smaller digits, of earlier
 // tiles and of earlier positions in the tile.  Wavefront w holds the tile's
 // positions [w * 64 N, (w + 1) * 64 N) in order of (item, lane).
-template <class I, int PER, int N>
+template <class I, int BITS, int N>
 __global__ void __launch_bounds__(256) k_sort_move(const I* tokens, const uint32_t* keys, const uint32_t* pos,
-                                                   int64_t n, int64_t vocab, int shift, int bits,
-                                                   const uint32_t* counts, uint32_t* keys_out, uint32_t* pos_out) {
+                                                   int64_t n, int64_t vocab, int shift, const uint32_t* counts,
+                                                   uint32_t* keys_out, uint32_t* pos_out) {
+  constexpr int PER = 1 << (BITS - 8);
   __shared__ uint32_t part[4][256 * PER];   // a wavefront's pairs of each digit, then where its first one goes
   __shared__ uint32_t first[256 * PER];     // pairs of each digit in all tiles, then of smaller digits
   __shared__ uint32_t sums[4];
@@ -218,7 +222,7 @@ __global__ void __launch_bounds__(256) k_sort_move(const I* tokens, const uint32
   for (int q = 0; q < PER; ++q) own[q] = first[tid * PER + q], all += own[q];
   const uint32_t incl = wave_prefix(all);
   if (lane == 63) sums[wave] = incl;
-  rank_keys<N>(key, rank, part[wave], base, n, shift, bits);
+  rank_keys<BITS, N>(key, rank, part[wave], base, n, shift);
   __syncthreads();
   uint32_t lower = incl - all;
   for (int w = 0; w < wave; ++w) lower += sums[w];
@@ -243,16 +247,16 @@ __global__ void __launch_bounds__(256) k_sort_move(const I* tokens, const uint32
 #pragma unroll
   for (int k = 0; k < N; ++k)
     if (base + k * 64 + lane < n) {
-      const uint32_t at = part[wave][(key[k] >> shift) & ((1u << bits) - 1)] + rank[k];
+      const uint32_t at = part[wave][(key[k] >> shift) & ((1u << BITS) - 1)] + rank[k];
       keys_out[at] = key[k];
       pos_out[at] = from[k];
     }
 }
 
 // The whole sort in one workgroup, for at most 1024 N tokens: pairs in LDS
-// between the passes, digits of at most 8 bits.
+// between the passes, digits of 8 bits.
 template <class I, int N>
-__global__ void __launch_bounds__(1024) k_sort_small(const I* tokens, int32_t n, int64_t vocab, int passes, int bits,
+__global__ void __launch_bounds__(1024) k_sort_small(const I* tokens, int32_t n, int64_t vocab, int passes,
                                                      uint32_t* keys_out, uint32_t* pos_out) {
   extern __shared__ uint32_t sort_lds[];
   uint32_t* keys = sort_lds;                                  // [1024 N]
@@ -269,10 +273,10 @@ __global__ void __launch_bounds__(1024) k_sort_small(const I* tokens, int32_t n,
     from[k] = (uint16_t)i;
   }
   for (int p = 0; p < passes; ++p) {
-    const int shift = p * bits;
+    const int shift = p * 8;
     for (int d = lane; d < 256; d += 64) part[wave][d] = 0;
     __syncthreads();
-    rank_keys<N>(key, rank, part[wave], base, n, shift, bits);
+    rank_keys<8, N>(key, rank, part[wave], base, n, shift);
     __syncthreads();
     uint32_t all = 0, incl = 0;
     if (tid < 256) {
@@ -296,7 +300,7 @@ __global__ void __launch_bounds__(1024) k_sort_small(const I* tokens, int32_t n,
 #pragma unroll
     for (int k = 0; k < N; ++k)
       if (base + k * 64 + lane < n) {
-        const uint32_t at = part[wave][(key[k] >> shift) & ((1u << bits) - 1)] + rank[k];
+        const uint32_t at = part[wave][(key[k] >> shift) & 255] + rank[k];
         keys[at] = key[k];
         pos[at] = from[k];
       }

@@ -149,22 +149,20 @@ void sort_small(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int key_b
   constexpr size_t lds = 1024 * N * 6 + 16 * 256 * 4 + 16;
   const void* k = (const void*)k_sort_small<I, N>;
   if (lds > 65536) HIPCHECK(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-  const int passes = (key_bits + 7) / 8, bits = (key_bits + passes - 1) / passes;
   hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_small<I, N>), dim3(1), dim3(1024), lds, st, tokens, (int32_t)d->n_tokens,
-                     d->vocab, passes, bits, w.keys[0], w.pos[0]);
+                     d->vocab, (key_bits + 7) / 8, w.keys[0], w.pos[0]);
 }
 
-template <class I, int PER, int N>
+template <class I, int BITS, int N>
 void sort_tiled(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int key_bits, int& in, hipStream_t st) {
   const int64_t n = d->n_tokens;
   const unsigned tiles = (unsigned)sort_tiles(n);
-  const int passes = (key_bits + kSortBits - 1) / kSortBits, bits = (key_bits + passes - 1) / passes;
-  for (int p = 0; p < passes; ++p, in ^= 1) {
+  for (int p = 0; p * BITS < key_bits; ++p, in ^= 1) {
     const uint32_t *k = p ? w.keys[in] : nullptr, *q = p ? w.pos[in] : nullptr;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_count<I, PER, N>), dim3(tiles), dim3(256), 0, st, tokens, k, n, d->vocab,
-                       p * bits, bits, w.counts);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_move<I, PER, N>), dim3(tiles), dim3(256), 0, st, tokens, k, q, n, d->vocab,
-                       p * bits, bits, (const uint32_t*)w.counts, w.keys[in ^ 1], w.pos[in ^ 1]);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_count<I, BITS, N>), dim3(tiles), dim3(256), 0, st, tokens, k, n, d->vocab,
+                       p * BITS, w.counts);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_move<I, BITS, N>), dim3(tiles), dim3(256), 0, st, tokens, k, q, n, d->vocab,
+                       p * BITS, (const uint32_t*)w.counts, w.keys[in ^ 1], w.pos[in ^ 1]);
   }
 }
 
@@ -178,17 +176,17 @@ void sort_tokens(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int& in,
   if (n <= 1024) return sort_small<I, 1>(d, tokens, w, key_bits, st);
   if (n <= 4096) return sort_small<I, 4>(d, tokens, w, key_bits, st);
   const int passes = (key_bits + kSortBits - 1) / kSortBits, bits = (key_bits + passes - 1) / passes;
-  const auto with = [&](auto per) {
-    constexpr int PER = decltype(per)::value;
+  const auto with = [&](auto digit) {
+    constexpr int BITS = decltype(digit)::value;
     switch (sort_items(n)) {
-      case 4: return sort_tiled<I, PER, 4>(d, tokens, w, key_bits, in, st);
-      case 8: return sort_tiled<I, PER, 8>(d, tokens, w, key_bits, in, st);
-      default: return sort_tiled<I, PER, 16>(d, tokens, w, key_bits, in, st);
+      case 4: return sort_tiled<I, BITS, 4>(d, tokens, w, key_bits, in, st);
+      case 8: return sort_tiled<I, BITS, 8>(d, tokens, w, key_bits, in, st);
+      default: return sort_tiled<I, BITS, 16>(d, tokens, w, key_bits, in, st);
     }
   };
-  if (bits <= 8) with(std::integral_constant<int, 1>{});
-  else if (bits == 9) with(std::integral_constant<int, 2>{});
-  else with(std::integral_constant<int, 4>{});
+  if (bits <= 8) with(std::integral_constant<int, 8>{});
+  else if (bits == 9) with(std::integral_constant<int, 9>{});
+  else with(std::integral_constant<int, 10>{});
 }
 
 // ------------------------------------------------------------------ gated
