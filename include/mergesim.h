@@ -619,8 +619,9 @@ ms_status ms_gated_lowpass_step(const ms_gated_step_desc* desc, const void* v, c
  * which moves the singular values of X towards one and keeps its singular
  * vectors.  MS_E_INVALID where c0..c2 let a singular value of an iterate, or
  * the polynomial, exceed 1000 in size.  The products run on 16-bit matrix instructions
- * with 32-bit sums: float32 matrices as the sum of two 16-bit parts (22 bits),
- * bf16 matrices as one (11 bits, finer than the result's rounding).
+ * with 32-bit sums, matrices as the sum of two 16-bit parts (22 bits), bf16
+ * results of 768 rows and columns and more with one (11 bits, finer than the
+ * result's rounding).
  *
  * ms_orthogonal_update trains a float32 weight with it:
  *     momentum <- momentum_decay * momentum + grad

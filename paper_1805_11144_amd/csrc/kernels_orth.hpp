@@ -131,18 +131,21 @@ __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* par
   const float* mom = UPDATE ? s.momentum + mat * s.rows * s.cols : nullptr;
   // source rows r0.. and columns c0.. of the tile
   const int64_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
-  for (int k = tid; k < 64 * 64; k += 256) {
-    const int dr = k / 64, dc = k % 64;
-    const int64_t r = r0 + dr, c = c0 + dc;
-    float v = 0.0f;
-    if (r < s.rows && c < s.cols) {
-      v = as_f32(x[r * s.row + c]);
-      if constexpr (UPDATE) {
-        const float m = mom[r * s.cols + c];
-        v = s.nesterov ? fmaf(s.decay, m, v) : m;
-      }
-      v = (float)(v * inv);
-    }
+  float in[16], mo[16];   // all on their way at once; past the matrix's end: read at its last value, and not used
+  const int dc = tid % 64;
+  const int64_t c = c0 + dc, cc = min(c, s.cols - 1);
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int64_t r = min(r0 + tid / 64 + 4 * k, s.rows - 1);
+    in[k] = as_f32(x[r * s.row + cc]);
+    if (UPDATE) mo[k] = mom[r * s.cols + cc];
+  }
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int dr = tid / 64 + 4 * k;
+    float v = in[k];
+    if constexpr (UPDATE) v = s.nesterov ? fmaf(s.decay, mo[k], v) : mo[k];
+    v = r0 + dr < s.rows && c < s.cols ? (float)(v * inv) : 0.0f;
     if (tall) tile[dc][dr] = v;
     else tile[dr][dc] = v;
   }
@@ -163,17 +166,20 @@ __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* par
   }
 }
 
-enum OrthEnd { kEndGram, kEndPoly, kEndNext, kEndOut, kEndUpdate };
+enum OrthEnd { kEndGram, kEndPoly, kEndNext, kEndOut, kEndUpdate, kEndPart };
 
 struct OrthGemm {
   const half_t *l, *r;        // L [M][K], R [N][K]
   int32_t M, N, K;            // padded
-  uint32_t per, whole;        // tiles of a matrix; tiles of all that are computed whole
+  uint32_t batch, per, whole; // tiles of a matrix; tiles of all that are computed whole
   half_t* c;                  // C [M][N], or null
   half_t* ct;                 // its transpose (kEndNext)
   const half_t* a;            // A (kEndPoly)
   float f;                    // sums to C's scale
   float c0, c1;               // kEndPoly, in C's scale (c1 times A's stored value)
+  // kEndPart: the sum over slices [part * slices, ..) alone, unscaled, to sums[part][matrix][M][M]
+  float* sums;
+  int32_t slices, parts;      // slices of a part (all of them, and 1, for other ends)
   // kEndOut, kEndUpdate
   void* out;
   int64_t mat, row, rows, cols;
@@ -204,11 +210,12 @@ __device__ __forceinline__ void barrier_but() {
 // LDS in lane order); chunk c of row r sits at c ^ (r / (128 / KS)), so the
 // rows of a fragment read different banks.
 template <int PL, int TILE, int WC, int KS, int ST, int KG, int END, class T>
-__device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_t mat, int32_t trow, int32_t tcol) {
+__device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_t mat, int32_t part, int32_t trow,
+                                          int32_t tcol) {
   constexpr int NW = 2 * WC, WM = TILE / 2, WN = TILE / WC, BI = WM / 32, BJ = WN / 32;
   constexpr int CH = KS / 8, U = PL * TILE * CH / (64 * NW);
   static_assert(BI >= 1 && BJ >= 1 && U >= 1, "work for every wavefront");
-  constexpr bool SYM = END == kEndGram || END == kEndPoly;
+  constexpr bool SYM = END == kEndGram || END == kEndPoly || END == kEndPart;
   constexpr int LEFT = PL * TILE * KS, SLAB = 2 * LEFT;   // of one slice; lds: [KG][ST][SLAB]
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % NW);
   const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW));
@@ -233,12 +240,29 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
       fetch_lds(R + p * rplane + slice * g.N * KS + off[q], own + buf * SLAB + LEFT + 8 * i0);
     }
   };
-  floatx16 acc[BI][BJ];
+  // where a wavefront has a single block, several sums for it, so that a product does not wait for the one before
+  constexpr int NA = BI * BJ > 1 ? 1 : PL == 2 ? 3 : 2;
+  floatx16 acc[BI][BJ], more[NA > 1 ? NA - 1 : 1];
 #pragma unroll
   for (int i = 0; i < BI; ++i)
 #pragma unroll
     for (int j = 0; j < BJ; ++j) acc[i][j] = floatx16{};
-  const int32_t slices = g.K / KS;
+#pragma unroll
+  for (int n = 0; n < NA - 1; ++n) more[n] = floatx16{};
+  // A's values for the polynomial, on their way while the product is made
+  [[maybe_unused]] half_t early[PL][16];
+  constexpr bool EARLY = END == kEndPoly && BI * BJ == 1;
+  if constexpr (EARLY) {
+    const half_t* A = g.a + mat * PL * lplane;   // A has the product's shape and K its side
+#pragma unroll
+    for (int p = 0; p < PL; ++p)
+#pragma unroll
+      for (int q = 0; q < 16; ++q)
+        early[p][q] = A[p * lplane + orth_at<KS>(g.M, trow + wm * WM + 8 * (q / 4) + 4 * (lane / 32) + q % 4,
+                                                 tcol + wn * WN + lane % 32)];
+  }
+  const int32_t slices = min(g.slices, g.K / KS - part * g.slices);
+  L += (int64_t)part * g.slices * g.M * KS, R += (int64_t)part * g.slices * g.N * KS;
 #pragma unroll
   for (int q = 0; q < ST - 1; ++q)
     if (q * KG + group < slices) fetch(q * KG + group, q);
@@ -278,15 +302,23 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
         for (int i = 0; i < BI; ++i)
 #pragma unroll
           for (int j = 0; j < BJ; ++j) {
+            floatx16& s0 = acc[i][j];
+            floatx16& s1 = NA > 1 ? more[0] : s0;
+            floatx16& s2 = NA > 2 ? more[NA > 2 ? 1 : 0] : s0;
             if constexpr (PL == 2) {
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][1][i], b[ks][0][j], acc[i][j], 0, 0, 0);
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][1][j], acc[i][j], 0, 0, 0);
+              s1 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][1][i], b[ks][0][j], s1, 0, 0, 0);
+              s2 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][1][j], s2, 0, 0, 0);
+              s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][0][j], s0, 0, 0, 0);
+            } else {
+              floatx16& s = ks % 2 ? s1 : s0;
+              s = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][0][j], s, 0, 0, 0);
             }
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][0][j], acc[i][j], 0, 0, 0);
           }
     }
     buf = buf + 1 == ST ? 0 : buf + 1;
   }
+#pragma unroll
+  for (int n = 0; n < NA - 1; ++n) acc[0][0] += more[n];
   if constexpr (KG == 2) {   // the second group's sums through LDS
     __syncthreads();
     float* sums = (float*)lds + wave * BI * BJ * 16 * 64 + lane;
@@ -327,7 +359,9 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
         for (int q = 0; q < 4; ++q) {
           const int64_t row = row0 + q;
           float v = g.f * acc[i][j][4 * q4 + q];
-          if constexpr (END == kEndOut || END == kEndUpdate) {
+          if constexpr (END == kEndPart) {
+            g.sums[((part * (int64_t)g.batch + mat) * g.M + row) * g.M + col] = acc[i][j][4 * q4 + q];
+          } else if constexpr (END == kEndOut || END == kEndUpdate) {
             const bool tall = g.rows > g.cols;
             const int64_t r = tall ? col : row, c = tall ? row : col;
             if (r < g.rows && c < g.cols) {
@@ -337,8 +371,14 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
             }
           } else {
             if constexpr (END == kEndPoly) {
-              float av = (float)A[orth_at<KS>(g.M, row, col)];
-              if (PL == 2) av += (float)A[cplane + orth_at<KS>(g.M, row, col)];
+              float av;
+              if constexpr (EARLY) {
+                av = (float)early[0][4 * q4 + q];
+                if (PL == 2) av += (float)early[PL - 1][4 * q4 + q];
+              } else {
+                av = (float)A[orth_at<KS>(g.M, row, col)];
+                if (PL == 2) av += (float)A[cplane + orth_at<KS>(g.M, row, col)];
+              }
               v += g.c1 * av + (row == col ? g.c0 : 0.0f);
             }
             half_t h, l;
@@ -348,7 +388,7 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
             if (PL == 2) C[cplane + orth_at<KS>(g.M, row, col)] = l;
           }
         }
-        if constexpr (SYM || END == kEndNext) {
+        if constexpr (END == kEndGram || END == kEndPoly || END == kEndNext) {
           if (END == kEndNext || brow != bcol) {
             half_t* D = (SYM ? C : CT) + orth_at<KS>(g.N, col, row0);
             *(halfx4*)D = hi;
@@ -375,7 +415,7 @@ __device__ __forceinline__ void orth_place(uint32_t u, uint32_t tm, uint32_t& ti
 // `whole` tiles, and the others in quarters.
 template <int PL, int TILE, int WC, int KS, int ST, int KG, int END, class T>
 __global__ void __launch_bounds__(128 * WC * KG) k_orth_gemm(OrthGemm g) {
-  constexpr bool SYM = END == kEndGram || END == kEndPoly;
+  constexpr bool SYM = END == kEndGram || END == kEndPoly || END == kEndPart;
   extern __shared__ __attribute__((aligned(16))) half_t orth_gemm_lds[];
   // workgroups i, i + 8.. run on one XCD: it gets a contiguous part of the
   // tiles, whose columns and rows it then finds in its L2
@@ -385,13 +425,37 @@ __global__ void __launch_bounds__(128 * WC * KG) k_orth_gemm(OrthGemm g) {
     const uint32_t tile = blockIdx.x % 8 * share + blockIdx.x / 8;
     if (tile >= g.whole) return;
     orth_place<SYM>(tile % g.per, g.M / TILE, ti, tj);
-    orth_tile<PL, TILE, WC, KS, ST, KG, END, T>(g, orth_gemm_lds, tile / g.per, ti * TILE, tj * TILE);
+    const uint32_t mat = tile / g.per;   // of the batch, once for each part
+    orth_tile<PL, TILE, WC, KS, ST, KG, END, T>(g, orth_gemm_lds, mat % g.batch, mat / g.batch, ti * TILE, tj * TILE);
   } else if constexpr (TILE > 64) {
     constexpr uint32_t HALF = TILE / 2;
     const uint32_t part = blockIdx.x - share * 8, tile = g.whole + part / 4;
     orth_place<SYM>(tile % g.per, g.M / TILE, ti, tj);
     ti = 2 * ti + part % 2, tj = 2 * tj + part / 2 % 2;
     if (SYM && ti > tj) return;
-    orth_tile<PL, HALF, WC, KS, ST, 1, END, T>(g, orth_gemm_lds, tile / g.per, ti * HALF, tj * HALF);
+    orth_tile<PL, HALF, WC, KS, ST, 1, END, T>(g, orth_gemm_lds, tile / g.per, 0, ti * HALF, tj * HALF);
+  }
+}
+
+// A from the parts of its sum, added in their order.  A thread takes a value of
+// the blocks on and above the diagonal, and its mirror image.
+template <int PL, int KS>
+__global__ void __launch_bounds__(256) k_orth_join(OrthGemm g) {
+  const int64_t size = (int64_t)g.M * g.M, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= g.batch * size) return;
+  const int64_t mat = i / size, row = i % size / g.M, col = i % g.M;
+  if (row / 32 > col / 32) return;
+  float v = 0.0f;
+#pragma unroll 8
+  for (int p = 0; p < g.parts; ++p) v += g.sums[p * (int64_t)g.batch * size + i];
+  half_t hi, lo;
+  split(g.f * v, hi, lo);
+  half_t* C = g.c + mat * PL * size;
+  const int64_t at = orth_at<KS>(g.M, row, col), mirror = orth_at<KS>(g.M, col, row);
+  C[at] = hi;
+  if (PL == 2) C[size + at] = lo;
+  if (row / 32 < col / 32) {
+    C[mirror] = hi;
+    if (PL == 2) C[size + mirror] = lo;
   }
 }

@@ -3,9 +3,9 @@
 //
 // X [n][m] (n <= 64 rows padded to 16 NT) is float32 in LDS, products run on
 // v_mfma_f32_16x16x4f32 (lane l of a wavefront holds row or column l % 16 and
-// k = l / 16; of the result, column l % 16 and rows 4 (l / 16) + q).  Rows lie
-// 4 banks apart modulo the 64 banks, so the 16 x 4 values of a fragment of A
-// come from 64 different ones.  An iteration:
+// one k of four; of the result, column l % 16 and rows 4 (l / 16) + q).  Rows
+// lie 4 banks apart modulo the 64 banks, so 16 lanes' 16-byte reads come from 64
+// different ones.  An iteration:
 //   A = X X'    the sum over m split over the wavefronts where A has few tiles,
 //               added up in their order; else a wavefront takes whole tiles
 //   Q           = c0 I + c1 A + c2 A A
@@ -56,16 +56,42 @@ __global__ void __launch_bounds__(64 * kOrthWaves) k_orth_small(OrthSmall p) {
   for (int i = tid; i < N * p.stride; i += THREADS) X[i] = 0.0f;
   __syncthreads();
   double sum = 0.0;
-  for (int i = tid; i < rows * cols; i += THREADS) {
-    const int r = i / cols, c = i - r * cols;
-    float v = as_f32(x[r * p.src.row + c]);
-    if constexpr (UPDATE) {
-      const float m = fmaf(p.src.decay, mom[i], v);
-      mom[i] = m;
-      v = p.src.nesterov ? fmaf(p.src.decay, m, v) : m;
+  const int n = rows * cols;
+  // value i = (r, c), and the step to value i + THREADS without a division
+  struct Place {
+    int r, c;
+  };
+  const int dr = THREADS / cols, dc = THREADS - dr * cols;
+  const auto onward = [&](Place& a) {
+    a.r += dr, a.c += dc;
+    if (a.c >= cols) a.c -= cols, ++a.r;
+  };
+  const Place begin{tid / cols, tid % cols};
+  const auto within = [&](const Place& a) { return tall ? a.c * p.stride + a.r : a.r * p.stride + a.c; };
+  Place at = begin;
+  for (int i0 = tid; i0 < n; i0 += 8 * THREADS) {
+    float in[8], mo[8];   // eight values on their way at once; past the end: the first one, not used
+    int to[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const bool live = i0 + q * THREADS < n;
+      in[q] = as_f32(x[live ? at.r * p.src.row + at.c : 0]);
+      if (UPDATE) mo[q] = mom[live ? i0 + q * THREADS : 0];
+      to[q] = within(at);
+      onward(at);
     }
-    X[tall ? c * p.stride + r : r * p.stride + c] = v;
-    sum += (double)v * v;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (i0 + q * THREADS < n) {
+        float v = in[q];
+        if constexpr (UPDATE) {
+          const float m = fmaf(p.src.decay, mo[q], v);
+          mom[i0 + q * THREADS] = m;
+          v = p.src.nesterov ? fmaf(p.src.decay, m, v) : m;
+        }
+        X[to[q]] = v;
+        sum += (double)v * v;
+      }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_down(sum, o, 64);
@@ -77,18 +103,25 @@ __global__ void __launch_bounds__(64 * kOrthWaves) k_orth_small(OrthSmall p) {
   const double inv = 1.0 / (sqrt(total) + p.eps);
   for (int i = tid; i < p.n * p.stride; i += THREADS) X[i] = (float)(X[i] * inv);
   __syncthreads();
-  const int kq = (p.m + 3) / 4, ctiles = (p.m + 15) / 16;
+  // one product takes 4 values of k, one from each quarter of the wavefront; a lane's four values of 16 lie side by
+  // side, so its part of a fragment of four products is one 16-byte read
+  const auto quad = [&](const float* row, int k16) { return *(const floatx4*)(row + 16 * k16 + 4 * l4); };
+  const int k16s = (p.m + 15) / 16, ctiles = k16s;
   for (int step = 0; step < p.steps; ++step) {
     if constexpr (NT <= 2) {
       floatx4 acc[TILES] = {};
-      for (int k = wave; k < kq; k += kOrthWaves) {
-        float f[NT];
+#pragma unroll 2
+      for (int k = wave; k < k16s; k += kOrthWaves) {
+        floatx4 f[NT];
 #pragma unroll
-        for (int i = 0; i < NT; ++i) f[i] = X[(16 * i + l16) * p.stride + 4 * k + l4];
+        for (int i = 0; i < NT; ++i) f[i] = quad(X + (16 * i + l16) * p.stride, k);
 #pragma unroll
-        for (int j = 0, t = 0; j < NT; ++j)
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int i = 0; i <= j; ++i, ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[i], f[j], acc[t], 0, 0, 0);
+          for (int j = 0, t = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i <= j; ++i, ++t)
+              acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[i][e], f[j][e], acc[t], 0, 0, 0);
       }
 #pragma unroll
       for (int t = 0; t < TILES; ++t)
@@ -110,15 +143,17 @@ __global__ void __launch_bounds__(64 * kOrthWaves) k_orth_small(OrthSmall p) {
         int tj = 0;
         while ((tj + 1) * (tj + 2) / 2 <= t) ++tj;
         const int ti = t - tj * (tj + 1) / 2;
-        floatx4 acc[2] = {};   // two sums, so that one product does not wait for the one before it
-        for (int k = 0; k < kq; ++k) {
-          const float a = X[(16 * ti + l16) * p.stride + 4 * k + l4], b = X[(16 * tj + l16) * p.stride + 4 * k + l4];
-          acc[k & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc[k & 1], 0, 0, 0);
+        floatx4 acc[4] = {};   // four sums, so that one product does not wait for the one before it
+#pragma unroll 4
+        for (int k = 0; k < k16s; ++k) {
+          const floatx4 a = quad(X + (16 * ti + l16) * p.stride, k), b = quad(X + (16 * tj + l16) * p.stride, k);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], acc[e], 0, 0, 0);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int r = 16 * ti + 4 * l4 + q, c = 16 * tj + l16;
-          const float s = acc[0][q] + acc[1][q];
+          const float s = (acc[0][q] + acc[1][q]) + (acc[2][q] + acc[3][q]);
           A[r * AS + c] = s;
           if (ti != tj) A[c * AS + r] = s;
         }
@@ -127,11 +162,14 @@ __global__ void __launch_bounds__(64 * kOrthWaves) k_orth_small(OrthSmall p) {
     __syncthreads();
     for (int t = wave; t < NT * NT; t += kOrthWaves) {
       const int ti = t / NT, tj = t % NT;
-      floatx4 acc = {};
+      floatx4 sum4[4] = {};
 #pragma unroll
-      for (int k = 0; k < N / 4; ++k)   // A is symmetric
-        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(A[(16 * ti + l16) * AS + 4 * k + l4], A[(16 * tj + l16) * AS + 4 * k + l4],
-                                                   acc, 0, 0, 0);
+      for (int k = 0; k < NT; ++k) {   // A is symmetric
+        const floatx4 a = quad(A + (16 * ti + l16) * AS, k), b = quad(A + (16 * tj + l16) * AS, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum4[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], sum4[e], 0, 0, 0);
+      }
+      const floatx4 acc = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int r = 16 * ti + 4 * l4 + q, c = 16 * tj + l16;
@@ -139,15 +177,25 @@ __global__ void __launch_bounds__(64 * kOrthWaves) k_orth_small(OrthSmall p) {
       }
     }
     __syncthreads();
+    floatx4 f[NT][NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int k = 0; k < NT; ++k) f[i][k] = quad(Q + (16 * i + l16) * AS, k);
     for (int u = wave; u < ctiles; u += kOrthWaves) {
       floatx4 acc[NT] = {};
+      float b[NT][4];
 #pragma unroll
-      for (int k = 0; k < N / 4; ++k) {
-        const float b = X[(4 * k + l4) * p.stride + 16 * u + l16];
+      for (int k = 0; k < NT; ++k)
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(Q[(16 * i + l16) * AS + 4 * k + l4], b, acc[i], 0, 0, 0);
-      }
+        for (int e = 0; e < 4; ++e) b[k][e] = X[(16 * k + 4 * l4 + e) * p.stride + 16 * u + l16];
+#pragma unroll
+      for (int k = 0; k < NT; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[i][k][e], b[k][e], acc[i], 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -157,11 +205,20 @@ __global__ void __launch_bounds__(64 * kOrthWaves) k_orth_small(OrthSmall p) {
   }
   using R = std::conditional_t<UPDATE, float, T>;
   R* out = (R*)p.out + mat * p.omat;
-  for (int i = tid; i < rows * cols; i += THREADS) {
-    const int r = i / cols, c = i - r * cols;
-    const float v = X[tall ? c * p.stride + r : r * p.stride + c];
-    R* o = out + r * p.orow + c;
-    if constexpr (UPDATE) *o = p.keep * *o - p.rate * v;
-    else *o = (R)v;
+  at = begin;
+  for (int i0 = tid; i0 < n; i0 += 8 * THREADS) {
+    float old[8], v[8];
+    R* o[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const bool live = i0 + q * THREADS < n;
+      o[q] = out + (live ? at.r * p.orow + at.c : 0);
+      if (UPDATE) old[q] = (float)*o[q];
+      v[q] = X[live ? within(at) : 0];
+      onward(at);
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (i0 + q * THREADS < n) *o[q] = UPDATE ? (R)(p.keep * old[q] - p.rate * v[q]) : (R)v[q];
   }
 }

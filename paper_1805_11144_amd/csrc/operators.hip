@@ -327,6 +327,7 @@ struct Orth {
   int64_t n, m, np, mp;
   int64_t pad;            // to whole tiles of this side
   int parts;              // fp16 parts of a value
+  int split;              // workgroups that share the sum over m of a tile of X X'
   double sx, sa, sq;      // scales of X, A and Q
   int64_t xm, xr, om, orow;
   int small;              // row tiles of 16 where a matrix fits into one workgroup's LDS, else 0
@@ -353,7 +354,9 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
   pair(d->x_stride, o.xm, o.xr);
   pair(d->out_stride, o.om, o.orow);
   o.n = std::min(d->rows, d->cols), o.m = std::max(d->rows, d->cols);
-  o.parts = update || d->dtype == MS_DTYPE_F32 ? 2 : 1;
+  // bf16: one part from 768 rows on, where products bound the time (4096 x 4096 1.8 ms, with two 4.4) and the
+  // result is at most 1.25 times as far off as its rounding alone; 1.34 times at 256 rows, for less than it saves
+  o.parts = !update && d->dtype == MS_DTYPE_BF16 && o.n >= 768 ? 1 : 2;
   // tiles of 128 x 128 read half as much; of 64 x 64 where the others would not fill the CUs
   double least = INFINITY;
   for (int64_t pad : {64, 128, 256}) {   // larger tiles pad more
@@ -365,6 +368,10 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
     if (cost < least) least = cost, o.pad = pad, o.np = n, o.mp = m;
   }
   need(d->batch <= kMaxBlocks / std::max<int64_t>(kOrthParts, (o.np / 64) * (o.mp / 64)), "too many matrices of this size");
+  // Few tiles and a long sum (16 x 9000: one tile, 282 slices): shared by so many workgroups that they fill half the
+  // CUs, none with fewer than 16 slices, and added up by one more launch.
+  const int64_t tiles = orth_tiles(kTile64, true, d->batch, o.np, o.np).per * std::max<int64_t>(d->batch, 1);
+  o.split = (int)std::max<int64_t>(1, std::min(kCUs / 2 / tiles, o.mp / kOrthSlice / 16));
   o.stride = up(o.m, 64) + 4;
   o.small = (int)up(o.n, 16) / 16;
   if (o.small > 4 || orth_small_floats(o.small, o.stride) * 4 > kOrthLds) o.small = 0;
@@ -402,6 +409,7 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
 struct OrthWork {
   double* parts;
   half_t *x, *t[2], *a, *q;
+  float* sums;
   int64_t bytes;
 };
 
@@ -416,6 +424,7 @@ OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
   w.t[1] = c.take<half_t>(big);
   w.a = c.take<half_t>(small);
   w.q = c.take<half_t>(small);
+  w.sums = c.take<float>(o.split > 1 ? o.split * d->batch * o.np * o.np : 0);
   w.bytes = c.used;
   return w;
 }
@@ -460,9 +469,19 @@ void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork
   using R = std::conditional_t<UPDATE, float, T>;
   for (int k = 0; k < d->steps; ++k) {
     OrthGemm g{};
+    g.batch = out.batch = (uint32_t)d->batch, g.parts = out.parts = 1;
+    g.slices = out.slices = INT32_MAX / 2;
     g.l = g.r = w.x, g.M = g.N = (int32_t)o.np, g.K = (int32_t)o.mp, g.c = w.a;
     g.f = (float)(o.sa / (o.sx * o.sx));
-    orth_gemm<PL, kEndGram, R>(g, o.pad, d->batch, st);
+    if (o.split > 1) {
+      g.sums = w.sums, g.parts = o.split, g.slices = (int32_t)((o.mp / kOrthSlice + o.split - 1) / o.split);
+      orth_launch<PL, kEndPart, R, 64, 2, 3, 2>(g, orth_tiles(kTile64, true, d->batch * o.split, o.np, o.np), st);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_join<PL, kOrthSlice>), dim3((unsigned)((d->batch * o.np * o.np + 255) / 256)),
+                         dim3(256), 0, st, g);
+    } else {
+      orth_gemm<PL, kEndGram, R>(g, o.pad, d->batch, st);
+    }
+    g.parts = 1, g.slices = INT32_MAX / 2;
     g.l = g.r = w.a, g.K = (int32_t)o.np, g.c = w.q, g.a = w.a;
     g.f = (float)(d->coef[2] * o.sq / (o.sa * o.sa));
     g.c0 = (float)(d->coef[0] * o.sq), g.c1 = (float)(d->coef[1] * o.sq / o.sa);
@@ -763,7 +782,8 @@ ms_status ms_orthogonalise(const ms_orth_desc* d, const void* x, void* out, void
     OrthSrc src{x, nullptr, o.xm, o.xr, d->rows, d->cols, 0.0f, 0};
     OrthGemm g{};
     g.out = out, g.mat = o.om, g.row = o.orow, g.rows = d->rows, g.cols = d->cols;
-    if (d->dtype == MS_DTYPE_BF16) orth<__bf16, false, 1>(d, o, src, w, g, st);
+    if (o.parts == 1) orth<__bf16, false, 1>(d, o, src, w, g, st);
+    else if (d->dtype == MS_DTYPE_BF16) orth<__bf16, false, 2>(d, o, src, w, g, st);
     else orth<float, false, 2>(d, o, src, w, g, st);
   });
 }
