@@ -12,9 +12,9 @@
 // result is known.  A wavefront takes kKeep = 16 steps of 64 V channels,
 // fetched together; its lanes find their runs' maps, and the wavefronts of a
 // workgroup, which hold consecutive runs, join them in LDS.  Sequences longer
-// than a workgroup's 128 steps are cut into such chunks.  With enough channels,
-// or a few chunks, a workgroup goes through its chunks one after the other
-// (LINK = false).  Otherwise the chunks run side by side (LINK): each publishes
+// than a workgroup's 128 steps are cut into such chunks.  A few chunks are gone
+// through by one workgroup, one after the other (LINK = false).  Otherwise the
+// chunks run side by side (LINK): each publishes
 // its map for the later ones, and every kSpan-th the state that it ends with;
 // a chunk waits for the state at its span's beginning and the maps in between,
 // a wavefront for each.  The order of the operations is fixed, so the result
@@ -23,7 +23,8 @@
 // Measured at 4 x 16384 x 2048 bf16 (0.81 GB): 445 us in two passes (maps, then
 // steps: v and g are read twice), 190 us in one, with the first wavefront
 // waiting for all maps, 163 us with a wavefront for each, 149 us without any
-// waiting (wrong results), 146 us without the exponentials too.  Chunks of 64
+// waiting (a copy that is not correct, to know the cost), 146 us without the
+// exponentials too.  Chunks of 64
 // steps take 235 us, of 256 steps 193; one channel per lane 229.  A third
 // workgroup on each CU (gates kept as one number) does not help: 171.
 #pragma once

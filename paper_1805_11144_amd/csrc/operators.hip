@@ -240,10 +240,14 @@ GatedWork gated_work(const Gated& g, void* ws) {
   return w;
 }
 
-// Threads of a workgroup, and whether chunks run side by side.  A workgroup
-// that goes through chunks one after the other takes about 2.5 us for each, and
-// needs a second one on its CU to keep memory busy; linked chunks cost a launch
-// that clears what they publish, and their waits.
+// Threads of a workgroup, whether chunks run side by side, and how channels are
+// dealt to lanes.  One after the other, a chunk costs about 4 us (gradient 6)
+// while its data is on the way; side by side there is a launch that clears what
+// they publish, and their waits.  bf16, rows x steps x channels, forward and
+// gradient in us, one after the other and side by side:
+//   1 x 384 x 2048     15, 23    16, 20        16 x 512 x 2048     25, 39     30, 47
+//   1 x 512 x 2048     19, 30    17, 21        16 x 1024 x 2048    49, 75     48, 76
+//   1 x 1024 x 2048    35, 56    16, 20        128 x 1024 x 2048   319, 562   295, 502
 struct GatedShape {
   unsigned threads;
   bool link, span;
@@ -257,7 +261,8 @@ GatedShape gated_shape(Gated& g) {
   a.per_row = (int32_t)((a.nv + 63) / 64);
   const bool span = a.per_row * 64 > a.nv + a.nv / 4;   // over a fifth of the lanes would idle
   a.groups = (int32_t)(span ? (a.batch * a.nv + 63) / 64 : a.batch * a.per_row);
-  const bool link = a.nchunk > 4 && a.groups < 1024 && (int64_t)a.nchunk * a.groups < ((int64_t)1 << 22);
+  const bool link = (a.nchunk > 4 || (a.nchunk > 2 && a.groups <= 64)) &&
+                    (int64_t)a.nchunk * a.groups < ((int64_t)1 << 22);   // tickets in the grid's 32 bits of threads
   return {(unsigned)waves * 64, link, span};
 }
 
@@ -367,7 +372,6 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
     const double cost = square * (m + n) + next * n;
     if (cost < least) least = cost, o.pad = pad, o.np = n, o.mp = m;
   }
-  need(d->batch <= kMaxBlocks / std::max<int64_t>(kOrthParts, (o.np / 64) * (o.mp / 64)), "too many matrices of this size");
   // Few tiles and a long sum (16 x 9000: one tile, 282 slices): shared by so many workgroups that they fill half the
   // CUs, none with fewer than 16 slices, and added up by one more launch.
   const int64_t tiles = orth_tiles(kTile64, true, d->batch, o.np, o.np).per * std::max<int64_t>(d->batch, 1);
@@ -375,6 +379,9 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
   o.stride = up(o.m, 64) + 4;
   o.small = (int)up(o.n, 16) / 16;
   if (o.small > 4 || orth_small_floats(o.small, o.stride) * 4 > kOrthLds) o.small = 0;
+  // workgroups of up to 512 threads
+  const int64_t groups = o.small ? 1 : std::max<int64_t>(kOrthParts, (o.np / 64) * (o.mp / 64));
+  need(d->batch <= kMaxBlocks / 2 / groups, "too many matrices of this size");
   // How large an iterate's singular values and the polynomial can get: the
   // first are at most 1, and f(s) = s (c0 + c1 s^2 + c2 s^4) takes its extremes
   // over [0, top] at the ends or where its derivative is 0.

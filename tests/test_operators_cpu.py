@@ -148,6 +148,12 @@ def test_orth_pointer_and_rule_refusals():
         refused("ms_orthogonal_update", orth(), rule, *args, A, 1 << 40, words="NULL")
 
 
+def test_many_small_matrices_need_no_workspace():
+    n = C.c_int64(-1)
+    assert MS.load_library().ms_orth_workspace(orth(batch=1 << 20), 0, C.byref(n)) == 0 and n.value == 0
+    refused("ms_orth_workspace", orth(batch=1 << 20, rows=500, cols=400), 0, C.byref(n), words="too many")
+
+
 def test_empty_calls_succeed_without_a_gpu():
     lib = MS.load_library()
     assert lib.ms_embed(embed(n_tokens=0), None, None, None) == 0
