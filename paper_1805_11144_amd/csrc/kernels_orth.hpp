@@ -339,6 +339,12 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
 #pragma unroll
         for (int q = 0; q < 16; ++q) acc[i][j][q] += sums[((i * BJ + j) * 16 + q) * 64];
   }
+  // Results in fp16 parts: a block of 32 x 32 is one piece of memory.  Where a wavefront has several, it writes them
+  // in 16-byte words, through its own 32 rows of 40 in LDS (4096 x 4096 in one part 1.75 -> 1.65 ms); a single one
+  // goes out as it lies in the registers (1024 x 784: 187 us, through LDS 204).
+  constexpr bool PARTS = END == kEndGram || END == kEndPoly || END == kEndNext, STAGED = PARTS && BI * BJ > 1;
+  half_t* block = lds + wave * 32 * 40;
+  if (STAGED) __syncthreads();   // the buffers are read
   const int64_t cplane = (int64_t)g.M * g.N;
   half_t* C = g.c + mat * PL * cplane;
   half_t* CT = END == kEndNext ? g.ct + mat * PL * cplane : nullptr;
@@ -351,6 +357,7 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
       const int32_t brow = trow + wm * WM + i * 32, bcol = tcol + wn * WN + j * 32;
       if (SYM && brow > bcol) continue;   // the mirror image of another block
       const int64_t col = bcol + lane % 32;
+      halfx4 low[4];
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4) {
         const int64_t row0 = brow + 8 * q4 + 4 * (lane / 32);
@@ -384,10 +391,15 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
             half_t h, l;
             split(v, h, l);
             hi[q] = h, lo[q] = l;
-            C[orth_at<KS>(g.M, row, col)] = h;
-            if (PL == 2) C[cplane + orth_at<KS>(g.M, row, col)] = l;
+            if constexpr (STAGED) {
+              block[(8 * q4 + 4 * (lane / 32) + q) * 40 + lane % 32] = h;
+            } else {
+              C[orth_at<KS>(g.M, row, col)] = h;
+              if (PL == 2) C[cplane + orth_at<KS>(g.M, row, col)] = l;
+            }
           }
         }
+        low[q4] = lo;
         if constexpr (END == kEndGram || END == kEndPoly || END == kEndNext) {
           if (END == kEndNext || brow != bcol) {
             half_t* D = (SYM ? C : CT) + orth_at<KS>(g.N, col, row0);
@@ -395,6 +407,23 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
             if (PL == 2) *(halfx4*)(D + cplane) = lo;
           }
         }
+      }
+      if constexpr (STAGED) {   // two lanes to a row
+        static_assert(KS == 32, "a block's rows lie behind each other");
+        half_t* D = C + orth_at<KS>(g.M, brow, bcol) + lane * 16;
+        const half_t* mine = block + lane / 2 * 40 + lane % 2 * 16;
+#pragma unroll
+        for (int p = 0; p < PL; ++p) {
+          if (p == 1) {
+            wave_order();
+#pragma unroll
+            for (int q = 0; q < 16; ++q) block[(8 * (q / 4) + 4 * (lane / 32) + q % 4) * 40 + lane % 32] = low[q / 4][q % 4];
+          }
+          wave_order();
+          *(halfx8*)(D + p * cplane) = *(const halfx8*)mine;
+          *(halfx8*)(D + p * cplane + 8) = *(const halfx8*)(mine + 8);
+        }
+        wave_order();
       }
     }
 }
