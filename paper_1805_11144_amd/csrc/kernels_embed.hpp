@@ -1,13 +1,22 @@
 // Table lookup and its gradient by sorted tokens.
 //
-// The lookup moves rows: out[i] = scale * table[token[i]].  It is bound by
-// memory; a row is read and written in words of up to 16 bytes per lane.
+// The lookup moves rows: out[i] = scale * table[token[i]].  Memory bounds it; a
+// group of threads reads and writes rows in words of up to 16 bytes, four rows
+// at a time.  131072 rows of 1024 bf16 from a table of 32768: 55 us, 6.1 TB/s of
+// the 0.34 GB that have to move.
 //
 // The gradient adds the rows of equal tokens.  Atomic additions would make
 // their order, and so the last bits, depend on timing; here (token, position)
 // pairs are brought into token order by a stable radix sort (least significant
 // digit first, 8 to 10 bits a pass), so each table row is the sum of a run of
-// positions in ascending order.
+// positions in ascending order.  A run of more than 64 is summed in pieces that
+// are added in their order, since a token's frequency falls with its rank and
+// the first ones fill whole batches: with one group of threads to a row 262144
+// rows took 12.8 ms, of which 12.4 were the longest run.
+// Measured, 262144 rows of 1024 bf16 into 65536 x 1024 float32 (0.81 GB): sort
+// 37 us, pieces (0.29 GB) 60, rows (0.52 GB) 95: 5.2 TB/s of the sums' bytes.
+// 12800 x 784 float32 into 10007 rows (71 MB): sort 19 us, pieces and row
+// beginnings 9, rows 17: launches that each wait for the one before.
 #pragma once
 
 #include <hip/hip_runtime.h>

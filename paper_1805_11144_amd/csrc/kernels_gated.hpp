@@ -14,19 +14,19 @@
 // workgroup, which hold consecutive runs, join them in LDS.  Sequences longer
 // than a workgroup's 128 steps are cut into such chunks.  A few chunks are gone
 // through by one workgroup, one after the other (LINK = false).  Otherwise the
-// chunks run side by side (LINK): each publishes
-// its map for the later ones, and every kSpan-th the state that it ends with;
-// a chunk waits for the state at its span's beginning and the maps in between,
-// a wavefront for each.  The order of the operations is fixed, so the result
-// does not depend on timing.
+// chunks run side by side (LINK): each publishes its map for the later ones,
+// and every kSpan-th the state that it ends with; a chunk waits for the state at
+// its span's beginning and the maps in between, a wavefront for each.  The order
+// of the operations is fixed, so the result does not depend on timing.
 //
 // Measured at 4 x 16384 x 2048 bf16 (0.81 GB): 445 us in two passes (maps, then
-// steps: v and g are read twice), 190 us in one, with the first wavefront
-// waiting for all maps, 163 us with a wavefront for each, 149 us without any
-// waiting (a copy that is not correct, to know the cost), 146 us without the
-// exponentials too.  Chunks of 64
-// steps take 235 us, of 256 steps 193; one channel per lane 229.  A third
-// workgroup on each CU (gates kept as one number) does not help: 171.
+// steps: v and g are read twice), 190 us in one with the first wavefront waiting
+// for all maps, 152 to 163 us with a wavefront for each (5.3 TB/s at best), 149
+// us without any waiting (a copy that is not correct, to know the cost), 146 us
+// without the exponentials too.  Chunks of 64 steps take 235 us, of 256 steps
+// 193; one channel per lane 229.  A third workgroup on each CU (gates kept as
+// one number) does not help: 171.  The gradient of 8 x 4096 x 2048 bf16 (0.71
+// GB with the kept states): 142 us, 5.0 TB/s.
 #pragma once
 
 #include "kernels_embed.hpp"
@@ -37,8 +37,8 @@ constexpr int kKeep = 16;
 constexpr int kGatedWaves = 8;   // of a workgroup, at most
 constexpr int kSpan = 8;         // chunks from one published state to the next
 
-// A lane takes V neighbouring channels of one batch row, V channels wide words
-// of at most 4 bytes.
+// A lane takes V neighbouring channels of one batch row, a word of at most 4
+// bytes.
 struct GatedArgs {
   int64_t batch, steps, dim, nv;    // nv = dim / V
   int64_t vb, vt, gb, gt, yb, yt;   // strides of v, g and y (dy in the gradient)
@@ -151,7 +151,7 @@ __device__ __forceinline__ GatedPlace gated_place(const GatedArgs& p, uint32_t* 
 // The channels of a lane.  SPAN: lanes are dealt to all rows' channels in
 // order, for rows that would leave many of a wavefront's idle.  Otherwise a
 // wavefront stays in one row: its addresses are a uniform part and one offset
-// per lane, which saves two thirds of the gradient's registers.
+// per lane.
 struct GatedLane {
   bool live;
   int64_t b;

@@ -11,8 +11,10 @@
 //   Q           = c0 I + c1 A + c2 A A
 //   X <- Q X    column tiles of 16: each depends on nothing but itself, so they
 //               are replaced in place
-// Only the launch, the read and the write touch the rest of the chip: 200
-// matrices of 500 x 16 take 314 us on the tiled kernels (17 launches).
+// Only the launch, the read and the write touch the rest of the chip.  Bound by
+// latency: barriers, LDS and dependent products.  200 matrices of 500 x 16 take
+// 19 us, and 238 on the tiled kernels (17 launches); one of 64 x 64 28 and 74,
+// one of 64 x 400 94 and 89, 64 of 64 x 300 76 and 120.
 #pragma once
 
 #include "kernels_orth.hpp"

@@ -1,6 +1,6 @@
 // The operators on device arrays of the C ABI: argument checks, workspace
 // layouts and launches.  The kernels are in kernels_embed.hpp,
-// kernels_gated.hpp and kernels_orth.hpp.
+// kernels_gated.hpp, kernels_orth.hpp and kernels_orth_small.hpp.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -8,12 +8,12 @@
 #include <cstring>
 #include <string>
 
-#include "hip_host.hpp"
 #include "host.hpp"
 #include "kernels_embed.hpp"
 #include "kernels_gated.hpp"
 #include "kernels_orth.hpp"
 #include "kernels_orth_small.hpp"
+#include "operators_host.hpp"
 
 using namespace ms;
 

@@ -1,5 +1,5 @@
-// Host-side helpers of the HIP sources: a failed runtime call as an ms::Error,
-// and the calling thread's device for the length of a scope.
+// Host-side helpers of operators.hip: a failed runtime call as an ms::Error, and
+// the calling thread's device for the length of a scope.
 #pragma once
 
 #include <hip/hip_runtime.h>

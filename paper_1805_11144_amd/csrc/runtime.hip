@@ -24,7 +24,6 @@
 
 #include <mutex>
 
-#include "hip_host.hpp"
 #include "host.hpp"
 #include "kernels.hpp"
 #include "kernels_window.hpp"
@@ -37,6 +36,13 @@ using namespace ms;
 // per GPU, held until the process ends.  In host code its name is only a
 // handle; its device address (per device) comes from hipGetSymbolAddress.
 static __device__ __align__(256) float scratch[MS_PROBE_READ_STATIC_MAX];
+
+#define HIPCHECK(expr)                                                                    \
+  do {                                                                                    \
+    hipError_t _e = (expr);                                                               \
+    if (_e != hipSuccess)                                                                 \
+      ms::fail(MS_E_HIP, std::string(#expr) + ": " + hipGetErrorString(_e));              \
+  } while (0)
 
 namespace {
 
@@ -217,6 +223,18 @@ struct ms_sim {
 };
 
 namespace {
+
+struct DeviceGuard {
+  int prev = 0;
+  explicit DeviceGuard(int dev) {
+    HIPCHECK(hipGetDevice(&prev));
+    if (prev != dev) HIPCHECK(hipSetDevice(dev));
+  }
+  ~DeviceGuard() {
+    int cur = 0;
+    if (hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
+  }
+};
 
 // Device address of `scratch` on each device, resolved once per device with
 // that device current (at simulator creation).
