@@ -11,8 +11,8 @@
 // digit first, 8 to 10 bits a pass), so each table row is the sum of a run of
 // positions in ascending order.  A run of more than 64 is summed in pieces that
 // are added in their order, since a token's frequency falls with its rank and
-// the first ones fill whole batches: with one group of threads to a row 262144
-// rows took 12.8 ms, of which 12.4 were the longest run.
+// the first ones fill whole batches: with one group of threads to every row
+// 262144 rows took 12.8 ms, in pieces 0.29.
 // Measured, 262144 rows of 1024 bf16 into 65536 x 1024 float32 (0.81 GB): sort
 // 37 us, pieces (0.29 GB) 60, rows (0.52 GB) 95: 5.2 TB/s of the sums' bytes.
 // 12800 x 784 float32 into 10007 rows (71 MB): sort 19 us, pieces and row
