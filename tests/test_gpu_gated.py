@@ -332,3 +332,26 @@ def test_any_nan_travels_between_chunks(dtype):
     dv, dg, dy0 = M.gated_lowpass_grad(v, g, kept, dy, dlast=dlast)
     assert torch.isnan(dv[0, :2501, 4]).all() and not torch.isnan(dv[0, 2501:, 4]).any() and torch.isnan(dv[0, :, 5]).all()
     assert torch.isnan(dy0[0, 2]) and torch.isnan(dy0[0, 4]) and torch.isnan(dy0[0, 5]) and not torch.isnan(dy0[0, 6])
+
+
+def test_outputs_in_wider_arrays_through_the_c_call():
+    """y with strides of its own: steps first, inside wider rows; nothing around it is written."""
+    import ctypes as C
+
+    from paper_1805_11144_amd import mergesim as MS
+    b, t, d = 3, 700, 40
+    v, g, y0, lengths, _, _ = inputs(b, t, d, F32, 16, True, True)
+    want, last = M.gated_lowpass(v, g, y0=y0, lengths=lengths)
+    wide = torch.full((t, b, d + 8), 7.0, device=DEV)
+    desc = MS.GatedLowpassDesc(batch=b, steps=t, dim=d, dtype=MS.DTYPE_F32, device=0,
+                               stream=torch.cuda.current_stream().cuda_stream)
+    desc.y_stride[0], desc.y_stride[1] = d + 8, b * (d + 8)
+    n = C.c_int64()
+    assert MS.load_library().ms_gated_lowpass_workspace(desc, C.byref(n)) == 0
+    ws = torch.empty(max(n.value, 1), dtype=torch.uint8, device=DEV)
+    got = torch.empty_like(last)
+    code = MS.load_library().ms_gated_lowpass(desc, v.data_ptr(), g.data_ptr(), y0.data_ptr(), lengths.data_ptr(),
+                                              wide[:, :, 4:].data_ptr(), got.data_ptr(), None, ws.data_ptr(), n.value)
+    assert code == 0
+    assert torch.equal(wide[:, :, 4:4 + d].transpose(0, 1), want) and torch.equal(got, last)
+    assert (wide[:, :, :4] == 7).all() and (wide[:, :, 4 + d:] == 7).all()

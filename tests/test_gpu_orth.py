@@ -164,3 +164,37 @@ def test_same_bits_again_on_another_stream_and_in_a_graph(batch, rows, cols):
         torch.cuda.synchronize()
         assert torch.equal(got, other if k % 2 else want)
         x.copy_(x.flip(1))
+
+
+@pytest.mark.parametrize("rows,cols", [(30, 20), (20, 30), (150, 90), (90, 150)])
+def test_outputs_in_wider_arrays_through_the_c_call(rows, cols):
+    """out with strides of its own; nothing around it is written."""
+    import ctypes as C
+
+    from paper_1805_11144_amd import mergesim as MS
+    x = matrices(3, rows, cols, 40).float().to(DEV)
+    want = M.orthogonalise(x)
+    wide = torch.full((3, rows + 1, cols + 8), 7.0, device=DEV)
+    desc = MS.OrthDesc(batch=3, rows=rows, cols=cols, eps=1e-7, steps=5, dtype=MS.DTYPE_F32, device=0,
+                       stream=torch.cuda.current_stream().cuda_stream)
+    desc.coef[:] = M.operators.NEWTON_SCHULZ
+    desc.out_stride[0], desc.out_stride[1] = (rows + 1) * (cols + 8), cols + 8
+    n = C.c_int64()
+    assert MS.load_library().ms_orth_workspace(desc, 0, C.byref(n)) == 0
+    ws = torch.empty(max(n.value, 1), dtype=torch.uint8, device=DEV)
+    assert MS.load_library().ms_orthogonalise(desc, x.data_ptr(), wide[:, :, 4:].data_ptr(), ws.data_ptr(), n.value) == 0
+    assert torch.equal(wide[:, :rows, 4:4 + cols], want)
+    assert (wide[:, :, :4] == 7).all() and (wide[:, :, 4 + cols:] == 7).all() and (wide[:, rows:] == 7).all()
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 900, 1000), (1, 768, 2300), (2, 2100, 800), (1, 2300, 2100)])
+def test_large_sides_in_16_bits(batch, rows, cols):
+    """One part for a value from 768 rows and columns on, on every size of tile, padded and not."""
+    x = matrices(batch, rows, cols, 41).to(BF16)
+    assert off(M.orthogonalise(x.to(DEV)), orth64(x)) <= TOL[BF16]
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 2300, 2100), (3, 1100, 1300)])
+def test_large_sides_in_32_bits(batch, rows, cols):
+    x = matrices(batch, rows, cols, 42).float()
+    assert off(M.orthogonalise(x.to(DEV)), orth64(x)) <= TOL[F32]
