@@ -524,7 +524,8 @@ ms_status ms_sim_set_train_param(ms_sim* sim, int32_t which, int32_t id, int32_t
  * equal bits, whatever ran before.
  *
  * Types: MS_DTYPE_F32 or MS_DTYPE_BF16 arrays; everything is computed in 32
- * bits and rounded to nearest even once, at the end.  Strides are in elements,
+ * bits and rounded to nearest even once, at the end, but for the matrices of
+ * orthogonalised updates (22 bits, see there).  Strides are in elements,
  * rows themselves are contiguous, and a stride of 0 in a descriptor stands for
  * the packed one.  Output arrays must not overlap other arrays.  Empty inputs
  * (no tokens, no steps, no rows) are valid.  MS_E_INVALID, before anything is
@@ -618,10 +619,13 @@ ms_status ms_gated_lowpass_step(const ms_gated_step_desc* desc, const void* v, c
  *                                                 products from the right where rows > cols)
  * which moves the singular values of X towards one and keeps its singular
  * vectors.  MS_E_INVALID where c0..c2 let a singular value of an iterate, or
- * the polynomial, exceed 1000 in size.  The products run on 16-bit matrix instructions
- * with 32-bit sums, matrices as the sum of two 16-bit parts (22 bits), bf16
- * results of 768 rows and columns and more with one (11 bits, finer than the
- * result's rounding).
+ * the polynomial, exceed 1000 in size.  Small matrices are computed in 32 bits
+ * throughout.  The products of the others run on 16-bit matrix instructions with
+ * 32-bit sums, matrices as the sum of two 16-bit parts: 22 bits, for results of
+ * either type, and none smaller than 2^-24 of fp16's 1 after a scaling that puts
+ * the largest value that c0..c2 allow at 8192 to 32768.  So values below about
+ * 2^-39 of that largest one are 0, as in a matrix whose norm is many orders of
+ * magnitude below eps.
  *
  * ms_orthogonal_update trains a float32 weight with it:
  *     momentum <- momentum_decay * momentum + grad

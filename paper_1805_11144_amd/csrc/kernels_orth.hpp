@@ -6,10 +6,12 @@
 // hi + lo, two fp16 numbers (22 bits), and a product of two matrices is
 // hi hi' + hi lo' + lo hi' in float32 sums; the missing lo lo' is 2^-22 of the
 // result, the size of a float32 sum's own rounding.  (Against 64 bits the result
-// is about half as far off as five iterations of float32 products are.)  Where
-// the result is rounded to bf16 one part can be enough (11 bits against the
-// result's 8).  Matrices are scaled by powers of two that their bounds allow,
-// so the parts stay clear of fp16's ends.
+// is about half as far off as five iterations of float32 products are.)  A bf16
+// result takes the same two parts: an iteration lets the rounding of small
+// singular values grow with them, by 3.4445^5 = 485 in all, and with one part
+// (11 bits) a matrix of 16 strong directions came out 4e-2 off, 25 times its own
+// rounding.  Matrices are scaled by powers of two that their bounds allow, so
+// the parts stay clear of fp16's ends.
 //
 // Layout: n = min(rows, cols) <= m = the other; X [n][m] and its transpose
 // [m][n] in fp16 parts, A and Q = c0 I + c1 A + c2 A A as [n][n], every side
@@ -18,15 +20,12 @@
 // A and Q are symmetric: blocks below the diagonal are the others' mirror
 // images and are not computed.
 //
-// What bounds it: large matrices the matrix cores (4096 x 4096, Q X in one
-// part 143 us, 0.96 PFLOP/s, where a large library product in bf16 reaches 1.2;
-// in two parts 333 us, 1.24 PFLOP/s of 16-bit products; X X' 92 us, its half of
-// the blocks at 0.75 PFLOP/s), small ones a launch's latency (1024 x 784: 12 to
-// 15 us for each of 15 products that take 2 at full rate).  Step by step at
-// 4096 x 4096 bf16: 2.9 ms with registers between memory and LDS; 2.2 straight
-// to LDS; 1.98 with the last tiles in quarters; 1.88 with slices of k behind
-// each other; 1.75 four slices deep, 256 x 256 tiles for Q X; 1.58 with results
-// in 16-byte words.
+// What bounds it: large matrices the matrix cores (4096 x 4096: Q X 333 us, 1.24
+// PFLOP/s of 16-bit products, where a large library product in bf16 reaches
+// 1.2), small ones a launch's latency (1024 x 784: 12 to 15 us for each of 15
+// products that take 2 at full rate).  Step by step at 4096 x 4096: 5.0 ms with
+// tiles straight from memory to LDS; 4.4 with slices of k behind each other and
+// 256 x 256 tiles for Q X; 4.2 with results in 16-byte words.
 #pragma once
 
 #include "kernels_embed.hpp"
@@ -37,6 +36,7 @@ typedef half_t halfx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int kOrthSlice = 32;    // values of k in a slice
+constexpr int kPair = 2;          // fp16 parts of a value: hi, lo
 constexpr int kOrthParts = 256;   // partial sums of a matrix's norm
 
 // A matrix as the caller holds it.
@@ -118,7 +118,7 @@ __device__ __forceinline__ int64_t orth_at(int64_t rows, int64_t row, int64_t k)
 
 // The first iterate, scale X / (|X| + eps), and its transpose.  grid: batch x
 // (mp / 64) x (np / 64) tiles of 64 x 64.
-template <class T, bool UPDATE, int PL, int KS>
+template <class T, bool UPDATE, int KS>
 __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* parts, double eps, double scale, half_t* X,
                                                     half_t* XT, int32_t np, int32_t mp) {
   __shared__ float tile[64][65];
@@ -161,8 +161,8 @@ __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* par
     else tile[dr][dc] = v;
   }
   __syncthreads();
-  half_t* x0 = X + mat * PL * np * (int64_t)mp;
-  half_t* t0 = XT + mat * PL * np * (int64_t)mp;
+  half_t* x0 = X + mat * kPair * np * (int64_t)mp;
+  half_t* t0 = XT + mat * kPair * np * (int64_t)mp;
   const int64_t plane = (int64_t)np * mp;
   for (int k = tid; k < 64 * 64; k += 256) {
     const int p = k / 64, q = k % 64;
@@ -170,10 +170,10 @@ __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* par
     split(tile[p][q], hi, lo);
     const int64_t xa = orth_at<KS>(np, i0 + p, j0 + q), ta = orth_at<KS>(mp, j0 + p, i0 + q);
     x0[xa] = hi;
-    if (PL == 2) x0[plane + xa] = lo;
+    x0[plane + xa] = lo;
     split(tile[q][p], hi, lo);
     t0[ta] = hi;
-    if (PL == 2) t0[plane + ta] = lo;
+    t0[plane + ta] = lo;
   }
 }
 
@@ -220,21 +220,21 @@ __device__ __forceinline__ void barrier_but() {
 // A slice's rows are KS / 8 chunks of 16 bytes without padding (memory goes to
 // LDS in lane order); chunk c of row r sits at c ^ (r / (128 / KS)), so the
 // rows of a fragment read different banks.
-template <int PL, int TILE, int WC, int KS, int ST, int KG, int END, class T>
+template <int TILE, int WC, int KS, int ST, int KG, int END, class T>
 __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_t mat, int32_t part, int32_t trow,
                                           int32_t tcol) {
   constexpr int NW = 2 * WC, WM = TILE / 2, WN = TILE / WC, BI = WM / 32, BJ = WN / 32;
-  constexpr int CH = KS / 8, U = PL * TILE * CH / (64 * NW);
+  constexpr int CH = KS / 8, U = kPair * TILE * CH / (64 * NW);
   static_assert(BI >= 1 && BJ >= 1 && U >= 1, "work for every wavefront");
   constexpr bool SYM = END == kEndGram || END == kEndPoly || END == kEndPart;
-  constexpr int LEFT = PL * TILE * KS, SLAB = 2 * LEFT;   // of one slice; lds: [KG][ST][SLAB]
+  constexpr int LEFT = kPair * TILE * KS, SLAB = 2 * LEFT;   // of one slice; lds: [KG][ST][SLAB]
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % NW);
   const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW));
   const int wm = wave / WC, wn = wave % WC;
   const auto swizzle = [](int row) { return row / (128 / KS) % CH; };
   const int64_t lplane = (int64_t)g.M * g.K, rplane = (int64_t)g.N * g.K;
-  const half_t* L = g.l + mat * PL * lplane + (int64_t)trow * KS;
-  const half_t* R = g.r + mat * PL * rplane + (int64_t)tcol * KS;
+  const half_t* L = g.l + mat * kPair * lplane + (int64_t)trow * KS;
+  const half_t* R = g.r + mat * kPair * rplane + (int64_t)tcol * KS;
   half_t* own = lds + group * ST * SLAB;
   // the lane's chunks of a slice, in values within a plane
   uint32_t off[U];
@@ -252,7 +252,7 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
     }
   };
   // where a wavefront has a single block, several sums for it, so that a product does not wait for the one before
-  constexpr int NA = BI * BJ > 1 ? 1 : PL == 2 ? 3 : 2;
+  constexpr int NA = BI * BJ > 1 ? 1 : 3;
   floatx16 acc[BI][BJ], more[NA > 1 ? NA - 1 : 1];
 #pragma unroll
   for (int i = 0; i < BI; ++i)
@@ -261,12 +261,12 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
 #pragma unroll
   for (int n = 0; n < NA - 1; ++n) more[n] = floatx16{};
   // A's values for the polynomial, on their way while the product is made
-  [[maybe_unused]] half_t early[PL][16];
+  [[maybe_unused]] half_t early[kPair][16];
   constexpr bool EARLY = END == kEndPoly && BI * BJ == 1;
   if constexpr (EARLY) {
-    const half_t* A = g.a + mat * PL * lplane;   // A has the product's shape and K its side
+    const half_t* A = g.a + mat * kPair * lplane;   // A has the product's shape and K its side
 #pragma unroll
-    for (int p = 0; p < PL; ++p)
+    for (int p = 0; p < kPair; ++p)
 #pragma unroll
       for (int q = 0; q < 16; ++q)
         early[p][q] = A[p * lplane + orth_at<KS>(g.M, trow + wm * WM + 8 * (q / 4) + 4 * (lane / 32) + q % 4,
@@ -285,12 +285,12 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
     if (s0 + (ST - 1) * KG <= slices) barrier_but<(ST - 2) * 2 * U>();
     else barrier_but<0>();
     const half_t *Ls = own + buf * SLAB, *Rs = Ls + LEFT;
-    halfx8 a[KS / 16][PL][BI], b[KS / 16][PL][BJ];
+    halfx8 a[KS / 16][kPair][BI], b[KS / 16][kPair][BJ];
     if (s < slices) {
 #pragma unroll
       for (int ks = 0; ks < KS / 16; ++ks)
 #pragma unroll
-        for (int p = 0; p < PL; ++p) {
+        for (int p = 0; p < kPair; ++p) {
           const int c = 2 * ks + lane / 32;
 #pragma unroll
           for (int i = 0; i < BI; ++i) {
@@ -316,14 +316,9 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
             floatx16& s0 = acc[i][j];
             floatx16& s1 = NA > 1 ? more[0] : s0;
             floatx16& s2 = NA > 2 ? more[NA > 2 ? 1 : 0] : s0;
-            if constexpr (PL == 2) {
-              s1 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][1][i], b[ks][0][j], s1, 0, 0, 0);
-              s2 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][1][j], s2, 0, 0, 0);
-              s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][0][j], s0, 0, 0, 0);
-            } else {
-              floatx16& s = ks % 2 ? s1 : s0;
-              s = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][0][j], s, 0, 0, 0);
-            }
+            s1 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][1][i], b[ks][0][j], s1, 0, 0, 0);
+            s2 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][1][j], s2, 0, 0, 0);
+            s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks][0][i], b[ks][0][j], s0, 0, 0, 0);
           }
     }
     buf = buf + 1 == ST ? 0 : buf + 1;
@@ -351,15 +346,15 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
         for (int q = 0; q < 16; ++q) acc[i][j][q] += sums[((i * BJ + j) * 16 + q) * 64];
   }
   // Results in fp16 parts: a block of 32 x 32 is one piece of memory.  Where a wavefront has several, it writes them
-  // in 16-byte words, through its own 32 rows of 40 in LDS (4096 x 4096 in one part 1.75 -> 1.65 ms); a single one
+  // in 16-byte words, through its own 32 rows of 40 in LDS (4096 x 4096 4.4 -> 4.2 ms); a single one
   // goes out as it lies in the registers (1024 x 784: 187 us, through LDS 204).
   constexpr bool PARTS = END == kEndGram || END == kEndPoly || END == kEndNext, STAGED = PARTS && BI * BJ > 1;
   half_t* block = lds + wave * 32 * 40;
   if (STAGED) __syncthreads();   // the buffers are read
   const int64_t cplane = (int64_t)g.M * g.N;
-  half_t* C = g.c + mat * PL * cplane;
-  half_t* CT = END == kEndNext ? g.ct + mat * PL * cplane : nullptr;
-  const half_t* A = END == kEndPoly ? g.a + mat * PL * cplane : nullptr;
+  half_t* C = g.c + mat * kPair * cplane;
+  half_t* CT = END == kEndNext ? g.ct + mat * kPair * cplane : nullptr;
+  const half_t* A = END == kEndPoly ? g.a + mat * kPair * cplane : nullptr;
 #pragma unroll
   for (int i = 0; i < BI; ++i)
 #pragma unroll
@@ -391,11 +386,9 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
             if constexpr (END == kEndPoly) {
               float av;
               if constexpr (EARLY) {
-                av = (float)early[0][4 * q4 + q];
-                if (PL == 2) av += (float)early[PL - 1][4 * q4 + q];
+                av = (float)early[0][4 * q4 + q] + (float)early[1][4 * q4 + q];
               } else {
-                av = (float)A[orth_at<KS>(g.M, row, col)];
-                if (PL == 2) av += (float)A[cplane + orth_at<KS>(g.M, row, col)];
+                av = (float)A[orth_at<KS>(g.M, row, col)] + (float)A[cplane + orth_at<KS>(g.M, row, col)];
               }
               v += g.c1 * av + (row == col ? g.c0 : 0.0f);
             }
@@ -406,7 +399,7 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
               block[(8 * q4 + 4 * (lane / 32) + q) * 40 + lane % 32] = h;
             } else {
               C[orth_at<KS>(g.M, row, col)] = h;
-              if (PL == 2) C[cplane + orth_at<KS>(g.M, row, col)] = l;
+              C[cplane + orth_at<KS>(g.M, row, col)] = l;
             }
           }
         }
@@ -415,7 +408,7 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
           if (END == kEndNext || brow != bcol) {
             half_t* D = (SYM ? C : CT) + orth_at<KS>(g.N, col, row0);
             *(halfx4*)D = hi;
-            if (PL == 2) *(halfx4*)(D + cplane) = lo;
+            *(halfx4*)(D + cplane) = lo;
           }
         }
       }
@@ -424,7 +417,7 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
         half_t* D = C + orth_at<KS>(g.M, brow, bcol) + lane * 16;
         const half_t* mine = block + lane / 2 * 40 + lane % 2 * 16;
 #pragma unroll
-        for (int p = 0; p < PL; ++p) {
+        for (int p = 0; p < kPair; ++p) {
           if (p == 1) {
             wave_order();
 #pragma unroll
@@ -453,7 +446,7 @@ __device__ __forceinline__ void orth_place(uint32_t u, uint32_t tm, uint32_t& ti
 }
 
 // `whole` tiles, and the others in quarters.
-template <int PL, int TILE, int WC, int KS, int ST, int KG, int END, class T>
+template <int TILE, int WC, int KS, int ST, int KG, int END, class T>
 __global__ void __launch_bounds__(128 * WC * KG) k_orth_gemm(OrthGemm g) {
   constexpr bool SYM = END == kEndGram || END == kEndPoly || END == kEndPart;
   extern __shared__ __attribute__((aligned(16))) half_t orth_gemm_lds[];
@@ -466,20 +459,20 @@ __global__ void __launch_bounds__(128 * WC * KG) k_orth_gemm(OrthGemm g) {
     if (tile >= g.whole) return;
     orth_place<SYM>(tile % g.per, g.M / TILE, ti, tj);
     const uint32_t mat = tile / g.per;   // of the batch, once for each part
-    orth_tile<PL, TILE, WC, KS, ST, KG, END, T>(g, orth_gemm_lds, mat % g.batch, mat / g.batch, ti * TILE, tj * TILE);
+    orth_tile<TILE, WC, KS, ST, KG, END, T>(g, orth_gemm_lds, mat % g.batch, mat / g.batch, ti * TILE, tj * TILE);
   } else if constexpr (TILE > 64) {
     constexpr uint32_t HALF = TILE / 2;
     const uint32_t part = blockIdx.x - share * 8, tile = g.whole + part / 4;
     orth_place<SYM>(tile % g.per, g.M / TILE, ti, tj);
     ti = 2 * ti + part % 2, tj = 2 * tj + part / 2 % 2;
     if (SYM && ti > tj) return;
-    orth_tile<PL, HALF, WC, KS, ST, 1, END, T>(g, orth_gemm_lds, tile / g.per, 0, ti * HALF, tj * HALF);
+    orth_tile<HALF, WC, KS, ST, 1, END, T>(g, orth_gemm_lds, tile / g.per, 0, ti * HALF, tj * HALF);
   }
 }
 
 // A from the parts of its sum, added in their order.  A thread takes a value of
 // the blocks on and above the diagonal, and its mirror image.
-template <int PL, int KS>
+template <int KS>
 __global__ void __launch_bounds__(256) k_orth_join(OrthGemm g) {
   const int64_t size = (int64_t)g.M * g.M, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= g.batch * size) return;
@@ -490,12 +483,12 @@ __global__ void __launch_bounds__(256) k_orth_join(OrthGemm g) {
   for (int p = 0; p < g.parts; ++p) v += g.sums[p * (int64_t)g.batch * size + i];
   half_t hi, lo;
   split(g.f * v, hi, lo);
-  half_t* C = g.c + mat * PL * size;
+  half_t* C = g.c + mat * kPair * size;
   const int64_t at = orth_at<KS>(g.M, row, col), mirror = orth_at<KS>(g.M, col, row);
   C[at] = hi;
-  if (PL == 2) C[size + at] = lo;
+  C[size + at] = lo;
   if (row / 32 < col / 32) {
     C[mirror] = hi;
-    if (PL == 2) C[size + mirror] = lo;
+    C[size + mirror] = lo;
   }
 }

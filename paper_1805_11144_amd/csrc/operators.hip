@@ -311,20 +311,20 @@ OrthTiles orth_tiles(OrthTile kind, bool sym, int64_t batch, int64_t rows, int64
 }
 
 // What a product takes with a kind of tile, in us for 4096 values of k: rounds
-// of the CUs times what one took on this card, for one part and two.
-double orth_cost(OrthTile kind, int parts, bool sym, int64_t batch, int64_t rows, int64_t cols) {
-  static const double round[2][3] = {{20, 38, 130}, {42, 112, 333}};
+// of the CUs times what one took on this card.
+double orth_cost(OrthTile kind, bool sym, int64_t batch, int64_t rows, int64_t cols) {
+  static const double round[3] = {42, 112, 333};
   const OrthTiles t = orth_tiles(kind, sym, batch, rows, cols);
-  return ((double)((t.whole + kCUs - 1) / kCUs) + (t.over ? 0.3 : 0.0)) * round[parts - 1][kind];
+  return ((double)((t.whole + kCUs - 1) / kCUs) + (t.over ? 0.3 : 0.0)) * round[kind];
 }
 
 // The cheapest tile whose sides divide `pad`: large ones read less, small ones
 // are more, for the CUs to share.
-OrthTile orth_choose(int64_t pad, int parts, bool sym, int64_t batch, int64_t rows, int64_t cols, double* cost) {
+OrthTile orth_choose(int64_t pad, bool sym, int64_t batch, int64_t rows, int64_t cols, double* cost) {
   OrthTile best = kTile64;
-  double least = orth_cost(best, parts, sym, batch, rows, cols);
+  double least = orth_cost(best, sym, batch, rows, cols);
   const auto offer = [&](OrthTile k) {
-    const double c = orth_cost(k, parts, sym, batch, rows, cols);
+    const double c = orth_cost(k, sym, batch, rows, cols);
     if (c < least) best = k, least = c;
   };
   if (pad >= 128) offer(kTile128);
@@ -336,7 +336,6 @@ OrthTile orth_choose(int64_t pad, int parts, bool sym, int64_t batch, int64_t ro
 struct Orth {
   int64_t n, m, np, mp;
   int64_t pad;            // to whole tiles of this side
-  int parts;              // fp16 parts of a value
   int split;              // workgroups that share the sum over m of a tile of X X'
   double sx, sa, sq;      // scales of X, A and Q
   int64_t xm, xr, om, orow;
@@ -346,7 +345,7 @@ struct Orth {
 
 constexpr int64_t kOrthLds = 156 * 1024;   // of 160 KB
 
-Orth check_orth(const ms_orth_desc* d, bool update) {
+Orth check_orth(const ms_orth_desc* d) {
   need(d != nullptr, "NULL descriptor");
   need(d->rows >= 1 && d->rows <= 65536 && d->cols >= 1 && d->cols <= 65536, "rows and cols must be in [1, 65536]");
   need(d->batch >= 0, "batch must not be negative");
@@ -364,16 +363,12 @@ Orth check_orth(const ms_orth_desc* d, bool update) {
   pair(d->x_stride, o.xm, o.xr);
   pair(d->out_stride, o.om, o.orow);
   o.n = std::min(d->rows, d->cols), o.m = std::max(d->rows, d->cols);
-  // bf16: one part from 768 rows on, where products bound the time (4096 x 4096 1.8 ms, with two 4.4) and the
-  // result is at most 1.25 times as far off as its rounding alone; 1.34 times at 256 rows, for less than it saves
-  o.parts = !update && d->dtype == MS_DTYPE_BF16 && o.n >= 768 ? 1 : 2;
-  // tiles of 128 x 128 read half as much; of 64 x 64 where the others would not fill the CUs
   double least = INFINITY;
   for (int64_t pad : {64, 128, 256}) {   // larger tiles pad more
     const int64_t n = up(o.n, pad), m = up(o.m, pad);
     double square, next;
-    orth_choose(pad, o.parts, true, d->batch, n, n, &square);
-    orth_choose(pad, o.parts, false, d->batch, n, m, &next);
+    orth_choose(pad, true, d->batch, n, n, &square);
+    orth_choose(pad, false, d->batch, n, m, &next);
     const double cost = square * (m + n) + next * n;
     if (cost < least) least = cost, o.pad = pad, o.np = n, o.mp = m;
   }
@@ -429,7 +424,7 @@ OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
   Carve c{(char*)ws};
   OrthWork w{};
   if (o.small) return w;
-  const int64_t big = d->batch * o.parts * o.np * o.mp, small = d->batch * o.parts * o.np * o.np;
+  const int64_t big = d->batch * kPair * o.np * o.mp, small = d->batch * kPair * o.np * o.np;
   w.parts = c.take<double>(d->batch * kOrthParts);
   w.x = c.take<half_t>(big);
   w.t[0] = c.take<half_t>(big);
@@ -441,29 +436,28 @@ OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
   return w;
 }
 
-template <int PL, int END, class T, int TILE, int WC, int ST, int KG>
+template <int END, class T, int TILE, int WC, int ST, int KG>
 void orth_launch(OrthGemm g, const OrthTiles& t, hipStream_t st) {
-  constexpr size_t lds = KG * ST * PL * 2 * TILE * kOrthSlice * sizeof(half_t);
+  constexpr size_t lds = KG * ST * kPair * 2 * TILE * kOrthSlice * sizeof(half_t);
   static_assert(lds >= (KG - 1) * TILE * TILE * sizeof(float) && lds <= 160 * 1024, "LDS");
   g.per = (uint32_t)t.per, g.whole = (uint32_t)t.whole;
-  constexpr auto k = k_orth_gemm<PL, TILE, WC, kOrthSlice, ST, KG, END, T>;
+  constexpr auto k = k_orth_gemm<TILE, WC, kOrthSlice, ST, KG, END, T>;
   if (lds >= 65536) HIPCHECK(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
   hipLaunchKernelGGL(k, dim3((unsigned)(up(t.whole, 8) + 4 * t.over)), dim3(128 * WC * KG), lds, st, g);
 }
 
-template <int PL, int END, class T>
+template <int END, class T>
 void orth_gemm(const OrthGemm& g, int64_t pad, int64_t batch, hipStream_t st) {
   constexpr bool SYM = END == kEndGram || END == kEndPoly;
-  constexpr int DEEP = PL == 1 ? 4 : 2;   // slices in LDS
-  const OrthTile kind = orth_choose(pad, PL, SYM, batch, g.M, g.N, nullptr);
+  const OrthTile kind = orth_choose(pad, SYM, batch, g.M, g.N, nullptr);
   const OrthTiles t = orth_tiles(kind, SYM, batch, g.M, g.N);
-  if (kind == kTile64) orth_launch<PL, END, T, 64, 2, 3, 2>(g, t, st);
-  else if (kind == kTile128) orth_launch<PL, END, T, 128, 2, DEEP, 1>(g, t, st);
-  else orth_launch<PL, END, T, 256, 4, DEEP, 1>(g, t, st);
+  if (kind == kTile64) orth_launch<END, T, 64, 2, 3, 2>(g, t, st);
+  else if (kind == kTile128) orth_launch<END, T, 128, 2, 2, 1>(g, t, st);
+  else orth_launch<END, T, 256, 4, 2, 1>(g, t, st);
 }
 
 // T: type of x (or the gradient); UPDATE: with momentum, into a weight.
-template <class T, bool UPDATE, int PL>
+template <class T, bool UPDATE>
 void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, OrthGemm out, hipStream_t st) {
   const int64_t blocks = d->batch * (o.np / 64) * (o.mp / 64);
   const dim3 norms((unsigned)(d->batch * kOrthParts));
@@ -476,7 +470,7 @@ void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork
            (uintptr_t)src.momentum % 16 == 0)
     norm(std::integral_constant<int, 4>{});
   else norm(std::integral_constant<int, 1>{});
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, PL, kOrthSlice>), dim3((unsigned)blocks), dim3(256), 0, st, src,
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, kOrthSlice>), dim3((unsigned)blocks), dim3(256), 0, st, src,
                      (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], (int32_t)o.np, (int32_t)o.mp);
   using R = std::conditional_t<UPDATE, float, T>;
   for (int k = 0; k < d->steps; ++k) {
@@ -487,25 +481,25 @@ void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork
     g.f = (float)(o.sa / (o.sx * o.sx));
     if (o.split > 1) {
       g.sums = w.sums, g.parts = o.split, g.slices = (int32_t)((o.mp / kOrthSlice + o.split - 1) / o.split);
-      orth_launch<PL, kEndPart, R, 64, 2, 3, 2>(g, orth_tiles(kTile64, true, d->batch * o.split, o.np, o.np), st);
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_join<PL, kOrthSlice>), dim3((unsigned)((d->batch * o.np * o.np + 255) / 256)),
+      orth_launch<kEndPart, R, 64, 2, 3, 2>(g, orth_tiles(kTile64, true, d->batch * o.split, o.np, o.np), st);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_join<kOrthSlice>), dim3((unsigned)((d->batch * o.np * o.np + 255) / 256)),
                          dim3(256), 0, st, g);
     } else {
-      orth_gemm<PL, kEndGram, R>(g, o.pad, d->batch, st);
+      orth_gemm<kEndGram, R>(g, o.pad, d->batch, st);
     }
     g.parts = 1, g.slices = INT32_MAX / 2;
     g.l = g.r = w.a, g.K = (int32_t)o.np, g.c = w.q, g.a = w.a;
     g.f = (float)(d->coef[2] * o.sq / (o.sa * o.sa));
     g.c0 = (float)(d->coef[0] * o.sq), g.c1 = (float)(d->coef[1] * o.sq / o.sa);
-    orth_gemm<PL, kEndPoly, R>(g, o.pad, d->batch, st);
+    orth_gemm<kEndPoly, R>(g, o.pad, d->batch, st);
     OrthGemm x = out;
     x.l = w.q, x.r = w.t[k % 2], x.M = (int32_t)o.np, x.N = (int32_t)o.mp, x.K = (int32_t)o.np;
     if (k + 1 < d->steps) {
       x.c = w.x, x.ct = w.t[(k + 1) % 2], x.f = (float)(1.0 / o.sq);
-      orth_gemm<PL, kEndNext, R>(x, o.pad, d->batch, st);
+      orth_gemm<kEndNext, R>(x, o.pad, d->batch, st);
     } else {
       x.f = (float)(1.0 / (o.sq * o.sx));
-      orth_gemm<PL, UPDATE ? kEndUpdate : kEndOut, R>(x, o.pad, d->batch, st);
+      orth_gemm<UPDATE ? kEndUpdate : kEndOut, R>(x, o.pad, d->batch, st);
     }
   }
   HIPCHECK(hipGetLastError());
@@ -536,11 +530,10 @@ void orth_small(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, const 
   HIPCHECK(hipGetLastError());
 }
 
-template <class T, bool UPDATE, int PL>
-void orth(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, const OrthGemm& out,
-                hipStream_t st) {
+template <class T, bool UPDATE>
+void orth(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, const OrthGemm& out, hipStream_t st) {
   if (o.small) orth_small<T, UPDATE>(d, o, src, out, st);
-  else orth_run<T, UPDATE, PL>(d, o, src, w, out, st);
+  else orth_run<T, UPDATE>(d, o, src, w, out, st);
 }
 
 }  // namespace
@@ -772,7 +765,7 @@ ms_status ms_gated_lowpass_step(const ms_gated_step_desc* d, const void* v, cons
 
 ms_status ms_orth_workspace(const ms_orth_desc* d, int32_t update, int64_t* bytes_out) {
   return guarded([&] {
-    const Orth o = check_orth(d, update != 0);
+    const Orth o = check_orth(d);
     need(bytes_out != nullptr, "NULL output");
     *bytes_out = orth_work(d, o, nullptr).bytes;
   });
@@ -780,7 +773,7 @@ ms_status ms_orth_workspace(const ms_orth_desc* d, int32_t update, int64_t* byte
 
 ms_status ms_orthogonalise(const ms_orth_desc* d, const void* x, void* out, void* workspace, int64_t workspace_bytes) {
   return guarded([&] {
-    const Orth o = check_orth(d, false);
+    const Orth o = check_orth(d);
     if (d->batch == 0) return;
     need(x && out, "NULL array");
     need(o.om >= (d->rows - 1) * o.orow + d->cols || d->batch <= 1, "the matrices of out must not overlap");
@@ -794,16 +787,15 @@ ms_status ms_orthogonalise(const ms_orth_desc* d, const void* x, void* out, void
     OrthSrc src{x, nullptr, o.xm, o.xr, d->rows, d->cols, 0.0f, 0};
     OrthGemm g{};
     g.out = out, g.mat = o.om, g.row = o.orow, g.rows = d->rows, g.cols = d->cols;
-    if (o.parts == 1) orth<__bf16, false, 1>(d, o, src, w, g, st);
-    else if (d->dtype == MS_DTYPE_BF16) orth<__bf16, false, 2>(d, o, src, w, g, st);
-    else orth<float, false, 2>(d, o, src, w, g, st);
+    if (d->dtype == MS_DTYPE_BF16) orth<__bf16, false>(d, o, src, w, g, st);
+    else orth<float, false>(d, o, src, w, g, st);
   });
 }
 
 ms_status ms_orthogonal_update(const ms_orth_desc* d, const ms_orth_rule* rule, float* weight, float* momentum,
                                const void* grad, void* workspace, int64_t workspace_bytes) {
   return guarded([&] {
-    const Orth o = check_orth(d, true);
+    const Orth o = check_orth(d);
     need(rule != nullptr, "NULL rule");
     need(std::isfinite(rule->rate) && std::isfinite(rule->momentum_decay) && std::isfinite(rule->weight_decay),
          "rates must be finite");
@@ -820,8 +812,8 @@ ms_status ms_orthogonal_update(const ms_orth_desc* d, const ms_orth_rule* rule, 
     OrthGemm g{};
     g.out = weight, g.mat = d->rows * d->cols, g.row = d->cols, g.rows = d->rows, g.cols = d->cols;
     g.keep = (float)(1.0 - rule->rate * rule->weight_decay), g.rate = (float)rule->rate;
-    if (d->dtype == MS_DTYPE_BF16) orth<__bf16, true, 2>(d, o, src, w, g, st);
-    else orth<float, true, 2>(d, o, src, w, g, st);
+    if (d->dtype == MS_DTYPE_BF16) orth<__bf16, true>(d, o, src, w, g, st);
+    else orth<float, true>(d, o, src, w, g, st);
   });
 }
 
