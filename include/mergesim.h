@@ -563,7 +563,9 @@ ms_status ms_embed_grad(const ms_embed_desc* desc, const void* tokens, const voi
 /* Gated lowpass: a lowpass synapse (y <- a y + (1 - a) v) whose coefficient is
  * set at every step and for every channel by a logit g:
  *     a = 1 / (1 + exp(-g));   y[t] = a[t] y[t-1] + (1 - a[t]) v[t],   y[-1] = y0.
- * g = -inf forgets the state (a sequence starts), g = +inf keeps it.
+ * g = -inf forgets the state (a sequence starts), g = +inf keeps it, and neither
+ * takes anything of the other side, were it infinite or NaN: where a is 0 in 32
+ * bits, a y[t-1] and a d are 0, where 1 - a is, (1 - a) v and (1 - a) d.
  * lengths (int32 [batch], clamped to [0, steps]; NULL = steps): what lies past
  * a row's length is not used, y there is 0 and the state stays.
  *   y0    [batch][dim] float32, or NULL for zeros
