@@ -53,6 +53,7 @@ struct GatedArgs {
   const int32_t* lengths;
   int32_t nchunk, groups;           // chunks of blockDim / 64 * kKeep steps; workgroups per chunk
   int32_t per_row;                  // workgroups per batch row (SPAN = false)
+  int64_t first;                    // the launch's first group (LINK = false)
   // LINK: what chunks leave for each other, all ones before the launch
   uint64_t* maps;                   // [nchunk][batch * dim]: (A, Y)
   uint32_t* states;                 // [nchunk / kSpan][batch * dim]
@@ -161,7 +162,7 @@ struct GatedPlace {
 
 template <bool LINK>
 __device__ __forceinline__ GatedPlace gated_place(const GatedArgs& p, uint32_t* box) {
-  if (!LINK) return {0, (int64_t)blockIdx.x};
+  if (!LINK) return {0, p.first + (int64_t)blockIdx.x};
   if (threadIdx.x == 0) *box = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   const uint32_t t = __builtin_amdgcn_readfirstlane(*box);

@@ -271,13 +271,18 @@ GatedShape gated_shape(Gated& g) {
   return {(unsigned)waves * 64, link, span};
 }
 
-// Calls f(link, span, grid) with the shape's choices as compile-time values.
+// Calls f(args, link, span, grid) with the shape's choices as compile-time
+// values: once, or for as many groups at a time as a grid holds (its threads fit
+// 31 bits).
 template <class F>
-void gated_launch(const GatedShape& s, const GatedArgs& a, F&& f) {
+void gated_launch(const GatedShape& s, GatedArgs a, F&& f) {
   const auto with = [&](auto link) {
-    const dim3 grid((unsigned)(s.link ? a.nchunk * a.groups : a.groups));
-    if (s.span) f(link, std::true_type{}, grid);
-    else f(link, std::false_type{}, grid);
+    const int64_t all = s.link ? a.nchunk * a.groups : a.groups, most = ((int64_t)1 << 31) / s.threads;
+    for (a.first = 0; a.first < all; a.first += most) {
+      const dim3 grid((unsigned)std::min(all - a.first, most));
+      if (s.span) f(a, link, std::true_type{}, grid);
+      else f(a, link, std::false_type{}, grid);
+    }
   };
   if (s.link) with(std::true_type{});
   else with(std::false_type{});
@@ -677,7 +682,7 @@ ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* d, const void* v, const 
     with_type<2, 1>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
-      gated_launch(shape, a, [&](auto link, auto span, dim3 grid) {
+      gated_launch(shape, a, [&](const GatedArgs& a, auto link, auto span, dim3 grid) {
         hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated<T, V, decltype(link)::value, decltype(span)::value>), grid,
                            dim3(shape.threads), 0, st, a, (const T*)v, (const T*)g, y0, (T*)y, last, kept);
       });
@@ -718,7 +723,7 @@ ms_status ms_gated_lowpass_grad(const ms_gated_lowpass_desc* d, const void* v, c
     with_type<2, 1>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
-      gated_launch(shape, a, [&](auto link, auto span, dim3 grid) {
+      gated_launch(shape, a, [&](const GatedArgs& a, auto link, auto span, dim3 grid) {
         hipLaunchKernelGGL(HIP_KERNEL_NAME(k_gated_grad<T, V, decltype(link)::value, decltype(span)::value>), grid,
                            dim3(shape.threads), 0, st, a, (const T*)v, (const T*)g, kept, (const T*)dy, dlast, (T*)dv, (T*)dg,
                            dy0);
