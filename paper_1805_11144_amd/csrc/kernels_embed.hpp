@@ -99,6 +99,7 @@ __global__ void __launch_bounds__(256) k_embed(const I* tokens, const T* table, 
 
 // ------------------------------------------------------------------ sort
 constexpr int kSortBits = 10;   // of a digit, at most
+constexpr int kSortBlock = 64;  // tiles whose counts k_sort_prefix adds up together
 
 // A digit has BITS bits, 8 to 10, and counters come in rows of 256 PER = 2^BITS.
 // A tile is 256 N pairs.
@@ -127,6 +128,40 @@ __global__ void __launch_bounds__(256) k_sort_count(const I* tokens, const uint3
 #pragma unroll
   for (int q = 0; q < PER; ++q)
     counts[((int64_t)blockIdx.x * PER + q) * 256 + threadIdx.x] = hist[q * 256 + threadIdx.x];
+}
+
+// Turns n rows of a column, `digits` apart, into the sums of the rows before;
+// returns the sum of all.
+__device__ __forceinline__ uint32_t column_prefix(uint32_t* c, int32_t n, int32_t digits) {
+  constexpr int A = 32;   // rows in flight
+  uint32_t sum = 0;
+  for (int32_t t = 0; t < n; t += A) {
+    uint32_t x[A];
+#pragma unroll
+    for (int u = 0; u < A; ++u) x[u] = t + u < n ? c[(int64_t)(t + u) * digits] : 0;
+#pragma unroll
+    for (int u = 0; u < A; ++u) {
+      if (t + u < n) c[(int64_t)(t + u) * digits] = sum;
+      sum += x[u];
+    }
+  }
+  return sum;
+}
+
+// Counts of many tiles as sums over the tiles before, so that a tile reads its
+// own and its block's and not all tiles' counts.  counts[tile][digit] becomes the
+// digit's pairs in the earlier tiles of its block of kSortBlock, and
+// block[b][digit] those of block b.  One thread to a column of a block.
+__global__ void __launch_bounds__(256) k_sort_prefix(uint32_t* counts, uint32_t* block, int32_t tiles, int32_t digits) {
+  const int64_t d = (int64_t)blockIdx.x % (digits / 256) * 256 + threadIdx.x, b = blockIdx.x / (digits / 256);
+  const int32_t n = (int32_t)min((int64_t)kSortBlock, tiles - b * kSortBlock);
+  block[b * digits + d] = column_prefix(counts + b * kSortBlock * digits + d, n, digits);
+}
+
+// The same over the blocks; block[blocks] ends as the digits' pairs in all.
+__global__ void __launch_bounds__(256) k_sort_blocks(uint32_t* block, int32_t blocks, int32_t digits) {
+  uint32_t* c = block + (int64_t)blockIdx.x * 256 + threadIdx.x;
+  c[(int64_t)blocks * digits] = column_prefix(c, blocks, digits);
 }
 
 // The lanes of a wavefront that hold live keys of this lane's digit.
@@ -172,11 +207,13 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
 
 // Moves each pair to its place: behind the pairs of smaller digits, of earlier
 // tiles and of earlier positions in the tile.  Wavefront w holds the tile's
-// positions [w * 64 N, (w + 1) * 64 N) in order of (item, lane).
+// positions [w * 64 N, (w + 1) * 64 N) in order of (item, lane).  `block`: the
+// sums that k_sort_prefix and k_sort_blocks left; NULL: every tile adds up the
+// counts of all.
 template <class I, int BITS, int N>
 __global__ void __launch_bounds__(256) k_sort_move(const I* tokens, const uint32_t* keys, const uint32_t* pos,
                                                    int64_t n, int64_t vocab, int shift, const uint32_t* counts,
-                                                   uint32_t* keys_out, uint32_t* pos_out) {
+                                                   const uint32_t* block, uint32_t* keys_out, uint32_t* pos_out) {
   constexpr int PER = 1 << (BITS - 8);
   __shared__ uint32_t part[4][256 * PER];   // a wavefront's pairs of each digit, then where its first one goes
   __shared__ uint32_t first[256 * PER];     // pairs of each digit in all tiles, then of smaller digits
@@ -193,9 +230,17 @@ __global__ void __launch_bounds__(256) k_sort_move(const I* tokens, const uint32
   // pairs of the thread's digits, q * 256 + tid, in all tiles and in the earlier ones
   uint32_t before[PER] = {}, total[PER] = {};
   const uint32_t* c = counts + tid;
-  const uint32_t tiles = gridDim.x;
+  const uint32_t tiles = block ? 0 : gridDim.x;
   constexpr int A = 64 / PER;   // tiles in flight
   uint32_t t = 0;
+  if (block) {
+    const uint32_t own = blockIdx.x / kSortBlock, blocks = (gridDim.x + kSortBlock - 1) / kSortBlock;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      before[q] = c[((int64_t)blockIdx.x * PER + q) * 256] + block[((int64_t)own * PER + q) * 256 + tid];
+      total[q] = block[((int64_t)blocks * PER + q) * 256 + tid];
+    }
+  }
   for (; t + A <= tiles; t += A) {
     uint32_t x[A][PER];
 #pragma unroll

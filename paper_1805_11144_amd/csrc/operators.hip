@@ -121,16 +121,21 @@ Embed check_embed(const ms_embed_desc* d) {
   return e;
 }
 
-// Items of a thread in the sort: a tile holds 256 times as many pairs.  Every
-// tile adds up the counts of all tiles, so tiles grow where they become many.
-// Gradients in us with 4, 8 and 16 items: 40000 tokens 50, 56, 64; 100000 59,
-// 62, 73; 262144 101, 98, 104; 524288 138, 112, 111; 1048576 290, 200, 176.
+// Items of a thread in the sort: a tile holds 256 times as many pairs.  Up to
+// kSortAll tiles each adds up the counts of all, so tiles grow where they become
+// many.  Gradients in us with 4, 8 and 16 items: 40000 tokens 50, 56, 64; 100000
+// 59, 62, 73; 262144 101, 98, 104; 524288 138, 112, 111; 1048576 290, 200, 176.
 int sort_items(int64_t n) { return n <= (1 << 17) ? 4 : n <= (1 << 19) ? 8 : 16; }
+
+// With more tiles two launches a digit add up their counts: 131072 tokens in 128
+// tiles 62 us, every tile for itself 56; 1048576 in 256 tiles 175 and 187; 16777216
+// in 4096 tiles 1.9 ms and 11.
+constexpr int64_t kSortAll = 255;
 
 int64_t sort_tiles(int64_t n) { return (n + 256 * sort_items(n) - 1) / (256 * sort_items(n)); }
 
 struct EmbedWork {
-  uint32_t *keys[2], *pos[2], *counts, *start;
+  uint32_t *keys[2], *pos[2], *counts, *block, *start;
   float* part;
   int64_t bytes;
 };
@@ -139,7 +144,9 @@ EmbedWork embed_work(const ms_embed_desc* d, void* ws) {
   Carve c{(char*)ws};
   EmbedWork w;
   for (int i = 0; i < 2; ++i) w.keys[i] = c.take<uint32_t>(d->n_tokens), w.pos[i] = c.take<uint32_t>(d->n_tokens);
-  w.counts = c.take<uint32_t>(sort_tiles(d->n_tokens) << kSortBits);
+  const int64_t tiles = sort_tiles(d->n_tokens);
+  w.counts = c.take<uint32_t>(tiles << kSortBits);
+  w.block = tiles > kSortAll ? c.take<uint32_t>((up(tiles, kSortBlock) / kSortBlock + 1) << kSortBits) : nullptr;
   w.start = c.take<uint32_t>(d->vocab + 1);
   w.part = c.take<float>((d->n_tokens + kRun - 1) / kRun * 2 * d->dim);
   w.bytes = c.used;
@@ -163,8 +170,16 @@ void sort_tiled(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int key_b
     const uint32_t *k = p ? w.keys[in] : nullptr, *q = p ? w.pos[in] : nullptr;
     hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_count<I, BITS, N>), dim3(tiles), dim3(256), 0, st, tokens, k, n, d->vocab,
                        p * BITS, w.counts);
+    if (tiles > kSortAll) {
+      constexpr int digits = 1 << BITS;
+      const unsigned blocks = (tiles + kSortBlock - 1) / kSortBlock;
+      hipLaunchKernelGGL(k_sort_prefix, dim3(blocks * (digits / 256)), dim3(256), 0, st, w.counts, w.block, (int32_t)tiles,
+                         digits);
+      hipLaunchKernelGGL(k_sort_blocks, dim3(digits / 256), dim3(256), 0, st, w.block, (int32_t)blocks, digits);
+    }
     hipLaunchKernelGGL(HIP_KERNEL_NAME(k_sort_move<I, BITS, N>), dim3(tiles), dim3(256), 0, st, tokens, k, q, n, d->vocab,
-                       p * BITS, (const uint32_t*)w.counts, w.keys[in ^ 1], w.pos[in ^ 1]);
+                       p * BITS, (const uint32_t*)w.counts, (const uint32_t*)(tiles > kSortAll ? w.block : nullptr),
+                       w.keys[in ^ 1], w.pos[in ^ 1]);
   }
 }
 
