@@ -4,6 +4,9 @@ Arrays are torch tensors on one GPU; a call runs on that GPU's current torch str
 results and scratch memory with torch and returns without waiting, so it can be captured into a graph.
 torch has to be imported before the library is first used in a process, so that both share one HIP
 runtime.
+
+torch's automatic differentiation does not see these calls: an array that requires a gradient is refused
+(outside torch.no_grad(), which is where a training step of one's own makes them).
 """
 from __future__ import annotations
 
@@ -41,14 +44,22 @@ def _gpu(t, dims, what):
         _setup()
     if not t.is_cuda or t.dim() not in dims:
         raise ValueError(f"{what} on a GPU is wanted, not {tuple(t.shape)} on {t.device}")
+    _undifferentiated(t, what)
     d = _DTYPES.get(t.dtype)
     if d is None:
         raise ValueError(f"{what} is {t.dtype}: float32 or bfloat16 is wanted")
     return d
 
 
+def _undifferentiated(t, what):
+    if t.requires_grad and _torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which torch cannot take through this call: detach it, or call "
+                         "under torch.no_grad() and use the operator's own gradient")
+
+
 def _like(t, first, name, shape, dtype):
     """Checks a tensor's device, shape and type."""
+    _undifferentiated(t, name)
     if t.device != first.device:
         raise ValueError(f"{name} must be on the GPU of the other arrays ({first.device}), not on {t.device}")
     if t.shape != shape:
