@@ -6,7 +6,8 @@ torch has to be imported before the library is first used in a process, so that 
 runtime.
 
 torch's automatic differentiation does not see these calls: an array that requires a gradient is refused
-(outside torch.no_grad(), which is where a training step of one's own makes them).
+(outside torch.no_grad(), which is where a training step of one's own makes them), and an array that a call
+writes in place counts as modified.
 """
 from __future__ import annotations
 
@@ -55,6 +56,14 @@ def _undifferentiated(t, what):
     if t.requires_grad and _torch.is_grad_enabled():
         raise ValueError(f"{what} requires a gradient, which torch cannot take through this call: detach it, or call "
                          "under torch.no_grad() and use the operator's own gradient")
+
+
+def _written(*tensors):
+    """Tells torch that a call writes these, so that a backward pass which saved one raises."""
+    for t in tensors:
+        if t.is_inference() and not _torch.is_inference_mode_enabled():
+            raise RuntimeError("an inference tensor can be written in place in torch.inference_mode() only")
+    _torch.autograd.graph.increment_version(tensors)
 
 
 def _like(t, first, name, shape, dtype):
@@ -130,12 +139,15 @@ def embed(tokens, table, scale=1.0, out=None):
     d = _embed_desc(tokens, table)
     tokens = tokens.contiguous()
     shape = (*tokens.shape, table.shape[1])
-    if out is None:
+    given = out is not None
+    if not given:
         out = _torch.empty(shape, dtype=table.dtype, device=table.device)
     d.vocab, d.dim = table.shape
     d.table_stride, d.scale, d.dtype = _row_stride(table, "table"), scale, dtype
-    _check(_lib.ms_embed(_on(d, table), tokens.data_ptr(), table.data_ptr(),
-                         _packed(out, table, "out", shape, table.dtype)))
+    outp = _packed(out, table, "out", shape, table.dtype)
+    if given:
+        _written(out)
+    _check(_lib.ms_embed(_on(d, table), tokens.data_ptr(), table.data_ptr(), outp))
     return out
 
 
@@ -148,7 +160,8 @@ def embed_grad(tokens, drows, vocab=None, scale=1.0, out=None, accumulate=False)
     dim = drows.shape[-1]
     d = _embed_desc(tokens, drows)
     _like(drows, drows, "drows", (*tokens.shape, dim), drows.dtype)
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate or vocab is None:
             raise ValueError("accumulate needs out" if accumulate else "vocab or out is wanted")
         out = _torch.empty((vocab, dim), dtype=_torch.float32, device=drows.device)
@@ -162,6 +175,8 @@ def embed_grad(tokens, drows, vocab=None, scale=1.0, out=None, accumulate=False)
     d.scale, d.dtype, d.grad_dtype, d.accumulate = scale, dtype, grad_dtype, int(bool(accumulate))
     ref = _on(d, drows)
     hold, ws, n = _scratch(drows, _size(_lib.ms_embed_grad_workspace, ref))
+    if given:
+        _written(out)
     _check(_lib.ms_embed_grad(ref, tokens.data_ptr(), rows.data_ptr(), out.data_ptr(), ws, n))
     return out
 
@@ -236,14 +251,16 @@ def gated_lowpass_step(v, g, state, slots=None, out=None):
     rows, dim = shape = v.shape
     _like(g, v, "g", shape, v.dtype)
     _like(state, v, "state", (state.shape[0], dim), _torch.float32)
+    written = (state,) if out is None else (state, out)
     if out is None:
         out = _torch.empty((rows, dim), dtype=v.dtype, device=v.device)
     else:
         _like(out, v, "out", shape, v.dtype)
     d = GatedStepDesc(rows, state.shape[0], dim, _row_stride(v, "v"), _row_stride(g, "g"), _row_stride(out, "out"),
                       _row_stride(state, "state"), dtype)
-    _check(_lib.ms_gated_lowpass_step(_on(d, v), v.data_ptr(), g.data_ptr(), state.data_ptr(),
-                                      _packed(slots, v, "slots", (rows,), _torch.int32), out.data_ptr()))
+    slotp = _packed(slots, v, "slots", (rows,), _torch.int32)
+    _written(*written)
+    _check(_lib.ms_gated_lowpass_step(_on(d, v), v.data_ptr(), g.data_ptr(), state.data_ptr(), slotp, out.data_ptr()))
     return out
 
 
@@ -267,11 +284,14 @@ def orthogonalise(x, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, out=None):
     """Brings the singular values of a matrix [rows, cols], or of each of a batch, towards one
     (ms_orthogonalise): X <- (c0 I + c1 XX' + c2 XX'XX') X, `steps` times from X / (|X| + eps)."""
     d, x = _orth_desc(x, steps, coefficients, eps)
-    if out is None:
+    given = out is not None
+    if not given:
         out = _torch.empty(x.shape, dtype=x.dtype, device=x.device)
     outp = _packed(out, x, "out", x.shape, x.dtype)
     ref = _on(d, x)
     hold, ws, n = _scratch(x, _size(_lib.ms_orth_workspace, ref, 0))
+    if given:
+        _written(out)
     _check(_lib.ms_orthogonalise(ref, x.data_ptr(), outp, ws, n))
     return out
 
@@ -289,4 +309,5 @@ def orthogonal_update(weight, momentum, grad, rate, momentum_decay=0.95, weight_
     rule = OrthRule(rate, momentum_decay, weight_decay, int(bool(nesterov)))
     ref = _on(d, grad)
     hold, ws, n = _scratch(grad, _size(_lib.ms_orth_workspace, ref, 1))
+    _written(weight, momentum)
     _check(_lib.ms_orthogonal_update(ref, C.byref(rule), wp, mp, grad.data_ptr(), ws, n))

@@ -1,5 +1,5 @@
 """GPU: the operators under torch's automatic differentiation, which they take no part in: an argument that asks for
-a gradient is refused."""
+a gradient is refused, and arrays that are written in place say so, so that a backward pass which saved them raises."""
 import pytest
 import torch
 
@@ -50,3 +50,30 @@ def test_arguments_that_ask_for_a_gradient(k):
             call(a)
         a[name].requires_grad_(False)
         call(a)
+
+
+@pytest.mark.parametrize("k", range(11))
+def test_written_arrays_say_so(k):
+    call, args, written = calls()[k]
+    before = {n: x._version for n, x in args.items()}
+    call(args)
+    for n, x in args.items():
+        assert (x._version > before[n]) == (n in written), n
+
+
+def test_a_backward_pass_that_saved_a_written_array_raises():
+    w, x = torch.randn(9, 7, device=DEV), torch.randn(7, 3, device=DEV, requires_grad=True)
+    loss = torch.matmul(w, x).sum()
+    M.orthogonal_update(w, torch.zeros_like(w), torch.randn(9, 7, device=DEV), rate=0.1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_inference_mode():
+    with torch.inference_mode():
+        state = torch.zeros(2, 8, device=DEV)
+        v = torch.randn(2, 8, device=DEV)
+        assert torch.equal(M.gated_lowpass_step(v, torch.zeros_like(v), state), 0.5 * v)
+    with pytest.raises(RuntimeError, match="[Ii]nference"):
+        M.gated_lowpass_step(v, torch.zeros_like(v), state)
+    assert torch.equal(state, 0.5 * v)
