@@ -114,7 +114,7 @@ Embed check_embed(const ms_embed_desc* d) {
   need_dtype(d->dtype);
   need_dtype(d->grad_dtype);
   need(d->ids == MS_IDS_I32 || d->ids == MS_IDS_I64, "unknown token type");
-  need(std::isfinite(d->scale), "scale must be finite");
+  need(std::isfinite((float)d->scale), "scale must be finite in 32 bits");
   Embed e{d->table_stride ? d->table_stride : d->dim, d->row_stride ? d->row_stride : d->dim};
   need(e.ts >= d->dim && e.ts < kMaxStride && e.os >= d->dim && e.os < kMaxStride,
        "row strides must be at least dim");
@@ -817,8 +817,9 @@ ms_status ms_orthogonal_update(const ms_orth_desc* d, const ms_orth_rule* rule, 
   return guarded([&] {
     const Orth o = check_orth(d);
     need(rule != nullptr, "NULL rule");
-    need(std::isfinite(rule->rate) && std::isfinite(rule->momentum_decay) && std::isfinite(rule->weight_decay),
-         "rates must be finite");
+    const float rate = (float)rule->rate, decay = (float)rule->momentum_decay,
+                keep = (float)(1.0 - rule->rate * rule->weight_decay);
+    need(std::isfinite(rate) && std::isfinite(decay) && std::isfinite(keep), "rates must be finite in 32 bits");
     if (d->batch == 0) return;
     need(weight && momentum && grad, "NULL array");
     need_aligned(weight, 4, "weight");
@@ -828,10 +829,10 @@ ms_status ms_orthogonal_update(const ms_orth_desc* d, const ms_orth_rule* rule, 
     need_workspace(workspace, workspace_bytes, w.bytes);
     DeviceGuard dg(d->device);
     const hipStream_t st = (hipStream_t)d->stream;
-    OrthSrc src{grad, momentum, o.xm, o.xr, d->rows, d->cols, (float)rule->momentum_decay, rule->nesterov};
+    OrthSrc src{grad, momentum, o.xm, o.xr, d->rows, d->cols, decay, rule->nesterov};
     OrthGemm g{};
     g.out = weight, g.mat = d->rows * d->cols, g.row = d->cols, g.rows = d->rows, g.cols = d->cols;
-    g.keep = (float)(1.0 - rule->rate * rule->weight_decay), g.rate = (float)rule->rate;
+    g.keep = keep, g.rate = rate;
     if (d->dtype == MS_DTYPE_BF16) orth<__bf16, true>(d, o, src, w, g, st);
     else orth<float, true>(d, o, src, w, g, st);
   });
