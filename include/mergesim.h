@@ -569,7 +569,8 @@ ms_status ms_embed_grad(const ms_embed_desc* desc, const void* tokens, const voi
  * lengths (int32 [batch], clamped to [0, steps]; NULL = steps): what lies past
  * a row's length is not used, y there is 0 and the state stays.
  *   y0    [batch][dim] float32, or NULL for zeros
- *   y     [batch][steps][dim] (y_stride)
+ *   y     [batch][steps][dim] (y_stride: one of the two passes over all that the
+ *         other reaches)
  *   last  [batch][dim] float32, the state after the last step; may be NULL
  *   kept  float32, ms_gated_lowpass_kept() elements: states that the gradient
  *         starts from, in a layout of the library's own; NULL if no gradient

@@ -220,6 +220,16 @@ void stride_pair(const int64_t* s, int64_t steps, int64_t dim, int64_t& b, int64
   need(b >= 0 && t >= 0 && b < kMaxStride && t < kMaxStride, "strides must not be negative");
 }
 
+// Whether runs of `dim` values at i * si + j * sj, i < ni, j < nj, are apart: one
+// stride steps over a run, the other over all that the first one reaches.
+bool apart(int64_t si, int64_t ni, int64_t sj, int64_t nj, int64_t dim) {
+  if (ni == 0 || nj == 0) return true;
+  const auto within = [&](int64_t inner, int64_t n, int64_t outer, int64_t m) {
+    return (n == 1 || inner >= dim) && (m == 1 || (__int128)outer >= (__int128)(n - 1) * inner + dim);
+  };
+  return within(sj, nj, si, ni) || within(si, ni, sj, nj);
+}
+
 Gated check_gated(const ms_gated_lowpass_desc* d) {
   need(d != nullptr, "NULL descriptor");
   need(d->steps >= 0 && d->steps < ((int64_t)1 << 31), "steps must be in [0, 2^31)");
@@ -671,8 +681,7 @@ ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* d, const void* v, const 
     GatedArgs& a = p.a;
     if (a.batch == 0) return;
     const size_t es = size_of(d->dtype);
-    need(a.yt >= a.dim || a.steps <= 1, "the steps of y must not overlap");
-    need(a.yb >= a.dim || a.batch <= 1 || a.steps == 0, "the rows of y must not overlap");
+    need(apart(a.yb, a.batch, a.yt, a.steps, a.dim), "the rows or steps of y overlap");
     need(a.steps == 0 || (v && g && y), "NULL array");
     for (const void* q : {v, g, (const void*)y}) need_aligned(q, es, "v, g or y");
     for (const void* q : {(const void*)y0, (const void*)lengths, (const void*)last, (const void*)kept})
