@@ -168,8 +168,8 @@ def embed_grad(tokens, drows, vocab=None, scale=1.0, out=None, accumulate=False)
     grad_dtype = _gpu(out, (2,), "out [vocab, dim]")
     _like(out, drows, "out", (out.shape[0] if vocab is None else vocab, dim), out.dtype)
     tokens, rows = tokens.contiguous(), drows.reshape(-1, dim)
-    if rows.shape[0] > 1 and (rows.stride(0) < dim or (dim > 1 and rows.stride(1) != 1)):
-        rows = rows.contiguous()   # a broadcast gradient
+    if (rows.shape[0] > 1 and rows.stride(0) < dim) or (dim > 1 and rows.stride(1) != 1):
+        rows = rows.contiguous()   # a broadcast gradient, or columns apart
     d.vocab, d.dim = out.shape
     d.table_stride, d.row_stride = _row_stride(out, "out"), _row_stride(rows, "drows")
     d.scale, d.dtype, d.grad_dtype, d.accumulate = scale, dtype, grad_dtype, int(bool(accumulate))
