@@ -456,7 +456,7 @@ def stored_traffic(kernel, workload):
 
 # sources that no simulator kernel is made of
 OPERATOR_SOURCES = ("operators.hip", "operators_host.hpp", "kernels_embed.hpp", "kernels_gated.hpp", "kernels_orth.hpp",
-                    "kernels_orth_small.hpp")
+                    "kernels_orth_small.hpp", "operators_rules.hpp")
 
 
 def source_sha():

@@ -98,7 +98,6 @@ __global__ void __launch_bounds__(256) k_embed(const I* tokens, const T* table, 
 }
 
 // ------------------------------------------------------------------ sort
-constexpr int kSortBits = 10;   // of a digit, at most
 constexpr int kSortBlock = 64;  // tiles whose counts k_sort_prefix adds up together
 
 // A digit has BITS bits, 8 to 10, and counters come in rows of 256 PER = 2^BITS.

@@ -38,11 +38,11 @@
 #pragma once
 
 #include "kernels_embed.hpp"
+#include "operators_rules.hpp"
 
-// Steps of a wavefront, and between the states that the forward pass leaves for
-// the gradient, which computes the states between them again.
-constexpr int kKeep = 16;
-constexpr int kGatedWaves = 8;   // of a workgroup, at most
+using ms::kGatedWaves;
+using ms::kKeep;   // steps of a wavefront
+
 constexpr int kSpan = 8;         // chunks from one published state to the next
 
 // A lane takes V neighbouring channels of one batch row, a word of at most 4

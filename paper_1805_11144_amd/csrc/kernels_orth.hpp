@@ -29,13 +29,15 @@
 #pragma once
 
 #include "kernels_embed.hpp"
+#include "operators_rules.hpp"
+
+using ms::kOrthSlice;
 
 typedef _Float16 half_t;
 typedef half_t halfx8 __attribute__((ext_vector_type(8)));
 typedef half_t halfx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr int kOrthSlice = 32;    // values of k in a slice
 constexpr int kPair = 2;          // fp16 parts of a value: hi, lo
 constexpr int kOrthParts = 256;   // partial sums of a matrix's norm
 

@@ -14,6 +14,7 @@
 #include "kernels_orth.hpp"
 #include "kernels_orth_small.hpp"
 #include "operators_host.hpp"
+#include "operators_rules.hpp"
 
 using namespace ms;
 
@@ -121,19 +122,6 @@ Embed check_embed(const ms_embed_desc* d) {
   return e;
 }
 
-// Items of a thread in the sort: a tile holds 256 times as many pairs.  Up to
-// kSortAll tiles each adds up the counts of all, so tiles grow where they become
-// many.  Gradients in us with 4, 8 and 16 items: 40000 tokens 50, 56, 64; 100000
-// 59, 62, 73; 262144 101, 98, 104; 524288 138, 112, 111; 1048576 290, 200, 176.
-int sort_items(int64_t n) { return n <= (1 << 17) ? 4 : n <= (1 << 19) ? 8 : 16; }
-
-// With more tiles two launches a digit add up their counts: 131072 tokens in 128
-// tiles 62 us, every tile for itself 56; 1048576 in 256 tiles 175 and 187; 16777216
-// in 4096 tiles 1.9 ms and 11.
-constexpr int64_t kSortAll = 255;
-
-int64_t sort_tiles(int64_t n) { return (n + 256 * sort_items(n) - 1) / (256 * sort_items(n)); }
-
 struct EmbedWork {
   uint32_t *keys[2], *pos[2], *counts, *block, *start;
   float* part;
@@ -187,13 +175,11 @@ void sort_tiled(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int key_b
 template <class I>
 void sort_tokens(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int& in, hipStream_t st) {
   const int64_t n = d->n_tokens;
-  int key_bits = 1;
-  while (d->vocab >> key_bits) ++key_bits;   // keys are in [0, vocab]
+  int key_bits;
+  const int bits = sort_bits(d->vocab, &key_bits), small = sort_small_items(n);   // keys are in [0, vocab]
   in = 0;
-  // one launch of one workgroup in place of four or more: 1000 tokens 20 us in all, and 29; 4096 tokens 35, and 41
-  if (n <= 1024) return sort_small<I, 1>(d, tokens, w, key_bits, st);
-  if (n <= 4096) return sort_small<I, 4>(d, tokens, w, key_bits, st);
-  const int passes = (key_bits + kSortBits - 1) / kSortBits, bits = (key_bits + passes - 1) / passes;
+  if (small == 1) return sort_small<I, 1>(d, tokens, w, key_bits, st);
+  if (small == 4) return sort_small<I, 4>(d, tokens, w, key_bits, st);
   const auto with = [&](auto digit) {
     constexpr int BITS = decltype(digit)::value;
     switch (sort_items(n)) {
@@ -202,7 +188,7 @@ void sort_tokens(const ms_embed_desc* d, const I* tokens, EmbedWork& w, int& in,
       default: return sort_tiled<I, BITS, 16>(d, tokens, w, key_bits, in, st);
     }
   };
-  if (bits <= 8) with(std::integral_constant<int, 8>{});
+  if (bits == 8) with(std::integral_constant<int, 8>{});
   else if (bits == 9) with(std::integral_constant<int, 9>{});
   else with(std::integral_constant<int, 10>{});
 }
@@ -268,34 +254,6 @@ GatedWork gated_work(const Gated& g, void* ws) {
   return w;
 }
 
-// Threads of a workgroup, whether chunks run side by side, and how channels are
-// dealt to lanes.  One after the other, a chunk costs about 4 us (gradient 6)
-// while its data is on the way; side by side there is a launch that clears what
-// they publish, and their waits.  bf16, rows x steps x channels, forward and
-// gradient in us, one after the other and side by side:
-//   1 x 384 x 2048     15, 23    16, 20        16 x 512 x 2048     25, 39     30, 47
-//   1 x 512 x 2048     19, 30    17, 21        16 x 1024 x 2048    49, 75     48, 76
-//   1 x 1024 x 2048    35, 56    16, 20        128 x 1024 x 2048   319, 562   295, 502
-struct GatedShape {
-  unsigned threads;
-  bool link, span;
-};
-
-GatedShape gated_shape(Gated& g) {
-  GatedArgs& a = g.a;
-  int waves = 1;
-  while (waves < kGatedWaves && waves < g.keeps) waves *= 2;
-  a.nchunk = (int32_t)((g.keeps + waves - 1) / waves);
-  a.per_row = (int32_t)((a.nv + 63) / 64);
-  // lanes over the rows where over a fifth would idle: forward and gradient of 256 x 1000 x 16 float32 23 and 32 us, a
-  // row each 36 and 44; of 64 x 1000 x 96 27 and 36, 30 and 42; of 64 x 1000 x 100, a fifth, 38 and 61, 37 and 57
-  const bool span = a.per_row * 64 > a.nv + a.nv / 4;
-  a.groups = (int32_t)(span ? (a.batch * a.nv + 63) / 64 : a.batch * a.per_row);
-  const bool link = (a.nchunk > 4 || (a.nchunk > 2 && a.groups <= 64)) &&
-                    (int64_t)a.nchunk * a.groups < ((int64_t)1 << 22);   // tickets in the grid's 32 bits of threads
-  return {(unsigned)waves * 64, link, span};
-}
-
 // Calls f(args, link, span, grid) with the shape's choices as compile-time
 // values: once, or for as many groups at a time as a grid holds (its threads fit
 // 31 bits).
@@ -321,52 +279,9 @@ void gated_clear(GatedArgs& a, const GatedWork& w, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------- orth
-constexpr int kCUs = 256;
-
-// Tiles that a product can take.
-enum OrthTile { kTile64, kTile128, kTile256 };
-
-// A launch's tiles: whole ones, and those computed in parts.  A few tiles more
-// than the CUs hold in whole rounds would take a round for themselves: up to
-// half a round of them is spread over the CUs in quarters.
-struct OrthTiles {
-  int64_t per, whole, over;
-};
-
-OrthTiles orth_tiles(OrthTile kind, bool sym, int64_t batch, int64_t rows, int64_t cols) {
-  const int64_t side = 64 << kind, r = (rows + side - 1) / side, c = (cols + side - 1) / side;
-  const int64_t per = sym ? r * (r + 1) / 2 : r * c, tiles = batch * per;
-  const int64_t over = kind != kTile64 && tiles > kCUs && tiles % kCUs <= kCUs / 2 ? tiles % kCUs : 0;
-  return {per, tiles - over, over};
-}
-
-// What a product takes with a kind of tile, in us for 4096 values of k: rounds
-// of the CUs times what one took on this card.
-double orth_cost(OrthTile kind, bool sym, int64_t batch, int64_t rows, int64_t cols) {
-  static const double round[3] = {42, 112, 333};
-  const OrthTiles t = orth_tiles(kind, sym, batch, rows, cols);
-  return ((double)((t.whole + kCUs - 1) / kCUs) + (t.over ? 0.3 : 0.0)) * round[kind];
-}
-
-// The cheapest tile whose sides divide `pad`: large ones read less, small ones
-// are more, for the CUs to share.
-OrthTile orth_choose(int64_t pad, bool sym, int64_t batch, int64_t rows, int64_t cols, double* cost) {
-  OrthTile best = kTile64;
-  double least = orth_cost(best, sym, batch, rows, cols);
-  const auto offer = [&](OrthTile k) {
-    const double c = orth_cost(k, sym, batch, rows, cols);
-    if (c < least) best = k, least = c;
-  };
-  if (pad >= 128) offer(kTile128);
-  if (pad >= 256) offer(kTile256);
-  if (cost) *cost = least;
-  return best;
-}
-
 struct Orth {
-  int64_t n, m, np, mp;
-  int64_t pad;            // to whole tiles of this side
-  int split;              // workgroups that share the sum over m of a tile of X X'
+  int64_t n, m;
+  OrthShape shape;        // tiled
   double sx, sa, sq;      // scales of X, A and Q
   int64_t xm, xr, om, orow;
   int small;              // row tiles of 16 where a matrix fits into one workgroup's LDS, else 0
@@ -393,24 +308,12 @@ Orth check_orth(const ms_orth_desc* d) {
   pair(d->x_stride, o.xm, o.xr);
   pair(d->out_stride, o.om, o.orow);
   o.n = std::min(d->rows, d->cols), o.m = std::max(d->rows, d->cols);
-  double least = INFINITY;
-  for (int64_t pad : {64, 128, 256}) {   // larger tiles pad more
-    const int64_t n = up(o.n, pad), m = up(o.m, pad);
-    double square, next;
-    orth_choose(pad, true, d->batch, n, n, &square);
-    orth_choose(pad, false, d->batch, n, m, &next);
-    const double cost = square * (m + n) + next * n;
-    if (cost < least) least = cost, o.pad = pad, o.np = n, o.mp = m;
-  }
-  // Few tiles and a long sum (16 x 9000: one tile, 282 slices): shared by so many workgroups that they fill half the
-  // CUs, none with fewer than 16 slices, and added up by one more launch.
-  const int64_t tiles = orth_tiles(kTile64, true, d->batch, o.np, o.np).per * std::max<int64_t>(d->batch, 1);
-  o.split = (int)std::max<int64_t>(1, std::min(kCUs / 2 / tiles, o.mp / kOrthSlice / 16));
+  o.shape = orth_shape(d->batch, o.n, o.m);
   o.stride = up(o.m, 64) + 4;
   o.small = (int)up(o.n, 16) / 16;
   if (o.small > 4 || orth_small_floats(o.small, o.stride) * 4 > kOrthLds) o.small = 0;
   // workgroups of up to 512 threads
-  const int64_t groups = o.small ? 1 : std::max<int64_t>(kOrthParts, (o.np / 64) * (o.mp / 64));
+  const int64_t groups = o.small ? 1 : std::max<int64_t>(kOrthParts, (o.shape.np / 64) * (o.shape.mp / 64));
   need(d->batch <= kMaxBlocks / 2 / groups, "too many matrices of this size");
   // How large an iterate's singular values and the polynomial can get: the
   // first are at most 1, and f(s) = s (c0 + c1 s^2 + c2 s^4) takes its extremes
@@ -454,14 +357,15 @@ OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
   Carve c{(char*)ws};
   OrthWork w{};
   if (o.small) return w;
-  const int64_t big = d->batch * kPair * o.np * o.mp, small = d->batch * kPair * o.np * o.np;
+  [[maybe_unused]] const auto [pad, np, mp, split] = o.shape;
+  const int64_t big = d->batch * kPair * np * mp, small = d->batch * kPair * np * np;
   w.parts = c.take<double>(d->batch * kOrthParts);
   w.x = c.take<half_t>(big);
   w.t[0] = c.take<half_t>(big);
   w.t[1] = c.take<half_t>(big);
   w.a = c.take<half_t>(small);
   w.q = c.take<half_t>(small);
-  w.sums = c.take<float>(o.split > 1 ? o.split * d->batch * o.np * o.np : 0);
+  w.sums = c.take<float>(split > 1 ? split * d->batch * np * np : 0);
   w.bytes = c.used;
   return w;
 }
@@ -489,7 +393,8 @@ void orth_gemm(const OrthGemm& g, int64_t pad, int64_t batch, hipStream_t st) {
 // T: type of x (or the gradient); UPDATE: with momentum, into a weight.
 template <class T, bool UPDATE>
 void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork& w, OrthGemm out, hipStream_t st) {
-  const int64_t blocks = d->batch * (o.np / 64) * (o.mp / 64);
+  const auto [pad, np, mp, split] = o.shape;
+  const int64_t blocks = d->batch * (np / 64) * (mp / 64);
   const dim3 norms((unsigned)(d->batch * kOrthParts));
   const auto norm = [&](auto width) {
     hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_norm<T, UPDATE, decltype(width)::value>), norms, dim3(256), 0, st, src, w.parts);
@@ -501,35 +406,35 @@ void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork
     norm(std::integral_constant<int, 4>{});
   else norm(std::integral_constant<int, 1>{});
   hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, kOrthSlice>), dim3((unsigned)blocks), dim3(256), 0, st, src,
-                     (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], (int32_t)o.np, (int32_t)o.mp);
+                     (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], (int32_t)np, (int32_t)mp);
   using R = std::conditional_t<UPDATE, float, T>;
   for (int k = 0; k < d->steps; ++k) {
     OrthGemm g{};
     g.batch = out.batch = (uint32_t)d->batch, g.parts = out.parts = 1;
     g.slices = out.slices = INT32_MAX / 2;
-    g.l = g.r = w.x, g.M = g.N = (int32_t)o.np, g.K = (int32_t)o.mp, g.c = w.a;
+    g.l = g.r = w.x, g.M = g.N = (int32_t)np, g.K = (int32_t)mp, g.c = w.a;
     g.f = (float)(o.sa / (o.sx * o.sx));
-    if (o.split > 1) {
-      g.sums = w.sums, g.parts = o.split, g.slices = (int32_t)((o.mp / kOrthSlice + o.split - 1) / o.split);
-      orth_launch<kEndPart, R, 64, 2, 3, 2>(g, orth_tiles(kTile64, true, d->batch * o.split, o.np, o.np), st);
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_join<kOrthSlice>), dim3((unsigned)((d->batch * o.np * o.np + 255) / 256)),
-                         dim3(256), 0, st, g);
+    if (split > 1) {
+      g.sums = w.sums, g.parts = split, g.slices = (int32_t)((mp / kOrthSlice + split - 1) / split);
+      orth_launch<kEndPart, R, 64, 2, 3, 2>(g, orth_tiles(kTile64, true, d->batch * split, np, np), st);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_join<kOrthSlice>), dim3((unsigned)((d->batch * np * np + 255) / 256)), dim3(256),
+                         0, st, g);
     } else {
-      orth_gemm<kEndGram, R>(g, o.pad, d->batch, st);
+      orth_gemm<kEndGram, R>(g, pad, d->batch, st);
     }
     g.parts = 1, g.slices = INT32_MAX / 2;
-    g.l = g.r = w.a, g.K = (int32_t)o.np, g.c = w.q, g.a = w.a;
+    g.l = g.r = w.a, g.K = (int32_t)np, g.c = w.q, g.a = w.a;
     g.f = (float)(d->coef[2] * o.sq / (o.sa * o.sa));
     g.c0 = (float)(d->coef[0] * o.sq), g.c1 = (float)(d->coef[1] * o.sq / o.sa);
-    orth_gemm<kEndPoly, R>(g, o.pad, d->batch, st);
+    orth_gemm<kEndPoly, R>(g, pad, d->batch, st);
     OrthGemm x = out;
-    x.l = w.q, x.r = w.t[k % 2], x.M = (int32_t)o.np, x.N = (int32_t)o.mp, x.K = (int32_t)o.np;
+    x.l = w.q, x.r = w.t[k % 2], x.M = (int32_t)np, x.N = (int32_t)mp, x.K = (int32_t)np;
     if (k + 1 < d->steps) {
       x.c = w.x, x.ct = w.t[(k + 1) % 2], x.f = (float)(1.0 / o.sq);
-      orth_gemm<kEndNext, R>(x, o.pad, d->batch, st);
+      orth_gemm<kEndNext, R>(x, pad, d->batch, st);
     } else {
       x.f = (float)(1.0 / (o.sq * o.sx));
-      orth_gemm<UPDATE ? kEndUpdate : kEndOut, R>(x, o.pad, d->batch, st);
+      orth_gemm<UPDATE ? kEndUpdate : kEndOut, R>(x, pad, d->batch, st);
     }
   }
   HIPCHECK(hipGetLastError());
@@ -701,7 +606,8 @@ ms_status ms_gated_lowpass(const ms_gated_lowpass_desc* d, const void* v, const 
     Wide wide = Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es).at(g, es).at(y, es);
     const int64_t w = std::min<int64_t>(4 / (int64_t)es, wide.at(kept, 4).v);   // a word of 4 bytes to a lane
     a.nv = a.dim / w;
-    const GatedShape shape = gated_shape(p);
+    const GatedShape shape = gated_shape(a.batch, p.keeps, a.nv);
+    a.nchunk = shape.nchunk, a.groups = shape.groups, a.per_row = shape.per_row;
     if (shape.link) gated_clear(a, work, st);
     with_type<2, 1>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
@@ -742,7 +648,8 @@ ms_status ms_gated_lowpass_grad(const ms_gated_lowpass_desc* d, const void* v, c
     const int64_t w = std::min<int64_t>(4 / (int64_t)es, Wide(es).of(a.dim).of(a.vb).of(a.vt).of(a.gb).of(a.gt).of(a.yb).of(a.yt).at(v, es)
                                                .at(g, es).at(dy, es).at(dv, es).at(dg, es).v);
     a.nv = a.dim / w;
-    const GatedShape shape = gated_shape(p);
+    const GatedShape shape = gated_shape(a.batch, p.keeps, a.nv);
+    a.nchunk = shape.nchunk, a.groups = shape.groups, a.per_row = shape.per_row;
     if (shape.link) gated_clear(a, work, st);
     with_type<2, 1>(d->dtype, w, [&](auto zero, auto width) {
       using T = decltype(zero);
