@@ -625,10 +625,9 @@ ms_status ms_gated_lowpass_step(const ms_gated_step_desc* desc, const void* v, c
  * the polynomial, exceed 1000 in size.  Small matrices are computed in 32 bits
  * throughout.  The products of the others run on 16-bit matrix instructions with
  * 32-bit sums, matrices as the sum of two 16-bit parts: 22 bits, for results of
- * either type, and none smaller than 2^-24 of fp16's 1 after a scaling that puts
- * the largest value that c0..c2 allow at 8192 to 32768.  So values below about
- * 2^-39 of that largest one are 0, as in a matrix whose norm is many orders of
- * magnitude below eps.
+ * either type, and steps no finer than 2^-38 of the largest singular value that
+ * c0..c2 allow (of 1, if they allow none above).  A matrix whose norm is five
+ * orders of magnitude below eps loses bits to that, and is 0 at ten.
  *
  * ms_orthogonal_update trains a float32 weight with it:
  *     momentum <- momentum_decay * momentum + grad
