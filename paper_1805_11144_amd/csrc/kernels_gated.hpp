@@ -27,14 +27,15 @@
 // its span's beginning and the maps in between, a wavefront for each.  The order
 // of the operations is fixed, so the result does not depend on timing.
 //
-// Measured at 4 x 16384 x 2048 bf16 (0.81 GB): 445 us in two passes (maps, then
+// Measured at 4 x 16384 x 2048 bf16 (0.81 GB): 165 to 180 us, 4.9 TB/s at best.
+// Step by step, before the looks at gates: 445 us in two passes (maps, then
 // steps: v and g are read twice), 190 us in one with the first wavefront waiting
-// for all maps, 152 to 163 us with a wavefront for each (5.3 TB/s at best), 149
-// us without any waiting (a copy that is not correct, to know the cost), 146 us
-// without the exponentials too.  Chunks of 64 steps take 235 us, of 256 steps
-// 193; one channel per lane 229.  A third workgroup on each CU (gates kept as
-// one number) does not help: 171.  The gradient of 8 x 4096 x 2048 bf16 (0.71
-// GB with the kept states): 142 us, 5.0 TB/s.
+// for all maps, 152 to 163 us with a wavefront for each, 149 us without any
+// waiting (a copy that is not correct, to know the cost), 146 us without the
+// exponentials too.  Chunks of 64 steps took 235 us, of 256 steps 193; one channel
+// per lane 229.  A third workgroup on each CU (gates kept as one number) did not
+// help: 171.  The gradient of 8 x 4096 x 2048 bf16 (0.71 GB with the kept
+// states): 145 to 150 us, 4.9 TB/s.
 #pragma once
 
 #include "kernels_embed.hpp"
@@ -65,7 +66,9 @@ __device__ __forceinline__ int32_t row_length(const GatedArgs& p, int64_t b) {
   return min(max(p.lengths[b], 0), (int32_t)p.steps);
 }
 
-// a and 1 - a from the logit: both to full precision, also where one is small.
+// a and 1 - a from the logit, each to a few units of its last bit and |g| / ln 2
+// half units of the exponential's argument, also where one is small (down to
+// about 1e-38; what is smaller may be 0).
 __device__ __forceinline__ void gate(float g, float& a, float& rest) {
   const float e = __expf(-fabsf(g));
   const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;

@@ -20,12 +20,14 @@
 // A and Q are symmetric: blocks below the diagonal are the others' mirror
 // images and are not computed.
 //
-// What bounds it: large matrices the matrix cores (4096 x 4096: Q X 333 us, 1.24
-// PFLOP/s of 16-bit products, where a large library product in bf16 reaches
-// 1.2), small ones a launch's latency (1024 x 784: 12 to 15 us for each of 15
-// products that take 2 at full rate).  Step by step at 4096 x 4096: 5.0 ms with
-// tiles straight from memory to LDS; 4.4 with slices of k behind each other and
-// 256 x 256 tiles for Q X; 4.2 with results in 16-byte words.
+// What bounds it: large matrices the matrix cores (4096 x 4096: Q X 335 to 350
+// us, 1.2 PFLOP/s of 16-bit products, as a large library product in bf16, the
+// cores busy 60% of the cycles; X X' and A A 250, half the blocks at 0.85: 528
+// tiles on 256 CUs), small ones a launch's latency (1024 x 784: 12 to 15 us for
+// each of 15 products that take 2 at full rate, the matrix cores busy 2200 to 4100
+// of some 25000 cycles).  Step by step at 4096 x 4096: 5.0 ms with tiles straight
+// from memory to LDS; 4.4 with slices of k behind each other and 256 x 256 tiles
+// for Q X; 4.2 with results in 16-byte words.
 #pragma once
 
 #include "kernels_embed.hpp"

@@ -13,8 +13,11 @@
 //               are replaced in place
 // Only the launch, the read and the write touch the rest of the chip.  Bound by
 // latency: barriers, LDS and dependent products.  200 matrices of 500 x 16 take
-// 19 us, and 238 on the tiled kernels (17 launches); one of 64 x 64 28 and 74,
-// one of 64 x 400 94 and 89, 64 of 64 x 300 76 and 120.
+// 19 us, and 238 on the tiled kernels (17 launches).  Taken wherever a matrix
+// fits, since one workgroup is the faster even for a single one: 64 x 64 29 us and
+// 72 tiled, 32 x 400 34 and 90, 48 x 600 83 and 97, 16 x 2000 50 and 115; 64 of 64 x
+// 300 76 and 120.  At the largest that fit, 64 x 400, up to eight matrices take
+// 94 and 90: even, so the number of matrices plays no part.
 #pragma once
 
 #include "kernels_orth.hpp"

@@ -45,13 +45,14 @@ constexpr int kKeep = 16;
 constexpr int kGatedWaves = 8;   // of a workgroup, at most
 
 // Threads of a workgroup, whether chunks run side by side, and how channels are
-// dealt to lanes.  One after the other, a chunk costs about 4 us (gradient 6)
+// dealt to lanes.  One after the other, a chunk costs about 5 us (gradient 9)
 // while its data is on the way; side by side there is a launch that clears what
 // they publish, and their waits.  bf16, rows x steps x channels, forward and
 // gradient in us, one after the other and side by side:
-//   1 x 384 x 2048     15, 23    16, 20        16 x 512 x 2048     25, 39     30, 47
-//   1 x 512 x 2048     19, 30    17, 21        16 x 1024 x 2048    49, 75     48, 76
-//   1 x 1024 x 2048    35, 56    16, 20        128 x 1024 x 2048   319, 562   295, 502
+//   1 x 384 x 2048     19, 29    16, 21        16 x 512 x 2048     27, 44     31, 47
+//   1 x 512 x 2048     24, 37    17, 21        16 x 1024 x 2048    53, 87     51, 80
+//   1 x 1024 x 2048    43, 70    17, 21        128 x 1024 x 2048   321, 570   319, 518
+// Five chunks are about even: 16 x 640 x 2048 34, 54 and 37, 56.
 struct GatedShape {
   int32_t threads;
   int32_t nchunk;    // chunks of threads / 64 * kKeep steps
@@ -68,8 +69,8 @@ inline GatedShape gated_shape(int64_t batch, int64_t keeps, int64_t nv) {
   s.threads = 64 * waves;
   s.nchunk = (int32_t)((keeps + waves - 1) / waves);
   s.per_row = (int32_t)((nv + 63) / 64);
-  // lanes over the rows where over a fifth would idle: forward and gradient of 256 x 1000 x 16 float32 23 and 32 us, a
-  // row each 36 and 44; of 64 x 1000 x 96 27 and 36, 30 and 42; of 64 x 1000 x 100, a fifth, 38 and 61, 37 and 57
+  // lanes over the rows where over a fifth would idle: forward and gradient of 256 x 1000 x 16 float32 24 and 31 us, a
+  // row each 37 and 49; of 64 x 1000 x 96 27 and 38, 30 and 42; of 64 x 1000 x 100, a fifth, 38 and 61, 37 and 58
   s.span = s.per_row * 64 > nv + nv / 4;
   s.groups = (int32_t)(s.span ? (batch * nv + 63) / 64 : batch * s.per_row);
   s.link = (s.nchunk > 4 || (s.nchunk > 2 && s.groups <= 64)) &&

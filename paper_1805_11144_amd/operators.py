@@ -17,7 +17,9 @@ from . import mergesim as _ms
 from .mergesim import (DTYPE_BF16, DTYPE_F32, IDS_I32, IDS_I64, EmbedDesc, GatedLowpassDesc, GatedStepDesc, OrthDesc,
                        OrthRule, _check)
 
-NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)   # raises small singular values fast; leaves them within 0.3 of one
+# Raises small singular values fast and leaves them within 0.3 of one: the coefficients published by K. Jordan et al.,
+# "Muon: An optimizer for hidden layers in neural networks" (2024).
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
 
 _torch = _lib = _stream = None
 _DTYPES, _IDS = {}, {}
