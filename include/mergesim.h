@@ -624,10 +624,8 @@ ms_status ms_gated_lowpass_step(const ms_gated_step_desc* desc, const void* v, c
  * vectors.  MS_E_INVALID where c0..c2 let a singular value of an iterate, or
  * the polynomial, exceed 1000 in size.  Small matrices are computed in 32 bits
  * throughout.  The products of the others run on 16-bit matrix instructions with
- * 32-bit sums, matrices as the sum of two 16-bit parts: 22 bits, for results of
- * either type, and steps no finer than 2^-38 of the largest singular value that
- * c0..c2 allow (of 1, if they allow none above).  A matrix whose norm is five
- * orders of magnitude below eps loses bits to that, and is 0 at ten.
+ * 32-bit sums, matrices as the sum of two 16-bit parts, 22 bits, for results of
+ * either type.
  *
  * ms_orthogonal_update trains a float32 weight with it:
  *     momentum <- momentum_decay * momentum + grad

@@ -11,7 +11,10 @@
 // singular values grow with them, by 3.4445^5 = 485 in all, and with one part
 // (11 bits) a matrix of 16 strong directions came out 4e-2 off, 25 times its own
 // rounding.  Matrices are scaled by powers of two that their bounds allow, so
-// the parts stay clear of fp16's ends.
+// the parts stay clear of fp16's ends.  A matrix whose norm is below eps, or that
+// the coefficients shrink, is also lifted: its norm is at most 2^-E from the
+// start, and at most 2^(g - E) after steps that let it grow by 2^g, so it is held
+// 2^max(0, E - g) times as large and stays below one.
 //
 // Layout: n = min(rows, cols) <= m = the other; X [n][m] and its transpose
 // [m][n] in fp16 parts, A and Q = c0 I + c1 A + c2 A A as [n][n], every side
@@ -120,11 +123,11 @@ __device__ __forceinline__ int64_t orth_at(int64_t rows, int64_t row, int64_t k)
   return (k / KS * rows + row) * KS + k % KS;
 }
 
-// The first iterate, scale X / (|X| + eps), and its transpose.  grid: batch x
-// (mp / 64) x (np / 64) tiles of 64 x 64.
+// The first iterate, scale X / (|X| + eps) lifted by 2^E, and its transpose; E to
+// lift[].  grid: batch x (mp / 64) x (np / 64) tiles of 64 x 64.
 template <class T, bool UPDATE, int KS>
 __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* parts, double eps, double scale, half_t* X,
-                                                    half_t* XT, int32_t np, int32_t mp) {
+                                                    half_t* XT, int32_t* lift, int32_t np, int32_t mp) {
   __shared__ float tile[64][65];
   __shared__ double inv_s;
   const int tid = threadIdx.x;
@@ -137,7 +140,12 @@ __global__ void __launch_bounds__(256) k_orth_first(OrthSrc s, const double* par
     for (int q = 0; q < kOrthParts / 64; ++q) p += parts[mat * kOrthParts + q * 64 + tid];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) p += __shfl_down(p, o, 64);
-    if (tid == 0) inv_s = scale / (sqrt(p) + eps);
+    if (tid == 0) {
+      const double norm = sqrt(p), ratio = (norm + eps) / norm;   // not finite for zeros
+      const int e = ratio < 1e300 ? ilogb(ratio) : 0;
+      inv_s = ldexp(scale / (norm + eps), e);
+      if (u == 0) lift[mat] = e;
+    }
   }
   __syncthreads();
   const double inv = inv_s;
@@ -192,6 +200,8 @@ struct OrthGemm {
   const half_t* a;            // A (kEndPoly)
   float f;                    // sums to C's scale
   float c0, c1;               // kEndPoly, in C's scale (c1 times A's stored value)
+  const int32_t* lift;        // E of each matrix
+  int32_t grown, grows;       // g before and after this step
   // kEndPart: the sum over slices [part * slices, ..) alone, unscaled, to sums[part][matrix][M][M]
   float* sums;
   int32_t slices, parts;      // slices of a part (all of them, and 1, for other ends)
@@ -264,6 +274,14 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
     for (int j = 0; j < BJ; ++j) acc[i][j] = floatx16{};
 #pragma unroll
   for (int n = 0; n < NA - 1; ++n) more[n] = floatx16{};
+  // what the iterates are lifted by, and what that makes of the sums
+  float f = g.f, c1 = g.c1;
+  int32_t shift = 0;
+  if constexpr (END != kEndGram && END != kEndPart) {
+    const int32_t now = max(0, g.lift[mat] - g.grown);
+    if constexpr (END == kEndPoly) f = ldexpf(f, -4 * now), c1 = ldexpf(c1, -2 * now);
+    else shift = END == kEndNext ? max(0, g.lift[mat] - g.grows) - now : -now;
+  }
   // A's values for the polynomial, on their way while the product is made
   [[maybe_unused]] half_t early[kPair][16];
   constexpr bool EARLY = END == kEndPoly && BI * BJ == 1;
@@ -375,7 +393,8 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int64_t row = row0 + q;
-          float v = g.f * acc[i][j][4 * q4 + q];
+          float v = f * acc[i][j][4 * q4 + q];
+          if (END == kEndNext || END == kEndOut || END == kEndUpdate) v = ldexpf(v, shift);
           if constexpr (END == kEndPart) {
             g.sums[((part * (int64_t)g.batch + mat) * g.M + row) * g.M + col] = acc[i][j][4 * q4 + q];
           } else if constexpr (END == kEndOut || END == kEndUpdate) {
@@ -394,7 +413,7 @@ __device__ __forceinline__ void orth_tile(const OrthGemm& g, half_t* lds, int64_
               } else {
                 av = (float)A[orth_at<KS>(g.M, row, col)] + (float)A[cplane + orth_at<KS>(g.M, row, col)];
               }
-              v += g.c1 * av + (row == col ? g.c0 : 0.0f);
+              v += c1 * av + (row == col ? g.c0 : 0.0f);
             }
             half_t h, l;
             split(v, h, l);

@@ -283,6 +283,7 @@ struct Orth {
   int64_t n, m;
   OrthShape shape;        // tiled
   double sx, sa, sq;      // scales of X, A and Q
+  int grown[101];         // log2 of what the steps before a step, at most, multiply an iterate's norm by
   int64_t xm, xr, om, orow;
   int small;              // row tiles of 16 where a matrix fits into one workgroup's LDS, else 0
   int64_t stride;         // of its rows there
@@ -321,8 +322,9 @@ Orth check_orth(const ms_orth_desc* d) {
   double top = 1.0, poly = 0.0;
   const double *c = d->coef;
   need(std::isfinite(c[0]) && std::isfinite(c[1]) && std::isfinite(c[2]), "coefficients must be finite");
-  double bound = 1.0;
+  double bound = 1.0, grown = 0.0;
   for (int k = 0; k < d->steps; ++k) {
+    o.grown[k] = (int)std::ceil(grown);
     const auto q = [&](double t) { return std::fabs(c[0] + c[1] * t + c[2] * t * t); };   // t = s^2
     double most_f = top * q(top * top), most_q = std::max(q(0.0), q(top * top));
     const auto at = [&](double t) {
@@ -336,18 +338,21 @@ Orth check_orth(const ms_orth_desc* d) {
       at(-c[0] / (3.0 * c[1]));
     }
     poly = std::max(poly, most_q);
+    grown += std::log2(std::max(most_q, 1e-30));
     top = most_f;
     bound = std::max(bound, top);
     need(bound <= 1000.0 && poly <= 1000.0, "the coefficients let the iterates grow past 1000");
   }
+  o.grown[d->steps] = (int)std::ceil(grown);
   // an entry is at most the largest singular value; a factor of two to spare
   const auto scale = [](double b) { return std::ldexp(1.0, (int)std::floor(std::log2(32768.0 / b))); };
-  o.sx = scale(bound), o.sa = scale(bound * bound), o.sq = scale(std::max(poly, 1e-3));
+  o.sx = scale(bound), o.sa = scale(bound * bound), o.sq = scale(std::max(poly, 1e-20));
   return o;
 }
 
 struct OrthWork {
   double* parts;
+  int32_t* lift;
   half_t *x, *t[2], *a, *q;
   float* sums;
   int64_t bytes;
@@ -360,6 +365,7 @@ OrthWork orth_work(const ms_orth_desc* d, const Orth& o, void* ws) {
   [[maybe_unused]] const auto [pad, np, mp, split] = o.shape;
   const int64_t big = d->batch * kPair * np * mp, small = d->batch * kPair * np * np;
   w.parts = c.take<double>(d->batch * kOrthParts);
+  w.lift = c.take<int32_t>(d->batch);
   w.x = c.take<half_t>(big);
   w.t[0] = c.take<half_t>(big);
   w.t[1] = c.take<half_t>(big);
@@ -406,11 +412,13 @@ void orth_run(const ms_orth_desc* d, const Orth& o, const OrthSrc& src, OrthWork
     norm(std::integral_constant<int, 4>{});
   else norm(std::integral_constant<int, 1>{});
   hipLaunchKernelGGL(HIP_KERNEL_NAME(k_orth_first<T, UPDATE, kOrthSlice>), dim3((unsigned)blocks), dim3(256), 0, st, src,
-                     (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], (int32_t)np, (int32_t)mp);
+                     (const double*)w.parts, d->eps, o.sx, w.x, w.t[0], w.lift, (int32_t)np, (int32_t)mp);
   using R = std::conditional_t<UPDATE, float, T>;
   for (int k = 0; k < d->steps; ++k) {
     OrthGemm g{};
     g.batch = out.batch = (uint32_t)d->batch, g.parts = out.parts = 1;
+    g.lift = out.lift = w.lift;
+    g.grown = out.grown = o.grown[k], g.grows = out.grows = o.grown[k + 1];
     g.slices = out.slices = INT32_MAX / 2;
     g.l = g.r = w.x, g.M = g.N = (int32_t)np, g.K = (int32_t)mp, g.c = w.a;
     g.f = (float)(o.sa / (o.sx * o.sx));
