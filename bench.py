@@ -456,7 +456,8 @@ def stored_traffic(kernel, workload):
 
 # sources that no simulator kernel is made of
 OPERATOR_SOURCES = ("operators.hip", "operators_host.hpp", "kernels_embed.hpp", "kernels_gated.hpp", "kernels_orth.hpp",
-                    "kernels_orth_small.hpp", "operators_rules.hpp")
+                    "kernels_orth_small.hpp", "operators_rules.hpp", "memory.hip", "kernels_delta.hpp",
+                    "kernels_delta_grad.hpp", "kernels_norm.hpp", "kernels_words.hpp")
 
 
 def source_sha():

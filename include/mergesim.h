@@ -510,8 +510,8 @@ ms_status ms_sim_set_train_param(ms_sim* sim, int32_t which, int32_t id, int32_t
 
 /* Operators for models that read and learn from tokens, called on arrays of
  * the caller's own (none is a part of the paper's method): a table of token
- * vectors, a lowpass synapse whose time constant the input sets, and
- * orthogonalised updates of weight matrices.  Their outputs are laid out as
+ * vectors, a lowpass synapse whose time constant the input sets, orthogonalised
+ * updates of weight matrices, and a memory by key that learns by the delta rule.  Their outputs are laid out as
  * feeds ([batch][steps][dim]).
  *
  * Every pointer but the descriptors is device memory on `device`; the calls
@@ -655,6 +655,74 @@ ms_status ms_orthogonalise(const ms_orth_desc* desc, const void* x, void* out, v
                            int64_t workspace_bytes);
 ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rule, float* weight,
                                float* momentum, const void* grad, void* workspace, int64_t workspace_bytes);
+
+/* The gated delta rule: a memory by key.  Each head holds a matrix S [keys]
+ * [values]; at every step it forgets by a = exp(decay), reads at the key, learns
+ * the error with the step's rate, and is read at the query:
+ *     P = a S;   z = v - P'k;   S <- P + rate k z';   y = scale S'q
+ * from s0 (zeros).  decay <= 0 is the logarithm of what is kept; -inf (any below
+ * -200) forgets everything: a sequence starts.  Where a row's first step forgets, s0
+ * may hold anything.  Else an infinity or NaN may reach every result of its row and
+ * head.  Heads share key heads: head h reads q and k of key head h * key_heads /
+ * heads.  lengths: as for the gated lowpass; y is 0 past a row's length and what lies
+ * there is not read.
+ *   q, k        [batch][steps][key_heads][keys], dtype
+ *   v, y        [batch][steps][heads][values], dtype
+ *   decay, rate [batch][steps][heads] float32
+ *   s0, last    [batch][heads][keys][values] float32, packed; may be NULL
+ *   kept        float32, ms_gated_delta_kept() elements, in a layout of the library's
+ *               own; NULL if no gradient is wanted
+ * Strides: between batch rows, steps, heads; 0, 0, 0 = packed.
+ * Everything is computed in 32 bits: products run on 16-bit matrix instructions with
+ * values as sums of three bf16 parts (24 bits); what passes into a bf16 y only, in two.
+ * Values beyond bf16's largest number (3.39e38) count as infinite.
+ *
+ * The gradient, from dL/dy and dL/dlast (NULL for zeros): dq, dk (sums over the heads
+ * that share a key head) and dv like q, k and v, packed; ddecay, drate float32, packed;
+ * ds0 float32, may be NULL; 0 past a row's length.  q, k, v, decay, rate, kept and
+ * lengths are those of the forward call. */
+typedef struct {
+  int64_t batch, steps;              /* >= 0 and < 2^31 */
+  int64_t heads, key_heads;          /* heads in [1, 65536], a multiple of key_heads */
+  int64_t keys, values;              /* keys in [1, 128], values in [1, 65536] */
+  int64_t q_stride[3], k_stride[3], v_stride[3];
+  int64_t y_stride[3];               /* of y, or of dy in the gradient */
+  int64_t decay_stride[3], rate_stride[3];
+  double scale;
+  int32_t dtype;                     /* MS_DTYPE_*: of q, k, v, y and their gradients */
+  int32_t device;
+  void* stream;
+} ms_gated_delta_desc;
+
+ms_status ms_gated_delta_kept(const ms_gated_delta_desc* desc, int64_t* elements_out);
+/* grad != 0: for ms_gated_delta_grad, else for ms_gated_delta. */
+ms_status ms_gated_delta_workspace(const ms_gated_delta_desc* desc, int32_t grad, int64_t* bytes_out);
+ms_status ms_gated_delta(const ms_gated_delta_desc* desc, const void* q, const void* k, const void* v,
+                         const float* decay, const float* rate, const float* s0, const int32_t* lengths,
+                         void* y, float* last, float* kept, void* workspace, int64_t workspace_bytes);
+ms_status ms_gated_delta_grad(const ms_gated_delta_desc* desc, const void* q, const void* k, const void* v,
+                              const float* decay, const float* rate, const float* kept,
+                              const int32_t* lengths, const void* dy, const float* dlast, void* dq, void* dk,
+                              void* dv, float* ddecay, float* drate, float* ds0, void* workspace,
+                              int64_t workspace_bytes);
+
+/* One step of the gated delta rule for sequences that are being served: row i
+ * advances the matrices in slot slots[i] of state [slots][heads][keys][values]
+ * (float32, updated in place; state_stride between slots).  Slots as in
+ * ms_gated_lowpass_step.  Strides: between rows, heads; 0, 0 = packed. */
+typedef struct {
+  int64_t rows, n_slots, heads, key_heads, keys, values;
+  int64_t q_stride[2], k_stride[2], v_stride[2], y_stride[2], decay_stride[2], rate_stride[2];
+  int64_t state_stride;              /* 0 = heads * keys * values */
+  double scale;
+  int32_t dtype;                     /* MS_DTYPE_*: of q, k, v and y */
+  int32_t device;
+  void* stream;
+} ms_gated_delta_step_desc;
+
+ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* desc, const void* q, const void* k,
+                              const void* v, const float* decay, const float* rate, float* state,
+                              const int32_t* slots, void* y);
 
 const char* ms_last_error(void);
 

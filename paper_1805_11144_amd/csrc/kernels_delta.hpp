@@ -1,0 +1,626 @@
+// The gated delta rule: a head's memory S [keys][values] forgets by a = exp(decay)
+// and learns, with rate b, the error z between a value and what is read at its key:
+//     P = a S,  z = v - P'k,  S <- P + b k z',  y = scale S'q.
+//
+// Chunks of C steps.  With G the sums of decays from the chunk's start, e = exp(G),
+// D[i][j] = exp(G[i] - G[j]) for i >= j and 0 above, o = D's last row:
+//     M = D o (K K') below the diagonal,  T = (I + M diag(b))^-1
+//     Z = T (V - diag(e) K S)
+//     Y = scale (diag(e) Q S + (D o (Q K')) diag(b) Z)
+//     S <- e[C-1] S + K' diag(o b) Z
+// k_delta_chunk computes T and the lower triangle of scale D o (Q K') diag(b) of
+// every chunk, all at once; k_delta_scan goes through the chunks in order.  The
+// columns of S (the values) never meet: a wavefront carries 16 of them through the
+// whole sequence in registers, and the rows of one product's result, four to a
+// lane, are the next product's operand as they are if the other operand's columns
+// are in the same order (32 of them: 0..3, 16..19 to lanes 0..15, 4..7, 20..23 to
+// 16..31, and so on).  Only K, K', Q and the two triangles pass through LDS, for
+// all wavefronts of a workgroup, laid out as the matrix instructions take them.
+//
+// Arithmetic: 16-bit matrix instructions, 16 times as fast as 32-bit ones.  A
+// 32-bit value is the sum of three bf16 parts (24 bits, and bf16 has float32's
+// range), bf16 inputs are one part, and products of parts below 2^-24 of the result
+// are left out: 3 products with an input, 6 between two 32-bit values.  What only
+// passes into a bf16 result, and not into the state (the second term of Y, and the
+// state read by Q), takes two parts, 16 bits for a result of 8.  The sums of decays
+// are 64-bit: a difference of two of them is good where each is large.
+#pragma once
+
+#include "kernels_words.hpp"
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Strides in values: between batch rows, steps, heads.
+struct Walk {
+  int64_t b, t, h;
+};
+
+struct DeltaArgs {
+  int64_t batch, nchunk;
+  int32_t steps, heads, group, dk, dv;   // group: heads that share a key head
+  Walk q, k, v, y, decay, rate;
+  const int32_t* lengths;
+  float scale;
+};
+
+// A chunk's steps: twice as many triangles fit into LDS where inputs are one part.
+template <class T>
+constexpr int kChunk = sizeof(T) == 2 ? 64 : 32;
+template <class T>
+constexpr int kIn = sizeof(T) == 2 ? 1 : 3;    // parts of an input
+template <class T>
+constexpr int kOut = sizeof(T) == 2 ? 2 : 3;   // of what only a result in T sees
+constexpr int kState = 3;                      // of everything else
+
+// Eight values of an operand's row, as P parts.
+template <int P>
+struct Op {
+  bf16x8 p[P];
+};
+
+template <int P>
+__device__ __forceinline__ Op<P> op_of(const float (&x)[8]) {
+  Op<P> o;
+  float r[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = x[j];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      o.p[p][j] = (__bf16)r[j];
+      if (p + 1 < P) r[j] -= (float)o.p[p][j];
+    }
+  return o;
+}
+
+template <int P>
+__device__ __forceinline__ Op<P> op_of(f32x4 a, f32x4 b) {
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  return op_of<P>(x);
+}
+
+// c + a b over the parts whose product is at least 2^(-8 (MAX - 1)) of the whole,
+// the smallest first.
+template <int MAX, int PA, int PB>
+__device__ __forceinline__ f32x4 op_mul(const Op<PA>& a, const Op<PB>& b, f32x4 c) {
+#pragma unroll
+  for (int s = MAX - 1; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+      if (s - i >= 0 && s - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], c, 0, 0, 0);
+  return c;
+}
+
+__device__ __forceinline__ f32x4 zero4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
+
+// a x, and nothing of x where a is 0.
+__device__ __forceinline__ float share_of(float a, float x) { return a == 0.0f ? 0.0f : a * x; }
+
+// Eight values from p, n of them there (below 0: none), the others zeros.
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, int n, float (&x)[8]) {
+  if constexpr (VEC) {
+    if (n > 0) {
+      constexpr int W = 16 / sizeof(T);
+#pragma unroll
+      for (int q = 0; q < 8; q += W) {
+        const Words<T, W> w = *(const Words<T, W>*)(p + q);
+#pragma unroll
+        for (int j = 0; j < W; ++j) x[q + j] = as_f32(w.v[j]);
+      }
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < n ? as_f32(p[j]) : 0.0f;
+  }
+}
+
+template <class T, bool VEC>
+__device__ __forceinline__ Op<kIn<T>> op_load(const T* p, int n) {
+  float x[8];
+  load8<T, VEC>(p, n, x);
+  return op_of<kIn<T>>(x);
+}
+
+// ---------------------------------------------------------------- triangles
+// A triangle's 16 x 32 pieces that are not all zeros, by rows: of a lower one piece
+// (mt, ks) with ks <= mt / 2, of an upper one its mirror image.
+__host__ __device__ constexpr int tri_pieces(int C) { return C / 32 * (C / 32 + 1); }
+template <int C, bool UPPER>
+__device__ __forceinline__ constexpr int tri_piece(int mt, int ks) {
+  const int m = UPPER ? C / 16 - 1 - mt : mt, k = UPPER ? C / 32 - 1 - ks : ks;
+  return m / 2 * (m / 2 + 1) + m % 2 * (m / 2 + 1) + k;
+}
+template <int C, bool UPPER>
+__device__ __forceinline__ constexpr bool tri_has(int mt, int ks) {
+  return UPPER ? ks >= mt / 2 : ks <= mt / 2;
+}
+
+// What k_delta_chunk leaves of a chunk: T in three parts, the reads' triangle in PA
+// parts, each piece 64 x 16 bytes, then e, o and b.
+template <int C, int PA>
+struct ChunkWork {
+  static constexpr int solve = 0, reads = kState * tri_pieces(C) * 1024, scales = reads + PA * tri_pieces(C) * 1024,
+                       bytes = scales + 3 * C * 4;
+};
+
+// The pieces of a triangle in LDS (rows LD apart), as operands, to memory.
+template <int C, int LD, bool UPPER, int P>
+__device__ __forceinline__ void tri_store(const float* m, char* out, int tid, int threads) {
+  for (int u = tid; u < C / 16 * (C / 32) * 64; u += threads) {
+    const int lane = u % 64, ks = u / 64 % (C / 32), mt = u / 64 / (C / 32);
+    if (!tri_has<C, UPPER>(mt, ks)) continue;
+    const int i = mt * 16 + lane % 16, j = ks * 32 + lane / 16 * 4;
+    float x[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int c = j + q % 4 + q / 4 * 16;
+      x[q] = UPPER ? m[c * LD + i] : m[i * LD + c];
+    }
+    const Op<P> o = op_of<P>(x);
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      *(bf16x8*)(out + ((p * tri_pieces(C) + tri_piece<C, UPPER>(mt, ks)) * 64 + lane) * 16) = o.p[p];
+  }
+}
+
+// T and the reads' triangle of every chunk.  GRAD: their transposes, the second one
+// without b.  A wavefront computes 16 rows of K K' and Q K'; the inverse of the
+// diagonal blocks of 16 goes column by column, a lane each, and blocks double by
+// [[A, 0], [B, C]]^-1 = [[A', 0], [-C' B A', C']] on 32-bit matrix instructions.
+template <class T, bool VEC, int DK, bool GRAD>
+__global__ void __launch_bounds__(kChunk<T> * 4)
+    k_delta_chunk(DeltaArgs p, const T* q, const T* k, const float* decay, const float* rate, char* work) {
+  constexpr int C = kChunk<T>, LD = C + 4, KS = DK / 32, PA = GRAD ? kState : kOut<T>;
+  using Work = ChunkWork<C, PA>;
+  __shared__ float m[C * LD], t[C * LD];
+  __shared__ double sum[C];
+  __shared__ float rates[C];
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, g = lane / 16;
+  const int64_t all = p.batch * p.heads * p.nchunk;
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const int64_t chunk = u % p.nchunk, b = u / p.nchunk / p.heads;
+    const int head = (int)(u / p.nchunk % p.heads), kh = head / p.group;
+    const int64_t t0 = chunk * C;
+    const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
+    const int n = (int)min((int64_t)C, len - t0);   // steps of this chunk that count
+    if (n <= 0) continue;                           // nothing reads it
+    char* out = work + u * Work::bytes;
+    if (tid < C) {
+      double d = 0.0;
+      float r = 0.0f;
+      if (tid < n) {
+        const float x = decay[b * p.decay.b + (t0 + tid) * p.decay.t + head * p.decay.h];
+        d = x < -200.0f ? -200.0 : (double)x;   // exp is 0 in 32 bits long before
+        r = rate[b * p.rate.b + (t0 + tid) * p.rate.t + head * p.rate.h];
+      }
+#pragma unroll
+      for (int o = 1; o < C; o *= 2) {
+        const double x = __shfl_up(d, o, 64);
+        if (tid >= o) d += x;
+      }
+      sum[tid] = d * 1.4426950408889634;
+      rates[tid] = r;
+    }
+    __syncthreads();
+    if (tid < C) {
+      float* s = (float*)(out + Work::scales);
+      s[tid] = __builtin_amdgcn_exp2f((float)sum[tid]);
+      s[C + tid] = __builtin_amdgcn_exp2f((float)(sum[C - 1] - sum[tid]));
+      s[2 * C + tid] = rates[tid];
+    }
+    // rows 16 wave .. of K K' and Q K'
+    f32x4 kk[C / 16], qk[C / 16];
+    {
+      const int i = wave * 16 + lane % 16;
+      const T* kb = k + b * p.k.b + t0 * p.k.t + kh * p.k.h;
+      const T* qb = q + b * p.q.b + t0 * p.q.t + kh * p.q.h;
+      Op<kIn<T>> ka[KS], qa[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int d = ks * 32 + g * 8, there = i < n ? p.dk - d : 0;
+        ka[ks] = op_load<T, VEC>(kb + (there > 0 ? i * p.k.t + d : 0), there);
+        qa[ks] = op_load<T, VEC>(qb + (there > 0 ? i * p.q.t + d : 0), there);
+      }
+#pragma unroll
+      for (int ct = 0; ct < C / 16; ++ct) {
+        kk[ct] = qk[ct] = zero4();
+        if (ct > wave) continue;
+        const int j = ct * 16 + lane % 16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int d = ks * 32 + g * 8, there = j < n ? p.dk - d : 0;
+          const Op<kIn<T>> kb_ = op_load<T, VEC>(kb + (there > 0 ? j * p.k.t + d : 0), there);
+          kk[ct] = op_mul<kIn<T>>(ka[ks], kb_, kk[ct]);
+          qk[ct] = op_mul<kIn<T>>(qa[ks], kb_, qk[ct]);
+        }
+      }
+    }
+#pragma unroll
+    for (int ct = 0; ct < C / 16; ++ct)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = wave * 16 + g * 4 + r, j = ct * 16 + lane % 16;
+        const float d = i >= j ? __builtin_amdgcn_exp2f((float)(sum[i] - sum[j])) : 0.0f;
+        m[i * LD + j] = i > j ? kk[ct][r] * d * rates[j] : 0.0f;
+        t[i * LD + j] = 0.0f;
+        qk[ct][r] *= d * p.scale * (GRAD ? 1.0f : rates[j]);
+      }
+    __syncthreads();
+    if (tid < C) {
+      const int at = tid / 16 * 16, c = tid % 16;
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float s = i == c ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < i; ++j) s = fmaf(-m[(at + i) * LD + at + j], x[j], s);
+        x[i] = s;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t[(at + i) * LD + at + c] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int size = 16; size < C; size *= 2) {
+      // B A', in the place of B, and then -C' of it; a tile of 16 x 16 to a wavefront
+      const int side = size / 16, per = side * side, tiles = C / (2 * size) * per;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        f32x4 c = zero4();
+        int r0 = 0, c0 = 0;
+        if (wave < tiles) {
+          const int pair = wave / per * 2 * size;
+          r0 = pair + size + wave % per / side * 16, c0 = pair + wave % side * 16;
+          for (int x = 0; x < size; x += 4) {
+            const float a = half ? t[(r0 + lane % 16) * LD + pair + size + x + g] : m[(r0 + lane % 16) * LD + pair + x + g];
+            const float v = half ? m[(pair + size + x + g) * LD + c0 + lane % 16] : t[(pair + x + g) * LD + c0 + lane % 16];
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(a, v, c, 0, 0, 0);
+          }
+        }
+        __syncthreads();
+        if (wave < tiles)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (half) t[(r0 + g * 4 + r) * LD + c0 + lane % 16] = -c[r];
+            else m[(r0 + g * 4 + r) * LD + c0 + lane % 16] = c[r];
+          }
+        __syncthreads();
+      }
+    }
+    tri_store<C, LD, GRAD, kState>(t, out + Work::solve, tid, C * 4);
+#pragma unroll
+    for (int ct = 0; ct < C / 16; ++ct)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m[(wave * 16 + g * 4 + r) * LD + ct * 16 + lane % 16] = qk[ct][r];
+    __syncthreads();
+    tri_store<C, LD, GRAD, PA>(m, out + Work::reads, tid, C * 4);
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ operands
+// A chunk of a matrix [C][DK] as operands in LDS: ROWS: its rows are steps, COLS:
+// they are keys (the transpose).  A thread takes blocks of 4 steps x 4 keys, which
+// are whole halves of an operand's 16 bytes either way.  Lane m + 16 g of a piece
+// lies at (m ^ g) + 16 g: the blocks of a wavefront then write to all banks.
+template <class T, bool VEC, int C, int DK, bool ROWS, bool COLS>
+__device__ __forceinline__ void stage_operands(const T* x, int64_t step, int n, int dk, char* rows, char* cols, int tid,
+                                               int threads) {
+  constexpr int P = kIn<T>, RP = C / 16 * (DK / 32), CP = DK / 16 * (C / 32);
+  for (int u = tid; u < C * DK / 16; u += threads) {
+    // 8 blocks of keys and 8 of steps to 64 threads
+    const int rest = u / 64, d0 = (u % 8 + rest % (DK / 32) * 8) * 4, t0 = (u / 8 % 8 + rest / (DK / 32) * 8) * 4;
+    float v[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool there = t0 + i < n;
+      if constexpr (VEC) {
+        Words<T, 4> w{};
+        if (there && d0 < dk) w = *(const Words<T, 4>*)(x + (t0 + i) * step + d0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = as_f32(w.v[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = there && d0 + j < dk ? as_f32(x[(t0 + i) * step + d0 + j]) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int part = 0; part < P; ++part) {
+      __bf16 h[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          h[i][j] = (__bf16)v[i][j];
+          if (part + 1 < P) v[i][j] -= (float)h[i][j];
+        }
+      if constexpr (ROWS) {
+        const int piece = t0 / 16 * (DK / 32) + d0 / 32, g = d0 / 4 % 4, half = d0 / 16 % 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *(bf16x4*)(rows + (((part * RP + piece) * 64 + ((t0 + i) % 16 ^ g) + 16 * g) * 16 + half * 8)) =
+              bf16x4{h[i][0], h[i][1], h[i][2], h[i][3]};
+      }
+      if constexpr (COLS) {
+        const int piece = d0 / 16 * (C / 32) + t0 / 32, g = t0 / 4 % 4, half = t0 / 16 % 2;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *(bf16x4*)(cols + (((part * CP + piece) * 64 + ((d0 + j) % 16 ^ g) + 16 * g) * 16 + half * 8)) =
+              bf16x4{h[0][j], h[1][j], h[2][j], h[3][j]};
+      }
+    }
+  }
+}
+
+// A piece of `pieces`, at this lane's place `at` (swizzled or not).
+template <int P>
+__device__ __forceinline__ Op<P> op_take(const char* lds, int pieces, int piece, int at) {
+  Op<P> o;
+#pragma unroll
+  for (int p = 0; p < P; ++p) o.p[p] = *(const bf16x8*)(lds + ((p * pieces + piece) * 64 + at) * 16);
+  return o;
+}
+
+// LDS of a scan: rows of Q and K, columns of K (GRAD: rows of K, columns of both), the chunk's triangles and scales.
+template <class T, int DK, bool GRAD>
+struct ScanLds {
+  static constexpr int C = kChunk<T>, one = kIn<T> * C * DK * 2, PA = GRAD ? kState : kOut<T>;
+  static constexpr int rows = 0, cols = one, q = 2 * one, work = 3 * one, bytes = work + ChunkWork<C, PA>::bytes;
+};
+
+// Copies a chunk's triangles and scales.
+__device__ __forceinline__ void copy_work(const char* from, char* to, int bytes, int tid, int threads) {
+  for (int i = tid * 16; i < bytes; i += threads * 16) *(uint4*)(to + i) = *(const uint4*)(from + i);
+}
+
+// Batch row, head and block of columns of a workgroup: the blocks of a head are 8
+// apart, on one of the 8 dies, whose L2 then reads the head's K, Q and triangles once.
+__device__ __forceinline__ bool scan_place(const DeltaArgs& p, int blocks, int64_t& bh, int& block) {
+  const int64_t x = blockIdx.x;
+  bh = x / (8 * blocks) * 8 + x % 8;
+  block = (int)(x / 8 % blocks);
+  return bh < p.batch * p.heads;
+}
+
+// The chunks of a head in order.  grid: see scan_place; a wavefront has 16 columns.
+// states: S before each chunk, z: the errors, for the gradient (NULL: not kept).
+template <class T, bool VEC, int DK>
+__global__ void __launch_bounds__(256)
+    k_delta_scan(DeltaArgs p, int blocks, const T* q, const T* k, const T* v, const float* s0, const char* work, T* y,
+                 float* last, float* states, float* errors) {
+  using Lds = ScanLds<T, DK, false>;
+  constexpr int C = Lds::C, KS = DK / 32, PA = Lds::PA, PI = kIn<T>, RP = C / 16 * KS, CP = DK / 16 * (C / 32);
+  using Work = ChunkWork<C, PA>;
+  extern __shared__ __align__(16) char lds[];
+  int64_t bh;
+  int block;
+  if (!scan_place(p, blocks, bh, block)) return;
+  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, at = (lane % 16 ^ g) + 16 * g;
+  const int64_t b = bh / p.heads;
+  const int head = (int)(bh % p.heads), kh = head / p.group;
+  const int col = (block * (int)(blockDim.x / 64) + tid / 64) * 16 + lane % 16;
+  const bool mine = col < p.dv;
+  const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
+  const T* vb = v + b * p.v.b + head * p.v.h + col;
+  T* yb = y + b * p.y.b + head * p.y.h + col;
+  f32x4 s[DK / 16];
+#pragma unroll
+  for (int m = 0; m < DK / 16; ++m)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int d = m * 16 + g * 4 + r;
+      s[m][r] = s0 && mine && d < p.dk ? s0[(bh * p.dk + d) * p.dv + col] : 0.0f;
+    }
+  int64_t chunk = 0;
+  for (; chunk * C < len; ++chunk) {
+    const int64_t t0 = chunk * C;
+    const int n = (int)min((int64_t)C, len - t0);
+    __syncthreads();
+    stage_operands<T, VEC, C, DK, true, true>(k + b * p.k.b + t0 * p.k.t + kh * p.k.h, p.k.t, n, p.dk, lds + Lds::rows,
+                                              lds + Lds::cols, tid, blockDim.x);
+    stage_operands<T, VEC, C, DK, true, false>(q + b * p.q.b + t0 * p.q.t + kh * p.q.h, p.q.t, n, p.dk, lds + Lds::q,
+                                               nullptr, tid, blockDim.x);
+    copy_work(work + (bh * p.nchunk + chunk) * Work::bytes, lds + Lds::work, Work::bytes, tid, blockDim.x);
+    f32x4 z[C / 16], o[C / 16];
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = m * 16 + g * 4 + r;
+        z[m][r] = mine && t < n ? as_f32(vb[(t0 + t) * p.v.t]) : 0.0f;
+      }
+    if (states && mine)
+#pragma unroll
+      for (int m = 0; m < DK / 16; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int d = m * 16 + g * 4 + r;
+          if (d < p.dk) states[((bh * p.nchunk + chunk) * p.dk + d) * p.dv + col] = s[m][r];
+        }
+    __syncthreads();
+    const float* e = (const float*)(lds + Lds::work + Work::scales);
+    Op<kState> sp[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m) {
+      f32x4 c = zero4(), w = zero4();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        c = op_mul<kState>(op_take<PI>(lds + Lds::rows, RP, m * KS + ks, at), sp[ks], c);
+        w = op_mul<kOut<T>>(op_take<PI>(lds + Lds::q, RP, m * KS + ks, at), sp[ks], w);
+      }
+      const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[m][r] -= share_of(em[r], c[r]), o[m][r] = share_of(em[r], w[r]) * p.scale;
+    }
+    Op<kState> zp[C / 32];
+#pragma unroll
+    for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m) {
+      z[m] = zero4();
+#pragma unroll
+      for (int ks = 0; ks <= m / 2; ++ks)
+        z[m] = op_mul<kState>(
+            op_take<kState>(lds + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zp[ks], z[m]);
+    }
+    if (errors && mine)
+#pragma unroll
+      for (int m = 0; m < C / 16; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          errors[((bh * p.nchunk + chunk) * C + m * 16 + g * 4 + r) * p.dv + col] = z[m][r];
+    Op<kOut<T>> zo[C / 32];
+#pragma unroll
+    for (int ks = 0; ks < C / 32; ++ks) zo[ks] = op_of<kOut<T>>(z[2 * ks], z[2 * ks + 1]);
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m) {
+#pragma unroll
+      for (int ks = 0; ks <= m / 2; ++ks)
+        o[m] = op_mul<kOut<T>>(
+            op_take<PA>(lds + Lds::work + Work::reads, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zo[ks], o[m]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = m * 16 + g * 4 + r;
+        if (mine && t0 + t < p.steps) yb[(t0 + t) * p.y.t] = t < n ? (T)o[m][r] : (T)0.0f;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[m][r] *= e[C + m * 16 + g * 4 + r] * e[2 * C + m * 16 + g * 4 + r];
+    }
+#pragma unroll
+    for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
+    const float keep = e[C - 1];
+#pragma unroll
+    for (int m = 0; m < DK / 16; ++m) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
+#pragma unroll
+      for (int ks = 0; ks < C / 32; ++ks)
+        s[m] = op_mul<kState>(op_take<PI>(lds + Lds::cols, CP, m * (C / 32) + ks, at), zp[ks], s[m]);
+    }
+  }
+  if (mine) {
+    for (int64_t t = chunk * C + g; t < p.steps; t += 4) yb[t * p.y.t] = (T)0.0f;
+    if (last)
+#pragma unroll
+      for (int m = 0; m < DK / 16; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int d = m * 16 + g * 4 + r;
+          if (d < p.dk) last[(bh * p.dk + d) * p.dv + col] = s[m][r];
+        }
+  }
+}
+
+// ---------------------------------------------------------------- single step
+struct DeltaStepArgs {
+  int64_t rows, slots, state;   // state: between slots
+  int32_t heads, group, dk, dv;
+  int64_t q[2], k[2], v[2], y[2], decay[2], rate[2];   // between rows, between heads
+  float scale;
+};
+
+constexpr int kStepRows = 16;   // of a matrix to a thread, at most
+
+// One step of a row's head: P'k and P'q are sums over the keys of one read of the
+// matrix, which stays in registers, y = scale (P'q + b z (k'q)).  `nl` threads (a
+// power of two, at most 32) take V columns each, the others of 256 further keys.
+template <class T, int V>
+__global__ void __launch_bounds__(256) k_delta_step(DeltaStepArgs p, int32_t nl, int32_t tiles, const T* q, const T* k,
+                                                    const T* v, const float* decay, const float* rate, float* state,
+                                                    const int32_t* slots, T* y) {
+  __shared__ float kq[2][128];
+  __shared__ float red[2][256 / 4 * 4][V];   // sums of up to 64 groups of columns and 4 wavefronts
+  __shared__ float dots[4];
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, groups = 256 / nl, rg = tid / nl;
+  const int64_t all = p.rows * p.heads * tiles;
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const int64_t i = u / tiles / p.heads;
+    const int head = (int)(u / tiles % p.heads), kh = head / p.group;
+    const int c = ((int)(u % tiles) * nl + tid % nl) * V;
+    const bool mine = c < p.dv;
+    const int64_t slot = slots ? (int64_t)slots[i] : i;
+    if (slot < 0 || slot >= p.slots) {   // idle
+      if (mine && rg == 0)
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[i * p.y[0] + head * p.y[1] + c + e] = (T)0.0f;
+      continue;
+    }
+    float* s = state + slot * p.state + (int64_t)head * p.dk * p.dv + c;
+    Words<float, V> m[kStepRows];
+#pragma unroll
+    for (int r = 0; r < kStepRows; ++r) {
+      const int d = rg + r * groups;
+#pragma unroll
+      for (int e = 0; e < V; ++e) m[r].v[e] = 0.0f;
+      if (mine && d < p.dk) m[r] = *(const Words<float, V>*)(s + (int64_t)d * p.dv);
+    }
+    float kd = 0.0f, qd = 0.0f;
+    if (tid < 128 && tid < p.dk) {
+      kd = as_f32(k[i * p.k[0] + kh * p.k[1] + tid]);
+      qd = as_f32(q[i * p.q[0] + kh * p.q[1] + tid]);
+    }
+    if (tid < 128) kq[0][tid] = kd, kq[1][tid] = qd;
+    float dot = kd * qd;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o, 64);
+    if (lane == 0) dots[wave] = dot;
+    const float a = expf(decay[i * p.decay[0] + head * p.decay[1]]);
+    const float b = rate[i * p.rate[0] + head * p.rate[1]];
+    __syncthreads();
+    dot = dots[0] + dots[1];
+    float w[V], o[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[e] = o[e] = 0.0f;
+#pragma unroll
+    for (int r = 0; r < kStepRows; ++r) {
+      const int d = rg + r * groups;
+      const float kr = d < 128 ? kq[0][d] : 0.0f, qr = d < 128 ? kq[1][d] : 0.0f;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        m[r].v[e] = share_of(a, m[r].v[e]);
+        w[e] = fmaf(m[r].v[e], kr, w[e]);
+        o[e] = fmaf(m[r].v[e], qr, o[e]);
+      }
+    }
+    for (int x = nl; x < 64; x *= 2)
+#pragma unroll
+      for (int e = 0; e < V; ++e) w[e] += __shfl_xor(w[e], x, 64), o[e] += __shfl_xor(o[e], x, 64);
+    if (lane < nl)
+#pragma unroll
+      for (int e = 0; e < V; ++e) red[0][wave * nl + lane][e] = w[e], red[1][wave * nl + lane][e] = o[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      w[e] = o[e] = 0.0f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[e] += red[0][x * nl + tid % nl][e], o[e] += red[1][x * nl + tid % nl][e];
+    }
+    if (mine) {
+      float z[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        z[e] = b * (as_f32(v[i * p.v[0] + head * p.v[1] + c + e]) - w[e]);
+        if (rg == 0) y[i * p.y[0] + head * p.y[1] + c + e] = (T)(p.scale * fmaf(z[e], dot, o[e]));
+      }
+#pragma unroll
+      for (int r = 0; r < kStepRows; ++r) {
+        const int d = rg + r * groups;
+        if (d >= p.dk) continue;
+        const float kr = kq[0][d];
+#pragma unroll
+        for (int e = 0; e < V; ++e) m[r].v[e] = fmaf(kr, z[e], m[r].v[e]);
+        *(Words<float, V>*)(s + (int64_t)d * p.dv) = m[r];
+      }
+    }
+    __syncthreads();   // kq, red and dots are free again
+  }
+}

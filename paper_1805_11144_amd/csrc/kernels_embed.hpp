@@ -19,44 +19,7 @@
 // beginnings 9, rows 17: launches that each wait for the one before.
 #pragma once
 
-#include <hip/hip_runtime.h>
-
-#include <cstdint>
-
-template <class T, int V>
-struct alignas(sizeof(T) * V) Words {
-  T v[V];
-};
-
-template <class T>
-__device__ __forceinline__ float as_f32(T x) {
-  return (float)x;
-}
-
-// Results go past the caches, which then keep what is read: a lookup of 131072
-// rows of 1024 bf16 took 83 us with plain stores and takes 55 with these.
-template <class T, int V>
-__device__ __forceinline__ void put_once(T* p, const Words<T, V>& w) {
-  constexpr int B = sizeof(T) * V;
-  if constexpr (B % 4 == 0) {
-    typedef uint32_t Raw __attribute__((ext_vector_type(B / 4)));
-    __builtin_nontemporal_store(__builtin_bit_cast(Raw, w), (Raw*)p);
-  } else {
-    *(Words<T, V>*)p = w;
-  }
-}
-
-// Reads of what is used once, the same way.
-template <class T, int V>
-__device__ __forceinline__ Words<T, V> take_once(const T* p) {
-  constexpr int B = sizeof(T) * V;
-  if constexpr (B % 4 == 0) {
-    typedef uint32_t Raw __attribute__((ext_vector_type(B / 4)));
-    return __builtin_bit_cast(Words<T, V>, __builtin_nontemporal_load((const Raw*)p));
-  } else {
-    return *(const Words<T, V>*)p;
-  }
-}
+#include "kernels_words.hpp"
 
 // LDS accesses of one wavefront stay in the order written here.
 __device__ __forceinline__ void wave_order() {

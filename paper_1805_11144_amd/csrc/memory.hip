@@ -1,0 +1,311 @@
+// The operators of keyed memories in the C ABI: argument checks, workspace layouts
+// and launches.  The kernels are in kernels_delta.hpp and kernels_delta_grad.hpp.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "host.hpp"
+#include "kernels_delta.hpp"
+#include "kernels_delta_grad.hpp"
+#include "operators_host.hpp"
+#include "operators_rules.hpp"
+
+using namespace ms;
+
+namespace {
+
+// Calls f with a key head's padded width.
+template <class F>
+void with_keys(int64_t dk, F&& f) {
+  if (dk <= 32) f(std::integral_constant<int, 32>{});
+  else if (dk <= 64) f(std::integral_constant<int, 64>{});
+  else f(std::integral_constant<int, 128>{});
+}
+
+template <class F>
+void with_flag(bool b, F&& f) {
+  if (b) f(std::true_type{});
+  else f(std::false_type{});
+}
+
+template <class F>
+void with_value(int32_t dtype, F&& f) {
+  if (dtype == MS_DTYPE_BF16) f((__bf16)0.0f);
+  else f(0.0f);
+}
+
+template <class K>
+void allow_lds(K k, size_t lds) {
+  if (lds > 65536) HIPCHECK(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+}
+
+// ------------------------------------------------------------------- delta
+Walk walk_of(const int64_t* s, int64_t steps, int64_t heads, int64_t dim) {
+  Walk w{s[0], s[1], s[2]};
+  if (s[0] == 0 && s[1] == 0 && s[2] == 0) w = {steps * heads * dim, heads * dim, dim};
+  need(w.b >= 0 && w.t >= 0 && w.h >= 0 && w.b < kMaxStride && w.t < kMaxStride && w.h < kMaxStride,
+       "strides must not be negative");
+  return w;
+}
+
+// Whether runs of `dim` values at these strides are apart: ordered by stride, each
+// steps over all that the ones before it reach.
+bool walk_apart(Walk w, int64_t batch, int64_t steps, int64_t heads, int64_t dim) {
+  if (batch == 0 || steps == 0 || heads == 0) return true;
+  std::pair<int64_t, int64_t> d[3] = {{w.b, batch}, {w.t, steps}, {w.h, heads}};
+  std::sort(d, d + 3);
+  __int128 reach = dim;
+  for (const auto& [stride, n] : d) {
+    if (n == 1) continue;
+    if (stride < reach) return false;
+    reach += (__int128)stride * (n - 1);
+  }
+  return true;
+}
+
+struct Delta {
+  DeltaArgs a;
+  int64_t chunks;            // of all heads and rows
+  int64_t chunk_steps, work;   // bytes a chunk
+  int blocks, waves;
+};
+
+template <class T>
+int64_t chunk_bytes(bool grad) {
+  return grad ? ChunkWork<kChunk<T>, kState>::bytes : ChunkWork<kChunk<T>, kOut<T>>::bytes;
+}
+
+Delta check_delta(const ms_gated_delta_desc* d, bool grad) {
+  need(d != nullptr, "NULL descriptor");
+  need(d->steps >= 0 && d->steps < ((int64_t)1 << 31), "steps must be in [0, 2^31)");
+  need(d->batch >= 0 && d->batch < ((int64_t)1 << 31), "batch must be in [0, 2^31)");
+  need(d->key_heads >= 1 && d->heads >= 1 && d->heads <= 65536 && d->heads % d->key_heads == 0,
+       "heads must be in [1, 65536], a multiple of key_heads");
+  need(d->keys >= 1 && d->keys <= 128, "keys must be in [1, 128]");
+  need(d->values >= 1 && d->values <= 65536, "values must be in [1, 65536]");
+  need_dtype(d->dtype);
+  need(std::isfinite((float)d->scale), "scale must be finite in 32 bits");
+  Delta p{};
+  DeltaArgs& a = p.a;
+  a.batch = d->batch, a.steps = (int32_t)d->steps, a.heads = (int32_t)d->heads;
+  a.group = (int32_t)(d->heads / d->key_heads), a.dk = (int32_t)d->keys, a.dv = (int32_t)d->values;
+  a.scale = (float)d->scale;
+  a.q = walk_of(d->q_stride, d->steps, d->key_heads, d->keys);
+  a.k = walk_of(d->k_stride, d->steps, d->key_heads, d->keys);
+  a.v = walk_of(d->v_stride, d->steps, d->heads, d->values);
+  a.y = walk_of(d->y_stride, d->steps, d->heads, d->values);
+  a.decay = walk_of(d->decay_stride, d->steps, d->heads, 1);
+  a.rate = walk_of(d->rate_stride, d->steps, d->heads, 1);
+  const bool half = d->dtype == MS_DTYPE_BF16;
+  p.chunk_steps = half ? kChunk<__bf16> : kChunk<float>;
+  a.nchunk = (d->steps + p.chunk_steps - 1) / p.chunk_steps;
+  const int tiles = (int)((d->values + 15) / 16);
+  p.blocks = (tiles + 3) / 4;
+  p.waves = (tiles + p.blocks - 1) / p.blocks;
+  need(d->batch * d->heads <= kMaxBlocks / p.blocks - 8, "batch * heads * values is too large");
+  p.chunks = d->batch * d->heads * a.nchunk;
+  need(p.chunks < ((int64_t)1 << 34), "batch * heads * steps is too large");
+  p.work = half ? chunk_bytes<__bf16>(grad) : chunk_bytes<float>(grad);
+  return p;
+}
+
+// What the gradient starts from: each chunk's state, then the errors.
+int64_t kept_states(const Delta& p) { return p.chunks * p.a.dk * p.a.dv; }
+int64_t kept_all(const Delta& p) { return kept_states(p) + p.chunks * p.chunk_steps * p.a.dv; }
+
+struct DeltaWork {
+  char* chunk;
+  float *dstates, *xs;
+  int64_t bytes;
+};
+
+DeltaWork delta_work(const Delta& p, bool grad, void* ws) {
+  Carve c{(char*)ws};
+  DeltaWork w{};
+  if (p.chunks > 0) {
+    w.chunk = c.take<char>(p.chunks * p.work);
+    if (grad) {
+      w.dstates = c.take<float>(kept_states(p));
+      w.xs = c.take<float>(p.chunks * p.chunk_steps * p.a.dv);
+    }
+  }
+  w.bytes = c.used;
+  return w;
+}
+
+bool words(const Walk& w, const void* p) { return w.b % 8 == 0 && w.t % 8 == 0 && w.h % 8 == 0 && (uintptr_t)p % 16 == 0; }
+
+dim3 scan_grid(const Delta& p) { return dim3((unsigned)(up(p.a.batch * p.a.heads, 8) * p.blocks)); }
+
+}  // namespace
+
+extern "C" {
+
+ms_status ms_gated_delta_kept(const ms_gated_delta_desc* d, int64_t* elements_out) {
+  return guarded([&] {
+    const Delta p = check_delta(d, false);
+    need(elements_out != nullptr, "NULL output");
+    *elements_out = kept_all(p);
+  });
+}
+
+ms_status ms_gated_delta_workspace(const ms_gated_delta_desc* d, int32_t grad, int64_t* bytes_out) {
+  return guarded([&] {
+    const Delta p = check_delta(d, grad != 0);
+    need(bytes_out != nullptr, "NULL output");
+    *bytes_out = delta_work(p, grad != 0, nullptr).bytes;
+  });
+}
+
+ms_status ms_gated_delta(const ms_gated_delta_desc* d, const void* q, const void* k, const void* v, const float* decay,
+                         const float* rate, const float* s0, const int32_t* lengths, void* y, float* last, float* kept,
+                         void* workspace, int64_t workspace_bytes) {
+  return guarded([&] {
+    Delta p = check_delta(d, false);
+    DeltaArgs& a = p.a;
+    if (a.batch == 0) return;
+    const size_t es = size_of(d->dtype);
+    need(walk_apart(a.y, a.batch, a.steps, a.heads, a.dv), "rows, steps or heads of y overlap");
+    need(a.steps == 0 || (q && k && v && decay && rate && y), "NULL array");
+    for (const void* x : {q, k, v, (const void*)y}) need_aligned(x, es, "q, k, v or y");
+    for (const void* x : {(const void*)decay, (const void*)rate, (const void*)s0, (const void*)lengths, (const void*)last,
+                          (const void*)kept})
+      need_aligned(x, 4, "decay, rate, s0, lengths, last or kept");
+    const DeltaWork w = delta_work(p, false, workspace);
+    need_workspace(workspace, workspace_bytes, w.bytes);
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    a.lengths = lengths;
+    float* errors = kept ? kept + kept_states(p) : nullptr;
+    with_value(d->dtype, [&](auto zero) {
+      using T = decltype(zero);
+      with_flag(a.dk % 8 == 0 && words(a.q, q) && words(a.k, k), [&](auto vec) {
+        with_keys(a.dk, [&](auto keys) {
+          constexpr int DK = decltype(keys)::value;
+          constexpr bool VEC = decltype(vec)::value;
+          if (p.chunks)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(k_delta_chunk<T, VEC, DK, false>),
+                               dim3((unsigned)std::min(p.chunks, kMaxBlocks)), dim3(kChunk<T> * 4), 0, st, a, (const T*)q,
+                               (const T*)k, decay, rate, w.chunk);
+          constexpr auto scan = k_delta_scan<T, VEC, DK>;
+          constexpr size_t lds = ScanLds<T, DK, false>::bytes;
+          allow_lds(scan, lds);
+          hipLaunchKernelGGL(scan, scan_grid(p), dim3(64 * p.waves), lds, st, a, p.blocks, (const T*)q, (const T*)k,
+                             (const T*)v, s0, (const char*)w.chunk, (T*)y, last, kept, errors);
+        });
+      });
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_gated_delta_grad(const ms_gated_delta_desc* d, const void* q, const void* k, const void* v, const float* decay,
+                              const float* rate, const float* kept, const int32_t* lengths, const void* dy,
+                              const float* dlast, void* dq, void* dk, void* dv, float* ddecay, float* drate, float* ds0,
+                              void* workspace, int64_t workspace_bytes) {
+  return guarded([&] {
+    Delta p = check_delta(d, true);
+    DeltaArgs& a = p.a;
+    if (a.batch == 0) return;
+    const size_t es = size_of(d->dtype);
+    need(a.steps == 0 || (q && k && v && decay && rate && kept && dy && dq && dk && dv && ddecay && drate), "NULL array");
+    for (const void* x : {q, k, v, dy, (const void*)dq, (const void*)dk, (const void*)dv})
+      need_aligned(x, es, "q, k, v, dy, dq, dk or dv");
+    for (const void* x : {(const void*)decay, (const void*)rate, (const void*)kept, (const void*)lengths, (const void*)dlast,
+                          (const void*)ddecay, (const void*)drate, (const void*)ds0})
+      need_aligned(x, 4, "decay, rate, kept, lengths, dlast, ddecay, drate or ds0");
+    const DeltaWork w = delta_work(p, true, workspace);
+    need_workspace(workspace, workspace_bytes, w.bytes);
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    a.lengths = lengths;
+    const int64_t cells = p.chunks / a.group;
+    const bool vec = a.dk % 8 == 0 && a.dv % 8 == 0 && words(a.q, q) && words(a.k, k) && words(a.y, dy) &&
+                     (uintptr_t)kept % 16 == 0;
+    with_value(d->dtype, [&](auto zero) {
+      using T = decltype(zero);
+      with_flag(vec, [&](auto flag) {
+        with_keys(a.dk, [&](auto keys) {
+          constexpr int DK = decltype(keys)::value;
+          constexpr bool VEC = decltype(flag)::value;
+          if (p.chunks)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(k_delta_chunk<T, VEC, DK, true>),
+                               dim3((unsigned)std::min(p.chunks, kMaxBlocks)), dim3(kChunk<T> * 4), 0, st, a, (const T*)q,
+                               (const T*)k, decay, rate, w.chunk);
+          constexpr auto back = k_delta_back<T, VEC, DK>;
+          constexpr size_t lds = ScanLds<T, DK, true>::bytes;
+          allow_lds(back, lds);
+          hipLaunchKernelGGL(back, scan_grid(p), dim3(64 * p.waves), lds, st, a, p.blocks, (const T*)q, (const T*)k,
+                             (const T*)dy, dlast, (const char*)w.chunk, (T*)dv, ds0, w.dstates, w.xs);
+          if (!p.chunks) return;
+          constexpr auto grad = k_delta_grad<T, VEC, VEC, DK>;
+          constexpr size_t more = GradLds<T, DK>::bytes;
+          allow_lds(grad, more);
+          hipLaunchKernelGGL(grad, dim3((unsigned)std::min(cells, kMaxBlocks)), dim3(kChunk<T> * 4), more, st, a, (const T*)q,
+                             (const T*)k, (const T*)dy, decay, rate, kept, kept + kept_states(p), (const float*)w.dstates,
+                             (const float*)w.xs, DeltaGradOut{dq, dk, ddecay, drate});
+        });
+      });
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* d, const void* q, const void* k, const void* v,
+                              const float* decay, const float* rate, float* state, const int32_t* slots, void* y) {
+  return guarded([&] {
+    need(d != nullptr, "NULL descriptor");
+    need(d->rows >= 0 && d->rows < ((int64_t)1 << 31) && d->n_slots >= 0 && d->n_slots < ((int64_t)1 << 31),
+         "rows and n_slots must be in [0, 2^31)");
+    need(d->key_heads >= 1 && d->heads >= 1 && d->heads <= 65536 && d->heads % d->key_heads == 0,
+         "heads must be in [1, 65536], a multiple of key_heads");
+    need(d->keys >= 1 && d->keys <= 128, "keys must be in [1, 128]");
+    need(d->values >= 1 && d->values <= 65536, "values must be in [1, 65536]");
+    need_dtype(d->dtype);
+    need(std::isfinite((float)d->scale), "scale must be finite in 32 bits");
+    DeltaStepArgs a{};
+    const auto pair = [&](const int64_t* s, int64_t heads, int64_t dim, int64_t* to) {
+      const bool packed = s[0] == 0 && s[1] == 0;
+      to[0] = packed ? heads * dim : s[0], to[1] = packed ? dim : s[1];
+      need(to[0] >= 0 && to[1] >= 0 && to[0] < kMaxStride && to[1] < kMaxStride, "strides must not be negative");
+    };
+    pair(d->q_stride, d->key_heads, d->keys, a.q);
+    pair(d->k_stride, d->key_heads, d->keys, a.k);
+    pair(d->v_stride, d->heads, d->values, a.v);
+    pair(d->y_stride, d->heads, d->values, a.y);
+    pair(d->decay_stride, d->heads, 1, a.decay);
+    pair(d->rate_stride, d->heads, 1, a.rate);
+    const int64_t matrices = d->heads * d->keys * d->values;
+    a.state = d->state_stride ? d->state_stride : matrices;
+    need(a.state >= matrices && a.state < kMaxStride, "strides between slots must be at least heads * keys * values");
+    if (d->rows == 0) return;
+    need(walk_apart({0, a.y[0], a.y[1]}, 1, d->rows, d->heads, d->values), "rows or heads of y overlap");
+    need(q && k && v && decay && rate && y && (state || d->n_slots == 0), "NULL array");
+    for (const void* x : {q, k, v, (const void*)y}) need_aligned(x, size_of(d->dtype), "q, k, v or y");
+    for (const void* x : {(const void*)decay, (const void*)rate, (const void*)state, (const void*)slots})
+      need_aligned(x, 4, "decay, rate, state or slots");
+    a.rows = d->rows, a.slots = d->n_slots, a.heads = (int32_t)d->heads, a.group = (int32_t)(d->heads / d->key_heads);
+    a.dk = (int32_t)d->keys, a.dv = (int32_t)d->values, a.scale = (float)d->scale;
+    DeviceGuard dg(d->device);
+    const bool vec = a.dv % 4 == 0 && a.state % 4 == 0 && (uintptr_t)state % 16 == 0;
+    const int width = vec ? 4 : 1;
+    int32_t nl = 1;
+    while (nl < 32 && nl * width < a.dv) nl *= 2;
+    const int32_t tiles = (a.dv + nl * width - 1) / (nl * width);
+    const int64_t all = d->rows * d->heads * tiles;
+    with_value(d->dtype, [&](auto zero) {
+      using T = decltype(zero);
+      with_flag(vec, [&](auto flag) {
+        constexpr int V = decltype(flag)::value ? 4 : 1;
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(k_delta_step<T, V>), dim3((unsigned)std::min(all, kMaxBlocks)), dim3(256), 0,
+                           (hipStream_t)d->stream, a, nl, tiles, (const T*)q, (const T*)k, (const T*)v, decay, rate, state,
+                           slots, (T*)y);
+      });
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+}  // extern "C"

@@ -104,6 +104,20 @@ class OrthRule(C.Structure):
                 ("nesterov", _i32)]
 
 
+class GatedDeltaDesc(C.Structure):
+    _fields_ = [("batch", _i64), ("steps", _i64), ("heads", _i64), ("key_heads", _i64), ("keys", _i64),
+                ("values", _i64), ("q_stride", _i64 * 3), ("k_stride", _i64 * 3), ("v_stride", _i64 * 3),
+                ("y_stride", _i64 * 3), ("decay_stride", _i64 * 3), ("rate_stride", _i64 * 3), ("scale", C.c_double),
+                ("dtype", _i32), ("device", _i32), ("stream", C.c_void_p)]
+
+
+class GatedDeltaStepDesc(C.Structure):
+    _fields_ = [("rows", _i64), ("n_slots", _i64), ("heads", _i64), ("key_heads", _i64), ("keys", _i64),
+                ("values", _i64), ("q_stride", _i64 * 2), ("k_stride", _i64 * 2), ("v_stride", _i64 * 2),
+                ("y_stride", _i64 * 2), ("decay_stride", _i64 * 2), ("rate_stride", _i64 * 2), ("state_stride", _i64),
+                ("scale", C.c_double), ("dtype", _i32), ("device", _i32), ("stream", C.c_void_p)]
+
+
 class MergesimError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"mergesim error {code}: {msg}")
@@ -157,6 +171,11 @@ _SIGNATURES = [
     ("ms_gated_lowpass_grad", [C.POINTER(GatedLowpassDesc), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64],
      _i32),
     ("ms_gated_lowpass_step", [C.POINTER(GatedStepDesc), _vp, _vp, _vp, _vp, _vp], _i32),
+    ("ms_gated_delta_kept", [C.POINTER(GatedDeltaDesc), C.POINTER(_i64)], _i32),
+    ("ms_gated_delta_workspace", [C.POINTER(GatedDeltaDesc), _i32, C.POINTER(_i64)], _i32),
+    ("ms_gated_delta", [C.POINTER(GatedDeltaDesc)] + [_vp] * 11 + [_i64], _i32),
+    ("ms_gated_delta_grad", [C.POINTER(GatedDeltaDesc)] + [_vp] * 16 + [_i64], _i32),
+    ("ms_gated_delta_step", [C.POINTER(GatedDeltaStepDesc)] + [_vp] * 8, _i32),
     ("ms_orth_workspace", [C.POINTER(OrthDesc), _i32, C.POINTER(_i64)], _i32),
     ("ms_orthogonalise", [C.POINTER(OrthDesc), _vp, _vp, _vp, _i64], _i32),
     ("ms_orthogonal_update", [C.POINTER(OrthDesc), C.POINTER(OrthRule), _vp, _vp, _vp, _vp, _i64], _i32),

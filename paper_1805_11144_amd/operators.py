@@ -14,8 +14,8 @@ from __future__ import annotations
 import ctypes as C
 
 from . import mergesim as _ms
-from .mergesim import (DTYPE_BF16, DTYPE_F32, IDS_I32, IDS_I64, EmbedDesc, GatedLowpassDesc, GatedStepDesc, OrthDesc,
-                       OrthRule, _check)
+from .mergesim import (DTYPE_BF16, DTYPE_F32, IDS_I32, IDS_I64, EmbedDesc, GatedDeltaDesc, GatedDeltaStepDesc,
+                       GatedLowpassDesc, GatedStepDesc, OrthDesc, OrthRule, _check)
 
 # Raises small singular values fast and leaves them within 0.3 of one: the coefficients published by K. Jordan et al.,
 # "Muon: An optimizer for hidden layers in neural networks" (2024).
@@ -263,6 +263,107 @@ def gated_lowpass_step(v, g, state, slots=None, out=None):
     slotp = _packed(slots, v, "slots", (rows,), _torch.int32)
     _written(*written)
     _check(_lib.ms_gated_lowpass_step(_on(d, v), v.data_ptr(), g.data_ptr(), state.data_ptr(), slotp, out.data_ptr()))
+    return out
+
+
+# --------------------------------------------------------------- gated delta rule
+def _walked(t, strides, inner=1):
+    """t [..., heads, dim] (inner=0: [..., heads]), its strides but those of the last `inner` dimensions written
+    down; copied where the last one is not contiguous (strides of 0 stand for a packed array)."""
+    if t.is_contiguous():
+        return t
+    n = t.dim() - inner
+    apart = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(n)]
+    if (inner and t.shape[-1] > 1 and t.stride(-1) != 1) or not any(apart):
+        return t.contiguous()
+    strides[:] = apart
+    return t
+
+
+def _delta_inputs(desc, dims, q, k, v, decay, rate):
+    """Fills a descriptor's sizes, types and strides; returns the arrays and the shapes of y and of a row's state."""
+    dtype = _gpu(v, (dims,), "v " + ("[rows, heads, values]" if dims == 3 else "[batch, steps, heads, values]"))
+    if q.dim() != dims:
+        raise ValueError(f"q has shape {tuple(q.shape)}: {dims} dimensions are wanted")
+    first, (heads, values), (key_heads, keys) = v.shape[:-2], v.shape[-2:], q.shape[-2:]
+    _like(q, v, "q", (*first, key_heads, keys), v.dtype)
+    _like(k, v, "k", q.shape, v.dtype)
+    for t, name in ((decay, "decay"), (rate, "rate")):
+        _like(t, v, name, (*first, heads), _torch.float32)
+    desc.heads, desc.key_heads, desc.keys, desc.values, desc.dtype = heads, key_heads, keys, values, dtype
+    return (_walked(q, desc.q_stride), _walked(k, desc.k_stride), _walked(v, desc.v_stride),
+            _walked(decay, desc.decay_stride, 0), _walked(rate, desc.rate_stride, 0), (heads, keys, values))
+
+
+def gated_delta(q, k, v, decay, rate, s0=None, lengths=None, scale=1.0, keep=False):
+    """The gated delta rule, a memory by key (ms_gated_delta): for each head, with P = exp(decay[:, t]) S and
+    z = v[:, t] - P'k[:, t], S <- P + rate[:, t] k[:, t] z' and y[:, t] = scale S'q[:, t], from s0 (zeros).
+
+    q, k [batch, steps, key_heads, keys], v [batch, steps, heads, values], float32 or bfloat16, heads a multiple of
+    key_heads and keys at most 128; decay (<= 0, -inf starts a sequence), rate [batch, steps, heads] float32;
+    s0 [batch, heads, keys, values] float32; lengths int32 [batch].
+    Returns (y, last): y like v, zeros past a row's length, and the state after its last step, float32.
+    keep: also what gated_delta_grad starts from."""
+    d = GatedDeltaDesc(scale=scale)
+    q, k, v, decay, rate, matrix = _delta_inputs(d, 4, q, k, v, decay, rate)
+    d.batch, d.steps = v.shape[:2]
+    f32, shape = _torch.float32, (v.shape[0], *matrix)
+    y, last = _torch.empty(v.shape, dtype=v.dtype, device=v.device), _torch.empty(shape, dtype=f32, device=v.device)
+    s0p, lp = _packed(s0, v, "s0", shape, f32), _packed(lengths, v, "lengths", v.shape[:1], _torch.int32)
+    ref = _on(d, v)
+    hold, ws, n = _scratch(v, _size(_lib.ms_gated_delta_workspace, ref, 0))
+    kept = _torch.empty(_size(_lib.ms_gated_delta_kept, ref), dtype=f32, device=v.device) if keep else None
+    _check(_lib.ms_gated_delta(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), decay.data_ptr(), rate.data_ptr(), s0p, lp,
+                               y.data_ptr(), last.data_ptr(), kept.data_ptr() if keep else None, ws, n))
+    return (y, last, kept) if keep else (y, last)
+
+
+def gated_delta_grad(q, k, v, decay, rate, kept, dy, dlast=None, lengths=None, scale=1.0):
+    """(dq, dk, dv, ddecay, drate, ds0) of gated_delta from dL/dy and dL/dlast (ms_gated_delta_grad); kept: what
+    the forward call with keep=True left."""
+    d = GatedDeltaDesc(scale=scale)
+    q, k, v, decay, rate, matrix = _delta_inputs(d, 4, q, k, v, decay, rate)
+    d.batch, d.steps = v.shape[:2]
+    _like(dy, v, "dy", v.shape, v.dtype)
+    dy = _walked(dy, d.y_stride)
+    f32, shape, dev = _torch.float32, (v.shape[0], *matrix), v.device
+    dq, dk, dv = (_torch.empty(t.shape, dtype=v.dtype, device=dev) for t in (q, k, v))
+    ddecay, drate = (_torch.empty(t.shape, dtype=f32, device=dev) for t in (decay, rate))
+    ds0 = _torch.empty(shape, dtype=f32, device=dev)
+    ref = _on(d, v)
+    keptp = _packed(kept, v, "kept", (_size(_lib.ms_gated_delta_kept, ref),), f32)
+    lp, dlp = _packed(lengths, v, "lengths", v.shape[:1], _torch.int32), _packed(dlast, v, "dlast", shape, f32)
+    hold, ws, n = _scratch(v, _size(_lib.ms_gated_delta_workspace, ref, 1))
+    _check(_lib.ms_gated_delta_grad(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), decay.data_ptr(), rate.data_ptr(), keptp,
+                                    lp, dy.data_ptr(), dlp, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ddecay.data_ptr(),
+                                    drate.data_ptr(), ds0.data_ptr(), ws, n))
+    return dq, dk, dv, ddecay, drate, ds0
+
+
+def gated_delta_step(q, k, v, decay, rate, state, slots=None, scale=1.0, out=None):
+    """One step for the sequences being served (ms_gated_delta_step): row i of q, k [rows, key_heads, keys], v
+    [rows, heads, values], decay and rate [rows, heads] advances state[slots[i]] (float32 [slots, heads, keys, values],
+    in place; row i's own slot without `slots`, int32) and returns what is read there, [rows, heads, values] in v's
+    type; a slot outside the cache marks an idle row, whose result is zeros."""
+    d = GatedDeltaStepDesc(scale=scale)
+    q, k, v, decay, rate, matrix = _delta_inputs(d, 3, q, k, v, decay, rate)
+    _like(state, v, "state", (state.shape[0], *matrix), _torch.float32)
+    d.rows, d.n_slots = v.shape[0], state.shape[0]
+    if not state.is_contiguous():
+        if not state[:1].is_contiguous():
+            raise ValueError("state's matrices must be contiguous")
+        d.state_stride = state.stride(0)
+    written = (state,) if out is None else (state, out)
+    if out is None:
+        out = _torch.empty(v.shape, dtype=v.dtype, device=v.device)
+    else:
+        _like(out, v, "out", v.shape, v.dtype)
+        if _walked(out, d.y_stride) is not out:
+            raise ValueError("out's heads must be contiguous")
+    slotp = _packed(slots, v, "slots", v.shape[:1], _torch.int32)
+    _written(*written)
+    _check(_lib.ms_gated_delta_step(_on(d, v), q.data_ptr(), k.data_ptr(), v.data_ptr(), decay.data_ptr(), rate.data_ptr(),
+                                    state.data_ptr(), slotp, out.data_ptr()))
     return out
 
 
