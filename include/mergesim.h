@@ -511,7 +511,8 @@ ms_status ms_sim_set_train_param(ms_sim* sim, int32_t which, int32_t id, int32_t
 /* Operators for models that read and learn from tokens, called on arrays of
  * the caller's own (none is a part of the paper's method): a table of token
  * vectors, a lowpass synapse whose time constant the input sets, orthogonalised
- * updates of weight matrices, and a memory by key that learns by the delta rule.  Their outputs are laid out as
+ * updates of weight matrices, a memory by key that learns by the delta rule, and a
+ * norm within groups of channels.  Their outputs are laid out as
  * feeds ([batch][steps][dim]).
  *
  * Every pointer but the descriptors is device memory on `device`; the calls
@@ -723,6 +724,44 @@ typedef struct {
 ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* desc, const void* q, const void* k,
                               const void* v, const float* decay, const float* rate, float* state,
                               const int32_t* slots, void* y);
+
+/* Group norm with an activation, channels last.  Over the positions of a batch row
+ * (its first lengths[row]; NULL = all) and the channels of a group:
+ *     h = (x - mean) / sqrt(variance + eps);  y = act(h weight + bias)
+ * with the variance of all n values (divided by n).  One position is a norm of every
+ * row's groups by themselves, as of heads; one group is a norm over all channels.
+ *   x, y         [batch][positions][channels], dtype; y is 0 past a row's length
+ *   weight, bias [channels] float32, or NULL for ones, zeros
+ *   lengths      int32 [batch], clamped to [0, positions]
+ *   kept         float32 [batch][groups][2]: mean and 1 / sqrt(variance + eps), from
+ *                which the gradient starts; NULL if none is wanted
+ * The gradient, from dL/dy: dx, packed (0 past a row's length); dweight and dbias
+ * float32 [channels], sums over all rows (also where weight or bias is NULL).  x,
+ * weight, bias, lengths and kept are those of the forward call.  What lies past a row's
+ * length is not read. */
+#define MS_ACT_NONE 0
+#define MS_ACT_RELU 1
+#define MS_ACT_SILU 2
+
+typedef struct {
+  int64_t batch, positions;     /* >= 0 and < 2^31 */
+  int64_t channels, groups;     /* channels in [1, 2^24), a multiple of groups; batch * groups < 2^40 */
+  int64_t x_stride[2];          /* between batch rows, between positions; 0, 0 = packed */
+  int64_t y_stride[2];          /* of y, or of dy in the gradient */
+  double eps;                   /* >= 0; not used by the gradient */
+  int32_t activation;           /* MS_ACT_* */
+  int32_t dtype;                /* MS_DTYPE_*: of x, y and their gradients */
+  int32_t device;
+  void* stream;
+} ms_group_norm_desc;
+
+/* grad != 0: for ms_group_norm_grad, else for ms_group_norm. */
+ms_status ms_group_norm_workspace(const ms_group_norm_desc* desc, int32_t grad, int64_t* bytes_out);
+ms_status ms_group_norm(const ms_group_norm_desc* desc, const void* x, const float* weight, const float* bias,
+                        const int32_t* lengths, void* y, float* kept, void* workspace, int64_t workspace_bytes);
+ms_status ms_group_norm_grad(const ms_group_norm_desc* desc, const void* x, const float* weight,
+                             const float* bias, const int32_t* lengths, const float* kept, const void* dy,
+                             void* dx, float* dweight, float* dbias, void* workspace, int64_t workspace_bytes);
 
 const char* ms_last_error(void);
 

@@ -1,0 +1,472 @@
+// Group norm with an activation, channels last, and its gradient:
+//     h = (x - mean) rstd,  z = h weight + bias,  y = act(z)
+// mean and rstd = 1 / sqrt(variance + eps) over the positions of a batch row and the
+// channels of a group.  With d = dy act'(z) and sums over the same n values
+//     dx = rstd (d weight - sum(d weight) / n - h sum(d weight h) / n)
+//     dweight = sum d h,  dbias = sum d  over all rows and positions.
+//
+// Memory bounds both.  A group of few values (one position: a head's read-out) stays
+// in the registers of a team of threads, read once: k_norm_team, k_norm_team_grad.
+// Others are read twice: sums over runs of positions, a thread to one channel word,
+// their join, and the results.  The variance is the sum of squares about a mean that
+// is known (of a team's values) or about the mean of a thread's few values, joined by
+// Chan's formula in 64 bits, so a large mean costs no digits.  Nothing is added by
+// atomics; every sum has one order.
+#pragma once
+
+#include "kernels_words.hpp"
+
+struct NormArgs {
+  int64_t batch, positions;
+  int32_t groups, width;         // channels of a group
+  int64_t xb, xt, yb, yt;        // strides of x, and of y or dy: between batch rows, positions
+  const int32_t* lengths;
+  const float *weight, *bias;    // NULL: ones, zeros
+  float* kept;                   // [batch][groups][2]: mean, rstd; NULL: not kept
+  float eps;
+  int32_t act;
+  int32_t nw;                    // words of a group's channels
+  // teams: threads of one, and batch rows side by side in the gradient
+  int32_t team, lanes;
+  // runs: of positions, side by side, and channel words to a workgroup's row
+  int32_t runs, run, wide;
+};
+
+enum { kActNone, kActRelu, kActSilu };
+
+__device__ __forceinline__ float gate_of_silu(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+
+__device__ __forceinline__ float activated(float z, int act) {
+  if (act == kActRelu) return z > 0.0f ? z : z != z ? z : 0.0f;
+  if (act == kActSilu) return z * gate_of_silu(z);
+  return z;
+}
+
+// dy act'(z)
+__device__ __forceinline__ float through_act(float dy, float z, int act) {
+  if (act == kActRelu) return z > 0.0f ? dy : 0.0f;
+  if (act == kActSilu) {
+    const float g = gate_of_silu(z);
+    return dy * g * fmaf(z, 1.0f - g, 1.0f);
+  }
+  return dy;
+}
+
+__device__ __forceinline__ int64_t norm_length(const NormArgs& p, int64_t b) {
+  if (!p.lengths) return p.positions;
+  return min(max((int64_t)p.lengths[b], (int64_t)0), p.positions);
+}
+
+template <int V>
+__device__ __forceinline__ Words<float, V> norm_param(const float* w, int64_t c, float other) {
+  if (w) return *(const Words<float, V>*)(w + c);
+  Words<float, V> r;
+#pragma unroll
+  for (int e = 0; e < V; ++e) r.v[e] = other;
+  return r;
+}
+
+// Sums over a team: lanes of a wavefront (a power of two), or the 4 wavefronts of a
+// workgroup.
+template <bool WIDE>
+__device__ __forceinline__ float team_sum(float s, int team, float* red) {
+  for (int o = 1; o < (WIDE ? 64 : team); o *= 2) s += __shfl_xor(s, o, 64);
+  if constexpr (WIDE) {
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = s;
+    __syncthreads();
+    s = (red[0] + red[1]) + (red[2] + red[3]);
+  }
+  return s;
+}
+
+constexpr int kTeamWords = 4;   // words of a thread, at most
+
+// A group's values in a team's registers.
+template <class T, int V, bool WIDE>
+__global__ void __launch_bounds__(256) k_norm_team(NormArgs p, const T* x, T* y) {
+  __shared__ float red[4];
+  const int team = WIDE ? 256 : p.team, me = threadIdx.x % team, teams = 256 / team;
+  const int64_t all = p.batch * p.groups, words = p.positions * p.nw;
+  for (int64_t u0 = (int64_t)blockIdx.x * teams; u0 < all; u0 += (int64_t)gridDim.x * teams) {
+    const bool live = u0 + threadIdx.x / team < all;
+    const int64_t u = live ? u0 + threadIdx.x / team : all - 1, b = u / p.groups;
+    const int g = (int)(u % p.groups);
+    const int64_t len = norm_length(p, b);
+    const T* xp = x + b * p.xb;
+    T* yp = y + b * p.yb;
+    Words<T, V> v[kTeamWords];
+    float s = 0.0f;
+#pragma unroll
+    for (int r = 0; r < kTeamWords; ++r) {
+      const int64_t j = me + (int64_t)r * team, t = j / p.nw;
+      if (j < words && t < len) v[r] = *(const Words<T, V>*)(xp + t * p.xt + (int64_t)g * p.width + j % p.nw * V);
+    }
+#pragma unroll
+    for (int r = 0; r < kTeamWords; ++r)
+      if (me + (int64_t)r * team < len * p.nw)
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += as_f32(v[r].v[e]);
+    const float n = (float)(max(len, (int64_t)1) * p.width);
+    const float mean = team_sum<WIDE>(s, team, red) / n;
+    s = 0.0f;
+#pragma unroll
+    for (int r = 0; r < kTeamWords; ++r)
+      if (me + (int64_t)r * team < len * p.nw)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float d = as_f32(v[r].v[e]) - mean;
+          s = fmaf(d, d, s);
+        }
+    const float rstd = 1.0f / sqrtf(team_sum<WIDE>(s, team, red) / n + p.eps);
+    if (!live) continue;
+    if (p.kept && me == 0) p.kept[2 * u] = mean, p.kept[2 * u + 1] = rstd;
+#pragma unroll
+    for (int r = 0; r < kTeamWords; ++r) {
+      const int64_t j = me + (int64_t)r * team, t = j / p.nw, c = (int64_t)g * p.width + j % p.nw * V;
+      if (j >= words) continue;
+      const Words<float, V> w = norm_param<V>(p.weight, c, 1.0f), a = norm_param<V>(p.bias, c, 0.0f);
+      Words<T, V> o;
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        o.v[e] = t < len ? (T)activated(fmaf((as_f32(v[r].v[e]) - mean) * rstd, w.v[e], a.v[e]), p.act) : (T)0.0f;
+      *(Words<T, V>*)(yp + t * p.yt + c) = o;
+    }
+  }
+}
+
+// The gradient of one position's groups.  A team keeps its group and goes through
+// every p.lanes-th batch row, with its part of dweight and dbias in registers:
+// parts [lanes][2][channels].
+template <class T, int V, bool WIDE>
+__global__ void __launch_bounds__(256)
+    k_norm_team_grad(NormArgs p, const T* x, const T* dy, T* dx, float* parts) {
+  __shared__ float red[4];
+  const int team = WIDE ? 256 : p.team, me = threadIdx.x % team, teams = 256 / team;
+  const int64_t slot = (int64_t)blockIdx.x * teams + threadIdx.x / team;
+  const bool mine = slot < (int64_t)p.lanes * p.groups;
+  const int g = (int)(slot % p.groups);
+  const int64_t lane = slot / p.groups, channels = (int64_t)p.groups * p.width;
+  Words<float, V> w[kTeamWords], a[kTeamWords], dw[kTeamWords], db[kTeamWords];
+#pragma unroll
+  for (int r = 0; r < kTeamWords; ++r) {
+    const int j = me + r * team;
+    const int64_t c = (int64_t)g * p.width + (j < p.nw ? j : 0) * V;
+    w[r] = norm_param<V>(p.weight, c, 1.0f), a[r] = norm_param<V>(p.bias, c, 0.0f);
+#pragma unroll
+    for (int e = 0; e < V; ++e) dw[r].v[e] = db[r].v[e] = 0.0f;
+  }
+  const float n = 1.0f / (float)p.width;
+  // a team of several wavefronts is a workgroup, and goes or stays as one
+  for (int64_t b = mine ? lane : p.batch; b < p.batch; b += p.lanes) {
+    const bool live = norm_length(p, b) > 0;
+    const float mean = p.kept[2 * (b * p.groups + g)], rstd = p.kept[2 * (b * p.groups + g) + 1];
+    Words<T, V> xv[kTeamWords], dv[kTeamWords];
+#pragma unroll
+    for (int r = 0; r < kTeamWords; ++r) {
+      const int j = me + r * team;
+      const int64_t c = (int64_t)g * p.width + j * V;
+      if (j < p.nw && live) {
+        xv[r] = *(const Words<T, V>*)(x + b * p.xb + c);
+        dv[r] = *(const Words<T, V>*)(dy + b * p.yb + c);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) xv[r].v[e] = dv[r].v[e] = (T)0.0f;
+      }
+    }
+    float s1 = 0.0f, s2 = 0.0f, h[kTeamWords][V], d[kTeamWords][V];
+#pragma unroll
+    for (int r = 0; r < kTeamWords; ++r)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        h[r][e] = (as_f32(xv[r].v[e]) - mean) * rstd;
+        const float t = through_act(as_f32(dv[r].v[e]), fmaf(h[r][e], w[r].v[e], a[r].v[e]), p.act);
+        if (me + r * team < p.nw && live) dw[r].v[e] = fmaf(t, h[r][e], dw[r].v[e]), db[r].v[e] += t;
+        d[r][e] = me + r * team < p.nw ? t * w[r].v[e] : 0.0f;
+        s1 += d[r][e];
+        s2 = fmaf(d[r][e], h[r][e], s2);
+      }
+    s1 = team_sum<WIDE>(s1, team, red) * n;
+    s2 = team_sum<WIDE>(s2, team, red) * n;
+#pragma unroll
+    for (int r = 0; r < kTeamWords; ++r) {
+      const int j = me + r * team;
+      if (j >= p.nw) continue;
+      Words<T, V> o;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o.v[e] = live ? (T)(rstd * (d[r][e] - s1 - h[r][e] * s2)) : (T)0.0f;
+      *(Words<T, V>*)(dx + b * channels + (int64_t)g * p.width + j * V) = o;
+    }
+  }
+  if (mine)
+#pragma unroll
+    for (int r = 0; r < kTeamWords; ++r) {
+      const int j = me + r * team;
+      if (j >= p.nw) continue;
+      float* o = parts + lane * 2 * channels + (int64_t)g * p.width + j * V;
+      *(Words<float, V>*)o = dw[r];
+      *(Words<float, V>*)(o + channels) = db[r];
+    }
+}
+
+// Column sums of parts [rows][2 channels] in order, one thread a column, 8 runs of rows.
+__global__ void __launch_bounds__(256) k_norm_columns(const float* parts, int64_t rows, int64_t channels, float* dweight,
+                                                      float* dbias) {
+  __shared__ float red[8][32];
+  const int c = threadIdx.x % 32, k = threadIdx.x / 32;
+  const int64_t col = (int64_t)blockIdx.x * 32 + c;
+  float s = 0.0f;
+  if (col < 2 * channels)
+    for (int64_t r = k; r < rows; r += 8) s += parts[r * 2 * channels + col];
+  red[k][c] = s;
+  __syncthreads();
+  if (k || col >= 2 * channels) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) s += red[i][c];
+  (col < channels ? dweight[col] : dbias[col - channels]) = s;
+}
+
+// ------------------------------------------------------------ many positions
+// Where a workgroup works: batch row, run of positions, block of channel words; a
+// thread's word and its first position.
+struct NormPlace {
+  int64_t b, len, t, end, word;
+  int step;
+  bool live;
+};
+
+template <int V>
+__device__ __forceinline__ NormPlace norm_place(const NormArgs& p, int64_t u) {
+  const int64_t words = (int64_t)p.groups * p.nw, blocks = (words + p.wide - 1) / p.wide;
+  NormPlace q;
+  q.b = u / blocks / p.runs;
+  q.len = norm_length(p, q.b);
+  const int64_t run = u / blocks % p.runs;
+  q.step = 256 / p.wide;
+  q.t = run * p.run + threadIdx.x / p.wide;
+  q.end = min((run + 1) * p.run, p.positions);
+  q.word = u % blocks * p.wide + threadIdx.x % p.wide;
+  q.live = q.word < words;
+  return q;
+}
+
+__device__ __forceinline__ int64_t norm_blocks(const NormArgs& p) {
+  return p.batch * p.runs * (((int64_t)p.groups * p.nw + p.wide - 1) / p.wide);
+}
+
+// Of every run and word: mean and sum of squares about it, parts [batch][runs][words][2].
+// A thread takes 8 positions at a time.
+template <class T, int V>
+__global__ void __launch_bounds__(256) k_norm_sums(NormArgs p, const T* x, float* parts) {
+  __shared__ float red[256][3];
+  const int64_t all = norm_blocks(p), words = (int64_t)p.groups * p.nw;
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const NormPlace q = norm_place<V>(p, u);
+    const int64_t end = min(q.end, q.len);
+    const T* xp = x + q.b * p.xb + (q.live ? q.word : 0) * V;
+    float n = 0.0f, mean = 0.0f, square = 0.0f;
+    for (int64_t t = q.t; q.live && t < end; t += 8 * q.step) {
+      Words<T, V> v[8];
+      const int have = (int)min((int64_t)8, (end - t + q.step - 1) / q.step);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) v[r] = *(const Words<T, V>*)(xp + min(t + r * q.step, end - 1) * p.xt);
+      float s = 0.0f, m2 = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += r < have ? as_f32(v[r].v[e]) : 0.0f;
+      const float here = (float)(have * V), m = s / here;
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float d = r < have ? as_f32(v[r].v[e]) - m : 0.0f;
+          m2 = fmaf(d, d, m2);
+        }
+      const float d = m - mean, both = n + here;
+      mean = fmaf(d, here / both, mean);
+      square += m2 + d * d * (n * here / both);
+      n = both;
+    }
+    red[threadIdx.x][0] = n, red[threadIdx.x][1] = mean, red[threadIdx.x][2] = square;
+    __syncthreads();
+    if (threadIdx.x < p.wide && q.live) {
+      for (int r = 1; r < q.step; ++r) {
+        const float *o = red[threadIdx.x + r * p.wide], here = o[0], both = n + here;
+        if (here == 0.0f) continue;
+        const float d = o[1] - mean;
+        mean = fmaf(d, here / both, mean);
+        square += o[2] + d * d * (n * here / both);
+        n = both;
+      }
+      float* o = parts + ((q.b * p.runs + u / ((words + p.wide - 1) / p.wide) % p.runs) * words + q.word) * 2;
+      o[0] = mean, o[1] = square;
+    }
+    __syncthreads();
+  }
+}
+
+__device__ __forceinline__ double norm_sum64(double s, double* red) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = s;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// mean and rstd of every batch row's groups from the runs': kept.
+template <int V>
+__global__ void __launch_bounds__(256) k_norm_join(NormArgs p, const float* parts) {
+  __shared__ double red[4];
+  const int64_t words = (int64_t)p.groups * p.nw, all = p.batch * p.groups;
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const int64_t b = u / p.groups, len = norm_length(p, b), first = u % p.groups * p.nw;
+    const int64_t runs = (len + p.run - 1) / p.run, n = runs * p.nw;
+    const auto count = [&](int64_t run) { return (double)(min((int64_t)p.run, len - run * p.run) * V); };
+    const float* at = parts + (b * p.runs * words + first) * 2;
+    double s = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += 256) s += count(i / p.nw) * at[(i / p.nw * words + i % p.nw) * 2];
+    const double total = (double)max(len, (int64_t)1) * p.width, mean = norm_sum64(s, red) / total;
+    s = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += 256) {
+      const float* o = at + (i / p.nw * words + i % p.nw) * 2;
+      const double d = o[0] - mean;
+      s += o[1] + count(i / p.nw) * d * d;
+    }
+    const double square = norm_sum64(s, red);
+    if (threadIdx.x == 0) p.kept[2 * u] = (float)mean, p.kept[2 * u + 1] = (float)(1.0 / sqrt(square / total + p.eps));
+  }
+}
+
+template <class T, int V>
+__global__ void __launch_bounds__(256) k_norm_apply(NormArgs p, const T* x, T* y) {
+  const int64_t all = norm_blocks(p);
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const NormPlace q = norm_place<V>(p, u);
+    if (!q.live) continue;
+    const int64_t c = q.word * V, g = q.b * p.groups + q.word / p.nw;
+    const float mean = p.kept[2 * g], rstd = p.kept[2 * g + 1];
+    const Words<float, V> w = norm_param<V>(p.weight, c, 1.0f), a = norm_param<V>(p.bias, c, 0.0f);
+    for (int64_t t = q.t; t < q.end; t += 4 * q.step) {
+      Words<T, V> v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (t + r * q.step < min(q.end, q.len)) v[r] = *(const Words<T, V>*)(x + q.b * p.xb + (t + r * q.step) * p.xt + c);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (t + r * q.step >= q.end) continue;
+        Words<T, V> o;
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          o.v[e] = t + r * q.step < q.len ? (T)activated(fmaf((as_f32(v[r].v[e]) - mean) * rstd, w.v[e], a.v[e]), p.act)
+                                          : (T)0.0f;
+        put_once(y + q.b * p.yb + (t + r * q.step) * p.yt + c, o);
+      }
+    }
+  }
+}
+
+// Of every run and channel: sums of d h and of d, parts [batch][runs][2][channels].
+template <class T, int V>
+__global__ void __launch_bounds__(256) k_norm_grad_sums(NormArgs p, const T* x, const T* dy, float* parts) {
+  __shared__ float red[256][2 * V + 1];
+  const int64_t all = norm_blocks(p), words = (int64_t)p.groups * p.nw, channels = words * V;
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const NormPlace q = norm_place<V>(p, u);
+    const int64_t end = min(q.end, q.len), c = (q.live ? q.word : 0) * V;
+    const int64_t g = q.b * p.groups + (q.live ? q.word : 0) / p.nw;
+    const float mean = p.kept[2 * g], rstd = p.kept[2 * g + 1];
+    const Words<float, V> w = norm_param<V>(p.weight, c, 1.0f), a = norm_param<V>(p.bias, c, 0.0f);
+    float dw[V], db[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) dw[e] = db[e] = 0.0f;
+    for (int64_t t = q.t; q.live && t < end; t += 4 * q.step) {
+      Words<T, V> xv[4], dv[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t at = min(t + r * q.step, end - 1);
+        xv[r] = *(const Words<T, V>*)(x + q.b * p.xb + at * p.xt + c);
+        dv[r] = *(const Words<T, V>*)(dy + q.b * p.yb + at * p.yt + c);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (t + r * q.step < end)
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float h = (as_f32(xv[r].v[e]) - mean) * rstd;
+            const float d = through_act(as_f32(dv[r].v[e]), fmaf(h, w.v[e], a.v[e]), p.act);
+            dw[e] = fmaf(d, h, dw[e]), db[e] += d;
+          }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) red[threadIdx.x][e] = dw[e], red[threadIdx.x][V + e] = db[e];
+    __syncthreads();
+    if (threadIdx.x < p.wide && q.live) {
+      for (int r = 1; r < q.step; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dw[e] += red[threadIdx.x + r * p.wide][e];
+          db[e] += red[threadIdx.x + r * p.wide][V + e];
+        }
+      float* o = parts + (q.b * p.runs + u / ((words + p.wide - 1) / p.wide) % p.runs) * 2 * channels + c;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] = dw[e], o[channels + e] = db[e];
+    }
+    __syncthreads();
+  }
+}
+
+// sum(d weight h) / n and sum(d weight) / n of every batch row's groups: sums.
+__global__ void __launch_bounds__(256) k_norm_grad_join(NormArgs p, const float* parts, float* sums) {
+  __shared__ double red[4];
+  const int64_t channels = (int64_t)p.groups * p.width, all = p.batch * p.groups;
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const int64_t b = u / p.groups, len = norm_length(p, b), first = u % p.groups * p.width;
+    const float* at = parts + b * p.runs * 2 * channels + first;
+    double s1 = 0.0, s2 = 0.0;
+    const int64_t n = (len + p.run - 1) / p.run * p.width;
+    for (int64_t i = threadIdx.x; i < n; i += 256) {
+      const int64_t o = i / p.width * 2 * channels + i % p.width;
+      const float w = p.weight ? p.weight[first + i % p.width] : 1.0f;
+      s1 += (double)w * at[o], s2 += (double)w * at[o + channels];
+    }
+    const double total = (double)max(len, (int64_t)1) * p.width;
+    s1 = norm_sum64(s1, red), s2 = norm_sum64(s2, red);
+    if (threadIdx.x == 0) sums[2 * u] = (float)(s1 / total), sums[2 * u + 1] = (float)(s2 / total);
+  }
+}
+
+template <class T, int V>
+__global__ void __launch_bounds__(256)
+    k_norm_grad_apply(NormArgs p, const T* x, const T* dy, const float* sums, T* dx) {
+  const int64_t all = norm_blocks(p), channels = (int64_t)p.groups * p.width;
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const NormPlace q = norm_place<V>(p, u);
+    if (!q.live) continue;
+    const int64_t c = q.word * V, g = q.b * p.groups + q.word / p.nw;
+    const float mean = p.kept[2 * g], rstd = p.kept[2 * g + 1], sh = sums[2 * g], sd = sums[2 * g + 1];
+    const Words<float, V> w = norm_param<V>(p.weight, c, 1.0f), a = norm_param<V>(p.bias, c, 0.0f);
+    for (int64_t t = q.t; t < q.end; t += 4 * q.step) {
+      Words<T, V> xv[4], dv[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (t + r * q.step < min(q.end, q.len)) {
+          xv[r] = *(const Words<T, V>*)(x + q.b * p.xb + (t + r * q.step) * p.xt + c);
+          dv[r] = *(const Words<T, V>*)(dy + q.b * p.yb + (t + r * q.step) * p.yt + c);
+        }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (t + r * q.step >= q.end) continue;
+        Words<T, V> o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float h = (as_f32(xv[r].v[e]) - mean) * rstd;
+          const float d = through_act(as_f32(dv[r].v[e]), fmaf(h, w.v[e], a.v[e]), p.act) * w.v[e];
+          o.v[e] = t + r * q.step < q.len ? (T)(rstd * (d - sd - h * sh)) : (T)0.0f;
+        }
+        put_once(dx + (q.b * p.positions + t + r * q.step) * channels + c, o);
+      }
+    }
+  }
+}

@@ -1,5 +1,6 @@
 // The operators of keyed memories in the C ABI: argument checks, workspace layouts
-// and launches.  The kernels are in kernels_delta.hpp and kernels_delta_grad.hpp.
+// and launches.  The kernels are in kernels_delta.hpp, kernels_delta_grad.hpp and
+// kernels_norm.hpp.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -9,6 +10,7 @@
 #include "host.hpp"
 #include "kernels_delta.hpp"
 #include "kernels_delta_grad.hpp"
+#include "kernels_norm.hpp"
 #include "operators_host.hpp"
 #include "operators_rules.hpp"
 
@@ -46,7 +48,7 @@ Walk walk_of(const int64_t* s, int64_t steps, int64_t heads, int64_t dim) {
   Walk w{s[0], s[1], s[2]};
   if (s[0] == 0 && s[1] == 0 && s[2] == 0) w = {steps * heads * dim, heads * dim, dim};
   need(w.b >= 0 && w.t >= 0 && w.h >= 0 && w.b < kMaxStride && w.t < kMaxStride && w.h < kMaxStride,
-       "strides must not be negative");
+       "strides must be in [0, 2^40)");
   return w;
 }
 
@@ -138,6 +140,89 @@ DeltaWork delta_work(const Delta& p, bool grad, void* ws) {
 bool words(const Walk& w, const void* p) { return w.b % 8 == 0 && w.t % 8 == 0 && w.h % 8 == 0 && (uintptr_t)p % 16 == 0; }
 
 dim3 scan_grid(const Delta& p) { return dim3((unsigned)(up(p.a.batch * p.a.heads, 8) * p.blocks)); }
+
+// -------------------------------------------------------------------- norm
+struct Norm {
+  NormArgs a;
+  NormShape shape;
+  int64_t channels, v;
+};
+
+static_assert(kNormWords == kTeamWords, "rule and kernels");
+static_assert(MS_ACT_NONE == kActNone && MS_ACT_RELU == kActRelu && MS_ACT_SILU == kActSilu, "activations");
+
+// v: values of a word, as sizes, strides and pointers allow (1 for workspaces, which hold for any).
+Norm check_norm(const ms_group_norm_desc* d) {
+  need(d != nullptr, "NULL descriptor");
+  need(d->batch >= 0 && d->batch < ((int64_t)1 << 31), "batch must be in [0, 2^31)");
+  need(d->positions >= 0 && d->positions < ((int64_t)1 << 31), "positions must be in [0, 2^31)");
+  need(d->groups >= 1 && d->channels >= 1 && d->channels < (1 << 24) && d->channels % d->groups == 0,
+       "channels must be in [1, 2^24), a multiple of groups");
+  need_dtype(d->dtype);
+  need(d->activation == MS_ACT_NONE || d->activation == MS_ACT_RELU || d->activation == MS_ACT_SILU, "unknown activation");
+  need(d->eps >= 0 && std::isfinite((float)d->eps), "eps must be finite in 32 bits and not negative");
+  need(d->batch * d->groups < ((int64_t)1 << 40) && d->batch * d->channels < ((int64_t)1 << 44), "batch * channels is too large");
+  Norm p{};
+  NormArgs& a = p.a;
+  p.channels = d->channels;
+  a.batch = d->batch, a.positions = d->positions;
+  a.groups = (int32_t)d->groups, a.width = (int32_t)(d->channels / d->groups);
+  const auto pair = [&](const int64_t* s, int64_t& b, int64_t& t) {
+    const bool packed = s[0] == 0 && s[1] == 0;
+    b = packed ? d->positions * d->channels : s[0], t = packed ? d->channels : s[1];
+    need(b >= 0 && t >= 0 && b < kMaxStride && t < kMaxStride, "strides must be in [0, 2^40)");
+  };
+  pair(d->x_stride, a.xb, a.xt);
+  pair(d->y_stride, a.yb, a.yt);
+  a.eps = (float)d->eps, a.act = d->activation;
+  return p;
+}
+
+void norm_choose(Norm& p, int64_t v, bool grad) {
+  NormArgs& a = p.a;
+  p.v = v;
+  a.nw = (int32_t)(a.width / v);
+  p.shape = norm_shape(a.batch, a.positions, a.groups, a.nw, grad);
+  a.team = p.shape.team, a.lanes = p.shape.lanes;
+  a.runs = p.shape.runs, a.run = p.shape.run, a.wide = p.shape.wide;
+}
+
+// Scratch memory: parts, then mean and rstd where the caller keeps none (or the
+// groups' sums of the gradient).  Without pointers: the most that any word takes.
+struct NormWork {
+  float *parts, *sums;
+  int64_t bytes;
+};
+
+NormWork norm_work(const Norm& p, bool grad, void* ws) {
+  Carve c{(char*)ws};
+  NormWork w{};
+  const NormArgs& a = p.a;
+  if (!grad && !a.team) {
+    w.parts = c.take<float>(a.batch * a.runs * a.groups * a.nw * 2);
+    w.sums = c.take<float>(a.batch * a.groups * 2);
+  } else if (grad) {
+    w.parts = c.take<float>((a.team ? (int64_t)a.lanes : a.batch * a.runs) * 2 * p.channels);
+    if (!a.team) w.sums = c.take<float>(a.batch * a.groups * 2);
+  }
+  w.bytes = c.used;
+  return w;
+}
+
+int64_t norm_most(Norm p, int32_t dtype, bool grad) {
+  int64_t most = 0;
+  for (int64_t v = 16 / (int64_t)size_of(dtype); v >= 1; v /= 2) {
+    if (p.a.width % v != 0) continue;
+    norm_choose(p, v, grad);
+    most = std::max(most, norm_work(p, grad, nullptr).bytes);
+  }
+  return most;
+}
+
+unsigned norm_grid(const Norm& p) {
+  const int64_t blocks = (p.a.groups * (int64_t)p.a.nw + p.a.wide - 1) / p.a.wide;
+  return (unsigned)std::min(p.a.batch * p.a.runs * blocks, kMaxBlocks);
+}
 
 }  // namespace
 
@@ -269,7 +354,7 @@ ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* d, const void* q, 
     const auto pair = [&](const int64_t* s, int64_t heads, int64_t dim, int64_t* to) {
       const bool packed = s[0] == 0 && s[1] == 0;
       to[0] = packed ? heads * dim : s[0], to[1] = packed ? dim : s[1];
-      need(to[0] >= 0 && to[1] >= 0 && to[0] < kMaxStride && to[1] < kMaxStride, "strides must not be negative");
+      need(to[0] >= 0 && to[1] >= 0 && to[0] < kMaxStride && to[1] < kMaxStride, "strides must be in [0, 2^40)");
     };
     pair(d->q_stride, d->key_heads, d->keys, a.q);
     pair(d->k_stride, d->key_heads, d->keys, a.k);
@@ -305,6 +390,103 @@ ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* d, const void* q, 
       });
     });
     HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_group_norm_workspace(const ms_group_norm_desc* d, int32_t grad, int64_t* bytes_out) {
+  return guarded([&] {
+    const Norm p = check_norm(d);
+    need(bytes_out != nullptr, "NULL output");
+    *bytes_out = norm_most(p, d->dtype, grad != 0);
+  });
+}
+
+ms_status ms_group_norm(const ms_group_norm_desc* d, const void* x, const float* weight, const float* bias,
+                        const int32_t* lengths, void* y, float* kept, void* workspace, int64_t workspace_bytes) {
+  return guarded([&] {
+    Norm p = check_norm(d);
+    NormArgs& a = p.a;
+    if (a.batch == 0 || a.positions == 0) return;
+    const size_t es = size_of(d->dtype);
+    need(walk_apart({0, a.yb, a.yt}, 1, a.batch, a.positions, p.channels), "rows or positions of y overlap");
+    need(x && y, "NULL array");
+    for (const void* q : {x, (const void*)y}) need_aligned(q, es, "x or y");
+    for (const void* q : {(const void*)weight, (const void*)bias, (const void*)lengths, (const void*)kept})
+      need_aligned(q, 4, "weight, bias, lengths or kept");
+    need_workspace(workspace, workspace_bytes, norm_most(p, d->dtype, false));
+    norm_choose(p, Wide(es).of(a.width).of(a.xb).of(a.xt).of(a.yb).of(a.yt).at(x, es).at(y, es).at(weight, 4).at(bias, 4).v,
+                false);
+    const NormWork w = norm_work(p, false, workspace);
+    a.weight = weight, a.bias = bias, a.lengths = lengths, a.kept = kept;
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    with_type<8, 4>(d->dtype, p.v, [&](auto zero, auto width) {
+      using T = decltype(zero);
+      constexpr int V = decltype(width)::value;
+      if (a.team) {
+        const int64_t blocks = (a.batch * a.groups * a.team + 255) / 256;
+        with_flag(a.team > 64, [&](auto many) {
+          hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_team<T, V, decltype(many)::value>),
+                             dim3((unsigned)std::min(blocks, kMaxBlocks)), dim3(256), 0, st, a, (const T*)x, (T*)y);
+        });
+        return;
+      }
+      if (!kept) a.kept = w.sums;
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_sums<T, V>), dim3(norm_grid(p)), dim3(256), 0, st, a, (const T*)x, w.parts);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_join<V>), dim3((unsigned)std::min(a.batch * a.groups, kMaxBlocks)), dim3(256),
+                         0, st, a, (const float*)w.parts);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_apply<T, V>), dim3(norm_grid(p)), dim3(256), 0, st, a, (const T*)x, (T*)y);
+    });
+    HIPCHECK(hipGetLastError());
+  });
+}
+
+ms_status ms_group_norm_grad(const ms_group_norm_desc* d, const void* x, const float* weight, const float* bias,
+                             const int32_t* lengths, const float* kept, const void* dy, void* dx, float* dweight,
+                             float* dbias, void* workspace, int64_t workspace_bytes) {
+  return guarded([&] {
+    Norm p = check_norm(d);
+    NormArgs& a = p.a;
+    const bool none = a.batch == 0 || a.positions == 0;
+    const size_t es = size_of(d->dtype);
+    need(none || (x && kept && dy && dx), "NULL array");
+    need(dweight && dbias, "NULL array");
+    for (const void* q : {x, dy, (const void*)dx}) need_aligned(q, es, "x, dy or dx");
+    for (const void* q : {(const void*)weight, (const void*)bias, (const void*)lengths, (const void*)kept, (const void*)dweight,
+                          (const void*)dbias})
+      need_aligned(q, 4, "weight, bias, lengths, kept, dweight or dbias");
+    if (!none) need_workspace(workspace, workspace_bytes, norm_most(p, d->dtype, true));
+    DeviceGuard dg(d->device);
+    const hipStream_t st = (hipStream_t)d->stream;
+    const auto columns = [&](const float* parts, int64_t rows) {
+      hipLaunchKernelGGL(k_norm_columns, dim3((unsigned)((2 * p.channels + 31) / 32)), dim3(256), 0, st, parts, rows,
+                         p.channels, dweight, dbias);
+      HIPCHECK(hipGetLastError());
+    };
+    if (none) return columns(nullptr, 0);
+    norm_choose(p, Wide(es).of(a.width).of(a.xb).of(a.xt).of(a.yb).of(a.yt).at(x, es).at(dy, es).at(dx, es).at(weight, 4)
+                       .at(bias, 4).v, true);
+    const NormWork w = norm_work(p, true, workspace);
+    a.weight = weight, a.bias = bias, a.lengths = lengths, a.kept = (float*)kept;
+    with_type<8, 4>(d->dtype, p.v, [&](auto zero, auto width) {
+      using T = decltype(zero);
+      constexpr int V = decltype(width)::value;
+      if (a.team) {
+        const int64_t blocks = ((int64_t)a.lanes * a.groups * a.team + 255) / 256;
+        with_flag(a.team > 64, [&](auto many) {
+          hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_team_grad<T, V, decltype(many)::value>), dim3((unsigned)blocks), dim3(256),
+                             0, st, a, (const T*)x, (const T*)dy, (T*)dx, w.parts);
+        });
+        return;
+      }
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_grad_sums<T, V>), dim3(norm_grid(p)), dim3(256), 0, st, a, (const T*)x,
+                         (const T*)dy, w.parts);
+      hipLaunchKernelGGL(k_norm_grad_join, dim3((unsigned)std::min(a.batch * a.groups, kMaxBlocks)), dim3(256), 0, st, a,
+                         (const float*)w.parts, w.sums);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_grad_apply<T, V>), dim3(norm_grid(p)), dim3(256), 0, st, a, (const T*)x,
+                         (const T*)dy, (const float*)w.sums, (T*)dx);
+    });
+    columns(w.parts, a.team ? (int64_t)a.lanes : a.batch * a.runs);
   });
 }
 

@@ -146,4 +146,43 @@ inline OrthShape orth_shape(int64_t batch, int64_t n, int64_t m) {
   return s;
 }
 
+// ------------------------------------------------------------------- norm
+constexpr int kNormWords = 4;   // of a thread that keeps its values, at most
+
+// How groups of `words` words (positions x words of a group's channels) are taken:
+// kept by a team of threads, or read twice in runs of positions.
+struct NormShape {
+  int32_t team;               // threads of a team: a power of two up to 64, or 256; 0: runs
+  int32_t lanes;              // of the gradient: batch rows side by side
+  int32_t runs, run, wide;    // runs of positions, positions of one, channel words to a row of threads
+};
+
+// nw: words of a group's channels; grad: teams for one position only, whose dweight
+// and dbias stay with the threads.
+inline NormShape norm_shape(int64_t batch, int64_t positions, int64_t groups, int64_t nw, bool grad) {
+  NormShape s{};
+  const int64_t words = positions * nw;
+  if (words <= 256 * kNormWords && (!grad || positions == 1)) {
+    s.team = 1;
+    while (s.team < 64 && s.team < words) s.team *= 2;
+    if (words > 64 * kNormWords) s.team = 256;
+    // one row of groups to 512 workgroups: dweight and dbias are 2 x 512 rows to join
+    const int64_t per = (groups * s.team + 255) / 256;
+    s.lanes = (int32_t)std::max<int64_t>(1, std::min(batch, 512 * 256 / s.team / groups));
+    if (per > 512) s.lanes = 1;
+    return s;
+  }
+  const int64_t row = groups * nw;
+  s.wide = 1;
+  while (s.wide < 256 && s.wide < row) s.wide *= 2;
+  const int64_t blocks = (row + s.wide - 1) / s.wide, step = 256 / s.wide;
+  // 2048 workgroups, and 8 positions to a thread at least
+  const int64_t most = std::max<int64_t>(1, (positions + 8 * step - 1) / (8 * step));
+  const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, batch * blocks));
+  const int64_t runs = std::max<int64_t>(std::min(most, want), (positions + (1 << 30)) >> 30);
+  s.run = (int32_t)std::max<int64_t>(1, (positions + runs - 1) / runs);
+  s.runs = (int32_t)((positions + s.run - 1) / s.run);
+  return s;
+}
+
 }  // namespace ms

@@ -118,6 +118,12 @@ class GatedDeltaStepDesc(C.Structure):
                 ("scale", C.c_double), ("dtype", _i32), ("device", _i32), ("stream", C.c_void_p)]
 
 
+class GroupNormDesc(C.Structure):
+    _fields_ = [("batch", _i64), ("positions", _i64), ("channels", _i64), ("groups", _i64), ("x_stride", _i64 * 2),
+                ("y_stride", _i64 * 2), ("eps", C.c_double), ("activation", _i32), ("dtype", _i32), ("device", _i32),
+                ("stream", C.c_void_p)]
+
+
 class MergesimError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"mergesim error {code}: {msg}")
@@ -176,6 +182,9 @@ _SIGNATURES = [
     ("ms_gated_delta", [C.POINTER(GatedDeltaDesc)] + [_vp] * 11 + [_i64], _i32),
     ("ms_gated_delta_grad", [C.POINTER(GatedDeltaDesc)] + [_vp] * 16 + [_i64], _i32),
     ("ms_gated_delta_step", [C.POINTER(GatedDeltaStepDesc)] + [_vp] * 8, _i32),
+    ("ms_group_norm_workspace", [C.POINTER(GroupNormDesc), _i32, C.POINTER(_i64)], _i32),
+    ("ms_group_norm", [C.POINTER(GroupNormDesc)] + [_vp] * 7 + [_i64], _i32),
+    ("ms_group_norm_grad", [C.POINTER(GroupNormDesc)] + [_vp] * 10 + [_i64], _i32),
     ("ms_orth_workspace", [C.POINTER(OrthDesc), _i32, C.POINTER(_i64)], _i32),
     ("ms_orthogonalise", [C.POINTER(OrthDesc), _vp, _vp, _vp, _i64], _i32),
     ("ms_orthogonal_update", [C.POINTER(OrthDesc), C.POINTER(OrthRule), _vp, _vp, _vp, _vp, _i64], _i32),

@@ -15,7 +15,7 @@ import ctypes as C
 
 from . import mergesim as _ms
 from .mergesim import (DTYPE_BF16, DTYPE_F32, IDS_I32, IDS_I64, EmbedDesc, GatedDeltaDesc, GatedDeltaStepDesc,
-                       GatedLowpassDesc, GatedStepDesc, OrthDesc, OrthRule, _check)
+                       GatedLowpassDesc, GatedStepDesc, GroupNormDesc, OrthDesc, OrthRule, _check)
 
 # Raises small singular values fast and leaves them within 0.3 of one: the coefficients published by K. Jordan et al.,
 # "Muon: An optimizer for hidden layers in neural networks" (2024).
@@ -365,6 +365,60 @@ def gated_delta_step(q, k, v, decay, rate, state, slots=None, scale=1.0, out=Non
     _check(_lib.ms_gated_delta_step(_on(d, v), q.data_ptr(), k.data_ptr(), v.data_ptr(), decay.data_ptr(), rate.data_ptr(),
                                     state.data_ptr(), slotp, out.data_ptr()))
     return out
+
+
+# --------------------------------------------------------------------- group norm
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}   # MS_ACT_*
+
+
+def _norm_desc(x, groups, activation, eps, weight, bias, lengths):
+    """(descriptor, x [batch, positions, channels], addresses of weight, bias and lengths)"""
+    dtype = _gpu(x, range(2, 64), "x [batch, ..., channels]")
+    channels = x.shape[-1]
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation is {activation!r}: one of {', '.join(ACTIVATIONS)} is wanted")
+    rows = x.flatten(1, -2) if x.dim() > 2 else x[:, None]
+    d = GroupNormDesc(batch=rows.shape[0], positions=rows.shape[1], channels=channels, groups=groups, eps=eps,
+                      activation=act, dtype=dtype)
+    rows = _sequence(rows, d.x_stride)
+    f32 = _torch.float32
+    return (d, rows, _packed(weight, x, "weight", (channels,), f32), _packed(bias, x, "bias", (channels,), f32),
+            _packed(lengths, x, "lengths", x.shape[:1], _torch.int32))
+
+
+def group_norm(x, groups, weight=None, bias=None, activation="none", eps=1e-5, lengths=None, keep=False):
+    """activation(h weight + bias) with h = (x - mean) / sqrt(variance + eps), mean and variance over the positions of
+    a batch row and the channels of a group (ms_group_norm): "none", "relu" or "silu".
+
+    x [batch, ..., channels], float32 or bfloat16, all dimensions between being positions ([batch, channels]: one);
+    weight, bias [channels] float32; lengths int32 [batch]: positions of a row that count, y is zeros past them.
+    keep: also what group_norm_grad starts from."""
+    d, rows, wp, bp, lp = _norm_desc(x, groups, activation, eps, weight, bias, lengths)
+    y = _torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    ref = _on(d, x)
+    hold, ws, n = _scratch(x, _size(_lib.ms_group_norm_workspace, ref, 0))
+    kept = _torch.empty((x.shape[0], groups, 2), dtype=_torch.float32, device=x.device) if keep else None
+    _check(_lib.ms_group_norm(ref, rows.data_ptr(), wp, bp, lp, y.data_ptr(), kept.data_ptr() if keep else None, ws, n))
+    return (y, kept) if keep else y
+
+
+def group_norm_grad(x, groups, kept, dy, weight=None, bias=None, activation="none", lengths=None):
+    """(dx, dweight, dbias) of group_norm from dL/dy (ms_group_norm_grad); kept: what the forward call with keep=True
+    left."""
+    d, rows, wp, bp, lp = _norm_desc(x, groups, activation, 0.0, weight, bias, lengths)
+    _like(dy, x, "dy", x.shape, x.dtype)
+    dy = _sequence(dy.reshape(rows.shape), d.y_stride)
+    f32 = _torch.float32
+    dx = _torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dweight, dbias = (_torch.empty(x.shape[-1], dtype=f32, device=x.device) for _ in range(2))
+    ref = _on(d, x)
+    size = _size(_lib.ms_group_norm_workspace, ref, 1)
+    keptp = _packed(kept, x, "kept", (x.shape[0], groups, 2), f32)
+    hold, ws, n = _scratch(x, size)
+    _check(_lib.ms_group_norm_grad(ref, rows.data_ptr(), wp, bp, lp, keptp, dy.data_ptr(), dx.data_ptr(), dweight.data_ptr(),
+                                   dbias.data_ptr(), ws, n))
+    return dx, dweight, dbias
 
 
 # ---------------------------------------------------------- orthogonalised updates
