@@ -685,8 +685,8 @@ ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rul
 typedef struct {
   int64_t batch, steps;              /* >= 0 and < 2^31 */
   int64_t heads, key_heads;          /* heads in [1, 65536], a multiple of key_heads */
-  int64_t keys, values;              /* keys in [1, 128], values in [1, 65536] */
-  int64_t q_stride[3], k_stride[3], v_stride[3];
+  int64_t keys, values;              /* keys in [1, 128], values in [1, 65536], heads * values < 2^24 */
+  int64_t q_stride[3], k_stride[3], v_stride[3];   /* between steps of v and y: below 2^24 */
   int64_t y_stride[3];               /* of y, or of dy in the gradient */
   int64_t decay_stride[3], rate_stride[3];
   double scale;

@@ -12,10 +12,13 @@
 // every chunk, all at once; k_delta_scan goes through the chunks in order.  The
 // columns of S (the values) never meet: a wavefront carries 16 of them through the
 // whole sequence in registers, and the rows of one product's result, four to a
-// lane, are the next product's operand as they are if the other operand's columns
-// are in the same order (32 of them: 0..3, 16..19 to lanes 0..15, 4..7, 20..23 to
-// 16..31, and so on).  Only K, K', Q and the two triangles pass through LDS, for
-// all wavefronts of a workgroup, laid out as the matrix instructions take them.
+// lane, are the next product's operand as they are: an operand's lane wants eight
+// values along the sum, which are its rows of two 16-row results, if the other
+// operand's columns are dealt to lanes in the same order (order_of).  Only K, Q and
+// the two triangles pass through LDS, for all wavefronts of a workgroup, laid out as
+// the matrix instructions take them; K' is read from K's rows by LDS's transposing
+// reads.  While a chunk is computed the next one's K and Q are on their way to
+// registers and its triangles to the other half of LDS.
 //
 // Arithmetic: 16-bit matrix instructions, 16 times as fast as 32-bit ones.  A
 // 32-bit value is the sum of three bf16 parts (24 bits, and bf16 has float32's
@@ -306,60 +309,12 @@ __global__ void __launch_bounds__(kChunk<T> * 4)
 }
 
 // ------------------------------------------------------------------ operands
-// A chunk of a matrix [C][DK] as operands in LDS: ROWS: its rows are steps, COLS:
-// they are keys (the transpose).  A thread takes blocks of 4 steps x 4 keys, which
-// are whole halves of an operand's 16 bytes either way.  Lane m + 16 g of a piece
-// lies at (m ^ g) + 16 g: the blocks of a wavefront then write to all banks.
-template <class T, bool VEC, int C, int DK, bool ROWS, bool COLS>
-__device__ __forceinline__ void stage_operands(const T* x, int64_t step, int n, int dk, char* rows, char* cols, int tid,
-                                               int threads) {
-  constexpr int P = kIn<T>, RP = C / 16 * (DK / 32), CP = DK / 16 * (C / 32);
-  for (int u = tid; u < C * DK / 16; u += threads) {
-    // 8 blocks of keys and 8 of steps to 64 threads
-    const int rest = u / 64, d0 = (u % 8 + rest % (DK / 32) * 8) * 4, t0 = (u / 8 % 8 + rest / (DK / 32) * 8) * 4;
-    float v[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool there = t0 + i < n;
-      if constexpr (VEC) {
-        Words<T, 4> w{};
-        if (there && d0 < dk) w = *(const Words<T, 4>*)(x + (t0 + i) * step + d0);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] = as_f32(w.v[j]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] = there && d0 + j < dk ? as_f32(x[(t0 + i) * step + d0 + j]) : 0.0f;
-      }
-    }
-#pragma unroll
-    for (int part = 0; part < P; ++part) {
-      __bf16 h[4][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          h[i][j] = (__bf16)v[i][j];
-          if (part + 1 < P) v[i][j] -= (float)h[i][j];
-        }
-      if constexpr (ROWS) {
-        const int piece = t0 / 16 * (DK / 32) + d0 / 32, g = d0 / 4 % 4, half = d0 / 16 % 2;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *(bf16x4*)(rows + (((part * RP + piece) * 64 + ((t0 + i) % 16 ^ g) + 16 * g) * 16 + half * 8)) =
-              bf16x4{h[i][0], h[i][1], h[i][2], h[i][3]};
-      }
-      if constexpr (COLS) {
-        const int piece = d0 / 16 * (C / 32) + t0 / 32, g = t0 / 4 % 4, half = t0 / 16 % 2;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *(bf16x4*)(cols + (((part * CP + piece) * 64 + ((d0 + j) % 16 ^ g) + 16 * g) * 16 + half * 8)) =
-              bf16x4{h[0][j], h[1][j], h[2][j], h[3][j]};
-      }
-    }
-  }
-}
+// Rows of 32 k values as operands in LDS, part by part: piece (rows / 16, k / 32) is
+// 64 x 16 bytes, and lane m + 16 g's eight values, row m, k = 8 g .., lie at
+// (m ^ 4 g) + 16 g: rows that are written or read together are in different banks.
+__device__ __forceinline__ constexpr int lane_place(int m, int g) { return (m ^ 4 * g) + 16 * g; }
 
-// A piece of `pieces`, at this lane's place `at` (swizzled or not).
+// A piece of `pieces`, at this lane's place `at`.
 template <int P>
 __device__ __forceinline__ Op<P> op_take(const char* lds, int pieces, int piece, int at) {
   Op<P> o;
@@ -368,17 +323,107 @@ __device__ __forceinline__ Op<P> op_take(const char* lds, int pieces, int piece,
   return o;
 }
 
-// LDS of a scan: rows of Q and K, columns of K (GRAD: rows of K, columns of both), the chunk's triangles and scales.
-template <class T, int DK, bool GRAD>
-struct ScanLds {
-  static constexpr int C = kChunk<T>, one = kIn<T> * C * DK * 2, PA = GRAD ? kState : kOut<T>;
-  static constexpr int rows = 0, cols = one, q = 2 * one, work = 3 * one, bytes = work + ChunkWork<C, PA>::bytes;
+// The transpose of such rows as an operand: 16 of the columns against 32 rows.  A
+// transposing read takes 4 rows x 16 columns from 16 lanes, 8 bytes each (lane s: row
+// s / 4, columns 4 (s % 4) ..), and gives lane i column i of them; the lanes of group
+// g take rows 4 g .. and, by a second read, 16 + 4 g ...  Columns of a tile are either
+// 16 in a row or (SPREAD) order_of: 4 of each of the four groups of 8.
+template <bool SPREAD>
+__device__ __forceinline__ int turn_place(int lane) {
+  const int s = lane % 16, g = lane / 16, row = 4 * g + s / 4;
+  return SPREAD ? lane_place(row, s % 4) * 16 : lane_place(row, s % 4 / 2) * 16 + s % 2 * 8;
+}
+
+// The two places above differ in the odd tile's: 8 bytes on, or two groups on.
+template <bool SPREAD>
+__device__ __forceinline__ int turn_odd(int lane) {
+  if (SPREAD) return turn_place<true>(lane) + 8;
+  const int s = lane % 16, g = lane / 16, row = 4 * g + s / 4;
+  return lane_place(row, 2 + s % 4 / 2) * 16 + s % 2 * 8;
+}
+
+// KS: pieces to a row of pieces; tile: of 16 columns; step: 32 rows; even, odd: this
+// lane's turn_place and turn_odd.
+template <int P, int KS>
+__device__ __forceinline__ Op<P> op_turn(const char* lds, int pieces, int tile, int step, int even, int odd) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4* From;
+  Op<P> o;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const char* at = lds + (p * pieces + 2 * step * KS + tile / 2) * 1024 + (tile % 2 ? odd : even);
+    const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)at)),
+                 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)(at + KS * 1024)));
+    o.p[p] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  return o;
+}
+
+// Row 4 g + r of the 16-row result m of a product over rows of SPREAD columns.
+__device__ __forceinline__ int order_of(int m, int g, int r) { return m / 2 * 32 + g * 8 + m % 2 * 4 + r; }
+
+// A chunk's rows of K or Q on their way from memory to LDS: in registers.
+template <class T, bool VEC, int ROWS, int COLS, int THREADS>
+struct RowsInFlight {
+  static constexpr int N = ROWS * COLS / 8, U = (N + THREADS - 1) / THREADS, KS = COLS / 32;
+  Words<T, 8> v[U];
+
+  // n rows and dk columns are there, the others zeros.
+  __device__ __forceinline__ void load(const T* x, int64_t stride, int n, int dk, int tid) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = tid + i * THREADS, row = u / (COLS / 8), d = u % (COLS / 8) * 8;
+      const bool there = row < n && d < dk;
+      const T* from = x + (there ? row * stride + d : 0);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i].v[j] = (T)0.0f;
+      if constexpr (VEC) {
+        constexpr int W = 16 / sizeof(T);
+        if (there)
+#pragma unroll
+          for (int q = 0; q < 8; q += W) *(Words<T, W>*)(v[i].v + q) = *(const Words<T, W>*)(from + q);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (there && d + j < dk) v[i].v[j] = from[j];
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(char* lds, int tid) const {
+    constexpr int P = kIn<T>;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = tid + i * THREADS, row = u / (COLS / 8), c = u % (COLS / 8);
+      if (N % THREADS != 0 && u >= N) continue;
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = as_f32(v[i].v[j]);
+      const Op<P> o = op_of<P>(x);
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        *(bf16x8*)(lds + ((p * (ROWS / 16) * KS + row / 16 * KS + c / 4) * 64 + lane_place(row % 16, c % 4)) * 16) = o.p[p];
+    }
+  }
 };
 
-// Copies a chunk's triangles and scales.
-__device__ __forceinline__ void copy_work(const char* from, char* to, int bytes, int tid, int threads) {
-  for (int i = tid * 16; i < bytes; i += threads * 16) *(uint4*)(to + i) = *(const uint4*)(from + i);
+// A chunk's triangles and scales from memory straight to LDS, 16 bytes a lane, lane
+// i's to 16 i of the wavefront's.
+template <int BYTES>
+__device__ __forceinline__ void fetch_work(const char* from, char* to, int tid) {
+#pragma unroll
+  for (int at = 0; at < BYTES; at += 4096)
+    if (at + tid * 16 < BYTES)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + at + tid * 16),
+                                       (__attribute__((address_space(3))) void*)(to + at + tid / 64 * 1024), 16, 0, 0);
 }
+
+// One of the two halves of a scan's LDS: rows of K and of Q, the chunk's triangles and scales.
+template <class T, int DK, bool GRAD>
+struct ScanLds {
+  static constexpr int C = kChunk<T>, PA = GRAD ? kState : kOut<T>;
+  static constexpr int k = 0, q = kIn<T> * C * DK * 2, work = 2 * q, bytes = work + ChunkWork<C, PA>::bytes;
+};
 
 // Batch row, head and block of columns of a workgroup: the blocks of a head are 8
 // apart, on one of the 8 dies, whose L2 then reads the head's K, Q and triangles once.
@@ -389,132 +434,166 @@ __device__ __forceinline__ bool scan_place(const DeltaArgs& p, int blocks, int64
   return bh < p.batch * p.heads;
 }
 
+// 16 steps' values of one column each, to or from results' registers: row 4 g + r of
+// result m is step 16 m + 4 g + r, of which n are there.
+template <class T, int C>
+__device__ __forceinline__ void take_steps(const T* x, int32_t stride, int n, int g, T (&out)[C / 16][4]) {
+#pragma unroll
+  for (int m = 0; m < C / 16; ++m)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) out[m][r] = x[(uint32_t)(min(m * 16 + g * 4 + r, n - 1) * stride)];
+}
+
 // The chunks of a head in order.  grid: see scan_place; a wavefront has 16 columns.
-// states: S before each chunk, z: the errors, for the gradient (NULL: not kept).
+// states: S before each chunk, errors: Z, for the gradient (NULL: not kept).
 template <class T, bool VEC, int DK>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 1)
     k_delta_scan(DeltaArgs p, int blocks, const T* q, const T* k, const T* v, const float* s0, const char* work, T* y,
                  float* last, float* states, float* errors) {
   using Lds = ScanLds<T, DK, false>;
-  constexpr int C = Lds::C, KS = DK / 32, PA = Lds::PA, PI = kIn<T>, RP = C / 16 * KS, CP = DK / 16 * (C / 32);
+  constexpr int C = Lds::C, KS = DK / 32, PA = Lds::PA, PI = kIn<T>, RP = C / 16 * KS;
   using Work = ChunkWork<C, PA>;
   extern __shared__ __align__(16) char lds[];
   int64_t bh;
   int block;
   if (!scan_place(p, blocks, bh, block)) return;
-  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, at = (lane % 16 ^ g) + 16 * g;
+  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, at = lane_place(lane % 16, g);
+  const int even = turn_place<true>(lane), odd = turn_odd<true>(lane);
   const int64_t b = bh / p.heads;
   const int head = (int)(bh % p.heads), kh = head / p.group;
-  const int col = (block * (int)(blockDim.x / 64) + tid / 64) * 16 + lane % 16;
-  const bool mine = col < p.dv;
+  const int first = (block * 4 + tid / 64) * 16, col = first + lane % 16, mcol = min(col, p.dv - 1);
+  const bool mine = col < p.dv, some = first < p.dv;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
-  const T* vb = v + b * p.v.b + head * p.v.h + col;
-  T* yb = y + b * p.y.b + head * p.y.h + col;
+  const int chunks = (len + C - 1) / C;
+  const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *vp = v + b * p.v.b + head * p.v.h + mcol;
+  T* yp = y + b * p.y.b + head * p.y.h + mcol;
+  const char* wp = work + bh * p.nchunk * Work::bytes;
+  const int32_t vt = (int32_t)p.v.t, yt = (int32_t)p.y.t;
   f32x4 s[DK / 16];
 #pragma unroll
   for (int m = 0; m < DK / 16; ++m)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int d = m * 16 + g * 4 + r;
+      const int d = order_of(m, g, r);
       s[m][r] = s0 && mine && d < p.dk ? s0[(bh * p.dk + d) * p.dv + col] : 0.0f;
     }
-  int64_t chunk = 0;
-  for (; chunk * C < len; ++chunk) {
-    const int64_t t0 = chunk * C;
-    const int n = (int)min((int64_t)C, len - t0);
-    __syncthreads();
-    stage_operands<T, VEC, C, DK, true, true>(k + b * p.k.b + t0 * p.k.t + kh * p.k.h, p.k.t, n, p.dk, lds + Lds::rows,
-                                              lds + Lds::cols, tid, blockDim.x);
-    stage_operands<T, VEC, C, DK, true, false>(q + b * p.q.b + t0 * p.q.t + kh * p.q.h, p.q.t, n, p.dk, lds + Lds::q,
-                                               nullptr, tid, blockDim.x);
-    copy_work(work + (bh * p.nchunk + chunk) * Work::bytes, lds + Lds::work, Work::bytes, tid, blockDim.x);
+  RowsInFlight<T, VEC, C, DK, 256> kr, qr;
+  T vr[C / 16][4];
+  if (chunks > 0) {
+    const int n = min(C, len);
+    fetch_work<Work::bytes>(wp, lds + Lds::work, tid);
+    kr.load(kp, p.k.t, n, p.dk, tid);
+    qr.load(qp, p.q.t, n, p.dk, tid);
+    take_steps<T, C>(vp, vt, n, g, vr);
+    kr.store(lds + Lds::k, tid);
+    qr.store(lds + Lds::q, tid);
+  }
+  for (int chunk = 0; chunk < chunks; ++chunk) {
+    char* const here = lds + (chunk & 1) * Lds::bytes;
+    char* const next = lds + (~chunk & 1) * Lds::bytes;
+    const int n = min(C, len - chunk * C), ahead = min(C, len - (chunk + 1) * C);
     f32x4 z[C / 16], o[C / 16];
 #pragma unroll
     for (int m = 0; m < C / 16; ++m)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = m * 16 + g * 4 + r;
-        z[m][r] = mine && t < n ? as_f32(vb[(t0 + t) * p.v.t]) : 0.0f;
+      for (int r = 0; r < 4; ++r) z[m][r] = m * 16 + g * 4 + r < n ? as_f32(vr[m][r]) : 0.0f;
+    __syncthreads();   // this chunk's operands are there, and the other half is read
+    if (ahead > 0) {
+      fetch_work<Work::bytes>(wp + (int64_t)(chunk + 1) * Work::bytes, next + Lds::work, tid);
+      kp += C * p.k.t, qp += C * p.q.t, vp += C * p.v.t;
+      kr.load(kp, p.k.t, ahead, p.dk, tid);
+      qr.load(qp, p.q.t, ahead, p.dk, tid);
+      take_steps<T, C>(vp, vt, ahead, g, vr);
+    }
+    if (some) {
+      if (states && mine) {
+        float* sp = states + (bh * p.nchunk + chunk) * p.dk * p.dv + col;
+#pragma unroll
+        for (int m = 0; m < DK / 16; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (order_of(m, g, r) < p.dk) sp[(uint32_t)(order_of(m, g, r) * p.dv)] = s[m][r];
       }
-    if (states && mine)
+      const float* e = (const float*)(here + Lds::work + Work::scales);
+      Op<kState> sp[KS];
 #pragma unroll
-      for (int m = 0; m < DK / 16; ++m)
+      for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = m * 16 + g * 4 + r;
-          if (d < p.dk) states[((bh * p.nchunk + chunk) * p.dk + d) * p.dv + col] = s[m][r];
+      for (int m = 0; m < C / 16; ++m) {
+        f32x4 c = zero4(), w = zero4();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          c = op_mul<kState>(op_take<PI>(here + Lds::k, RP, m * KS + ks, at), sp[ks], c);
+          w = op_mul<kOut<T>>(op_take<PI>(here + Lds::q, RP, m * KS + ks, at), sp[ks], w);
         }
-    __syncthreads();
-    const float* e = (const float*)(lds + Lds::work + Work::scales);
-    Op<kState> sp[KS];
+        const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
-#pragma unroll
-    for (int m = 0; m < C / 16; ++m) {
-      f32x4 c = zero4(), w = zero4();
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        c = op_mul<kState>(op_take<PI>(lds + Lds::rows, RP, m * KS + ks, at), sp[ks], c);
-        w = op_mul<kOut<T>>(op_take<PI>(lds + Lds::q, RP, m * KS + ks, at), sp[ks], w);
+        for (int r = 0; r < 4; ++r) z[m][r] -= share_of(em[r], c[r]), o[m][r] = share_of(em[r], w[r]) * p.scale;
       }
-      const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
+      Op<kState> zp[C / 32];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[m][r] -= share_of(em[r], c[r]), o[m][r] = share_of(em[r], w[r]) * p.scale;
-    }
-    Op<kState> zp[C / 32];
+      for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
 #pragma unroll
-    for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
+      for (int m = 0; m < C / 16; ++m) {
+        z[m] = zero4();
 #pragma unroll
-    for (int m = 0; m < C / 16; ++m) {
-      z[m] = zero4();
-#pragma unroll
-      for (int ks = 0; ks <= m / 2; ++ks)
-        z[m] = op_mul<kState>(
-            op_take<kState>(lds + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zp[ks], z[m]);
-    }
-    if (errors && mine)
-#pragma unroll
-      for (int m = 0; m < C / 16; ++m)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          errors[((bh * p.nchunk + chunk) * C + m * 16 + g * 4 + r) * p.dv + col] = z[m][r];
-    Op<kOut<T>> zo[C / 32];
-#pragma unroll
-    for (int ks = 0; ks < C / 32; ++ks) zo[ks] = op_of<kOut<T>>(z[2 * ks], z[2 * ks + 1]);
-#pragma unroll
-    for (int m = 0; m < C / 16; ++m) {
-#pragma unroll
-      for (int ks = 0; ks <= m / 2; ++ks)
-        o[m] = op_mul<kOut<T>>(
-            op_take<PA>(lds + Lds::work + Work::reads, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zo[ks], o[m]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = m * 16 + g * 4 + r;
-        if (mine && t0 + t < p.steps) yb[(t0 + t) * p.y.t] = t < n ? (T)o[m][r] : (T)0.0f;
+        for (int ks = 0; ks <= m / 2; ++ks)
+          z[m] = op_mul<kState>(
+              op_take<kState>(here + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zp[ks], z[m]);
       }
+      if (errors && mine) {
+        float* ep = errors + ((bh * p.nchunk + chunk) * C) * p.dv + col;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[m][r] *= e[C + m * 16 + g * 4 + r] * e[2 * C + m * 16 + g * 4 + r];
+        for (int m = 0; m < C / 16; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) ep[(uint32_t)((m * 16 + g * 4 + r) * p.dv)] = z[m][r];
+      }
+      Op<kOut<T>> zo[C / 32];
+#pragma unroll
+      for (int ks = 0; ks < C / 32; ++ks) zo[ks] = op_of<kOut<T>>(z[2 * ks], z[2 * ks + 1]);
+#pragma unroll
+      for (int m = 0; m < C / 16; ++m) {
+#pragma unroll
+        for (int ks = 0; ks <= m / 2; ++ks)
+          o[m] = op_mul<kOut<T>>(
+              op_take<PA>(here + Lds::work + Work::reads, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zo[ks], o[m]);
+        const f32x4 om = *(const f32x4*)(e + C + m * 16 + g * 4), bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[m][r] *= om[r] * bm[r];
+      }
+      if (mine)
+#pragma unroll
+        for (int m = 0; m < C / 16; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (m * 16 + g * 4 + r < n) yp[(uint32_t)((m * 16 + g * 4 + r) * yt)] = (T)o[m][r];
+#pragma unroll
+      for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
+      const float keep = e[C - 1];
+#pragma unroll
+      for (int m = 0; m < DK / 16; ++m) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
+#pragma unroll
+        for (int ks = 0; ks < C / 32; ++ks)
+          s[m] = op_mul<kState>(op_turn<PI, KS>(here + Lds::k, RP, m, ks, even, odd), zp[ks], s[m]);
+      }
+      yp += C * p.y.t;
     }
-#pragma unroll
-    for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
-    const float keep = e[C - 1];
-#pragma unroll
-    for (int m = 0; m < DK / 16; ++m) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
-#pragma unroll
-      for (int ks = 0; ks < C / 32; ++ks)
-        s[m] = op_mul<kState>(op_take<PI>(lds + Lds::cols, CP, m * (C / 32) + ks, at), zp[ks], s[m]);
+    if (ahead > 0) {
+      kr.store(next + Lds::k, tid);
+      qr.store(next + Lds::q, tid);
     }
   }
   if (mine) {
-    for (int64_t t = chunk * C + g; t < p.steps; t += 4) yb[t * p.y.t] = (T)0.0f;
+    T* ye = y + b * p.y.b + head * p.y.h + col;
+    for (int64_t t = len + g; t < p.steps; t += 4) ye[t * p.y.t] = (T)0.0f;
     if (last)
 #pragma unroll
       for (int m = 0; m < DK / 16; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int d = m * 16 + g * 4 + r;
+          const int d = order_of(m, g, r);
           if (d < p.dk) last[(bh * p.dk + d) * p.dv + col] = s[m][r];
         }
   }

@@ -24,125 +24,147 @@
 
 // Columns of the state's gradient through the chunks in reverse order.
 template <class T, bool VEC, int DK>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 1)
     k_delta_back(DeltaArgs p, int blocks, const T* q, const T* k, const T* dy, const float* dlast, const char* work, T* dv,
                  float* ds0, float* dstates, float* xs) {
   using Lds = ScanLds<T, DK, true>;
-  constexpr int C = Lds::C, KS = DK / 32, PI = kIn<T>, RP = C / 16 * KS, CP = DK / 16 * (C / 32);
+  constexpr int C = Lds::C, KS = DK / 32, PI = kIn<T>, RP = C / 16 * KS;
   using Work = ChunkWork<C, kState>;
   extern __shared__ __align__(16) char lds[];
   int64_t bh;
   int block;
   if (!scan_place(p, blocks, bh, block)) return;
-  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, at = (lane % 16 ^ g) + 16 * g;
+  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, at = lane_place(lane % 16, g);
+  const int even = turn_place<true>(lane), odd = turn_odd<true>(lane);
   const int64_t b = bh / p.heads;
   const int head = (int)(bh % p.heads), kh = head / p.group;
-  const int col = (block * (int)(blockDim.x / 64) + tid / 64) * 16 + lane % 16;
-  const bool mine = col < p.dv;
+  const int first = (block * 4 + tid / 64) * 16, col = first + lane % 16, mcol = min(col, p.dv - 1);
+  const bool mine = col < p.dv, some = first < p.dv;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
-  const T* yb = dy + b * p.y.b + head * p.y.h + col;
-  T* vb = dv + (b * p.steps * p.heads + head) * p.dv + col;
-  const int64_t vt = (int64_t)p.heads * p.dv;
+  const int chunks = (len + C - 1) / C;
+  const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *yp = dy + b * p.y.b + head * p.y.h + mcol;
+  T* const vp = dv + (b * p.steps * p.heads + head) * p.dv + mcol;
+  const char* wp = work + bh * p.nchunk * Work::bytes;
+  const int32_t yt = (int32_t)p.y.t, vt = p.heads * p.dv;
   f32x4 s[DK / 16];
 #pragma unroll
   for (int m = 0; m < DK / 16; ++m)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int d = m * 16 + g * 4 + r;
+      const int d = order_of(m, g, r);
       s[m][r] = dlast && mine && d < p.dk ? dlast[(bh * p.dk + d) * p.dv + col] : 0.0f;
     }
-  const int64_t chunks = (len + C - 1) / C;
   if (mine)
-    for (int64_t t = chunks * C + g; t < p.steps; t += 4) vb[t * vt] = (T)0.0f;
-  for (int64_t chunk = chunks - 1; chunk >= 0; --chunk) {
-    const int64_t t0 = chunk * C;
-    const int n = (int)min((int64_t)C, len - t0);
-    __syncthreads();
-    stage_operands<T, VEC, C, DK, true, true>(k + b * p.k.b + t0 * p.k.t + kh * p.k.h, p.k.t, n, p.dk, lds + Lds::rows,
-                                              lds + Lds::cols, tid, blockDim.x);
-    stage_operands<T, VEC, C, DK, false, true>(q + b * p.q.b + t0 * p.q.t + kh * p.q.h, p.q.t, n, p.dk, nullptr,
-                                               lds + Lds::q, tid, blockDim.x);
-    copy_work(work + (bh * p.nchunk + chunk) * Work::bytes, lds + Lds::work, Work::bytes, tid, blockDim.x);
+    for (int64_t t = len + g; t < p.steps; t += 4) vp[t * vt] = (T)0.0f;
+  RowsInFlight<T, VEC, C, DK, 256> kr, qr;
+  T yr[C / 16][4];
+  const auto ahead_of = [&](int chunk, char* to) {
+    const int n = min(C, len - chunk * C);
+    const int64_t t0 = (int64_t)chunk * C;
+    fetch_work<Work::bytes>(wp + (int64_t)chunk * Work::bytes, to + Lds::work, tid);
+    kr.load(kp + t0 * p.k.t, p.k.t, n, p.dk, tid);
+    qr.load(qp + t0 * p.q.t, p.q.t, n, p.dk, tid);
+    take_steps<T, C>(yp + t0 * p.y.t, yt, n, g, yr);
+  };
+  if (chunks > 0) {
+    char* const to = lds + ((chunks - 1) & 1) * Lds::bytes;
+    ahead_of(chunks - 1, to);
+    kr.store(to + Lds::k, tid);
+    qr.store(to + Lds::q, tid);
+  }
+  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+    char* const here = lds + (chunk & 1) * Lds::bytes;
+    char* const next = lds + (~chunk & 1) * Lds::bytes;
+    const int n = min(C, len - chunk * C);
     f32x4 dyr[C / 16], x[C / 16];
 #pragma unroll
     for (int m = 0; m < C / 16; ++m)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = m * 16 + g * 4 + r;
-        dyr[m][r] = mine && t < n ? as_f32(yb[(t0 + t) * p.y.t]) : 0.0f;
+      for (int r = 0; r < 4; ++r) dyr[m][r] = m * 16 + g * 4 + r < n ? as_f32(yr[m][r]) : 0.0f;
+    __syncthreads();   // this chunk's operands are there, and the other half is read
+    if (chunk > 0) ahead_of(chunk - 1, next);
+    if (some) {
+      if (mine) {
+        float* sp = dstates + (bh * p.nchunk + chunk) * p.dk * p.dv + col;
+#pragma unroll
+        for (int m = 0; m < DK / 16; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (order_of(m, g, r) < p.dk) sp[(uint32_t)(order_of(m, g, r) * p.dv)] = s[m][r];
       }
-    if (mine)
+      const float* e = (const float*)(here + Lds::work + Work::scales);
+      {
+        Op<kState> sp[KS];
 #pragma unroll
-      for (int m = 0; m < DK / 16; ++m)
+        for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = m * 16 + g * 4 + r;
-          if (d < p.dk) dstates[((bh * p.nchunk + chunk) * p.dk + d) * p.dv + col] = s[m][r];
+        for (int m = 0; m < C / 16; ++m) {
+          x[m] = zero4();
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) x[m] = op_mul<kState>(op_take<PI>(here + Lds::k, RP, m * KS + ks, at), sp[ks], x[m]);
+          const f32x4 om = *(const f32x4*)(e + C + m * 16 + g * 4);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[m][r] = share_of(om[r], x[m][r]);
         }
-    __syncthreads();
-    const float* e = (const float*)(lds + Lds::work + Work::scales);
-    {
-      Op<kState> sp[KS];
+      }
+      {
+        Op<PI> dp[C / 32];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
+        for (int ks = 0; ks < C / 32; ++ks) dp[ks] = op_of<PI>(dyr[2 * ks], dyr[2 * ks + 1]);
+#pragma unroll
+        for (int m = 0; m < C / 16; ++m) {
+#pragma unroll
+          for (int ks = m / 2; ks < C / 32; ++ks)
+            x[m] = op_mul<kState>(
+                op_take<kState>(here + Lds::work + Work::reads, tri_pieces(C), tri_piece<C, true>(m, ks), lane), dp[ks], x[m]);
+          const f32x4 bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[m][r] *= bm[r];
+        }
+      }
+      Op<kState> xp[C / 32];
+#pragma unroll
+      for (int ks = 0; ks < C / 32; ++ks) xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
+      float* ep = xs + ((bh * p.nchunk + chunk) * C) * p.dv + mcol;
+      T* vc = vp + (int64_t)chunk * C * vt;
 #pragma unroll
       for (int m = 0; m < C / 16; ++m) {
         x[m] = zero4();
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) x[m] = op_mul<kState>(op_take<PI>(lds + Lds::rows, RP, m * KS + ks, at), sp[ks], x[m]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[m][r] = share_of(e[C + m * 16 + g * 4 + r], x[m][r]);
-      }
-    }
-    {
-      Op<PI> dp[C / 32];
-#pragma unroll
-      for (int ks = 0; ks < C / 32; ++ks) dp[ks] = op_of<PI>(dyr[2 * ks], dyr[2 * ks + 1]);
-#pragma unroll
-      for (int m = 0; m < C / 16; ++m) {
-#pragma unroll
         for (int ks = m / 2; ks < C / 32; ++ks)
-          x[m] = op_mul<kState>(op_take<kState>(lds + Lds::work + Work::reads, tri_pieces(C), tri_piece<C, true>(m, ks), lane),
-                                dp[ks], x[m]);
+          x[m] = op_mul<kState>(op_take<kState>(here + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, true>(m, ks), lane),
+                                xp[ks], x[m]);
+        const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[m][r] *= e[2 * C + m * 16 + g * 4 + r];
+        for (int r = 0; r < 4; ++r) {
+          const int t = m * 16 + g * 4 + r;
+          if (mine) ep[(uint32_t)(t * p.dv)] = x[m][r];
+          if (mine && t < n) vc[(uint32_t)(t * vt)] = (T)x[m][r];
+          x[m][r] *= -em[r];
+          dyr[m][r] *= p.scale * em[r];
+        }
       }
-    }
-    Op<kState> xp[C / 32];
-#pragma unroll
-    for (int ks = 0; ks < C / 32; ++ks) xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
-#pragma unroll
-    for (int m = 0; m < C / 16; ++m) {
-      x[m] = zero4();
-#pragma unroll
-      for (int ks = m / 2; ks < C / 32; ++ks)
-        x[m] = op_mul<kState>(op_take<kState>(lds + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, true>(m, ks), lane),
-                              xp[ks], x[m]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = m * 16 + g * 4 + r;
-        if (mine) xs[((bh * p.nchunk + chunk) * C + t) * p.dv + col] = x[m][r];
-        if (mine && t0 + t < p.steps) vb[(t0 + t) * vt] = t < n ? (T)x[m][r] : (T)0.0f;
-        x[m][r] *= -e[t];
-        dyr[m][r] *= p.scale * e[t];
-      }
-    }
-    Op<kState> dp[C / 32];
-#pragma unroll
-    for (int ks = 0; ks < C / 32; ++ks) {
-      xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
-      dp[ks] = op_of<kState>(dyr[2 * ks], dyr[2 * ks + 1]);
-    }
-    const float keep = e[C - 1];
-#pragma unroll
-    for (int m = 0; m < DK / 16; ++m) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
+      Op<kState> dp[C / 32];
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) {
-        s[m] = op_mul<kState>(op_take<PI>(lds + Lds::q, CP, m * (C / 32) + ks, at), dp[ks], s[m]);
-        s[m] = op_mul<kState>(op_take<PI>(lds + Lds::cols, CP, m * (C / 32) + ks, at), xp[ks], s[m]);
+        xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
+        dp[ks] = op_of<kState>(dyr[2 * ks], dyr[2 * ks + 1]);
       }
+      const float keep = e[C - 1];
+#pragma unroll
+      for (int m = 0; m < DK / 16; ++m) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
+#pragma unroll
+        for (int ks = 0; ks < C / 32; ++ks) {
+          s[m] = op_mul<kState>(op_turn<PI, KS>(here + Lds::q, RP, m, ks, even, odd), dp[ks], s[m]);
+          s[m] = op_mul<kState>(op_turn<PI, KS>(here + Lds::k, RP, m, ks, even, odd), xp[ks], s[m]);
+        }
+      }
+    }
+    if (chunk > 0) {
+      kr.store(next + Lds::k, tid);
+      qr.store(next + Lds::q, tid);
     }
   }
   if (ds0 && mine)
@@ -150,33 +172,23 @@ __global__ void __launch_bounds__(256)
     for (int m = 0; m < DK / 16; ++m)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int d = m * 16 + g * 4 + r;
+        const int d = order_of(m, g, r);
         if (d < p.dk) ds0[(bh * p.dk + d) * p.dv + col] = s[m][r];
       }
 }
 
-// `rows` rows of 32 values as operands in LDS, part by part, lane m + 16 g of a piece
-// at (m ^ 4 g) + 16 g; `there` rows and `width` values of a row are there.
-template <int P, class T, bool VEC>
-__device__ __forceinline__ void stage_slab(const T* x, int64_t stride, int rows, int there, int width, char* out, int tid,
-                                           int threads) {
-  for (int u = tid; u < rows * 4; u += threads) {
-    const int row = u / 4, g = u % 4;
-    float v[8];
-    load8<T, VEC>(x + (row < there ? row * stride + g * 8 : 0), row < there ? width - g * 8 : 0, v);
-    const Op<P> o = op_of<P>(v);
-#pragma unroll
-    for (int q = 0; q < P; ++q)
-      *(bf16x8*)(out + ((q * (rows / 16) + row / 16) * 64 + (row % 16 ^ 4 * g) + 16 * g) * 16) = o.p[q];
-  }
-}
+// Wavefronts of k_delta_grad: C / 16 tiles of steps, and the keys dealt to so many of each.
+template <class T, int DK>
+constexpr int kGradParts = kChunk<T> == 64 ? 2 : DK >= 64 ? 4 : 2;
+template <class T, int DK>
+constexpr int kGradThreads = kChunk<T> * 4 * kGradParts<T, DK>;
 
 template <class T, int DK>
 struct GradLds {
-  static constexpr int C = kChunk<T>, PI = kIn<T>;
-  static constexpr int kc = 0, qc = kc + PI * C * DK * 2, s = qc + PI * C * DK * 2, ds = s + kState * DK * 64,
+  static constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T, DK>;
+  static constexpr int k = 0, q = k + PI * C * DK * 2, s = q + PI * C * DK * 2, ds = s + kState * DK * 64,
                        z = ds + kState * DK * 64, x = z + kState * C * 64, dy = x + kState * C * 64,
-                       sums = dy + PI * C * 64, bytes = sums + (3 * C + C + 16) * 4 + C * 8;
+                       sums = dy + PI * C * 64, bytes = sums + (3 * C + 2 * NP * C + 16) * 4 + C * 8;
 };
 
 struct DeltaGradOut {
@@ -184,23 +196,54 @@ struct DeltaGradOut {
   float *ddecay, *drate;
 };
 
+// 32 columns of rows of the state, its gradient, Z, X and dY, on their way to LDS.
+template <class T, bool VEC, int ROWS, int THREADS>
+struct SlabInFlight {
+  static constexpr int U = (ROWS * 4 + THREADS - 1) / THREADS;
+  float v[U][8];
+
+  __device__ __forceinline__ void load(const T* x, int64_t stride, int there, int width, int tid) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = tid + i * THREADS, row = u / 4, c = u % 4 * 8;
+      const bool some = row < there && c < width;
+      load8<T, VEC>(x + (some ? row * stride + c : 0), some ? width - c : 0, v[i]);
+    }
+  }
+
+  template <int P>
+  __device__ __forceinline__ void store(char* lds, int tid) const {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = tid + i * THREADS, row = u / 4;
+      if (ROWS * 4 % THREADS != 0 && u >= ROWS * 4) continue;
+      const Op<P> o = op_of<P>(v[i]);
+#pragma unroll
+      for (int q = 0; q < P; ++q)
+        *(bf16x8*)(lds + ((q * (ROWS / 16) + row / 16) * 64 + lane_place(row % 16, u % 4)) * 16) = o.p[q];
+    }
+  }
+};
+
 // dQ, dK and the gates of a chunk of one key head, its heads one after the other.  A
-// wavefront has 16 steps, as rows of its results and as columns of the four products
-// z dy', z x', dy z', x z' over the values, whose sums are the operands that multiply
-// K and Q.
-template <class T, bool VEC, bool VECV, int DK>
-__global__ void __launch_bounds__(kChunk<T> * 4)
+// wavefront has 16 steps and a part of the keys; the steps are rows of its results and
+// columns of the four products z dy', z x', dy z', x z' over the values, whose sums
+// are the operands that multiply K and Q.
+template <class T, bool VEC, int DK>
+__global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
     k_delta_grad(DeltaArgs p, const T* q, const T* k, const T* dy, const float* decay, const float* rate,
                  const float* states, const float* errors, const float* dstates, const float* xs, DeltaGradOut out) {
   using Lds = GradLds<T, DK>;
-  constexpr int C = kChunk<T>, PI = kIn<T>, NT = DK / 16, RT = C / 16, KC = C / 32, threads = C * 4;
+  constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T, DK>, THREADS = kGradThreads<T, DK>;
+  constexpr int RT = C / 16, KC = C / 32, NT = DK / 16, MT = NT / NP, KS = DK / 32, RP = RT * KS;
   extern __shared__ __align__(16) char lds[];
   float* const sc = (float*)(lds + Lds::sums);   // e, o, b
-  float* const dg = sc + 3 * C;                  // gradients of G
-  float* const red = dg + C;
+  float* const dg = sc + 3 * C;                  // gradients of G, and k W, by parts
+  float* const kw = dg + NP * C;
+  float* const red = kw + NP * C;
   double* const sum = (double*)(red + 16);
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, g = lane / 16;
-  const int at = (lane % 16 ^ g) + 16 * g, as = (lane % 16 ^ 4 * g) + 16 * g;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64 % RT, part = tid / 64 / RT, g = lane / 16;
+  const int at = lane_place(lane % 16, g), even = turn_place<false>(lane), odd = turn_odd<false>(lane);
   const int key_heads = p.heads / p.group;
   const int64_t all = p.batch * key_heads * p.nchunk;
   for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
@@ -208,22 +251,36 @@ __global__ void __launch_bounds__(kChunk<T> * 4)
     const int kh = (int)(u / p.nchunk % key_heads);
     const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
     const int n = (int)max((int64_t)0, min((int64_t)C, len - t0)), in = (int)min((int64_t)C, p.steps - t0);
-    const T *kb = k + b * p.k.b + t0 * p.k.t + kh * p.k.h, *qb = q + b * p.q.b + t0 * p.q.t + kh * p.q.h;
-    f32x4 dq[NT], dk[NT];
+    f32x4 dq[MT], dk[MT];
 #pragma unroll
-    for (int m = 0; m < NT; ++m) dq[m] = dk[m] = zero4();
+    for (int m = 0; m < MT; ++m) dq[m] = dk[m] = zero4();
     __syncthreads();
     if (n > 0) {
-      stage_operands<T, VEC, C, DK, false, true>(kb, p.k.t, n, p.dk, nullptr, lds + Lds::kc, tid, threads);
-      stage_operands<T, VEC, C, DK, false, true>(qb, p.q.t, n, p.dk, nullptr, lds + Lds::qc, tid, threads);
+      RowsInFlight<T, VEC, C, DK, THREADS> kr, qr;
+      kr.load(k + b * p.k.b + t0 * p.k.t + kh * p.k.h, p.k.t, n, p.dk, tid);
+      qr.load(q + b * p.q.b + t0 * p.q.t + kh * p.q.h, p.q.t, n, p.dk, tid);
+      kr.store(lds + Lds::k, tid);
+      qr.store(lds + Lds::q, tid);
     }
     for (int h = 0; h < p.group; ++h) {
       const int head = kh * p.group + h;
       const int64_t bh = b * p.heads + head, cell = bh * p.nchunk + chunk, gate = (b * p.steps + t0) * p.heads + head;
       if (n == 0) {
-        for (int t = tid; t < in; t += threads) out.ddecay[gate + (int64_t)t * p.heads] = out.drate[gate + (int64_t)t * p.heads] = 0.0f;
+        for (int t = tid; t < in; t += THREADS)
+          out.ddecay[gate + (int64_t)t * p.heads] = out.drate[gate + (int64_t)t * p.heads] = 0.0f;
         continue;
       }
+      SlabInFlight<float, VEC, DK, THREADS> sr, dsr;
+      SlabInFlight<float, VEC, C, THREADS> zr, xr;
+      SlabInFlight<T, VEC, C, THREADS> yr;
+      const auto ahead = [&](int c) {
+        sr.load(states + cell * p.dk * p.dv + c, p.dv, p.dk, p.dv - c, tid);
+        dsr.load(dstates + cell * p.dk * p.dv + c, p.dv, p.dk, p.dv - c, tid);
+        zr.load(errors + cell * C * p.dv + c, p.dv, n, p.dv - c, tid);
+        xr.load(xs + cell * C * p.dv + c, p.dv, n, p.dv - c, tid);
+        yr.load(dy + b * p.y.b + t0 * p.y.t + head * p.y.h + c, p.y.t, n, p.dv - c, tid);
+      };
+      ahead(0);
       bool forgets = false;
       if (tid < C) {
         double d = 0.0;
@@ -231,7 +288,7 @@ __global__ void __launch_bounds__(kChunk<T> * 4)
         if (tid < n) {
           const float x = decay[b * p.decay.b + (t0 + tid) * p.decay.t + head * p.decay.h];
           forgets = x < -200.0f;
-          d = x < -200.0f ? -200.0 : (double)x;
+          d = forgets ? -200.0 : (double)x;
           r = rate[b * p.rate.b + (t0 + tid) * p.rate.t + head * p.rate.h];
         }
 #pragma unroll
@@ -247,49 +304,44 @@ __global__ void __launch_bounds__(kChunk<T> * 4)
         sc[2 * C + tid] = r;
       }
       // sums over the values, 32 at a time
-      f32x4 eq[NT], er[NT], ew[NT], zy[RT], zx[RT], yz[RT], xz[RT];
+      f32x4 eq[MT], er[MT], ew[MT], zy[RT], zx[RT], yz[RT], xz[RT];
       float inner = 0.0f;   // <dS, S>, this thread's part
 #pragma unroll
-      for (int m = 0; m < NT; ++m) eq[m] = er[m] = ew[m] = zero4();
+      for (int m = 0; m < MT; ++m) eq[m] = er[m] = ew[m] = zero4();
 #pragma unroll
       for (int m = 0; m < RT; ++m) zy[m] = zx[m] = yz[m] = xz[m] = zero4();
       for (int c0 = 0; c0 < p.dv; c0 += 32) {
-        const int width = p.dv - c0;
         __syncthreads();
-        stage_slab<kState, float, VECV>(states + cell * p.dk * p.dv + c0, p.dv, DK, p.dk, width, lds + Lds::s, tid, threads);
-        stage_slab<kState, float, VECV>(dstates + cell * p.dk * p.dv + c0, p.dv, DK, p.dk, width, lds + Lds::ds, tid, threads);
-        stage_slab<kState, float, VECV>(errors + cell * C * p.dv + c0, p.dv, C, n, width, lds + Lds::z, tid, threads);
-        stage_slab<kState, float, VECV>(xs + cell * C * p.dv + c0, p.dv, C, n, width, lds + Lds::x, tid, threads);
-        stage_slab<PI, T, VECV>(dy + b * p.y.b + t0 * p.y.t + head * p.y.h + c0, p.y.t, C, n, width, lds + Lds::dy, tid, threads);
-        for (int w = tid; w < p.dk * 4; w += threads) {
-          float x[8], y[8];
-          const int64_t from = (cell * p.dk + w / 4) * p.dv + c0 + w % 4 * 8;
-          const int there = width - w % 4 * 8;
-          load8<float, VECV>(states + (there > 0 ? from : 0), there, x);
-          load8<float, VECV>(dstates + (there > 0 ? from : 0), there, y);
+        sr.template store<kState>(lds + Lds::s, tid);
+        dsr.template store<kState>(lds + Lds::ds, tid);
+        zr.template store<kState>(lds + Lds::z, tid);
+        xr.template store<kState>(lds + Lds::x, tid);
+        yr.template store<PI>(lds + Lds::dy, tid);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) inner = fmaf(x[j], y[j], inner);
-        }
+        for (int i = 0; i < decltype(sr)::U; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) inner = fmaf(sr.v[i][j], dsr.v[i][j], inner);
         __syncthreads();
-        const Op<kState> zo = op_take<kState>(lds + Lds::z, RT, wave, as), xo = op_take<kState>(lds + Lds::x, RT, wave, as);
-        const Op<PI> yo = op_take<PI>(lds + Lds::dy, RT, wave, as);
+        if (c0 + 32 < p.dv) ahead(c0 + 32);
+        const Op<kState> zo = op_take<kState>(lds + Lds::z, RT, wave, at), xo = op_take<kState>(lds + Lds::x, RT, wave, at);
+        const Op<PI> yo = op_take<PI>(lds + Lds::dy, RT, wave, at);
 #pragma unroll
-        for (int m = 0; m < NT; ++m) {
-          const Op<kState> so = op_take<kState>(lds + Lds::s, NT, m, as), go = op_take<kState>(lds + Lds::ds, NT, m, as);
+        for (int m = 0; m < MT; ++m) {
+          const Op<kState> so = op_take<kState>(lds + Lds::s, NT, part * MT + m, at);
           eq[m] = op_mul<kState>(yo, so, eq[m]);
           er[m] = op_mul<kState>(xo, so, er[m]);
-          ew[m] = op_mul<kState>(zo, go, ew[m]);
+          ew[m] = op_mul<kState>(zo, op_take<kState>(lds + Lds::ds, NT, part * MT + m, at), ew[m]);
         }
 #pragma unroll
         for (int m = 0; m < RT; ++m) {
-          const Op<kState> za = op_take<kState>(lds + Lds::z, RT, m, as);
           if (m <= wave) {
+            const Op<kState> za = op_take<kState>(lds + Lds::z, RT, m, at);
             zy[m] = op_mul<kState>(za, yo, zy[m]);
             zx[m] = op_mul<kState>(za, xo, zx[m]);
           }
           if (m >= wave) {
-            yz[m] = op_mul<kState>(op_take<PI>(lds + Lds::dy, RT, m, as), zo, yz[m]);
-            xz[m] = op_mul<kState>(op_take<kState>(lds + Lds::x, RT, m, as), zo, xz[m]);
+            yz[m] = op_mul<kState>(op_take<PI>(lds + Lds::dy, RT, m, at), zo, yz[m]);
+            xz[m] = op_mul<kState>(op_take<kState>(lds + Lds::x, RT, m, at), zo, xz[m]);
           }
         }
       }
@@ -314,49 +366,52 @@ __global__ void __launch_bounds__(kChunk<T> * 4)
       for (int r = 0; r < 4; ++r) rows[r] = wk[r] = 0.0f;
       const f32x4 re = *(const f32x4*)(sc + wave * 16 + g * 4), ro = *(const f32x4*)(sc + C + wave * 16 + g * 4),
                   rb = *(const f32x4*)(sc + 2 * C + wave * 16 + g * 4);
-      Op<kState> zyp[KC], zxp[KC], yzp[KC], xzp[KC];
+      // K or Q of step 4 g + r of this tile, key 16 m + lane % 16
+      const auto value = [&](const char* from, int m, int r) {
+        float x = 0.0f;
 #pragma unroll
-      for (int ks = 0; ks < KC; ++ks) {
-        zyp[ks] = op_of<kState>(zy[2 * ks], zy[2 * ks + 1]);
-        zxp[ks] = op_of<kState>(zx[2 * ks], zx[2 * ks + 1]);
-        yzp[ks] = op_of<kState>(yz[2 * ks], yz[2 * ks + 1]);
-        xzp[ks] = op_of<kState>(xz[2 * ks], xz[2 * ks + 1]);
-      }
+        for (int o = PI - 1; o >= 0; --o)
+          x += (float)*(const __bf16*)(from + ((o * RP + wave * KS + m / 2) * 64 +
+                                               lane_place(4 * g + r, m % 2 * 2 + lane % 16 / 8)) * 16 + lane % 8 * 2);
+        return x;
+      };
 #pragma unroll
-      for (int m = 0; m < NT; ++m) {
-        float kv[4], qv[4];
-        const int d = m * 16 + lane % 16;
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int t = wave * 16 + g * 4 + r;
-          const bool there = t < n && d < p.dk;
-          kv[r] = there ? as_f32(kb[t * p.k.t + d]) : 0.0f;
-          qv[r] = there ? as_f32(qb[t * p.q.t + d]) : 0.0f;
           eq[m][r] = share_of(re[r], eq[m][r]) * p.scale;
           er[m][r] = share_of(re[r], er[m][r]);
           ew[m][r] = share_of(ro[r], ew[m][r]);
-          end = fmaf(rb[r] * kv[r], ew[m][r], end);
+          end = fmaf(rb[r] * value(lds + Lds::k, part * MT + m, r), ew[m][r], end);
         }
 #pragma unroll
-        for (int ks = 0; ks < KC; ++ks) {
-          const Op<PI> kc = op_take<PI>(lds + Lds::kc, NT * KC, m * KC + ks, at), qc = op_take<PI>(lds + Lds::qc, NT * KC, m * KC + ks, at);
-          if (ks <= wave / 2) {
-            eq[m] = op_mul<kState>(zyp[ks], kc, eq[m]);
-            er[m] = op_mul<kState>(zxp[ks], kc, er[m]);
+      for (int ks = 0; ks < KC; ++ks) {
+        const bool before = ks <= wave / 2, after = ks >= wave / 2;
+        const Op<kState> zyp = op_of<kState>(zy[2 * ks], zy[2 * ks + 1]), zxp = op_of<kState>(zx[2 * ks], zx[2 * ks + 1]);
+        const Op<kState> yzp = op_of<kState>(yz[2 * ks], yz[2 * ks + 1]), xzp = op_of<kState>(xz[2 * ks], xz[2 * ks + 1]);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const Op<PI> kc = op_turn<PI, KS>(lds + Lds::k, RP, part * MT + m, ks, even, odd);
+          if (before) {
+            eq[m] = op_mul<kState>(zyp, kc, eq[m]);
+            er[m] = op_mul<kState>(zxp, kc, er[m]);
           }
-          if (ks >= wave / 2) {
-            ew[m] = op_mul<kState>(yzp[ks], qc, ew[m]);
-            ew[m] = op_mul<kState>(xzp[ks], kc, ew[m]);
+          if (after) {
+            ew[m] = op_mul<kState>(yzp, op_turn<PI, KS>(lds + Lds::q, RP, part * MT + m, ks, even, odd), ew[m]);
+            ew[m] = op_mul<kState>(xzp, kc, ew[m]);
           }
         }
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          wk[r] = fmaf(kv[r], ew[m][r], wk[r]);
-          rows[r] += qv[r] * eq[m][r] - kv[r] * er[m][r];
+          const float kv = value(lds + Lds::k, part * MT + m, r), qv = value(lds + Lds::q, part * MT + m, r);
+          wk[r] = fmaf(kv, ew[m][r], wk[r]);
+          rows[r] += qv * eq[m][r] - kv * er[m][r];
           dq[m][r] += eq[m][r];
           dk[m][r] += fmaf(rb[r], ew[m][r], -er[m][r]);
         }
-      }
       // sums over the 16 lanes of a row, and over the workgroup
 #pragma unroll
       for (int o = 1; o < 16; o *= 2)
@@ -365,34 +420,40 @@ __global__ void __launch_bounds__(kChunk<T> * 4)
       inner = share_of(sc[C - 1], inner) + end;
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) inner += __shfl_xor(inner, o, 64);
-      if (lane == 0) red[wave] = inner;
+      if (lane == 0) red[tid / 64] = inner;
       if (lane % 16 == 0)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int t = wave * 16 + g * 4 + r;
-          dg[t] = rows[r] - rb[r] * wk[r];
-          if (t < in) out.drate[gate + (int64_t)t * p.heads] = t < n ? wk[r] : 0.0f;
+          dg[part * C + t] = rows[r] - rb[r] * wk[r];
+          kw[part * C + t] = wk[r];
         }
       __syncthreads();
       if (tid < C) {
-        float s = dg[tid];
+        float s = 0.0f, w = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) s += dg[i * C + tid], w += kw[i * C + tid];
         if (tid == C - 1)
-          for (int w = 0; w < threads / 64; ++w) s += red[w];
+#pragma unroll
+          for (int i = 0; i < THREADS / 64; ++i) s += red[i];
 #pragma unroll
         for (int o = 1; o < C; o *= 2) {
           const float x = __shfl_down(s, o, 64);
           if (tid + o < C) s += x;
         }
-        if (tid < in) out.ddecay[gate + (int64_t)tid * p.heads] = tid < n && !forgets ? s : 0.0f;
+        if (tid < in) {
+          out.ddecay[gate + (int64_t)tid * p.heads] = tid < n && !forgets ? s : 0.0f;
+          out.drate[gate + (int64_t)tid * p.heads] = tid < n ? w : 0.0f;
+        }
       }
     }
     T* const dqb = (T*)out.dq + ((b * p.steps + t0) * key_heads + kh) * p.dk;
     T* const dkb = (T*)out.dk + ((b * p.steps + t0) * key_heads + kh) * p.dk;
 #pragma unroll
-    for (int m = 0; m < NT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int t = wave * 16 + g * 4 + r, d = m * 16 + lane % 16;
+        const int t = wave * 16 + g * 4 + r, d = (part * MT + m) * 16 + lane % 16;
         if (t < in && d < p.dk) {
           dqb[(int64_t)t * key_heads * p.dk + d] = (T)dq[m][r];
           dkb[(int64_t)t * key_heads * p.dk + d] = (T)dk[m][r];

@@ -71,7 +71,7 @@ struct Delta {
   DeltaArgs a;
   int64_t chunks;            // of all heads and rows
   int64_t chunk_steps, work;   // bytes a chunk
-  int blocks, waves;
+  int blocks;   // of four tiles of 16 columns
 };
 
 template <class T>
@@ -100,12 +100,14 @@ Delta check_delta(const ms_gated_delta_desc* d, bool grad) {
   a.y = walk_of(d->y_stride, d->steps, d->heads, d->values);
   a.decay = walk_of(d->decay_stride, d->steps, d->heads, 1);
   a.rate = walk_of(d->rate_stride, d->steps, d->heads, 1);
+  // a chunk's offsets from its first step are 32 bits
+  need(std::max(a.v.t, a.y.t) < (1 << 24) && d->heads * d->values < (1 << 24),
+       "heads * values and the strides between steps of v, y and dy must be below 2^24");
   const bool half = d->dtype == MS_DTYPE_BF16;
   p.chunk_steps = half ? kChunk<__bf16> : kChunk<float>;
   a.nchunk = (d->steps + p.chunk_steps - 1) / p.chunk_steps;
   const int tiles = (int)((d->values + 15) / 16);
   p.blocks = (tiles + 3) / 4;
-  p.waves = (tiles + p.blocks - 1) / p.blocks;
   need(d->batch * d->heads <= kMaxBlocks / p.blocks - 8, "batch * heads * values is too large");
   p.chunks = d->batch * d->heads * a.nchunk;
   need(p.chunks < ((int64_t)1 << 34), "batch * heads * steps is too large");
@@ -275,9 +277,9 @@ ms_status ms_gated_delta(const ms_gated_delta_desc* d, const void* q, const void
                                dim3((unsigned)std::min(p.chunks, kMaxBlocks)), dim3(kChunk<T> * 4), 0, st, a, (const T*)q,
                                (const T*)k, decay, rate, w.chunk);
           constexpr auto scan = k_delta_scan<T, VEC, DK>;
-          constexpr size_t lds = ScanLds<T, DK, false>::bytes;
+          constexpr size_t lds = 2 * ScanLds<T, DK, false>::bytes;
           allow_lds(scan, lds);
-          hipLaunchKernelGGL(scan, scan_grid(p), dim3(64 * p.waves), lds, st, a, p.blocks, (const T*)q, (const T*)k,
+          hipLaunchKernelGGL(scan, scan_grid(p), dim3(256), lds, st, a, p.blocks, (const T*)q, (const T*)k,
                              (const T*)v, s0, (const char*)w.chunk, (T*)y, last, kept, errors);
         });
       });
@@ -320,15 +322,15 @@ ms_status ms_gated_delta_grad(const ms_gated_delta_desc* d, const void* q, const
                                dim3((unsigned)std::min(p.chunks, kMaxBlocks)), dim3(kChunk<T> * 4), 0, st, a, (const T*)q,
                                (const T*)k, decay, rate, w.chunk);
           constexpr auto back = k_delta_back<T, VEC, DK>;
-          constexpr size_t lds = ScanLds<T, DK, true>::bytes;
+          constexpr size_t lds = 2 * ScanLds<T, DK, true>::bytes;
           allow_lds(back, lds);
-          hipLaunchKernelGGL(back, scan_grid(p), dim3(64 * p.waves), lds, st, a, p.blocks, (const T*)q, (const T*)k,
+          hipLaunchKernelGGL(back, scan_grid(p), dim3(256), lds, st, a, p.blocks, (const T*)q, (const T*)k,
                              (const T*)dy, dlast, (const char*)w.chunk, (T*)dv, ds0, w.dstates, w.xs);
           if (!p.chunks) return;
-          constexpr auto grad = k_delta_grad<T, VEC, VEC, DK>;
+          constexpr auto grad = k_delta_grad<T, VEC, DK>;
           constexpr size_t more = GradLds<T, DK>::bytes;
           allow_lds(grad, more);
-          hipLaunchKernelGGL(grad, dim3((unsigned)std::min(cells, kMaxBlocks)), dim3(kChunk<T> * 4), more, st, a, (const T*)q,
+          hipLaunchKernelGGL(grad, dim3((unsigned)std::min(cells, kMaxBlocks / 2)), dim3(kGradThreads<T, DK>), more, st, a, (const T*)q,
                              (const T*)k, (const T*)dy, decay, rate, kept, kept + kept_states(p), (const float*)w.dstates,
                              (const float*)w.xs, DeltaGradOut{dq, dk, ddecay, drate});
         });

@@ -269,12 +269,13 @@ def gated_lowpass_step(v, g, state, slots=None, out=None):
 # --------------------------------------------------------------- gated delta rule
 def _walked(t, strides, inner=1):
     """t [..., heads, dim] (inner=0: [..., heads]), its strides but those of the last `inner` dimensions written
-    down; copied where the last one is not contiguous (strides of 0 stand for a packed array)."""
+    down; copied where the last one is not contiguous or steps are 2^24 apart (strides of 0 stand for a packed
+    array)."""
     if t.is_contiguous():
         return t
     n = t.dim() - inner
     apart = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(n)]
-    if (inner and t.shape[-1] > 1 and t.stride(-1) != 1) or not any(apart):
+    if (inner and t.shape[-1] > 1 and t.stride(-1) != 1) or not any(apart) or (n == 3 and apart[1] >= 1 << 24):
         return t.contiguous()
     strides[:] = apart
     return t

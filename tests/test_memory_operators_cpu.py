@@ -46,6 +46,7 @@ BIG = 1 << 40
     (dict(dtype=2), "dtype"), (dict(scale=float("nan")), "scale"), (dict(scale=1e300), "scale"),
     (dict(q_stride=(-1, 1, 1)), "strides"), (dict(k_stride=(1, -1, 1)), "strides"), (dict(v_stride=(1, 1, -1)), "strides"),
     (dict(decay_stride=(-8, 8, 1)), "strides"), (dict(rate_stride=(8, 1 << 40, 1)), "strides"),
+    (dict(heads=1024, values=16384), "2^24"), (dict(v_stride=(1, 1 << 24, 1)), "2^24"), (dict(y_stride=(1, 1 << 24, 1)), "2^24"),
     (dict(batch=1 << 22), "too large"), (dict(batch=1 << 20, steps=1 << 30), "too large")])
 def test_delta_refusals(kw, words):
     refused("ms_gated_delta", delta(**kw), *[A] * 11, BIG, words=words)
