@@ -671,8 +671,8 @@ ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rul
  *   v, y        [batch][steps][heads][values], dtype
  *   decay, rate [batch][steps][heads] float32
  *   s0, last    [batch][heads][keys][values] float32, packed; may be NULL
- *   kept        float32, ms_gated_delta_kept() elements, in a layout of the library's
- *               own; NULL if no gradient is wanted
+ *   kept        float32, ms_gated_delta_kept() elements, 16-byte aligned, in a layout of
+ *               the library's own; NULL if no gradient is wanted
  * Strides: between batch rows, steps, heads; 0, 0, 0 = packed.
  * Everything is computed in 32 bits: products run on 16-bit matrix instructions with
  * values as sums of three bf16 parts (24 bits); what passes into a bf16 y only, in two.

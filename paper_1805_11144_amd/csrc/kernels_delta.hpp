@@ -434,19 +434,66 @@ __device__ __forceinline__ bool scan_place(const DeltaArgs& p, int blocks, int64
   return bh < p.batch * p.heads;
 }
 
-// 16 steps' values of one column each, to or from results' registers: row 4 g + r of
-// result m is step 16 m + 4 g + r, of which n are there.
+// A column's values at a chunk's steps, to or from results' registers: row 4 g + r of
+// result m is step 16 m + 4 g + r, of which n are there (past them: the last one's).
 template <class T, int C>
-__device__ __forceinline__ void take_steps(const T* x, int32_t stride, int n, int g, T (&out)[C / 16][4]) {
+__device__ __forceinline__ void take_steps(const T* x, int32_t col, int32_t stride, int n, int g, T (&out)[C / 16][4]) {
+  if (n == C) {
+    const uint32_t at = g * 4 * stride + col;
 #pragma unroll
-  for (int m = 0; m < C / 16; ++m)
+    for (int m = 0; m < C / 16; ++m)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) out[m][r] = x[(uint32_t)(min(m * 16 + g * 4 + r, n - 1) * stride)];
+      for (int r = 0; r < 4; ++r) out[m][r] = (x + (m * 16 + r) * stride)[at];
+  } else {
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out[m][r] = x[(uint32_t)(min(m * 16 + g * 4 + r, n - 1) * stride + col)];
+  }
+}
+
+template <class T, int C>
+__device__ __forceinline__ void put_steps(T* x, int32_t col, int32_t stride, int n, int g, const f32x4 (&v)[C / 16]) {
+  const uint32_t at = g * 4 * stride + col;
+  if (n == C) {
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) (x + (m * 16 + r) * stride)[at] = (T)v[m][r];
+  } else {
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (m * 16 + g * 4 + r < n) (x + (m * 16 + r) * stride)[at] = (T)v[m][r];
+  }
+}
+
+// What the passes leave for k_delta_grad of a chunk: its state, or the state's
+// gradient, [columns][keys], and Z or X, [columns][C]: a column's values side by side,
+// as a lane has them, columns padded to 32 (zeros) and keys to 8.
+__host__ __device__ constexpr int pad_keys(int dk) { return (dk + 7) / 8 * 8; }
+__host__ __device__ constexpr int pad_columns(int dv) { return (dv + 31) / 32 * 32; }
+
+template <int DK>
+__device__ __forceinline__ void put_state(float* x, int dk, int col, int g, const f32x4 (&s)[DK / 16]) {
+  const int kp = pad_keys(dk);
+  float* const at = x + (uint32_t)(col * kp + g * 8);
+#pragma unroll
+  for (int m = 0; m < DK / 16; ++m)
+    if (order_of(m, g, 0) < kp) *(f32x4*)(at + order_of(m, 0, 0)) = s[m];
+}
+
+template <int C>
+__device__ __forceinline__ void put_rows(float* x, int col, int g, const f32x4 (&z)[C / 16]) {
+  float* const at = x + (uint32_t)(col * C + g * 4);
+#pragma unroll
+  for (int m = 0; m < C / 16; ++m) *(f32x4*)(at + m * 16) = z[m];
 }
 
 // The chunks of a head in order.  grid: see scan_place; a wavefront has 16 columns.
-// states: S before each chunk, errors: Z, for the gradient (NULL: not kept).
-template <class T, bool VEC, int DK>
+// KEEP: S before each chunk to `states` and Z to `errors`, for the gradient.
+template <class T, bool VEC, int DK, bool KEEP>
 __global__ void __launch_bounds__(256, 1)
     k_delta_scan(DeltaArgs p, int blocks, const T* q, const T* k, const T* v, const float* s0, const char* work, T* y,
                  float* last, float* states, float* errors) {
@@ -462,11 +509,11 @@ __global__ void __launch_bounds__(256, 1)
   const int64_t b = bh / p.heads;
   const int head = (int)(bh % p.heads), kh = head / p.group;
   const int first = (block * 4 + tid / 64) * 16, col = first + lane % 16, mcol = min(col, p.dv - 1);
-  const bool mine = col < p.dv, some = first < p.dv;
+  const bool mine = col < p.dv, some = first < (KEEP ? pad_columns(p.dv) : p.dv);
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
   const int chunks = (len + C - 1) / C;
-  const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *vp = v + b * p.v.b + head * p.v.h + mcol;
-  T* yp = y + b * p.y.b + head * p.y.h + mcol;
+  const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *vp = v + b * p.v.b + head * p.v.h;
+  T* yp = y + b * p.y.b + head * p.y.h;
   const char* wp = work + bh * p.nchunk * Work::bytes;
   const int32_t vt = (int32_t)p.v.t, yt = (int32_t)p.y.t;
   f32x4 s[DK / 16];
@@ -484,7 +531,7 @@ __global__ void __launch_bounds__(256, 1)
     fetch_work<Work::bytes>(wp, lds + Lds::work, tid);
     kr.load(kp, p.k.t, n, p.dk, tid);
     qr.load(qp, p.q.t, n, p.dk, tid);
-    take_steps<T, C>(vp, vt, n, g, vr);
+    take_steps<T, C>(vp, mcol, vt, n, g, vr);
     kr.store(lds + Lds::k, tid);
     qr.store(lds + Lds::q, tid);
   }
@@ -496,24 +543,17 @@ __global__ void __launch_bounds__(256, 1)
 #pragma unroll
     for (int m = 0; m < C / 16; ++m)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[m][r] = m * 16 + g * 4 + r < n ? as_f32(vr[m][r]) : 0.0f;
+      for (int r = 0; r < 4; ++r) z[m][r] = mine && m * 16 + g * 4 + r < n ? as_f32(vr[m][r]) : 0.0f;
     __syncthreads();   // this chunk's operands are there, and the other half is read
     if (ahead > 0) {
       fetch_work<Work::bytes>(wp + (int64_t)(chunk + 1) * Work::bytes, next + Lds::work, tid);
       kp += C * p.k.t, qp += C * p.q.t, vp += C * p.v.t;
       kr.load(kp, p.k.t, ahead, p.dk, tid);
       qr.load(qp, p.q.t, ahead, p.dk, tid);
-      take_steps<T, C>(vp, vt, ahead, g, vr);
+      take_steps<T, C>(vp, mcol, vt, ahead, g, vr);
     }
     if (some) {
-      if (states && mine) {
-        float* sp = states + (bh * p.nchunk + chunk) * p.dk * p.dv + col;
-#pragma unroll
-        for (int m = 0; m < DK / 16; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (order_of(m, g, r) < p.dk) sp[(uint32_t)(order_of(m, g, r) * p.dv)] = s[m][r];
-      }
+      if (KEEP) put_state<DK>(states + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
       const float* e = (const float*)(here + Lds::work + Work::scales);
       Op<kState> sp[KS];
 #pragma unroll
@@ -541,13 +581,7 @@ __global__ void __launch_bounds__(256, 1)
           z[m] = op_mul<kState>(
               op_take<kState>(here + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zp[ks], z[m]);
       }
-      if (errors && mine) {
-        float* ep = errors + ((bh * p.nchunk + chunk) * C) * p.dv + col;
-#pragma unroll
-        for (int m = 0; m < C / 16; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) ep[(uint32_t)((m * 16 + g * 4 + r) * p.dv)] = z[m][r];
-      }
+      if (KEEP) put_rows<C>(errors + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, z);
       Op<kOut<T>> zo[C / 32];
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) zo[ks] = op_of<kOut<T>>(z[2 * ks], z[2 * ks + 1]);
@@ -561,12 +595,7 @@ __global__ void __launch_bounds__(256, 1)
 #pragma unroll
         for (int r = 0; r < 4; ++r) z[m][r] *= om[r] * bm[r];
       }
-      if (mine)
-#pragma unroll
-        for (int m = 0; m < C / 16; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (m * 16 + g * 4 + r < n) yp[(uint32_t)((m * 16 + g * 4 + r) * yt)] = (T)o[m][r];
+      if (mine) put_steps<T, C>(yp, col, yt, n, g, o);
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
       const float keep = e[C - 1];

@@ -39,11 +39,11 @@ __global__ void __launch_bounds__(256, 1)
   const int64_t b = bh / p.heads;
   const int head = (int)(bh % p.heads), kh = head / p.group;
   const int first = (block * 4 + tid / 64) * 16, col = first + lane % 16, mcol = min(col, p.dv - 1);
-  const bool mine = col < p.dv, some = first < p.dv;
+  const bool mine = col < p.dv, some = first < pad_columns(p.dv);
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
   const int chunks = (len + C - 1) / C;
-  const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *yp = dy + b * p.y.b + head * p.y.h + mcol;
-  T* const vp = dv + (b * p.steps * p.heads + head) * p.dv + mcol;
+  const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *yp = dy + b * p.y.b + head * p.y.h;
+  T* const vp = dv + (b * p.steps * p.heads + head) * p.dv;
   const char* wp = work + bh * p.nchunk * Work::bytes;
   const int32_t yt = (int32_t)p.y.t, vt = p.heads * p.dv;
   f32x4 s[DK / 16];
@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(256, 1)
       s[m][r] = dlast && mine && d < p.dk ? dlast[(bh * p.dk + d) * p.dv + col] : 0.0f;
     }
   if (mine)
-    for (int64_t t = len + g; t < p.steps; t += 4) vp[t * vt] = (T)0.0f;
+    for (int64_t t = len + g; t < p.steps; t += 4) vp[t * vt + col] = (T)0.0f;
   RowsInFlight<T, VEC, C, DK, 256> kr, qr;
   T yr[C / 16][4];
   const auto ahead_of = [&](int chunk, char* to) {
@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(256, 1)
     fetch_work<Work::bytes>(wp + (int64_t)chunk * Work::bytes, to + Lds::work, tid);
     kr.load(kp + t0 * p.k.t, p.k.t, n, p.dk, tid);
     qr.load(qp + t0 * p.q.t, p.q.t, n, p.dk, tid);
-    take_steps<T, C>(yp + t0 * p.y.t, yt, n, g, yr);
+    take_steps<T, C>(yp + t0 * p.y.t, mcol, yt, n, g, yr);
   };
   if (chunks > 0) {
     char* const to = lds + ((chunks - 1) & 1) * Lds::bytes;
@@ -80,18 +80,11 @@ __global__ void __launch_bounds__(256, 1)
 #pragma unroll
     for (int m = 0; m < C / 16; ++m)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) dyr[m][r] = m * 16 + g * 4 + r < n ? as_f32(yr[m][r]) : 0.0f;
+      for (int r = 0; r < 4; ++r) dyr[m][r] = mine && m * 16 + g * 4 + r < n ? as_f32(yr[m][r]) : 0.0f;
     __syncthreads();   // this chunk's operands are there, and the other half is read
     if (chunk > 0) ahead_of(chunk - 1, next);
     if (some) {
-      if (mine) {
-        float* sp = dstates + (bh * p.nchunk + chunk) * p.dk * p.dv + col;
-#pragma unroll
-        for (int m = 0; m < DK / 16; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (order_of(m, g, r) < p.dk) sp[(uint32_t)(order_of(m, g, r) * p.dv)] = s[m][r];
-      }
+      put_state<DK>(dstates + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
       const float* e = (const float*)(here + Lds::work + Work::scales);
       {
         Op<kState> sp[KS];
@@ -125,8 +118,6 @@ __global__ void __launch_bounds__(256, 1)
       Op<kState> xp[C / 32];
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
-      float* ep = xs + ((bh * p.nchunk + chunk) * C) * p.dv + mcol;
-      T* vc = vp + (int64_t)chunk * C * vt;
 #pragma unroll
       for (int m = 0; m < C / 16; ++m) {
         x[m] = zero4();
@@ -134,15 +125,14 @@ __global__ void __launch_bounds__(256, 1)
         for (int ks = m / 2; ks < C / 32; ++ks)
           x[m] = op_mul<kState>(op_take<kState>(here + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, true>(m, ks), lane),
                                 xp[ks], x[m]);
+      }
+      put_rows<C>(xs + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, x);
+      if (mine) put_steps<T, C>(vp + (int64_t)chunk * C * vt, col, vt, n, g, x);
+#pragma unroll
+      for (int m = 0; m < C / 16; ++m) {
         const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = m * 16 + g * 4 + r;
-          if (mine) ep[(uint32_t)(t * p.dv)] = x[m][r];
-          if (mine && t < n) vc[(uint32_t)(t * vt)] = (T)x[m][r];
-          x[m][r] *= -em[r];
-          dyr[m][r] *= p.scale * em[r];
-        }
+        for (int r = 0; r < 4; ++r) x[m][r] *= -em[r], dyr[m][r] *= p.scale * em[r];
       }
       Op<kState> dp[C / 32];
 #pragma unroll
@@ -183,12 +173,16 @@ constexpr int kGradParts = kChunk<T> == 64 ? 2 : DK >= 64 ? 4 : 2;
 template <class T, int DK>
 constexpr int kGradThreads = kChunk<T> * 4 * kGradParts<T, DK>;
 
+// 32 columns of a chunk at a time: rows of K and Q, then rows of S, dS (a column's
+// keys), Z, X (a column's steps) and dY (a step's columns); then, in their place, the
+// four products as operands, 16 steps x 32 steps a piece.
 template <class T, int DK>
 struct GradLds {
-  static constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T, DK>;
+  static constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T, DK>, product = kState * tri_pieces(C) * 1024;
   static constexpr int k = 0, q = k + PI * C * DK * 2, s = q + PI * C * DK * 2, ds = s + kState * DK * 64,
                        z = ds + kState * DK * 64, x = z + kState * C * 64, dy = x + kState * C * 64,
-                       sums = dy + PI * C * 64, bytes = sums + (3 * C + 2 * NP * C + 16) * 4 + C * 8;
+                       products = s, after = dy + PI * C * 64 > s + 4 * product ? dy + PI * C * 64 : s + 4 * product,
+                       sums = after, bytes = sums + (3 * C + 2 * NP * C + 16) * 4 + C * 8;
 };
 
 struct DeltaGradOut {
@@ -196,10 +190,45 @@ struct DeltaGradOut {
   float *ddecay, *drate;
 };
 
-// 32 columns of rows of the state, its gradient, Z, X and dY, on their way to LDS.
-template <class T, bool VEC, int ROWS, int THREADS>
+// The row in LDS of column j of 32: a transposing operand's lanes of group g take rows
+// 4 g .. and 16 + 4 g .., and get columns 8 g .. 8 g + 7, as rows' operands do.
+__device__ __forceinline__ int column_row(int j) { return j / 8 * 4 + j % 4 + j % 8 / 4 * 16; }
+
+// 32 columns of COLS values side by side (`there` of them in memory), on their way to LDS.
+template <int COLS, int THREADS>
 struct SlabInFlight {
-  static constexpr int U = (ROWS * 4 + THREADS - 1) / THREADS;
+  static constexpr int N = 32 * COLS / 8, U = (N + THREADS - 1) / THREADS, KS = COLS / 32;
+  f32x4 v[U][2];
+
+  __device__ __forceinline__ void load(const float* x, int there, int tid) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = tid + i * THREADS, row = u / (COLS / 8), c = u % (COLS / 8) * 8;
+      v[i][0] = v[i][1] = zero4();
+      if ((N % THREADS == 0 || u < N) && c < there) {
+        const f32x4* from = (const f32x4*)(x + (uint32_t)(row * there + c));
+        v[i][0] = from[0], v[i][1] = from[1];
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(char* lds, int tid) const {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = tid + i * THREADS, row = column_row(u / (COLS / 8)), c = u % (COLS / 8);
+      if (N % THREADS != 0 && u >= N) continue;
+      const Op<kState> o = op_of<kState>(v[i][0], v[i][1]);
+#pragma unroll
+      for (int p = 0; p < kState; ++p)
+        *(bf16x8*)(lds + ((p * 2 * KS + row / 16 * KS + c / 4) * 64 + lane_place(row % 16, c % 4)) * 16) = o.p[p];
+    }
+  }
+};
+
+// 32 columns of dY, rows of steps, the same way.
+template <class T, bool VEC, int C, int THREADS>
+struct StepsInFlight {
+  static constexpr int N = C * 4, U = (N + THREADS - 1) / THREADS;
   float v[U][8];
 
   __device__ __forceinline__ void load(const T* x, int64_t stride, int there, int width, int tid) {
@@ -211,24 +240,24 @@ struct SlabInFlight {
     }
   }
 
-  template <int P>
   __device__ __forceinline__ void store(char* lds, int tid) const {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = tid + i * THREADS, row = u / 4;
-      if (ROWS * 4 % THREADS != 0 && u >= ROWS * 4) continue;
-      const Op<P> o = op_of<P>(v[i]);
+      if (N % THREADS != 0 && u >= N) continue;
+      const Op<kIn<T>> o = op_of<kIn<T>>(v[i]);
 #pragma unroll
-      for (int q = 0; q < P; ++q)
-        *(bf16x8*)(lds + ((q * (ROWS / 16) + row / 16) * 64 + lane_place(row % 16, u % 4)) * 16) = o.p[q];
+      for (int p = 0; p < kIn<T>; ++p)
+        *(bf16x8*)(lds + ((p * (C / 16) + row / 16) * 64 + lane_place(row % 16, u % 4)) * 16) = o.p[p];
     }
   }
 };
 
 // dQ, dK and the gates of a chunk of one key head, its heads one after the other.  A
-// wavefront has 16 steps and a part of the keys; the steps are rows of its results and
-// columns of the four products z dy', z x', dy z', x z' over the values, whose sums
-// are the operands that multiply K and Q.
+// wavefront has 16 steps and a part of the keys.  The four products over the values
+// z dy', z x' (of earlier steps with later ones), dy z', x z' (of later with earlier)
+// are computed beside them, in tiles dealt to all wavefronts, and then are the
+// operands that multiply K and Q.
 template <class T, bool VEC, int DK>
 __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
     k_delta_grad(DeltaArgs p, const T* q, const T* k, const T* dy, const float* decay, const float* rate,
@@ -236,15 +265,17 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
   using Lds = GradLds<T, DK>;
   constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T, DK>, THREADS = kGradThreads<T, DK>;
   constexpr int RT = C / 16, KC = C / 32, NT = DK / 16, MT = NT / NP, KS = DK / 32, RP = RT * KS;
+  constexpr int JOBS = RT * (RT + 1), WAVES = THREADS / 64, MINE = (JOBS + WAVES - 1) / WAVES;
   extern __shared__ __align__(16) char lds[];
   float* const sc = (float*)(lds + Lds::sums);   // e, o, b
   float* const dg = sc + 3 * C;                  // gradients of G, and k W, by parts
   float* const kw = dg + NP * C;
   float* const red = kw + NP * C;
   double* const sum = (double*)(red + 16);
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64 % RT, part = tid / 64 / RT, g = lane / 16;
+  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16;
+  const int all_waves = __builtin_amdgcn_readfirstlane(tid / 64), wave = all_waves % RT, part = all_waves / RT;
   const int at = lane_place(lane % 16, g), even = turn_place<false>(lane), odd = turn_odd<false>(lane);
-  const int key_heads = p.heads / p.group;
+  const int key_heads = p.heads / p.group, kp = pad_keys(p.dk), cols = pad_columns(p.dv);
   const int64_t all = p.batch * key_heads * p.nchunk;
   for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
     const int64_t chunk = u % p.nchunk, b = u / p.nchunk / key_heads, t0 = chunk * C;
@@ -254,14 +285,6 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
     f32x4 dq[MT], dk[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) dq[m] = dk[m] = zero4();
-    __syncthreads();
-    if (n > 0) {
-      RowsInFlight<T, VEC, C, DK, THREADS> kr, qr;
-      kr.load(k + b * p.k.b + t0 * p.k.t + kh * p.k.h, p.k.t, n, p.dk, tid);
-      qr.load(q + b * p.q.b + t0 * p.q.t + kh * p.q.h, p.q.t, n, p.dk, tid);
-      kr.store(lds + Lds::k, tid);
-      qr.store(lds + Lds::q, tid);
-    }
     for (int h = 0; h < p.group; ++h) {
       const int head = kh * p.group + h;
       const int64_t bh = b * p.heads + head, cell = bh * p.nchunk + chunk, gate = (b * p.steps + t0) * p.heads + head;
@@ -270,17 +293,30 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
           out.ddecay[gate + (int64_t)t * p.heads] = out.drate[gate + (int64_t)t * p.heads] = 0.0f;
         continue;
       }
-      SlabInFlight<float, VEC, DK, THREADS> sr, dsr;
-      SlabInFlight<float, VEC, C, THREADS> zr, xr;
-      SlabInFlight<T, VEC, C, THREADS> yr;
+      SlabInFlight<DK, THREADS> sr, dsr;
+      SlabInFlight<C, THREADS> zr, xr;
+      StepsInFlight<T, VEC, C, THREADS> yr;
+      const float *sp = states + cell * kp * cols, *dsp = dstates + cell * kp * cols, *zp = errors + cell * C * cols,
+                  *xp = xs + cell * C * cols;
+      const T* yp = dy + b * p.y.b + t0 * p.y.t + head * p.y.h;
       const auto ahead = [&](int c) {
-        sr.load(states + cell * p.dk * p.dv + c, p.dv, p.dk, p.dv - c, tid);
-        dsr.load(dstates + cell * p.dk * p.dv + c, p.dv, p.dk, p.dv - c, tid);
-        zr.load(errors + cell * C * p.dv + c, p.dv, n, p.dv - c, tid);
-        xr.load(xs + cell * C * p.dv + c, p.dv, n, p.dv - c, tid);
-        yr.load(dy + b * p.y.b + t0 * p.y.t + head * p.y.h + c, p.y.t, n, p.dv - c, tid);
+        sr.load(sp + c * kp, kp, tid);
+        dsr.load(dsp + c * kp, kp, tid);
+        zr.load(zp + c * C, C, tid);
+        xr.load(xp + c * C, C, tid);
+        yr.load(yp + c, p.y.t, n, p.dv - c, tid);
       };
-      ahead(0);
+      if (h == 0) {
+        RowsInFlight<T, VEC, C, DK, THREADS> kr, qr;
+        kr.load(k + b * p.k.b + t0 * p.k.t + kh * p.k.h, p.k.t, n, p.dk, tid);
+        qr.load(q + b * p.q.b + t0 * p.q.t + kh * p.q.h, p.q.t, n, p.dk, tid);
+        ahead(0);
+        __syncthreads();   // what was there is read
+        kr.store(lds + Lds::k, tid);
+        qr.store(lds + Lds::q, tid);
+      } else {
+        ahead(0);
+      }
       bool forgets = false;
       if (tid < C) {
         double d = 0.0;
@@ -304,114 +340,170 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
         sc[2 * C + tid] = r;
       }
       // sums over the values, 32 at a time
-      f32x4 eq[MT], er[MT], ew[MT], zy[RT], zx[RT], yz[RT], xz[RT];
+      f32x4 eq[MT], er[MT], ew[MT], py[MINE], px[MINE];
       float inner = 0.0f;   // <dS, S>, this thread's part
 #pragma unroll
       for (int m = 0; m < MT; ++m) eq[m] = er[m] = ew[m] = zero4();
 #pragma unroll
-      for (int m = 0; m < RT; ++m) zy[m] = zx[m] = yz[m] = xz[m] = zero4();
-      for (int c0 = 0; c0 < p.dv; c0 += 32) {
+      for (int i = 0; i < MINE; ++i) py[i] = px[i] = zero4();
+      for (int c0 = 0; c0 < cols; c0 += 32) {
         __syncthreads();
-        sr.template store<kState>(lds + Lds::s, tid);
-        dsr.template store<kState>(lds + Lds::ds, tid);
-        zr.template store<kState>(lds + Lds::z, tid);
-        xr.template store<kState>(lds + Lds::x, tid);
-        yr.template store<PI>(lds + Lds::dy, tid);
+        sr.store(lds + Lds::s, tid);
+        dsr.store(lds + Lds::ds, tid);
+        zr.store(lds + Lds::z, tid);
+        xr.store(lds + Lds::x, tid);
+        yr.store(lds + Lds::dy, tid);
 #pragma unroll
         for (int i = 0; i < decltype(sr)::U; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) inner = fmaf(sr.v[i][j], dsr.v[i][j], inner);
+          for (int j = 0; j < 8; ++j) inner = fmaf(sr.v[i][j / 4][j % 4], dsr.v[i][j / 4][j % 4], inner);
         __syncthreads();
-        if (c0 + 32 < p.dv) ahead(c0 + 32);
-        const Op<kState> zo = op_take<kState>(lds + Lds::z, RT, wave, at), xo = op_take<kState>(lds + Lds::x, RT, wave, at);
-        const Op<PI> yo = op_take<PI>(lds + Lds::dy, RT, wave, at);
+        if (c0 + 32 < cols) ahead(c0 + 32);
+        {
+          const Op<kState> zo = op_turn<kState, KC>(lds + Lds::z, 2 * KC, wave, 0, even, odd),
+                           xo = op_turn<kState, KC>(lds + Lds::x, 2 * KC, wave, 0, even, odd);
+          const Op<PI> yo = op_take<PI>(lds + Lds::dy, RT, wave, at);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const Op<kState> so = op_take<kState>(lds + Lds::s, NT, part * MT + m, at);
-          eq[m] = op_mul<kState>(yo, so, eq[m]);
-          er[m] = op_mul<kState>(xo, so, er[m]);
-          ew[m] = op_mul<kState>(zo, op_take<kState>(lds + Lds::ds, NT, part * MT + m, at), ew[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < RT; ++m) {
-          if (m <= wave) {
-            const Op<kState> za = op_take<kState>(lds + Lds::z, RT, m, at);
-            zy[m] = op_mul<kState>(za, yo, zy[m]);
-            zx[m] = op_mul<kState>(za, xo, zx[m]);
+          for (int m = 0; m < MT; ++m) {
+            const Op<kState> so = op_turn<kState, KS>(lds + Lds::s, 2 * KS, part * MT + m, 0, even, odd);
+            eq[m] = op_mul<kState>(yo, so, eq[m]);
+            er[m] = op_mul<kState>(xo, so, er[m]);
+            ew[m] = op_mul<kState>(zo, op_turn<kState, KS>(lds + Lds::ds, 2 * KS, part * MT + m, 0, even, odd), ew[m]);
           }
-          if (m >= wave) {
-            yz[m] = op_mul<kState>(op_take<PI>(lds + Lds::dy, RT, m, at), zo, yz[m]);
-            xz[m] = op_mul<kState>(op_take<kState>(lds + Lds::x, RT, m, at), zo, xz[m]);
+        }
+        // tile i of the first half: steps 16 a .. of Z against 16 c .. of dY and X, a <= c;
+        // of the second: 16 c .. of dY and X against 16 a .. of Z
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+          const int job = all_waves + i * WAVES;
+          if (job >= JOBS) continue;
+          const int half = job < JOBS / 2 ? job : job - JOBS / 2;
+          const int c = half < 1 ? 0 : half < 3 ? 1 : half < 6 ? 2 : 3, a = half - c * (c + 1) / 2;
+          const Op<kState> zo = op_turn<kState, KC>(lds + Lds::z, 2 * KC, a, 0, even, odd),
+                           xo = op_turn<kState, KC>(lds + Lds::x, 2 * KC, c, 0, even, odd);
+          const Op<PI> yo = op_take<PI>(lds + Lds::dy, RT, c, at);
+          if (job < JOBS / 2) {
+            py[i] = op_mul<kState>(zo, yo, py[i]);
+            px[i] = op_mul<kState>(zo, xo, px[i]);
+          } else {
+            py[i] = op_mul<kState>(yo, zo, py[i]);
+            px[i] = op_mul<kState>(xo, zo, px[i]);
           }
         }
       }
-      // this lane's column of the four products is step `own`
-      const int own = wave * 16 + lane % 16;
-      const double here = sum[own];
+      __syncthreads();   // the products take the slabs' place
 #pragma unroll
-      for (int m = 0; m < RT; ++m)
+      for (int i = 0; i < MINE; ++i) {
+        const int job = all_waves + i * WAVES;
+        if (job >= JOBS) continue;
+        const bool first = job < JOBS / 2;
+        const int half = first ? job : job - JOBS / 2;
+        const int c = half < 1 ? 0 : half < 3 ? 1 : half < 6 ? 2 : 3, a = half - c * (c + 1) / 2;
+        // the operand's row is the lane's column, its 32 columns rows of this result and the next
+        const int mt = first ? c : a, kt = first ? a : c, row = mt * 16 + lane % 16;
+        const int piece = (first ? tri_piece<C, false>(mt, kt / 2) : tri_piece<C, true>(mt, kt / 2)) * 64 + lane;
+        const double mine = sum[row];
+        f32x4 y = py[i], x = px[i];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int t = m * 16 + g * 4 + r;
-          const float before = t <= own ? __builtin_amdgcn_exp2f((float)(here - sum[t])) * sc[2 * C + t] : 0.0f;
-          const float after = t >= own ? __builtin_amdgcn_exp2f((float)(sum[t] - here)) : 0.0f;
-          zy[m][r] = t <= own ? zy[m][r] * before * p.scale : 0.0f;
-          zx[m][r] = t < own ? zx[m][r] * before : 0.0f;
-          yz[m][r] = t >= own ? yz[m][r] * after * p.scale : 0.0f;
-          xz[m][r] = t > own ? -xz[m][r] * after : 0.0f;
+          const int t = kt * 16 + g * 4 + r;
+          const bool there = first ? t <= row : t >= row;
+          const float d = there ? __builtin_amdgcn_exp2f((float)(first ? mine - sum[t] : sum[t] - mine)) : 0.0f;
+          const float w = first ? d * sc[2 * C + t] : d;
+          y[r] = there ? y[r] * w * p.scale : 0.0f;
+          x[r] = there && t != row ? (first ? x[r] * w : -x[r] * w) : 0.0f;
         }
+        char* const to = lds + Lds::products + (first ? 0 : 2 * Lds::product) + piece * 16 + kt % 2 * 8;
+#pragma unroll
+        for (int o = 0; o < kState; ++o) {
+          bf16x4 hy, hx;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            hy[r] = (__bf16)y[r], hx[r] = (__bf16)x[r];
+            y[r] -= (float)hy[r], x[r] -= (float)hx[r];
+          }
+          *(bf16x4*)(to + o * tri_pieces(C) * 1024) = hy;
+          *(bf16x4*)(to + Lds::product + o * tri_pieces(C) * 1024) = hx;
+        }
+      }
+      // the halves of a piece on the diagonal that no tile fills
+      if (all_waves < RT) {
+        const int other = wave ^ 1;
+        const bool first = wave % 2 == 0;   // rows of an even tile have nothing from the next one, and of an odd one nothing after
+        const int piece = (first ? tri_piece<C, false>(wave, wave / 2) : tri_piece<C, true>(wave, wave / 2)) * 64 + lane;
+        char* const to = lds + Lds::products + (first ? 0 : 2 * Lds::product) + piece * 16 + other % 2 * 8;
+#pragma unroll
+        for (int o = 0; o < kState; ++o)
+          *(bf16x4*)(to + o * tri_pieces(C) * 1024) = *(bf16x4*)(to + Lds::product + o * tri_pieces(C) * 1024) = bf16x4{};
+      }
       float end = 0.0f;   // o[t] b[t] k[t] dS z[t], this lane's part: <dS, K' diag(o b) Z>
       float rows[4], wk[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) rows[r] = wk[r] = 0.0f;
       const f32x4 re = *(const f32x4*)(sc + wave * 16 + g * 4), ro = *(const f32x4*)(sc + C + wave * 16 + g * 4),
                   rb = *(const f32x4*)(sc + 2 * C + wave * 16 + g * 4);
-      // K or Q of step 4 g + r of this tile, key 16 m + lane % 16
-      const auto value = [&](const char* from, int m, int r) {
-        float x = 0.0f;
+      // K or Q of this tile's steps 4 g + r, key 16 m + lane % 16: a transposing read of 4 rows
+      const auto values = [&](const char* from, int m) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4* From;
+        f32x4 x = zero4();
 #pragma unroll
-        for (int o = PI - 1; o >= 0; --o)
-          x += (float)*(const __bf16*)(from + ((o * RP + wave * KS + m / 2) * 64 +
-                                               lane_place(4 * g + r, m % 2 * 2 + lane % 16 / 8)) * 16 + lane % 8 * 2);
+        for (int o = PI - 1; o >= 0; --o) {
+          const char* a = from + (o * RP + wave * KS + m / 2) * 1024 + (m % 2 ? odd : even);
+          const bf16x4 h = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)a));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[r] += (float)h[r];
+        }
         return x;
       };
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int m = 0; m < MT; ++m) {
+        const f32x4 kv = values(lds + Lds::k, part * MT + m);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           eq[m][r] = share_of(re[r], eq[m][r]) * p.scale;
           er[m][r] = share_of(re[r], er[m][r]);
           ew[m][r] = share_of(ro[r], ew[m][r]);
-          end = fmaf(rb[r] * value(lds + Lds::k, part * MT + m, r), ew[m][r], end);
+          end = fmaf(rb[r] * kv[r], ew[m][r], end);
         }
+      }
+      __syncthreads();
 #pragma unroll
       for (int ks = 0; ks < KC; ++ks) {
-        const bool before = ks <= wave / 2, after = ks >= wave / 2;
-        const Op<kState> zyp = op_of<kState>(zy[2 * ks], zy[2 * ks + 1]), zxp = op_of<kState>(zx[2 * ks], zx[2 * ks + 1]);
-        const Op<kState> yzp = op_of<kState>(yz[2 * ks], yz[2 * ks + 1]), xzp = op_of<kState>(xz[2 * ks], xz[2 * ks + 1]);
+        const char* const products = lds + Lds::products;
+        if (ks <= wave / 2) {
+          const int piece = tri_piece<C, false>(wave, ks);
+          const Op<kState> y = op_take<kState>(products, tri_pieces(C), piece, lane),
+                           x = op_take<kState>(products + Lds::product, tri_pieces(C), piece, lane);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const Op<PI> kc = op_turn<PI, KS>(lds + Lds::k, RP, part * MT + m, ks, even, odd);
-          if (before) {
-            eq[m] = op_mul<kState>(zyp, kc, eq[m]);
-            er[m] = op_mul<kState>(zxp, kc, er[m]);
+          for (int m = 0; m < MT; ++m) {
+            const Op<PI> kc = op_turn<PI, KS>(lds + Lds::k, RP, part * MT + m, ks, even, odd);
+            eq[m] = op_mul<kState>(y, kc, eq[m]);
+            er[m] = op_mul<kState>(x, kc, er[m]);
           }
-          if (after) {
-            ew[m] = op_mul<kState>(yzp, op_turn<PI, KS>(lds + Lds::q, RP, part * MT + m, ks, even, odd), ew[m]);
-            ew[m] = op_mul<kState>(xzp, kc, ew[m]);
+        }
+        if (ks >= wave / 2) {
+          const int piece = tri_piece<C, true>(wave, ks);
+          const Op<kState> y = op_take<kState>(products + 2 * Lds::product, tri_pieces(C), piece, lane),
+                           x = op_take<kState>(products + 3 * Lds::product, tri_pieces(C), piece, lane);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            ew[m] = op_mul<kState>(y, op_turn<PI, KS>(lds + Lds::q, RP, part * MT + m, ks, even, odd), ew[m]);
+            ew[m] = op_mul<kState>(x, op_turn<PI, KS>(lds + Lds::k, RP, part * MT + m, ks, even, odd), ew[m]);
           }
         }
       }
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int m = 0; m < MT; ++m) {
+        const f32x4 kv = values(lds + Lds::k, part * MT + m), qv = values(lds + Lds::q, part * MT + m);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float kv = value(lds + Lds::k, part * MT + m, r), qv = value(lds + Lds::q, part * MT + m, r);
-          wk[r] = fmaf(kv, ew[m][r], wk[r]);
-          rows[r] += qv * eq[m][r] - kv * er[m][r];
+          wk[r] = fmaf(kv[r], ew[m][r], wk[r]);
+          rows[r] += qv[r] * eq[m][r] - kv[r] * er[m][r];
           dq[m][r] += eq[m][r];
           dk[m][r] += fmaf(rb[r], ew[m][r], -er[m][r]);
         }
+      }
       // sums over the 16 lanes of a row, and over the workgroup
 #pragma unroll
       for (int o = 1; o < 16; o *= 2)
@@ -420,7 +512,7 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
       inner = share_of(sc[C - 1], inner) + end;
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) inner += __shfl_xor(inner, o, 64);
-      if (lane == 0) red[tid / 64] = inner;
+      if (lane == 0) red[all_waves] = inner;
       if (lane % 16 == 0)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -435,7 +527,7 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
         for (int i = 0; i < NP; ++i) s += dg[i * C + tid], w += kw[i * C + tid];
         if (tid == C - 1)
 #pragma unroll
-          for (int i = 0; i < THREADS / 64; ++i) s += red[i];
+          for (int i = 0; i < WAVES; ++i) s += red[i];
 #pragma unroll
         for (int o = 1; o < C; o *= 2) {
           const float x = __shfl_down(s, o, 64);

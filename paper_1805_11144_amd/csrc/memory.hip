@@ -116,8 +116,8 @@ Delta check_delta(const ms_gated_delta_desc* d, bool grad) {
 }
 
 // What the gradient starts from: each chunk's state, then the errors.
-int64_t kept_states(const Delta& p) { return p.chunks * p.a.dk * p.a.dv; }
-int64_t kept_all(const Delta& p) { return kept_states(p) + p.chunks * p.chunk_steps * p.a.dv; }
+int64_t kept_states(const Delta& p) { return p.chunks * pad_keys(p.a.dk) * pad_columns(p.a.dv); }
+int64_t kept_rows(const Delta& p) { return p.chunks * p.chunk_steps * pad_columns(p.a.dv); }
 
 struct DeltaWork {
   char* chunk;
@@ -132,7 +132,7 @@ DeltaWork delta_work(const Delta& p, bool grad, void* ws) {
     w.chunk = c.take<char>(p.chunks * p.work);
     if (grad) {
       w.dstates = c.take<float>(kept_states(p));
-      w.xs = c.take<float>(p.chunks * p.chunk_steps * p.a.dv);
+      w.xs = c.take<float>(kept_rows(p));
     }
   }
   w.bytes = c.used;
@@ -234,7 +234,7 @@ ms_status ms_gated_delta_kept(const ms_gated_delta_desc* d, int64_t* elements_ou
   return guarded([&] {
     const Delta p = check_delta(d, false);
     need(elements_out != nullptr, "NULL output");
-    *elements_out = kept_all(p);
+    *elements_out = kept_states(p) + kept_rows(p);
   });
 }
 
@@ -260,6 +260,7 @@ ms_status ms_gated_delta(const ms_gated_delta_desc* d, const void* q, const void
     for (const void* x : {(const void*)decay, (const void*)rate, (const void*)s0, (const void*)lengths, (const void*)last,
                           (const void*)kept})
       need_aligned(x, 4, "decay, rate, s0, lengths, last or kept");
+    need((uintptr_t)kept % 16 == 0, "kept must be 16-byte aligned");
     const DeltaWork w = delta_work(p, false, workspace);
     need_workspace(workspace, workspace_bytes, w.bytes);
     DeviceGuard dg(d->device);
@@ -276,11 +277,13 @@ ms_status ms_gated_delta(const ms_gated_delta_desc* d, const void* q, const void
             hipLaunchKernelGGL(HIP_KERNEL_NAME(k_delta_chunk<T, VEC, DK, false>),
                                dim3((unsigned)std::min(p.chunks, kMaxBlocks)), dim3(kChunk<T> * 4), 0, st, a, (const T*)q,
                                (const T*)k, decay, rate, w.chunk);
-          constexpr auto scan = k_delta_scan<T, VEC, DK>;
-          constexpr size_t lds = 2 * ScanLds<T, DK, false>::bytes;
-          allow_lds(scan, lds);
-          hipLaunchKernelGGL(scan, scan_grid(p), dim3(256), lds, st, a, p.blocks, (const T*)q, (const T*)k,
-                             (const T*)v, s0, (const char*)w.chunk, (T*)y, last, kept, errors);
+          with_flag(kept != nullptr, [&](auto keep) {
+            constexpr auto scan = k_delta_scan<T, VEC, DK, decltype(keep)::value>;
+            constexpr size_t lds = 2 * ScanLds<T, DK, false>::bytes;
+            allow_lds(scan, lds);
+            hipLaunchKernelGGL(scan, scan_grid(p), dim3(256), lds, st, a, p.blocks, (const T*)q, (const T*)k, (const T*)v, s0,
+                               (const char*)w.chunk, (T*)y, last, kept, errors);
+          });
         });
       });
     });
@@ -303,14 +306,14 @@ ms_status ms_gated_delta_grad(const ms_gated_delta_desc* d, const void* q, const
     for (const void* x : {(const void*)decay, (const void*)rate, (const void*)kept, (const void*)lengths, (const void*)dlast,
                           (const void*)ddecay, (const void*)drate, (const void*)ds0})
       need_aligned(x, 4, "decay, rate, kept, lengths, dlast, ddecay, drate or ds0");
+    need((uintptr_t)kept % 16 == 0, "kept must be 16-byte aligned");
     const DeltaWork w = delta_work(p, true, workspace);
     need_workspace(workspace, workspace_bytes, w.bytes);
     DeviceGuard dg(d->device);
     const hipStream_t st = (hipStream_t)d->stream;
     a.lengths = lengths;
     const int64_t cells = p.chunks / a.group;
-    const bool vec = a.dk % 8 == 0 && a.dv % 8 == 0 && words(a.q, q) && words(a.k, k) && words(a.y, dy) &&
-                     (uintptr_t)kept % 16 == 0;
+    const bool vec = a.dk % 8 == 0 && a.dv % 8 == 0 && words(a.q, q) && words(a.k, k) && words(a.y, dy);
     with_value(d->dtype, [&](auto zero) {
       using T = decltype(zero);
       with_flag(vec, [&](auto flag) {
