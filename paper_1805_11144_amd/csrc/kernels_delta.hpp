@@ -17,8 +17,8 @@
 // operand's columns are dealt to lanes in the same order (order_of).  Only K, Q and
 // the two triangles pass through LDS, for all wavefronts of a workgroup, laid out as
 // the matrix instructions take them; K' is read from K's rows by LDS's transposing
-// reads.  While a chunk is computed the next one's K and Q are on their way to
-// registers and its triangles to the other half of LDS.
+// reads.  While a chunk is computed the next one's operands are on their way to
+// registers, and go to the other half of LDS when it is done.
 //
 // Arithmetic: 16-bit matrix instructions, 16 times as fast as 32-bit ones.  A
 // 32-bit value is the sum of three bf16 parts (24 bits, and bf16 has float32's
@@ -28,6 +28,9 @@
 // state read by Q), takes two parts, 16 bits for a result of 8.  The sums of decays
 // are 64-bit: a difference of two of them is good where each is large.
 #pragma once
+
+#include <type_traits>
+#include <utility>
 
 #include "kernels_words.hpp"
 
@@ -407,16 +410,94 @@ struct RowsInFlight {
   }
 };
 
-// A chunk's triangles and scales from memory straight to LDS, 16 bytes a lane, lane
-// i's to 16 i of the wavefront's.
-template <int BYTES>
-__device__ __forceinline__ void fetch_work(const char* from, char* to, int tid) {
+// A chunk's triangles and scales on their way, the same way.  (Loads straight to LDS
+// make the compiler wait for them before any read of LDS: a chunk then took 6.5 us.)
+template <int BYTES, int THREADS>
+struct WorkInFlight {
+  static constexpr int U = (BYTES / 16 + THREADS - 1) / THREADS;
+  typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+  Raw v[U];
+
+  __device__ __forceinline__ void load(const char* from, int tid) {
 #pragma unroll
-  for (int at = 0; at < BYTES; at += 4096)
-    if (at + tid * 16 < BYTES)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + at + tid * 16),
-                                       (__attribute__((address_space(3))) void*)(to + at + tid / 64 * 1024), 16, 0, 0);
+    for (int i = 0; i < U; ++i) v[i] = *(const Raw*)(from + min((tid + i * THREADS) * 16, BYTES - 16));
+  }
+
+  __device__ __forceinline__ void store(char* to, int tid) const {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (tid + i * THREADS < BYTES / 16) *(Raw*)(to + (tid + i * THREADS) * 16) = v[i];
+  }
+};
+
+// Operands 0 .. N - 1, read from LDS D ahead of their use: a read takes as long as
+// eight matrix instructions, and left to itself the compiler waits for each.
+template <int N, int D, class B, class F>
+struct Ahead {
+  B b[D + 1];
+  F load;
+
+  __device__ __forceinline__ explicit Ahead(F f) : load(f) {
+#pragma unroll
+    for (int i = 0; i < D && i < N; ++i) b[i] = load(i);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  __device__ __forceinline__ const B& operator()(int i) {
+    if (i + D < N) b[(i + D) % (D + 1)] = load(i + D);
+    __builtin_amdgcn_sched_barrier(0);
+    return b[i % (D + 1)];
+  }
+};
+
+template <int N, int D, class F>
+__device__ __forceinline__ auto ahead_of(F f) {
+  return Ahead<N, D, decltype(f(0)), F>(f);
 }
+
+// The triangle's piece i of those that are there, by rows.
+template <int C, bool UPPER>
+__device__ __forceinline__ constexpr int tri_row(int i) {
+  int m = 0;
+  for (int n = 0; m < C / 16; ++m) {
+    const int here = UPPER ? C / 32 - m / 2 : m / 2 + 1;
+    if (i < n + here) break;
+    n += here;
+  }
+  return m;
+}
+template <int C, bool UPPER>
+__device__ __forceinline__ constexpr int tri_column(int i) {
+  int n = 0;
+  for (int m = 0; m < C / 16; ++m) {
+    const int here = UPPER ? C / 32 - m / 2 : m / 2 + 1;
+    if (i < n + here) break;
+    n += here;
+  }
+  return i - n + (UPPER ? tri_row<C, UPPER>(i) / 2 : 0);
+}
+
+// Where the upper triangle's piece i, by rows, lies: as the mirror image's, from the end.
+template <int C>
+__device__ __forceinline__ constexpr int tri_upper(int i) {
+  return tri_pieces(C) - 1 - i;
+}
+
+// f(0) .. f(N - 1), each with its number as a compile-time value.
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(F&& f) {
+  each_of(f, std::make_integer_sequence<int, N>{});
+}
+
+template <int A, int B>
+struct OpPair {
+  Op<A> a;
+  Op<B> b;
+};
 
 // One of the two halves of a scan's LDS: rows of K and of Q, the chunk's triangles and scales.
 template <class T, int DK, bool GRAD>
@@ -525,13 +606,15 @@ __global__ void __launch_bounds__(256, 1)
       s[m][r] = s0 && mine && d < p.dk ? s0[(bh * p.dk + d) * p.dv + col] : 0.0f;
     }
   RowsInFlight<T, VEC, C, DK, 256> kr, qr;
+  WorkInFlight<Work::bytes, 256> wr;
   T vr[C / 16][4];
   if (chunks > 0) {
     const int n = min(C, len);
-    fetch_work<Work::bytes>(wp, lds + Lds::work, tid);
+    wr.load(wp, tid);
     kr.load(kp, p.k.t, n, p.dk, tid);
     qr.load(qp, p.q.t, n, p.dk, tid);
     take_steps<T, C>(vp, mcol, vt, n, g, vr);
+    wr.store(lds + Lds::work, tid);
     kr.store(lds + Lds::k, tid);
     qr.store(lds + Lds::q, tid);
   }
@@ -546,7 +629,7 @@ __global__ void __launch_bounds__(256, 1)
       for (int r = 0; r < 4; ++r) z[m][r] = mine && m * 16 + g * 4 + r < n ? as_f32(vr[m][r]) : 0.0f;
     __syncthreads();   // this chunk's operands are there, and the other half is read
     if (ahead > 0) {
-      fetch_work<Work::bytes>(wp + (int64_t)(chunk + 1) * Work::bytes, next + Lds::work, tid);
+      wr.load(wp + (int64_t)(chunk + 1) * Work::bytes, tid);
       kp += C * p.k.t, qp += C * p.q.t, vp += C * p.v.t;
       kr.load(kp, p.k.t, ahead, p.dk, tid);
       qr.load(qp, p.q.t, ahead, p.dk, tid);
@@ -555,6 +638,11 @@ __global__ void __launch_bounds__(256, 1)
     if (some) {
       if (KEEP) put_state<DK>(states + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
       const float* e = (const float*)(here + Lds::work + Work::scales);
+      constexpr int TRI = tri_pieces(C), NEAR = sizeof(T) == 2 ? 3 : 1;   // 5 products to a pair, or 12
+      const char* const tri = here + Lds::work;
+      auto kq = ahead_of<RP, NEAR>([&](int i) {
+        return OpPair<PI, PI>{op_take<PI>(here + Lds::k, RP, i, at), op_take<PI>(here + Lds::q, RP, i, at)};
+      });
       Op<kState> sp[KS];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
@@ -563,39 +651,41 @@ __global__ void __launch_bounds__(256, 1)
         f32x4 c = zero4(), w = zero4();
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          c = op_mul<kState>(op_take<PI>(here + Lds::k, RP, m * KS + ks, at), sp[ks], c);
-          w = op_mul<kOut<T>>(op_take<PI>(here + Lds::q, RP, m * KS + ks, at), sp[ks], w);
+          const auto& x = kq(m * KS + ks);
+          c = op_mul<kState>(x.a, sp[ks], c);
+          w = op_mul<kOut<T>>(x.b, sp[ks], w);
         }
         const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) z[m][r] -= share_of(em[r], c[r]), o[m][r] = share_of(em[r], w[r]) * p.scale;
       }
+      auto solve = ahead_of<TRI, 2>([&](int i) { return op_take<kState>(tri + Work::solve, TRI, i, lane); });
       Op<kState> zp[C / 32];
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
 #pragma unroll
-      for (int m = 0; m < C / 16; ++m) {
-        z[m] = zero4();
-#pragma unroll
-        for (int ks = 0; ks <= m / 2; ++ks)
-          z[m] = op_mul<kState>(
-              op_take<kState>(here + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zp[ks], z[m]);
-      }
+      for (int m = 0; m < C / 16; ++m) z[m] = zero4();
+      each<TRI>([&](auto i) {
+        constexpr int m = tri_row<C, false>(i), ks = tri_column<C, false>(i);
+        z[m] = op_mul<kState>(solve(i), zp[ks], z[m]);
+      });
       if (KEEP) put_rows<C>(errors + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, z);
+      auto reads = ahead_of<TRI, 3>([&](int i) { return op_take<PA>(tri + Work::reads, TRI, i, lane); });
       Op<kOut<T>> zo[C / 32];
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) zo[ks] = op_of<kOut<T>>(z[2 * ks], z[2 * ks + 1]);
+      each<TRI>([&](auto i) {
+        constexpr int m = tri_row<C, false>(i), ks = tri_column<C, false>(i);
+        o[m] = op_mul<kOut<T>>(reads(i), zo[ks], o[m]);
+      });
+      auto turned = ahead_of<RP, NEAR + 1>(
+          [&](int i) { return op_turn<PI, KS>(here + Lds::k, RP, i / (C / 32), i % (C / 32), even, odd); });
 #pragma unroll
       for (int m = 0; m < C / 16; ++m) {
-#pragma unroll
-        for (int ks = 0; ks <= m / 2; ++ks)
-          o[m] = op_mul<kOut<T>>(
-              op_take<PA>(here + Lds::work + Work::reads, tri_pieces(C), tri_piece<C, false>(m, ks), lane), zo[ks], o[m]);
         const f32x4 om = *(const f32x4*)(e + C + m * 16 + g * 4), bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) z[m][r] *= om[r] * bm[r];
       }
-      if (mine) put_steps<T, C>(yp, col, yt, n, g, o);
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
       const float keep = e[C - 1];
@@ -604,12 +694,13 @@ __global__ void __launch_bounds__(256, 1)
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
 #pragma unroll
-        for (int ks = 0; ks < C / 32; ++ks)
-          s[m] = op_mul<kState>(op_turn<PI, KS>(here + Lds::k, RP, m, ks, even, odd), zp[ks], s[m]);
+        for (int ks = 0; ks < C / 32; ++ks) s[m] = op_mul<kState>(turned(m * (C / 32) + ks), zp[ks], s[m]);
       }
+      if (mine) put_steps<T, C>(yp, col, yt, n, g, o);
       yp += C * p.y.t;
     }
     if (ahead > 0) {
+      wr.store(next + Lds::work, tid);
       kr.store(next + Lds::k, tid);
       qr.store(next + Lds::q, tid);
     }

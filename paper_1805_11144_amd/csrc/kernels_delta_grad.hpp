@@ -57,18 +57,20 @@ __global__ void __launch_bounds__(256, 1)
   if (mine)
     for (int64_t t = len + g; t < p.steps; t += 4) vp[t * vt + col] = (T)0.0f;
   RowsInFlight<T, VEC, C, DK, 256> kr, qr;
+  WorkInFlight<Work::bytes, 256> wr;
   T yr[C / 16][4];
-  const auto ahead_of = [&](int chunk, char* to) {
+  const auto load = [&](int chunk) {
     const int n = min(C, len - chunk * C);
     const int64_t t0 = (int64_t)chunk * C;
-    fetch_work<Work::bytes>(wp + (int64_t)chunk * Work::bytes, to + Lds::work, tid);
+    wr.load(wp + (int64_t)chunk * Work::bytes, tid);
     kr.load(kp + t0 * p.k.t, p.k.t, n, p.dk, tid);
     qr.load(qp + t0 * p.q.t, p.q.t, n, p.dk, tid);
     take_steps<T, C>(yp + t0 * p.y.t, mcol, yt, n, g, yr);
   };
   if (chunks > 0) {
     char* const to = lds + ((chunks - 1) & 1) * Lds::bytes;
-    ahead_of(chunks - 1, to);
+    load(chunks - 1);
+    wr.store(to + Lds::work, tid);
     kr.store(to + Lds::k, tid);
     qr.store(to + Lds::q, tid);
   }
@@ -82,11 +84,14 @@ __global__ void __launch_bounds__(256, 1)
 #pragma unroll
       for (int r = 0; r < 4; ++r) dyr[m][r] = mine && m * 16 + g * 4 + r < n ? as_f32(yr[m][r]) : 0.0f;
     __syncthreads();   // this chunk's operands are there, and the other half is read
-    if (chunk > 0) ahead_of(chunk - 1, next);
+    if (chunk > 0) load(chunk - 1);
     if (some) {
       put_state<DK>(dstates + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
       const float* e = (const float*)(here + Lds::work + Work::scales);
+      constexpr int TRI = tri_pieces(C), NEAR = sizeof(T) == 2 ? 4 : 1;
+      const char* const tri = here + Lds::work;
       {
+        auto rows = ahead_of<RP, NEAR>([&](int i) { return op_take<PI>(here + Lds::k, RP, i, at); });
         Op<kState> sp[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
@@ -94,38 +99,42 @@ __global__ void __launch_bounds__(256, 1)
         for (int m = 0; m < C / 16; ++m) {
           x[m] = zero4();
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) x[m] = op_mul<kState>(op_take<PI>(here + Lds::k, RP, m * KS + ks, at), sp[ks], x[m]);
+          for (int ks = 0; ks < KS; ++ks) x[m] = op_mul<kState>(rows(m * KS + ks), sp[ks], x[m]);
           const f32x4 om = *(const f32x4*)(e + C + m * 16 + g * 4);
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[m][r] = share_of(om[r], x[m][r]);
         }
       }
       {
+        auto reads = ahead_of<TRI, 2>([&](int i) {
+          return op_take<kState>(tri + Work::reads, TRI, tri_upper<C>(i), lane);
+        });
         Op<PI> dp[C / 32];
 #pragma unroll
         for (int ks = 0; ks < C / 32; ++ks) dp[ks] = op_of<PI>(dyr[2 * ks], dyr[2 * ks + 1]);
-#pragma unroll
-        for (int m = 0; m < C / 16; ++m) {
-#pragma unroll
-          for (int ks = m / 2; ks < C / 32; ++ks)
-            x[m] = op_mul<kState>(
-                op_take<kState>(here + Lds::work + Work::reads, tri_pieces(C), tri_piece<C, true>(m, ks), lane), dp[ks], x[m]);
-          const f32x4 bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[m][r] *= bm[r];
-        }
+        each<TRI>([&](auto i) {
+          constexpr int m = tri_row<C, true>(i), ks = tri_column<C, true>(i);
+          x[m] = op_mul<kState>(reads(i), dp[ks], x[m]);
+        });
       }
+      auto solve = ahead_of<TRI, 2>([&](int i) {
+        return op_take<kState>(tri + Work::solve, TRI, tri_upper<C>(i), lane);
+      });
       Op<kState> xp[C / 32];
+#pragma unroll
+      for (int m = 0; m < C / 16; ++m) {
+        const f32x4 bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[m][r] *= bm[r];
+      }
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
 #pragma unroll
-      for (int m = 0; m < C / 16; ++m) {
-        x[m] = zero4();
-#pragma unroll
-        for (int ks = m / 2; ks < C / 32; ++ks)
-          x[m] = op_mul<kState>(op_take<kState>(here + Lds::work + Work::solve, tri_pieces(C), tri_piece<C, true>(m, ks), lane),
-                                xp[ks], x[m]);
-      }
+      for (int m = 0; m < C / 16; ++m) x[m] = zero4();
+      each<TRI>([&](auto i) {
+        constexpr int m = tri_row<C, true>(i), ks = tri_column<C, true>(i);
+        x[m] = op_mul<kState>(solve(i), xp[ks], x[m]);
+      });
       put_rows<C>(xs + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, x);
       if (mine) put_steps<T, C>(vp + (int64_t)chunk * C * vt, col, vt, n, g, x);
 #pragma unroll
@@ -134,6 +143,10 @@ __global__ void __launch_bounds__(256, 1)
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[m][r] *= -em[r], dyr[m][r] *= p.scale * em[r];
       }
+      auto turned = ahead_of<RP, NEAR / 2 + 1>([&](int i) {
+        return OpPair<PI, PI>{op_turn<PI, KS>(here + Lds::q, RP, i / (C / 32), i % (C / 32), even, odd),
+                              op_turn<PI, KS>(here + Lds::k, RP, i / (C / 32), i % (C / 32), even, odd)};
+      });
       Op<kState> dp[C / 32];
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) {
@@ -147,12 +160,14 @@ __global__ void __launch_bounds__(256, 1)
         for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
 #pragma unroll
         for (int ks = 0; ks < C / 32; ++ks) {
-          s[m] = op_mul<kState>(op_turn<PI, KS>(here + Lds::q, RP, m, ks, even, odd), dp[ks], s[m]);
-          s[m] = op_mul<kState>(op_turn<PI, KS>(here + Lds::k, RP, m, ks, even, odd), xp[ks], s[m]);
+          const auto& o = turned(m * (C / 32) + ks);
+          s[m] = op_mul<kState>(o.a, dp[ks], s[m]);
+          s[m] = op_mul<kState>(o.b, xp[ks], s[m]);
         }
       }
     }
     if (chunk > 0) {
+      wr.store(next + Lds::work, tid);
       kr.store(next + Lds::k, tid);
       qr.store(next + Lds::q, tid);
     }
