@@ -17,8 +17,8 @@
 // operand's columns are dealt to lanes in the same order (order_of).  Only K, Q and
 // the two triangles pass through LDS, for all wavefronts of a workgroup, laid out as
 // the matrix instructions take them; K' is read from K's rows by LDS's transposing
-// reads.  While a chunk is computed the next one's operands are on their way to
-// registers, and go to the other half of LDS when it is done.
+// reads.  Four wavefronts of a workgroup compute and four feed them: they bring the
+// next chunk's operands from memory to the other half of LDS and take results out.
 //
 // Arithmetic: 16-bit matrix instructions, 16 times as fast as 32-bit ones.  A
 // 32-bit value is the sum of three bf16 parts (24 bits, and bf16 has float32's
@@ -499,11 +499,166 @@ struct OpPair {
   Op<B> b;
 };
 
-// One of the two halves of a scan's LDS: rows of K and of Q, the chunk's triangles and scales.
+// 64 columns of a chunk of V, Y or dY in LDS.  16 bits: V and dY by steps, Y by
+// columns, 128 bytes a row, its 16-byte words mixed by the row so that transposing
+// reads and writes of columns meet different banks; 32 bits: by steps, 68 values apart.
+template <class T>
+struct Panel {
+  static constexpr int C = kChunk<T>, bytes = sizeof(T) == 2 ? 64 * 128 : C * 68 * 4;
+  static __device__ __forceinline__ int at(int row, int i) {   // 16 bits: value i of a row
+    return row * 128 + (i / 8 ^ row % 8) * 16 + i % 8 * 2;
+  }
+};
+
+// 64 columns of V or dY on their way there, by 256 threads; n steps and `there`
+// columns are there, the others zeros.
+template <class T, bool VEC>
+struct PanelInFlight {
+  static constexpr int C = kChunk<T>, U = C * 8 / 256;
+  Words<T, 8> v[U];
+
+  __device__ __forceinline__ void load(const T* x, int32_t stride, int n, int there, int tid) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int row = tid / 8 + i * 32, c = tid % 8 * 8;
+      const bool some = row < n && c < there;
+      const T* from = x + (some ? (int64_t)(uint32_t)(row * stride) + c : 0);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i].v[j] = (T)0.0f;
+      if constexpr (VEC) {
+        constexpr int W = 16 / sizeof(T);
+        if (some)
+#pragma unroll
+          for (int q = 0; q < 8; q += W) *(Words<T, W>*)(v[i].v + q) = *(const Words<T, W>*)(from + q);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (some && c + j < there) v[i].v[j] = from[j];
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(char* lds, int tid) const {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int row = tid / 8 + i * 32, c = tid % 8 * 8;
+      if constexpr (sizeof(T) == 2) {
+        *(Words<T, 8>*)(lds + Panel<T>::at(row, c)) = v[i];
+      } else {
+        *(Words<T, 4>*)(lds + (row * 68 + c) * 4) = *(const Words<T, 4>*)v[i].v;
+        *(Words<T, 4>*)(lds + (row * 68 + c + 4) * 4) = *(const Words<T, 4>*)(v[i].v + 4);
+      }
+    }
+  }
+};
+
+// This wavefront's 16 columns (of tile `wave`) as results' registers: row 4 g + r of
+// result m is step 16 m + 4 g + r.
+template <class T>
+__device__ __forceinline__ void panel_take(const char* lds, int wave, int lane, f32x4 (&z)[kChunk<T> / 16]) {
+  const int g = lane / 16;
+#pragma unroll
+  for (int m = 0; m < kChunk<T> / 16; ++m) {
+    if constexpr (sizeof(T) == 2) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4* From;
+      const char* from = lds + Panel<T>::at(m * 16 + g * 4 + lane % 16 / 4, wave * 16 + lane % 4 * 4);
+      const bf16x4 h = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)from));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[m][r] = (float)h[r];
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[m][r] = *(const float*)(lds + ((m * 16 + g * 4 + r) * 68 + wave * 16 + lane % 16) * 4);
+    }
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void panel_put(char* lds, int wave, int lane, const f32x4 (&o)[kChunk<T> / 16]) {
+  const int g = lane / 16;
+#pragma unroll
+  for (int m = 0; m < kChunk<T> / 16; ++m) {
+    if constexpr (sizeof(T) == 2) {
+      *(bf16x4*)(lds + Panel<T>::at(wave * 16 + lane % 16, m * 16 + g * 4)) =
+          bf16x4{(__bf16)o[m][0], (__bf16)o[m][1], (__bf16)o[m][2], (__bf16)o[m][3]};
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) *(float*)(lds + ((m * 16 + g * 4 + r) * 68 + wave * 16 + lane % 16) * 4) = o[m][r];
+    }
+  }
+}
+
+// What panel_put left, to memory, by 256 threads.
+template <class T, bool VEC>
+__device__ __forceinline__ void panel_out(const char* lds, T* y, int32_t stride, int n, int there, int tid) {
+  constexpr int C = kChunk<T>;
+#pragma unroll
+  for (int i = 0; i < C * 8 / 256; ++i) {
+    Words<T, 8> w;
+    int t, c;
+    if constexpr (sizeof(T) == 2) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4* From;
+      const int group = tid / 16 + i * 16, s = tid % 16;
+      c = group % 8 * 8, t = group / 8 * 16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const char* from = lds + Panel<T>::at(c + h * 4 + s / 4, t + s % 4 * 4);
+        *(s16x4*)(w.v + h * 4) = __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)from);
+      }
+      t += s;
+    } else {
+      t = tid / 8 + i * 32, c = tid % 8 * 8;
+      *(Words<T, 4>*)w.v = *(const Words<T, 4>*)(lds + (t * 68 + c) * 4);
+      *(Words<T, 4>*)(w.v + 4) = *(const Words<T, 4>*)(lds + (t * 68 + c + 4) * 4);
+    }
+    if (t >= n || c >= there) continue;
+    T* to = y + (int64_t)(uint32_t)(t * stride) + c;
+    if constexpr (VEC) {
+      constexpr int W = 16 / sizeof(T);
+#pragma unroll
+      for (int q = 0; q < 8; q += W) *(Words<T, W>*)(to + q) = *(const Words<T, W>*)(w.v + q);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < there) to[j] = w.v[j];
+    }
+  }
+}
+
+// One of the two halves of a scan's LDS: rows of K and of Q, the chunk's triangles and
+// scales, V or dY; behind them two panels of Y.
 template <class T, int DK, bool GRAD>
 struct ScanLds {
   static constexpr int C = kChunk<T>, PA = GRAD ? kState : kOut<T>;
-  static constexpr int k = 0, q = kIn<T> * C * DK * 2, work = 2 * q, bytes = work + ChunkWork<C, PA>::bytes;
+  static constexpr int k = 0, q = kIn<T> * C * DK * 2, work = 2 * q, panel = work + ChunkWork<C, PA>::bytes,
+                       bytes = panel + Panel<T>::bytes, out = 2 * bytes, all = out + (GRAD ? 0 : 2 * Panel<T>::bytes);
+};
+
+// A chunk's operands on their way from memory to one half, by 256 threads.
+template <class T, bool VEC, int DK, bool GRAD>
+struct ChunkInFlight {
+  using Lds = ScanLds<T, DK, GRAD>;
+  static constexpr int C = Lds::C, BYTES = ChunkWork<C, Lds::PA>::bytes;
+  RowsInFlight<T, VEC, C, DK, 256> k, q;
+  WorkInFlight<BYTES, 256> w;
+  PanelInFlight<T, VEC> x;
+
+  __device__ __forceinline__ void load(const DeltaArgs& p, const T* kp, const T* qp, const T* xp, const Walk& xw,
+                                       const char* wp, int64_t chunk, int n, int there, int tid) {
+    const int64_t t0 = chunk * C;
+    w.load(wp + chunk * BYTES, tid);
+    k.load(kp + t0 * p.k.t, p.k.t, n, p.dk, tid);
+    q.load(qp + t0 * p.q.t, p.q.t, n, p.dk, tid);
+    x.load(xp + t0 * xw.t, (int32_t)xw.t, n, there, tid);
+  }
+
+  __device__ __forceinline__ void store(char* half, int tid) const {
+    w.store(half + Lds::work, tid);
+    k.store(half + Lds::k, tid);
+    q.store(half + Lds::q, tid);
+    x.store(half + Lds::panel, tid);
+  }
 };
 
 // Batch row, head and block of columns of a workgroup: the blocks of a head are 8
@@ -513,41 +668,6 @@ __device__ __forceinline__ bool scan_place(const DeltaArgs& p, int blocks, int64
   bh = x / (8 * blocks) * 8 + x % 8;
   block = (int)(x / 8 % blocks);
   return bh < p.batch * p.heads;
-}
-
-// A column's values at a chunk's steps, to or from results' registers: row 4 g + r of
-// result m is step 16 m + 4 g + r, of which n are there (past them: the last one's).
-template <class T, int C>
-__device__ __forceinline__ void take_steps(const T* x, int32_t col, int32_t stride, int n, int g, T (&out)[C / 16][4]) {
-  if (n == C) {
-    const uint32_t at = g * 4 * stride + col;
-#pragma unroll
-    for (int m = 0; m < C / 16; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) out[m][r] = (x + (m * 16 + r) * stride)[at];
-  } else {
-#pragma unroll
-    for (int m = 0; m < C / 16; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) out[m][r] = x[(uint32_t)(min(m * 16 + g * 4 + r, n - 1) * stride + col)];
-  }
-}
-
-template <class T, int C>
-__device__ __forceinline__ void put_steps(T* x, int32_t col, int32_t stride, int n, int g, const f32x4 (&v)[C / 16]) {
-  const uint32_t at = g * 4 * stride + col;
-  if (n == C) {
-#pragma unroll
-    for (int m = 0; m < C / 16; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) (x + (m * 16 + r) * stride)[at] = (T)v[m][r];
-  } else {
-#pragma unroll
-    for (int m = 0; m < C / 16; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (m * 16 + g * 4 + r < n) (x + (m * 16 + r) * stride)[at] = (T)v[m][r];
-  }
 }
 
 // What the passes leave for k_delta_grad of a chunk: its state, or the state's
@@ -572,12 +692,13 @@ __device__ __forceinline__ void put_rows(float* x, int col, int g, const f32x4 (
   for (int m = 0; m < C / 16; ++m) *(f32x4*)(at + m * 16) = z[m];
 }
 
-// The chunks of a head in order.  grid: see scan_place; a wavefront has 16 columns.
+// The chunks of a head in order, 64 columns to a workgroup (grid: see scan_place) and
+// 16 to a computing wavefront.
 // KEEP: S before each chunk to `states` and Z to `errors`, for the gradient.
 template <class T, bool VEC, int DK, bool KEEP>
-__global__ void __launch_bounds__(256, 1)
-    k_delta_scan(DeltaArgs p, int blocks, const T* q, const T* k, const T* v, const float* s0, const char* work, T* y,
-                 float* last, float* states, float* errors) {
+__global__ void __launch_bounds__(512, 1)
+    k_delta_scan(DeltaArgs p, int blocks, const T* q, const T* k, const T* v, const float* decay, const float* s0,
+                 const char* work, T* y, float* last, float* states, float* errors) {
   using Lds = ScanLds<T, DK, false>;
   constexpr int C = Lds::C, KS = DK / 32, PA = Lds::PA, PI = kIn<T>, RP = C / 16 * KS;
   using Work = ChunkWork<C, PA>;
@@ -585,138 +706,127 @@ __global__ void __launch_bounds__(256, 1)
   int64_t bh;
   int block;
   if (!scan_place(p, blocks, bh, block)) return;
-  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, at = lane_place(lane % 16, g);
-  const int even = turn_place<true>(lane), odd = turn_odd<true>(lane);
   const int64_t b = bh / p.heads;
-  const int head = (int)(bh % p.heads), kh = head / p.group;
-  const int first = (block * 4 + tid / 64) * 16, col = first + lane % 16, mcol = min(col, p.dv - 1);
-  const bool mine = col < p.dv, some = first < (KEEP ? pad_columns(p.dv) : p.dv);
+  const int head = (int)(bh % p.heads), kh = head / p.group, first = block * 64;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
   const int chunks = (len + C - 1) / C;
-  const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *vp = v + b * p.v.b + head * p.v.h;
-  T* yp = y + b * p.y.b + head * p.y.h;
-  const char* wp = work + bh * p.nchunk * Work::bytes;
-  const int32_t vt = (int32_t)p.v.t, yt = (int32_t)p.y.t;
+  if (threadIdx.x >= 256) {   // feeds
+    const int tid = threadIdx.x - 256, there = p.dv - first;
+    const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *vp = v + b * p.v.b + head * p.v.h + first;
+    T* const yp = y + b * p.y.b + head * p.y.h + first;
+    const char* wp = work + bh * p.nchunk * Work::bytes;
+    ChunkInFlight<T, VEC, DK, false> f;
+    if (chunks > 0) {
+      f.load(p, kp, qp, vp, p.v, wp, 0, min(C, len), there, tid);
+      f.store(lds, tid);
+    }
+    if (chunks > 1) f.load(p, kp, qp, vp, p.v, wp, 1, min(C, len - C), there, tid);
+    for (int64_t t = len + tid / 64; t < p.steps; t += 4)
+      if (tid % 64 < there) yp[t * p.y.t + tid % 64] = (T)0.0f;
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+      __syncthreads();   // this chunk's operands are there, the other half is read and the last results are written
+      if (chunk + 1 < chunks) f.store(lds + (~chunk & 1) * Lds::bytes, tid);
+      if (chunk + 2 < chunks) f.load(p, kp, qp, vp, p.v, wp, chunk + 2, min(C, len - (chunk + 2) * C), there, tid);
+      if (chunk > 0)
+        panel_out<T, VEC>(lds + Lds::out + (~chunk & 1) * Panel<T>::bytes, yp + (int64_t)(chunk - 1) * C * p.y.t,
+                          (int32_t)p.y.t, C, there, tid);
+    }
+    __syncthreads();
+    if (chunks > 0)
+      panel_out<T, VEC>(lds + Lds::out + (~chunks & 1) * Panel<T>::bytes, yp + (int64_t)(chunks - 1) * C * p.y.t,
+                        (int32_t)p.y.t, len - (chunks - 1) * C, there, tid);
+    return;
+  }
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = lane / 16, at = lane_place(lane % 16, g);
+  const int even = turn_place<true>(lane), odd = turn_odd<true>(lane);
+  const int tile = first + wave * 16, col = tile + lane % 16;
+  const bool mine = col < p.dv, some = tile < (KEEP ? pad_columns(p.dv) : p.dv);
   f32x4 s[DK / 16];
+  // where the first step forgets, what s0 holds does not count
+  const bool fresh = !s0 || (len > 0 && decay[b * p.decay.b + head * p.decay.h] < -200.0f);
 #pragma unroll
   for (int m = 0; m < DK / 16; ++m)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int d = order_of(m, g, r);
-      s[m][r] = s0 && mine && d < p.dk ? s0[(bh * p.dk + d) * p.dv + col] : 0.0f;
+      s[m][r] = !fresh && mine && d < p.dk ? s0[(bh * p.dk + d) * p.dv + col] : 0.0f;
     }
-  RowsInFlight<T, VEC, C, DK, 256> kr, qr;
-  WorkInFlight<Work::bytes, 256> wr;
-  T vr[C / 16][4];
-  if (chunks > 0) {
-    const int n = min(C, len);
-    wr.load(wp, tid);
-    kr.load(kp, p.k.t, n, p.dk, tid);
-    qr.load(qp, p.q.t, n, p.dk, tid);
-    take_steps<T, C>(vp, mcol, vt, n, g, vr);
-    wr.store(lds + Lds::work, tid);
-    kr.store(lds + Lds::k, tid);
-    qr.store(lds + Lds::q, tid);
-  }
   for (int chunk = 0; chunk < chunks; ++chunk) {
-    char* const here = lds + (chunk & 1) * Lds::bytes;
-    char* const next = lds + (~chunk & 1) * Lds::bytes;
-    const int n = min(C, len - chunk * C), ahead = min(C, len - (chunk + 1) * C);
+    const char* const here = lds + (chunk & 1) * Lds::bytes;
+    __syncthreads();
+    if (!some) continue;
+    if (KEEP) put_state<DK>(states + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
+    constexpr int TRI = tri_pieces(C), NEAR = sizeof(T) == 2 ? 3 : 1;   // 5 products to a pair, or 12
+    const char* const tri = here + Lds::work;
+    const float* e = (const float*)(tri + Work::scales);
+    auto kq = ahead_of<RP, NEAR>([&](int i) {
+      return OpPair<PI, PI>{op_take<PI>(here + Lds::k, RP, i, at), op_take<PI>(here + Lds::q, RP, i, at)};
+    });
     f32x4 z[C / 16], o[C / 16];
+    panel_take<T>(here + Lds::panel, wave, lane, z);
+    Op<kState> sp[KS];
 #pragma unroll
-    for (int m = 0; m < C / 16; ++m)
+    for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[m][r] = mine && m * 16 + g * 4 + r < n ? as_f32(vr[m][r]) : 0.0f;
-    __syncthreads();   // this chunk's operands are there, and the other half is read
-    if (ahead > 0) {
-      wr.load(wp + (int64_t)(chunk + 1) * Work::bytes, tid);
-      kp += C * p.k.t, qp += C * p.q.t, vp += C * p.v.t;
-      kr.load(kp, p.k.t, ahead, p.dk, tid);
-      qr.load(qp, p.q.t, ahead, p.dk, tid);
-      take_steps<T, C>(vp, mcol, vt, ahead, g, vr);
+    for (int m = 0; m < C / 16; ++m) {
+      f32x4 c = zero4(), w = zero4();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const auto& x = kq(m * KS + ks);
+        c = op_mul<kState>(x.a, sp[ks], c);
+        w = op_mul<kOut<T>>(x.b, sp[ks], w);
+      }
+      const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[m][r] = fmaf(-em[r], c[r], z[m][r]), o[m][r] = em[r] * p.scale * w[r];
     }
-    if (some) {
-      if (KEEP) put_state<DK>(states + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
-      const float* e = (const float*)(here + Lds::work + Work::scales);
-      constexpr int TRI = tri_pieces(C), NEAR = sizeof(T) == 2 ? 3 : 1;   // 5 products to a pair, or 12
-      const char* const tri = here + Lds::work;
-      auto kq = ahead_of<RP, NEAR>([&](int i) {
-        return OpPair<PI, PI>{op_take<PI>(here + Lds::k, RP, i, at), op_take<PI>(here + Lds::q, RP, i, at)};
-      });
-      Op<kState> sp[KS];
+    auto solve = ahead_of<TRI, 2>([&](int i) { return op_take<kState>(tri + Work::solve, TRI, i, lane); });
+    Op<kState> zp[C / 32];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
+    for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
 #pragma unroll
-      for (int m = 0; m < C / 16; ++m) {
-        f32x4 c = zero4(), w = zero4();
+    for (int m = 0; m < C / 16; ++m) z[m] = zero4();
+    each<TRI>([&](auto i) {
+      constexpr int m = tri_row<C, false>(i), ks = tri_column<C, false>(i);
+      z[m] = op_mul<kState>(solve(i), zp[ks], z[m]);
+    });
+    if (KEEP) put_rows<C>(errors + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, z);
+    auto reads = ahead_of<TRI, 3>([&](int i) { return op_take<PA>(tri + Work::reads, TRI, i, lane); });
+    Op<kOut<T>> zo[C / 32];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const auto& x = kq(m * KS + ks);
-          c = op_mul<kState>(x.a, sp[ks], c);
-          w = op_mul<kOut<T>>(x.b, sp[ks], w);
-        }
-        const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
+    for (int ks = 0; ks < C / 32; ++ks) zo[ks] = op_of<kOut<T>>(z[2 * ks], z[2 * ks + 1]);
+    each<TRI>([&](auto i) {
+      constexpr int m = tri_row<C, false>(i), ks = tri_column<C, false>(i);
+      o[m] = op_mul<kOut<T>>(reads(i), zo[ks], o[m]);
+    });
+    auto turned = ahead_of<RP, NEAR + 1>(
+        [&](int i) { return op_turn<PI, KS>(here + Lds::k, RP, i / (C / 32), i % (C / 32), even, odd); });
+    panel_put<T>(lds + Lds::out + (chunk & 1) * Panel<T>::bytes, wave, lane, o);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z[m][r] -= share_of(em[r], c[r]), o[m][r] = share_of(em[r], w[r]) * p.scale;
-      }
-      auto solve = ahead_of<TRI, 2>([&](int i) { return op_take<kState>(tri + Work::solve, TRI, i, lane); });
-      Op<kState> zp[C / 32];
+    for (int m = 0; m < C / 16; ++m) {
+      const f32x4 om = *(const f32x4*)(e + C + m * 16 + g * 4), bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
 #pragma unroll
-      for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
-#pragma unroll
-      for (int m = 0; m < C / 16; ++m) z[m] = zero4();
-      each<TRI>([&](auto i) {
-        constexpr int m = tri_row<C, false>(i), ks = tri_column<C, false>(i);
-        z[m] = op_mul<kState>(solve(i), zp[ks], z[m]);
-      });
-      if (KEEP) put_rows<C>(errors + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, z);
-      auto reads = ahead_of<TRI, 3>([&](int i) { return op_take<PA>(tri + Work::reads, TRI, i, lane); });
-      Op<kOut<T>> zo[C / 32];
-#pragma unroll
-      for (int ks = 0; ks < C / 32; ++ks) zo[ks] = op_of<kOut<T>>(z[2 * ks], z[2 * ks + 1]);
-      each<TRI>([&](auto i) {
-        constexpr int m = tri_row<C, false>(i), ks = tri_column<C, false>(i);
-        o[m] = op_mul<kOut<T>>(reads(i), zo[ks], o[m]);
-      });
-      auto turned = ahead_of<RP, NEAR + 1>(
-          [&](int i) { return op_turn<PI, KS>(here + Lds::k, RP, i / (C / 32), i % (C / 32), even, odd); });
-#pragma unroll
-      for (int m = 0; m < C / 16; ++m) {
-        const f32x4 om = *(const f32x4*)(e + C + m * 16 + g * 4), bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) z[m][r] *= om[r] * bm[r];
-      }
-#pragma unroll
-      for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
-      const float keep = e[C - 1];
-#pragma unroll
-      for (int m = 0; m < DK / 16; ++m) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
-#pragma unroll
-        for (int ks = 0; ks < C / 32; ++ks) s[m] = op_mul<kState>(turned(m * (C / 32) + ks), zp[ks], s[m]);
-      }
-      if (mine) put_steps<T, C>(yp, col, yt, n, g, o);
-      yp += C * p.y.t;
+      for (int r = 0; r < 4; ++r) z[m][r] *= om[r] * bm[r];
     }
-    if (ahead > 0) {
-      wr.store(next + Lds::work, tid);
-      kr.store(next + Lds::k, tid);
-      qr.store(next + Lds::q, tid);
+#pragma unroll
+    for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
+    const float keep = e[C - 1];
+#pragma unroll
+    for (int m = 0; m < DK / 16; ++m) {
+      s[m] *= keep;
+#pragma unroll
+      for (int ks = 0; ks < C / 32; ++ks) s[m] = op_mul<kState>(turned(m * (C / 32) + ks), zp[ks], s[m]);
     }
   }
-  if (mine) {
-    T* ye = y + b * p.y.b + head * p.y.h + col;
-    for (int64_t t = len + g; t < p.steps; t += 4) ye[t * p.y.t] = (T)0.0f;
-    if (last)
+  __syncthreads();
+  if (last && mine)
 #pragma unroll
-      for (int m = 0; m < DK / 16; ++m)
+    for (int m = 0; m < DK / 16; ++m)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = order_of(m, g, r);
-          if (d < p.dk) last[(bh * p.dk + d) * p.dv + col] = s[m][r];
-        }
-  }
+      for (int r = 0; r < 4; ++r) {
+        const int d = order_of(m, g, r);
+        if (d < p.dk) last[(bh * p.dk + d) * p.dv + col] = s[m][r];
+      }
 }
 
 // ---------------------------------------------------------------- single step

@@ -9,7 +9,7 @@
 //     dS <- e[C-1] dS + Q' diag(scale e) dY - K' diag(e) X
 // k_delta_back goes through the chunks in reverse order like k_delta_scan, 16 columns
 // to a wavefront, and leaves X and each chunk's dS.  k_delta_grad computes the rest
-// for all chunks at once, sums over the values:
+// for all chunks at once, sums over the values, and writes X out as dV:
 //     dQ[s] = scale (e[s] S dy[s] + sum_{t <= s} D[s][t] b[t] k[t] (z[t] dy[s]))
 //     W[t]  = o[t] dS z[t] + sum_{s >= t} D[s][t] scale q[s] (dy[s] z[t])
 //                          - sum_{s > t} D[s][t] k[s] (x[s] z[t])                (H z)
@@ -24,8 +24,8 @@
 
 // Columns of the state's gradient through the chunks in reverse order.
 template <class T, bool VEC, int DK>
-__global__ void __launch_bounds__(256, 1)
-    k_delta_back(DeltaArgs p, int blocks, const T* q, const T* k, const T* dy, const float* dlast, const char* work, T* dv,
+__global__ void __launch_bounds__(512, 1)
+    k_delta_back(DeltaArgs p, int blocks, const T* q, const T* k, const T* dy, const float* dlast, const char* work,
                  float* ds0, float* dstates, float* xs) {
   using Lds = ScanLds<T, DK, true>;
   constexpr int C = Lds::C, KS = DK / 32, PI = kIn<T>, RP = C / 16 * KS;
@@ -34,18 +34,32 @@ __global__ void __launch_bounds__(256, 1)
   int64_t bh;
   int block;
   if (!scan_place(p, blocks, bh, block)) return;
-  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, at = lane_place(lane % 16, g);
-  const int even = turn_place<true>(lane), odd = turn_odd<true>(lane);
   const int64_t b = bh / p.heads;
-  const int head = (int)(bh % p.heads), kh = head / p.group;
-  const int first = (block * 4 + tid / 64) * 16, col = first + lane % 16, mcol = min(col, p.dv - 1);
-  const bool mine = col < p.dv, some = first < pad_columns(p.dv);
+  const int head = (int)(bh % p.heads), kh = head / p.group, first = block * 64;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
   const int chunks = (len + C - 1) / C;
-  const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *yp = dy + b * p.y.b + head * p.y.h;
-  T* const vp = dv + (b * p.steps * p.heads + head) * p.dv;
-  const char* wp = work + bh * p.nchunk * Work::bytes;
-  const int32_t yt = (int32_t)p.y.t, vt = p.heads * p.dv;
+  if (threadIdx.x >= 256) {   // feeds
+    const int tid = threadIdx.x - 256, there = p.dv - first;
+    const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *yp = dy + b * p.y.b + head * p.y.h + first;
+    const char* wp = work + bh * p.nchunk * Work::bytes;
+    ChunkInFlight<T, VEC, DK, true> f;
+    const auto load = [&](int chunk) { f.load(p, kp, qp, yp, p.y, wp, chunk, min(C, len - chunk * C), there, tid); };
+    if (chunks > 0) {
+      load(chunks - 1);
+      f.store(lds + (~chunks & 1) * Lds::bytes, tid);
+    }
+    if (chunks > 1) load(chunks - 2);
+    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+      __syncthreads();   // this chunk's operands are there, and the other half is read
+      if (chunk > 0) f.store(lds + (~chunk & 1) * Lds::bytes, tid);
+      if (chunk > 1) load(chunk - 2);
+    }
+    return;
+  }
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = lane / 16, at = lane_place(lane % 16, g);
+  const int even = turn_place<true>(lane), odd = turn_odd<true>(lane);
+  const int tile = first + wave * 16, col = tile + lane % 16;
+  const bool mine = col < p.dv, some = tile < pad_columns(p.dv);
   f32x4 s[DK / 16];
 #pragma unroll
   for (int m = 0; m < DK / 16; ++m)
@@ -54,122 +68,77 @@ __global__ void __launch_bounds__(256, 1)
       const int d = order_of(m, g, r);
       s[m][r] = dlast && mine && d < p.dk ? dlast[(bh * p.dk + d) * p.dv + col] : 0.0f;
     }
-  if (mine)
-    for (int64_t t = len + g; t < p.steps; t += 4) vp[t * vt + col] = (T)0.0f;
-  RowsInFlight<T, VEC, C, DK, 256> kr, qr;
-  WorkInFlight<Work::bytes, 256> wr;
-  T yr[C / 16][4];
-  const auto load = [&](int chunk) {
-    const int n = min(C, len - chunk * C);
-    const int64_t t0 = (int64_t)chunk * C;
-    wr.load(wp + (int64_t)chunk * Work::bytes, tid);
-    kr.load(kp + t0 * p.k.t, p.k.t, n, p.dk, tid);
-    qr.load(qp + t0 * p.q.t, p.q.t, n, p.dk, tid);
-    take_steps<T, C>(yp + t0 * p.y.t, mcol, yt, n, g, yr);
-  };
-  if (chunks > 0) {
-    char* const to = lds + ((chunks - 1) & 1) * Lds::bytes;
-    load(chunks - 1);
-    wr.store(to + Lds::work, tid);
-    kr.store(to + Lds::k, tid);
-    qr.store(to + Lds::q, tid);
-  }
   for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-    char* const here = lds + (chunk & 1) * Lds::bytes;
-    char* const next = lds + (~chunk & 1) * Lds::bytes;
-    const int n = min(C, len - chunk * C);
+    const char* const here = lds + (chunk & 1) * Lds::bytes;
+    __syncthreads();
+    if (!some) continue;
+    put_state<DK>(dstates + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
+    constexpr int TRI = tri_pieces(C), NEAR = sizeof(T) == 2 ? 4 : 1;
+    const char* const tri = here + Lds::work;
+    const float* e = (const float*)(tri + Work::scales);
     f32x4 dyr[C / 16], x[C / 16];
+    {
+      auto rows = ahead_of<RP, NEAR>([&](int i) { return op_take<PI>(here + Lds::k, RP, i, at); });
+      Op<kState> sp[KS];
 #pragma unroll
-    for (int m = 0; m < C / 16; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) dyr[m][r] = mine && m * 16 + g * 4 + r < n ? as_f32(yr[m][r]) : 0.0f;
-    __syncthreads();   // this chunk's operands are there, and the other half is read
-    if (chunk > 0) load(chunk - 1);
-    if (some) {
-      put_state<DK>(dstates + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
-      const float* e = (const float*)(here + Lds::work + Work::scales);
-      constexpr int TRI = tri_pieces(C), NEAR = sizeof(T) == 2 ? 4 : 1;
-      const char* const tri = here + Lds::work;
-      {
-        auto rows = ahead_of<RP, NEAR>([&](int i) { return op_take<PI>(here + Lds::k, RP, i, at); });
-        Op<kState> sp[KS];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
-#pragma unroll
-        for (int m = 0; m < C / 16; ++m) {
-          x[m] = zero4();
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) x[m] = op_mul<kState>(rows(m * KS + ks), sp[ks], x[m]);
-          const f32x4 om = *(const f32x4*)(e + C + m * 16 + g * 4);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[m][r] = share_of(om[r], x[m][r]);
-        }
-      }
-      {
-        auto reads = ahead_of<TRI, 2>([&](int i) {
-          return op_take<kState>(tri + Work::reads, TRI, tri_upper<C>(i), lane);
-        });
-        Op<PI> dp[C / 32];
-#pragma unroll
-        for (int ks = 0; ks < C / 32; ++ks) dp[ks] = op_of<PI>(dyr[2 * ks], dyr[2 * ks + 1]);
-        each<TRI>([&](auto i) {
-          constexpr int m = tri_row<C, true>(i), ks = tri_column<C, true>(i);
-          x[m] = op_mul<kState>(reads(i), dp[ks], x[m]);
-        });
-      }
-      auto solve = ahead_of<TRI, 2>([&](int i) {
-        return op_take<kState>(tri + Work::solve, TRI, tri_upper<C>(i), lane);
-      });
-      Op<kState> xp[C / 32];
+      for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
 #pragma unroll
       for (int m = 0; m < C / 16; ++m) {
-        const f32x4 bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
+        x[m] = zero4();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[m][r] *= bm[r];
-      }
-#pragma unroll
-      for (int ks = 0; ks < C / 32; ++ks) xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
-#pragma unroll
-      for (int m = 0; m < C / 16; ++m) x[m] = zero4();
-      each<TRI>([&](auto i) {
-        constexpr int m = tri_row<C, true>(i), ks = tri_column<C, true>(i);
-        x[m] = op_mul<kState>(solve(i), xp[ks], x[m]);
-      });
-      put_rows<C>(xs + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, x);
-      if (mine) put_steps<T, C>(vp + (int64_t)chunk * C * vt, col, vt, n, g, x);
-#pragma unroll
-      for (int m = 0; m < C / 16; ++m) {
-        const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[m][r] *= -em[r], dyr[m][r] *= p.scale * em[r];
-      }
-      auto turned = ahead_of<RP, NEAR / 2 + 1>([&](int i) {
-        return OpPair<PI, PI>{op_turn<PI, KS>(here + Lds::q, RP, i / (C / 32), i % (C / 32), even, odd),
-                              op_turn<PI, KS>(here + Lds::k, RP, i / (C / 32), i % (C / 32), even, odd)};
-      });
-      Op<kState> dp[C / 32];
-#pragma unroll
-      for (int ks = 0; ks < C / 32; ++ks) {
-        xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
-        dp[ks] = op_of<kState>(dyr[2 * ks], dyr[2 * ks + 1]);
-      }
-      const float keep = e[C - 1];
-#pragma unroll
-      for (int m = 0; m < DK / 16; ++m) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[m][r] = share_of(keep, s[m][r]);
-#pragma unroll
-        for (int ks = 0; ks < C / 32; ++ks) {
-          const auto& o = turned(m * (C / 32) + ks);
-          s[m] = op_mul<kState>(o.a, dp[ks], s[m]);
-          s[m] = op_mul<kState>(o.b, xp[ks], s[m]);
-        }
+        for (int ks = 0; ks < KS; ++ks) x[m] = op_mul<kState>(rows(m * KS + ks), sp[ks], x[m]);
+        x[m] *= *(const f32x4*)(e + C + m * 16 + g * 4);
       }
     }
-    if (chunk > 0) {
-      wr.store(next + Lds::work, tid);
-      kr.store(next + Lds::k, tid);
-      qr.store(next + Lds::q, tid);
+    {
+      auto reads = ahead_of<TRI, 2>([&](int i) { return op_take<kState>(tri + Work::reads, TRI, tri_upper<C>(i), lane); });
+      panel_take<T>(here + Lds::panel, wave, lane, dyr);
+      Op<PI> dp[C / 32];
+#pragma unroll
+      for (int ks = 0; ks < C / 32; ++ks) dp[ks] = op_of<PI>(dyr[2 * ks], dyr[2 * ks + 1]);
+      each<TRI>([&](auto i) {
+        constexpr int m = tri_row<C, true>(i), ks = tri_column<C, true>(i);
+        x[m] = op_mul<kState>(reads(i), dp[ks], x[m]);
+      });
+    }
+    auto solve = ahead_of<TRI, 2>([&](int i) { return op_take<kState>(tri + Work::solve, TRI, tri_upper<C>(i), lane); });
+    Op<kState> xp[C / 32], dp[C / 32];
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m) x[m] *= *(const f32x4*)(e + 2 * C + m * 16 + g * 4);
+#pragma unroll
+    for (int ks = 0; ks < C / 32; ++ks) xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m) x[m] = zero4();
+    each<TRI>([&](auto i) {
+      constexpr int m = tri_row<C, true>(i), ks = tri_column<C, true>(i);
+      x[m] = op_mul<kState>(solve(i), xp[ks], x[m]);
+    });
+    put_rows<C>(xs + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, x);
+    auto turned = ahead_of<RP, NEAR / 2 + 1>([&](int i) {
+      return OpPair<PI, PI>{op_turn<PI, KS>(here + Lds::q, RP, i / (C / 32), i % (C / 32), even, odd),
+                            op_turn<PI, KS>(here + Lds::k, RP, i / (C / 32), i % (C / 32), even, odd)};
+    });
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m) {
+      const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
+      x[m] *= -em;
+      dyr[m] *= p.scale * em;
+    }
+#pragma unroll
+    for (int ks = 0; ks < C / 32; ++ks) {
+      xp[ks] = op_of<kState>(x[2 * ks], x[2 * ks + 1]);
+      dp[ks] = op_of<kState>(dyr[2 * ks], dyr[2 * ks + 1]);
+    }
+    const float keep = e[C - 1];
+#pragma unroll
+    for (int m = 0; m < DK / 16; ++m) {
+      s[m] *= keep;
+#pragma unroll
+      for (int ks = 0; ks < C / 32; ++ks) {
+        const auto& o = turned(m * (C / 32) + ks);
+        s[m] = op_mul<kState>(o.a, dp[ks], s[m]);
+        s[m] = op_mul<kState>(o.b, xp[ks], s[m]);
+      }
     }
   }
   if (ds0 && mine)
@@ -201,7 +170,7 @@ struct GradLds {
 };
 
 struct DeltaGradOut {
-  void *dq, *dk;   // packed
+  void *dq, *dk, *dv;   // packed
   float *ddecay, *drate;
 };
 
@@ -303,7 +272,9 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
     for (int h = 0; h < p.group; ++h) {
       const int head = kh * p.group + h;
       const int64_t bh = b * p.heads + head, cell = bh * p.nchunk + chunk, gate = (b * p.steps + t0) * p.heads + head;
+      T* const dvp = (T*)out.dv + ((b * p.steps + t0) * p.heads + head) * p.dv;
       if (n == 0) {
+        for (int i = tid; i < in * p.dv; i += THREADS) dvp[(int64_t)(i / p.dv) * p.heads * p.dv + i % p.dv] = (T)0.0f;
         for (int t = tid; t < in; t += THREADS)
           out.ddecay[gate + (int64_t)t * p.heads] = out.drate[gate + (int64_t)t * p.heads] = 0.0f;
         continue;
@@ -374,6 +345,34 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
           for (int j = 0; j < 8; ++j) inner = fmaf(sr.v[i][j / 4][j % 4], dsr.v[i][j / 4][j % 4], inner);
         __syncthreads();
         if (c0 + 32 < cols) ahead(c0 + 32);
+        // X's four columns of a step, as dV
+        for (int i = tid; i < C * 8; i += THREADS) {
+          typedef short s16x4 __attribute__((ext_vector_type(4)));
+          typedef __attribute__((address_space(3))) s16x4* From;
+          const int s = i % 16, j = i / 16 % 8, tile = i / 128, t = tile * 16 + s, c = c0 + j * 4;
+          const int row = column_row(j * 4) + s / 4;   // columns of one transposing read, in order
+          Words<T, 4> w;
+          f32x4 x = zero4();
+#pragma unroll
+          for (int o = PI - 1; o >= 0; --o) {
+            const char* from = lds + Lds::x + (o * 2 * KC + row / 16 * KC + tile / 2) * 1024 +
+                               lane_place(row % 16, tile % 2 * 2 + s % 4 / 2) * 16 + s % 2 * 8;
+            const bf16x4 h = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)from));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] += (float)h[r];
+          }
+          if (t >= in || c >= p.dv) continue;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) w.v[r] = (T)x[r];
+          T* const to = dvp + (int64_t)t * p.heads * p.dv + c;
+          if constexpr (VEC) {
+            *(Words<T, 4>*)to = w;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (c + r < p.dv) to[r] = w.v[r];
+          }
+        }
         {
           const Op<kState> zo = op_turn<kState, KC>(lds + Lds::z, 2 * KC, wave, 0, even, odd),
                            xo = op_turn<kState, KC>(lds + Lds::x, 2 * KC, wave, 0, even, odd);

@@ -108,7 +108,7 @@ Delta check_delta(const ms_gated_delta_desc* d, bool grad) {
   a.nchunk = (d->steps + p.chunk_steps - 1) / p.chunk_steps;
   const int tiles = (int)((d->values + 15) / 16);
   p.blocks = (tiles + 3) / 4;
-  need(d->batch * d->heads <= kMaxBlocks / p.blocks - 8, "batch * heads * values is too large");
+  need(d->batch * d->heads <= kMaxBlocks / 2 / p.blocks - 8, "batch * heads * values is too large");
   p.chunks = d->batch * d->heads * a.nchunk;
   need(p.chunks < ((int64_t)1 << 34), "batch * heads * steps is too large");
   p.work = half ? chunk_bytes<__bf16>(grad) : chunk_bytes<float>(grad);
@@ -269,7 +269,8 @@ ms_status ms_gated_delta(const ms_gated_delta_desc* d, const void* q, const void
     float* errors = kept ? kept + kept_states(p) : nullptr;
     with_value(d->dtype, [&](auto zero) {
       using T = decltype(zero);
-      with_flag(a.dk % 8 == 0 && words(a.q, q) && words(a.k, k), [&](auto vec) {
+      const bool wide = a.dk % 8 == 0 && a.dv % 8 == 0 && words(a.q, q) && words(a.k, k) && words(a.v, v) && words(a.y, y);
+      with_flag(wide, [&](auto vec) {
         with_keys(a.dk, [&](auto keys) {
           constexpr int DK = decltype(keys)::value;
           constexpr bool VEC = decltype(vec)::value;
@@ -279,10 +280,11 @@ ms_status ms_gated_delta(const ms_gated_delta_desc* d, const void* q, const void
                                (const T*)k, decay, rate, w.chunk);
           with_flag(kept != nullptr, [&](auto keep) {
             constexpr auto scan = k_delta_scan<T, VEC, DK, decltype(keep)::value>;
-            constexpr size_t lds = 2 * ScanLds<T, DK, false>::bytes;
+            constexpr size_t lds = ScanLds<T, DK, false>::all;
+            static_assert(lds <= 160 * 1024, "LDS");
             allow_lds(scan, lds);
-            hipLaunchKernelGGL(scan, scan_grid(p), dim3(256), lds, st, a, p.blocks, (const T*)q, (const T*)k, (const T*)v, s0,
-                               (const char*)w.chunk, (T*)y, last, kept, errors);
+            hipLaunchKernelGGL(scan, scan_grid(p), dim3(512), lds, st, a, p.blocks, (const T*)q, (const T*)k, (const T*)v,
+                               decay, s0, (const char*)w.chunk, (T*)y, last, kept, errors);
           });
         });
       });
@@ -313,7 +315,8 @@ ms_status ms_gated_delta_grad(const ms_gated_delta_desc* d, const void* q, const
     const hipStream_t st = (hipStream_t)d->stream;
     a.lengths = lengths;
     const int64_t cells = p.chunks / a.group;
-    const bool vec = a.dk % 8 == 0 && a.dv % 8 == 0 && words(a.q, q) && words(a.k, k) && words(a.y, dy);
+    const bool vec = a.dk % 8 == 0 && a.dv % 8 == 0 && words(a.q, q) && words(a.k, k) && words(a.y, dy) &&
+                     (uintptr_t)dv % 16 == 0;
     with_value(d->dtype, [&](auto zero) {
       using T = decltype(zero);
       with_flag(vec, [&](auto flag) {
@@ -325,17 +328,18 @@ ms_status ms_gated_delta_grad(const ms_gated_delta_desc* d, const void* q, const
                                dim3((unsigned)std::min(p.chunks, kMaxBlocks)), dim3(kChunk<T> * 4), 0, st, a, (const T*)q,
                                (const T*)k, decay, rate, w.chunk);
           constexpr auto back = k_delta_back<T, VEC, DK>;
-          constexpr size_t lds = 2 * ScanLds<T, DK, true>::bytes;
+          constexpr size_t lds = ScanLds<T, DK, true>::all;
+          static_assert(lds <= 160 * 1024, "LDS");
           allow_lds(back, lds);
-          hipLaunchKernelGGL(back, scan_grid(p), dim3(256), lds, st, a, p.blocks, (const T*)q, (const T*)k,
-                             (const T*)dy, dlast, (const char*)w.chunk, (T*)dv, ds0, w.dstates, w.xs);
+          hipLaunchKernelGGL(back, scan_grid(p), dim3(512), lds, st, a, p.blocks, (const T*)q, (const T*)k, (const T*)dy,
+                             dlast, (const char*)w.chunk, ds0, w.dstates, w.xs);
           if (!p.chunks) return;
           constexpr auto grad = k_delta_grad<T, VEC, DK>;
           constexpr size_t more = GradLds<T, DK>::bytes;
           allow_lds(grad, more);
           hipLaunchKernelGGL(grad, dim3((unsigned)std::min(cells, kMaxBlocks / 2)), dim3(kGradThreads<T, DK>), more, st, a, (const T*)q,
                              (const T*)k, (const T*)dy, decay, rate, kept, kept + kept_states(p), (const float*)w.dstates,
-                             (const float*)w.xs, DeltaGradOut{dq, dk, ddecay, drate});
+                             (const float*)w.xs, DeltaGradOut{dq, dk, dv, ddecay, drate});
         });
       });
     });
