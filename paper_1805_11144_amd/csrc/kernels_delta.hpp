@@ -176,141 +176,6 @@ __device__ __forceinline__ void tri_store(const float* m, char* out, int tid, in
   }
 }
 
-// T and the reads' triangle of every chunk.  GRAD: their transposes, the second one
-// without b.  A wavefront computes 16 rows of K K' and Q K'; the inverse of the
-// diagonal blocks of 16 goes column by column, a lane each, and blocks double by
-// [[A, 0], [B, C]]^-1 = [[A', 0], [-C' B A', C']] on 32-bit matrix instructions.
-template <class T, bool VEC, int DK, bool GRAD>
-__global__ void __launch_bounds__(kChunk<T> * 4)
-    k_delta_chunk(DeltaArgs p, const T* q, const T* k, const float* decay, const float* rate, char* work) {
-  constexpr int C = kChunk<T>, LD = C + 4, KS = DK / 32, PA = GRAD ? kState : kOut<T>;
-  using Work = ChunkWork<C, PA>;
-  __shared__ float m[C * LD], t[C * LD];
-  __shared__ double sum[C];
-  __shared__ float rates[C];
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, g = lane / 16;
-  const int64_t all = p.batch * p.heads * p.nchunk;
-  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
-    const int64_t chunk = u % p.nchunk, b = u / p.nchunk / p.heads;
-    const int head = (int)(u / p.nchunk % p.heads), kh = head / p.group;
-    const int64_t t0 = chunk * C;
-    const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
-    const int n = (int)min((int64_t)C, len - t0);   // steps of this chunk that count
-    if (n <= 0) continue;                           // nothing reads it
-    char* out = work + u * Work::bytes;
-    if (tid < C) {
-      double d = 0.0;
-      float r = 0.0f;
-      if (tid < n) {
-        const float x = decay[b * p.decay.b + (t0 + tid) * p.decay.t + head * p.decay.h];
-        d = x < -200.0f ? -200.0 : (double)x;   // exp is 0 in 32 bits long before
-        r = rate[b * p.rate.b + (t0 + tid) * p.rate.t + head * p.rate.h];
-      }
-#pragma unroll
-      for (int o = 1; o < C; o *= 2) {
-        const double x = __shfl_up(d, o, 64);
-        if (tid >= o) d += x;
-      }
-      sum[tid] = d * 1.4426950408889634;
-      rates[tid] = r;
-    }
-    __syncthreads();
-    if (tid < C) {
-      float* s = (float*)(out + Work::scales);
-      s[tid] = __builtin_amdgcn_exp2f((float)sum[tid]);
-      s[C + tid] = __builtin_amdgcn_exp2f((float)(sum[C - 1] - sum[tid]));
-      s[2 * C + tid] = rates[tid];
-    }
-    // rows 16 wave .. of K K' and Q K'
-    f32x4 kk[C / 16], qk[C / 16];
-    {
-      const int i = wave * 16 + lane % 16;
-      const T* kb = k + b * p.k.b + t0 * p.k.t + kh * p.k.h;
-      const T* qb = q + b * p.q.b + t0 * p.q.t + kh * p.q.h;
-      Op<kIn<T>> ka[KS], qa[KS];
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int d = ks * 32 + g * 8, there = i < n ? p.dk - d : 0;
-        ka[ks] = op_load<T, VEC>(kb + (there > 0 ? i * p.k.t + d : 0), there);
-        qa[ks] = op_load<T, VEC>(qb + (there > 0 ? i * p.q.t + d : 0), there);
-      }
-#pragma unroll
-      for (int ct = 0; ct < C / 16; ++ct) {
-        kk[ct] = qk[ct] = zero4();
-        if (ct > wave) continue;
-        const int j = ct * 16 + lane % 16;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const int d = ks * 32 + g * 8, there = j < n ? p.dk - d : 0;
-          const Op<kIn<T>> kb_ = op_load<T, VEC>(kb + (there > 0 ? j * p.k.t + d : 0), there);
-          kk[ct] = op_mul<kIn<T>>(ka[ks], kb_, kk[ct]);
-          qk[ct] = op_mul<kIn<T>>(qa[ks], kb_, qk[ct]);
-        }
-      }
-    }
-#pragma unroll
-    for (int ct = 0; ct < C / 16; ++ct)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = wave * 16 + g * 4 + r, j = ct * 16 + lane % 16;
-        const float d = i >= j ? __builtin_amdgcn_exp2f((float)(sum[i] - sum[j])) : 0.0f;
-        m[i * LD + j] = i > j ? kk[ct][r] * d * rates[j] : 0.0f;
-        t[i * LD + j] = 0.0f;
-        qk[ct][r] *= d * p.scale * (GRAD ? 1.0f : rates[j]);
-      }
-    __syncthreads();
-    if (tid < C) {
-      const int at = tid / 16 * 16, c = tid % 16;
-      float x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float s = i == c ? 1.0f : 0.0f;
-#pragma unroll
-        for (int j = 0; j < i; ++j) s = fmaf(-m[(at + i) * LD + at + j], x[j], s);
-        x[i] = s;
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) t[(at + i) * LD + at + c] = x[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int size = 16; size < C; size *= 2) {
-      // B A', in the place of B, and then -C' of it; a tile of 16 x 16 to a wavefront
-      const int side = size / 16, per = side * side, tiles = C / (2 * size) * per;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        f32x4 c = zero4();
-        int r0 = 0, c0 = 0;
-        if (wave < tiles) {
-          const int pair = wave / per * 2 * size;
-          r0 = pair + size + wave % per / side * 16, c0 = pair + wave % side * 16;
-          for (int x = 0; x < size; x += 4) {
-            const float a = half ? t[(r0 + lane % 16) * LD + pair + size + x + g] : m[(r0 + lane % 16) * LD + pair + x + g];
-            const float v = half ? m[(pair + size + x + g) * LD + c0 + lane % 16] : t[(pair + x + g) * LD + c0 + lane % 16];
-            c = __builtin_amdgcn_mfma_f32_16x16x4f32(a, v, c, 0, 0, 0);
-          }
-        }
-        __syncthreads();
-        if (wave < tiles)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            if (half) t[(r0 + g * 4 + r) * LD + c0 + lane % 16] = -c[r];
-            else m[(r0 + g * 4 + r) * LD + c0 + lane % 16] = c[r];
-          }
-        __syncthreads();
-      }
-    }
-    tri_store<C, LD, GRAD, kState>(t, out + Work::solve, tid, C * 4);
-#pragma unroll
-    for (int ct = 0; ct < C / 16; ++ct)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) m[(wave * 16 + g * 4 + r) * LD + ct * 16 + lane % 16] = qk[ct][r];
-    __syncthreads();
-    tri_store<C, LD, GRAD, PA>(m, out + Work::reads, tid, C * 4);
-    __syncthreads();
-  }
-}
-
 // ------------------------------------------------------------------ operands
 // Rows of 32 k values as operands in LDS, part by part: piece (rows / 16, k / 32) is
 // 64 x 16 bytes, and lane m + 16 g's eight values, row m, k = 8 g .., lie at
@@ -499,6 +364,155 @@ struct OpPair {
   Op<B> b;
 };
 
+// ----------------------------------------------------------- chunks, all at once
+// T and the reads' triangle of every chunk.  GRAD: their transposes, the second one
+// without b.  A wavefront computes 16 rows of K K' and Q K'; the inverse of the
+// diagonal blocks of 16 goes column by column, a lane each, and blocks double by
+// [[A, 0], [B, C]]^-1 = [[A', 0], [-C' B A', C']] on 32-bit matrix instructions.
+template <class T, bool VEC, int DK, bool GRAD>
+__global__ void __launch_bounds__(kChunk<T> * 4, sizeof(T) == 2 ? 4 : 3)
+    k_delta_chunk(DeltaArgs p, const T* q, const T* k, const float* decay, const float* rate, char* work) {
+  constexpr int C = kChunk<T>, LD = C + 4, KS = DK / 32, PI = kIn<T>, PA = GRAD ? kState : kOut<T>, RP = C / 16 * KS;
+  using Work = ChunkWork<C, PA>;
+  constexpr int ROWS = PI * C * DK * 2, BOTH = 2 * C * LD * 4;
+  __shared__ __align__(16) char lds[ROWS > BOTH ? ROWS : BOTH];   // K's rows; then the two triangles
+  float *const m = (float*)lds, *const t = m + C * LD;
+  __shared__ double sum[C];
+  __shared__ float rates[C];
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), g = lane / 16;
+  const int at = lane_place(lane % 16, g);
+  const int64_t all = p.batch * p.heads * p.nchunk;
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const int64_t chunk = u % p.nchunk, b = u / p.nchunk / p.heads;
+    const int head = (int)(u / p.nchunk % p.heads), kh = head / p.group;
+    const int64_t t0 = chunk * C;
+    const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
+    const int n = (int)min((int64_t)C, len - t0);   // steps of this chunk that count
+    if (n <= 0) continue;                           // nothing reads it
+    char* out = work + u * Work::bytes;
+    RowsInFlight<T, VEC, C, DK, C * 4> kr;
+    kr.load(k + b * p.k.b + t0 * p.k.t + kh * p.k.h, p.k.t, n, p.dk, tid);
+    Op<PI> qa[KS];
+    {
+      const int i = wave * 16 + lane % 16;
+      const T* qb = q + b * p.q.b + t0 * p.q.t + kh * p.q.h;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int d = ks * 32 + g * 8, there = i < n ? p.dk - d : 0;
+        qa[ks] = op_load<T, VEC>(qb + (there > 0 ? i * p.q.t + d : 0), there);
+      }
+    }
+    if (tid < C) {
+      double d = 0.0;
+      float r = 0.0f;
+      if (tid < n) {
+        const float x = decay[b * p.decay.b + (t0 + tid) * p.decay.t + head * p.decay.h];
+        d = x < -200.0f ? -200.0 : (double)x;   // exp is 0 in 32 bits long before
+        r = rate[b * p.rate.b + (t0 + tid) * p.rate.t + head * p.rate.h];
+      }
+#pragma unroll
+      for (int o = 1; o < C; o *= 2) {
+        const double x = __shfl_up(d, o, 64);
+        if (tid >= o) d += x;
+      }
+      d *= 1.4426950408889634;
+      const double end = __shfl(d, C - 1, 64);
+      sum[tid] = d;
+      rates[tid] = r;
+      float* s = (float*)(out + Work::scales);
+      s[tid] = __builtin_amdgcn_exp2f((float)d);
+      s[C + tid] = __builtin_amdgcn_exp2f((float)(end - d));
+      s[2 * C + tid] = r;
+    }
+    kr.store(lds, tid);
+    __syncthreads();
+    // rows 16 wave .. of K K' and Q K'
+    f32x4 kk[C / 16], qk[C / 16];
+    {
+      Op<PI> ka[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) ka[ks] = op_take<PI>(lds, RP, wave * KS + ks, at);
+#pragma unroll
+      for (int ct = 0; ct < C / 16; ++ct) {
+        kk[ct] = qk[ct] = zero4();
+        if (ct > wave) continue;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const Op<PI> kb = op_take<PI>(lds, RP, ct * KS + ks, at);
+          kk[ct] = op_mul<PI>(ka[ks], kb, kk[ct]);
+          qk[ct] = op_mul<PI>(qa[ks], kb, qk[ct]);
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ct = 0; ct < C / 16; ++ct)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = wave * 16 + g * 4 + r, j = ct * 16 + lane % 16;
+        float d = 0.0f, x = 0.0f;
+        if (ct <= wave) {
+          d = i >= j ? __builtin_amdgcn_exp2f((float)(sum[i] - sum[j])) : 0.0f;
+          x = i > j ? kk[ct][r] * d * rates[j] : 0.0f;
+          qk[ct][r] *= d * p.scale * (GRAD ? 1.0f : rates[j]);
+        }
+        m[i * LD + j] = x;
+        t[i * LD + j] = 0.0f;
+      }
+    __syncthreads();
+    if (tid < C) {
+      const int d0 = tid / 16 * 16, c = tid % 16;
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float s = i == c ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < i; ++j) s = fmaf(-m[(d0 + i) * LD + d0 + j], x[j], s);
+        x[i] = s;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t[(d0 + i) * LD + d0 + c] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int size = 16; size < C; size *= 2) {
+      // B A', in the place of B, and then -C' of it; a tile of 16 x 16 to a wavefront
+      const int side = size / 16, per = side * side, tiles = C / (2 * size) * per;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        f32x4 c = zero4();
+        int r0 = 0, c0 = 0;
+        if (wave < tiles) {
+          const int pair = wave / per * 2 * size;
+          r0 = pair + size + wave % per / side * 16, c0 = pair + wave % side * 16;
+          for (int x = 0; x < size; x += 4) {
+            const float a = half ? t[(r0 + lane % 16) * LD + pair + size + x + g] : m[(r0 + lane % 16) * LD + pair + x + g];
+            const float v = half ? m[(pair + size + x + g) * LD + c0 + lane % 16] : t[(pair + x + g) * LD + c0 + lane % 16];
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(a, v, c, 0, 0, 0);
+          }
+        }
+        __syncthreads();
+        if (wave < tiles)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (half) t[(r0 + g * 4 + r) * LD + c0 + lane % 16] = -c[r];
+            else m[(r0 + g * 4 + r) * LD + c0 + lane % 16] = c[r];
+          }
+        __syncthreads();
+      }
+    }
+    tri_store<C, LD, GRAD, kState>(t, out + Work::solve, tid, C * 4);
+#pragma unroll
+    for (int ct = 0; ct < C / 16; ++ct)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m[(wave * 16 + g * 4 + r) * LD + ct * 16 + lane % 16] = qk[ct][r];
+    __syncthreads();
+    tri_store<C, LD, GRAD, PA>(m, out + Work::reads, tid, C * 4);
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- chunks in order
 // 64 columns of a chunk of V, Y or dY in LDS.  16 bits: V and dY by steps, Y by
 // columns, 128 bytes a row, its 16-byte words mixed by the row so that transposing
 // reads and writes of columns meet different banks; 32 bits: by steps, 68 values apart.
