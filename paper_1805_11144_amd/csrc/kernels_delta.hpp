@@ -230,7 +230,8 @@ __device__ __forceinline__ Op<P> op_turn(const char* lds, int pieces, int tile, 
 // Row 4 g + r of the 16-row result m of a product over rows of SPREAD columns.
 __device__ __forceinline__ int order_of(int m, int g, int r) { return m / 2 * 32 + g * 8 + m % 2 * 4 + r; }
 
-// A chunk's rows of K or Q on their way from memory to LDS: in registers.
+// A chunk's rows of K or Q on their way from memory to LDS: in registers.  Four threads
+// take 32 values of a row, the next four the next row: 16 of them write to all banks.
 template <class T, bool VEC, int ROWS, int COLS, int THREADS>
 struct RowsInFlight {
   static constexpr int N = ROWS * COLS / 8, U = (N + THREADS - 1) / THREADS, KS = COLS / 32;
@@ -240,7 +241,7 @@ struct RowsInFlight {
   __device__ __forceinline__ void load(const T* x, int64_t stride, int n, int dk, int tid) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = tid + i * THREADS, row = u / (COLS / 8), d = u % (COLS / 8) * 8;
+      const int u = tid + i * THREADS, row = u / 4 % ROWS, d = u / (4 * ROWS) * 32 + u % 4 * 8;
       const bool there = row < n && d < dk;
       const T* from = x + (there ? row * stride + d : 0);
 #pragma unroll
@@ -262,7 +263,7 @@ struct RowsInFlight {
     constexpr int P = kIn<T>;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = tid + i * THREADS, row = u / (COLS / 8), c = u % (COLS / 8);
+      const int u = tid + i * THREADS, row = u / 4 % ROWS, c = u / (4 * ROWS) * 4 + u % 4;
       if (N % THREADS != 0 && u >= N) continue;
       float x[8];
 #pragma unroll

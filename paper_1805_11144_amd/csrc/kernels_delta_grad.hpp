@@ -151,22 +151,22 @@ __global__ void __launch_bounds__(512, 1)
       }
 }
 
-// Wavefronts of k_delta_grad: C / 16 tiles of steps, and the keys dealt to so many of each.
-template <class T, int DK>
-constexpr int kGradParts = kChunk<T> == 64 ? 2 : DK >= 64 ? 4 : 2;
-template <class T, int DK>
-constexpr int kGradThreads = kChunk<T> * 4 * kGradParts<T, DK>;
+// Four computing wavefronts: C / 16 tiles of steps, and the keys dealt to so many of each.
+template <class T>
+constexpr int kGradParts = 64 / kChunk<T>;
 
-// 32 columns of a chunk at a time: rows of K and Q, then rows of S, dS (a column's
-// keys), Z, X (a column's steps) and dY (a step's columns); then, in their place, the
-// four products as operands, 16 steps x 32 steps a piece.
+// 32 columns of a chunk at a time: rows of S, dS (a column's keys), Z, X (a column's
+// steps) and dY (a step's columns), two of these beside each other.  Behind the last
+// ones the rows of K and Q come, and then the four products in the place of the last
+// ones, as operands, 16 steps x 32 steps a piece.
 template <class T, int DK>
 struct GradLds {
-  static constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T, DK>, product = kState * tri_pieces(C) * 1024;
-  static constexpr int k = 0, q = k + PI * C * DK * 2, s = q + PI * C * DK * 2, ds = s + kState * DK * 64,
-                       z = ds + kState * DK * 64, x = z + kState * C * 64, dy = x + kState * C * 64,
-                       products = s, after = dy + PI * C * 64 > s + 4 * product ? dy + PI * C * 64 : s + 4 * product,
-                       sums = after, bytes = sums + (3 * C + 2 * NP * C + 16) * 4 + C * 8;
+  static constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T>, product = kState * tri_pieces(C) * 1024;
+  static constexpr int s = 0, ds = kState * DK * 64, z = 2 * ds, x = z + kState * C * 64, dy = x + kState * C * 64,
+                       slabs = dy + PI * C * 64, k = 0, q = PI * C * DK * 2, rows = 2 * q;
+  static constexpr int most(int a, int b) { return a > b ? a : b; }
+  static constexpr int half = most(slabs, most(rows, 4 * product)), sums = 2 * half,
+                       bytes = sums + (3 * C + 2 * NP * C + 16) * 4 + C * 8;
 };
 
 struct DeltaGradOut {
@@ -187,7 +187,7 @@ struct SlabInFlight {
   __device__ __forceinline__ void load(const float* x, int there, int tid) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = tid + i * THREADS, row = u / (COLS / 8), c = u % (COLS / 8) * 8;
+      const int u = tid + i * THREADS, row = u / 4 % 32, c = u / 128 * 32 + u % 4 * 8;
       v[i][0] = v[i][1] = zero4();
       if ((N % THREADS == 0 || u < N) && c < there) {
         const f32x4* from = (const f32x4*)(x + (uint32_t)(row * there + c));
@@ -199,7 +199,7 @@ struct SlabInFlight {
   __device__ __forceinline__ void store(char* lds, int tid) const {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = tid + i * THREADS, row = column_row(u / (COLS / 8)), c = u % (COLS / 8);
+      const int u = tid + i * THREADS, row = column_row(u / 4 % 32), c = u / 128 * 4 + u % 4;
       if (N % THREADS != 0 && u >= N) continue;
       const Op<kState> o = op_of<kState>(v[i][0], v[i][1]);
 #pragma unroll
@@ -237,165 +237,238 @@ struct StepsInFlight {
   }
 };
 
-// dQ, dK and the gates of a chunk of one key head, its heads one after the other.  A
-// wavefront has 16 steps and a part of the keys.  The four products over the values
-// z dy', z x' (of earlier steps with later ones), dy z', x z' (of later with earlier)
-// are computed beside them, in tiles dealt to all wavefronts, and then are the
-// operands that multiply K and Q.
-template <class T, bool VEC, int DK>
-__global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
+// Chunk u of all key heads and rows: n steps count, `in` are in the arrays.
+struct GradPlace {
+  int64_t chunk, b, t0, step;
+  int kh, n, in;
+  __device__ __forceinline__ GradPlace(const DeltaArgs& p, int key_heads, int64_t u, int C) {
+    chunk = u % p.nchunk, b = u / p.nchunk / key_heads, kh = (int)(u / p.nchunk % key_heads);
+    t0 = chunk * C, step = b * p.steps + t0;
+    const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
+    n = (int)max((int64_t)0, min((int64_t)C, len - t0)), in = (int)min((int64_t)C, p.steps - t0);
+  }
+};
+
+// dQ, dK and the gates of a chunk of one key head, its heads one after the other, and
+// dV.  A workgroup to a CU goes from chunk to chunk.  Four wavefronts feed (256 threads): the next columns' values to the other half
+// of LDS as operands, X out as dV, the gates' sums.  Of the four that compute each
+// has 16 steps and a part of the keys.  The four products over the values z dy', z x'
+// (of earlier steps with later ones), dy z', x z' (of later with earlier) are computed
+// beside, in tiles dealt to all of them, and then are the operands that multiply K, Q.
+// GROUP: heads share key heads, and dQ and dK stay in registers from head to head.
+template <class T, bool VEC, int DK, bool GROUP>
+__global__ void __launch_bounds__(512, 1)
     k_delta_grad(DeltaArgs p, const T* q, const T* k, const T* dy, const float* decay, const float* rate,
                  const float* states, const float* errors, const float* dstates, const float* xs, DeltaGradOut out) {
   using Lds = GradLds<T, DK>;
-  constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T, DK>, THREADS = kGradThreads<T, DK>;
+  constexpr int C = kChunk<T>, PI = kIn<T>, NP = kGradParts<T>;
   constexpr int RT = C / 16, KC = C / 32, NT = DK / 16, MT = NT / NP, KS = DK / 32, RP = RT * KS;
-  constexpr int JOBS = RT * (RT + 1), WAVES = THREADS / 64, MINE = (JOBS + WAVES - 1) / WAVES;
+  constexpr int JOBS = RT * (RT + 1), MINE = (JOBS + 3) / 4;
   extern __shared__ __align__(16) char lds[];
   float* const sc = (float*)(lds + Lds::sums);   // e, o, b
   float* const dg = sc + 3 * C;                  // gradients of G, and k W, by parts
   float* const kw = dg + NP * C;
-  float* const red = kw + NP * C;
+  float* const red = kw + NP * C;                // <dS, S>: of the feeding wavefronts, then the others' part
   double* const sum = (double*)(red + 16);
-  const int tid = threadIdx.x, lane = tid % 64, g = lane / 16;
-  const int all_waves = __builtin_amdgcn_readfirstlane(tid / 64), wave = all_waves % RT, part = all_waves / RT;
-  const int at = lane_place(lane % 16, g), even = turn_place<false>(lane), odd = turn_odd<false>(lane);
-  const int key_heads = p.heads / p.group, kp = pad_keys(p.dk), cols = pad_columns(p.dv);
+  const int key_heads = p.heads / p.group, kp = pad_keys(p.dk), cols = pad_columns(p.dv), rounds = cols / 32;
   const int64_t all = p.batch * key_heads * p.nchunk;
-  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
-    const int64_t chunk = u % p.nchunk, b = u / p.nchunk / key_heads, t0 = chunk * C;
-    const int kh = (int)(u / p.nchunk % key_heads);
-    const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
-    const int n = (int)max((int64_t)0, min((int64_t)C, len - t0)), in = (int)min((int64_t)C, p.steps - t0);
-    f32x4 dq[MT], dk[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) dq[m] = dk[m] = zero4();
-    for (int h = 0; h < p.group; ++h) {
-      const int head = kh * p.group + h;
-      const int64_t bh = b * p.heads + head, cell = bh * p.nchunk + chunk, gate = (b * p.steps + t0) * p.heads + head;
-      T* const dvp = (T*)out.dv + ((b * p.steps + t0) * p.heads + head) * p.dv;
-      if (n == 0) {
-        for (int i = tid; i < in * p.dv; i += THREADS) dvp[(int64_t)(i / p.dv) * p.heads * p.dv + i % p.dv] = (T)0.0f;
-        for (int t = tid; t < in; t += THREADS)
-          out.ddecay[gate + (int64_t)t * p.heads] = out.drate[gate + (int64_t)t * p.heads] = 0.0f;
-        continue;
-      }
-      SlabInFlight<DK, THREADS> sr, dsr;
-      SlabInFlight<C, THREADS> zr, xr;
-      StepsInFlight<T, VEC, C, THREADS> yr;
-      const float *sp = states + cell * kp * cols, *dsp = dstates + cell * kp * cols, *zp = errors + cell * C * cols,
-                  *xp = xs + cell * C * cols;
-      const T* yp = dy + b * p.y.b + t0 * p.y.t + head * p.y.h;
-      const auto ahead = [&](int c) {
-        sr.load(sp + c * kp, kp, tid);
-        dsr.load(dsp + c * kp, kp, tid);
-        zr.load(zp + c * C, C, tid);
-        xr.load(xp + c * C, C, tid);
-        yr.load(yp + c, p.y.t, n, p.dv - c, tid);
-      };
-      if (h == 0) {
-        RowsInFlight<T, VEC, C, DK, THREADS> kr, qr;
-        kr.load(k + b * p.k.b + t0 * p.k.t + kh * p.k.h, p.k.t, n, p.dk, tid);
-        qr.load(q + b * p.q.b + t0 * p.q.t + kh * p.q.h, p.q.t, n, p.dk, tid);
-        ahead(0);
-        __syncthreads();   // what was there is read
-        kr.store(lds + Lds::k, tid);
-        qr.store(lds + Lds::q, tid);
-      } else {
-        ahead(0);
-      }
-      bool forgets = false;
-      if (tid < C) {
-        double d = 0.0;
-        float r = 0.0f;
-        if (tid < n) {
-          const float x = decay[b * p.decay.b + (t0 + tid) * p.decay.t + head * p.decay.h];
-          forgets = x < -200.0f;
-          d = forgets ? -200.0 : (double)x;
-          r = rate[b * p.rate.b + (t0 + tid) * p.rate.t + head * p.rate.h];
+  if (threadIdx.x >= 256) {   // feeds
+    const int tid = threadIdx.x - 256;
+    // the next chunk from u on that has steps; dQ, dK, dV and the gates of those without are zeros
+    const auto some_from = [&](int64_t u) {
+      for (; u < all; u += gridDim.x) {
+        const GradPlace w(p, key_heads, u, C);
+        if (w.n > 0) break;
+        for (int i = tid; i < w.in * p.dk; i += 256) {
+          const int64_t to = ((w.step + i / p.dk) * key_heads + w.kh) * p.dk + i % p.dk;
+          ((T*)out.dq)[to] = ((T*)out.dk)[to] = (T)0.0f;
         }
+        for (int h = w.kh * p.group; h < (w.kh + 1) * p.group; ++h) {
+          for (int i = tid; i < w.in * p.dv; i += 256)
+            ((T*)out.dv)[((w.step + i / p.dv) * p.heads + h) * p.dv + i % p.dv] = (T)0.0f;
+          for (int t = tid; t < w.in; t += 256) out.ddecay[(w.step + t) * p.heads + h] = out.drate[(w.step + t) * p.heads + h] = 0.0f;
+        }
+      }
+      return u;
+    };
+    RowsInFlight<T, VEC, C, DK, 256> kr, qr;
+    SlabInFlight<DK, 256> sr, dsr;
+    SlabInFlight<C, 256> zr, xr;
+    StepsInFlight<T, VEC, C, 256> yr;
+    float dx = 0.0f, rx = 0.0f;   // this thread's step's gates
+    const auto load = [&](const GradPlace& w, int h, int c) {
+      const int64_t cell = (w.b * p.heads + w.kh * p.group + h) * p.nchunk + w.chunk;
+      sr.load(states + cell * kp * cols + c * kp, kp, tid);
+      dsr.load(dstates + cell * kp * cols + c * kp, kp, tid);
+      zr.load(errors + cell * C * cols + c * C, C, tid);
+      xr.load(xs + cell * C * cols + c * C, C, tid);
+      yr.load(dy + w.b * p.y.b + w.t0 * p.y.t + (w.kh * p.group + h) * p.y.h + c, p.y.t, w.n, p.dv - c, tid);
+    };
+    const auto begin = [&](const GradPlace& w, int h) {
+      if (tid < w.n && tid < C) {
+        const int head = w.kh * p.group + h;
+        dx = decay[w.b * p.decay.b + (w.t0 + tid) * p.decay.t + head * p.decay.h];
+        rx = rate[w.b * p.rate.b + (w.t0 + tid) * p.rate.t + head * p.rate.h];
+      }
+      load(w, h, 0);
+      if (h == 0) {
+        kr.load(k + w.b * p.k.b + w.t0 * p.k.t + w.kh * p.k.h, p.k.t, w.n, p.dk, tid);
+        qr.load(q + w.b * p.q.b + w.t0 * p.q.t + w.kh * p.q.h, p.q.t, w.n, p.dk, tid);
+      }
+    };
+    int64_t u = some_from(blockIdx.x);
+    int h = 0;
+    if (u < all) begin(GradPlace(p, key_heads, u, C), 0);
+    while (u < all) {
+      const GradPlace w(p, key_heads, u, C);
+      const int64_t gate = w.step * p.heads + w.kh * p.group + h;
+      const bool counts = tid < C && tid < w.n, forgets = counts && dx < -200.0f;
+      float inner = 0.0f, all_kept = 0.0f;   // <dS, S>, this thread's part
+      const auto store = [&](char* half) {
+        sr.store(half + Lds::s, tid);
+        dsr.store(half + Lds::ds, tid);
+        zr.store(half + Lds::z, tid);
+        xr.store(half + Lds::x, tid);
+        yr.store(half + Lds::dy, tid);
+#pragma unroll
+        for (int i = 0; i < decltype(sr)::U; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) inner = fmaf(sr.v[i][j / 4][j % 4], dsr.v[i][j / 4][j % 4], inner);
+      };
+      if (tid < C) {
+        double d = counts ? forgets ? -200.0 : (double)dx : 0.0;
 #pragma unroll
         for (int o = 1; o < C; o *= 2) {
           const double x = __shfl_up(d, o, 64);
           if (tid >= o) d += x;
         }
         d *= 1.4426950408889634;
-        sum[tid] = d;
         const double end = __shfl(d, C - 1, 64);
+        all_kept = __builtin_amdgcn_exp2f((float)end);
+        sum[tid] = d;
         sc[tid] = __builtin_amdgcn_exp2f((float)d);
         sc[C + tid] = __builtin_amdgcn_exp2f((float)(end - d));
-        sc[2 * C + tid] = r;
+        sc[2 * C + tid] = counts ? rx : 0.0f;
       }
+      store(lds);
+      if (rounds > 1) load(w, h, 32);
+      for (int round = 0; round < rounds; ++round) {
+        __syncthreads();   // this round's values are there, and the other half is read
+        char* const next = lds + (~round & 1) * Lds::half;
+        if (round + 1 < rounds) {
+          store(next);
+          if (round + 2 < rounds) load(w, h, (round + 2) * 32);
+        } else {
+          kr.store(next + Lds::k, tid);
+          qr.store(next + Lds::q, tid);
+        }
+        // X's four columns of a step, as dV
+#pragma unroll
+        for (int j0 = 0; j0 < C * 8; j0 += 256) {
+          typedef short s16x4 __attribute__((ext_vector_type(4)));
+          typedef __attribute__((address_space(3))) s16x4* From;
+          const int i = j0 + tid, s = i % 16, j = i / 16 % 8, tile = i / 128, t = tile * 16 + s, c = round * 32 + j * 4;
+          const int r0 = column_row(j * 4) + s / 4;   // columns of one transposing read, in order
+          f32x4 x = zero4();
+#pragma unroll
+          for (int o = PI - 1; o >= 0; --o) {
+            const char* from = lds + (round & 1) * Lds::half + Lds::x + (o * 2 * KC + r0 / 16 * KC + tile / 2) * 1024 +
+                               lane_place(r0 % 16, tile % 2 * 2 + s % 4 / 2) * 16 + s % 2 * 8;
+            const bf16x4 v = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)from));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] += (float)v[r];
+          }
+          if (t >= w.in || c >= p.dv) continue;
+          Words<T, 4> o;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o.v[r] = (T)x[r];
+          T* const to = (T*)out.dv + (gate + (int64_t)t * p.heads) * p.dv + c;
+          if constexpr (VEC) {
+            *(Words<T, 4>*)to = o;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (c + r < p.dv) to[r] = o.v[r];
+          }
+        }
+      }
+      // the next head's or chunk's first values, while this one's last products are computed
+      if (++h == p.group) h = 0, u = some_from(u + gridDim.x);
+      if (u < all) begin(GradPlace(p, key_heads, u, C), h);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) inner += __shfl_xor(inner, o, 64);
+      if (tid % 64 == 0) red[tid / 64] = inner;
+      __syncthreads();   // K and Q are there, and the last values are read
+      __syncthreads();   // the products are there
+      __syncthreads();   // and read: the sums are there
+      if (tid < C) {
+        float s = 0.0f, v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) s += dg[i * C + tid], v += kw[i * C + tid];
+        if (tid == C - 1) s += all_kept * ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
+#pragma unroll
+        for (int o = 1; o < C; o *= 2) {
+          const float x = __shfl_down(s, o, 64);
+          if (tid + o < C) s += x;
+        }
+        if (tid < w.in) {
+          out.ddecay[gate + (int64_t)tid * p.heads] = counts && !forgets ? s : 0.0f;
+          out.drate[gate + (int64_t)tid * p.heads] = counts ? v : 0.0f;
+        }
+      }
+    }
+    return;
+  }
+  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+    const GradPlace w(p, key_heads, u, C);
+    if (w.n == 0) continue;
+    T* const dqb = (T*)out.dq + (w.step * key_heads + w.kh) * p.dk;
+    T* const dkb = (T*)out.dk + (w.step * key_heads + w.kh) * p.dk;
+    const int in = w.in;
+    const int lane = threadIdx.x % 64, g = lane / 16, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wave = all_waves % RT, part = all_waves / RT;
+    const int at = lane_place(lane % 16, g), even = turn_place<false>(lane), odd = turn_odd<false>(lane);
+    f32x4 dq[MT], dk[MT];
+    if (GROUP)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) dq[m] = dk[m] = zero4();
+    for (int h = 0; h < p.group; ++h) {
       // sums over the values, 32 at a time
       f32x4 eq[MT], er[MT], ew[MT], py[MINE], px[MINE];
-      float inner = 0.0f;   // <dS, S>, this thread's part
 #pragma unroll
       for (int m = 0; m < MT; ++m) eq[m] = er[m] = ew[m] = zero4();
 #pragma unroll
       for (int i = 0; i < MINE; ++i) py[i] = px[i] = zero4();
-      for (int c0 = 0; c0 < cols; c0 += 32) {
+      for (int round = 0; round < rounds; ++round) {
         __syncthreads();
-        sr.store(lds + Lds::s, tid);
-        dsr.store(lds + Lds::ds, tid);
-        zr.store(lds + Lds::z, tid);
-        xr.store(lds + Lds::x, tid);
-        yr.store(lds + Lds::dy, tid);
-#pragma unroll
-        for (int i = 0; i < decltype(sr)::U; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) inner = fmaf(sr.v[i][j / 4][j % 4], dsr.v[i][j / 4][j % 4], inner);
-        __syncthreads();
-        if (c0 + 32 < cols) ahead(c0 + 32);
-        // X's four columns of a step, as dV
-        for (int i = tid; i < C * 8; i += THREADS) {
-          typedef short s16x4 __attribute__((ext_vector_type(4)));
-          typedef __attribute__((address_space(3))) s16x4* From;
-          const int s = i % 16, j = i / 16 % 8, tile = i / 128, t = tile * 16 + s, c = c0 + j * 4;
-          const int row = column_row(j * 4) + s / 4;   // columns of one transposing read, in order
-          Words<T, 4> w;
-          f32x4 x = zero4();
-#pragma unroll
-          for (int o = PI - 1; o >= 0; --o) {
-            const char* from = lds + Lds::x + (o * 2 * KC + row / 16 * KC + tile / 2) * 1024 +
-                               lane_place(row % 16, tile % 2 * 2 + s % 4 / 2) * 16 + s % 2 * 8;
-            const bf16x4 h = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)from));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] += (float)h[r];
-          }
-          if (t >= in || c >= p.dv) continue;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) w.v[r] = (T)x[r];
-          T* const to = dvp + (int64_t)t * p.heads * p.dv + c;
-          if constexpr (VEC) {
-            *(Words<T, 4>*)to = w;
-          } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (c + r < p.dv) to[r] = w.v[r];
-          }
-        }
+        const char* const here = lds + (round & 1) * Lds::half;
         {
-          const Op<kState> zo = op_turn<kState, KC>(lds + Lds::z, 2 * KC, wave, 0, even, odd),
-                           xo = op_turn<kState, KC>(lds + Lds::x, 2 * KC, wave, 0, even, odd);
-          const Op<PI> yo = op_take<PI>(lds + Lds::dy, RT, wave, at);
+          const Op<kState> zo = op_turn<kState, KC>(here + Lds::z, 2 * KC, wave, 0, even, odd),
+                           xo = op_turn<kState, KC>(here + Lds::x, 2 * KC, wave, 0, even, odd);
+          const Op<PI> yo = op_take<PI>(here + Lds::dy, RT, wave, at);
+          auto states_of = ahead_of<2 * MT, 1>([&](int i) {
+            return op_turn<kState, KS>(here + (i % 2 ? Lds::ds : Lds::s), 2 * KS, part * MT + i / 2, 0, even, odd);
+          });
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
-            const Op<kState> so = op_turn<kState, KS>(lds + Lds::s, 2 * KS, part * MT + m, 0, even, odd);
-            eq[m] = op_mul<kState>(yo, so, eq[m]);
-            er[m] = op_mul<kState>(xo, so, er[m]);
-            ew[m] = op_mul<kState>(zo, op_turn<kState, KS>(lds + Lds::ds, 2 * KS, part * MT + m, 0, even, odd), ew[m]);
+            const Op<kState>& o = states_of(2 * m);
+            eq[m] = op_mul<kState>(yo, o, eq[m]);
+            er[m] = op_mul<kState>(xo, o, er[m]);
+            ew[m] = op_mul<kState>(zo, states_of(2 * m + 1), ew[m]);
           }
         }
         // tile i of the first half: steps 16 a .. of Z against 16 c .. of dY and X, a <= c;
         // of the second: 16 c .. of dY and X against 16 a .. of Z
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
-          const int job = all_waves + i * WAVES;
-          if (job >= JOBS) continue;
+          int job = all_waves + i * 4;
+          asm volatile("" : "+s"(job));   // what follows from it is computed here, not kept in registers from round to round
+          if (JOBS % 4 != 0 && job >= JOBS) continue;
           const int half = job < JOBS / 2 ? job : job - JOBS / 2;
           const int c = half < 1 ? 0 : half < 3 ? 1 : half < 6 ? 2 : 3, a = half - c * (c + 1) / 2;
-          const Op<kState> zo = op_turn<kState, KC>(lds + Lds::z, 2 * KC, a, 0, even, odd),
-                           xo = op_turn<kState, KC>(lds + Lds::x, 2 * KC, c, 0, even, odd);
-          const Op<PI> yo = op_take<PI>(lds + Lds::dy, RT, c, at);
+          const Op<kState> zo = op_turn<kState, KC>(here + Lds::z, 2 * KC, a, 0, even, odd),
+                           xo = op_turn<kState, KC>(here + Lds::x, 2 * KC, c, 0, even, odd);
+          const Op<PI> yo = op_take<PI>(here + Lds::dy, RT, c, at);
           if (job < JOBS / 2) {
             py[i] = op_mul<kState>(zo, yo, py[i]);
             px[i] = op_mul<kState>(zo, xo, px[i]);
@@ -405,29 +478,32 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
           }
         }
       }
-      __syncthreads();   // the products take the slabs' place
+      __syncthreads();   // K and Q are there, and the last values are read
+      const char* const rows = lds + (rounds & 1) * Lds::half;
+      char* const products = lds + (~rounds & 1) * Lds::half;
 #pragma unroll
       for (int i = 0; i < MINE; ++i) {
-        const int job = all_waves + i * WAVES;
-        if (job >= JOBS) continue;
+        int job = all_waves + i * 4;
+        asm volatile("" : "+s"(job));
+        if (JOBS % 4 != 0 && job >= JOBS) continue;
         const bool first = job < JOBS / 2;
         const int half = first ? job : job - JOBS / 2;
         const int c = half < 1 ? 0 : half < 3 ? 1 : half < 6 ? 2 : 3, a = half - c * (c + 1) / 2;
         // the operand's row is the lane's column, its 32 columns rows of this result and the next
-        const int mt = first ? c : a, kt = first ? a : c, row = mt * 16 + lane % 16;
+        const int mt = first ? c : a, kt = first ? a : c, step = mt * 16 + lane % 16;
         const int piece = (first ? tri_piece<C, false>(mt, kt / 2) : tri_piece<C, true>(mt, kt / 2)) * 64 + lane;
-        const double mine = sum[row];
+        const double mine = sum[step];
         f32x4 y = py[i], x = px[i];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int t = kt * 16 + g * 4 + r;
-          const bool there = first ? t <= row : t >= row;
+          const bool there = first ? t <= step : t >= step;
           const float d = there ? __builtin_amdgcn_exp2f((float)(first ? mine - sum[t] : sum[t] - mine)) : 0.0f;
           const float w = first ? d * sc[2 * C + t] : d;
           y[r] = there ? y[r] * w * p.scale : 0.0f;
-          x[r] = there && t != row ? (first ? x[r] * w : -x[r] * w) : 0.0f;
+          x[r] = there && t != step ? (first ? x[r] * w : -x[r] * w) : 0.0f;
         }
-        char* const to = lds + Lds::products + (first ? 0 : 2 * Lds::product) + piece * 16 + kt % 2 * 8;
+        char* const to = products + (first ? 0 : 2 * Lds::product) + piece * 16 + kt % 2 * 8;
 #pragma unroll
         for (int o = 0; o < kState; ++o) {
           bf16x4 hy, hx;
@@ -440,20 +516,18 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
           *(bf16x4*)(to + Lds::product + o * tri_pieces(C) * 1024) = hx;
         }
       }
-      // the halves of a piece on the diagonal that no tile fills
+      // the halves of a piece on the diagonal that no tile fills: rows of an even tile have
+      // nothing from the next one, and of an odd one nothing after
       if (all_waves < RT) {
-        const int other = wave ^ 1;
-        const bool first = wave % 2 == 0;   // rows of an even tile have nothing from the next one, and of an odd one nothing after
+        const bool first = wave % 2 == 0;
         const int piece = (first ? tri_piece<C, false>(wave, wave / 2) : tri_piece<C, true>(wave, wave / 2)) * 64 + lane;
-        char* const to = lds + Lds::products + (first ? 0 : 2 * Lds::product) + piece * 16 + other % 2 * 8;
+        char* const to = products + (first ? 0 : 2 * Lds::product) + piece * 16 + (first ? 8 : 0);
 #pragma unroll
         for (int o = 0; o < kState; ++o)
           *(bf16x4*)(to + o * tri_pieces(C) * 1024) = *(bf16x4*)(to + Lds::product + o * tri_pieces(C) * 1024) = bf16x4{};
       }
       float end = 0.0f;   // o[t] b[t] k[t] dS z[t], this lane's part: <dS, K' diag(o b) Z>
-      float rows[4], wk[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) rows[r] = wk[r] = 0.0f;
+      f32x4 total = zero4(), wk = zero4();
       const f32x4 re = *(const f32x4*)(sc + wave * 16 + g * 4), ro = *(const f32x4*)(sc + C + wave * 16 + g * 4),
                   rb = *(const f32x4*)(sc + 2 * C + wave * 16 + g * 4);
       // K or Q of this tile's steps 4 g + r, key 16 m + lane % 16: a transposing read of 4 rows
@@ -464,34 +538,31 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
 #pragma unroll
         for (int o = PI - 1; o >= 0; --o) {
           const char* a = from + (o * RP + wave * KS + m / 2) * 1024 + (m % 2 ? odd : even);
-          const bf16x4 h = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)a));
+          const bf16x4 v = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((From)a));
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[r] += (float)h[r];
+          for (int r = 0; r < 4; ++r) x[r] += (float)v[r];
         }
         return x;
       };
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const f32x4 kv = values(lds + Lds::k, part * MT + m);
+        const f32x4 kv = values(rows + Lds::k, part * MT + m);
+        eq[m] *= re * p.scale, er[m] *= re, ew[m] *= ro;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          eq[m][r] = share_of(re[r], eq[m][r]) * p.scale;
-          er[m][r] = share_of(re[r], er[m][r]);
-          ew[m][r] = share_of(ro[r], ew[m][r]);
-          end = fmaf(rb[r] * kv[r], ew[m][r], end);
-        }
+        for (int r = 0; r < 4; ++r) end = fmaf(rb[r] * kv[r], ew[m][r], end);
       }
-      __syncthreads();
+      __syncthreads();   // the products are there
 #pragma unroll
       for (int ks = 0; ks < KC; ++ks) {
-        const char* const products = lds + Lds::products;
         if (ks <= wave / 2) {
           const int piece = tri_piece<C, false>(wave, ks);
           const Op<kState> y = op_take<kState>(products, tri_pieces(C), piece, lane),
                            x = op_take<kState>(products + Lds::product, tri_pieces(C), piece, lane);
+          auto keys = ahead_of<MT, 2>(
+              [&](int m) { return op_turn<PI, KS>(rows + Lds::k, RP, part * MT + m, ks, even, odd); });
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
-            const Op<PI> kc = op_turn<PI, KS>(lds + Lds::k, RP, part * MT + m, ks, even, odd);
+            const auto& kc = keys(m);
             eq[m] = op_mul<kState>(y, kc, eq[m]);
             er[m] = op_mul<kState>(x, kc, er[m]);
           }
@@ -500,70 +571,50 @@ __global__ void __launch_bounds__((kGradThreads<T, DK>), 1)
           const int piece = tri_piece<C, true>(wave, ks);
           const Op<kState> y = op_take<kState>(products + 2 * Lds::product, tri_pieces(C), piece, lane),
                            x = op_take<kState>(products + 3 * Lds::product, tri_pieces(C), piece, lane);
+          auto both = ahead_of<MT, 1>([&](int m) {
+            return OpPair<PI, PI>{op_turn<PI, KS>(rows + Lds::q, RP, part * MT + m, ks, even, odd),
+                                  op_turn<PI, KS>(rows + Lds::k, RP, part * MT + m, ks, even, odd)};
+          });
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
-            ew[m] = op_mul<kState>(y, op_turn<PI, KS>(lds + Lds::q, RP, part * MT + m, ks, even, odd), ew[m]);
-            ew[m] = op_mul<kState>(x, op_turn<PI, KS>(lds + Lds::k, RP, part * MT + m, ks, even, odd), ew[m]);
+            const auto& o = both(m);
+            ew[m] = op_mul<kState>(y, o.a, ew[m]);
+            ew[m] = op_mul<kState>(x, o.b, ew[m]);
           }
         }
       }
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const f32x4 kv = values(lds + Lds::k, part * MT + m), qv = values(lds + Lds::q, part * MT + m);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          wk[r] = fmaf(kv[r], ew[m][r], wk[r]);
-          rows[r] += qv[r] * eq[m][r] - kv[r] * er[m][r];
-          dq[m][r] += eq[m][r];
-          dk[m][r] += fmaf(rb[r], ew[m][r], -er[m][r]);
-        }
+        const f32x4 kv = values(rows + Lds::k, part * MT + m), qv = values(rows + Lds::q, part * MT + m);
+        wk += kv * ew[m];
+        total += qv * eq[m] - kv * er[m];
+        er[m] = rb * ew[m] - er[m];
+        if (GROUP) dq[m] += eq[m], dk[m] += er[m];
       }
       // sums over the 16 lanes of a row, and over the workgroup
 #pragma unroll
       for (int o = 1; o < 16; o *= 2)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) rows[r] += __shfl_xor(rows[r], o, 64), wk[r] += __shfl_xor(wk[r], o, 64);
-      inner = share_of(sc[C - 1], inner) + end;
+        for (int r = 0; r < 4; ++r) total[r] += __shfl_xor(total[r], o, 64), wk[r] += __shfl_xor(wk[r], o, 64);
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) inner += __shfl_xor(inner, o, 64);
-      if (lane == 0) red[all_waves] = inner;
-      if (lane % 16 == 0)
+      for (int o = 32; o > 0; o >>= 1) end += __shfl_xor(end, o, 64);
+      if (lane == 0) red[4 + all_waves] = end;
+      if (lane % 16 == 0) {
+        *(f32x4*)(dg + part * C + wave * 16 + g * 4) = total - rb * wk;
+        *(f32x4*)(kw + part * C + wave * 16 + g * 4) = wk;
+      }
+      __syncthreads();   // the products are read: the sums are there
+      if (GROUP && h + 1 < p.group) continue;
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int t = wave * 16 + g * 4 + r;
-          dg[part * C + t] = rows[r] - rb[r] * wk[r];
-          kw[part * C + t] = wk[r];
+          const int t = wave * 16 + g * 4 + r, d = (part * MT + m) * 16 + lane % 16;
+          if (t < in && d < p.dk) {
+            dqb[(int64_t)t * key_heads * p.dk + d] = (T)(GROUP ? dq[m][r] : eq[m][r]);
+            dkb[(int64_t)t * key_heads * p.dk + d] = (T)(GROUP ? dk[m][r] : er[m][r]);
+          }
         }
-      __syncthreads();
-      if (tid < C) {
-        float s = 0.0f, w = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) s += dg[i * C + tid], w += kw[i * C + tid];
-        if (tid == C - 1)
-#pragma unroll
-          for (int i = 0; i < WAVES; ++i) s += red[i];
-#pragma unroll
-        for (int o = 1; o < C; o *= 2) {
-          const float x = __shfl_down(s, o, 64);
-          if (tid + o < C) s += x;
-        }
-        if (tid < in) {
-          out.ddecay[gate + (int64_t)tid * p.heads] = tid < n && !forgets ? s : 0.0f;
-          out.drate[gate + (int64_t)tid * p.heads] = tid < n ? w : 0.0f;
-        }
-      }
     }
-    T* const dqb = (T*)out.dq + ((b * p.steps + t0) * key_heads + kh) * p.dk;
-    T* const dkb = (T*)out.dk + ((b * p.steps + t0) * key_heads + kh) * p.dk;
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = wave * 16 + g * 4 + r, d = (part * MT + m) * 16 + lane % 16;
-        if (t < in && d < p.dk) {
-          dqb[(int64_t)t * key_heads * p.dk + d] = (T)dq[m][r];
-          dkb[(int64_t)t * key_heads * p.dk + d] = (T)dk[m][r];
-        }
-      }
   }
 }

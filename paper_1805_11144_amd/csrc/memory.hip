@@ -334,12 +334,15 @@ ms_status ms_gated_delta_grad(const ms_gated_delta_desc* d, const void* q, const
           hipLaunchKernelGGL(back, scan_grid(p), dim3(512), lds, st, a, p.blocks, (const T*)q, (const T*)k, (const T*)dy,
                              dlast, (const char*)w.chunk, ds0, w.dstates, w.xs);
           if (!p.chunks) return;
-          constexpr auto grad = k_delta_grad<T, VEC, DK>;
-          constexpr size_t more = GradLds<T, DK>::bytes;
-          allow_lds(grad, more);
-          hipLaunchKernelGGL(grad, dim3((unsigned)std::min(cells, kMaxBlocks / 2)), dim3(kGradThreads<T, DK>), more, st, a, (const T*)q,
-                             (const T*)k, (const T*)dy, decay, rate, kept, kept + kept_states(p), (const float*)w.dstates,
-                             (const float*)w.xs, DeltaGradOut{dq, dk, dv, ddecay, drate});
+          with_flag(a.group > 1, [&](auto group) {
+            constexpr auto grad = k_delta_grad<T, VEC, DK, decltype(group)::value>;
+            constexpr size_t more = GradLds<T, DK>::bytes;
+            static_assert(more <= 160 * 1024, "LDS");
+            allow_lds(grad, more);
+            hipLaunchKernelGGL(grad, dim3((unsigned)std::min<int64_t>(cells, kCUs)), dim3(512), more, st, a, (const T*)q,
+                               (const T*)k, (const T*)dy, decay, rate, kept, kept + kept_states(p), (const float*)w.dstates,
+                               (const float*)w.xs, DeltaGradOut{dq, dk, dv, ddecay, drate});
+          });
         });
       });
     });
