@@ -80,150 +80,177 @@ __device__ __forceinline__ float team_sum(float s, int team, float* red) {
   return s;
 }
 
-constexpr int kTeamWords = 4;   // words of a thread, at most
-
-// A group's values in a team's registers.
-template <class T, int V, bool WIDE>
+// A group's values in a team's registers, R words of each thread; ONE: one position.
+template <class T, int V, int R, bool WIDE, bool ONE>
 __global__ void __launch_bounds__(256) k_norm_team(NormArgs p, const T* x, T* y) {
   __shared__ float red[4];
-  const int team = WIDE ? 256 : p.team, me = threadIdx.x % team, teams = 256 / team;
-  const int64_t all = p.batch * p.groups, words = p.positions * p.nw;
-  for (int64_t u0 = (int64_t)blockIdx.x * teams; u0 < all; u0 += (int64_t)gridDim.x * teams) {
+  const uint32_t team = WIDE ? 256 : p.team, me = threadIdx.x % team, teams = 256 / team;
+  const uint32_t all = (uint32_t)(p.batch * p.groups), nw = p.nw, words = (uint32_t)p.positions * nw;
+  for (uint32_t u0 = blockIdx.x * teams; u0 < all; u0 += gridDim.x * teams) {
     const bool live = u0 + threadIdx.x / team < all;
-    const int64_t u = live ? u0 + threadIdx.x / team : all - 1, b = u / p.groups;
-    const int g = (int)(u % p.groups);
+    const uint32_t u = live ? u0 + threadIdx.x / team : all - 1, b = u / p.groups, g = u % p.groups;
     const int64_t len = norm_length(p, b);
-    const T* xp = x + b * p.xb;
-    T* yp = y + b * p.yb;
-    Words<T, V> v[kTeamWords];
+    const uint32_t inside = (uint32_t)len * nw;
+    const T* xp = x + b * p.xb + (int64_t)g * p.width;
+    T* yp = y + b * p.yb + (int64_t)g * p.width;
+    Words<T, V> v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint32_t j = me + r * team;
+      if (j < inside) v[r] = *(const Words<T, V>*)(ONE ? xp + j * V : xp + j / nw * p.xt + j % nw * V);
+    }
     float s = 0.0f;
 #pragma unroll
-    for (int r = 0; r < kTeamWords; ++r) {
-      const int64_t j = me + (int64_t)r * team, t = j / p.nw;
-      if (j < words && t < len) v[r] = *(const Words<T, V>*)(xp + t * p.xt + (int64_t)g * p.width + j % p.nw * V);
-    }
-#pragma unroll
-    for (int r = 0; r < kTeamWords; ++r)
-      if (me + (int64_t)r * team < len * p.nw)
+    for (int r = 0; r < R; ++r)
+      if (me + r * team < inside)
 #pragma unroll
         for (int e = 0; e < V; ++e) s += as_f32(v[r].v[e]);
-    const float n = (float)(max(len, (int64_t)1) * p.width);
-    const float mean = team_sum<WIDE>(s, team, red) / n;
+    const float n = 1.0f / (float)(max(len, (int64_t)1) * p.width);
+    const float mean = team_sum<WIDE>(s, team, red) * n;
     s = 0.0f;
 #pragma unroll
-    for (int r = 0; r < kTeamWords; ++r)
-      if (me + (int64_t)r * team < len * p.nw)
+    for (int r = 0; r < R; ++r)
+      if (me + r * team < inside)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float d = as_f32(v[r].v[e]) - mean;
           s = fmaf(d, d, s);
         }
-    const float rstd = 1.0f / sqrtf(team_sum<WIDE>(s, team, red) / n + p.eps);
+    const float rstd = 1.0f / sqrtf(team_sum<WIDE>(s, team, red) * n + p.eps);
     if (!live) continue;
-    if (p.kept && me == 0) p.kept[2 * u] = mean, p.kept[2 * u + 1] = rstd;
+    if (p.kept && me == 0) p.kept[2 * (int64_t)u] = mean, p.kept[2 * (int64_t)u + 1] = rstd;
 #pragma unroll
-    for (int r = 0; r < kTeamWords; ++r) {
-      const int64_t j = me + (int64_t)r * team, t = j / p.nw, c = (int64_t)g * p.width + j % p.nw * V;
+    for (int r = 0; r < R; ++r) {
+      const uint32_t j = me + r * team;
       if (j >= words) continue;
-      const Words<float, V> w = norm_param<V>(p.weight, c, 1.0f), a = norm_param<V>(p.bias, c, 0.0f);
+      const uint32_t c = ONE ? j * V : j % nw * V;
       Words<T, V> o;
+      if (j < inside) {
+        const Words<float, V> w = norm_param<V>(p.weight, (int64_t)g * p.width + c, 1.0f),
+                              a = norm_param<V>(p.bias, (int64_t)g * p.width + c, 0.0f);
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        o.v[e] = t < len ? (T)activated(fmaf((as_f32(v[r].v[e]) - mean) * rstd, w.v[e], a.v[e]), p.act) : (T)0.0f;
-      *(Words<T, V>*)(yp + t * p.yt + c) = o;
+        for (int e = 0; e < V; ++e) o.v[e] = (T)activated(fmaf((as_f32(v[r].v[e]) - mean) * rstd, w.v[e], a.v[e]), p.act);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) o.v[e] = (T)0.0f;
+      }
+      put_once(ONE ? yp + c : yp + j / nw * p.yt + c, o);
     }
   }
 }
 
 // The gradient of one position's groups.  A team keeps its group and goes through
-// every p.lanes-th batch row, with its part of dweight and dbias in registers:
-// parts [lanes][2][channels].
-template <class T, int V, bool WIDE>
+// every p.lanes-th batch row, U of them on their way at a time, with its part of
+// dweight and dbias in registers: parts [lanes][2][channels].
+template <class T, int V, int R, bool WIDE>
 __global__ void __launch_bounds__(256)
     k_norm_team_grad(NormArgs p, const T* x, const T* dy, T* dx, float* parts) {
+  constexpr int U = R * V * sizeof(T) <= 16 ? 4 : R * V * sizeof(T) <= 32 ? 2 : 1;
   __shared__ float red[4];
   const int team = WIDE ? 256 : p.team, me = threadIdx.x % team, teams = 256 / team;
   const int64_t slot = (int64_t)blockIdx.x * teams + threadIdx.x / team;
   const bool mine = slot < (int64_t)p.lanes * p.groups;
   const int g = (int)(slot % p.groups);
   const int64_t lane = slot / p.groups, channels = (int64_t)p.groups * p.width;
-  Words<float, V> w[kTeamWords], a[kTeamWords], dw[kTeamWords], db[kTeamWords];
+  const int64_t first = (int64_t)g * p.width + me * V;
+  bool has[R];
+  Words<float, V> w[R], a[R], dw[R], db[R];
 #pragma unroll
-  for (int r = 0; r < kTeamWords; ++r) {
-    const int j = me + r * team;
-    const int64_t c = (int64_t)g * p.width + (j < p.nw ? j : 0) * V;
+  for (int r = 0; r < R; ++r) {
+    has[r] = me + r * team < p.nw;
+    const int64_t c = has[r] ? first + r * team * V : 0;
     w[r] = norm_param<V>(p.weight, c, 1.0f), a[r] = norm_param<V>(p.bias, c, 0.0f);
 #pragma unroll
     for (int e = 0; e < V; ++e) dw[r].v[e] = db[r].v[e] = 0.0f;
   }
   const float n = 1.0f / (float)p.width;
   // a team of several wavefronts is a workgroup, and goes or stays as one
-  for (int64_t b = mine ? lane : p.batch; b < p.batch; b += p.lanes) {
-    const bool live = norm_length(p, b) > 0;
-    const float mean = p.kept[2 * (b * p.groups + g)], rstd = p.kept[2 * (b * p.groups + g) + 1];
-    Words<T, V> xv[kTeamWords], dv[kTeamWords];
+  for (int64_t b0 = mine ? lane : p.batch; b0 < p.batch; b0 += (int64_t)U * p.lanes) {
+    Words<T, V> xv[U][R], dv[U][R];
+    Words<float, 2> st[U];
 #pragma unroll
-    for (int r = 0; r < kTeamWords; ++r) {
-      const int j = me + r * team;
-      const int64_t c = (int64_t)g * p.width + j * V;
-      if (j < p.nw && live) {
-        xv[r] = *(const Words<T, V>*)(x + b * p.xb + c);
-        dv[r] = *(const Words<T, V>*)(dy + b * p.yb + c);
-      } else {
+    for (int q = 0; q < U; ++q) {
+      const int64_t b = min(b0 + q * (int64_t)p.lanes, p.batch - 1);   // past the last row: read, and not used
+      st[q] = *(const Words<float, 2>*)(p.kept + 2 * (b * p.groups + g));
 #pragma unroll
-        for (int e = 0; e < V; ++e) xv[r].v[e] = dv[r].v[e] = (T)0.0f;
-      }
+      for (int r = 0; r < R; ++r)
+        if (has[r]) {
+          xv[q][r] = *(const Words<T, V>*)(x + b * p.xb + first + r * team * V);
+          dv[q][r] = *(const Words<T, V>*)(dy + b * p.yb + first + r * team * V);
+        }
     }
-    float s1 = 0.0f, s2 = 0.0f, h[kTeamWords][V], d[kTeamWords][V];
 #pragma unroll
-    for (int r = 0; r < kTeamWords; ++r)
+    for (int q = 0; q < U; ++q) {
+      const int64_t b = b0 + q * (int64_t)p.lanes;
+      if (b >= p.batch) continue;
+      const bool live = norm_length(p, b) > 0;   // else nothing that was read counts
+      const float mean = st[q].v[0], rstd = st[q].v[1];
+      float s1 = 0.0f, s2 = 0.0f, h[R][V], d[R][V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        h[r][e] = (as_f32(xv[r].v[e]) - mean) * rstd;
-        const float t = through_act(as_f32(dv[r].v[e]), fmaf(h[r][e], w[r].v[e], a[r].v[e]), p.act);
-        if (me + r * team < p.nw && live) dw[r].v[e] = fmaf(t, h[r][e], dw[r].v[e]), db[r].v[e] += t;
-        d[r][e] = me + r * team < p.nw ? t * w[r].v[e] : 0.0f;
-        s1 += d[r][e];
-        s2 = fmaf(d[r][e], h[r][e], s2);
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const bool in = has[r] && live;
+          h[r][e] = in ? (as_f32(xv[q][r].v[e]) - mean) * rstd : 0.0f;
+          const float t = in ? through_act(as_f32(dv[q][r].v[e]), fmaf(h[r][e], w[r].v[e], a[r].v[e]), p.act) : 0.0f;
+          dw[r].v[e] = fmaf(t, h[r][e], dw[r].v[e]), db[r].v[e] += t;
+          d[r][e] = t * w[r].v[e];
+          s1 += d[r][e];
+          s2 = fmaf(d[r][e], h[r][e], s2);
+        }
+      s1 = team_sum<WIDE>(s1, team, red) * n;
+      s2 = team_sum<WIDE>(s2, team, red) * n;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (!has[r]) continue;
+        Words<T, V> o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o.v[e] = live ? (T)(rstd * (d[r][e] - s1 - h[r][e] * s2)) : (T)0.0f;
+        put_once(dx + b * channels + first + r * team * V, o);
       }
-    s1 = team_sum<WIDE>(s1, team, red) * n;
-    s2 = team_sum<WIDE>(s2, team, red) * n;
-#pragma unroll
-    for (int r = 0; r < kTeamWords; ++r) {
-      const int j = me + r * team;
-      if (j >= p.nw) continue;
-      Words<T, V> o;
-#pragma unroll
-      for (int e = 0; e < V; ++e) o.v[e] = live ? (T)(rstd * (d[r][e] - s1 - h[r][e] * s2)) : (T)0.0f;
-      *(Words<T, V>*)(dx + b * channels + (int64_t)g * p.width + j * V) = o;
     }
   }
   if (mine)
 #pragma unroll
-    for (int r = 0; r < kTeamWords; ++r) {
-      const int j = me + r * team;
-      if (j >= p.nw) continue;
-      float* o = parts + lane * 2 * channels + (int64_t)g * p.width + j * V;
+    for (int r = 0; r < R; ++r) {
+      if (!has[r]) continue;
+      float* o = parts + lane * 2 * channels + first + r * team * V;
       *(Words<float, V>*)o = dw[r];
       *(Words<float, V>*)(o + channels) = db[r];
     }
 }
 
-// Column sums of parts [rows][2 channels] in order, one thread a column, 8 runs of rows.
-__global__ void __launch_bounds__(256) k_norm_columns(const float* parts, int64_t rows, int64_t channels, float* dweight,
-                                                      float* dbias) {
-  __shared__ float red[8][32];
+// Sums of runs of kColumnRows rows of parts [rows][cols], to [runs][cols], or, if there
+// is one run, to dweight and dbias: 32 columns to a workgroup, 32 rows side by side.
+constexpr int kColumnRows = 512;
+
+__global__ void __launch_bounds__(1024) k_norm_columns(const float* parts, int64_t rows, int64_t channels, float* next,
+                                                       float* dweight, float* dbias) {
+  __shared__ float red[32][33];
   const int c = threadIdx.x % 32, k = threadIdx.x / 32;
-  const int64_t col = (int64_t)blockIdx.x * 32 + c;
-  float s = 0.0f;
-  if (col < 2 * channels)
-    for (int64_t r = k; r < rows; r += 8) s += parts[r * 2 * channels + col];
-  red[k][c] = s;
-  __syncthreads();
-  if (k || col >= 2 * channels) return;
+  const int64_t cols = 2 * channels, blocks = (cols + 31) / 32, runs = max((rows + kColumnRows - 1) / kColumnRows, (int64_t)1);
+  for (int64_t u = blockIdx.x; u < blocks * runs; u += gridDim.x) {
+    const int64_t col = u % blocks * 32 + c, row = u / blocks * kColumnRows + k;
+    float v[kColumnRows / 32];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) s += red[i][c];
-  (col < channels ? dweight[col] : dbias[col - channels]) = s;
+    for (int i = 0; i < kColumnRows / 32; ++i)
+      v[i] = col < cols && row + i * 32 < rows ? parts[(row + i * 32) * cols + col] : 0.0f;
+    float s = v[0];
+#pragma unroll
+    for (int i = 1; i < kColumnRows / 32; ++i) s += v[i];
+    red[k][c] = s;
+    __syncthreads();
+    // 32 sums of a column to the lanes of half a wavefront
+    s = red[c][k];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor(s, o, 32);
+    const int64_t mine = u % blocks * 32 + k;
+    if (c == 0 && mine < cols) {
+      if (next) next[u / blocks * cols + mine] = s;
+      else (mine < channels ? dweight[mine] : dbias[mine - channels]) = s;
+    }
+    __syncthreads();
+  }
 }
 
 // ------------------------------------------------------------ many positions
@@ -322,17 +349,17 @@ __global__ void __launch_bounds__(256) k_norm_join(NormArgs p, const float* part
   const int64_t words = (int64_t)p.groups * p.nw, all = p.batch * p.groups;
   for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
     const int64_t b = u / p.groups, len = norm_length(p, b), first = u % p.groups * p.nw;
-    const int64_t runs = (len + p.run - 1) / p.run, n = runs * p.nw;
-    const auto count = [&](int64_t run) { return (double)(min((int64_t)p.run, len - run * p.run) * V); };
+    const uint32_t nw = p.nw, n = (uint32_t)((len + p.run - 1) / p.run) * nw;
+    const auto count = [&](uint32_t run) { return (double)(min((int64_t)p.run, len - (int64_t)run * p.run) * V); };
     const float* at = parts + (b * p.runs * words + first) * 2;
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 256) s += count(i / p.nw) * at[(i / p.nw * words + i % p.nw) * 2];
+    for (uint32_t i = threadIdx.x; i < n; i += 256) s += count(i / nw) * at[(i / nw * words + i % nw) * 2];
     const double total = (double)max(len, (int64_t)1) * p.width, mean = norm_sum64(s, red) / total;
     s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 256) {
-      const float* o = at + (i / p.nw * words + i % p.nw) * 2;
+    for (uint32_t i = threadIdx.x; i < n; i += 256) {
+      const float* o = at + (i / nw * words + i % nw) * 2;
       const double d = o[0] - mean;
-      s += o[1] + count(i / p.nw) * d * d;
+      s += o[1] + count(i / nw) * d * d;
     }
     const double square = norm_sum64(s, red);
     if (threadIdx.x == 0) p.kept[2 * u] = (float)mean, p.kept[2 * u + 1] = (float)(1.0 / sqrt(square / total + p.eps));
@@ -425,10 +452,10 @@ __global__ void __launch_bounds__(256) k_norm_grad_join(NormArgs p, const float*
     const int64_t b = u / p.groups, len = norm_length(p, b), first = u % p.groups * p.width;
     const float* at = parts + b * p.runs * 2 * channels + first;
     double s1 = 0.0, s2 = 0.0;
-    const int64_t n = (len + p.run - 1) / p.run * p.width;
-    for (int64_t i = threadIdx.x; i < n; i += 256) {
-      const int64_t o = i / p.width * 2 * channels + i % p.width;
-      const float w = p.weight ? p.weight[first + i % p.width] : 1.0f;
+    const uint32_t width = p.width, n = (uint32_t)((len + p.run - 1) / p.run) * width;
+    for (uint32_t i = threadIdx.x; i < n; i += 256) {
+      const int64_t o = (int64_t)(i / width) * 2 * channels + i % width;
+      const float w = p.weight ? p.weight[first + i % width] : 1.0f;
       s1 += (double)w * at[o], s2 += (double)w * at[o + channels];
     }
     const double total = (double)max(len, (int64_t)1) * p.width;

@@ -150,7 +150,6 @@ struct Norm {
   int64_t channels, v;
 };
 
-static_assert(kNormWords == kTeamWords, "rule and kernels");
 static_assert(MS_ACT_NONE == kActNone && MS_ACT_RELU == kActRelu && MS_ACT_SILU == kActSilu, "activations");
 
 // v: values of a word, as sizes, strides and pointers allow (1 for workspaces, which hold for any).
@@ -192,7 +191,7 @@ void norm_choose(Norm& p, int64_t v, bool grad) {
 // Scratch memory: parts, then mean and rstd where the caller keeps none (or the
 // groups' sums of the gradient).  Without pointers: the most that any word takes.
 struct NormWork {
-  float *parts, *sums;
+  float *parts, *sums, *next;
   int64_t bytes;
 };
 
@@ -204,7 +203,11 @@ NormWork norm_work(const Norm& p, bool grad, void* ws) {
     w.parts = c.take<float>(a.batch * a.runs * a.groups * a.nw * 2);
     w.sums = c.take<float>(a.batch * a.groups * 2);
   } else if (grad) {
-    w.parts = c.take<float>((a.team ? (int64_t)a.lanes : a.batch * a.runs) * 2 * p.channels);
+    const int64_t rows = a.team ? (int64_t)a.lanes : a.batch * a.runs;
+    w.parts = c.take<float>(rows * 2 * p.channels);
+    int64_t joined = 0;   // rows of all later levels
+    for (int64_t r = rows; r > kColumnRows;) joined += r = (r + kColumnRows - 1) / kColumnRows;
+    w.next = c.take<float>(joined * 2 * p.channels);
     if (!a.team) w.sums = c.take<float>(a.batch * a.groups * 2);
   }
   w.bytes = c.used;
@@ -219,6 +222,14 @@ int64_t norm_most(Norm p, int32_t dtype, bool grad) {
     most = std::max(most, norm_work(p, grad, nullptr).bytes);
   }
   return most;
+}
+
+// Calls f with a team's words to a thread.
+template <class F>
+void with_words(int32_t words, F&& f) {
+  if (words == 1) f(std::integral_constant<int, 1>{});
+  else if (words == 2) f(std::integral_constant<int, 2>{});
+  else f(std::integral_constant<int, 4>{});
 }
 
 unsigned norm_grid(const Norm& p) {
@@ -436,11 +447,25 @@ ms_status ms_group_norm(const ms_group_norm_desc* d, const void* x, const float*
       using T = decltype(zero);
       constexpr int V = decltype(width)::value;
       if (a.team) {
-        const int64_t blocks = (a.batch * a.groups * a.team + 255) / 256;
-        with_flag(a.team > 64, [&](auto many) {
-          hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_team<T, V, decltype(many)::value>),
-                             dim3((unsigned)std::min(blocks, kMaxBlocks)), dim3(256), 0, st, a, (const T*)x, (T*)y);
-        });
+        // groups are counted in 32 bits: as many rows at a time as that allows
+        const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / a.groups), batch = a.batch;
+        for (int64_t b0 = 0; b0 < batch; b0 += most) {
+          NormArgs part = a;
+          part.batch = std::min(most, batch - b0);
+          if (a.lengths) part.lengths += b0;
+          if (a.kept) part.kept += b0 * a.groups * 2;
+          const int64_t blocks = (part.batch * a.groups * a.team + 255) / 256;
+          with_words(p.shape.words, [&](auto each) {
+            with_flag(a.team > 64, [&](auto many) {
+              with_flag(a.positions == 1, [&](auto one) {
+                hipLaunchKernelGGL(
+                    HIP_KERNEL_NAME(k_norm_team<T, V, decltype(each)::value, decltype(many)::value, decltype(one)::value>),
+                    dim3((unsigned)std::min(blocks, kMaxBlocks / 2)), dim3(256), 0, st, part, (const T*)x + b0 * a.xb,
+                    (T*)y + b0 * a.yb);
+              });
+            });
+          });
+        }
         return;
       }
       if (!kept) a.kept = w.sums;
@@ -470,12 +495,18 @@ ms_status ms_group_norm_grad(const ms_group_norm_desc* d, const void* x, const f
     if (!none) need_workspace(workspace, workspace_bytes, norm_most(p, d->dtype, true));
     DeviceGuard dg(d->device);
     const hipStream_t st = (hipStream_t)d->stream;
-    const auto columns = [&](const float* parts, int64_t rows) {
-      hipLaunchKernelGGL(k_norm_columns, dim3((unsigned)((2 * p.channels + 31) / 32)), dim3(256), 0, st, parts, rows,
-                         p.channels, dweight, dbias);
+    const auto columns = [&](const float* parts, int64_t rows, float* next) {
+      const int64_t blocks = (2 * p.channels + 31) / 32;
+      while (true) {
+        const int64_t runs = std::max<int64_t>(1, (rows + kColumnRows - 1) / kColumnRows);
+        hipLaunchKernelGGL(k_norm_columns, dim3((unsigned)std::min(blocks * runs, kMaxBlocks / 4)), dim3(1024), 0, st, parts, rows, p.channels,
+                           runs > 1 ? next : nullptr, dweight, dbias);
+        if (runs == 1) break;
+        parts = next, rows = runs, next += runs * 2 * p.channels;
+      }
       HIPCHECK(hipGetLastError());
     };
-    if (none) return columns(nullptr, 0);
+    if (none) return columns(nullptr, 0, nullptr);
     norm_choose(p, Wide(es).of(a.width).of(a.xb).of(a.xt).of(a.yb).of(a.yt).at(x, es).at(dy, es).at(dx, es).at(weight, 4)
                        .at(bias, 4).v, true);
     const NormWork w = norm_work(p, true, workspace);
@@ -485,9 +516,11 @@ ms_status ms_group_norm_grad(const ms_group_norm_desc* d, const void* x, const f
       constexpr int V = decltype(width)::value;
       if (a.team) {
         const int64_t blocks = ((int64_t)a.lanes * a.groups * a.team + 255) / 256;
-        with_flag(a.team > 64, [&](auto many) {
-          hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_team_grad<T, V, decltype(many)::value>), dim3((unsigned)blocks), dim3(256),
-                             0, st, a, (const T*)x, (const T*)dy, (T*)dx, w.parts);
+        with_words(p.shape.words, [&](auto each) {
+          with_flag(a.team > 64, [&](auto many) {
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_team_grad<T, V, decltype(each)::value, decltype(many)::value>),
+                               dim3((unsigned)blocks), dim3(256), 0, st, a, (const T*)x, (const T*)dy, (T*)dx, w.parts);
+          });
         });
         return;
       }
@@ -498,7 +531,7 @@ ms_status ms_group_norm_grad(const ms_group_norm_desc* d, const void* x, const f
       hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_grad_apply<T, V>), dim3(norm_grid(p)), dim3(256), 0, st, a, (const T*)x,
                          (const T*)dy, (const float*)w.sums, (T*)dx);
     });
-    columns(w.parts, a.team ? (int64_t)a.lanes : a.batch * a.runs);
+    columns(w.parts, a.team ? (int64_t)a.lanes : a.batch * a.runs, w.next);
   });
 }
 

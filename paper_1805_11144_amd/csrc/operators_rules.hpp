@@ -153,6 +153,7 @@ constexpr int kNormWords = 4;   // of a thread that keeps its values, at most
 // kept by a team of threads, or read twice in runs of positions.
 struct NormShape {
   int32_t team;               // threads of a team: a power of two up to 64, or 256; 0: runs
+  int32_t words;              // of a thread of it: 1, 2 or 4
   int32_t lanes;              // of the gradient: batch rows side by side
   int32_t runs, run, wide;    // runs of positions, positions of one, channel words to a row of threads
 };
@@ -166,19 +167,19 @@ inline NormShape norm_shape(int64_t batch, int64_t positions, int64_t groups, in
     s.team = 1;
     while (s.team < 64 && s.team < words) s.team *= 2;
     if (words > 64 * kNormWords) s.team = 256;
-    // one row of groups to 512 workgroups: dweight and dbias are 2 x 512 rows to join
-    const int64_t per = (groups * s.team + 255) / 256;
+    const int64_t each = (words + s.team - 1) / s.team;
+    s.words = each == 1 ? 1 : each == 2 ? 2 : 4;
+    // rows of groups for 512 workgroups: what dweight and dbias are joined from
     s.lanes = (int32_t)std::max<int64_t>(1, std::min(batch, 512 * 256 / s.team / groups));
-    if (per > 512) s.lanes = 1;
     return s;
   }
   const int64_t row = groups * nw;
   s.wide = 1;
   while (s.wide < 256 && s.wide < row) s.wide *= 2;
   const int64_t blocks = (row + s.wide - 1) / s.wide, step = 256 / s.wide;
-  // 2048 workgroups, and 8 positions to a thread at least
+  // 1024 workgroups, and 8 positions to a thread at least
   const int64_t most = std::max<int64_t>(1, (positions + 8 * step - 1) / (8 * step));
-  const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, batch * blocks));
+  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, batch * blocks));
   const int64_t runs = std::max<int64_t>(std::min(most, want), (positions + (1 << 30)) >> 30);
   s.run = (int32_t)std::max<int64_t>(1, (positions + runs - 1) / runs);
   s.runs = (int32_t)((positions + s.run - 1) / s.run);
