@@ -676,12 +676,13 @@ ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rul
  * Strides: between batch rows, steps, heads; 0, 0, 0 = packed.
  * Everything is computed in 32 bits: products run on 16-bit matrix instructions with
  * values as sums of three bf16 parts (24 bits); what passes into a bf16 y only, in two.
- * Values beyond bf16's largest number (3.39e38) count as infinite.
+ * Values beyond bf16's largest number (3.39e38) count as infinite, and those below
+ * 1e-30 keep fewer bits.
  *
  * The gradient, from dL/dy and dL/dlast (NULL for zeros): dq, dk (sums over the heads
  * that share a key head) and dv like q, k and v, packed; ddecay, drate float32, packed;
- * ds0 float32, may be NULL; 0 past a row's length.  q, k, v, decay, rate, kept and
- * lengths are those of the forward call. */
+ * ds0 float32, may be NULL; 0 past a row's length.  q, k, v, decay, rate, kept, lengths
+ * and scale are those of the forward call. */
 typedef struct {
   int64_t batch, steps;              /* >= 0 and < 2^31 */
   int64_t heads, key_heads;          /* heads in [1, 65536], a multiple of key_heads */

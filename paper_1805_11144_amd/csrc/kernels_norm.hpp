@@ -167,11 +167,11 @@ __global__ void __launch_bounds__(256)
   // a team of several wavefronts is a workgroup, and goes or stays as one
   for (int64_t b0 = mine ? lane : p.batch; b0 < p.batch; b0 += (int64_t)U * p.lanes) {
     Words<T, V> xv[U][R], dv[U][R];
-    Words<float, 2> st[U];
+    float mean_of[U], rstd_of[U];
 #pragma unroll
     for (int q = 0; q < U; ++q) {
       const int64_t b = min(b0 + q * (int64_t)p.lanes, p.batch - 1);   // past the last row: read, and not used
-      st[q] = *(const Words<float, 2>*)(p.kept + 2 * (b * p.groups + g));
+      mean_of[q] = p.kept[2 * (b * p.groups + g)], rstd_of[q] = p.kept[2 * (b * p.groups + g) + 1];
 #pragma unroll
       for (int r = 0; r < R; ++r)
         if (has[r]) {
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(256)
       const int64_t b = b0 + q * (int64_t)p.lanes;
       if (b >= p.batch) continue;
       const bool live = norm_length(p, b) > 0;   // else nothing that was read counts
-      const float mean = st[q].v[0], rstd = st[q].v[1];
+      const float mean = mean_of[q], rstd = rstd_of[q];
       float s1 = 0.0f, s2 = 0.0f, h[R][V], d[R][V];
 #pragma unroll
       for (int r = 0; r < R; ++r)

@@ -87,7 +87,8 @@ def check(got, want, name):
 # batch, positions, groups, channels of a group
 SHAPES = [(1, 1, 1, 1), (3, 1, 2, 5), (70, 1, 16, 128), (9, 1, 3, 37), (5, 1, 2, 700), (3, 1, 1, 5000), (2, 1, 70, 1),
           (4, 7, 3, 6), (2, 16, 4, 16), (3, 100, 2, 10), (1, 1000, 5, 8), (3, 777, 9, 37), (2, 300, 2, 640), (2, 64, 1, 4),
-          (300, 3, 1, 8), (1, 40, 1, 2100)]
+          (300, 3, 1, 8), (1, 40, 1, 2100), (5, 1, 2, 800), (3, 1, 2, 101), (4, 1, 2, 203), (2, 1, 3, 401), (2, 1, 1, 1000),
+          (3, 5, 2, 20), (2, 11, 2, 19), (2, 9, 2, 45), (2, 20, 1, 50)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
