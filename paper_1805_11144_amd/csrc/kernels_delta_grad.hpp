@@ -242,7 +242,8 @@ struct GradPlace {
   int64_t chunk, b, t0, step;
   int kh, n, in;
   __device__ __forceinline__ GradPlace(const DeltaArgs& p, int key_heads, int64_t u, int C) {
-    chunk = u % p.nchunk, b = u / p.nchunk / key_heads, kh = (int)(u / p.nchunk % key_heads);
+    const uint32_t nchunk = (uint32_t)p.nchunk, of = (uint32_t)u / nchunk;   // fewer than 2^31 chunks
+    chunk = (uint32_t)u % nchunk, b = of / key_heads, kh = (int)(of % key_heads);
     t0 = chunk * C, step = b * p.steps + t0;
     const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
     n = (int)max((int64_t)0, min((int64_t)C, len - t0)), in = (int)min((int64_t)C, p.steps - t0);
@@ -494,14 +495,15 @@ __global__ void __launch_bounds__(512, 1)
         const int piece = (first ? tri_piece<C, false>(mt, kt / 2) : tri_piece<C, true>(mt, kt / 2)) * 64 + lane;
         const double mine = sum[step];
         f32x4 y = py[i], x = px[i];
+        const int t0 = kt * 16 + g * 4;
+        const f32x4 bt = first ? *(const f32x4*)(sc + 2 * C + t0) : f32x4{1.0f, 1.0f, 1.0f, 1.0f};
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int t = kt * 16 + g * 4 + r;
-          const bool there = first ? t <= step : t >= step;
-          const float d = there ? __builtin_amdgcn_exp2f((float)(first ? mine - sum[t] : sum[t] - mine)) : 0.0f;
-          const float w = first ? d * sc[2 * C + t] : d;
-          y[r] = there ? y[r] * w * p.scale : 0.0f;
-          x[r] = there && t != step ? (first ? x[r] * w : -x[r] * w) : 0.0f;
+          const float apart = (float)(first ? mine - sum[t0 + r] : sum[t0 + r] - mine);
+          const float d = __builtin_amdgcn_exp2f(fminf(apart, 0.0f)) * bt[r];
+          const int before = first ? step - (t0 + r) : t0 + r - step;   // below 0: on the wrong side
+          y[r] = before >= 0 ? y[r] * d * p.scale : 0.0f;
+          x[r] = before > 0 ? x[r] * (first ? d : -d) : 0.0f;
         }
         char* const to = products + (first ? 0 : 2 * Lds::product) + piece * 16 + kt % 2 * 8;
 #pragma unroll

@@ -110,7 +110,7 @@ Delta check_delta(const ms_gated_delta_desc* d, bool grad) {
   p.blocks = (tiles + 3) / 4;
   need(d->batch * d->heads <= kMaxBlocks / 2 / p.blocks - 8, "batch * heads * values is too large");
   p.chunks = d->batch * d->heads * a.nchunk;
-  need(p.chunks < ((int64_t)1 << 34), "batch * heads * steps is too large");
+  need(p.chunks < ((int64_t)1 << 31), "batch * heads * steps is too large");
   p.work = half ? chunk_bytes<__bf16>(grad) : chunk_bytes<float>(grad);
   return p;
 }
