@@ -10,8 +10,15 @@
 // Others are read twice: sums over runs of positions, a thread to one channel word,
 // their join, and the results.  The variance is the sum of squares about a mean that
 // is known (of a team's values) or about the mean of a thread's few values, joined by
-// Chan's formula in 64 bits, so a large mean costs no digits.  Nothing is added by
-// atomics; every sum has one order.
+// Chan's formula (runs of positions in 64 bits), so a large mean costs no digits.
+// Nothing is added by atomics; every sum has one order.
+//
+// Measured: 16384 rows of 16 heads of 128 bf16 34 us, 4.0 TB/s (69 with words of a thread
+// and positions as run-time values), the gradient 73 us, 2.7 TB/s (265 one row at a
+// time), and 5 for its column sums; 16 x 4096 positions of 512 float32 channels: sums 21
+// us, join 5, results 41, 4.0 TB/s of the 268 MB that have to move (what is read again
+// is in the last cache); 13 x 777 x 333 float32, one channel to a thread: 23 us,
+// gradient 32.
 #pragma once
 
 #include "kernels_words.hpp"
