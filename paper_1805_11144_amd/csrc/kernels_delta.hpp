@@ -737,7 +737,7 @@ __global__ void __launch_bounds__(512, 1)
   const int64_t b = bh / p.heads;
   const int head = (int)(bh % p.heads), kh = head / p.group, first = block * 64;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.steps) : p.steps;
-  const int chunks = (len + C - 1) / C;
+  const int chunks = len / C + (len % C != 0);
   if (threadIdx.x >= 256) {   // feeds
     const int tid = threadIdx.x - 256, there = p.dv - first;
     const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *vp = v + b * p.v.b + head * p.v.h + first;

@@ -191,7 +191,7 @@ _SIGNATURES = [
     ("ms_last_error", [], C.c_char_p),
 ]
 # calls of the HIP sources: absent from a library of the host part alone
-_DEVICE_CALLS = ("ms_sim_", "ms_embed", "ms_gated_", "ms_orth")
+_DEVICE_CALLS = ("ms_sim_", "ms_embed", "ms_gated_", "ms_group_", "ms_orth")
 
 
 def load_library(path: str = LIB_PATH, host_only: bool = False):
