@@ -281,3 +281,27 @@ def test_gradients_against_differences():
         z = z * (r[g].double().norm() / (r[g].double() * z.double()).sum().abs()).clamp(max=3).float()
         slope = (loss(dict(i, **{n: i[n] + 1e-3 * z})) - loss(dict(i, **{n: i[n] - 1e-3 * z}))) / 2e-3
         assert abs(slope - float((r[g].double() * z.double()).sum())) <= 2e-3 * float(r[g].norm() * 3 + 1), n
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["one key", "long keys", "two keys", "large values", "small values", "short keys", "strong decays"])
+def test_inputs_far_from_ordinary_ones(kind, dtype):
+    """Keys that repeat without forgetting (a step then undoes the one before it), keys that a step overshoots with,
+    values and keys of other sizes: the bounds are relative, and hold as they are."""
+    i = inputs(1, 320, 1, 2, 64, 48, dtype, 12)
+    if kind == "one key":
+        i.update(k=i["k"][:, :1].expand_as(i["k"]), rate=torch.ones_like(i["rate"]), decay=torch.zeros_like(i["decay"]))
+    elif kind == "long keys":
+        i.update(k=i["k"] * 1.3, rate=torch.ones_like(i["rate"]), decay=torch.zeros_like(i["decay"]))
+    elif kind == "two keys":
+        i.update(k=i["k"][:, :2].repeat(1, 160, 1, 1), rate=torch.full_like(i["rate"], 0.9))
+    elif kind in ("large values", "small values"):
+        f = 1e5 if kind == "large values" else 1e-20
+        i.update(v=(i["v"].float() * f).to(dtype), s0=i["s0"] * f)
+    elif kind == "short keys":
+        i.update(k=(i["k"].float() * 1e-3).to(dtype))
+    else:
+        i.update(decay=i["decay"] * 100)
+    want = reference(i)
+    for name, x in both_passes(i).items():
+        check(x, want[name], name, want["sizes"].get(name))
