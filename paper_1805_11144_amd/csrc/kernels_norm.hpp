@@ -13,9 +13,10 @@
 // Chan's formula (runs of positions in 64 bits), so a large mean costs no digits.
 // Nothing is added by atomics; every sum has one order.
 //
-// Measured: 16384 rows of 16 heads of 128 bf16 34 us, 4.0 TB/s (69 with words of a thread
-// and positions as run-time values), the gradient 73 us, 2.7 TB/s (265 one row at a
-// time), and 5 for its column sums; 16 x 4096 positions of 512 float32 channels: sums 21
+// Measured: 16384 rows of 16 heads of 128 bf16 32 us, 4.2 TB/s (69 with words of a thread
+// and positions as run-time values, 34 with a team's sums through LDS), the gradient 63
+// us, 3.2 TB/s (265 one row at a time, 73 with sums through LDS), and 5 for its column
+// sums; 16 x 4096 positions of 512 float32 channels: sums 21
 // us, join 5, results 41, 4.0 TB/s of the 268 MB that have to move (what is read again
 // is in the last cache); 13 x 777 x 333 float32, one channel to a thread: 23 us,
 // gradient 32.
@@ -73,11 +74,24 @@ __device__ __forceinline__ Words<float, V> norm_param(const float* w, int64_t c,
   return r;
 }
 
+// x of another lane: CTRL says which, within 16 lanes and without a way through LDS.
+template <int CTRL>
+__device__ __forceinline__ float lane_dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+
 // Sums over a team: lanes of a wavefront (a power of two), or the 4 wavefronts of a
-// workgroup.
+// workgroup.  Up to 16 lanes each adds its pair's, its four's other pair's, its eight's
+// other four's and the other eight's, the last two from the mirror image, which holds
+// the same sum in every lane of that half.
 template <bool WIDE>
 __device__ __forceinline__ float team_sum(float s, int team, float* red) {
-  for (int o = 1; o < (WIDE ? 64 : team); o *= 2) s += __shfl_xor(s, o, 64);
+  const int lanes = WIDE ? 64 : team;
+  if (lanes > 1) s += lane_dpp<0xB1>(s);    // quad_perm 1 0 3 2
+  if (lanes > 2) s += lane_dpp<0x4E>(s);    // quad_perm 2 3 0 1
+  if (lanes > 4) s += lane_dpp<0x141>(s);   // row_half_mirror
+  if (lanes > 8) s += lane_dpp<0x140>(s);   // row_mirror
+  for (int o = 16; o < lanes; o *= 2) s += __shfl_xor(s, o, 64);
   if constexpr (WIDE) {
     __syncthreads();
     if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = s;
