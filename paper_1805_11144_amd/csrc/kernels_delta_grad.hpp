@@ -31,7 +31,7 @@
 // waiting for values.  Step by step: 1290 us with everything in one group of
 // wavefronts, 880 with the four products computed once a workgroup, 500 with
 // wavefronts that feed and go on to the next chunk, 440 with the decays between steps
-// without branches.  Two rounds of values on their way need more registers than there
+// without branches.  Two sets of values on their way need more registers than there
 // are: 590 to 650.
 #pragma once
 
@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(512, 1)
       store(lds);
       if (rounds > 1) load(w, h, 32);
       for (int round = 0; round < rounds; ++round) {
-        __syncthreads();   // this round's values are there, and the other half is read
+        __syncthreads();   // these columns' values are there, and the other half is read
         char* const next = lds + (~round & 1) * Lds::half;
         if (round + 1 < rounds) {
           store(next);
