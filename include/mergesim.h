@@ -686,7 +686,7 @@ ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rul
  * ds0 float32, may be NULL; 0 past a row's length.  q, k, v, decay, rate, kept, lengths
  * and scale are those of the forward call. */
 typedef struct {
-  int64_t batch, steps;              /* >= 0 and < 2^31 */
+  int64_t batch, steps;              /* >= 0 and < 2^31; batch * heads * ceil(values / 64) < 2^22 - 2^13 */
   int64_t heads, key_heads;          /* heads in [1, 65536], a multiple of key_heads */
   int64_t keys, values;              /* keys in [1, 128], values in [1, 65536], heads * values < 2^24 */
   int64_t q_stride[3], k_stride[3], v_stride[3];   /* between steps of v and y: below 2^24 */
