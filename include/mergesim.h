@@ -675,8 +675,8 @@ ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rul
  *               the library's own; NULL if no gradient is wanted
  * Strides: between batch rows, steps, heads; 0, 0, 0 = packed.
  * Everything is computed in 32 bits: products run on 16-bit matrix instructions with
- * values as sums of three bf16 parts (24 bits); what passes into a bf16 y only, in two.
- * The workspace takes about 500 bytes a step and head; `kept`, and the gradient's
+ * values as sums of three bf16 parts (24 bits), and y is rounded once.
+ * The workspace takes about 600 bytes a step and head (float32: 400); `kept`, and the gradient's
  * workspace again, a matrix each 64 (float32: 32) steps and 4 bytes a value of v.
  * Values beyond bf16's largest number (3.39e38) count as infinite, and those below
  * 1e-30 keep fewer bits.

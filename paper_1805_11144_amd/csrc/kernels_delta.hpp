@@ -23,10 +23,10 @@
 // Arithmetic: 16-bit matrix instructions, 16 times as fast as 32-bit ones.  A
 // 32-bit value is the sum of three bf16 parts (24 bits, and bf16 has float32's
 // range), bf16 inputs are one part, and products of parts below 2^-24 of the result
-// are left out: 3 products with an input, 6 between two 32-bit values.  What only
-// passes into a bf16 result, and not into the state (the second term of Y, and the
-// state read by Q), takes two parts, 16 bits for a result of 8.  The sums of decays
-// are 64-bit: a difference of two of them is good where each is large.
+// are left out: 3 products with an input, 6 between two 32-bit values.  So it is also for
+// what passes into a bf16 result only (the second term of Y, and the state read by Q):
+// with two parts, a read that cancels lost more than the result's own rounding.  The
+// sums of decays are 64-bit: a difference of two of them is good where each is large.
 //
 // What bounds it.  The scan: a chunk's chain of dependent products.  2 x 16384 steps of
 // 16 heads of 128 x 128 bf16, 32 heads on 64 workgroups: 770 us, 256 chunks of 3.0 us or
@@ -64,14 +64,12 @@ struct DeltaArgs {
 
 // A chunk's steps.  Products with the state take the same time for any length, those
 // within a chunk grow with it, and the chain of chunks shrinks; the operands of two
-// chunks of 64 steps in one part take 157 KB of LDS, of 32 steps in three parts 155.
+// chunks of 64 steps in one part take 154 KB of LDS, of 32 steps in three parts 155.
 template <class T>
 constexpr int kChunk = sizeof(T) == 2 ? 64 : 32;
 template <class T>
 constexpr int kIn = sizeof(T) == 2 ? 1 : 3;    // parts of an input
-template <class T>
-constexpr int kOut = sizeof(T) == 2 ? 2 : 3;   // of what only a result in T sees
-constexpr int kState = 3;                      // of everything else
+constexpr int kState = 3;                      // of what is computed
 
 // Eight values of an operand's row, as P parts.
 template <int P>
@@ -161,12 +159,11 @@ __device__ __forceinline__ constexpr bool tri_has(int mt, int ks) {
   return UPPER ? ks >= mt / 2 : ks <= mt / 2;
 }
 
-// What k_delta_chunk leaves of a chunk: T in three parts, the reads' triangle in PA
-// parts, each piece 64 x 16 bytes, then e, o and b.
-template <int C, int PA>
+// What k_delta_chunk leaves of a chunk: T and the reads' triangle in three parts, each
+// piece 64 x 16 bytes, then e, o and b.
+template <int C>
 struct ChunkWork {
-  static constexpr int solve = 0, reads = kState * tri_pieces(C) * 1024, scales = reads + PA * tri_pieces(C) * 1024,
-                       bytes = scales + 3 * C * 4;
+  static constexpr int solve = 0, reads = kState * tri_pieces(C) * 1024, scales = 2 * reads, bytes = scales + 3 * C * 4;
 };
 
 // The pieces of a triangle in LDS (rows LD apart), as operands, to memory.
@@ -386,8 +383,8 @@ struct OpPair {
 template <class T, bool VEC, int DK, bool GRAD>
 __global__ void __launch_bounds__(kChunk<T> * 4, sizeof(T) == 2 ? 4 : 3)
     k_delta_chunk(DeltaArgs p, const T* q, const T* k, const float* decay, const float* rate, char* work) {
-  constexpr int C = kChunk<T>, LD = C + 4, KS = DK / 32, PI = kIn<T>, PA = GRAD ? kState : kOut<T>, RP = C / 16 * KS;
-  using Work = ChunkWork<C, PA>;
+  constexpr int C = kChunk<T>, LD = C + 4, KS = DK / 32, PI = kIn<T>, RP = C / 16 * KS;
+  using Work = ChunkWork<C>;
   constexpr int ROWS = PI * C * DK * 2, BOTH = 2 * C * LD * 4;
   __shared__ __align__(16) char lds[ROWS > BOTH ? ROWS : BOTH];   // K's rows; then the two triangles
   float *const m = (float*)lds, *const t = m + C * LD;
@@ -521,7 +518,7 @@ __global__ void __launch_bounds__(kChunk<T> * 4, sizeof(T) == 2 ? 4 : 3)
 #pragma unroll
       for (int r = 0; r < 4; ++r) m[(wave * 16 + g * 4 + r) * LD + ct * 16 + lane % 16] = qk[ct][r];
     __syncthreads();
-    tri_store<C, LD, GRAD, PA>(m, out + Work::reads, tid, C * 4);
+    tri_store<C, LD, GRAD, kState>(m, out + Work::reads, tid, C * 4);
     __syncthreads();
   }
 }
@@ -655,37 +652,41 @@ __device__ __forceinline__ void panel_out(const char* lds, T* y, int32_t stride,
 }
 
 // One of the two halves of a scan's LDS: rows of K and of Q, the chunk's triangles and
-// scales, V or dY; behind them two panels of Y.
+// scales; behind them panels of V or dY, and of Y.  PAIRS: two of each panel, one for
+// each half; chunks of 64 steps of 128 keys leave room for one, and pay for it with a
+// barrier more.
 template <class T, int DK, bool GRAD>
 struct ScanLds {
-  static constexpr int C = kChunk<T>, PA = GRAD ? kState : kOut<T>;
-  static constexpr int k = 0, q = kIn<T> * C * DK * 2, work = 2 * q, panel = work + ChunkWork<C, PA>::bytes,
-                       bytes = panel + Panel<T>::bytes, out = 2 * bytes, all = out + (GRAD ? 0 : 2 * Panel<T>::bytes);
+  static constexpr int C = kChunk<T>, each = Panel<T>::bytes;
+  static constexpr int k = 0, q = kIn<T> * C * DK * 2, work = 2 * q, bytes = work + ChunkWork<C>::bytes, panel = 2 * bytes;
+  static constexpr bool PAIRS = GRAD || panel + 4 * each <= 160 * 1024;
+  static constexpr int out = panel + (PAIRS ? 2 : 1) * each, all = out + (GRAD ? 0 : out - panel);
+  static __device__ __forceinline__ int panel_of(int chunk) { return PAIRS ? panel + (chunk & 1) * each : panel; }
+  static __device__ __forceinline__ int out_of(int chunk) { return PAIRS ? out + (chunk & 1) * each : out; }
 };
 
 // A chunk's operands on their way from memory to one half, by 256 threads.
 template <class T, bool VEC, int DK, bool GRAD>
 struct ChunkInFlight {
   using Lds = ScanLds<T, DK, GRAD>;
-  static constexpr int C = Lds::C, BYTES = ChunkWork<C, Lds::PA>::bytes;
+  static constexpr int C = Lds::C, BYTES = ChunkWork<C>::bytes;
   RowsInFlight<T, VEC, C, DK, 256> k, q;
   WorkInFlight<BYTES, 256> w;
   PanelInFlight<T, VEC> x;
 
-  __device__ __forceinline__ void load(const DeltaArgs& p, const T* kp, const T* qp, const T* xp, const Walk& xw,
-                                       const char* wp, int64_t chunk, int n, int there, int tid) {
+  // all but the panel
+  __device__ __forceinline__ void load(const DeltaArgs& p, const T* kp, const T* qp, const char* wp, int64_t chunk, int n,
+                                       int tid) {
     const int64_t t0 = chunk * C;
     w.load(wp + chunk * BYTES, tid);
     k.load(kp + t0 * p.k.t, p.k.t, n, p.dk, tid);
     q.load(qp + t0 * p.q.t, p.q.t, n, p.dk, tid);
-    x.load(xp + t0 * xw.t, (int32_t)xw.t, n, there, tid);
   }
 
   __device__ __forceinline__ void store(char* half, int tid) const {
     w.store(half + Lds::work, tid);
     k.store(half + Lds::k, tid);
     q.store(half + Lds::q, tid);
-    x.store(half + Lds::panel, tid);
   }
 };
 
@@ -728,8 +729,8 @@ __global__ void __launch_bounds__(512, 1)
     k_delta_scan(DeltaArgs p, int blocks, const T* q, const T* k, const T* v, const float* decay, const float* s0,
                  const char* work, T* y, float* last, float* states, float* errors) {
   using Lds = ScanLds<T, DK, false>;
-  constexpr int C = Lds::C, KS = DK / 32, PA = Lds::PA, PI = kIn<T>, RP = C / 16 * KS;
-  using Work = ChunkWork<C, PA>;
+  constexpr int C = Lds::C, KS = DK / 32, PI = kIn<T>, RP = C / 16 * KS;
+  using Work = ChunkWork<C>;
   extern __shared__ __align__(16) char lds[];
   int64_t bh;
   int block;
@@ -744,25 +745,33 @@ __global__ void __launch_bounds__(512, 1)
     T* const yp = y + b * p.y.b + head * p.y.h + first;
     const char* wp = work + bh * p.nchunk * Work::bytes;
     ChunkInFlight<T, VEC, DK, false> f;
-    if (chunks > 0) {
-      f.load(p, kp, qp, vp, p.v, wp, 0, min(C, len), there, tid);
-      f.store(lds, tid);
-    }
-    if (chunks > 1) f.load(p, kp, qp, vp, p.v, wp, 1, min(C, len - C), there, tid);
+    const auto load = [&](int chunk) { f.load(p, kp, qp, wp, chunk, min(C, len - chunk * C), tid); };
+    const auto load_panel = [&](int chunk) {
+      f.x.load(vp + (int64_t)chunk * C * p.v.t, (int32_t)p.v.t, min(C, len - chunk * C), there, tid);
+    };
+    const auto store = [&](int chunk) { f.store(lds + (chunk & 1) * Lds::bytes, tid); };
+    const auto store_panel = [&](int chunk) { f.x.store(lds + Lds::panel_of(chunk), tid); };
+    const auto out = [&](int chunk) {
+      panel_out<T, VEC>(lds + Lds::out_of(chunk), yp + (int64_t)chunk * C * p.y.t, (int32_t)p.y.t, min(C, len - chunk * C),
+                        there, tid);
+    };
+    if (chunks > 0) load(0), load_panel(0), store(0), store_panel(0);
+    if (chunks > 1) load(1), load_panel(1);
     for (int64_t t = len + tid / 64; t < p.steps; t += 4)
       if (tid % 64 < there) yp[t * p.y.t + tid % 64] = (T)0.0f;
     for (int chunk = 0; chunk < chunks; ++chunk) {
+      const bool next = chunk + 1 < chunks, after = chunk + 2 < chunks;
       __syncthreads();   // this chunk's operands are there, the other half is read and the last results are written
-      if (chunk + 1 < chunks) f.store(lds + (~chunk & 1) * Lds::bytes, tid);
-      if (chunk + 2 < chunks) f.load(p, kp, qp, vp, p.v, wp, chunk + 2, min(C, len - (chunk + 2) * C), there, tid);
-      if (chunk > 0)
-        panel_out<T, VEC>(lds + Lds::out + (~chunk & 1) * Panel<T>::bytes, yp + (int64_t)(chunk - 1) * C * p.y.t,
-                          (int32_t)p.y.t, C, there, tid);
+      if (!Lds::PAIRS && chunk > 0) out(chunk - 1);
+      if (next) store(chunk + 1);
+      if (after) load(chunk + 2);
+      if (!Lds::PAIRS) __syncthreads();   // V is read, and the last results are out
+      if (next) store_panel(chunk + 1);
+      if (after) load_panel(chunk + 2);
+      if (Lds::PAIRS && chunk > 0) out(chunk - 1);
     }
     __syncthreads();
-    if (chunks > 0)
-      panel_out<T, VEC>(lds + Lds::out + (~chunks & 1) * Panel<T>::bytes, yp + (int64_t)(chunks - 1) * C * p.y.t,
-                        (int32_t)p.y.t, len - (chunks - 1) * C, there, tid);
+    if (chunks > 0) out(chunks - 1);
     return;
   }
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = lane / 16, at = lane_place(lane % 16, g);
@@ -782,7 +791,10 @@ __global__ void __launch_bounds__(512, 1)
   for (int chunk = 0; chunk < chunks; ++chunk) {
     const char* const here = lds + (chunk & 1) * Lds::bytes;
     __syncthreads();
-    if (!some) continue;
+    if (!some) {
+      if (!Lds::PAIRS) __syncthreads();
+      continue;
+    }
     if (KEEP) put_state<DK>(states + (bh * p.nchunk + chunk) * pad_keys(p.dk) * pad_columns(p.dv), p.dk, col, g, s);
     constexpr int TRI = tri_pieces(C), NEAR = sizeof(T) == 2 ? 3 : 1;   // 5 products to a pair, or 12
     const char* const tri = here + Lds::work;
@@ -791,7 +803,7 @@ __global__ void __launch_bounds__(512, 1)
       return OpPair<PI, PI>{op_take<PI>(here + Lds::k, RP, i, at), op_take<PI>(here + Lds::q, RP, i, at)};
     });
     f32x4 z[C / 16], o[C / 16];
-    panel_take<T>(here + Lds::panel, wave, lane, z);
+    panel_take<T>(lds + Lds::panel_of(chunk), wave, lane, z);
     Op<kState> sp[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) sp[ks] = op_of<kState>(s[2 * ks], s[2 * ks + 1]);
@@ -802,7 +814,7 @@ __global__ void __launch_bounds__(512, 1)
       for (int ks = 0; ks < KS; ++ks) {
         const auto& x = kq(m * KS + ks);
         c = op_mul<kState>(x.a, sp[ks], c);
-        w = op_mul<kOut<T>>(x.b, sp[ks], w);
+        w = op_mul<kState>(x.b, sp[ks], w);
       }
       const f32x4 em = *(const f32x4*)(e + m * 16 + g * 4);
 #pragma unroll
@@ -819,17 +831,17 @@ __global__ void __launch_bounds__(512, 1)
       z[m] = op_mul<kState>(solve(i), zp[ks], z[m]);
     });
     if (KEEP) put_rows<C>(errors + (bh * p.nchunk + chunk) * C * pad_columns(p.dv), col, g, z);
-    auto reads = ahead_of<TRI, 3>([&](int i) { return op_take<PA>(tri + Work::reads, TRI, i, lane); });
-    Op<kOut<T>> zo[C / 32];
+    auto reads = ahead_of<TRI, 3>([&](int i) { return op_take<kState>(tri + Work::reads, TRI, i, lane); });
 #pragma unroll
-    for (int ks = 0; ks < C / 32; ++ks) zo[ks] = op_of<kOut<T>>(z[2 * ks], z[2 * ks + 1]);
+    for (int ks = 0; ks < C / 32; ++ks) zp[ks] = op_of<kState>(z[2 * ks], z[2 * ks + 1]);
     each<TRI>([&](auto i) {
       constexpr int m = tri_row<C, false>(i), ks = tri_column<C, false>(i);
-      o[m] = op_mul<kOut<T>>(reads(i), zo[ks], o[m]);
+      o[m] = op_mul<kState>(reads(i), zp[ks], o[m]);
     });
+    if (!Lds::PAIRS) __syncthreads();   // V is read, and the last results are out
     auto turned = ahead_of<RP, NEAR + 1>(
         [&](int i) { return op_turn<PI, KS>(here + Lds::k, RP, i / (C / 32), i % (C / 32), even, odd); });
-    panel_put<T>(lds + Lds::out + (chunk & 1) * Panel<T>::bytes, wave, lane, o);
+    panel_put<T>(lds + Lds::out_of(chunk), wave, lane, o);
 #pragma unroll
     for (int m = 0; m < C / 16; ++m) {
       const f32x4 om = *(const f32x4*)(e + C + m * 16 + g * 4), bm = *(const f32x4*)(e + 2 * C + m * 16 + g * 4);

@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(512, 1)
                  float* ds0, float* dstates, float* xs) {
   using Lds = ScanLds<T, DK, true>;
   constexpr int C = Lds::C, KS = DK / 32, PI = kIn<T>, RP = C / 16 * KS;
-  using Work = ChunkWork<C, kState>;
+  using Work = ChunkWork<C>;
   extern __shared__ __align__(16) char lds[];
   int64_t bh;
   int block;
@@ -58,15 +58,20 @@ __global__ void __launch_bounds__(512, 1)
     const T *kp = k + b * p.k.b + kh * p.k.h, *qp = q + b * p.q.b + kh * p.q.h, *yp = dy + b * p.y.b + head * p.y.h + first;
     const char* wp = work + bh * p.nchunk * Work::bytes;
     ChunkInFlight<T, VEC, DK, true> f;
-    const auto load = [&](int chunk) { f.load(p, kp, qp, yp, p.y, wp, chunk, min(C, len - chunk * C), there, tid); };
-    if (chunks > 0) {
-      load(chunks - 1);
-      f.store(lds + (~chunks & 1) * Lds::bytes, tid);
-    }
+    const auto load = [&](int chunk) {
+      const int n = min(C, len - chunk * C);
+      f.load(p, kp, qp, wp, chunk, n, tid);
+      f.x.load(yp + (int64_t)chunk * C * p.y.t, (int32_t)p.y.t, n, there, tid);
+    };
+    const auto store = [&](int chunk) {
+      f.store(lds + (chunk & 1) * Lds::bytes, tid);
+      f.x.store(lds + Lds::panel_of(chunk), tid);
+    };
+    if (chunks > 0) load(chunks - 1), store(chunks - 1);
     if (chunks > 1) load(chunks - 2);
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
       __syncthreads();   // this chunk's operands are there, and the other half is read
-      if (chunk > 0) f.store(lds + (~chunk & 1) * Lds::bytes, tid);
+      if (chunk > 0) store(chunk - 1);
       if (chunk > 1) load(chunk - 2);
     }
     return;
@@ -107,7 +112,7 @@ __global__ void __launch_bounds__(512, 1)
     }
     {
       auto reads = ahead_of<TRI, 2>([&](int i) { return op_take<kState>(tri + Work::reads, TRI, tri_upper<C>(i), lane); });
-      panel_take<T>(here + Lds::panel, wave, lane, dyr);
+      panel_take<T>(lds + Lds::panel_of(chunk), wave, lane, dyr);
       Op<PI> dp[C / 32];
 #pragma unroll
       for (int ks = 0; ks < C / 32; ++ks) dp[ks] = op_of<PI>(dyr[2 * ks], dyr[2 * ks + 1]);

@@ -74,12 +74,7 @@ struct Delta {
   int blocks;   // of four tiles of 16 columns
 };
 
-template <class T>
-int64_t chunk_bytes(bool grad) {
-  return grad ? ChunkWork<kChunk<T>, kState>::bytes : ChunkWork<kChunk<T>, kOut<T>>::bytes;
-}
-
-Delta check_delta(const ms_gated_delta_desc* d, bool grad) {
+Delta check_delta(const ms_gated_delta_desc* d) {
   need(d != nullptr, "NULL descriptor");
   need(d->steps >= 0 && d->steps < ((int64_t)1 << 31), "steps must be in [0, 2^31)");
   need(d->batch >= 0 && d->batch < ((int64_t)1 << 31), "batch must be in [0, 2^31)");
@@ -111,7 +106,7 @@ Delta check_delta(const ms_gated_delta_desc* d, bool grad) {
   need(d->batch * d->heads <= kMaxBlocks / 2 / p.blocks - 8, "batch * heads * values is too large");
   p.chunks = d->batch * d->heads * a.nchunk;
   need(p.chunks < ((int64_t)1 << 31), "batch * heads * steps is too large");
-  p.work = half ? chunk_bytes<__bf16>(grad) : chunk_bytes<float>(grad);
+  p.work = half ? ChunkWork<kChunk<__bf16>>::bytes : ChunkWork<kChunk<float>>::bytes;
   return p;
 }
 
@@ -243,7 +238,7 @@ extern "C" {
 
 ms_status ms_gated_delta_kept(const ms_gated_delta_desc* d, int64_t* elements_out) {
   return guarded([&] {
-    const Delta p = check_delta(d, false);
+    const Delta p = check_delta(d);
     need(elements_out != nullptr, "NULL output");
     *elements_out = kept_states(p) + kept_rows(p);
   });
@@ -251,7 +246,7 @@ ms_status ms_gated_delta_kept(const ms_gated_delta_desc* d, int64_t* elements_ou
 
 ms_status ms_gated_delta_workspace(const ms_gated_delta_desc* d, int32_t grad, int64_t* bytes_out) {
   return guarded([&] {
-    const Delta p = check_delta(d, grad != 0);
+    const Delta p = check_delta(d);
     need(bytes_out != nullptr, "NULL output");
     *bytes_out = delta_work(p, grad != 0, nullptr).bytes;
   });
@@ -261,7 +256,7 @@ ms_status ms_gated_delta(const ms_gated_delta_desc* d, const void* q, const void
                          const float* rate, const float* s0, const int32_t* lengths, void* y, float* last, float* kept,
                          void* workspace, int64_t workspace_bytes) {
   return guarded([&] {
-    Delta p = check_delta(d, false);
+    Delta p = check_delta(d);
     DeltaArgs& a = p.a;
     if (a.batch == 0) return;
     const size_t es = size_of(d->dtype);
@@ -309,7 +304,7 @@ ms_status ms_gated_delta_grad(const ms_gated_delta_desc* d, const void* q, const
                               const float* dlast, void* dq, void* dk, void* dv, float* ddecay, float* drate, float* ds0,
                               void* workspace, int64_t workspace_bytes) {
   return guarded([&] {
-    Delta p = check_delta(d, true);
+    Delta p = check_delta(d);
     DeltaArgs& a = p.a;
     if (a.batch == 0) return;
     const size_t es = size_of(d->dtype);
