@@ -353,6 +353,8 @@ def gated_delta_step(q, k, v, decay, rate, state, slots=None, scale=1.0, out=Non
     if not state.is_contiguous():
         if not state[:1].is_contiguous():
             raise ValueError("state's matrices must be contiguous")
+        if state.stride(0) < state[0].numel():   # an expanded array's 0 would stand for a packed one
+            raise ValueError("state's slots overlap")
         d.state_stride = state.stride(0)
     written = (state,) if out is None else (state, out)
     if out is None:
