@@ -713,7 +713,8 @@ ms_status ms_gated_delta_grad(const ms_gated_delta_desc* desc, const void* q, co
 /* One step of the gated delta rule for sequences that are being served: row i
  * advances the matrices in slot slots[i] of state [slots][heads][keys][values]
  * (float32, updated in place; state_stride between slots).  Slots as in
- * ms_gated_lowpass_step.  Strides: between rows, heads; 0, 0 = packed. */
+ * ms_gated_lowpass_step.  Strides: between rows, heads; 0, 0 = packed.  y may be v
+ * itself, at v's strides, and must not share memory with any other array. */
 typedef struct {
   int64_t rows, n_slots, heads, key_heads, keys, values;
   int64_t q_stride[2], k_stride[2], v_stride[2], y_stride[2], decay_stride[2], rate_stride[2];

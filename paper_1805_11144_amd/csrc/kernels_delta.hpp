@@ -921,6 +921,9 @@ __global__ void __launch_bounds__(256) k_delta_step(DeltaStepArgs p, int32_t nl,
       qd = as_f32(q[i * p.q[0] + kh * p.q[1] + tid]);
     }
     if (tid < 128) kq[0][tid] = kd, kq[1][tid] = qd;
+    float vc[V];   // before the barriers: y, written behind them, may lie in the place of v
+#pragma unroll
+    for (int e = 0; e < V; ++e) vc[e] = mine ? as_f32(v[i * p.v[0] + head * p.v[1] + c + e]) : 0.0f;
     float dot = kd * qd;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o, 64);
@@ -960,7 +963,7 @@ __global__ void __launch_bounds__(256) k_delta_step(DeltaStepArgs p, int32_t nl,
       float z[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        z[e] = b * (as_f32(v[i * p.v[0] + head * p.v[1] + c + e]) - w[e]);
+        z[e] = b * (vc[e] - w[e]);
         if (rg == 0) y[i * p.y[0] + head * p.y[1] + c + e] = (T)(p.scale * fmaf(z[e], dot, o[e]));
       }
 #pragma unroll

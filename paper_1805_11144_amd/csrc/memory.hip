@@ -67,6 +67,39 @@ bool walk_apart(Walk w, int64_t batch, int64_t steps, int64_t heads, int64_t dim
   return true;
 }
 
+// Runs of `run` bytes, n of them `stride` bytes apart, and so on outwards.
+struct Runs {
+  const void* at;
+  int64_t run;
+  std::pair<int64_t, int64_t> level[2];   // stride, n: outer, inner
+};
+
+// Whether two arrays may share a byte, the second one's begin `apart` bytes behind the
+// first one's.  Exact where their levels have equal strides, and inner ones lie within
+// a step of the outer (columns of one buffer); else as their whole ranges do.
+bool may_share(const Runs& x, const Runs& y, int level, __int128 apart) {
+  while (level < 2 && x.level[level].second == 1 && y.level[level].second == 1) ++level;
+  const auto reach = [](const Runs& r, int from) {
+    __int128 n = r.run;
+    for (int i = from; i < 2; ++i) n += (__int128)r.level[i].first * (r.level[i].second - 1);
+    return n;
+  };
+  if (apart >= reach(x, level) || -apart >= reach(y, level)) return false;
+  if (level == 2) return true;
+  const auto [sx, nx] = x.level[level];
+  const auto [sy, ny] = y.level[level];
+  const int64_t step = nx == 1 ? sy : sx;
+  if ((ny > 1 && sy != step) || step <= 0 || reach(x, level + 1) > step || reach(y, level + 1) > step) return true;
+  // y's run of the level j lies apart + (j - i) step behind x's i: only two differences can bring them together
+  for (__int128 m = apart / step - 1; m <= apart / step + 1; ++m)
+    if (-m < ny && m < nx && may_share(x, y, level + 1, apart - m * step)) return true;
+  return false;
+}
+
+bool may_share(const Runs& x, const Runs& y) {
+  return may_share(x, y, 0, (__int128)(uintptr_t)y.at - (__int128)(uintptr_t)x.at);
+}
+
 struct Delta {
   DeltaArgs a;
   int64_t chunks;            // of all heads and rows
@@ -389,6 +422,20 @@ ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* d, const void* q, 
     for (const void* x : {q, k, v, (const void*)y}) need_aligned(x, size_of(d->dtype), "q, k, v or y");
     for (const void* x : {(const void*)decay, (const void*)rate, (const void*)state, (const void*)slots})
       need_aligned(x, 4, "decay, rate, state or slots");
+    const int64_t es = (int64_t)size_of(d->dtype);
+    const auto runs = [&](const void* x, const int64_t* s, int64_t heads, int64_t dim, int64_t size) {
+      Runs r{x, dim * size, {{s[0] * size, d->rows}, {s[1] * size, heads}}};
+      if (d->rows > 1 && heads > 1 && s[0] < s[1]) std::swap(r.level[0], r.level[1]);
+      return r;
+    };
+    const Runs to = runs(y, a.y, d->heads, d->values, es);
+    const bool same = y == v && (d->rows == 1 || a.y[0] == a.v[0]) && (d->heads == 1 || a.y[1] == a.v[1]);
+    need((same || !may_share(to, runs(v, a.v, d->heads, d->values, es))) &&
+             !may_share(to, runs(q, a.q, d->key_heads, d->keys, es)) && !may_share(to, runs(k, a.k, d->key_heads, d->keys, es)) &&
+             !may_share(to, runs(decay, a.decay, d->heads, 1, 4)) && !may_share(to, runs(rate, a.rate, d->heads, 1, 4)) &&
+             (d->n_slots == 0 || !may_share(to, Runs{state, matrices * 4, {{a.state * 4, d->n_slots}, {0, 1}}})) &&
+             (!slots || !may_share(to, Runs{slots, d->rows * 4, {{0, 1}, {0, 1}}})),
+         "y overlaps another array (it may be v itself)");
     a.rows = d->rows, a.slots = d->n_slots, a.heads = (int32_t)d->heads, a.group = (int32_t)(d->heads / d->key_heads);
     a.dk = (int32_t)d->keys, a.dv = (int32_t)d->values, a.scale = (float)d->scale;
     DeviceGuard dg(d->device);

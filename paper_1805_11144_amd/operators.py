@@ -345,7 +345,7 @@ def gated_delta_step(q, k, v, decay, rate, state, slots=None, scale=1.0, out=Non
     """One step for the sequences being served (ms_gated_delta_step): row i of q, k [rows, key_heads, keys], v
     [rows, heads, values], decay and rate [rows, heads] advances state[slots[i]] (float32 [slots, heads, keys, values],
     in place; row i's own slot without `slots`, int32) and returns what is read there, [rows, heads, values] in v's
-    type; a slot outside the cache marks an idle row, whose result is zeros."""
+    type; a slot outside the cache marks an idle row, whose result is zeros.  out may be v, and no other argument."""
     d = GatedDeltaStepDesc(scale=scale)
     q, k, v, decay, rate, matrix = _delta_inputs(d, 3, q, k, v, decay, rate)
     _like(state, v, "state", (state.shape[0], *matrix), _torch.float32)
