@@ -17,7 +17,9 @@
 //     dK = b W - R,   drate = k W
 // The decays: G[t] scales what t reads and undoes what it writes, so that
 //     dG[t] = q dQ - k R - b (k W),  and behind the last step <dS, S behind the chunk>,
-// and decay[t] is in all G from t on: a sum from the chunk's end.
+// and decay[t] is in all G from t on: a sum from the chunk's end, or from the next step
+// whose a is 0 in 32 bits.  What lies from there on cancels in it, but only to the
+// rounding of its own size, which may be any number of times what is before.
 //
 // Everything here takes three parts, also for bf16 results: the gates' gradients are 32
 // bits and differences of the same products.
@@ -343,7 +345,8 @@ __global__ void __launch_bounds__(512, 1)
     while (u < all) {
       const GradPlace w(p, key_heads, u, C);
       const int64_t gate = w.step * p.heads + w.kh * p.group + h;
-      const bool counts = tid < C && tid < w.n, forgets = counts && dx < -200.0f;
+      const bool counts = tid < C && tid < w.n,
+                 forgets = counts && __builtin_amdgcn_exp2f((float)((double)dx * 1.4426950408889634)) == 0.0f;
       float inner = 0.0f, all_kept = 0.0f;   // <dS, S>, this thread's part
       const auto store = [&](char* half) {
         sr.store(half + Lds::s, tid);
@@ -357,7 +360,7 @@ __global__ void __launch_bounds__(512, 1)
           for (int j = 0; j < 8; ++j) inner = fmaf(sr.v[i][j / 4][j % 4], dsr.v[i][j / 4][j % 4], inner);
       };
       if (tid < C) {
-        double d = counts ? forgets ? -200.0 : (double)dx : 0.0;
+        double d = counts ? dx < -200.0f ? -200.0 : (double)dx : 0.0;
 #pragma unroll
         for (int o = 1; o < C; o *= 2) {
           const double x = __shfl_up(d, o, 64);
@@ -427,10 +430,13 @@ __global__ void __launch_bounds__(512, 1)
 #pragma unroll
         for (int i = 0; i < NP; ++i) s += dg[i * C + tid], v += kw[i * C + tid];
         if (tid == C - 1) s += all_kept * ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
+        int ends = __shfl_down((int)forgets, 1, 64);   // the sum of this step and those behind it stops within
+        if (tid == C - 1) ends = 1;
 #pragma unroll
         for (int o = 1; o < C; o *= 2) {
           const float x = __shfl_down(s, o, 64);
-          if (tid + o < C) s += x;
+          const int there = __shfl_down(ends, o, 64);
+          if (!ends) s += x, ends = there;
         }
         if (tid < w.in) {
           out.ddecay[gate + (int64_t)tid * p.heads] = counts && !forgets ? s : 0.0f;
