@@ -661,8 +661,8 @@ ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rul
  * [values]; at every step it forgets by a = exp(decay), reads at the key, learns
  * the error with the step's rate, and is read at the query:
  *     P = a S;   z = v - P'k;   S <- P + rate k z';   y = scale S'q
- * from s0 (zeros).  decay <= 0 is the logarithm of what is kept; -inf (any below
- * -200) forgets everything: a sequence starts.  Where a row's first step forgets, s0
+ * from s0 (zeros).  decay is the logarithm of what is kept, <= 0 in a memory (above 0 a
+ * matrix grows); -inf (any below -200) forgets everything: a sequence starts.  Where a row's first step forgets, s0
  * may hold anything.  Else an infinity or NaN may reach every result of its row and
  * head.  Heads share key heads: head h reads q and k of key head h * key_heads /
  * heads.  lengths: as for the gated lowpass; y is 0 past a row's length and what lies

@@ -526,8 +526,8 @@ __global__ void __launch_bounds__(512, 1)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float apart = (float)(first ? mine - sum[t0 + r] : sum[t0 + r] - mine);
-          const float d = __builtin_amdgcn_exp2f(fminf(apart, 0.0f)) * bt[r];
-          const int before = first ? step - (t0 + r) : t0 + r - step;   // below 0: on the wrong side
+          const float d = __builtin_amdgcn_exp2f(apart) * bt[r];
+          const int before = first ? step - (t0 + r) : t0 + r - step;   // below 0: on the wrong side, where d may be infinite
           y[r] = before >= 0 ? y[r] * d * p.scale : 0.0f;
           x[r] = before > 0 ? x[r] * (first ? d : -d) : 0.0f;
         }
