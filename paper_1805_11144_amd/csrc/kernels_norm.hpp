@@ -424,7 +424,9 @@ __global__ void __launch_bounds__(256) k_norm_apply(NormArgs p, const T* x, T* y
   }
 }
 
-// Of every run and channel: sums of d h and of d, parts [batch][runs][2][channels].
+// Of every run and channel: sums of d h and of d, parts [batch][runs][2][channels].  A
+// thread's positions are added up 64 at a time, and those in 64 bits: a sum of thousands
+// one after the other loses as many roundings of its own size.
 template <class T, int V>
 __global__ void __launch_bounds__(256) k_norm_grad_sums(NormArgs p, const T* x, const T* dy, float* parts) {
   __shared__ float red[256][2 * V + 1];
@@ -435,29 +437,36 @@ __global__ void __launch_bounds__(256) k_norm_grad_sums(NormArgs p, const T* x, 
     const int64_t g = q.b * p.groups + (q.live ? q.word : 0) / p.nw;
     const float mean = p.kept[2 * g], rstd = p.kept[2 * g + 1];
     const Words<float, V> w = norm_param<V>(p.weight, c, 1.0f), a = norm_param<V>(p.bias, c, 0.0f);
-    float dw[V], db[V];
+    double dw[V], db[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) dw[e] = db[e] = 0.0f;
-    for (int64_t t = q.t; q.live && t < end; t += 4 * q.step) {
-      Words<T, V> xv[4], dv[4];
+    for (int e = 0; e < V; ++e) dw[e] = db[e] = 0.0;
+    for (int64_t t = q.t; q.live && t < end;) {
+      float sw[V], sb[V];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t at = min(t + r * q.step, end - 1);
-        xv[r] = *(const Words<T, V>*)(x + q.b * p.xb + at * p.xt + c);
-        dv[r] = *(const Words<T, V>*)(dy + q.b * p.yb + at * p.yt + c);
+      for (int e = 0; e < V; ++e) sw[e] = sb[e] = 0.0f;
+      for (int i = 0; i < 16 && t < end; ++i, t += 4 * q.step) {
+        Words<T, V> xv[4], dv[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t at = min(t + r * q.step, end - 1);
+          xv[r] = *(const Words<T, V>*)(x + q.b * p.xb + at * p.xt + c);
+          dv[r] = *(const Words<T, V>*)(dy + q.b * p.yb + at * p.yt + c);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (t + r * q.step < end)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              const float h = (as_f32(xv[r].v[e]) - mean) * rstd;
+              const float d = through_act(as_f32(dv[r].v[e]), fmaf(h, w.v[e], a.v[e]), p.act);
+              sw[e] = fmaf(d, h, sw[e]), sb[e] += d;
+            }
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (t + r * q.step < end)
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float h = (as_f32(xv[r].v[e]) - mean) * rstd;
-            const float d = through_act(as_f32(dv[r].v[e]), fmaf(h, w.v[e], a.v[e]), p.act);
-            dw[e] = fmaf(d, h, dw[e]), db[e] += d;
-          }
+      for (int e = 0; e < V; ++e) dw[e] += sw[e], db[e] += sb[e];
     }
 #pragma unroll
-    for (int e = 0; e < V; ++e) red[threadIdx.x][e] = dw[e], red[threadIdx.x][V + e] = db[e];
+    for (int e = 0; e < V; ++e) red[threadIdx.x][e] = (float)dw[e], red[threadIdx.x][V + e] = (float)db[e];
     __syncthreads();
     if (threadIdx.x < p.wide && q.live) {
       for (int r = 1; r < q.step; ++r)
@@ -468,7 +477,7 @@ __global__ void __launch_bounds__(256) k_norm_grad_sums(NormArgs p, const T* x, 
         }
       float* o = parts + (q.b * p.runs + u / ((words + p.wide - 1) / p.wide) % p.runs) * 2 * channels + c;
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[e] = dw[e], o[channels + e] = db[e];
+      for (int e = 0; e < V; ++e) o[e] = (float)dw[e], o[channels + e] = (float)db[e];
     }
     __syncthreads();
   }
