@@ -178,6 +178,7 @@ struct Norm {
   int64_t channels, v;
 };
 
+static_assert(kNormRows % 4 == 0, "k_norm_team_grad has up to 4 rows on their way");
 static_assert(MS_ACT_NONE == kActNone && MS_ACT_RELU == kActRelu && MS_ACT_SILU == kActSilu, "activations");
 
 // v: values of a word, as sizes, strides and pointers allow (1 for workspaces, which hold for any).
@@ -212,7 +213,7 @@ void norm_choose(Norm& p, int64_t v, bool grad) {
   p.v = v;
   a.nw = (int32_t)(a.width / v);
   p.shape = norm_shape(a.batch, a.positions, a.groups, a.nw, grad);
-  a.team = p.shape.team, a.lanes = p.shape.lanes;
+  a.team = p.shape.team, a.lanes = p.shape.lanes, a.pieces = p.shape.pieces;
   a.runs = p.shape.runs, a.run = p.shape.run, a.wide = p.shape.wide;
 }
 
@@ -231,7 +232,7 @@ NormWork norm_work(const Norm& p, bool grad, void* ws) {
     w.parts = c.take<float>(a.batch * a.runs * a.groups * a.nw * 2);
     w.sums = c.take<float>(a.batch * a.groups * 2);
   } else if (grad) {
-    const int64_t rows = a.team ? (int64_t)a.lanes : a.batch * a.runs;
+    const int64_t rows = a.team ? (int64_t)a.lanes * a.pieces : a.batch * a.runs;
     w.parts = c.take<float>(rows * 2 * p.channels);
     int64_t joined = 0;   // rows of all later levels
     for (int64_t r = rows; r > kColumnRows;) joined += r = (r + kColumnRows - 1) / kColumnRows;
@@ -573,7 +574,7 @@ ms_status ms_group_norm_grad(const ms_group_norm_desc* d, const void* x, const f
       hipLaunchKernelGGL(HIP_KERNEL_NAME(k_norm_grad_apply<T, V>), dim3(norm_grid(p)), dim3(256), 0, st, a, (const T*)x,
                          (const T*)dy, (const float*)w.sums, (T*)dx);
     });
-    columns(w.parts, a.team ? (int64_t)a.lanes : a.batch * a.runs, w.next);
+    columns(w.parts, a.team ? (int64_t)a.lanes * a.pieces : a.batch * a.runs, w.next);
   });
 }
 

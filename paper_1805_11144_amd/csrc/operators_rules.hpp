@@ -148,14 +148,14 @@ inline OrthShape orth_shape(int64_t batch, int64_t n, int64_t m) {
 
 // ------------------------------------------------------------------- norm
 constexpr int kNormWords = 4;   // of a thread that keeps its values, at most
-constexpr int kNormRows = 64;   // that a thread adds up one after the other, at most
+constexpr int kNormRows = 64;   // that a team adds up one after the other, at most
 
 // How groups of `words` words (positions x words of a group's channels) are taken:
 // kept by a team of threads, or read twice in runs of positions.
 struct NormShape {
   int32_t team;               // threads of a team: a power of two up to 64, or 256; 0: runs
   int32_t words;              // of a thread of it: 1, 2 or 4
-  int32_t lanes;              // of the gradient: batch rows side by side
+  int32_t lanes, pieces;      // of the gradient: batch rows side by side, and times kNormRows one after the other
   int32_t runs, run, wide;    // runs of positions, positions of one, channel words to a row of threads
 };
 
@@ -175,11 +175,9 @@ inline NormShape norm_shape(int64_t batch, int64_t positions, int64_t groups, in
     if (words > 64 * kNormWords) s.team = 256;
     const int64_t each = (words + s.team - 1) / s.team;
     s.words = each == 1 ? 1 : each == 2 ? 2 : 4;
-    // rows of groups for 512 workgroups: what dweight and dbias are joined from; more where each would add up over 64
-    // rows one after the other, as far as the grid goes
-    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / s.team / groups);
-    s.lanes = (int32_t)std::max<int64_t>(
-        1, std::min(batch, std::max(512 * 256 / s.team / groups, std::min((batch + kNormRows - 1) / kNormRows, most))));
+    // rows of groups for 512 workgroups: what dweight and dbias are joined from, one sum of theirs for every 64 rows
+    s.lanes = (int32_t)std::max<int64_t>(1, std::min(batch, 512 * 256 / s.team / groups));
+    s.pieces = (int32_t)std::max<int64_t>(1, (batch + kNormRows * (int64_t)s.lanes - 1) / (kNormRows * (int64_t)s.lanes));
     return s;
   }
   const int64_t row = groups * nw;
