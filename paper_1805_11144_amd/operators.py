@@ -21,13 +21,13 @@ from .mergesim import (DTYPE_BF16, DTYPE_F32, IDS_I32, IDS_I64, EmbedDesc, Gated
 # "Muon: An optimizer for hidden layers in neural networks" (2024).
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
 
-_torch = _lib = _stream = None
+_torch = _lib = _stream = _forward = None
 _DTYPES, _IDS = {}, {}
 
 
 def _setup():
     """Loads torch and the library, once, and checks that they share one HIP runtime."""
-    global _torch, _lib, _stream
+    global _torch, _lib, _stream, _forward
     import torch
     lib = _ms.load_library()
     with open("/proc/self/maps") as f:
@@ -39,7 +39,7 @@ def _setup():
     _IDS.update({torch.int32: IDS_I32, torch.int64: IDS_I64})
     # the current stream's handle without a Stream object around it: 2 of the 11 us of a small call
     _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-    _torch, _lib = torch, lib
+    _torch, _lib, _forward = torch, lib, torch.autograd.forward_ad
 
 
 def _gpu(t, dims, what):
@@ -58,8 +58,8 @@ def _undifferentiated(t, what):
     if t.requires_grad and _torch.is_grad_enabled():
         raise ValueError(f"{what} requires a gradient, which torch cannot take through this call: detach it, or call "
                          "under torch.no_grad() and use the operator's own gradient")
-    forward = _torch.autograd.forward_ad   # a level of its own is open in forward mode only: 0.1 us of a call else
-    if forward._current_level >= 0 and forward.unpack_dual(t).tangent is not None:
+    # a level is open in forward mode only, and unpacking costs a microsecond
+    if _forward._current_level >= 0 and _forward.unpack_dual(t).tangent is not None:
         raise ValueError(f"{what} carries a tangent, which torch's forward mode cannot take through this call: give its "
                          "primal (torch.autograd.forward_ad.unpack_dual)")
 

@@ -20,6 +20,7 @@ def calls(monkeypatch):
             seen.append((d, state))
             return 0
     monkeypatch.setattr(O, "_torch", torch)
+    monkeypatch.setattr(O, "_forward", torch.autograd.forward_ad)
     monkeypatch.setattr(O, "_lib", Library)
     monkeypatch.setattr(O, "_gpu", lambda t, dims, what: MS.DTYPE_F32)
     monkeypatch.setattr(O, "_on", lambda d, t: d)
