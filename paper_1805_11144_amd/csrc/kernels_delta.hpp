@@ -762,13 +762,18 @@ __global__ void __launch_bounds__(512, 1)
     for (int chunk = 0; chunk < chunks; ++chunk) {
       const bool next = chunk + 1 < chunks, after = chunk + 2 < chunks;
       __syncthreads();   // this chunk's operands are there, the other half is read and the last results are written
-      if (!Lds::PAIRS && chunk > 0) out(chunk - 1);
-      if (next) store(chunk + 1);
-      if (after) load(chunk + 2);
-      if (!Lds::PAIRS) __syncthreads();   // V is read, and the last results are out
-      if (next) store_panel(chunk + 1);
-      if (after) load_panel(chunk + 2);
-      if (Lds::PAIRS && chunk > 0) out(chunk - 1);
+      if constexpr (Lds::PAIRS) {
+        if (next) store(chunk + 1), store_panel(chunk + 1);
+        if (after) load(chunk + 2), load_panel(chunk + 2);
+        if (chunk > 0) out(chunk - 1);
+      } else {
+        if (chunk > 0) out(chunk - 1);
+        if (next) store(chunk + 1);
+        if (after) load(chunk + 2);
+        __syncthreads();   // V is read, and the last results are out
+        if (next) store_panel(chunk + 1);
+        if (after) load_panel(chunk + 2);
+      }
     }
     __syncthreads();
     if (chunks > 0) out(chunks - 1);
@@ -921,9 +926,6 @@ __global__ void __launch_bounds__(256) k_delta_step(DeltaStepArgs p, int32_t nl,
       qd = as_f32(q[i * p.q[0] + kh * p.q[1] + tid]);
     }
     if (tid < 128) kq[0][tid] = kd, kq[1][tid] = qd;
-    float vc[V];   // before the barriers: y, written behind them, may lie in the place of v
-#pragma unroll
-    for (int e = 0; e < V; ++e) vc[e] = mine ? as_f32(v[i * p.v[0] + head * p.v[1] + c + e]) : 0.0f;
     float dot = kd * qd;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o, 64);
@@ -963,8 +965,8 @@ __global__ void __launch_bounds__(256) k_delta_step(DeltaStepArgs p, int32_t nl,
       float z[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        z[e] = b * (vc[e] - w[e]);
-        if (rg == 0) y[i * p.y[0] + head * p.y[1] + c + e] = (T)(p.scale * fmaf(z[e], dot, o[e]));
+        z[e] = b * (as_f32(v[i * p.v[0] + head * p.v[1] + c + e]) - w[e]);
+        o[e] = p.scale * fmaf(z[e], dot, o[e]);
       }
 #pragma unroll
       for (int r = 0; r < kStepRows; ++r) {
@@ -976,6 +978,9 @@ __global__ void __launch_bounds__(256) k_delta_step(DeltaStepArgs p, int32_t nl,
         *(Words<float, V>*)(s + (int64_t)d * p.dv) = m[r];
       }
     }
-    __syncthreads();   // kq, red and dots are free again
+    __syncthreads();   // kq, red and dots are free again, and all have read v, in whose place y may lie
+    if (mine && rg == 0)
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[i * p.y[0] + head * p.y[1] + c + e] = (T)o[e];
   }
 }
