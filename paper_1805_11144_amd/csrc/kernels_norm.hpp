@@ -54,9 +54,13 @@ __device__ __forceinline__ float gate_of_silu(float z) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(rest, ln2, 1.0f));
 }
 
+// act(z), a result in T.  For one of 16 bits the product alone is enough: 5e-6 of silu at
+// z = -88, a thousandth of the rounding to come, and 16384 x 16 heads of 128 bf16 take
+// 29 us in place of 31.
+template <class T>
 __device__ __forceinline__ float activated(float z, int act) {
   if (act == kActRelu) return z > 0.0f ? z : z != z ? z : 0.0f;
-  if (act == kActSilu) return z * gate_of_silu(z);
+  if (act == kActSilu) return z * (sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.0f + __expf(-z)) : gate_of_silu(z));
   return z;
 }
 
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(256) k_norm_team(NormArgs p, const T* x, T* y)
         const Words<float, V> w = norm_param<V>(p.weight, (int64_t)g * p.width + c, 1.0f),
                               a = norm_param<V>(p.bias, (int64_t)g * p.width + c, 0.0f);
 #pragma unroll
-        for (int e = 0; e < V; ++e) o.v[e] = (T)activated(fmaf((as_f32(v[r].v[e]) - mean) * rstd, w.v[e], a.v[e]), p.act);
+        for (int e = 0; e < V; ++e) o.v[e] = (T)activated<T>(fmaf((as_f32(v[r].v[e]) - mean) * rstd, w.v[e], a.v[e]), p.act);
       } else {
 #pragma unroll
         for (int e = 0; e < V; ++e) o.v[e] = (T)0.0f;
@@ -423,7 +427,7 @@ __global__ void __launch_bounds__(256) k_norm_apply(NormArgs p, const T* x, T* y
         Words<T, V> o;
 #pragma unroll
         for (int e = 0; e < V; ++e)
-          o.v[e] = t + r * q.step < q.len ? (T)activated(fmaf((as_f32(v[r].v[e]) - mean) * rstd, w.v[e], a.v[e]), p.act)
+          o.v[e] = t + r * q.step < q.len ? (T)activated<T>(fmaf((as_f32(v[r].v[e]) - mean) * rstd, w.v[e], a.v[e]), p.act)
                                           : (T)0.0f;
         put_once(y + q.b * p.yb + (t + r * q.step) * p.yt + c, o);
       }
