@@ -662,9 +662,9 @@ ms_status ms_orthogonal_update(const ms_orth_desc* desc, const ms_orth_rule* rul
  * the error with the step's rate, and is read at the query:
  *     P = a S;   z = v - P'k;   S <- P + rate k z';   y = scale S'q
  * from s0 (zeros).  decay is the logarithm of what is kept, <= 0 in a memory (above 0 a
- * matrix grows); -inf (any below -200) forgets everything: a sequence starts.  Where a row's first step forgets, s0
- * may hold anything.  Else an infinity or NaN may reach every result of its row and
- * head.  Heads share key heads: head h reads q and k of key head h * key_heads /
+ * matrix grows); -inf (any below -200) forgets everything: a sequence starts.  Where a
+ * row's first step forgets, s0 may hold anything.  Else an infinity or NaN may reach
+ * every result of its row and head.  Heads share key heads: head h reads q and k of key head h * key_heads /
  * heads.  lengths: as for the gated lowpass; y is 0 past a row's length and what lies
  * there is not read.
  *   q, k        [batch][steps][key_heads][keys], dtype
@@ -732,7 +732,8 @@ ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* desc, const void* 
 /* Group norm with an activation, channels last.  Over the positions of a batch row
  * (its first lengths[row]; NULL = all) and the channels of a group:
  *     h = (x - mean) / sqrt(variance + eps);  y = act(h weight + bias)
- * with the variance of all n values (divided by n).  One position is a norm of every
+ * with the variance of all n values (divided by n), from squares in 32 bits: sums of
+ * squared differences from the mean beyond 3e38 are infinite.  One position is a norm of every
  * row's groups by themselves, as of heads; one group is a norm over all channels.
  *   x, y         [batch][positions][channels], dtype; y is 0 past a row's length
  *   weight, bias [channels] float32, or NULL for ones, zeros
@@ -742,7 +743,7 @@ ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* desc, const void* 
  * The gradient, from dL/dy: dx, packed (0 past a row's length); dweight and dbias
  * float32 [channels], sums over all rows (also where weight or bias is NULL).  x,
  * weight, bias, lengths and kept are those of the forward call.  What lies past a row's
- * length is not read. */
+ * length is not used. */
 #define MS_ACT_NONE 0
 #define MS_ACT_RELU 1
 #define MS_ACT_SILU 2

@@ -29,15 +29,15 @@
 // sums of decays are 64-bit: a difference of two of them is good where each is large.
 //
 // What bounds it.  The scan: a chunk's chain of dependent products.  2 x 16384 steps of
-// 16 heads of 128 x 128 bf16, 32 heads on 64 workgroups: 770 us, 256 chunks of 3.0 us or
-// 7300 cycles, of which matrix instructions take 2900 and the splitting of results
+// 16 heads of 128 x 128 bf16, 32 heads on 64 workgroups: 890 us, 256 chunks of 3.5 us or
+// 8400 cycles, of which matrix instructions take 3450 and the splitting of results
 // into parts, which the wavefront cannot do beside them, most of the rest.  A chunk
 // took 20 us with everything between two barriers, 6.7 with the next one's operands
 // on their way, 5.4 with operands read ahead of their use, 3.0 with wavefronts that
-// only feed.  Sums of two tiles in turn, splitting placed between matrix
-// instructions, and orders of instructions given to the compiler changed nothing.
-// The chunks at once: memory, 8192 of them 159 us for 268 MB read and 254 MB of
-// triangles written (250 us at two workgroups to a CU).
+// only feed and two parts of what only y sees, 3.5 with three.  Sums of two tiles in turn,
+// splitting placed between matrix instructions, and orders of instructions given to the
+// compiler changed nothing.  The chunks at once: memory, 8192 of them 165 us for 268 MB
+// read and 308 MB of triangles written (250 us at two workgroups to a CU, with 254 MB).
 #pragma once
 
 #include <type_traits>
@@ -888,8 +888,8 @@ constexpr int kStepRows = 16;   // of a matrix to a thread, at most
 // matrix, which stays in registers, y = scale (P'q + b z (k'q)).  `nl` threads (a
 // power of two, at most 32) take V columns each, the others of 256 further keys.
 // Memory bounds it: 112 served rows of 32 heads of 128 x 128, 470 MB read and written,
-// 86 us, 5.5 TB/s.  8 rows of 4 heads of 64 x 64: 7 us, of which the call's 13 us are
-// the host's time.
+// 86 us, 5.5 TB/s (v read ahead of the barriers instead of y written behind them: 3 us
+// more).  8 rows of 4 heads of 64 x 64: 7 us; the call's 14 us are the host's time.
 template <class T, int V>
 __global__ void __launch_bounds__(256) k_delta_step(DeltaStepArgs p, int32_t nl, int32_t tiles, const T* q, const T* k,
                                                     const T* v, const float* decay, const float* rate, float* state,

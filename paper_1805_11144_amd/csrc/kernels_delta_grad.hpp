@@ -25,7 +25,7 @@
 // bits and differences of the same products.
 //
 // Measured, 8 x 2048 steps of 16 heads of 128 x 128 bf16, 4096 chunks: k_delta_back 190
-// to 200 us, like the scan; k_delta_grad 430 to 460.  It has to read 980 MB (states and
+// to 206 us (the scan 215 to 230); k_delta_grad 430 to 490.  It has to read 980 MB (states and
 // their gradients, 32 bits each, are most), 210 us at a copy's rate; the matrix
 // instructions take 12900 cycles of a chunk, 90 us.  Of a chunk's 62000 cycles (before
 // the last step) a computing wavefront spent 24000 on sums over the values, 11200 on the

@@ -14,9 +14,10 @@
 // Nothing is added by atomics; every sum has one order.
 //
 // Measured: 16384 rows of 16 heads of 128 bf16 32 us, 4.2 TB/s (69 with words of a thread
-// and positions as run-time values, 34 with a team's sums through LDS), the gradient 63
-// us, 3.2 TB/s (265 one row at a time, 73 with sums through LDS), and 5 for its column
-// sums; 16 x 4096 positions of 512 float32 channels: sums 21
+// and positions as run-time values, 34 with a team's sums through LDS), the gradient 64
+// us, 3.1 TB/s (265 one row at a time, 73 with sums through LDS), and 5 for its column
+// sums.  Of the gradient's wavefronts' time 51% is waiting for memory, two workgroups to a
+// CU that load four rows and then compute them, and 30% vector instructions.  16 x 4096 positions of 512 float32 channels: sums 21
 // us, join 5, results 41, 4.0 TB/s of the 268 MB that have to move (what is read again
 // is in the last cache); 13 x 777 x 333 float32, one channel to a thread: 23 us,
 // gradient 32.
