@@ -733,8 +733,9 @@ ms_status ms_gated_delta_step(const ms_gated_delta_step_desc* desc, const void* 
  * (its first lengths[row]; NULL = all) and the channels of a group:
  *     h = (x - mean) / sqrt(variance + eps);  y = act(h weight + bias)
  * with the variance of all n values (divided by n), from squares in 32 bits: sums of
- * squared differences from the mean beyond 3e38 are infinite.  One position is a norm of every
- * row's groups by themselves, as of heads; one group is a norm over all channels.
+ * squared differences from the mean beyond 3e38 are infinite.  One position is a norm
+ * of every row's groups by themselves, as of heads; one group is a norm over all
+ * channels.
  *   x, y         [batch][positions][channels], dtype; y is 0 past a row's length
  *   weight, bias [channels] float32, or NULL for ones, zeros
  *   lengths      int32 [batch], clamped to [0, positions]

@@ -426,20 +426,21 @@ __global__ void __launch_bounds__(512, 1)
       __syncthreads();   // the products are there
       __syncthreads();   // and read: the sums are there
       if (tid < C) {
-        float s = 0.0f, v = 0.0f;
+        double s = 0.0;   // what lies behind a step cancels in its sum
+        float v = 0.0f;
 #pragma unroll
         for (int i = 0; i < NP; ++i) s += dg[i * C + tid], v += kw[i * C + tid];
-        if (tid == C - 1) s += all_kept * ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
+        if (tid == C - 1) s += (double)all_kept * ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
         int ends = __shfl_down((int)forgets, 1, 64);   // the sum of this step and those behind it stops within
         if (tid == C - 1) ends = 1;
 #pragma unroll
         for (int o = 1; o < C; o *= 2) {
-          const float x = __shfl_down(s, o, 64);
+          const double x = __shfl_down(s, o, 64);
           const int there = __shfl_down(ends, o, 64);
           if (!ends) s += x, ends = there;
         }
         if (tid < w.in) {
-          out.ddecay[gate + (int64_t)tid * p.heads] = counts && !forgets ? s : 0.0f;
+          out.ddecay[gate + (int64_t)tid * p.heads] = counts && !forgets ? (float)s : 0.0f;
           out.drate[gate + (int64_t)tid * p.heads] = counts ? v : 0.0f;
         }
       }
